@@ -578,6 +578,151 @@ typedef struct es_tile_info {
 int es_tile_layout(uint64_t addr, uint64_t numel, uint32_t offset8, es_tile_info_t* out,
                    uint64_t cap, uint64_t* n_tiles);
 
+/* ---------------------------------------------------------------------------
+ * Scoring a member: its attention over a paged cache of keys and values.
+ *
+ * Between two moves of the parameters a member is evaluated: prompts run
+ * through the weights and then tokens are drawn one by one (Section 3: "apply,
+ * evaluate, revert").  These calls are what that evaluation needs besides matrix
+ * products.  They are forward only: evolution strategies take no gradients.
+ *
+ * Layout.  The cache is a pool of pages of `page` tokens each (64, 128, 256,
+ * 512 or 1024).  Keys are stored by token and values by dimension, so that both
+ * products of attention read rows of consecutive elements:
+ *   k_pages[n_pages][kv_heads][page][head_dim]
+ *   v_pages[n_pages][kv_heads][head_dim][page]
+ * A token's slot is its page's index times `page` plus its place in the page.
+ * A sequence is a list of pages: token i lies in its table's entry i / page.
+ *
+ * Formats.  ES_KV_BF16: bf16 values.  ES_KV_INT8, ES_KV_E4M3: codes of the
+ * quantized plans' two formats with one binary32 scale per token and head in
+ *   k_scales[n_pages][kv_heads][page], v_scales[n_pages][kv_heads][page]:
+ * with M the largest |x| of the head's row and Q = 127 or 448, the scale is
+ * M / Q and the code RNE(x (Q / M)), all in binary32.  A row with M < 2^-100 has
+ * scale 0 and codes 0 (it reads back as zeros).
+ * A token whose rotated key or whose value is not finite throughout in some
+ * head is void there: its key reads as NaN, its value is stored as zeros and
+ * reads back as NaN.  A row that sees a void token returns NaN in that head; a
+ * row that does not is not affected.
+ * ------------------------------------------------------------------------- */
+#define ES_KV_INT8 ES_QFORMAT_INT8
+#define ES_KV_E4M3 ES_QFORMAT_E4M3
+#define ES_KV_BF16 2u
+
+/* Bits that a call ORs into its status word (a device uint32 which the caller
+ * clears; NULL: not reported) when values in device memory are out of range.
+ * Nothing is read or written out of bounds in either case. */
+#define ES_KV_BAD_SLOT     1u  /* append, read: slot >= n_pages * page.  Not stored; reads back as NaN */
+#define ES_KV_BAD_POSITION 2u  /* append: position outside the rotation table: the token is void and
+                                  its query NaN */
+#define ES_KV_BAD_PAGE     4u  /* attend: a page that a row sees is not in the pool: the row is NaN */
+#define ES_KV_BAD_LENGTH   8u  /* attend: lengths or starts out of range: clamped into it */
+
+typedef struct es_kv_desc {
+    void*    k_pages;           /* 16-byte aligned */
+    void*    v_pages;           /* 16-byte aligned */
+    float*   k_scales;          /* NULL for ES_KV_BF16; otherwise 16-byte aligned */
+    float*   v_scales;
+    uint32_t n_pages;           /* 1 .. 2^31 / page */
+    uint32_t page;              /* tokens of a page: 64, 128, 256, 512 or 1024 */
+    uint32_t kv_heads;          /* 1 .. 1024 */
+    uint32_t head_dim;          /* 64, 128 or 256 */
+    uint32_t format;            /* ES_KV_BF16, ES_KV_INT8 or ES_KV_E4M3 */
+    uint32_t reserved;          /* 0 */
+} es_kv_desc_t;
+
+/* Opaque handle over a cache: its description, checked once, and the scratch
+ * in which es_kv_attend joins the parts of a long history. */
+typedef struct es_kv es_kv_t;
+
+/* The pages are the caller's; they must stay allocated and unmoved while the
+ * handle exists.  Their contents are not touched.  Errors: INVALID_ARG, ALIGN, and NOMEM / HIP for
+ * the scratch (es_kv_device_bytes reports its size). */
+int es_kv_create(const es_kv_desc_t* desc, es_kv_t** out);
+int es_kv_destroy(es_kv_t* kv);
+uint64_t es_kv_device_bytes(const es_kv_t* kv);
+
+/* One call appends `tokens` new tokens, and normalises and rotates their
+ * queries in the same pass.  A row is one head of one token (head_dim bf16
+ * values); heads of a token are adjacent, tokens are `*_stride` elements apart
+ * (any stride: a packed projection can be passed as it is).
+ *
+ * For queries and keys, in binary32: x <- x rsqrt(mean(x^2) + eps) gain
+ * (where the gain is given), then the rotation of the first `rot` dimensions:
+ * with c = rope[p][i], s = rope[p][rot / 2 + i], p the token's position and
+ * i < rot / 2, the pair (a, b) of dimensions i and i + rot / 2 (with
+ * ES_KV_ADJACENT: 2 i and 2 i + 1) becomes (a c - b s, b c + a s).  Queries
+ * are rounded once, to bf16 (RNE); keys are stored in the cache's format
+ * from binary32, values as they come.
+ * slots[t] is where token t is stored; a negative slot stores nothing (a padding
+ * row).  Two tokens of one call must not share a slot.  Which values a
+ * token's slot holds never depends on the other tokens of the call. */
+#define ES_KV_ADJACENT 1u
+typedef struct es_kv_append {
+    const void*    q;           /* bf16 [tokens][q_heads][head_dim], or NULL with q_heads 0 */
+    const void*    k;           /* bf16 [tokens][kv_heads][head_dim] */
+    const void*    v;
+    void*          q_out;       /* bf16 [tokens][q_heads][head_dim]; may be q itself with its stride */
+    uint64_t       q_stride, k_stride, v_stride, q_out_stride;   /* elements from token to token */
+    const void*    q_gain;      /* bf16 [head_dim], or NULL: queries are not normalised */
+    const void*    k_gain;      /* bf16 [head_dim], or NULL: keys are not normalised */
+    const float*   rope;        /* binary32 [rope_rows][rot], or NULL with rot 0 */
+    const int32_t* positions;   /* [tokens]; NULL with rot 0 */
+    const int64_t* slots;       /* [tokens] */
+    uint32_t*      status;
+    uint32_t       tokens;      /* 0 .. 2^24 */
+    uint32_t       q_heads;     /* 0 .. 1024 */
+    uint32_t       rot;         /* a multiple of 16, at most head_dim */
+    uint32_t       rope_rows;
+    float          eps;         /* > 0 where a gain is given */
+    uint32_t       flags;       /* ES_KV_ADJACENT */
+} es_kv_append_t;
+int es_kv_append(es_kv_t* kv, const es_kv_append_t* args, es_stream_t stream);
+
+/* Read tokens back: row t of k_out and v_out (bf16 [tokens][kv_heads][head_dim],
+ * `*_stride` elements from token to token) is what slots[t] holds, code times
+ * scale rounded once (RNE).  A negative slot gives zeros. */
+int es_kv_read(es_kv_t* kv, const int64_t* slots, uint32_t tokens, void* k_out, uint64_t k_stride,
+               void* v_out, uint64_t v_stride, uint32_t* status, es_stream_t stream);
+
+/* Attention of `rows` query rows (tokens of all sequences, packed) over the
+ * cache.  Sequence s has the rows starts[s] .. starts[s + 1] and lengths[s]
+ * tokens in the cache, its rows' own tokens among them: row i of its n
+ * stands at position p = lengths[s] - n + i.  It sees the keys first <= j < limit,
+ * by default 0 <= j <= p; first[row] and limit[row] set other intervals (packed
+ * documents, a prefix that all rows see, a window), clipped to 0 .. lengths[s].
+ * For query head h, over key head h / (q_heads / kv_heads):
+ *   t_j = scale q . k_j;  t_j <- cap tanh(t_j / cap) where cap > 0;
+ *   t_j <- t_j - slopes[h] |p - j| where slopes are given;
+ *   out = sum_j softmax(t)_j v_j, rounded once to bf16 (RNE).
+ * A row that sees nothing returns zeros.  Rows that no sequence has are not
+ * written.  Sums, maxima and products are held in binary32; the softmax's
+ * weights (times the values' scales) are rounded to bf16 for the matrix unit.
+ * max_rows and max_length are the largest rows and lengths[s] that the caller
+ * expects: they choose how the work is cut, and nothing is lost where a
+ * sequence exceeds them.  Calls on one handle must be ordered (one stream, or
+ * externally synchronised): they share its scratch. */
+typedef struct es_kv_attend {
+    const void*    q;           /* bf16 [rows][q_heads][head_dim] */
+    void*          out;         /* bf16 [rows][q_heads][head_dim]; not q */
+    uint64_t       q_stride, out_stride;       /* elements from row to row */
+    const int32_t* tables;      /* [n_seqs][table_stride] pages of each sequence */
+    const int32_t* lengths;     /* [n_seqs] */
+    const int32_t* starts;      /* [n_seqs + 1] */
+    const int32_t* first;       /* [rows], or NULL: 0 */
+    const int32_t* limit;       /* [rows], or NULL: the row's position + 1 */
+    const float*   slopes;      /* [q_heads], or NULL */
+    uint32_t*      status;
+    uint32_t       rows;        /* 0 .. 2^24 */
+    uint32_t       n_seqs;      /* 1 .. 65536 */
+    uint32_t       table_stride;
+    uint32_t       q_heads;     /* a multiple of kv_heads, at most 64 times as many */
+    uint32_t       max_rows, max_length;
+    float          scale;
+    float          cap;         /* 0: scores are not capped */
+} es_kv_attend_t;
+int es_kv_attend(es_kv_t* kv, const es_kv_attend_t* args, es_stream_t stream);
+
 /* Static name of an error code; detail of the calling thread's last error. */
 const char* es_strerror(int code);
 const char* es_last_error(void);

@@ -34,6 +34,9 @@ fp8 path (fp8.py) does the same on the grid of the E4M3 format, rounding the
 scaled value stochastically onto it; the paper lists quantized ES as future
 work (Appendix A.2).
 
+attention.py holds the rows of the paged cache (norm, rotation, quantisation)
+and the attention over it, with which a member is scored.
+
 Pin status of every function is listed in the module docstrings; all functions
 are pinned (none is "parity unpinned").
 """
@@ -51,8 +54,10 @@ from .checksum import mix64, checksum, qchecksum, plan_checksum
 from . import fp8
 from .fp8 import (E4M3_MAX, e4m3_decode, e4m3_encode, grid_floor, round_onto_grid, f8perturb,
                   f8restore, f8update_values, f8update)
+from . import attention
 
 __all__ = [
+    "attention",
     "philox4x32_10", "philox4x32_10_bigint", "MASK32",
     "key_words", "counter_words", "uniform_from_word", "angle_from_word", "box_muller",
     "noise_words", "normals", "rounding_draws", "spare_draws",

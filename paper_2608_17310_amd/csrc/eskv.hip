@@ -1,0 +1,407 @@
+// Scoring a member: the paged cache of keys and values and the attention over
+// it (include/esopt.h, es_kv_*).  Host side: checks of arguments, the choice of
+// kernels and launches; the kernels are in kv_place.hpp and kv_attend.hpp.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+#include <new>
+
+#include "../../include/esopt.h"
+#include "es_host.hpp"
+#include "kv_attend.hpp"
+#include "kv_place.hpp"
+
+using namespace es_host;
+using namespace eskv;
+
+// Parts that a split launch aims at, and the rows of a tile at most: they bound the scratch.
+static constexpr uint32_t kTargetParts = 1024;
+static constexpr uint32_t kMinBlocks = 4;          // blocks of a part at least: one a wave
+
+struct es_kv {
+    int device = -1;
+    es_kv_desc_t d{};
+    Cache c{};
+    float* scratch = nullptr;                      // partial results of es_kv_attend
+    uint64_t scratch_bytes = 0;
+    float* part_ml = nullptr;                      // behind them, maxima and sums
+};
+
+namespace {
+
+// Tiles of 16 rows that a wave of the split kernel holds at most: one of wide heads, whose
+// keys, values and accumulators fill the registers.
+constexpr uint32_t split_tiles_max(uint32_t dim) { return dim == 256 ? 1 : 2; }
+
+int check_kv_device(const es_kv_t* kv, const char* name) {
+    int dev = -1;
+    const hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return hip_fail(e, "hipGetDevice");
+    if (dev != kv->device)
+        return fail_in(ES_ERR_DEVICE, name, "current device differs from the cache's");
+    return ES_OK;
+}
+
+bool odd(const void* p, uintptr_t align) { return reinterpret_cast<uintptr_t>(p) % align != 0; }
+
+// `rows` rows of `width` bf16, `stride` elements apart.
+int check_rows(const void* p, uint64_t rows, uint64_t width, uint64_t stride, int device,
+               const char* name, const char* part) {
+    if (stride > (uint64_t(1) << 40))
+        return fail(ES_ERR_INVALID_ARG, std::string(name) + part + ": stride above 2^40");
+    return check_access(p, 2 * ((rows - 1) * stride + width), device, name, part);
+}
+
+int launch_error(const char* what) {
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? ES_OK : hip_fail(e, what);
+}
+
+using AppendKernel = void (*)(AppendArgs);
+using ReadKernel = void (*)(ReadArgs);
+using AttendKernel = void (*)(AttendArgs);
+using JoinKernel = void (*)(AttendArgs, int);
+
+template <class K, template <int, int> class Make>
+K by_dim_format(uint32_t dim, uint32_t format) {
+    switch (dim) {
+        case 64: return format == kInt8   ? Make<64, kInt8>::get()
+                        : format == kE4M3 ? Make<64, kE4M3>::get()
+                                          : Make<64, kBf16>::get();
+        case 128: return format == kInt8   ? Make<128, kInt8>::get()
+                         : format == kE4M3 ? Make<128, kE4M3>::get()
+                                           : Make<128, kBf16>::get();
+        default: return format == kInt8   ? Make<256, kInt8>::get()
+                        : format == kE4M3 ? Make<256, kE4M3>::get()
+                                          : Make<256, kBf16>::get();
+    }
+}
+template <int D, int F>
+struct MakeAppend {
+    static AppendKernel get() { return es_kv_append_kernel<D, F>; }
+};
+template <int D, int F>
+struct MakeRead {
+    static ReadKernel get() { return es_kv_read_kernel<D, F>; }
+};
+template <int T>
+struct MakeSplit {
+    template <int D, int F>
+    struct Of {
+        static AttendKernel get() {
+            return es_kv_split_kernel<D, (D == 256 ? 1 : T), F>;
+        }
+    };
+};
+template <bool kPlain>
+struct MakeTile {
+    template <int D, int F>
+    struct Of {
+        static AttendKernel get() { return es_kv_tile_kernel<D, F, kPlain>; }
+    };
+};
+
+}  // namespace
+
+extern "C" {
+
+int es_kv_create(const es_kv_desc_t* desc, es_kv_t** out) try {
+    const char* const name = "es_kv_create";
+    if (desc == nullptr || out == nullptr) return fail_in(ES_ERR_INVALID_ARG, name, "null pointer");
+    *out = nullptr;
+    const es_kv_desc_t& d = *desc;
+    if (d.format != ES_KV_BF16 && d.format != ES_KV_INT8 && d.format != ES_KV_E4M3)
+        return fail_in(ES_ERR_INVALID_ARG, name, "unknown format");
+    if (d.reserved != 0) return fail_in(ES_ERR_INVALID_ARG, name, "reserved is not 0");
+    if (d.page < 64 || d.page > 1024 || (d.page & (d.page - 1)) != 0)
+        return fail_in(ES_ERR_INVALID_ARG, name, "page is not 64, 128, 256, 512 or 1024");
+    if (d.n_pages == 0 || uint64_t(d.n_pages) * d.page > (uint64_t(1) << 31))
+        return fail_in(ES_ERR_INVALID_ARG, name, "n_pages out of range (1 .. 2^31 / page)");
+    if (d.kv_heads == 0 || d.kv_heads > 1024)
+        return fail_in(ES_ERR_INVALID_ARG, name, "kv_heads out of range (1 .. 1024)");
+    if (d.head_dim != 64 && d.head_dim != 128 && d.head_dim != 256)
+        return fail_in(ES_ERR_INVALID_ARG, name, "head_dim is not 64, 128 or 256");
+    const bool scaled = d.format != ES_KV_BF16;
+    if (d.k_pages == nullptr || d.v_pages == nullptr ||
+        (scaled && (d.k_scales == nullptr || d.v_scales == nullptr)))
+        return fail_in(ES_ERR_INVALID_ARG, name, "null pages or scales");
+    if (!scaled && (d.k_scales != nullptr || d.v_scales != nullptr))
+        return fail_in(ES_ERR_INVALID_ARG, name, "bf16 pages have no scales");
+    if (odd(d.k_pages, 16) || odd(d.v_pages, 16) || odd(d.k_scales, 16) || odd(d.v_scales, 16))
+        return fail_in(ES_ERR_ALIGN, name, "pages or scales not 16-byte aligned");
+    int device = -1;
+    int rc = current_device(&device);
+    if (rc != ES_OK) return rc;
+    const uint64_t rows = uint64_t(d.n_pages) * d.page * d.kv_heads;
+    const uint64_t bytes = rows * d.head_dim * (scaled ? 1 : 2);
+    const struct { const void* p; uint64_t bytes; const char* what; } parts[] = {
+        {d.k_pages, bytes, ": keys"}, {d.v_pages, bytes, ": values"},
+        {d.k_scales, scaled ? 4 * rows : 0, ": key scales"},
+        {d.v_scales, scaled ? 4 * rows : 0, ": value scales"}};
+    for (const auto& p : parts) {
+        rc = check_access(p.p, p.bytes, device, name, p.what);
+        if (rc != ES_OK) return rc;
+    }
+    for (const auto& p : parts)
+        for (const auto& q : parts) {
+            const uintptr_t x = reinterpret_cast<uintptr_t>(p.p), y = reinterpret_cast<uintptr_t>(q.p);
+            if (&p != &q && p.bytes != 0 && q.bytes != 0 && x < y + q.bytes && y < x + p.bytes)
+                return fail_in(ES_ERR_INVALID_ARG, name, "pages and scales overlap");
+        }
+    es_kv* kv = new es_kv;
+    kv->device = device;
+    kv->d = d;
+    kv->c = Cache{static_cast<uint8_t*>(d.k_pages), static_cast<uint8_t*>(d.v_pages), d.k_scales,
+                  d.v_scales, d.n_pages, d.kv_heads, d.page,
+                  static_cast<uint32_t>(__builtin_ctz(d.page))};
+    // at most two slots for each part aimed at (a sequence cut into c > 1 parts
+    // has more than c - 1 parts' blocks)
+    const uint64_t slot_rows = uint64_t(2) * kTargetParts * 16 * split_tiles_max(d.head_dim);
+    kv->scratch_bytes = slot_rows * (d.head_dim + 2) * 4;
+    const hipError_t e = hipMalloc(reinterpret_cast<void**>(&kv->scratch), kv->scratch_bytes);
+    if (e != hipSuccess) {
+        (void)hipGetLastError();
+        delete kv;
+        return fail_in(ES_ERR_NOMEM, name, "device allocation of the scratch failed");
+    }
+    kv->part_ml = kv->scratch + slot_rows * d.head_dim;
+    *out = kv;
+    return ES_OK;
+} catch (const std::bad_alloc&) {
+    return fail(ES_ERR_NOMEM, "es_kv_create: host allocation failed");
+}
+
+int es_kv_destroy(es_kv_t* kv) {
+    if (kv == nullptr) return ES_OK;
+    const int rc = release_device_memory(kv->device, kv->scratch, nullptr, "es_kv_destroy");
+    delete kv;
+    return rc;
+}
+
+uint64_t es_kv_device_bytes(const es_kv_t* kv) { return kv == nullptr ? 0 : kv->scratch_bytes; }
+
+int es_kv_append(es_kv_t* kv, const es_kv_append_t* args, es_stream_t stream) try {
+    const char* const name = "es_kv_append";
+    if (kv == nullptr || args == nullptr) return fail_in(ES_ERR_INVALID_ARG, name, "null pointer");
+    const es_kv_append_t& x = *args;
+    const uint32_t dim = kv->d.head_dim;
+    if (x.tokens > (1u << 24)) return fail_in(ES_ERR_INVALID_ARG, name, "tokens above 2^24");
+    if (x.q_heads > 1024) return fail_in(ES_ERR_INVALID_ARG, name, "q_heads above 1024");
+    if ((x.flags & ~ES_KV_ADJACENT) != 0) return fail_in(ES_ERR_INVALID_ARG, name, "unknown flags");
+    if (x.rot % 16 != 0 || x.rot > dim)
+        return fail_in(ES_ERR_INVALID_ARG, name, "rot not a multiple of 16 up to head_dim");
+    if ((x.q_gain != nullptr || x.k_gain != nullptr) && !(x.eps > 0.0f && std::isfinite(x.eps)))
+        return fail_in(ES_ERR_INVALID_ARG, name, "eps not positive and finite");
+    if (x.rot != 0 && (x.rope == nullptr || x.positions == nullptr || x.rope_rows == 0))
+        return fail_in(ES_ERR_INVALID_ARG, name, "rotation without table or positions");
+    if (x.tokens == 0) return ES_OK;
+    if (x.k == nullptr || x.v == nullptr || x.slots == nullptr ||
+        (x.q_heads != 0 && (x.q == nullptr || x.q_out == nullptr)))
+        return fail_in(ES_ERR_INVALID_ARG, name, "null pointer");
+    if (x.q_heads != 0 && x.tokens > 1 && x.q_out_stride < uint64_t(x.q_heads) * dim)
+        return fail_in(ES_ERR_INVALID_ARG, name, "q_out's rows overlap");
+    if (odd(x.q, 2) || odd(x.k, 2) || odd(x.v, 2) || odd(x.q_out, 2) || odd(x.q_gain, 2) ||
+        odd(x.k_gain, 2) || odd(x.rope, 4) || odd(x.positions, 4) || odd(x.slots, 8) ||
+        odd(x.status, 4))
+        return fail_in(ES_ERR_ALIGN, name, "array not aligned to its elements");
+    int rc = check_kv_device(kv, name);
+    const int dev = kv->device;
+    const uint64_t kw = uint64_t(kv->d.kv_heads) * dim, qw = uint64_t(x.q_heads) * dim;
+    if (rc == ES_OK) rc = check_rows(x.k, x.tokens, kw, x.k_stride, dev, name, ": keys");
+    if (rc == ES_OK) rc = check_rows(x.v, x.tokens, kw, x.v_stride, dev, name, ": values");
+    if (rc == ES_OK && qw != 0) rc = check_rows(x.q, x.tokens, qw, x.q_stride, dev, name, ": queries");
+    if (rc == ES_OK && qw != 0)
+        rc = check_rows(x.q_out, x.tokens, qw, x.q_out_stride, dev, name, ": query output");
+    if (rc == ES_OK && x.q_gain != nullptr)
+        rc = check_access(x.q_gain, 2 * dim, dev, name, ": query gain");
+    if (rc == ES_OK && x.k_gain != nullptr)
+        rc = check_access(x.k_gain, 2 * dim, dev, name, ": key gain");
+    if (rc == ES_OK && x.rot != 0)
+        rc = check_access(x.rope, uint64_t(4) * x.rot * x.rope_rows, dev, name, ": rotation table");
+    if (rc == ES_OK && x.rot != 0)
+        rc = check_access(x.positions, uint64_t(4) * x.tokens, dev, name, ": positions");
+    if (rc == ES_OK) rc = check_access(x.slots, uint64_t(8) * x.tokens, dev, name, ": slots");
+    if (rc == ES_OK && x.status != nullptr) rc = check_access(x.status, 4, dev, name, ": status");
+    if (rc != ES_OK) return rc;
+    AppendArgs a{};
+    a.q = static_cast<const uint16_t*>(x.q);
+    a.k = static_cast<const uint16_t*>(x.k);
+    a.v = static_cast<const uint16_t*>(x.v);
+    a.q_out = static_cast<uint16_t*>(x.q_out);
+    a.q_stride = x.q_stride;
+    a.k_stride = x.k_stride;
+    a.v_stride = x.v_stride;
+    a.q_out_stride = x.q_out_stride;
+    a.q_gain = static_cast<const uint16_t*>(x.q_gain);
+    a.k_gain = static_cast<const uint16_t*>(x.k_gain);
+    a.rope = x.rope;
+    a.positions = x.positions;
+    a.slots = x.slots;
+    a.status = x.status;
+    a.tokens = x.tokens;
+    a.q_heads = x.q_heads;
+    a.rot = x.rot;
+    a.rope_rows = x.rope_rows;
+    a.eps = x.eps;
+    a.adjacent = (x.flags & ES_KV_ADJACENT) != 0;
+    a.c = kv->c;
+    const AppendKernel kernel = by_dim_format<AppendKernel, MakeAppend>(dim, kv->d.format);
+    const dim3 grid((x.tokens + kPlaceTokens - 1) / kPlaceTokens, x.q_heads + kv->d.kv_heads);
+    hipLaunchKernelGGL(kernel, grid, dim3(kPlaceThreads), 0, static_cast<hipStream_t>(stream), a);
+    return launch_error("es_kv_append_kernel launch");
+} catch (const std::bad_alloc&) {
+    return fail(ES_ERR_NOMEM, "es_kv_append: host allocation failed");
+}
+
+int es_kv_read(es_kv_t* kv, const int64_t* slots, uint32_t tokens, void* k_out, uint64_t k_stride,
+               void* v_out, uint64_t v_stride, uint32_t* status, es_stream_t stream) try {
+    const char* const name = "es_kv_read";
+    if (kv == nullptr) return fail_in(ES_ERR_INVALID_ARG, name, "null pointer");
+    if (tokens > (1u << 24)) return fail_in(ES_ERR_INVALID_ARG, name, "tokens above 2^24");
+    if (tokens == 0) return ES_OK;
+    if (slots == nullptr || k_out == nullptr || v_out == nullptr)
+        return fail_in(ES_ERR_INVALID_ARG, name, "null pointer");
+    const uint64_t width = uint64_t(kv->d.kv_heads) * kv->d.head_dim;
+    if (tokens > 1 && (k_stride < width || v_stride < width))
+        return fail_in(ES_ERR_INVALID_ARG, name, "the output's rows overlap");
+    if (odd(slots, 8) || odd(k_out, 2) || odd(v_out, 2) || odd(status, 4))
+        return fail_in(ES_ERR_ALIGN, name, "array not aligned to its elements");
+    int rc = check_kv_device(kv, name);
+    const int dev = kv->device;
+    if (rc == ES_OK) rc = check_access(slots, uint64_t(8) * tokens, dev, name, ": slots");
+    if (rc == ES_OK) rc = check_rows(k_out, tokens, width, k_stride, dev, name, ": key output");
+    if (rc == ES_OK) rc = check_rows(v_out, tokens, width, v_stride, dev, name, ": value output");
+    if (rc == ES_OK && status != nullptr) rc = check_access(status, 4, dev, name, ": status");
+    if (rc != ES_OK) return rc;
+    ReadArgs a{};
+    a.slots = slots;
+    a.k_out = static_cast<uint16_t*>(k_out);
+    a.v_out = static_cast<uint16_t*>(v_out);
+    a.k_stride = k_stride;
+    a.v_stride = v_stride;
+    a.status = status;
+    a.tokens = tokens;
+    a.c = kv->c;
+    const ReadKernel kernel = by_dim_format<ReadKernel, MakeRead>(kv->d.head_dim, kv->d.format);
+    const dim3 grid((tokens + kPlaceTokens - 1) / kPlaceTokens, kv->d.kv_heads);
+    hipLaunchKernelGGL(kernel, grid, dim3(kPlaceThreads), 0, static_cast<hipStream_t>(stream), a);
+    return launch_error("es_kv_read_kernel launch");
+} catch (const std::bad_alloc&) {
+    return fail(ES_ERR_NOMEM, "es_kv_read: host allocation failed");
+}
+
+int es_kv_attend(es_kv_t* kv, const es_kv_attend_t* args, es_stream_t stream) try {
+    const char* const name = "es_kv_attend";
+    if (kv == nullptr || args == nullptr) return fail_in(ES_ERR_INVALID_ARG, name, "null pointer");
+    const es_kv_attend_t& x = *args;
+    const uint32_t dim = kv->d.head_dim, heads = kv->d.kv_heads;
+    if (x.rows > (1u << 24)) return fail_in(ES_ERR_INVALID_ARG, name, "rows above 2^24");
+    if (x.n_seqs == 0 || x.n_seqs > 65536)
+        return fail_in(ES_ERR_INVALID_ARG, name, "n_seqs out of range (1 .. 65536)");
+    if (x.q_heads == 0 || x.q_heads % heads != 0 || x.q_heads / heads > 64)
+        return fail_in(ES_ERR_INVALID_ARG, name,
+                       "q_heads is not a multiple (1 .. 64) of the cache's kv_heads");
+    if (!std::isfinite(x.scale)) return fail_in(ES_ERR_INVALID_ARG, name, "scale is not finite");
+    if (!(x.cap >= 0.0f) || !std::isfinite(x.cap))
+        return fail_in(ES_ERR_INVALID_ARG, name, "cap is negative or not finite");
+    if (x.table_stride == 0) return fail_in(ES_ERR_INVALID_ARG, name, "table_stride is 0");
+    if (x.rows == 0) return ES_OK;
+    if (x.q == nullptr || x.out == nullptr || x.tables == nullptr || x.lengths == nullptr ||
+        x.starts == nullptr)
+        return fail_in(ES_ERR_INVALID_ARG, name, "null pointer");
+    const uint64_t width = uint64_t(x.q_heads) * dim;
+    if (x.rows > 1 && x.out_stride < width)
+        return fail_in(ES_ERR_INVALID_ARG, name, "the output's rows overlap");
+    if (odd(x.q, 2) || odd(x.out, 2) || odd(x.tables, 4) || odd(x.lengths, 4) || odd(x.starts, 4) ||
+        odd(x.first, 4) || odd(x.limit, 4) || odd(x.slopes, 4) || odd(x.status, 4))
+        return fail_in(ES_ERR_ALIGN, name, "array not aligned to its elements");
+    int rc = check_kv_device(kv, name);
+    const int dev = kv->device;
+    if (rc == ES_OK) rc = check_rows(x.q, x.rows, width, x.q_stride, dev, name, ": queries");
+    if (rc == ES_OK) rc = check_rows(x.out, x.rows, width, x.out_stride, dev, name, ": output");
+    const struct { const void* p; uint64_t bytes; const char* what; } arrays[] = {
+        {x.tables, uint64_t(4) * x.n_seqs * x.table_stride, ": tables"},
+        {x.lengths, uint64_t(4) * x.n_seqs, ": lengths"},
+        {x.starts, uint64_t(4) * (uint64_t(x.n_seqs) + 1), ": starts"},
+        {x.first, x.first != nullptr ? uint64_t(4) * x.rows : 0, ": first"},
+        {x.limit, x.limit != nullptr ? uint64_t(4) * x.rows : 0, ": limit"},
+        {x.slopes, x.slopes != nullptr ? uint64_t(4) * x.q_heads : 0, ": slopes"},
+        {x.status, x.status != nullptr ? uint64_t(4) : 0, ": status"}};
+    for (const auto& p : arrays)
+        if (rc == ES_OK) rc = check_access(p.p, p.bytes, dev, name, p.what);
+    if (rc != ES_OK) return rc;
+
+    AttendArgs a{};
+    a.q = static_cast<const uint16_t*>(x.q);
+    a.out = static_cast<uint16_t*>(x.out);
+    a.q_stride = x.q_stride;
+    a.out_stride = x.out_stride;
+    a.tables = x.tables;
+    a.lengths = x.lengths;
+    a.starts = x.starts;
+    a.first = x.first;
+    a.limit = x.limit;
+    a.slopes = x.slopes;
+    a.status = x.status;
+    a.part_o = kv->scratch;
+    a.part_ml = kv->part_ml;
+    a.rows = x.rows;
+    a.n_seqs = x.n_seqs;
+    a.table_stride = x.table_stride;
+    a.q_heads = x.q_heads;
+    a.group = x.q_heads / heads;
+    a.target = kTargetParts;
+    a.min_blocks = kMinBlocks;
+    a.scale = x.scale;
+    a.cap = x.cap;
+    a.c = kv->c;
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    const uint64_t all_rows = uint64_t(x.rows) * a.group;      // of one key head
+    const uint64_t seq_rows = std::min<uint64_t>(x.rows, std::max(1u, x.max_rows)) * a.group;
+    if (seq_rows <= 64) {
+        const uint32_t tiles = seq_rows <= 16 ? 1 : split_tiles_max(dim);
+        const AttendKernel kernel =
+            tiles == 1 ? by_dim_format<AttendKernel, MakeSplit<1>::Of>(dim, kv->d.format)
+                       : by_dim_format<AttendKernel, MakeSplit<2>::Of>(dim, kv->d.format);
+        const uint32_t tile_rows = 16 * tiles;
+        // tiles of all sequences at most, and parts: one more than its share for each
+        const uint64_t n_tiles = all_rows / tile_rows + x.n_seqs;
+        const uint64_t n_parts = kTargetParts / heads + n_tiles;
+        if (n_parts * heads >= (uint64_t(1) << 24))
+            return fail_in(ES_ERR_INVALID_ARG, name, "too many rows for one call");
+        hipLaunchKernelGGL(kernel, dim3(n_parts * heads), dim3(kSplitThreads), 0, s, a);
+        rc = launch_error("es_kv_split_kernel launch");
+        if (rc != ES_OK) return rc;
+        const JoinKernel join = dim == 64    ? es_kv_join_kernel<64>
+                                : dim == 128 ? es_kv_join_kernel<128>
+                                             : es_kv_join_kernel<256>;
+        const uint32_t y = static_cast<uint32_t>(std::min<uint64_t>(tile_rows, seq_rows));
+        hipLaunchKernelGGL(join, dim3(n_tiles * heads, y), dim3(kSplitThreads), 0, s, a,
+                           static_cast<int>(tile_rows));
+        return launch_error("es_kv_join_kernel launch");
+    }
+    const bool plain = x.cap == 0.0f && x.slopes == nullptr;
+    const AttendKernel kernel =
+        plain ? by_dim_format<AttendKernel, MakeTile<true>::Of>(dim, kv->d.format)
+              : by_dim_format<AttendKernel, MakeTile<false>::Of>(dim, kv->d.format);
+    const uint32_t tile_rows = dim == 64    ? TileShape<64>::kRows
+                               : dim == 128 ? TileShape<128>::kRows
+                                            : TileShape<256>::kRows;
+    const uint32_t threads = dim == 64    ? TileShape<64>::kThreads
+                             : dim == 128 ? TileShape<128>::kThreads
+                                          : TileShape<256>::kThreads;
+    const size_t lds = dim == 64    ? TileShape<64>::kLds
+                       : dim == 128 ? TileShape<128>::kLds
+                                    : TileShape<256>::kLds;
+    const uint64_t n_tiles = all_rows / tile_rows + x.n_seqs;
+    if (n_tiles * heads >= (uint64_t(1) << 22))
+        return fail_in(ES_ERR_INVALID_ARG, name, "too many rows for one call");
+    hipLaunchKernelGGL(kernel, dim3(n_tiles * heads), dim3(threads), lds, s, a);
+    return launch_error("es_kv_tile_kernel launch");
+} catch (const std::bad_alloc&) {
+    return fail(ES_ERR_NOMEM, "es_kv_attend: host allocation failed");
+}
+
+}  // extern "C"

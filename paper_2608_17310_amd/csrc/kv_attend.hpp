@@ -1,0 +1,905 @@
+// Attention over the cache: out = softmax(scores) V for the rows of a batch of
+// sequences, each over its own interval of keys.
+//
+// Both kernels form the transposed products
+//   S^T = K Q^T     (keys by rows)        O^T = V^T P^T     (dimensions by rows)
+// with rows = query rows in the columns of the matrix instructions.  A
+// column of S^T then lives in the lanes n, n + 16, ... (n + 32) of a wave, so a
+// row's running maximum and sum are one register a lane, and the exponentials
+// are, as they stand in the registers, the second product's right operand: nothing
+// moves between lanes.  For that the keys are dealt to the rows of S^T in the
+// order in which a lane of V^T reads them: consecutive tokens, one 16-byte word,
+// because the cache holds values by dimension.
+//
+// The rows of a tile are pairs (token, query head of the group of one key
+// head), numbered token-major: a group of any size shares its keys' loads.
+//
+// Softmax in units of log2, in binary32, over one pass with a running maximum.
+// Weights are rounded to bf16 (RNE) for the matrix unit, after the product
+// with the value's scale; their sum is taken before the rounding.
+#pragma once
+
+#include "kv_common.hpp"
+
+namespace eskv {
+
+constexpr int kBlock = 64;                  // keys of a block: never more than a page
+
+struct AttendArgs {
+    const uint16_t* q;
+    uint16_t* out;
+    uint64_t q_stride, out_stride;
+    const int32_t* tables;
+    const int32_t* lengths;
+    const int32_t* starts;
+    const int32_t* first;
+    const int32_t* limit;
+    const float* slopes;
+    uint32_t* status;
+    float* part_o;                          // [slots][rows of a tile][D], split kernel
+    float* part_ml;                         // [slots][rows of a tile][2]: maximum, sum
+    uint32_t rows, n_seqs, table_stride, q_heads, group;
+    uint32_t target, min_blocks;            // split kernel: parts aimed at, blocks of a part at least
+    float scale, cap;
+    Cache c;
+};
+
+// A sequence of the batch: its rows [start, start + n) and its length, clamped
+// into what q and the table hold.
+struct Seq {
+    int start, n, len;
+};
+
+__device__ __forceinline__ Seq read_seq(const AttendArgs& a, uint32_t s) {
+    const int rows = static_cast<int>(a.rows);
+    const int s0 = a.starts[s], s1 = a.starts[s + 1], len = a.lengths[s];
+    const int64_t room = int64_t(a.table_stride) << a.c.page_shift;
+    Seq q;
+    q.start = min(max(s0, 0), rows);
+    q.n = min(max(s1, q.start), rows) - q.start;
+    q.len = static_cast<int>(min(int64_t(max(len, 0)), room));
+    if (a.status != nullptr &&
+        (q.start != s0 || q.start + q.n != s1 || q.len != len || q.n > q.len))
+        atomicOr(a.status, ES_KV_BAD_LENGTH);
+    return q;
+}
+
+// The keys [first, limit) that row i of a sequence sees, empty as (0, 0).
+__device__ __forceinline__ void interval(const AttendArgs& a, const Seq& s, int i, int& lo, int& hi) {
+    lo = a.first != nullptr ? max(a.first[s.start + i], 0) : 0;
+    hi = a.limit != nullptr ? a.limit[s.start + i] : s.len - s.n + i + 1;
+    hi = min(hi, s.len);
+    if (lo >= hi) lo = hi = 0;
+}
+
+constexpr float kWideCap = 256.0f;
+
+// Scores as the matrix unit leaves them, to the softmax's units.
+struct ScoreMap {
+    float scale;                            // log2(e) times the scale (without cap)
+    float cap, cap_in;                      // cap log2(e); 2 log2(e) scale / cap
+    float slope;                            // log2(e) times the slope of this lane's row
+    bool capped, wide, sloped;
+};
+
+template <bool kPlain>
+__device__ __forceinline__ float score(const ScoreMap& m, float s, float key_scale, int away) {
+    if constexpr (kPlain) return s * (m.scale * key_scale);
+    float t;
+    if (m.capped) {
+        // tanh(y) = 1 - 2 / (1 + e^(2 y)); e^(2 y) may be infinite
+        const float z = s * (m.cap_in * key_scale);          // 2 y log2(e)
+        const float e = __builtin_amdgcn_exp2f(z);
+        t = m.cap - 2.0f * m.cap * __builtin_amdgcn_rcpf(1.0f + e);
+        if (m.wide) {
+            // the difference is off by about 2^-23 cap, which a wide cap makes
+            // large beside a small score: there the series of tanh, to y^9
+            const float y = z * 0.34657359f, y2 = y * y;     // ln(2) / 2
+            float f = __builtin_fmaf(y2, 62.0f / 2835.0f, -17.0f / 315.0f);
+            f = __builtin_fmaf(y2, f, 2.0f / 15.0f);
+            f = __builtin_fmaf(y2, f, -1.0f / 3.0f);
+            f = __builtin_fmaf(y2 * y, f, y);
+            t = __builtin_fabsf(y) < 0.25f ? m.cap * f : t;
+        }
+    } else {
+        t = s * (m.scale * key_scale);
+    }
+    return m.sloped ? t - m.slope * static_cast<float>(away < 0 ? -away : away) : t;
+}
+
+__device__ __forceinline__ ScoreMap score_map(const AttendArgs& a) {
+    ScoreMap m;
+    m.scale = a.scale * kLog2e;
+    m.capped = a.cap > 0.0f;
+    m.wide = a.cap > kWideCap;
+    m.cap = a.cap * kLog2e;
+    m.cap_in = m.capped ? 2.0f * kLog2e * a.scale / a.cap : 0.0f;
+    m.sloped = a.slopes != nullptr;
+    m.slope = 0.0f;
+    return m;
+}
+
+// ----------------------------------------------------------------------------
+// Few rows over long histories: the keys of every sequence are cut into parts,
+// a workgroup each, and joined by a second kernel.  Bound by the cache's bytes:
+// a wave streams blocks of 64 keys straight from memory into the matrix
+// unit's operands, with no LDS and no barrier before the workgroup's own join.
+//
+// The cut is made on the device from the lengths, so that a step can be
+// replayed from a graph while histories grow: all sequences' parts have the same
+// number of blocks, C = ceil(all blocks / target), and a workgroup finds its
+// sequence by a scan over the batch (a wave, 64 sequences at a time).
+// ----------------------------------------------------------------------------
+
+constexpr int kSplitThreads = 256;
+constexpr int kSplitWaves = kSplitThreads / 64;
+constexpr int kScanRows = 64;               // rows of a sequence whose intervals the scan reads
+
+struct Span {                               // a sequence's blocks
+    Seq seq;
+    int block0, blocks;                     // the first block that some row sees, and their number
+    uint32_t tiles;                         // tiles of rows
+};
+
+__device__ __forceinline__ Span read_span(const AttendArgs& a, uint32_t s, int tile_rows) {
+    Span p;
+    p.seq = Seq{0, 0, 0};
+    p.block0 = p.blocks = 0;
+    p.tiles = 0;
+    if (s >= a.n_seqs) return p;
+    p.seq = read_seq(a, s);
+    int lo = 0, hi = p.seq.len;
+    if (p.seq.n <= kScanRows && (a.first != nullptr || a.limit != nullptr)) {
+        lo = p.seq.len;
+        hi = 0;
+        for (int i = 0; i < p.seq.n; ++i) {
+            int f, l;
+            interval(a, p.seq, i, f, l);
+            if (f < l) {
+                lo = min(lo, f);
+                hi = max(hi, l);
+            }
+        }
+    }
+    p.tiles = (uint32_t(p.seq.n) * a.group + tile_rows - 1) / tile_rows;
+    if (lo < hi && p.tiles > 0) {
+        p.block0 = lo / kBlock;
+        p.blocks = (hi - 1) / kBlock + 1 - p.block0;
+    }
+    return p;
+}
+
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {          // inclusive
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int m = 1; m < 64; m *= 2) {
+        const uint32_t y = __shfl_up(x, m);
+        if (lane >= m) x += y;
+    }
+    return x;
+}
+__device__ __forceinline__ int from_lane(int x, int lane) {
+    return __builtin_amdgcn_readlane(x, lane);
+}
+
+// A tile of rows of one sequence, and (kParts) one part of its blocks.
+struct Place {
+    Seq seq;
+    uint32_t s;                             // the sequence
+    int block0, blocks;                     // the sequence's blocks
+    uint32_t tile, chunk, chunks, per;      // per: blocks of a part
+    uint32_t slot;                          // of the tile's first part, over the batch (chunks > 1)
+    bool found;
+};
+
+// The place numbered `unit` among all parts (kParts) or tiles of the batch.
+// Every lane of the wave calls it and gets the same answer.
+template <bool kParts>
+__device__ __forceinline__ Place find_place(const AttendArgs& a, int tile_rows, uint32_t unit) {
+    const uint32_t lane = threadIdx.x & 63;
+    Span mine = read_span(a, lane, tile_rows);
+    uint64_t total = uint64_t(mine.blocks) * mine.tiles;
+    for (uint32_t s0 = 64; s0 < a.n_seqs; s0 += 64) {
+        const Span p = read_span(a, s0 + lane, tile_rows);
+        total += uint64_t(p.blocks) * p.tiles;
+    }
+#pragma unroll
+    for (int m = 1; m < 64; m *= 2) total += __shfl_xor(total, m);
+    total *= a.c.heads;
+    const uint64_t per64 = max((total + a.target - 1) / a.target, uint64_t(a.min_blocks));
+    Place r;
+    r.per = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(per64));
+    r.found = false;
+    uint32_t units0 = 0, slots0 = 0;
+    for (uint32_t s0 = 0; s0 < a.n_seqs; s0 += 64) {
+        const Span p = s0 == 0 ? mine : read_span(a, s0 + lane, tile_rows);
+        const uint32_t chunks = max(1u, (uint32_t(p.blocks) + r.per - 1) / r.per);
+        const uint32_t units = p.tiles * (kParts ? chunks : 1u);
+        const uint32_t slots = chunks > 1 ? p.tiles * chunks : 0u;
+        const uint32_t units1 = wave_scan(units), slots1 = wave_scan(slots);
+        const uint64_t past = __ballot(units0 + units1 > unit);
+        if (past != 0) {
+            const int src = __builtin_ctzll(past);
+            r.seq = Seq{from_lane(p.seq.start, src), from_lane(p.seq.n, src),
+                        from_lane(p.seq.len, src)};
+            r.s = s0 + src;
+            r.block0 = from_lane(p.block0, src);
+            r.blocks = from_lane(p.blocks, src);
+            r.chunks = from_lane(chunks, src);
+            const uint32_t in = unit - units0 - from_lane(units1 - units, src);
+            r.tile = kParts ? in / r.chunks : in;
+            r.chunk = kParts ? in % r.chunks : 0u;
+            r.slot = slots0 + from_lane(slots1 - slots, src) + r.tile * r.chunks;
+            r.found = r.tile < uint32_t(from_lane(p.tiles, src));
+            return r;
+        }
+        units0 += from_lane(units1, 63);
+        slots0 += from_lane(slots1, 63);
+    }
+    return r;
+}
+
+// This lane's 16 bytes of a token-major row or of a dimension's row of tokens.
+__device__ __forceinline__ u32x4_t zero4() { return u32x4_t{0u, 0u, 0u, 0u}; }
+
+// Keep the first n of the tokens of a 16-byte word.
+template <int kFmt>
+__device__ __forceinline__ u32x4_t token_mask(int n) {
+    constexpr int kPer = 4 / kCodeBytes<kFmt>;               // tokens of a 32-bit word
+    constexpr int kBits = 8 * kCodeBytes<kFmt>;
+    u32x4_t m;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const int k = n - kPer * w;
+        m[w] = k <= 0 ? 0u : k >= kPer ? ~0u : (1u << (kBits * k)) - 1u;
+    }
+    return m;
+}
+
+template <int D, int kTiles, int kFmt>
+__global__ __launch_bounds__(kSplitThreads) void es_kv_split_kernel(AttendArgs a) {
+    constexpr int kRowsOfTile = 16 * kTiles;
+    constexpr int kSteps = D / 32;                           // 32 dimensions a product
+    constexpr int kDims = D / 16;                            // 16 dimensions a tile of O^T
+    constexpr bool kBytes = kFmt != kBf16;
+    // 16-byte words of a lane: of a key's row, and of a dimension's 64 tokens
+    constexpr int kKeyWords = kBytes ? kSteps / 2 : kSteps;
+    constexpr int kValWords = kBytes ? 1 : 2;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int n = lane & 15, g = lane >> 4;
+    const uint32_t h = blockIdx.x % a.c.heads;
+
+    const Place at = find_place<true>(a, kRowsOfTile, blockIdx.x / a.c.heads);
+    if (!at.found) return;
+
+    // this lane's rows: column n of each tile of 16.  Columns past the last row
+    // repeat it and are not written.
+    const int n_rows = at.seq.n * static_cast<int>(a.group);
+    const int row0 = static_cast<int>(at.tile) * kRowsOfTile;
+    ScoreMap map[kTiles];
+    int first[kTiles], limit[kTiles], pos[kTiles];
+    bf16x8_t q[kTiles][kSteps];
+    int lo_any = at.seq.len, hi_any = 0, lo_all = 0, hi_all = at.seq.len;
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+        const int r = min(row0 + 16 * t + n, n_rows - 1);
+        const int i = r / static_cast<int>(a.group);
+        const uint32_t head = h * a.group + (r - i * static_cast<int>(a.group));
+        interval(a, at.seq, i, first[t], limit[t]);
+        pos[t] = at.seq.len - at.seq.n + i;
+        map[t] = score_map(a);
+        if (map[t].sloped) map[t].slope = a.slopes[head] * kLog2e;
+        if (first[t] < limit[t]) {
+            lo_any = min(lo_any, first[t]);
+            hi_any = max(hi_any, limit[t]);
+        }
+        lo_all = max(lo_all, first[t]);
+        hi_all = min(hi_all, limit[t]);
+        const uint16_t* src = a.q + uint64_t(at.seq.start + i) * a.q_stride + uint64_t(head) * D;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            // the dimensions that a lane's words of a key hold: 8 of 32, or 16 of 64
+            const int d = kBytes ? 64 * (s / 2) + 16 * g + 8 * (s & 1) : 32 * s + 8 * g;
+            q[t][s] = __builtin_bit_cast(bf16x8_t, load_row8(src + d));
+        }
+    }
+#pragma unroll
+    for (int m = 1; m < 16; m *= 2) {
+        lo_any = min(lo_any, __shfl_xor(lo_any, m));
+        hi_any = max(hi_any, __shfl_xor(hi_any, m));
+        lo_all = max(lo_all, __shfl_xor(lo_all, m));
+        hi_all = min(hi_all, __shfl_xor(hi_all, m));
+    }
+    lo_any = __builtin_amdgcn_readfirstlane(lo_any);
+    hi_any = __builtin_amdgcn_readfirstlane(hi_any);
+    lo_all = __builtin_amdgcn_readfirstlane(lo_all);
+    hi_all = __builtin_amdgcn_readfirstlane(hi_all);
+
+    float top[kTiles], sum[kTiles];
+    f32x4_t o[kTiles][kDims];
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+        top[t] = -inf();
+        sum[t] = 0.0f;
+#pragma unroll
+        for (int d = 0; d < kDims; ++d) o[t][d] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+
+    const int b_end0 = at.block0 + at.blocks;
+    const int b_begin = at.block0 + static_cast<int>(at.chunk * at.per);
+    const int b_end = min(b_end0, b_begin + static_cast<int>(at.per));
+    const int32_t* table = a.tables + uint64_t(at.s) * a.table_stride;
+    for (int b = b_begin + wave; b < b_end; b += kSplitWaves) {
+        const int key0 = b * kBlock;
+        if (key0 >= hi_any || key0 + kBlock <= lo_any) continue;
+        const uint32_t page = table[key0 >> a.c.page_shift];
+        const bool bad = page >= a.c.n_pages;
+        const uint64_t head_at = uint64_t(bad ? 0u : page) * a.c.heads + h;
+        const uint32_t off = uint32_t(key0) & (a.c.page - 1);
+        const uint64_t token = head_at * a.c.page + off;
+
+        // the block's keys: word w of the key that row n of tile t stands for
+        u32x4_t kw[4][kKeyWords];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const int key = kBytes ? 16 * (n >> 2) + 4 * t + (n & 3)
+                                   : 32 * (t >> 1) + 8 * (n >> 2) + 4 * (t & 1) + (n & 3);
+            const uint8_t* src = a.c.k + (token + key) * (D * kCodeBytes<kFmt>) + 16 * g;
+#pragma unroll
+            for (int w = 0; w < kKeyWords; ++w) kw[t][w] = load<u32x4_t>(src + 64 * w);
+        }
+        // its values: dimension 16 d + n, this lane's tokens
+        u32x4_t vw[kDims][kValWords];
+        const uint8_t* vsrc =
+            a.c.v + ((head_at * D + n) * a.c.page + off) * kCodeBytes<kFmt> + 16 * g;
+        const uint64_t vstep = uint64_t(16) * a.c.page * kCodeBytes<kFmt>;
+#pragma unroll
+        for (int d = 0; d < kDims; ++d)
+#pragma unroll
+            for (int w = 0; w < kValWords; ++w) vw[d][w] = load<u32x4_t>(vsrc + d * vstep + 64 * w);
+        // its scales: this lane's keys are 16 g .. 16 g + 15
+        f32x4_t ks[4], vs[4];
+        if constexpr (kBytes) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                ks[t] = load<f32x4_t>(a.c.ks + token + 16 * g + 4 * t);
+                vs[t] = load<f32x4_t>(a.c.vs + token + 16 * g + 4 * t);
+            }
+        }
+
+        const bool masked = key0 < lo_all || key0 + kBlock > hi_all;
+        bf16x8_t p[kTiles][2];
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) {
+            f32x4_t s[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                s[k] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int w = 0; w < kKeyWords; ++w) {
+                    if constexpr (kBytes) {
+                        const u32x4_t x0 = codes_to_bf16<kFmt>(u32x2_t{kw[k][w][0], kw[k][w][1]});
+                        const u32x4_t x1 = codes_to_bf16<kFmt>(u32x2_t{kw[k][w][2], kw[k][w][3]});
+                        s[k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                            __builtin_bit_cast(bf16x8_t, x0), q[t][2 * w], s[k], 0, 0, 0);
+                        s[k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                            __builtin_bit_cast(bf16x8_t, x1), q[t][2 * w + 1], s[k], 0, 0, 0);
+                    } else {
+                        s[k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                            __builtin_bit_cast(bf16x8_t, kw[k][w]), q[t][w], s[k], 0, 0, 0);
+                    }
+                }
+            }
+            // scores of this lane's 16 keys, in the softmax's units
+            float peak = -inf();
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int key = key0 + (kBytes ? 16 * g + 4 * k + i
+                                                   : 32 * (k >> 1) + 8 * g + 4 * (k & 1) + i);
+                    float x = score<false>(map[t], s[k][i], kBytes ? ks[k][i] : 1.0f, pos[t] - key);
+                    if (bad) x = nan();
+                    if (masked && (key < first[t] || key >= limit[t])) x = -inf();
+                    s[k][i] = x;
+                    peak = __builtin_fmaxf(peak, x);
+                }
+            peak = __builtin_fmaxf(peak, __shfl_xor(peak, 16));
+            peak = __builtin_fmaxf(peak, __shfl_xor(peak, 32));
+            const float now = __builtin_fmaxf(top[t], peak);
+            // nothing seen so far: any finite stand-in gives weights of zero
+            const float base = now == -inf() ? 0.0f : now;
+            if (__any(now > top[t])) {
+                const float shrink = __builtin_amdgcn_exp2f(top[t] - base);
+                sum[t] *= shrink;
+#pragma unroll
+                for (int d = 0; d < kDims; ++d) o[t][d] *= shrink;
+            }
+            top[t] = now;
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                u32x4_t w;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    float e[2];
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const int k = 2 * u + (j >> 1), i = 2 * (j & 1) + x;
+                        e[x] = __builtin_amdgcn_exp2f(s[k][i] - base);
+                        sum[t] += e[x];
+                        // a weight of zero stays zero whatever stands in a slot unseen
+                        if constexpr (kBytes) e[x] = e[x] == 0.0f ? 0.0f : e[x] * vs[k][i];
+                    }
+                    w[j] = pack_bf16(e[0], e[1]);
+                }
+                p[t][u] = __builtin_bit_cast(bf16x8_t, w);
+            }
+        }
+        if (bad && a.status != nullptr && lane == 0) atomicOr(a.status, ES_KV_BAD_PAGE);
+        if (bad || key0 + kBlock > at.seq.len) {
+            // slots past the sequence's end may hold anything
+            const int left = bad ? 0 : at.seq.len - key0;
+#pragma unroll
+            for (int w = 0; w < kValWords; ++w) {
+                const u32x4_t keep = token_mask<kFmt>(left - (kBytes ? 16 * g : 32 * w + 8 * g));
+#pragma unroll
+                for (int d = 0; d < kDims; ++d) vw[d][w] &= keep;
+            }
+        }
+#pragma unroll
+        for (int d = 0; d < kDims; ++d) {
+            bf16x8_t v[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                if constexpr (kBytes)
+                    v[u] = __builtin_bit_cast(
+                        bf16x8_t, codes_to_bf16<kFmt>(u32x2_t{vw[d][0][2 * u], vw[d][0][2 * u + 1]}));
+                else
+                    v[u] = __builtin_bit_cast(bf16x8_t, vw[d][u]);
+            }
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+                    o[t][d] =
+                        __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[u], p[t][u], o[t][d], 0, 0, 0);
+        }
+    }
+
+    // join the waves: the others hand their sums to wave 0 through LDS
+    __shared__ float ml[kSplitWaves][2][16];
+    __shared__ __attribute__((aligned(16))) f32x4_t part[kSplitWaves - 1][kDims][64];
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+        float l = sum[t];
+        l += __shfl_xor(l, 16);
+        l += __shfl_xor(l, 32);
+        if (t > 0) __syncthreads();
+        if (g == 0) {
+            ml[wave][0][n] = top[t];
+            ml[wave][1][n] = l;
+        }
+        __syncthreads();
+        float m = -inf();
+#pragma unroll
+        for (int w = 0; w < kSplitWaves; ++w) m = __builtin_fmaxf(m, ml[w][0][n]);
+        const float base = m == -inf() ? 0.0f : m;
+        const float mine = __builtin_amdgcn_exp2f(top[t] - base);
+        if (wave > 0) {
+#pragma unroll
+            for (int d = 0; d < kDims; ++d) part[wave - 1][d][lane] = o[t][d] * mine;
+        }
+        __syncthreads();
+        if (wave > 0) continue;
+        float total = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kSplitWaves; ++w)
+            total += ml[w][1][n] * __builtin_amdgcn_exp2f(ml[w][0][n] - base);
+        const int r = row0 + 16 * t + n;
+        const bool real = r < n_rows;
+        const int i = min(r, n_rows - 1) / static_cast<int>(a.group);
+        const uint32_t head = h * a.group + (min(r, n_rows - 1) - i * static_cast<int>(a.group));
+        const bool whole = at.chunks == 1;
+        const float inv = total > 0.0f || total != total ? 1.0f / total : 0.0f;
+        const uint64_t slot =
+            ((uint64_t(at.slot) + at.chunk) * a.c.heads + h) * kRowsOfTile + 16 * t + n;
+        uint16_t* out = a.out + uint64_t(at.seq.start + i) * a.out_stride + uint64_t(head) * D;
+#pragma unroll
+        for (int d = 0; d < kDims; ++d) {
+            f32x4_t x = o[t][d] * mine;
+#pragma unroll
+            for (int w = 0; w < kSplitWaves - 1; ++w) x += part[w][d][lane];
+            if (!real) continue;
+            if (whole) {
+                x *= inv;
+                u32x2_t y;
+                y = u32x2_t{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+                store_row4(out + 16 * d + 4 * g, y);
+            } else {
+                store<f32x4_t>(a.part_o + slot * D + 16 * d + 4 * g, x);
+            }
+        }
+        if (real && !whole && g == 0) {
+            a.part_ml[2 * slot] = m;
+            a.part_ml[2 * slot + 1] = total;
+        }
+    }
+}
+
+// Join the parts of each row: out = sum_c 2^(m_c - M) o_c / sum_c 2^(m_c - M) l_c.
+// A workgroup per row of a tile (rows blockIdx.y, + gridDim.y, ...); D / 4 lanes
+// hold a row, and the others take other parts.
+template <int D>
+__global__ __launch_bounds__(kSplitThreads) void es_kv_join_kernel(AttendArgs a, int tile_rows) {
+    constexpr int kLanes = D / 4;
+    constexpr int kGroups = kSplitThreads / kLanes;
+    const uint32_t h = blockIdx.x % a.c.heads;
+    const Place at = find_place<false>(a, tile_rows, blockIdx.x / a.c.heads);
+    if (!at.found || at.chunks <= 1) return;
+    const int n_rows = at.seq.n * static_cast<int>(a.group);
+    const int lane = threadIdx.x % kLanes, grp = threadIdx.x / kLanes;
+    __shared__ float ml[kGroups][2];
+    __shared__ __attribute__((aligned(16))) f32x4_t part[kGroups][kLanes];
+    for (int y = blockIdx.y; y < tile_rows; y += gridDim.y) {
+        const int r = static_cast<int>(at.tile) * tile_rows + y;
+        if (r >= n_rows) break;
+        float m = -inf(), l = 0.0f;
+        f32x4_t o = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (uint32_t c = grp; c < at.chunks; c += kGroups) {
+            const uint64_t slot =
+                ((uint64_t(at.slot) + c) * a.c.heads + h) * tile_rows + y;
+            const float mc = a.part_ml[2 * slot], lc = a.part_ml[2 * slot + 1];
+            const f32x4_t oc = load<f32x4_t>(a.part_o + slot * D + 4 * lane);
+            const float now = __builtin_fmaxf(m, mc);
+            const float base = now == -inf() ? 0.0f : now;
+            const float x = __builtin_amdgcn_exp2f(m - base), z = __builtin_amdgcn_exp2f(mc - base);
+            l = l * x + lc * z;
+            o = o * x + oc * z;
+            m = now;
+        }
+        if (lane == 0) {
+            ml[grp][0] = m;
+            ml[grp][1] = l;
+        }
+        part[grp][lane] = o;
+        __syncthreads();
+        if (grp == 0) {
+            float top = -inf(), total = 0.0f;
+#pragma unroll
+            for (int k = 0; k < kGroups; ++k) top = __builtin_fmaxf(top, ml[k][0]);
+            const float base = top == -inf() ? 0.0f : top;
+            f32x4_t x = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int k = 0; k < kGroups; ++k) {
+                const float z = __builtin_amdgcn_exp2f(ml[k][0] - base);
+                total += ml[k][1] * z;
+                x += part[k][lane] * z;
+            }
+            x *= total > 0.0f || total != total ? 1.0f / total : 0.0f;
+            const int i = r / static_cast<int>(a.group);
+            const uint32_t head = h * a.group + (r - i * static_cast<int>(a.group));
+            u32x2_t w;
+            w = u32x2_t{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+            store_row4(a.out + uint64_t(at.seq.start + i) * a.out_stride + uint64_t(head) * D +
+                            4 * lane, w);
+        }
+        __syncthreads();
+    }
+}
+
+// ----------------------------------------------------------------------------
+// Many rows: a workgroup of kWaves waves takes 32 kWaves rows of one key head,
+// 32 to a wave, over all blocks that some of them see.  Bound by the matrix
+// unit beside the exponentials: keys and values are staged in LDS as bf16, once
+// for all waves (codes are converted on their way in), double-buffered, the
+// next block's loads in flight under the present block's products.
+//
+// LDS rows are 2 D bytes (keys) and 128 bytes (values); their 16-byte words
+// are exchanged by the row's number so that 16 rows of one word lie in 16
+// different groups of banks.
+// ----------------------------------------------------------------------------
+
+template <int D>
+struct TileShape {
+    static constexpr int kWaves = D == 128 ? 8 : 4;
+    static constexpr int kThreads = 64 * kWaves;
+    static constexpr int kRows = 32 * kWaves;
+    static constexpr int kKeyBytes = kBlock * D * 2;
+    static constexpr int kBuffer = 2 * kKeyBytes;            // keys, then as many bytes of values
+    static constexpr int kLds = 2 * kBuffer + 256 * 4;       //   and the scales of both
+};
+
+// Byte offsets of 16-byte words in the staged tiles.
+template <int D>
+__device__ __forceinline__ int key_word(int row, int w) {
+    if constexpr (D == 64) return row * 128 + 16 * (w ^ ((row >> 1) & 7));
+    return row * (2 * D) + 16 * (w ^ (row & 15));
+}
+__device__ __forceinline__ int val_word(int row, int w) {
+    return row * 128 + 16 * (w ^ ((row >> 1) & 7));
+}
+
+// A workgroup's tile of rows: the sequence and the tile, found like a part.
+__device__ __forceinline__ Place find_tile(const AttendArgs& a, int tile_rows, uint32_t unit) {
+    const uint32_t lane = threadIdx.x & 63;
+    Place r;
+    r.found = false;
+    uint32_t units0 = 0;
+    for (uint32_t s0 = 0; s0 < a.n_seqs; s0 += 64) {
+        const uint32_t s = s0 + lane;
+        const Seq q = s < a.n_seqs ? read_seq(a, s) : Seq{0, 0, 0};
+        const uint32_t units = (uint32_t(q.n) * a.group + tile_rows - 1) / tile_rows;
+        const uint32_t units1 = wave_scan(units);
+        const uint64_t past = __ballot(units0 + units1 > unit);
+        if (past != 0) {
+            const int src = __builtin_ctzll(past);
+            r.seq = Seq{from_lane(q.start, src), from_lane(q.n, src), from_lane(q.len, src)};
+            r.s = s0 + src;
+            // the last tiles, which see the most keys, first
+            const uint32_t in = unit - units0 - from_lane(units1 - units, src);
+            r.found = in < uint32_t(from_lane(units, src));
+            r.tile = from_lane(units, src) - 1 - in;
+            return r;
+        }
+        units0 += from_lane(units1, 63);
+    }
+    return r;
+}
+
+template <int D, int kFmt, bool kPlain>
+__global__ __launch_bounds__(TileShape<D>::kThreads) void es_kv_tile_kernel(AttendArgs a) {
+    using S = TileShape<D>;
+    constexpr bool kBytes = kFmt != kBf16;
+    constexpr int kSteps = D / 16;                           // 16 dimensions a product
+    constexpr int kDims = D / 32;                            // 32 dimensions a tile of O^T
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int n = lane & 31, g = lane >> 5;
+    const uint32_t h = blockIdx.x % a.c.heads;
+
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+    __shared__ int bounds[2][S::kWaves];
+
+    const Place at = find_tile(a, S::kRows, blockIdx.x / a.c.heads);
+    if (!at.found) return;
+
+    const int n_rows = at.seq.n * static_cast<int>(a.group);
+    const int r = static_cast<int>(at.tile) * S::kRows + 32 * wave + n;
+    const int rr = min(r, n_rows - 1);
+    const int i = rr / static_cast<int>(a.group);
+    const uint32_t head = h * a.group + (rr - i * static_cast<int>(a.group));
+    int first, limit;
+    interval(a, at.seq, i, first, limit);
+    const int pos = at.seq.len - at.seq.n + i;
+    ScoreMap map = score_map(a);
+    if (map.sloped) map.slope = a.slopes[head] * kLog2e;
+
+    bf16x8_t q[kSteps];
+    {
+        const uint16_t* src = a.q + uint64_t(at.seq.start + i) * a.q_stride + uint64_t(head) * D;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s)
+            q[s] = __builtin_bit_cast(bf16x8_t, load_row8(src + 16 * s + 8 * g));
+    }
+
+    // what the wave's rows see, some and all of them; and the workgroup's
+    int lo_any = first < limit ? first : at.seq.len, hi_any = limit;
+    int lo_all = first, hi_all = limit;
+#pragma unroll
+    for (int m = 1; m < 32; m *= 2) {
+        lo_any = min(lo_any, __shfl_xor(lo_any, m));
+        hi_any = max(hi_any, __shfl_xor(hi_any, m));
+        lo_all = max(lo_all, __shfl_xor(lo_all, m));
+        hi_all = min(hi_all, __shfl_xor(hi_all, m));
+    }
+    lo_any = __builtin_amdgcn_readfirstlane(lo_any);
+    hi_any = __builtin_amdgcn_readfirstlane(hi_any);
+    lo_all = __builtin_amdgcn_readfirstlane(lo_all);
+    hi_all = __builtin_amdgcn_readfirstlane(hi_all);
+    if (lane == 0) {
+        bounds[0][wave] = lo_any;
+        bounds[1][wave] = hi_any;
+    }
+    __syncthreads();
+    int lo = at.seq.len, hi = 0;
+#pragma unroll
+    for (int w = 0; w < S::kWaves; ++w) {
+        lo = min(lo, bounds[0][w]);
+        hi = max(hi, bounds[1][w]);
+    }
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    hi = __builtin_amdgcn_readfirstlane(hi);
+    const int b_begin = lo / kBlock, b_end = hi > lo ? (hi - 1) / kBlock + 1 : b_begin;
+
+    // staging: 16-byte words of codes, each thread kStage of the keys' and of the values'
+    constexpr int kWordsK = kBlock * D * kCodeBytes<kFmt> / 16;
+    constexpr int kStage = kWordsK / S::kThreads;
+    static_assert(kStage >= 1 && kWordsK % S::kThreads == 0, "staging covers the block");
+    constexpr int kKeyWords = D * kCodeBytes<kFmt> / 16;     // words of a key's row
+    constexpr int kValWords = kBlock * kCodeBytes<kFmt> / 16;    // of a dimension's tokens
+    u32x4_t sk[kStage], sv[kStage];
+    float sscale = 0.0f;
+    bool bad = false;
+    const int32_t* table = a.tables + uint64_t(at.s) * a.table_stride;
+    auto fetch = [&](int b) {
+        const int key0 = b * kBlock;
+        const uint32_t page = table[key0 >> a.c.page_shift];
+        bad = page >= a.c.n_pages;
+        const uint64_t head_at = uint64_t(bad ? 0u : page) * a.c.heads + h;
+        const uint32_t off = uint32_t(key0) & (a.c.page - 1);
+        const uint64_t token = head_at * a.c.page + off;
+        const uint8_t* ksrc = a.c.k + token * (D * kCodeBytes<kFmt>);
+        const uint8_t* vsrc = a.c.v + (head_at * D * a.c.page + off) * kCodeBytes<kFmt>;
+#pragma unroll
+        for (int x = 0; x < kStage; ++x) {
+            const int w = threadIdx.x + S::kThreads * x;
+            sk[x] = load<u32x4_t>(ksrc + 16 * w);
+            sv[x] = load<u32x4_t>(vsrc + uint64_t(w / kValWords) * a.c.page * kCodeBytes<kFmt> +
+                                  16 * (w % kValWords));
+        }
+        if constexpr (kBytes) {
+            if (threadIdx.x < 2 * kBlock)
+                sscale = load<float>((threadIdx.x < kBlock ? a.c.ks : a.c.vs) + token +
+                                     (threadIdx.x & (kBlock - 1)));
+        }
+    };
+    auto stage = [&](int b, uint8_t* buf, float* scales) {
+        const int left = bad ? 0 : at.seq.len - b * kBlock;  // tokens of the block
+#pragma unroll
+        for (int x = 0; x < kStage; ++x) {
+            const int w = threadIdx.x + S::kThreads * x;
+            const int kr = w / kKeyWords, kc = w % kKeyWords;
+            const int vr = w / kValWords, vc = w % kValWords;
+            u32x4_t v = sv[x];
+            if (left < kBlock) v &= token_mask<kFmt>(left - vc * (16 / kCodeBytes<kFmt>));
+            if constexpr (kBytes) {
+                *reinterpret_cast<u32x4_t*>(buf + key_word<D>(kr, 2 * kc)) =
+                    codes_to_bf16<kFmt>(u32x2_t{sk[x][0], sk[x][1]});
+                *reinterpret_cast<u32x4_t*>(buf + key_word<D>(kr, 2 * kc + 1)) =
+                    codes_to_bf16<kFmt>(u32x2_t{sk[x][2], sk[x][3]});
+                *reinterpret_cast<u32x4_t*>(buf + S::kKeyBytes + val_word(vr, 2 * vc)) =
+                    codes_to_bf16<kFmt>(u32x2_t{v[0], v[1]});
+                *reinterpret_cast<u32x4_t*>(buf + S::kKeyBytes + val_word(vr, 2 * vc + 1)) =
+                    codes_to_bf16<kFmt>(u32x2_t{v[2], v[3]});
+            } else {
+                const u32x4_t not_a_number = {0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u};
+                *reinterpret_cast<u32x4_t*>(buf + key_word<D>(kr, kc)) = bad ? not_a_number : sk[x];
+                *reinterpret_cast<u32x4_t*>(buf + S::kKeyBytes + val_word(vr, vc)) = v;
+            }
+        }
+        if constexpr (kBytes) {
+            if (threadIdx.x < 2 * kBlock) scales[threadIdx.x] = bad ? nan() : sscale;
+        }
+        if (bad && a.status != nullptr && threadIdx.x == 0) atomicOr(a.status, ES_KV_BAD_PAGE);
+    };
+
+    float top = -inf(), sum = 0.0f;
+    f32x16_t o[kDims];
+#pragma unroll
+    for (int d = 0; d < kDims; ++d)
+#pragma unroll
+        for (int x = 0; x < 16; ++x) o[d][x] = 0.0f;
+
+    float* const scales0 = reinterpret_cast<float*>(lds + 2 * S::kBuffer);
+    // the key that row m of a tile of S^T stands for: bits 2 and 3 exchanged
+    const int krow = (n & 0x13) | ((n & 4) << 1) | ((n & 8) >> 1);
+
+    if (b_begin < b_end) {
+        fetch(b_begin);
+        stage(b_begin, lds, scales0);
+        __syncthreads();
+    }
+    for (int b = b_begin; b < b_end; ++b) {
+        const int cur = (b - b_begin) & 1;
+        uint8_t* const buf = lds + cur * S::kBuffer;
+        float* const scales = scales0 + cur * 128;
+        const bool more = b + 1 < b_end;
+        if (more) fetch(b + 1);
+        const int key0 = b * kBlock;
+        if (key0 < hi_any && key0 + kBlock > lo_any) {
+            f32x16_t s[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+#pragma unroll
+                for (int x = 0; x < 16; ++x) s[t][x] = 0.0f;
+#pragma unroll
+                for (int c = 0; c < kSteps; ++c) {
+                    const bf16x8_t k = *reinterpret_cast<const bf16x8_t*>(
+                        buf + key_word<D>(32 * t + krow, 2 * c + g));
+                    s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[c], s[t], 0, 0, 0);
+                }
+            }
+            // register x of tile t: key 32 t + 16 (x / 8) + 8 g + x % 8
+            f32x4_t kscale[2][4], vscale[2][4];
+            if constexpr (kBytes) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) {
+                        const int k = 32 * t + 16 * (y >> 1) + 8 * g + 4 * (y & 1);
+                        kscale[t][y] = *reinterpret_cast<const f32x4_t*>(scales + k);
+                        vscale[t][y] = *reinterpret_cast<const f32x4_t*>(scales + 64 + k);
+                    }
+            }
+            float peak = -inf();
+            const bool masked = key0 < lo_all || key0 + kBlock > hi_all;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int x = 0; x < 16; ++x) {
+                    const int key = key0 + 32 * t + 16 * (x >> 3) + 8 * g + (x & 7);
+                    s[t][x] = score<kPlain>(map, s[t][x], kBytes ? kscale[t][x >> 2][x & 3] : 1.0f,
+                                            pos - key);
+                }
+            if (masked) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) {
+                        const int key = key0 + 32 * t + 16 * (x >> 3) + 8 * g + (x & 7);
+                        if (key < first || key >= limit) s[t][x] = -inf();
+                    }
+            }
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int x = 0; x < 16; ++x) peak = __builtin_fmaxf(peak, s[t][x]);
+            peak = __builtin_fmaxf(peak, __shfl_xor(peak, 32));
+            const float now = __builtin_fmaxf(top, peak);
+            const float base = now == -inf() ? 0.0f : now;
+            if (__any(now > top)) {
+                const float shrink = __builtin_amdgcn_exp2f(top - base);
+                sum *= shrink;
+#pragma unroll
+                for (int d = 0; d < kDims; ++d) o[d] *= shrink;
+            }
+            top = now;
+            bf16x8_t p[4];
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    u32x4_t w;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        float e[2];
+#pragma unroll
+                        for (int y = 0; y < 2; ++y) {
+                            const int x = 8 * u + 2 * j + y;
+                            e[y] = __builtin_amdgcn_exp2f(s[t][x] - base);
+                            sum += e[y];
+                            if constexpr (kBytes)
+                                e[y] = e[y] == 0.0f ? 0.0f : e[y] * vscale[t][x >> 2][x & 3];
+                        }
+                        w[j] = pack_bf16(e[0], e[1]);
+                    }
+                    p[2 * t + u] = __builtin_bit_cast(bf16x8_t, w);
+                }
+#pragma unroll
+            for (int d = 0; d < kDims; ++d)
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const bf16x8_t v = *reinterpret_cast<const bf16x8_t*>(
+                        buf + S::kKeyBytes + val_word(32 * d + n, 2 * u + g));
+                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p[u], o[d], 0, 0, 0);
+                }
+        }
+        if (more) stage(b + 1, lds + (cur ^ 1) * S::kBuffer, scales0 + (cur ^ 1) * 128);
+        __syncthreads();
+    }
+
+    sum += __shfl_xor(sum, 32);
+    const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+    if (r >= n_rows) return;
+    uint16_t* out = a.out + uint64_t(at.seq.start + i) * a.out_stride + uint64_t(head) * D;
+#pragma unroll
+    for (int d = 0; d < kDims; ++d)
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+            u32x2_t w;
+            w = u32x2_t{pack_bf16(o[d][4 * y] * inv, o[d][4 * y + 1] * inv),
+                          pack_bf16(o[d][4 * y + 2] * inv, o[d][4 * y + 3] * inv)};
+            store_row4(out + 32 * d + 8 * y + 4 * g, w);
+        }
+}
+
+}  // namespace eskv

@@ -68,6 +68,29 @@ class EsUpdateOpts(ctypes.Structure):
                 ("round_seed", _u64)]
 
 
+class EsKvDesc(ctypes.Structure):
+    _fields_ = [("k_pages", _vp), ("v_pages", _vp), ("k_scales", _vp), ("v_scales", _vp),
+                ("n_pages", _u32), ("page", _u32), ("kv_heads", _u32), ("head_dim", _u32),
+                ("format", _u32), ("reserved", _u32)]
+
+
+class EsKvAppend(ctypes.Structure):
+    _fields_ = [("q", _vp), ("k", _vp), ("v", _vp), ("q_out", _vp),
+                ("q_stride", _u64), ("k_stride", _u64), ("v_stride", _u64),
+                ("q_out_stride", _u64), ("q_gain", _vp), ("k_gain", _vp), ("rope", _vp),
+                ("positions", _vp), ("slots", _vp), ("status", _vp), ("tokens", _u32),
+                ("q_heads", _u32), ("rot", _u32), ("rope_rows", _u32), ("eps", _f32),
+                ("flags", _u32)]
+
+
+class EsKvAttend(ctypes.Structure):
+    _fields_ = [("q", _vp), ("out", _vp), ("q_stride", _u64), ("out_stride", _u64),
+                ("tables", _vp), ("lengths", _vp), ("starts", _vp), ("first", _vp),
+                ("limit", _vp), ("slopes", _vp), ("status", _vp), ("rows", _u32),
+                ("n_seqs", _u32), ("table_stride", _u32), ("q_heads", _u32),
+                ("max_rows", _u32), ("max_length", _u32), ("scale", _f32), ("cap", _f32)]
+
+
 SIGNATURES = {
     "es_plan_create": (ctypes.c_int, [ctypes.POINTER(EsTensor), _u32, ctypes.POINTER(_vp)]),
     "es_plan_create_blocks": (ctypes.c_int, [ctypes.POINTER(EsBlock), _u32,
@@ -114,6 +137,12 @@ SIGNATURES = {
     "es_normals": (ctypes.c_int, [_u64, _u32, _u64, _u64, _vp, _vp]),
     "es_tile_layout": (ctypes.c_int, [_u64, _u64, _u32, ctypes.POINTER(EsTileInfo), _u64,
                                       ctypes.POINTER(_u64)]),
+    "es_kv_create": (ctypes.c_int, [ctypes.POINTER(EsKvDesc), ctypes.POINTER(_vp)]),
+    "es_kv_destroy": (ctypes.c_int, [_vp]),
+    "es_kv_device_bytes": (_u64, [_vp]),
+    "es_kv_append": (ctypes.c_int, [_vp, ctypes.POINTER(EsKvAppend), _vp]),
+    "es_kv_read": (ctypes.c_int, [_vp, _vp, _u32, _vp, _u64, _vp, _u64, _vp, _vp]),
+    "es_kv_attend": (ctypes.c_int, [_vp, ctypes.POINTER(EsKvAttend), _vp]),
     "es_strerror": (ctypes.c_char_p, [ctypes.c_int]),
     "es_last_error": (ctypes.c_char_p, []),
 }

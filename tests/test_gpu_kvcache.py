@@ -1,0 +1,678 @@
+"""The paged cache and the attention over it (es_kv_*), against the fp64 oracle.
+
+Tolerances are the kernels' roundings.  bf16 has 8 significant bits: rounding to
+nearest is off by at most U = 2^-8 of the value (1 + 2^-8, halfway between
+neighbours, attains it).  Queries: one rounding of a binary32 result.  Stored
+rows: half a step of their format, and the read's rounding to bf16.  Attention:
+one rounding of the output (U of it) and one of each weight (U sum p |v|), and
+the binary32 errors of scores and sums (a 64th of U, and a few units of the
+largest score's last place).
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import attention as oa
+from paper_2608_17310_amd import esopt
+from paper_2608_17310_amd import kvcache as kvc
+from paper_2608_17310_amd.kvcache import KVCache
+
+pytestmark = pytest.mark.gpu
+
+FORMATS = ["bf16", "int8", "e4m3"]
+EPS = 1e-6
+U = 2.0 ** -8
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    torch.cuda.set_device(0)
+
+
+def f64(t):
+    return t.detach().float().cpu().numpy().astype(np.float64)
+
+
+def dev(x, dtype):
+    return torch.from_numpy(np.asarray(x)).to(dtype).cuda()
+
+
+def rows(rng, *shape, std=1.0):
+    return torch.from_numpy((rng.standard_normal(shape) * std).astype(np.float32)).to(torch.bfloat16).cuda()
+
+
+def rope_table(n, rot):
+    angle = np.arange(n)[:, None] * 10000.0 ** (-np.arange(rot // 2) * 2.0 / rot)
+    return dev(np.concatenate([np.cos(angle), np.sin(angle)], 1).astype(np.float32), torch.float32)
+
+
+def step_of(x, form):
+    """Half the distance of stored values around x (rows), with the read's
+    rounding to bf16 and binary32's in norm, rotation and scale."""
+    x = np.abs(x)
+    top = x.max(axis=-1, keepdims=True)
+    half = {"bf16": np.zeros_like(x), "int8": np.broadcast_to(top / 254, x.shape),
+            # a value next to a binade's edge may be rounded in the coarser one
+            "e4m3": np.maximum(x / 16 * (1 + 1e-4), top / 448 * 2.0 ** -10)}[form]
+    return half * (1 + 1e-4) + (x + half) * (U + 2.0 ** -20) + top * 2.0 ** -20
+
+
+def shuffled_slots(rng, n, page, pages):
+    """Slots of a sequence of n tokens over shuffled pages, from its start."""
+    order = rng.permutation(pages)
+    i = np.arange(n)
+    return order[i // page] * page + i % page
+
+
+# ------------------------------------------------------------ append, read --
+
+@pytest.mark.parametrize("form", FORMATS)
+@pytest.mark.parametrize("dim,q_heads,kv_heads", [(128, 10, 2), (64, 3, 3), (256, 8, 1)])
+@pytest.mark.parametrize("tokens", [1, 5, 63, 64, 65, 200])
+def test_append_and_read(form, dim, q_heads, kv_heads, tokens):
+    rng = np.random.default_rng([dim, tokens, FORMATS.index(form)])
+    page = int(rng.choice([64, 128, 1024]))
+    at = int(rng.integers(0, 40))                         # the tokens start inside a page
+    cache = KVCache.allocate(-(-(tokens + at) // page) + 1, kv_heads, dim, form, page)
+    rot, adjacent = int(rng.choice([dim, dim // 2, 16])), bool(rng.integers(2))
+    table = rope_table(500, rot)
+    pos = rng.integers(0, 500, tokens)
+    packed = rows(rng, tokens, (q_heads + 2 * kv_heads) * dim + 24, std=2.0)
+    q = packed[:, 8:8 + q_heads * dim].view(tokens, q_heads, dim)
+    k = packed[:, 8 + q_heads * dim:][:, :kv_heads * dim].view(tokens, kv_heads, dim)
+    v = packed[:, 13 + (q_heads + kv_heads) * dim:][:, :kv_heads * dim].view(tokens, kv_heads, dim)
+    gq, gk = rows(rng, dim), rows(rng, dim)
+    slots = shuffled_slots(rng, tokens + at, page, cache.pages)[at:]
+    got = cache.append(k, v, dev(slots, torch.int64), q=q, q_gain=gq, k_gain=gk, eps=EPS,
+                       rope=table, positions=dev(pos, torch.int32), adjacent=adjacent)
+    rk, rv = cache.read(dev(slots, torch.int64))
+    turn = f64(table)[pos]
+    want = oa.norm_rotate(f64(q), f64(gq), EPS, turn, adjacent)
+    top = np.abs(want).max(axis=-1, keepdims=True)
+    assert np.all(np.abs(f64(got) - want) <= np.abs(want) * (U + 2.0 ** -20) + top * 2.0 ** -20)
+    want = oa.norm_rotate(f64(k), f64(gk), EPS, turn, adjacent)
+    assert np.all(np.abs(f64(rk) - want) <= step_of(want, form))
+    assert np.all(np.abs(f64(rv) - f64(v)) <= step_of(f64(v), form))
+    # no other slot was written
+    taken = np.zeros(cache.pages * page, bool)
+    taken[slots] = True
+    free = np.flatnonzero(~taken)
+    raw = cache.k_pages.view(torch.uint8).view(cache.pages, kv_heads, page, -1).cpu().numpy()
+    assert not raw.transpose(0, 2, 1, 3).reshape(len(taken), -1)[free].any()
+    rv_all = cache.v_pages.view(torch.int16 if form == "bf16" else torch.uint8).cpu().numpy()
+    assert not rv_all.transpose(0, 3, 1, 2).reshape(len(taken), -1)[free].any()
+
+
+@pytest.mark.parametrize("form", ["int8", "e4m3"])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_codes_and_scales_bit_for_bit(form, dim):
+    """Without norm and rotation the stored bits follow from the definition in
+    binary32 exactly: bf16 rows of every magnitude, ties, zeros, tiny rows."""
+    rng = np.random.default_rng([7, dim])
+    tokens, heads, page = 150, 3, 64
+    k = rng.standard_normal((tokens, heads, dim)) * np.exp2(rng.integers(-130, 120, (tokens, heads, 1)))
+    k[3] = 0
+    k[4, :, 1:] = 0
+    k[5] = 2.0 ** -101                                     # below the smallest row that is kept
+    k[6] = 2.0 ** -100
+    k[7] = rng.integers(-127, 128, (heads, dim)) * 0.5     # ties of int8 when the top is 127
+    k[7, :, 0] = 127
+    k[8] = 0
+    k[8, :, 0] = 3.3e38
+    k = torch.from_numpy(k.astype(np.float32)).to(torch.bfloat16).cuda()
+    v = k.flip(0).contiguous()
+    cache = KVCache.allocate(4, heads, dim, form, page)
+    slots = rng.permutation(4 * page)[:tokens]
+    cache.append(k, v, dev(slots, torch.int64))
+    for x, name in ((k, "k"), (v, "v")):
+        codes, scale = oa.quantise_f32(f64(x).astype(np.float32), form)
+        raw = (cache.k_pages if name == "k" else cache.v_pages.view(torch.uint8).transpose(2, 3)
+               .contiguous()).view(torch.uint8).cpu().numpy()
+        raw = raw.transpose(0, 2, 1, 3).reshape(4 * page, heads, dim)[slots]
+        if form == "e4m3":                                 # a zero keeps its sign
+            raw = np.where(raw == 0x80, 0, raw)
+        np.testing.assert_array_equal(raw, codes.view(np.uint8))
+        s = (cache.k_scales if name == "k" else cache.v_scales).cpu().numpy()
+        s = s.transpose(0, 2, 1).reshape(4 * page, heads)[slots]
+        np.testing.assert_array_equal(s, scale)
+    rk, rv = cache.read(dev(slots, torch.int64))
+    for x, got in ((k, rk), (v, rv)):
+        want = oa.code_values(*oa.quantise_f32(f64(x).astype(np.float32), form), form)
+        # code times scale rounds to binary32 and then to bf16
+        want = torch.from_numpy(want.astype(np.float32)).to(torch.bfloat16)
+        np.testing.assert_array_equal(f64(got), f64(want))
+
+
+@pytest.mark.parametrize("form", FORMATS)
+def test_void_tokens_and_negative_slots(form):
+    """A token with an infinity or a NaN in its key or value reads as NaN in
+    that head alone; a negative slot stores nothing and reads as zeros."""
+    rng = np.random.default_rng(8)
+    tokens, heads, dim = 70, 2, 128
+    k, v = rows(rng, tokens, heads, dim), rows(rng, tokens, heads, dim)
+    k[3, 0, 5] = float("inf")
+    k[9, 1, 127] = float("nan")
+    v[9, 0, 64] = float("-inf")
+    v[40, 1, 0] = float("nan")
+    slots = np.arange(tokens) + 3
+    slots[50:53] = -1
+    cache = KVCache.allocate(3, heads, dim, form, 64)
+    s = dev(slots, torch.int64)
+    cache.append(k, v, s, k_gain=torch.ones(dim, dtype=torch.bfloat16, device="cuda"))
+    rk, rv = (f64(t) for t in cache.read(s))
+    dead = np.zeros((tokens, heads), bool)
+    for t, h in ((3, 0), (9, 1), (9, 0), (40, 1)):
+        dead[t, h] = True
+    assert np.isnan(rk[dead]).all() and np.isnan(rv[dead]).all()
+    assert np.isfinite(rk[~dead]).all() and np.isfinite(rv[~dead]).all()
+    assert not rk[50:53].any() and not rv[50:53].any()
+    stored = cache.v_pages.float()
+    assert torch.isfinite(stored).all()                    # values in the cache are always finite
+
+
+@pytest.mark.parametrize("form", FORMATS)
+def test_norm_of_very_large_and_small_rows(form):
+    """Squares of bf16 values leave binary32's range; their norms do not."""
+    tokens, dim = 6, 128
+    rng = np.random.default_rng(9)
+    base = rng.standard_normal((tokens, 1, dim))
+    scale = np.array([2.0 ** 100, 2.0 ** 64, 2.0 ** 55, 1.0, 2.0 ** -60, 2.0 ** -20])
+    k = torch.from_numpy((base * scale[:, None, None]).astype(np.float32)).to(torch.bfloat16).cuda()
+    gain = torch.ones(dim, dtype=torch.bfloat16, device="cuda")
+    cache = KVCache.allocate(1, 1, dim, form, 64)
+    slots = dev(np.arange(tokens), torch.int64)
+    q = cache.append(k, k.clone(), slots, q=k, q_gain=gain, k_gain=gain)
+    want = oa.norm_rotate(f64(k), np.ones(dim), EPS)
+    top = np.abs(want).max(axis=-1, keepdims=True)
+    assert np.all(np.abs(f64(q) - want) <= np.abs(want) * (U + 2.0 ** -20) + top * 2.0 ** -20)
+    rk, _ = cache.read(slots)
+    assert np.all(np.abs(f64(rk) - want) <= step_of(want, form))
+
+
+def test_in_place_queries_and_a_broadcast_input():
+    rng = np.random.default_rng(10)
+    tokens, dim = 33, 64
+    packed = rows(rng, tokens, 6 * dim)
+    q = packed[:, :4 * dim].view(tokens, 4, dim)
+    k = rows(rng, 1, 1, dim).expand(tokens, 1, dim)        # stride 0: one key for all
+    v = packed[:, 5 * dim:].view(tokens, 1, dim)
+    gain = rows(rng, dim)
+    want = oa.norm_rotate(f64(q), f64(gain), EPS)
+    rest = packed[:, 4 * dim:].clone()
+    cache = KVCache.allocate(1, 1, dim, "bf16", 64)
+    slots = dev(np.arange(tokens), torch.int64)
+    out = cache.append(k, v, slots, q=q, q_out=q, q_gain=gain)
+    assert out is q and torch.equal(packed[:, 4 * dim:], rest)
+    assert np.all(np.abs(f64(q) - want) <= np.abs(want) * (U + 2.0 ** -18) + 1e-6)
+    rk, rv = cache.read(slots)
+    assert torch.equal(rk, k.contiguous()) and torch.equal(rv, v.contiguous())
+
+
+@pytest.mark.parametrize("form", FORMATS)
+def test_a_token_is_stored_the_same_alone_and_in_a_batch(form):
+    rng = np.random.default_rng(11)
+    tokens, heads, dim = 131, 2, 128
+    k, v, q = (rows(rng, tokens, heads, dim) for _ in range(3))
+    gain = rows(rng, dim)
+    table, pos = rope_table(tokens, dim), dev(np.arange(tokens), torch.int32)
+    slots = dev(rng.permutation(192)[:tokens], torch.int64)
+    a, b = (KVCache.allocate(3, heads, dim, form, 64) for _ in range(2))
+    qa = a.append(k, v, slots, q=q, q_gain=gain, k_gain=gain, rope=table, positions=pos)
+    qb = torch.empty_like(qa)
+    for t in range(tokens):
+        s = slice(t, t + 1)
+        b.append(k[s], v[s], slots[s], q=q[s], q_out=qb[s], q_gain=gain, k_gain=gain, rope=table,
+                 positions=pos[s])
+    assert torch.equal(qa, qb)
+    for x, y in ((a.k_pages, b.k_pages), (a.v_pages, b.v_pages)):
+        assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+    if form != "bf16":
+        assert torch.equal(a.k_scales, b.k_scales) and torch.equal(a.v_scales, b.v_scales)
+
+
+def test_slots_and_positions_out_of_range_are_reported():
+    rng = np.random.default_rng(12)
+    dim = 64
+    cache = KVCache.allocate(2, 1, dim, "int8", 64)
+    k, v, q = (rows(rng, 5, 1, dim) for _ in range(3))
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    table = rope_table(10, dim)
+    good = dev([0, 1, 2, 3, 4], torch.int64)
+    out = cache.append(k, v, good, q=q, rope=table, positions=dev([0, 9, 3, 4, 5], torch.int32),
+                       status=status)
+    assert status.item() == 0 and torch.isfinite(out.float()).all()
+    out = cache.append(k, v, good, q=q, rope=table, positions=dev([0, 10, 3, -1, 5], torch.int32),
+                       status=status)
+    assert status.item() == kvc.ES_KV_BAD_POSITION
+    bad = torch.isnan(out.float()).all(-1).flatten().cpu().tolist()
+    assert bad == [False, True, False, True, False]
+    rk, rv = cache.read(good)
+    assert torch.isnan(rk.float()).all(-1).flatten().cpu().tolist() == bad
+    assert torch.isnan(rv.float()).all(-1).flatten().cpu().tolist() == bad
+    status.zero_()
+    before = [t.clone() for t in (cache.k_scales, cache.v_scales)]
+    wild = dev([128, 1 << 40, (1 << 62), 127, -(1 << 62)], torch.int64)
+    cache.append(k, v, wild, status=status)
+    assert status.item() == kvc.ES_KV_BAD_SLOT
+    for x, y in zip(before, (cache.k_scales, cache.v_scales)):
+        x[1, 0, 63] = y[1, 0, 63]                          # slot 127 alone was written
+        assert torch.equal(x.view(torch.int32), y.view(torch.int32))
+    status.zero_()
+    rk, rv = cache.read(wild, status=status)
+    assert status.item() == kvc.ES_KV_BAD_SLOT
+    assert torch.isnan(rk.float()[:3]).all() and torch.isnan(rv.float()[:3]).all()
+    assert torch.isfinite(rk.float()[3:]).all() and not rk[4].any()
+
+
+# ------------------------------------------------------------------ attend --
+
+class Batch:
+    """Sequences with random cached rows: pages shuffled, slots past each
+    length and pages of no sequence filled with not-a-number bits."""
+
+    def __init__(self, rng, form, dim, group, kv_heads, page, lengths, rows_of, std=1.0):
+        self.form, self.dim, self.group, self.heads, self.page = form, dim, group, kv_heads, page
+        self.lengths, self.rows_of = lengths, rows_of
+        need = [max(1, -(-n // page)) for n in lengths]
+        pages = sum(need) + 2
+        order = rng.permutation(pages)
+        self.table = np.full((len(lengths), max(need) + 1), -7, np.int32)   # unused entries: no page
+        self.cache = KVCache.allocate(pages, kv_heads, dim, form, page)
+        fill = 0x7F if form != "int8" else 0x55
+        for t in (self.cache.k_pages, self.cache.v_pages):
+            t.view(torch.uint8).fill_(fill if form != "bf16" else 0x7F)
+            if form == "bf16":
+                t.view(torch.int16).fill_(0x7FC1)
+        if form != "bf16":
+            self.cache.k_scales.fill_(float("nan"))
+            self.cache.v_scales.fill_(float("inf"))
+        self.k, self.v = [], []
+        at = 0
+        for s, n in enumerate(lengths):
+            self.table[s, :need[s]] = order[at:at + need[s]]
+            at += need[s]
+            k, v = rows(rng, n, kv_heads, dim, std=std), rows(rng, n, kv_heads, dim)
+            i = np.arange(n)
+            slots = dev(self.table[s, i // page].astype(np.int64) * page + i % page, torch.int64)
+            self.cache.append(k, v, slots)
+            if form == "bf16":
+                self.k.append(f64(k))
+                self.v.append(f64(v))
+            else:
+                raw = [t.cpu().numpy() for t in (self.cache.k_pages.view(torch.uint8),
+                                                 self.cache.v_pages.view(torch.uint8))]
+                sl = slots.cpu().numpy()
+                kc = raw[0].transpose(0, 2, 1, 3).reshape(-1, kv_heads, dim)[sl]
+                vc = raw[1].transpose(0, 3, 1, 2).reshape(-1, kv_heads, dim)[sl]
+                ks, vs = (t.cpu().numpy().transpose(0, 2, 1).reshape(-1, kv_heads)[sl]
+                          for t in (self.cache.k_scales, self.cache.v_scales))
+                self.k.append(oa.code_values(kc, ks, form))
+                self.v.append(oa.code_values(vc, vs, form))
+        self.starts = np.concatenate([[0], np.cumsum(rows_of)]).astype(np.int32)
+        self.q = rows(rng, int(self.starts[-1]), group * kv_heads, dim, std=std)
+
+    def args(self):
+        return (dev(self.table, torch.int32), dev(np.array(self.lengths), torch.int32),
+                dev(self.starts, torch.int32))
+
+    def attend(self, **kw):
+        for name in ("first", "limit"):
+            if kw.get(name) is not None:
+                kw[name] = dev(np.asarray(kw[name]), torch.int32)
+        if kw.get("slopes") is not None:
+            kw["slopes"] = dev(np.asarray(kw["slopes"], np.float32), torch.float32)
+        kw.setdefault("max_rows", max(self.rows_of))
+        kw.setdefault("max_length", max(self.lengths))
+        return self.cache.attend(self.q, *self.args(), **kw)
+
+    def check(self, got, first=None, limit=None, scale=None, cap=0.0, slopes=None):
+        got, q = f64(got), f64(self.q)
+        for s, n in enumerate(self.rows_of):
+            r = slice(int(self.starts[s]), int(self.starts[s + 1]))
+            if n == 0:
+                continue
+            want, spread = oa.attend(
+                q[r], self.k[s], self.v[s], self.dim ** -0.5 if scale is None else scale, cap,
+                slopes, None if first is None else first[r], None if limit is None else limit[r])
+            # scores are products and sums in binary32: relative errors of the
+            # weights up to a few units of the largest score's last place
+            j = np.arange(q.shape[1]) // self.group
+            size = np.linalg.norm(q[r], axis=-1) * np.linalg.norm(self.k[s], axis=-1).max(
+                axis=0, initial=0.0)[j]
+            size = size * abs(self.dim ** -0.5 if scale is None else scale)
+            bound = U * np.abs(want) + (U * (1 + 2.0 ** -6) + 2.0 ** -21 * size[..., None]) * spread
+            off = np.abs(got[r] - want)
+            assert np.all(off <= bound), (s, n, self.lengths[s], float(np.max(off - bound)),
+                                          np.argwhere(~(off <= bound))[:4])
+
+
+@pytest.mark.parametrize("form", FORMATS)
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("group,kv_heads", [(1, 3), (5, 2), (16, 1), (17, 1)])
+def test_steps(form, dim, group, kv_heads):
+    """One row of each sequence, lengths from one token to several parts."""
+    rng = np.random.default_rng([dim, group, FORMATS.index(form)])
+    b = Batch(rng, form, dim, group, kv_heads, 64, [1, 2, 63, 64, 65, 257, 1000, 0, 3000],
+              [1, 1, 1, 1, 1, 1, 1, 0, 1])
+    b.check(b.attend())
+
+
+@pytest.mark.parametrize("form", FORMATS)
+@pytest.mark.parametrize("dim,group,kv_heads", [(64, 2, 2), (128, 5, 2), (256, 4, 1)])
+def test_few_rows_of_long_histories(form, dim, group, kv_heads):
+    rng = np.random.default_rng([dim, group, 3])
+    b = Batch(rng, form, dim, group, kv_heads, 128, [5000, 3, 129, 700, 8], [3, 2, 5, 1, 4])
+    slopes = 2.0 ** -rng.integers(1, 9, group * kv_heads)
+    b.check(b.attend(slopes=slopes, cap=5.0), slopes=slopes, cap=5.0)
+
+
+@pytest.mark.parametrize("form", FORMATS)
+@pytest.mark.parametrize("dim,group,kv_heads,page", [(64, 1, 3, 64), (128, 5, 2, 128), (256, 4, 1, 256),
+                                                     (128, 1, 2, 1024), (64, 7, 1, 64)])
+def test_prompts(form, dim, group, kv_heads, page):
+    """Whole prompts and prompts behind a history, ragged, plain and with
+    every change of the scores."""
+    rng = np.random.default_rng([dim, group, page])
+    b = Batch(rng, form, dim, group, kv_heads, page, [300, 65, 1, 700, 64, 130],
+              [300, 65, 1, 200, 64, 129], std=1.5)
+    b.check(b.attend())
+    slopes = 2.0 ** -rng.integers(0, 6, group * kv_heads)
+    b.check(b.attend(slopes=slopes, cap=3.0, scale=0.2), slopes=slopes, cap=3.0, scale=0.2)
+
+
+@pytest.mark.parametrize("form", FORMATS)
+@pytest.mark.parametrize("n", [1, 4, 300])
+def test_intervals(form, n):
+    """Documents, prefixes, windows, keys ahead of the row, intervals past the
+    end, and rows that see nothing, alone and beside rows that see something."""
+    rng = np.random.default_rng([13, n])
+    b = Batch(rng, form, 128, 4, 2, 64, [900, 400, 301], [n, n, n])
+    total = 3 * n
+    for kind in range(6):
+        pos = np.concatenate([np.arange(m - n, m) for m in b.lengths])
+        if kind == 0:                                      # packed documents
+            first, limit = pos // 97 * 97, pos + 1
+        elif kind == 1:                                    # a prefix, and keys ahead of the row
+            first, limit = None, np.maximum(pos + 1, 250)
+        elif kind == 2:                                    # a window
+            first, limit = np.maximum(0, pos - 70), None
+        elif kind == 3:                                    # anything, empty ones among them
+            first = rng.integers(-5, 950, total)
+            limit = rng.integers(-5, 950, total)
+        elif kind == 4:                                    # nothing at all
+            first, limit = np.full(total, 10), np.full(total, 10)
+        else:                                              # beyond the end; lowest and highest
+            first = np.full(total, -(1 << 31))
+            limit = np.full(total, (1 << 31) - 1)
+        cap = 4.0 if kind % 2 else 0.0
+        got = b.attend(first=first, limit=limit, cap=cap)
+        b.check(got, first=first, limit=limit, cap=cap)
+        if kind == 4:
+            assert not got.any()
+
+
+@pytest.mark.parametrize("form", FORMATS)
+@pytest.mark.parametrize("n", [1, 3, 200])
+def test_void_tokens_reach_only_rows_that_see_them(form, n):
+    rng = np.random.default_rng([14, n])
+    b = Batch(rng, form, 128, 2, 2, 64, [500], [n])
+    clean = b.attend(first=np.full(n, 301), limit=np.full(n, 400))
+    # token 300 of head 0 and token 420 of head 1 are void now
+    k, v = rows(rng, 2, 2, 128), rows(rng, 2, 2, 128)
+    k[0, 0, 3] = float("nan")
+    v[1, 1, 7] = float("inf")
+    at = np.array([300, 420])
+    slots = b.table[0, at // 64].astype(np.int64) * 64 + at % 64
+    b.cache.append(k, v, dev(slots, torch.int64))
+    assert torch.equal(b.attend(first=np.full(n, 301), limit=np.full(n, 400)), clean)
+    first, limit = np.full(n, 301), np.full(n, 400)
+    first[n // 2] = 300                                    # this row sees the one,
+    limit[n - 1] = 421                                     # and this the other
+    got = b.attend(first=first, limit=limit)
+    nan = torch.isnan(got.float()).all(-1).cpu().numpy()   # [rows, query heads]
+    want = np.zeros((n, 4), bool)
+    want[n // 2, :2] = True
+    want[n - 1, 2:] = True
+    np.testing.assert_array_equal(nan, want)
+    same = torch.ones(n, dtype=torch.bool, device="cuda")
+    same[n // 2] = same[n - 1] = False                     # these see one key more, or 21
+    assert torch.equal(got[same], clean[same])
+
+
+def test_large_scores_and_infinite_ones():
+    """Scores far beyond the exponential's range, and -inf through an infinite
+    bias: weights of the rest are exact, nothing overflows."""
+    rng = np.random.default_rng(15)
+    for n in (1, 150):
+        b = Batch(rng, "bf16", 64, 2, 1, 64, [400], [n], std=30.0)
+        b.check(b.attend(scale=3.0), scale=3.0)
+        b.check(b.attend(scale=-3.0), scale=-3.0)
+        b.check(b.attend(scale=0.0), scale=0.0)
+        slopes = np.array([1e30, 0.0])
+        b.check(b.attend(slopes=slopes), slopes=slopes)
+        b.check(b.attend(cap=1e-3), cap=1e-3)
+        b.check(b.attend(cap=1e6), cap=1e6)
+
+
+@pytest.mark.parametrize("n", [1, 2, 100])
+def test_many_sequences(n):
+    """More sequences than a wave scans at once, some without rows."""
+    rng = np.random.default_rng([16, n])
+    lengths = [int(x) for x in rng.integers(n, 400, 150)]
+    rows_of = [n if i % 7 else 0 for i in range(150)]
+    b = Batch(rng, "e4m3", 64, 3, 1, 64, lengths, rows_of)
+    b.check(b.attend())
+    first = rng.integers(0, 300, sum(rows_of))
+    b.check(b.attend(first=first), first=first)
+
+
+def test_hints_choose_launches_not_results():
+    """Whatever the caller expects, every row is computed."""
+    rng = np.random.default_rng(17)
+    b = Batch(rng, "int8", 128, 5, 2, 64, [900, 70, 2000], [90, 70, 1])
+    for max_rows, max_length in ((1, 1), (90, 2000), (1, 1 << 20), (1 << 20, 1), (13, 2000)):
+        b.check(b.attend(max_rows=max_rows, max_length=max_length))
+
+
+def test_strided_rows_and_untouched_ones():
+    rng = np.random.default_rng(18)
+    for n in (2, 120):
+        b = Batch(rng, "bf16", 64, 2, 2, 64, [200, 150], [n, n])
+        want = b.attend()
+        wide = torch.zeros(2 * n, 4 * 64 + 5, dtype=torch.bfloat16, device="cuda")
+        qs = wide[:, 3:3 + 4 * 64].view(2 * n, 4, 64)
+        qs.copy_(b.q)
+        out = torch.full((2 * n + 3, 4 * 64 + 1), 7.0, dtype=torch.bfloat16, device="cuda")
+        view = out[:2 * n, 1:].view(2 * n, 4, 64)
+        b.q = qs
+        b.attend(out=view)
+        assert torch.equal(view, want)
+        assert (out[2 * n:] == 7).all() and (out[:, 0] == 7).all()
+        # rows of no sequence are not written
+        t, l, s = b.args()
+        more = torch.full((2 * n + 3, 4, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+        q = torch.cat([b.q, b.q[:2], b.q[:1]])
+        b.cache.attend(q, t, l, s, max_rows=n, max_length=200, out=more)
+        assert torch.equal(more[:2 * n], want) and (more[2 * n:] == 7).all()
+
+
+@pytest.mark.parametrize("n", [1, 200])
+def test_pages_lengths_and_starts_out_of_range(n):
+    rng = np.random.default_rng([19, n])
+    b = Batch(rng, "e4m3", 128, 2, 1, 64, [300, 300], [n, n])
+    want = b.attend()
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    b.attend(status=status)
+    assert status.item() == 0
+    for entry in (-1, b.cache.pages, (1 << 31) - 1):
+        t, l, s = b.args()
+        t[1, 1] = entry                                    # keys 64 .. 127 of the second sequence
+        got = b.cache.attend(b.q, t, l, s, max_rows=n, max_length=300, status=status)
+        assert status.item() == kvc.ES_KV_BAD_PAGE
+        status.zero_()
+        assert torch.equal(got[:n], want[:n])
+        pos = np.arange(300 - n, 300)
+        hit = torch.from_numpy(pos >= 64).cuda()
+        assert torch.isnan(got[n:][hit].float()).all() and torch.equal(got[n:][~hit], want[n:][~hit])
+    # a length beyond the table is the table's
+    t, l, s = b.args()
+    t, l = t[:, :2].contiguous(), l.clone()
+    l[0] = 1 << 30
+    got = b.cache.attend(b.q, t, l, s, max_rows=n, max_length=300, status=status)
+    assert status.item() & kvc.ES_KV_BAD_LENGTH
+    l[0], l[1] = -5, -(1 << 31)
+    status.zero_()
+    got = b.cache.attend(b.q, t, l, s, max_rows=n, max_length=300, status=status)
+    assert status.item() == kvc.ES_KV_BAD_LENGTH and not got.any()
+    # starts out of order or out of the rows: what they leave is computed, the rest untouched
+    status.zero_()
+    t, l, _ = b.args()
+    out = torch.full_like(want, 7.0)
+    b.cache.attend(b.q, t, l, dev([-3, n, 1 << 30], torch.int32), max_rows=n, max_length=300,
+                   status=status, out=out)
+    assert status.item() == kvc.ES_KV_BAD_LENGTH and torch.equal(out, want)
+
+
+def test_deterministic_and_on_another_stream():
+    rng = np.random.default_rng(20)
+    for n, lengths in ((1, [5000, 300, 40]), (130, [700, 300, 130])):
+        b = Batch(rng, "int8", 128, 4, 2, 64, lengths, [n] * 3)
+        want = b.attend()
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        for _ in range(5):
+            assert torch.equal(b.attend(), want)
+            with torch.cuda.stream(side):
+                got = b.attend()
+            side.synchronize()
+            assert torch.equal(got, want)
+        args = b.args()
+        torch.cuda.synchronize()
+        out = torch.empty_like(want)
+        b.cache.attend(b.q, *args, max_rows=n, max_length=max(lengths), out=out, stream=side)
+        side.synchronize()
+        assert torch.equal(out, want)
+
+
+def test_offsets_beyond_32_bits():
+    """Pages whose elements and bytes lie past 2^32 of the pool."""
+    heads, dim, page = 8, 128, 64
+    pages = (9 << 30) // (heads * dim * page * 2)           # 9 GB of keys, and of values
+    k = torch.empty(pages, heads, page, dim, dtype=torch.bfloat16, device="cuda")
+    v = torch.empty(pages, heads, dim, page, dtype=torch.bfloat16, device="cuda")
+    cache = KVCache(k, v)
+    rng = np.random.default_rng(21)
+    n = 200
+    table = np.array([[pages - 1, 0, pages - 2, pages // 2 + 1]], np.int32)
+    ks, vs = rows(rng, n, heads, dim), rows(rng, n, heads, dim)
+    i = np.arange(n)
+    slots = dev(table[0, i // page].astype(np.int64) * page + i % page, torch.int64)
+    cache.append(ks, vs, slots)
+    rk, rv = cache.read(slots)
+    assert torch.equal(rk, ks) and torch.equal(rv, vs)
+    for m in (1, n):
+        q = rows(rng, m, heads, dim)
+        got = cache.attend(q, dev(table, torch.int32), dev([n], torch.int32), dev([0, m], torch.int32))
+        want, spread = oa.attend(f64(q), f64(ks), f64(vs), dim ** -0.5)
+        assert np.all(np.abs(f64(got) - want) <= U * np.abs(want) + (U * (1 + 2.0 ** -6) + 2.0 ** -16) * spread)
+    cache.close()
+    del k, v, cache
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("form", FORMATS)
+def test_a_captured_step_replays_while_histories_grow(form):
+    """Lengths, tables and slots live on the GPU: one captured step (append,
+    attend) serves every later token."""
+    rng = np.random.default_rng(22)
+    heads, group, dim, page, seqs = 2, 4, 128, 64, 3
+    cache, twin = (KVCache.allocate(30, heads, dim, form, page) for _ in range(2))
+    table = dev(rng.permutation(30)[:24].reshape(3, 8), torch.int32)
+    lengths = np.array([60, 5, 130])
+    for s in range(seqs):
+        n = int(lengths[s])
+        i = np.arange(n)
+        slots = dev(table[s].cpu().numpy()[i // page].astype(np.int64) * page + i % page, torch.int64)
+        k, v = rows(rng, n, heads, dim), rows(rng, n, heads, dim)
+        for c in (cache, twin):
+            c.append(k, v, slots)
+    q, k, v = (rows(rng, seqs, h, dim) for h in (heads * group, heads, heads))
+    gain = rows(rng, dim)
+    rope = rope_table(400, dim)
+    length_d, pos_d = dev(lengths + 1, torch.int32), dev(lengths, torch.int32)
+    slots_d = torch.zeros(seqs, dtype=torch.int64, device="cuda")
+    starts = dev(np.arange(seqs + 1), torch.int32)
+    out = torch.empty(seqs, heads * group, dim, dtype=torch.bfloat16, device="cuda")
+    qn = torch.empty_like(out)
+
+    def step(c, out, qn):
+        c.append(k, v, slots_d, q=q, q_out=qn, q_gain=gain, k_gain=gain, rope=rope, positions=pos_d)
+        c.attend(qn, table, length_d, starts, max_rows=1, max_length=512, out=out)
+
+    def place(lengths):
+        p = table.cpu().numpy()[np.arange(seqs), lengths // page].astype(np.int64)
+        slots_d.copy_(dev(p * page + lengths % page, torch.int64))
+        length_d.copy_(dev(lengths + 1, torch.int32))
+        pos_d.copy_(dev(lengths, torch.int32))
+    place(lengths)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        step(cache, out, qn)
+    torch.cuda.synchronize()
+    out2, qn2 = torch.empty_like(out), torch.empty_like(out)
+    for t in range(8):
+        place(lengths + 17 * t)                            # the tokens between are whatever is there
+        for c, x in ((q, 1), (k, 2), (v, 3)):
+            c.copy_(rows(np.random.default_rng([t, x]), *c.shape))
+        if t == 0:
+            first = out.clone()
+        g.replay()
+        torch.cuda.synchronize()
+        step(twin, out2, qn2)                              # eager work between replays
+        torch.cuda.synchronize()
+        assert torch.equal(out, out2) and torch.equal(qn, qn2)
+    assert not torch.equal(out, first)
+
+
+def test_no_device_memory_is_allocated_by_calls():
+    rng = np.random.default_rng(23)
+    b = Batch(rng, "e4m3", 128, 4, 2, 64, [700, 300], [1, 1])
+    out, args = torch.empty_like(b.q), b.args()
+    torch.cuda.synchronize()
+    free = torch.cuda.mem_get_info()[0]
+    for _ in range(20):
+        b.cache.attend(b.q, *args, max_rows=1, max_length=700, out=out)
+    torch.cuda.synchronize()
+    assert torch.cuda.mem_get_info()[0] == free
+    assert 0 < b.cache.device_bytes < 256 << 20
+
+
+def test_memory_that_the_device_cannot_use_is_refused():
+    cache = KVCache.allocate(2, 1, 64, "bf16", 64)
+    k = torch.zeros(4, 1, 64, dtype=torch.bfloat16, device="cuda")
+    host = np.zeros(4, np.int64)
+    lib = esopt.load()
+    import ctypes
+    a = esopt.EsKvAppend()
+    a.k = a.v = k.data_ptr()
+    a.k_stride = a.v_stride = 64
+    a.tokens = 4
+    a.slots = host.ctypes.data
+    assert lib.es_kv_append(cache._h, ctypes.byref(a), None) == esopt.ES_ERR_INVALID_ARG
+    assert "slots" in esopt.last_error()
+    slots = torch.arange(4, device="cuda")
+    a.slots = slots.data_ptr()
+    a.k_stride = 1 << 30                                   # rows far past the end
+    assert lib.es_kv_append(cache._h, ctypes.byref(a), None) == esopt.ES_ERR_INVALID_ARG
+    assert "keys" in esopt.last_error()
+    d = esopt.EsKvDesc(cache.k_pages.data_ptr(), cache.v_pages.data_ptr(), None, None, 1 << 20, 64,
+                       1, 64, kvc.ES_KV_BF16, 0)
+    h = ctypes.c_void_p()
+    assert lib.es_kv_create(ctypes.byref(d), ctypes.byref(h)) == esopt.ES_ERR_INVALID_ARG
+    assert "past the end" in esopt.last_error()
+    with pytest.raises(ValueError):
+        cache.attend(k.float(), *[slots] * 3)
