@@ -42,7 +42,13 @@ inline int current_device(int* dev) {
 // leaves no error behind for later launch checks.
 // (The name of the checked array is `name` followed by `part`; it is
 // formatted only on failure.)
-inline int check_access(const void* p, uint64_t bytes, int device, const char* name, const char* part) {
+// `range`: set to the allocation that holds p, where the runtime knows it.
+struct Range {
+    uintptr_t base = 0;
+    uint64_t size = 0;
+};
+inline int check_access(const void* p, uint64_t bytes, int device, const char* name,
+                        const char* part, Range* range = nullptr) {
     if (bytes == 0) return ES_OK;
     auto what = [&]() { return std::string(name) + part; };
     hipPointerAttribute_t a{};
@@ -73,8 +79,26 @@ inline int check_access(const void* p, uint64_t bytes, int device, const char* n
     if (q < b || q - b > size || bytes > size - (q - b))
         return fail(ES_ERR_INVALID_ARG, what() + ": " + std::to_string(bytes) +
                                             " bytes extend past the end of its allocation");
+    if (range != nullptr) *range = Range{b, size};
     return ES_OK;
 }
+
+// The checks of one call's arrays: an array inside the allocation that the one
+// before it was found in needs no second query (0.4 us each, and a call at a
+// single token has ten arrays, most of them in one of the caller's pools).
+struct Accesses {
+    int device;
+    const char* name;
+    Range last;
+    int rc = ES_OK;                         // of the first check that failed
+    void check(const void* p, uint64_t bytes, const char* part) {
+        if (rc != ES_OK || bytes == 0) return;
+        const uintptr_t q = reinterpret_cast<uintptr_t>(p);
+        if (q - last.base < last.size && bytes <= last.size - (q - last.base)) return;
+        rc = check_access(p, bytes, device, name, part, &last);
+    }
+};
+
 inline int check_access(const void* p, uint64_t bytes, int device, const std::string& what) {
     return check_access(p, bytes, device, what.c_str(), "");
 }

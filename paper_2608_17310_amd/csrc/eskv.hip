@@ -47,11 +47,11 @@ int check_kv_device(const es_kv_t* kv, const char* name) {
 bool odd(const void* p, uintptr_t align) { return reinterpret_cast<uintptr_t>(p) % align != 0; }
 
 // `rows` rows of `width` bf16, `stride` elements apart.
-int check_rows(const void* p, uint64_t rows, uint64_t width, uint64_t stride, int device,
-               const char* name, const char* part) {
-    if (stride > (uint64_t(1) << 40))
-        return fail(ES_ERR_INVALID_ARG, std::string(name) + part + ": stride above 2^40");
-    return check_access(p, 2 * ((rows - 1) * stride + width), device, name, part);
+void check_rows(Accesses& x, const void* p, uint64_t rows, uint64_t width, uint64_t stride,
+                const char* part) {
+    if (x.rc == ES_OK && stride > (uint64_t(1) << 40))
+        x.rc = fail(ES_ERR_INVALID_ARG, std::string(x.name) + part + ": stride above 2^40");
+    x.check(p, 2 * ((rows - 1) * stride + width), part);
 }
 
 int launch_error(const char* what) {
@@ -206,25 +206,23 @@ int es_kv_append(es_kv_t* kv, const es_kv_append_t* args, es_stream_t stream) tr
         odd(x.k_gain, 2) || odd(x.rope, 4) || odd(x.positions, 4) || odd(x.slots, 8) ||
         odd(x.status, 4))
         return fail_in(ES_ERR_ALIGN, name, "array not aligned to its elements");
-    int rc = check_kv_device(kv, name);
-    const int dev = kv->device;
-    const uint64_t kw = uint64_t(kv->d.kv_heads) * dim, qw = uint64_t(x.q_heads) * dim;
-    if (rc == ES_OK) rc = check_rows(x.k, x.tokens, kw, x.k_stride, dev, name, ": keys");
-    if (rc == ES_OK) rc = check_rows(x.v, x.tokens, kw, x.v_stride, dev, name, ": values");
-    if (rc == ES_OK && qw != 0) rc = check_rows(x.q, x.tokens, qw, x.q_stride, dev, name, ": queries");
-    if (rc == ES_OK && qw != 0)
-        rc = check_rows(x.q_out, x.tokens, qw, x.q_out_stride, dev, name, ": query output");
-    if (rc == ES_OK && x.q_gain != nullptr)
-        rc = check_access(x.q_gain, 2 * dim, dev, name, ": query gain");
-    if (rc == ES_OK && x.k_gain != nullptr)
-        rc = check_access(x.k_gain, 2 * dim, dev, name, ": key gain");
-    if (rc == ES_OK && x.rot != 0)
-        rc = check_access(x.rope, uint64_t(4) * x.rot * x.rope_rows, dev, name, ": rotation table");
-    if (rc == ES_OK && x.rot != 0)
-        rc = check_access(x.positions, uint64_t(4) * x.tokens, dev, name, ": positions");
-    if (rc == ES_OK) rc = check_access(x.slots, uint64_t(8) * x.tokens, dev, name, ": slots");
-    if (rc == ES_OK && x.status != nullptr) rc = check_access(x.status, 4, dev, name, ": status");
+    const int rc = check_kv_device(kv, name);
     if (rc != ES_OK) return rc;
+    const uint64_t kw = uint64_t(kv->d.kv_heads) * dim, qw = uint64_t(x.q_heads) * dim;
+    Accesses ok{kv->device, name, {}};
+    check_rows(ok, x.k, x.tokens, kw, x.k_stride, ": keys");
+    check_rows(ok, x.v, x.tokens, kw, x.v_stride, ": values");
+    if (qw != 0) {
+        check_rows(ok, x.q, x.tokens, qw, x.q_stride, ": queries");
+        check_rows(ok, x.q_out, x.tokens, qw, x.q_out_stride, ": query output");
+    }
+    ok.check(x.q_gain, x.q_gain != nullptr ? 2 * dim : 0, ": query gain");
+    ok.check(x.k_gain, x.k_gain != nullptr ? 2 * dim : 0, ": key gain");
+    ok.check(x.rope, uint64_t(4) * x.rot * x.rope_rows, ": rotation table");
+    ok.check(x.positions, x.rot != 0 ? uint64_t(4) * x.tokens : 0, ": positions");
+    ok.check(x.slots, uint64_t(8) * x.tokens, ": slots");
+    ok.check(x.status, x.status != nullptr ? 4 : 0, ": status");
+    if (ok.rc != ES_OK) return ok.rc;
     AppendArgs a{};
     a.q = static_cast<const uint16_t*>(x.q);
     a.k = static_cast<const uint16_t*>(x.k);
@@ -268,13 +266,14 @@ int es_kv_read(es_kv_t* kv, const int64_t* slots, uint32_t tokens, void* k_out, 
         return fail_in(ES_ERR_INVALID_ARG, name, "the output's rows overlap");
     if (odd(slots, 8) || odd(k_out, 2) || odd(v_out, 2) || odd(status, 4))
         return fail_in(ES_ERR_ALIGN, name, "array not aligned to its elements");
-    int rc = check_kv_device(kv, name);
-    const int dev = kv->device;
-    if (rc == ES_OK) rc = check_access(slots, uint64_t(8) * tokens, dev, name, ": slots");
-    if (rc == ES_OK) rc = check_rows(k_out, tokens, width, k_stride, dev, name, ": key output");
-    if (rc == ES_OK) rc = check_rows(v_out, tokens, width, v_stride, dev, name, ": value output");
-    if (rc == ES_OK && status != nullptr) rc = check_access(status, 4, dev, name, ": status");
+    const int rc = check_kv_device(kv, name);
     if (rc != ES_OK) return rc;
+    Accesses ok{kv->device, name, {}};
+    ok.check(slots, uint64_t(8) * tokens, ": slots");
+    check_rows(ok, k_out, tokens, width, k_stride, ": key output");
+    check_rows(ok, v_out, tokens, width, v_stride, ": value output");
+    ok.check(status, status != nullptr ? 4 : 0, ": status");
+    if (ok.rc != ES_OK) return ok.rc;
     ReadArgs a{};
     a.slots = slots;
     a.k_out = static_cast<uint16_t*>(k_out);
@@ -318,21 +317,18 @@ int es_kv_attend(es_kv_t* kv, const es_kv_attend_t* args, es_stream_t stream) tr
         odd(x.first, 4) || odd(x.limit, 4) || odd(x.slopes, 4) || odd(x.status, 4))
         return fail_in(ES_ERR_ALIGN, name, "array not aligned to its elements");
     int rc = check_kv_device(kv, name);
-    const int dev = kv->device;
-    if (rc == ES_OK) rc = check_rows(x.q, x.rows, width, x.q_stride, dev, name, ": queries");
-    if (rc == ES_OK) rc = check_rows(x.out, x.rows, width, x.out_stride, dev, name, ": output");
-    const struct { const void* p; uint64_t bytes; const char* what; } arrays[] = {
-        {x.tables, uint64_t(4) * x.n_seqs * x.table_stride, ": tables"},
-        {x.lengths, uint64_t(4) * x.n_seqs, ": lengths"},
-        {x.starts, uint64_t(4) * (uint64_t(x.n_seqs) + 1), ": starts"},
-        {x.first, x.first != nullptr ? uint64_t(4) * x.rows : 0, ": first"},
-        {x.limit, x.limit != nullptr ? uint64_t(4) * x.rows : 0, ": limit"},
-        {x.slopes, x.slopes != nullptr ? uint64_t(4) * x.q_heads : 0, ": slopes"},
-        {x.status, x.status != nullptr ? uint64_t(4) : 0, ": status"}};
-    for (const auto& p : arrays)
-        if (rc == ES_OK) rc = check_access(p.p, p.bytes, dev, name, p.what);
     if (rc != ES_OK) return rc;
-
+    Accesses ok{kv->device, name, {}};
+    check_rows(ok, x.q, x.rows, width, x.q_stride, ": queries");
+    check_rows(ok, x.out, x.rows, width, x.out_stride, ": output");
+    ok.check(x.tables, uint64_t(4) * x.n_seqs * x.table_stride, ": tables");
+    ok.check(x.lengths, uint64_t(4) * x.n_seqs, ": lengths");
+    ok.check(x.starts, uint64_t(4) * (uint64_t(x.n_seqs) + 1), ": starts");
+    ok.check(x.first, x.first != nullptr ? uint64_t(4) * x.rows : 0, ": first");
+    ok.check(x.limit, x.limit != nullptr ? uint64_t(4) * x.rows : 0, ": limit");
+    ok.check(x.slopes, x.slopes != nullptr ? uint64_t(4) * x.q_heads : 0, ": slopes");
+    ok.check(x.status, x.status != nullptr ? 4 : 0, ": status");
+    if (ok.rc != ES_OK) return ok.rc;
     AttendArgs a{};
     a.q = static_cast<const uint16_t*>(x.q);
     a.out = static_cast<uint16_t*>(x.out);

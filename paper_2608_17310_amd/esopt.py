@@ -140,9 +140,10 @@ SIGNATURES = {
     "es_kv_create": (ctypes.c_int, [ctypes.POINTER(EsKvDesc), ctypes.POINTER(_vp)]),
     "es_kv_destroy": (ctypes.c_int, [_vp]),
     "es_kv_device_bytes": (_u64, [_vp]),
-    "es_kv_append": (ctypes.c_int, [_vp, ctypes.POINTER(EsKvAppend), _vp]),
+    # the argument structs as addresses: a ctypes.byref or packed bytes
+    "es_kv_append": (ctypes.c_int, [_vp, _vp, _vp]),
     "es_kv_read": (ctypes.c_int, [_vp, _vp, _u32, _vp, _u64, _vp, _u64, _vp, _vp]),
-    "es_kv_attend": (ctypes.c_int, [_vp, ctypes.POINTER(EsKvAttend), _vp]),
+    "es_kv_attend": (ctypes.c_int, [_vp, _vp, _vp]),
     "es_strerror": (ctypes.c_char_p, [ctypes.c_int]),
     "es_last_error": (ctypes.c_char_p, []),
 }

@@ -12,10 +12,11 @@ give, and can be captured in a graph.
 """
 
 import ctypes
+import struct
 
 import torch
 
-from .esopt import (EsKvAppend, EsKvAttend, EsKvDesc, _check, _stream, _u32_arg, load)
+from .esopt import EsKvDesc, ES_OK, _check, _stream, load
 
 ES_KV_INT8 = 0
 ES_KV_E4M3 = 1
@@ -30,15 +31,28 @@ _FORMATS = {torch.int8: ES_KV_INT8, torch.float8_e4m3fn: ES_KV_E4M3, torch.bfloa
 _DTYPES = {"int8": torch.int8, "e4m3": torch.float8_e4m3fn, "bf16": torch.bfloat16}
 
 
+# The argument structs of include/esopt.h, packed in one step: at single tokens
+# the calls are bound by the host, and setting twenty ctypes fields one by one
+# takes 3 us of them.
+_APPEND = struct.Struct("=3Q Q 4Q 6Q 4I f I")
+_ATTEND = struct.Struct("=2Q 2Q 7Q 6I 2f")
+
+
+def _current_stream(stream):
+    """The raw handle of `stream`, or of PyTorch's current one."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    return _stream(stream)
+
+
 def _rows(t, shape, what):
     """Pointer and token stride of [tokens, heads, dim] bf16 rows whose heads
     are adjacent (a slice of a packed projection qualifies)."""
-    if t.dtype != torch.bfloat16 or not t.is_cuda or t.dim() != 3:
-        raise ValueError(f"{what} must be a bf16 CUDA tensor [tokens, heads, head_dim]")
-    if tuple(t.shape) != shape:
-        raise ValueError(f"{what} has shape {tuple(t.shape)}, expected {shape}")
+    if t.dtype != torch.bfloat16 or not t.is_cuda or t.shape != shape:
+        raise ValueError(f"{what} must be a bf16 CUDA tensor of shape {tuple(shape)}, not "
+                         f"{tuple(t.shape)} {t.dtype}")
     s = t.stride()
-    if t.numel() and ((shape[2] > 1 and s[2] != 1) or (shape[1] > 1 and s[1] != shape[2])):
+    if (s[2] != 1 or s[1] != shape[2]) and t.numel() and (s[2] != 1 or shape[1] > 1):
         raise ValueError(f"{what}: a token's heads must be adjacent")
     if s[0] < 0:
         raise ValueError(f"{what}: negative stride")
@@ -46,13 +60,26 @@ def _rows(t, shape, what):
 
 
 def _array(t, dtype, n, what):
+    """Address of a contiguous tensor of n elements; 0 for None."""
     if t is None:
-        return None
+        return 0
     if t.dtype != dtype or not t.is_cuda or not t.is_contiguous():
         raise ValueError(f"{what} must be a contiguous {dtype} CUDA tensor")
     if t.numel() != n:
         raise ValueError(f"{what} has {t.numel()} elements, expected {n}")
     return t.data_ptr()
+
+
+def _heads(t, what):
+    if t.dim() != 3:
+        raise ValueError(f"{what} must be [tokens, heads, head_dim]")
+    return t.shape[1]
+
+
+def _count(x, what):
+    if not 0 <= x < (1 << 32):
+        raise ValueError(f"{what} must be in [0, 2^32), got {x}")
+    return x
 
 
 class KVCache:
@@ -95,6 +122,7 @@ class KVCache:
         with torch.cuda.device(self.device):
             _check(load().es_kv_create(ctypes.byref(d), ctypes.byref(handle)), "es_kv_create")
         self._h = handle
+        self._lib = load()
 
     @classmethod
     def allocate(cls, pages, kv_heads, head_dim, format="bf16", page=64, device="cuda"):
@@ -142,54 +170,61 @@ class KVCache:
         adjacent pairs dimensions 2 i and 2 i + 1 instead of i and
         i + rot / 2.  q_out may be q.  status: uint32-sized CUDA tensor
         (int32) that collects the ES_KV_BAD_* bits."""
-        tokens = int(k.shape[0])
-        shape = (tokens, self.kv_heads, self.head_dim)
-        a = EsKvAppend()
-        a.k, a.k_stride = _rows(k, shape, "k")
-        a.v, a.v_stride = _rows(v, shape, "v")
+        tokens = k.shape[0] if k.dim() == 3 else -1
+        dim = self.head_dim
+        shape = (tokens, self.kv_heads, dim)
+        k_at, k_stride = _rows(k, shape, "k")
+        v_at, v_stride = _rows(v, shape, "v")
+        q_at = q_stride = out_at = out_stride = q_heads = 0
         if q is not None:
-            heads = int(q.shape[1]) if q.dim() == 3 else 0
-            q_shape = (tokens, heads, self.head_dim)
-            a.q, a.q_stride = _rows(q, q_shape, "q")
+            q_heads = _heads(q, "q")
+            shape = (tokens, q_heads, dim)
+            q_at, q_stride = _rows(q, shape, "q")
             if q_out is None:
-                q_out = torch.empty(q_shape, dtype=torch.bfloat16, device=q.device)
-            a.q_out, a.q_out_stride = _rows(q_out, q_shape, "q_out")
-            a.q_heads = heads
+                q_out = torch.empty(shape, dtype=torch.bfloat16, device=q.device)
+            out_at, out_stride = _rows(q_out, shape, "q_out")
         elif q_out is not None:
             raise ValueError("q_out without q")
-        a.q_gain = _array(q_gain, torch.bfloat16, self.head_dim, "q_gain")
-        a.k_gain = _array(k_gain, torch.bfloat16, self.head_dim, "k_gain")
-        a.eps = float(eps)
+        rope_at = pos_at = rope_rows = rot = 0
         if rope is not None:
             if rope.dim() != 2 or positions is None:
                 raise ValueError("rope must be [positions, rot], with positions")
-            a.rope = _array(rope, torch.float32, rope.numel(), "rope")
-            a.rope_rows, a.rot = rope.shape
-            a.positions = _array(positions, torch.int32, tokens, "positions")
+            rope_rows, rot = rope.shape
+            rope_at = _array(rope, torch.float32, rope_rows * rot, "rope")
+            pos_at = _array(positions, torch.int32, tokens, "positions")
         elif positions is not None:
             raise ValueError("positions without rope")
-        a.slots = _array(slots, torch.int64, tokens, "slots")
-        a.status = _array(status, torch.int32, 1, "status")
-        a.tokens = _u32_arg(tokens, "tokens")
-        a.flags = ES_KV_ADJACENT if adjacent else 0
-        _check(load().es_kv_append(self._h, ctypes.byref(a), _stream(stream)), "es_kv_append")
+        args = _APPEND.pack(
+            q_at, k_at, v_at, out_at, q_stride, k_stride, v_stride, out_stride,
+            _array(q_gain, torch.bfloat16, dim, "q_gain"),
+            _array(k_gain, torch.bfloat16, dim, "k_gain"), rope_at, pos_at,
+            _array(slots, torch.int64, tokens, "slots"), _array(status, torch.int32, 1, "status"),
+            _count(tokens, "tokens"), q_heads, rot, _count(rope_rows, "rope rows"), eps,
+            ES_KV_ADJACENT if adjacent else 0)
+        rc = self._lib.es_kv_append(self._h, args, _current_stream(stream))
+        if rc != ES_OK:
+            _check(rc, "es_kv_append")
         return q_out
 
     def read(self, slots, k_out=None, v_out=None, status=None, stream=None):
         """The keys and values that slots [tokens] int64 hold, as bf16
         [tokens, kv_heads, dim] (a negative slot: zeros)."""
-        tokens = int(slots.numel())
+        tokens = slots.numel()
         shape = (tokens, self.kv_heads, self.head_dim)
-        outs = []
-        for t, what in ((k_out, "k_out"), (v_out, "v_out")):
-            if t is None:
-                t = torch.empty(shape, dtype=torch.bfloat16, device=self.device)
-            outs.append((t, *_rows(t, shape, what)))
-        _check(load().es_kv_read(self._h, _array(slots, torch.int64, tokens, "slots"),
-                                 _u32_arg(tokens, "tokens"), outs[0][1], outs[0][2], outs[1][1],
-                                 outs[1][2], _array(status, torch.int32, 1, "status"),
-                                 _stream(stream)), "es_kv_read")
-        return outs[0][0], outs[1][0]
+        if k_out is None and v_out is None:
+            k_out, v_out = torch.empty((2,) + shape, dtype=torch.bfloat16,
+                                       device=self.device).unbind(0)
+        elif k_out is None or v_out is None:
+            raise ValueError("give both outputs or none")
+        k_at, k_stride = _rows(k_out, shape, "k_out")
+        v_at, v_stride = _rows(v_out, shape, "v_out")
+        rc = self._lib.es_kv_read(self._h, _array(slots, torch.int64, tokens, "slots"),
+                                  _count(tokens, "tokens"), k_at, k_stride, v_at, v_stride,
+                                  _array(status, torch.int32, 1, "status"),
+                                  _current_stream(stream))
+        if rc != ES_OK:
+            _check(rc, "es_kv_read")
+        return k_out, v_out
 
     def attend(self, q, tables, lengths, starts, max_rows=None, max_length=None, out=None,
                first=None, limit=None, scale=None, cap=0.0, slopes=None, status=None,
@@ -203,28 +238,29 @@ class KVCache:
         caps scores by a tanh; slopes [q_heads] float32 weigh a bias by
         distance.  max_rows and max_length, the caller's bounds of rows and
         length of a sequence, choose how the work is cut."""
-        rows, heads = int(q.shape[0]), int(q.shape[1]) if q.dim() == 3 else 0
+        heads = _heads(q, "q")
+        rows = q.shape[0]
         shape = (rows, heads, self.head_dim)
-        a = EsKvAttend()
-        a.q, a.q_stride = _rows(q, shape, "q")
+        q_at, q_stride = _rows(q, shape, "q")
         if out is None:
             out = torch.empty(shape, dtype=torch.bfloat16, device=q.device)
-        a.out, a.out_stride = _rows(out, shape, "out")
+        out_at, out_stride = _rows(out, shape, "out")
         if tables.dim() != 2:
             raise ValueError("tables must be [seqs, pages]")
-        seqs, a.table_stride = tables.shape
-        a.tables = _array(tables, torch.int32, tables.numel(), "tables")
-        a.lengths = _array(lengths, torch.int32, seqs, "lengths")
-        a.starts = _array(starts, torch.int32, seqs + 1, "starts")
-        a.first = _array(first, torch.int32, rows, "first")
-        a.limit = _array(limit, torch.int32, rows, "limit")
-        a.slopes = _array(slopes, torch.float32, heads, "slopes")
-        a.status = _array(status, torch.int32, 1, "status")
-        a.rows, a.n_seqs, a.q_heads = _u32_arg(rows, "rows"), _u32_arg(seqs, "seqs"), heads
-        a.max_rows = _u32_arg(rows if max_rows is None else max_rows, "max_rows")
-        a.max_length = _u32_arg(tables.shape[1] * self.page if max_length is None else max_length,
-                                "max_length")
-        a.scale = float(self.head_dim ** -0.5 if scale is None else scale)
-        a.cap = float(cap)
-        _check(load().es_kv_attend(self._h, ctypes.byref(a), _stream(stream)), "es_kv_attend")
+        seqs, width = tables.shape
+        args = _ATTEND.pack(
+            q_at, out_at, q_stride, out_stride,
+            _array(tables, torch.int32, seqs * width, "tables"),
+            _array(lengths, torch.int32, seqs, "lengths"),
+            _array(starts, torch.int32, seqs + 1, "starts"),
+            _array(first, torch.int32, rows, "first"), _array(limit, torch.int32, rows, "limit"),
+            _array(slopes, torch.float32, heads, "slopes"),
+            _array(status, torch.int32, 1, "status"), _count(rows, "rows"),
+            _count(seqs, "seqs"), _count(width, "table width"), heads,
+            _count(rows if max_rows is None else max_rows, "max_rows"),
+            _count(width * self.page if max_length is None else max_length, "max_length"),
+            self.head_dim ** -0.5 if scale is None else scale, cap)
+        rc = self._lib.es_kv_attend(self._h, args, _current_stream(stream))
+        if rc != ES_OK:
+            _check(rc, "es_kv_attend")
         return out

@@ -42,6 +42,8 @@ def test_header_layouts_match_the_binding(lib, tmp_path):
     assert got["values"] == [str(v) for v in (
         kvc.ES_KV_INT8, kvc.ES_KV_E4M3, kvc.ES_KV_BF16, kvc.ES_KV_ADJACENT, kvc.ES_KV_BAD_SLOT,
         kvc.ES_KV_BAD_POSITION, kvc.ES_KV_BAD_PAGE, kvc.ES_KV_BAD_LENGTH)]
+    assert kvc._APPEND.size == ctypes.sizeof(esopt.EsKvAppend)
+    assert kvc._ATTEND.size == ctypes.sizeof(esopt.EsKvAttend)
     assert got["create_null"] == [str(E)] and got["attend_null"] == [str(E)]
     assert got["destroy_null"] == ["0"]
 
