@@ -86,20 +86,18 @@ template <int D, int F>
 struct MakeRead {
     static ReadKernel get() { return es_kv_read_kernel<D, F>; }
 };
-template <int T>
+template <int T, int kMode>
 struct MakeSplit {
     template <int D, int F>
     struct Of {
-        static AttendKernel get() {
-            return es_kv_split_kernel<D, (D == 256 ? 1 : T), F>;
-        }
+        static AttendKernel get() { return es_kv_split_kernel<D, (D == 256 ? 1 : T), F, kMode>; }
     };
 };
-template <bool kPlain>
+template <int kMode>
 struct MakeTile {
     template <int D, int F>
     struct Of {
-        static AttendKernel get() { return es_kv_tile_kernel<D, F, kPlain>; }
+        static AttendKernel get() { return es_kv_tile_kernel<D, F, kMode>; }
     };
 };
 
@@ -353,14 +351,25 @@ int es_kv_attend(es_kv_t* kv, const es_kv_attend_t* args, es_stream_t stream) tr
     a.scale = x.scale;
     a.cap = x.cap;
     a.c = kv->c;
+    const uint32_t format = kv->d.format;
+    const int mode = x.scale <= 0.0f || x.cap > kWideCap || (x.cap > 0.0f && x.slopes != nullptr)
+                         ? kAny
+                     : x.cap > 0.0f          ? kCapped
+                     : x.slopes != nullptr   ? kSloped
+                                             : kPlain;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const uint64_t all_rows = uint64_t(x.rows) * a.group;      // of one key head
     const uint64_t seq_rows = std::min<uint64_t>(x.rows, std::max(1u, x.max_rows)) * a.group;
     if (seq_rows <= 64) {
         const uint32_t tiles = seq_rows <= 16 ? 1 : split_tiles_max(dim);
+        // a history's scores cost nothing beside its bytes: one kernel for every mode but plain
         const AttendKernel kernel =
-            tiles == 1 ? by_dim_format<AttendKernel, MakeSplit<1>::Of>(dim, kv->d.format)
-                       : by_dim_format<AttendKernel, MakeSplit<2>::Of>(dim, kv->d.format);
+            tiles == 1 ? (mode == kPlain
+                              ? by_dim_format<AttendKernel, MakeSplit<1, kPlain>::Of>(dim, format)
+                              : by_dim_format<AttendKernel, MakeSplit<1, kAny>::Of>(dim, format))
+                       : (mode == kPlain
+                              ? by_dim_format<AttendKernel, MakeSplit<2, kPlain>::Of>(dim, format)
+                              : by_dim_format<AttendKernel, MakeSplit<2, kAny>::Of>(dim, format));
         const uint32_t tile_rows = 16 * tiles;
         // tiles of all sequences at most, and parts: one more than its share for each
         const uint64_t n_tiles = all_rows / tile_rows + x.n_seqs;
@@ -378,10 +387,11 @@ int es_kv_attend(es_kv_t* kv, const es_kv_attend_t* args, es_stream_t stream) tr
                            static_cast<int>(tile_rows));
         return launch_error("es_kv_join_kernel launch");
     }
-    const bool plain = x.cap == 0.0f && x.slopes == nullptr;
     const AttendKernel kernel =
-        plain ? by_dim_format<AttendKernel, MakeTile<true>::Of>(dim, kv->d.format)
-              : by_dim_format<AttendKernel, MakeTile<false>::Of>(dim, kv->d.format);
+        mode == kPlain    ? by_dim_format<AttendKernel, MakeTile<kPlain>::Of>(dim, format)
+        : mode == kCapped ? by_dim_format<AttendKernel, MakeTile<kCapped>::Of>(dim, format)
+        : mode == kSloped ? by_dim_format<AttendKernel, MakeTile<kSloped>::Of>(dim, format)
+                          : by_dim_format<AttendKernel, MakeTile<kAny>::Of>(dim, format);
     const uint32_t tile_rows = dim == 64    ? TileShape<64>::kRows
                                : dim == 128 ? TileShape<128>::kRows
                                             : TileShape<256>::kRows;

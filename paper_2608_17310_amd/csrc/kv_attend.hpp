@@ -74,40 +74,23 @@ __device__ __forceinline__ void interval(const AttendArgs& a, const Seq& s, int 
 
 constexpr float kWideCap = 256.0f;
 
-// Scores as the matrix unit leaves them, to the softmax's units.
+// From the matrix unit's products to the softmax's units (log2), by what a call
+// asks for.  Plain scores leave the scale to the exponential's multiply-add: a
+// weight is 2^(unit x - base).  kAny is any of the others together, a cap too wide
+// for the closed form, or a scale that is not positive (which would turn the
+// maximum of unscaled products round).
+enum Mode : int { kPlain = 0, kCapped = 1, kSloped = 2, kAny = 3 };
+
 struct ScoreMap {
-    float scale;                            // log2(e) times the scale (without cap)
+    float scale;                            // log2(e) times the scale
     float cap, cap_in;                      // cap log2(e); 2 log2(e) scale / cap
     float slope;                            // log2(e) times the slope of this lane's row
-    bool capped, wide, sloped;
+    float unit;                             // of transformed scores
+    bool capped, wide, sloped;              // read by kAny
 };
 
-template <bool kPlain>
-__device__ __forceinline__ float score(const ScoreMap& m, float s, float key_scale, int away) {
-    if constexpr (kPlain) return s * (m.scale * key_scale);
-    float t;
-    if (m.capped) {
-        // tanh(y) = 1 - 2 / (1 + e^(2 y)); e^(2 y) may be infinite
-        const float z = s * (m.cap_in * key_scale);          // 2 y log2(e)
-        const float e = __builtin_amdgcn_exp2f(z);
-        t = m.cap - 2.0f * m.cap * __builtin_amdgcn_rcpf(1.0f + e);
-        if (m.wide) {
-            // the difference is off by about 2^-23 cap, which a wide cap makes
-            // large beside a small score: there the series of tanh, to y^9
-            const float y = z * 0.34657359f, y2 = y * y;     // ln(2) / 2
-            float f = __builtin_fmaf(y2, 62.0f / 2835.0f, -17.0f / 315.0f);
-            f = __builtin_fmaf(y2, f, 2.0f / 15.0f);
-            f = __builtin_fmaf(y2, f, -1.0f / 3.0f);
-            f = __builtin_fmaf(y2 * y, f, y);
-            t = __builtin_fabsf(y) < 0.25f ? m.cap * f : t;
-        }
-    } else {
-        t = s * (m.scale * key_scale);
-    }
-    return m.sloped ? t - m.slope * static_cast<float>(away < 0 ? -away : away) : t;
-}
-
-__device__ __forceinline__ ScoreMap score_map(const AttendArgs& a) {
+template <int kMode>
+__device__ __forceinline__ ScoreMap score_map(const AttendArgs& a, uint32_t head) {
     ScoreMap m;
     m.scale = a.scale * kLog2e;
     m.capped = a.cap > 0.0f;
@@ -115,8 +98,47 @@ __device__ __forceinline__ ScoreMap score_map(const AttendArgs& a) {
     m.cap = a.cap * kLog2e;
     m.cap_in = m.capped ? 2.0f * kLog2e * a.scale / a.cap : 0.0f;
     m.sloped = a.slopes != nullptr;
-    m.slope = 0.0f;
+    m.slope = kMode >= kSloped && m.sloped ? a.slopes[head] * kLog2e : 0.0f;
+    m.unit = kMode == kPlain ? m.scale : 1.0f;
     return m;
+}
+
+// tanh(y) = 1 - 2 / (1 + e^(2 y)), z = 2 y log2(e); e^(2 y) may be infinite.
+__device__ __forceinline__ float cap_score(const ScoreMap& m, float z) {
+    const float r = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z));
+    return __builtin_fmaf(-2.0f * m.cap, r, m.cap);
+}
+
+// The closed form is off by about 2^-23 cap, which a wide cap makes large beside
+// a small score: there the series of tanh, to y^9.
+__device__ __forceinline__ float wide_cap(const ScoreMap& m, float z, float t) {
+    const float y = z * 0.34657359f, y2 = y * y;             // ln(2) / 2
+    float f = __builtin_fmaf(y2, 62.0f / 2835.0f, -17.0f / 315.0f);
+    f = __builtin_fmaf(y2, f, 2.0f / 15.0f);
+    f = __builtin_fmaf(y2, f, -1.0f / 3.0f);
+    f = __builtin_fmaf(y2 * y, f, y);
+    return __builtin_fabsf(y) < 0.25f ? m.cap * f : t;
+}
+
+// N products of one row, key i of them away(i) positions before the row.
+template <int kMode, int N, class Away>
+__device__ __forceinline__ void map_scores(const ScoreMap& m, float (&x)[N], Away away) {
+    if constexpr (kMode == kPlain) return;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        if constexpr (kMode == kCapped) {
+            x[i] = cap_score(m, x[i] * m.cap_in);
+        } else if constexpr (kMode == kSloped) {
+            x[i] = __builtin_fmaf(-m.slope, __builtin_fabsf(away(i)),
+                                  x[i] * m.scale);
+        } else {
+            const float z = x[i] * m.cap_in, t = cap_score(m, z);
+            const float y = !m.capped ? x[i] * m.scale : m.wide ? wide_cap(m, z, t) : t;
+            x[i] = m.sloped
+                       ? __builtin_fmaf(-m.slope, __builtin_fabsf(away(i)), y)
+                       : y;
+        }
+    }
 }
 
 // ----------------------------------------------------------------------------
@@ -256,7 +278,7 @@ __device__ __forceinline__ u32x4_t token_mask(int n) {
     return m;
 }
 
-template <int D, int kTiles, int kFmt>
+template <int D, int kTiles, int kFmt, int kMode>
 __global__ __launch_bounds__(kSplitThreads) void es_kv_split_kernel(AttendArgs a) {
     constexpr int kRowsOfTile = 16 * kTiles;
     constexpr int kSteps = D / 32;                           // 32 dimensions a product
@@ -265,7 +287,8 @@ __global__ __launch_bounds__(kSplitThreads) void es_kv_split_kernel(AttendArgs a
     // 16-byte words of a lane: of a key's row, and of a dimension's 64 tokens
     constexpr int kKeyWords = kBytes ? kSteps / 2 : kSteps;
     constexpr int kValWords = kBytes ? 1 : 2;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 15, g = lane >> 4;
     const uint32_t h = blockIdx.x % a.c.heads;
 
@@ -287,8 +310,7 @@ __global__ __launch_bounds__(kSplitThreads) void es_kv_split_kernel(AttendArgs a
         const uint32_t head = h * a.group + (r - i * static_cast<int>(a.group));
         interval(a, at.seq, i, first[t], limit[t]);
         pos[t] = at.seq.len - at.seq.n + i;
-        map[t] = score_map(a);
-        if (map[t].sloped) map[t].slope = a.slopes[head] * kLog2e;
+        map[t] = score_map<kMode>(a, head);
         if (first[t] < limit[t]) {
             lo_any = min(lo_any, first[t]);
             hi_any = max(hi_any, limit[t]);
@@ -332,7 +354,7 @@ __global__ __launch_bounds__(kSplitThreads) void es_kv_split_kernel(AttendArgs a
     for (int b = b_begin + wave; b < b_end; b += kSplitWaves) {
         const int key0 = b * kBlock;
         if (key0 >= hi_any || key0 + kBlock <= lo_any) continue;
-        const uint32_t page = table[key0 >> a.c.page_shift];
+        const uint32_t page = load_uniform(table + (key0 >> a.c.page_shift));
         const bool bad = page >= a.c.n_pages;
         const uint64_t head_at = uint64_t(bad ? 0u : page) * a.c.heads + h;
         const uint32_t off = uint32_t(key0) & (a.c.page - 1);
@@ -390,20 +412,30 @@ __global__ __launch_bounds__(kSplitThreads) void es_kv_split_kernel(AttendArgs a
                     }
                 }
             }
-            // scores of this lane's 16 keys, in the softmax's units
+            // scores of this lane's 16 keys: key_of(4 k + i) in s[k][i]
+            auto key_of = [&](int x) {
+                const int k = x >> 2, i = x & 3;
+                return key0 + (kBytes ? 16 * g + 4 * k + i
+                                      : 32 * (k >> 1) + 8 * g + 4 * (k & 1) + i);
+            };
+            float x[16];
+#pragma unroll
+            for (int k = 0; k < 16; ++k)
+                x[k] = kBytes ? s[k >> 2][k & 3] * ks[k >> 2][k & 3] : s[k >> 2][k & 3];
+            map_scores<kMode>(map[t], x, [&](int k) { return static_cast<float>(pos[t] - key_of(k)); });
+            if (bad) {
+#pragma unroll
+                for (int k = 0; k < 16; ++k) x[k] = nan();
+            }
+            if (masked) {
+#pragma unroll
+                for (int k = 0; k < 16; ++k)
+                    if (key_of(k) < first[t] || key_of(k) >= limit[t]) x[k] = -inf();
+            }
             float peak = -inf();
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int key = key0 + (kBytes ? 16 * g + 4 * k + i
-                                                   : 32 * (k >> 1) + 8 * g + 4 * (k & 1) + i);
-                    float x = score<false>(map[t], s[k][i], kBytes ? ks[k][i] : 1.0f, pos[t] - key);
-                    if (bad) x = nan();
-                    if (masked && (key < first[t] || key >= limit[t])) x = -inf();
-                    s[k][i] = x;
-                    peak = __builtin_fmaxf(peak, x);
-                }
+            for (int k = 0; k < 16; ++k) peak = __builtin_fmaxf(peak, x[k]);
+            peak *= map[t].unit;
             peak = __builtin_fmaxf(peak, __shfl_xor(peak, 16));
             peak = __builtin_fmaxf(peak, __shfl_xor(peak, 32));
             const float now = __builtin_fmaxf(top[t], peak);
@@ -423,12 +455,13 @@ __global__ __launch_bounds__(kSplitThreads) void es_kv_split_kernel(AttendArgs a
                 for (int j = 0; j < 4; ++j) {
                     float e[2];
 #pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        const int k = 2 * u + (j >> 1), i = 2 * (j & 1) + x;
-                        e[x] = __builtin_amdgcn_exp2f(s[k][i] - base);
-                        sum[t] += e[x];
+                    for (int y = 0; y < 2; ++y) {
+                        const int k = 2 * u + (j >> 1), i = 2 * (j & 1) + y;
+                        e[y] = __builtin_amdgcn_exp2f(
+                            __builtin_fmaf(x[4 * k + i], map[t].unit, -base));
+                        sum[t] += e[y];
                         // a weight of zero stays zero whatever stands in a slot unseen
-                        if constexpr (kBytes) e[x] = e[x] == 0.0f ? 0.0f : e[x] * vs[k][i];
+                        if constexpr (kBytes) e[y] = e[y] == 0.0f ? 0.0f : e[y] * vs[k][i];
                     }
                     w[j] = pack_bf16(e[0], e[1]);
                 }
@@ -588,11 +621,14 @@ __global__ __launch_bounds__(kSplitThreads) void es_kv_join_kernel(AttendArgs a,
 }
 
 // ----------------------------------------------------------------------------
-// Many rows: a workgroup of kWaves waves takes 32 kWaves rows of one key head,
-// 32 to a wave, over all blocks that some of them see.  Bound by the matrix
-// unit beside the exponentials: keys and values are staged in LDS as bf16, once
-// for all waves (codes are converted on their way in), double-buffered, the
-// next block's loads in flight under the present block's products.
+// Many rows: a workgroup of four waves takes 128 rows of one key head, 32 to a
+// wave, over all blocks that some of them see.  Bound by the matrix unit beside
+// the exponentials: keys and values are staged in LDS as bf16, once for all
+// waves, double-buffered, the next block on its way under the present one's
+// products: bf16 straight into LDS, codes through registers (converted once).
+// Two workgroups share a compute unit: with a barrier a block, waves of one
+// workgroup compute products and exponentials at the same time, and only
+// another workgroup's fill the other unit meanwhile.
 //
 // LDS rows are 2 D bytes (keys) and 128 bytes (values); their 16-byte words
 // are exchanged by the row's number so that 16 rows of one word lie in 16
@@ -601,13 +637,18 @@ __global__ __launch_bounds__(kSplitThreads) void es_kv_join_kernel(AttendArgs a,
 
 template <int D>
 struct TileShape {
-    static constexpr int kWaves = D == 128 ? 8 : 4;
+    static constexpr int kWaves = 4;
     static constexpr int kThreads = 64 * kWaves;
     static constexpr int kRows = 32 * kWaves;
     static constexpr int kKeyBytes = kBlock * D * 2;
     static constexpr int kBuffer = 2 * kKeyBytes;            // keys, then as many bytes of values
     static constexpr int kLds = 2 * kBuffer + 256 * 4;       //   and the scales of both
+    static constexpr int kPerSimd = D == 256 ? 1 : 2;        // waves of a SIMD that the registers leave
 };
+
+// A running maximum is kept until a score exceeds it by this much (log2): weights
+// are at most 2^8 then, and the accumulators are seldom rescaled.
+constexpr float kSlack = 8.0f;
 
 // Byte offsets of 16-byte words in the staged tiles.
 template <int D>
@@ -646,13 +687,22 @@ __device__ __forceinline__ Place find_tile(const AttendArgs& a, int tile_rows, u
     return r;
 }
 
-template <int D, int kFmt, bool kPlain>
-__global__ __launch_bounds__(TileShape<D>::kThreads) void es_kv_tile_kernel(AttendArgs a) {
+// The larger of a value and the other half-wave's.
+__device__ __forceinline__ float max_halves(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false,
+                                                    false);
+    return __builtin_fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+template <int D, int kFmt, int kMode>
+__global__ __launch_bounds__(TileShape<D>::kThreads, TileShape<D>::kPerSimd) void
+es_kv_tile_kernel(AttendArgs a) {
     using S = TileShape<D>;
     constexpr bool kBytes = kFmt != kBf16;
     constexpr int kSteps = D / 16;                           // 16 dimensions a product
     constexpr int kDims = D / 32;                            // 32 dimensions a tile of O^T
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 31, g = lane >> 5;
     const uint32_t h = blockIdx.x % a.c.heads;
 
@@ -670,8 +720,7 @@ __global__ __launch_bounds__(TileShape<D>::kThreads) void es_kv_tile_kernel(Atte
     int first, limit;
     interval(a, at.seq, i, first, limit);
     const int pos = at.seq.len - at.seq.n + i;
-    ScoreMap map = score_map(a);
-    if (map.sloped) map.slope = a.slopes[head] * kLog2e;
+    const ScoreMap map = score_map<kMode>(a, head);
 
     bf16x8_t q[kSteps];
     {
@@ -711,65 +760,78 @@ __global__ __launch_bounds__(TileShape<D>::kThreads) void es_kv_tile_kernel(Atte
     const int b_begin = lo / kBlock, b_end = hi > lo ? (hi - 1) / kBlock + 1 : b_begin;
 
     // staging: 16-byte words of codes, each thread kStage of the keys' and of the values'
-    constexpr int kWordsK = kBlock * D * kCodeBytes<kFmt> / 16;
-    constexpr int kStage = kWordsK / S::kThreads;
-    static_assert(kStage >= 1 && kWordsK % S::kThreads == 0, "staging covers the block");
+    constexpr int kStage = kBlock * D * kCodeBytes<kFmt> / 16 / S::kThreads;
+    static_assert(kStage * S::kThreads * 16 == kBlock * D * kCodeBytes<kFmt>,
+                  "staging covers the block");
     constexpr int kKeyWords = D * kCodeBytes<kFmt> / 16;     // words of a key's row
     constexpr int kValWords = kBlock * kCodeBytes<kFmt> / 16;    // of a dimension's tokens
-    u32x4_t sk[kStage], sv[kStage];
+    const uint32_t val_row = a.c.page * kCodeBytes<kFmt>;    // bytes of a dimension's page
+    // bf16: word p of the staged tile is the 16 bytes at these offsets of the block
+    uint32_t k_off[kStage], v_off[kStage];
+#pragma unroll
+    for (int x = 0; x < kStage; ++x) {
+        const int p = (wave * kStage + x) * 64 + lane;
+        const int kr = p / kKeyWords, kw = p % kKeyWords, vr = p / kValWords, vw = p % kValWords;
+        k_off[x] = key_word<D>(kr, kw);
+        v_off[x] = vr * val_row + 16 * (vw ^ ((vr >> 1) & 7));
+    }
+    u32x4_t sk[kBytes ? kStage : 1], sv[kBytes ? kStage : 1];
     float sscale = 0.0f;
-    bool bad = false;
+    bool bad = false, bad_next = false;
     const int32_t* table = a.tables + uint64_t(at.s) * a.table_stride;
-    auto fetch = [&](int b) {
+    auto fetch = [&](int b, uint8_t* buf) {
         const int key0 = b * kBlock;
-        const uint32_t page = table[key0 >> a.c.page_shift];
-        bad = page >= a.c.n_pages;
-        const uint64_t head_at = uint64_t(bad ? 0u : page) * a.c.heads + h;
+        const uint32_t page = load_uniform(table + (key0 >> a.c.page_shift));
+        bad_next = page >= a.c.n_pages;
+        const uint64_t head_at = uint64_t(bad_next ? 0u : page) * a.c.heads + h;
         const uint32_t off = uint32_t(key0) & (a.c.page - 1);
         const uint64_t token = head_at * a.c.page + off;
         const uint8_t* ksrc = a.c.k + token * (D * kCodeBytes<kFmt>);
         const uint8_t* vsrc = a.c.v + (head_at * D * a.c.page + off) * kCodeBytes<kFmt>;
-#pragma unroll
-        for (int x = 0; x < kStage; ++x) {
-            const int w = threadIdx.x + S::kThreads * x;
-            sk[x] = load<u32x4_t>(ksrc + 16 * w);
-            sv[x] = load<u32x4_t>(vsrc + uint64_t(w / kValWords) * a.c.page * kCodeBytes<kFmt> +
-                                  16 * (w % kValWords));
-        }
         if constexpr (kBytes) {
+#pragma unroll
+            for (int x = 0; x < kStage; ++x) {
+                const int w = threadIdx.x + S::kThreads * x;
+                sk[x] = load<u32x4_t>(ksrc + 16 * w);
+                sv[x] = load<u32x4_t>(vsrc + uint32_t(w / kValWords) * val_row +
+                                      16 * (w % kValWords));
+            }
             if (threadIdx.x < 2 * kBlock)
                 sscale = load<float>((threadIdx.x < kBlock ? a.c.ks : a.c.vs) + token +
                                      (threadIdx.x & (kBlock - 1)));
-        }
-    };
-    auto stage = [&](int b, uint8_t* buf, float* scales) {
-        const int left = bad ? 0 : at.seq.len - b * kBlock;  // tokens of the block
+        } else {
 #pragma unroll
-        for (int x = 0; x < kStage; ++x) {
-            const int w = threadIdx.x + S::kThreads * x;
-            const int kr = w / kKeyWords, kc = w % kKeyWords;
-            const int vr = w / kValWords, vc = w % kValWords;
-            u32x4_t v = sv[x];
-            if (left < kBlock) v &= token_mask<kFmt>(left - vc * (16 / kCodeBytes<kFmt>));
-            if constexpr (kBytes) {
+            for (int x = 0; x < kStage; ++x) {
+                load_to_lds(ksrc + k_off[x], buf + (wave * kStage + x) * 1024);
+                load_to_lds(vsrc + v_off[x], buf + S::kKeyBytes + (wave * kStage + x) * 1024);
+            }
+        }
+        if (bad_next && a.status != nullptr && threadIdx.x == 0)
+            atomicOr(a.status, ES_KV_BAD_PAGE);
+    };
+    auto stage = [&](uint8_t* buf, float* scales) {
+        if constexpr (kBytes) {
+#pragma unroll
+            for (int x = 0; x < kStage; ++x) {
+                const int w = threadIdx.x + S::kThreads * x;
+                const int kr = w / kKeyWords, kc = w % kKeyWords;
+                const int vr = w / kValWords, vc = w % kValWords;
                 *reinterpret_cast<u32x4_t*>(buf + key_word<D>(kr, 2 * kc)) =
                     codes_to_bf16<kFmt>(u32x2_t{sk[x][0], sk[x][1]});
                 *reinterpret_cast<u32x4_t*>(buf + key_word<D>(kr, 2 * kc + 1)) =
                     codes_to_bf16<kFmt>(u32x2_t{sk[x][2], sk[x][3]});
                 *reinterpret_cast<u32x4_t*>(buf + S::kKeyBytes + val_word(vr, 2 * vc)) =
-                    codes_to_bf16<kFmt>(u32x2_t{v[0], v[1]});
+                    codes_to_bf16<kFmt>(u32x2_t{sv[x][0], sv[x][1]});
                 *reinterpret_cast<u32x4_t*>(buf + S::kKeyBytes + val_word(vr, 2 * vc + 1)) =
-                    codes_to_bf16<kFmt>(u32x2_t{v[2], v[3]});
-            } else {
-                const u32x4_t not_a_number = {0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u};
-                *reinterpret_cast<u32x4_t*>(buf + key_word<D>(kr, kc)) = bad ? not_a_number : sk[x];
-                *reinterpret_cast<u32x4_t*>(buf + S::kKeyBytes + val_word(vr, vc)) = v;
+                    codes_to_bf16<kFmt>(u32x2_t{sv[x][2], sv[x][3]});
             }
+            if (threadIdx.x < 2 * kBlock) scales[threadIdx.x] = sscale;
         }
-        if constexpr (kBytes) {
-            if (threadIdx.x < 2 * kBlock) scales[threadIdx.x] = bad ? nan() : sscale;
-        }
-        if (bad && a.status != nullptr && threadIdx.x == 0) atomicOr(a.status, ES_KV_BAD_PAGE);
+    };
+    // the block has landed in LDS for every wave
+    auto arrive = [&]() {
+        if constexpr (!kBytes) wait_loads();
+        __syncthreads();
     };
 
     float top = -inf(), sum = 0.0f;
@@ -784,107 +846,117 @@ __global__ __launch_bounds__(TileShape<D>::kThreads) void es_kv_tile_kernel(Atte
     const int krow = (n & 0x13) | ((n & 4) << 1) | ((n & 8) >> 1);
 
     if (b_begin < b_end) {
-        fetch(b_begin);
-        stage(b_begin, lds, scales0);
-        __syncthreads();
+        fetch(b_begin, lds);
+        stage(lds, scales0);
+        arrive();
     }
     for (int b = b_begin; b < b_end; ++b) {
         const int cur = (b - b_begin) & 1;
         uint8_t* const buf = lds + cur * S::kBuffer;
         float* const scales = scales0 + cur * 128;
         const bool more = b + 1 < b_end;
-        if (more) fetch(b + 1);
         const int key0 = b * kBlock;
+        bad = bad_next;
+        if (more) fetch(b + 1, lds + (cur ^ 1) * S::kBuffer);
+        if (bad || key0 + kBlock > at.seq.len) {
+            // slots past the sequence's end may hold anything: their values are cleared
+            const int left = bad ? 0 : at.seq.len - key0;
+            for (int w = threadIdx.x; w < D * 8; w += S::kThreads) {
+                u32x4_t* const v =
+                    reinterpret_cast<u32x4_t*>(buf + S::kKeyBytes + val_word(w >> 3, w & 7));
+                *v &= token_mask<kBf16>(left - 8 * (w & 7));
+            }
+            __syncthreads();
+        }
         if (key0 < hi_any && key0 + kBlock > lo_any) {
             f32x16_t s[2];
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
 #pragma unroll
-                for (int x = 0; x < 16; ++x) s[t][x] = 0.0f;
-#pragma unroll
                 for (int c = 0; c < kSteps; ++c) {
                     const bf16x8_t k = *reinterpret_cast<const bf16x8_t*>(
                         buf + key_word<D>(32 * t + krow, 2 * c + g));
-                    s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[c], s[t], 0, 0, 0);
+                    s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[c], c == 0 ? f32x16_t{} : s[t],
+                                                                   0, 0, 0);
                 }
             }
             // register x of tile t: key 32 t + 16 (x / 8) + 8 g + x % 8
-            f32x4_t kscale[2][4], vscale[2][4];
+            float x[32];
+#pragma unroll
+            for (int y = 0; y < 32; ++y) x[y] = s[y >> 4][y & 15];
             if constexpr (kBytes) {
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
+                for (int y = 0; y < 8; ++y) {
+                    const f32x4_t k4 = *reinterpret_cast<const f32x4_t*>(
+                        scales + 32 * (y >> 2) + 16 * ((y >> 1) & 1) + 8 * g + 4 * (y & 1));
 #pragma unroll
-                    for (int y = 0; y < 4; ++y) {
-                        const int k = 32 * t + 16 * (y >> 1) + 8 * g + 4 * (y & 1);
-                        kscale[t][y] = *reinterpret_cast<const f32x4_t*>(scales + k);
-                        vscale[t][y] = *reinterpret_cast<const f32x4_t*>(scales + 64 + k);
-                    }
-            }
-            float peak = -inf();
-            const bool masked = key0 < lo_all || key0 + kBlock > hi_all;
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int x = 0; x < 16; ++x) {
-                    const int key = key0 + 32 * t + 16 * (x >> 3) + 8 * g + (x & 7);
-                    s[t][x] = score<kPlain>(map, s[t][x], kBytes ? kscale[t][x >> 2][x & 3] : 1.0f,
-                                            pos - key);
+                    for (int z = 0; z < 4; ++z) x[4 * y + z] *= k4[z];
                 }
-            if (masked) {
-#pragma unroll
-                for (int t = 0; t < 2; ++t)
-#pragma unroll
-                    for (int x = 0; x < 16; ++x) {
-                        const int key = key0 + 32 * t + 16 * (x >> 3) + 8 * g + (x & 7);
-                        if (key < first || key >= limit) s[t][x] = -inf();
-                    }
             }
+            const float away = static_cast<float>(pos - (key0 + 8 * g));
+            map_scores<kMode>(map, x, [&](int y) {
+                return away - static_cast<float>(32 * (y >> 4) + 16 * ((y >> 3) & 1) + (y & 7));
+            });
+            if (bad) {
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+                for (int y = 0; y < 32; ++y) x[y] = nan();
+            }
+            if (key0 < lo_all || key0 + kBlock > hi_all) {
+                // against the key's constant part: no register holds a key's number
+                const int from = first - (key0 + 8 * g), to = limit - (key0 + 8 * g);
 #pragma unroll
-                for (int x = 0; x < 16; ++x) peak = __builtin_fmaxf(peak, s[t][x]);
-            peak = __builtin_fmaxf(peak, __shfl_xor(peak, 32));
-            const float now = __builtin_fmaxf(top, peak);
-            const float base = now == -inf() ? 0.0f : now;
-            if (__any(now > top)) {
-                const float shrink = __builtin_amdgcn_exp2f(top - base);
+                for (int y = 0; y < 32; ++y) {
+                    const int k = 32 * (y >> 4) + 16 * ((y >> 3) & 1) + (y & 7);
+                    if (k < from || k >= to) x[y] = -inf();
+                }
+            }
+            float peak = x[0];
+#pragma unroll
+            for (int y = 1; y < 32; ++y) peak = __builtin_fmaxf(peak, x[y]);
+            const float now = __builtin_fmaxf(top, max_halves(peak) * map.unit);
+            if (__any(now > top + kSlack)) {
+                const float shrink = __builtin_amdgcn_exp2f(top - (now == -inf() ? 0.0f : now));
                 sum *= shrink;
 #pragma unroll
                 for (int d = 0; d < kDims; ++d) o[d] *= shrink;
+                top = now;
             }
-            top = now;
+            // nothing seen so far: any finite stand-in gives weights of zero
+            const float base = top == -inf() ? 0.0f : top;
             bf16x8_t p[4];
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+            for (int u = 0; u < 4; ++u) {
+                u32x4_t w;
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    u32x4_t w;
+                for (int j = 0; j < 2; ++j) {
+                    float e[4];
+                    f32x4_t v4;
+                    if constexpr (kBytes)
+                        v4 = *reinterpret_cast<const f32x4_t*>(scales + 64 + 16 * u + 8 * g + 4 * j);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        float e[2];
-#pragma unroll
-                        for (int y = 0; y < 2; ++y) {
-                            const int x = 8 * u + 2 * j + y;
-                            e[y] = __builtin_amdgcn_exp2f(s[t][x] - base);
-                            sum += e[y];
-                            if constexpr (kBytes)
-                                e[y] = e[y] == 0.0f ? 0.0f : e[y] * vscale[t][x >> 2][x & 3];
-                        }
-                        w[j] = pack_bf16(e[0], e[1]);
+                    for (int y = 0; y < 4; ++y) {
+                        e[y] = __builtin_amdgcn_exp2f(
+                            __builtin_fmaf(x[8 * u + 4 * j + y], map.unit, -base));
+                        sum += e[y];
+                        // a weight of zero stays zero whatever stands in a slot unseen
+                        if constexpr (kBytes) e[y] = e[y] == 0.0f ? 0.0f : e[y] * v4[y];
                     }
-                    p[2 * t + u] = __builtin_bit_cast(bf16x8_t, w);
+                    w[2 * j] = pack_bf16(e[0], e[1]);
+                    w[2 * j + 1] = pack_bf16(e[2], e[3]);
                 }
+                p[u] = __builtin_bit_cast(bf16x8_t, w);
+            }
 #pragma unroll
-            for (int d = 0; d < kDims; ++d)
+            for (int u = 0; u < 4; ++u)
 #pragma unroll
-                for (int u = 0; u < 4; ++u) {
+                for (int d = 0; d < kDims; ++d) {
                     const bf16x8_t v = *reinterpret_cast<const bf16x8_t*>(
                         buf + S::kKeyBytes + val_word(32 * d + n, 2 * u + g));
                     o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p[u], o[d], 0, 0, 0);
                 }
         }
-        if (more) stage(b + 1, lds + (cur ^ 1) * S::kBuffer, scales0 + (cur ^ 1) * 128);
-        __syncthreads();
+        if (more) stage(lds + (cur ^ 1) * S::kBuffer, scales0 + (cur ^ 1) * 128);
+        arrive();
     }
 
     sum += __shfl_xor(sum, 32);
@@ -894,12 +966,10 @@ __global__ __launch_bounds__(TileShape<D>::kThreads) void es_kv_tile_kernel(Atte
 #pragma unroll
     for (int d = 0; d < kDims; ++d)
 #pragma unroll
-        for (int y = 0; y < 4; ++y) {
-            u32x2_t w;
-            w = u32x2_t{pack_bf16(o[d][4 * y] * inv, o[d][4 * y + 1] * inv),
-                          pack_bf16(o[d][4 * y + 2] * inv, o[d][4 * y + 3] * inv)};
-            store_row4(out + 32 * d + 8 * y + 4 * g, w);
-        }
+        for (int y = 0; y < 4; ++y)
+            store_row4(out + 32 * d + 8 * y + 4 * g,
+                       u32x2_t{pack_bf16(o[d][4 * y] * inv, o[d][4 * y + 1] * inv),
+                               pack_bf16(o[d][4 * y + 2] * inv, o[d][4 * y + 3] * inv)});
 }
 
 }  // namespace eskv

@@ -48,6 +48,12 @@ __device__ __forceinline__ f32x4_t load_float4(const float* p) {
     return *reinterpret_cast<const ESKV_GLOBAL f32x4_at4_t*>(reinterpret_cast<uintptr_t>(p));
 }
 
+// A value at an address that is the same for the wave, through the scalar cache.
+__device__ __forceinline__ int32_t load_uniform(const int32_t* p) {
+    return *reinterpret_cast<const __attribute__((address_space(4))) int32_t*>(
+        reinterpret_cast<uintptr_t>(p));
+}
+
 enum Format : int { kInt8 = ES_KV_INT8, kE4M3 = ES_KV_E4M3, kBf16 = ES_KV_BF16 };
 
 template <int kFmt>
@@ -57,6 +63,17 @@ constexpr float kCodeMax = kFmt == kInt8 ? 127.0f : 448.0f;
 constexpr float kTinyRow = 0x1p-100f;       // rows whose largest |x| is below read as zeros
 
 constexpr float kLog2e = 1.4426950408889634f;
+
+// 16 bytes a lane from memory into LDS, at `dst` (the same for the wave) + 16 lane,
+// without passing registers; wait_loads() before the wave's own barrier.
+__device__ __forceinline__ void load_to_lds(const void* src, void* dst) {
+    __builtin_amdgcn_global_load_lds(
+        reinterpret_cast<const ESKV_GLOBAL void*>(reinterpret_cast<uintptr_t>(src)),
+        reinterpret_cast<__attribute__((address_space(3))) void*>(
+            static_cast<uint32_t>(reinterpret_cast<uintptr_t>(dst))),
+        16, 0, 0);
+}
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 __device__ __forceinline__ float inf() { return __builtin_inff(); }
 __device__ __forceinline__ float nan() { return __builtin_nanf(""); }
