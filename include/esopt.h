@@ -719,7 +719,7 @@ typedef struct es_kv_attend {
     uint32_t       q_heads;     /* a multiple of kv_heads, at most 64 times as many */
     uint32_t       max_rows, max_length;
     float          scale;
-    float          cap;         /* 0: scores are not capped */
+    float          cap;         /* 0: scores are not capped; otherwise at least 2^-60 */
 } es_kv_attend_t;
 int es_kv_attend(es_kv_t* kv, const es_kv_attend_t* args, es_stream_t stream);
 

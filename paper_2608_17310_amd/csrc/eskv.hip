@@ -303,6 +303,8 @@ int es_kv_attend(es_kv_t* kv, const es_kv_attend_t* args, es_stream_t stream) tr
     if (!std::isfinite(x.scale)) return fail_in(ES_ERR_INVALID_ARG, name, "scale is not finite");
     if (!(x.cap >= 0.0f) || !std::isfinite(x.cap))
         return fail_in(ES_ERR_INVALID_ARG, name, "cap is negative or not finite");
+    if (x.cap > 0.0f && x.cap < 0x1p-60f)
+        return fail_in(ES_ERR_INVALID_ARG, name, "cap below 2^-60");
     if (x.table_stride == 0) return fail_in(ES_ERR_INVALID_ARG, name, "table_stride is 0");
     if (x.rows == 0) return ES_OK;
     if (x.q == nullptr || x.out == nullptr || x.tables == nullptr || x.lengths == nullptr ||

@@ -75,38 +75,47 @@ __device__ __forceinline__ void interval(const AttendArgs& a, const Seq& s, int 
 constexpr float kWideCap = 256.0f;
 
 // From the matrix unit's products to the softmax's units (log2), by what a call
-// asks for.  Plain scores leave the scale to the exponential's multiply-add: a
-// weight is 2^(unit x - base).  kAny is any of the others together, a cap too wide
-// for the closed form, or a scale that is not positive (which would turn the
-// maximum of unscaled products round).
+// asks for.  A score is kept as x with t = unit x + offset, and a weight is
+// 2^(unit x + (offset - base)), so that the last multiply and add are the
+// exponential's: plain scores leave the scale to it, capped ones the cap.  kAny
+// is several of the others together, a cap too wide for the closed form, or a
+// scale that is not positive (which would turn the maximum of unscaled products
+// round).
 enum Mode : int { kPlain = 0, kCapped = 1, kSloped = 2, kAny = 3 };
 
 struct ScoreMap {
-    float scale;                            // log2(e) times the scale
-    float cap, cap_in;                      // cap log2(e); 2 log2(e) scale / cap
+    float factor;                           // of a product, first: log2(e) scale, or, capped,
+                                            //   2 log2(e) scale / cap
+    float unit, offset;
+    float scale, cap;                       // log2(e) times the scale and the cap
     float slope;                            // log2(e) times the slope of this lane's row
-    float unit;                             // of transformed scores
     bool capped, wide, sloped;              // read by kAny
 };
 
-template <int kMode>
+template <int kMode, bool kBytes>
 __device__ __forceinline__ ScoreMap score_map(const AttendArgs& a, uint32_t head) {
     ScoreMap m;
     m.scale = a.scale * kLog2e;
     m.capped = a.cap > 0.0f;
     m.wide = a.cap > kWideCap;
     m.cap = a.cap * kLog2e;
-    m.cap_in = m.capped ? 2.0f * kLog2e * a.scale / a.cap : 0.0f;
     m.sloped = a.slopes != nullptr;
     m.slope = kMode >= kSloped && m.sloped ? a.slopes[head] * kLog2e : 0.0f;
-    m.unit = kMode == kPlain ? m.scale : 1.0f;
+    m.factor = (kMode == kCapped || kMode == kAny) && m.capped ? 2.0f * kLog2e * a.scale / a.cap
+                                                               : m.scale;
+    m.unit = kMode == kCapped ? -2.0f * m.cap : kMode == kPlain && !kBytes ? m.scale : 1.0f;
+    m.offset = kMode == kCapped ? m.cap : 0.0f;
     return m;
 }
 
-// tanh(y) = 1 - 2 / (1 + e^(2 y)), z = 2 y log2(e); e^(2 y) may be infinite.
-__device__ __forceinline__ float cap_score(const ScoreMap& m, float z) {
-    const float r = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z));
-    return __builtin_fmaf(-2.0f * m.cap, r, m.cap);
+// What x starts a maximum as, what stands for an unseen key, and the larger score.
+template <int kMode>
+__device__ __forceinline__ float unseen() {
+    return kMode == kCapped ? inf() : -inf();
+}
+template <int kMode>
+__device__ __forceinline__ float larger(float x, float y) {
+    return kMode == kCapped ? __builtin_fminf(x, y) : __builtin_fmaxf(x, y);
 }
 
 // The closed form is off by about 2^-23 cap, which a wide cap makes large beside
@@ -120,23 +129,49 @@ __device__ __forceinline__ float wide_cap(const ScoreMap& m, float z, float t) {
     return __builtin_fabsf(y) < 0.25f ? m.cap * f : t;
 }
 
-// N products of one row, key i of them away(i) positions before the row.
-template <int kMode, int N, class Away>
-__device__ __forceinline__ void map_scores(const ScoreMap& m, float (&x)[N], Away away) {
+// Products x of one row with N keys, key i of them at[i] places after a first
+// one that lies `away` positions before the row; 8-bit keys' products come
+// multiplied by the key's scale and m.factor.  `behind`: none of the keys lies
+// ahead of any of the wave's rows.
+template <int kMode, bool kBytes, int N, class At>
+__device__ __forceinline__ void map_scores(const ScoreMap& m, float (&x)[N], float away, At at,
+                                           bool behind) {
     if constexpr (kMode == kPlain) return;
+    if constexpr (kMode == kCapped) {
+        // tanh(y) = 1 - 2 / (1 + e^(2 y)), and x is the quotient; e^(2 y) may be infinite
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        if constexpr (kMode == kCapped) {
-            x[i] = cap_score(m, x[i] * m.cap_in);
-        } else if constexpr (kMode == kSloped) {
-            x[i] = __builtin_fmaf(-m.slope, __builtin_fabsf(away(i)),
-                                  x[i] * m.scale);
+        for (int i = 0; i < N; ++i) {
+            const float z = kBytes ? x[i] : x[i] * m.factor;
+            x[i] = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z));
+        }
+    } else if constexpr (kMode == kSloped) {
+        const float f = kBytes ? 1.0f : m.factor;
+        if (behind) {
+            // the distance is away - at: a term of the key and one of the row
+            const float row = -m.slope * away;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float bias = __builtin_fmaf(m.slope, static_cast<float>(at(i)), row);
+                x[i] = kBytes ? x[i] + bias : __builtin_fmaf(x[i], f, bias);
+            }
         } else {
-            const float z = x[i] * m.cap_in, t = cap_score(m, z);
-            const float y = !m.capped ? x[i] * m.scale : m.wide ? wide_cap(m, z, t) : t;
-            x[i] = m.sloped
-                       ? __builtin_fmaf(-m.slope, __builtin_fabsf(away(i)), y)
-                       : y;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float d = __builtin_fabsf(away - static_cast<float>(at(i)));
+                x[i] = __builtin_fmaf(-m.slope, d, kBytes ? x[i] : x[i] * f);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            float t = kBytes ? x[i] : x[i] * m.factor;
+            if (m.capped) {
+                const float r = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(t));
+                const float near = __builtin_fmaf(-2.0f * m.cap, r, m.cap);
+                t = m.wide ? wide_cap(m, t, near) : near;
+            }
+            const float d = __builtin_fabsf(away - static_cast<float>(at(i)));
+            x[i] = m.sloped ? __builtin_fmaf(-m.slope, d, t) : t;
         }
     }
 }
@@ -290,6 +325,7 @@ __global__ __launch_bounds__(kSplitThreads) void es_kv_split_kernel(AttendArgs a
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 15, g = lane >> 4;
+    const int base_key = (kBytes ? 16 : 8) * g;              // of this lane's keys in a block
     const uint32_t h = blockIdx.x % a.c.heads;
 
     const Place at = find_place<true>(a, kRowsOfTile, blockIdx.x / a.c.heads);
@@ -310,7 +346,7 @@ __global__ __launch_bounds__(kSplitThreads) void es_kv_split_kernel(AttendArgs a
         const uint32_t head = h * a.group + (r - i * static_cast<int>(a.group));
         interval(a, at.seq, i, first[t], limit[t]);
         pos[t] = at.seq.len - at.seq.n + i;
-        map[t] = score_map<kMode>(a, head);
+        map[t] = score_map<kMode, kBytes>(a, head);
         if (first[t] < limit[t]) {
             lo_any = min(lo_any, first[t]);
             hi_any = max(hi_any, limit[t]);
@@ -388,8 +424,19 @@ __global__ __launch_bounds__(kSplitThreads) void es_kv_split_kernel(AttendArgs a
                 vs[t] = load<f32x4_t>(a.c.vs + token + 16 * g + 4 * t);
             }
         }
+        const int left = bad ? 0 : at.seq.len - key0;        // tokens of the block
 
         const bool masked = key0 < lo_all || key0 + kBlock > hi_all;
+        if constexpr (kBytes) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t) ks[t] *= map[0].factor;
+            if (left < kBlock) {
+                // slots past the sequence's end may hold anything
+#pragma unroll
+                for (int t = 0; t < 16; ++t)
+                    if (16 * g + t >= left) vs[t >> 2][t & 3] = 0.0f;
+            }
+        }
         bf16x8_t p[kTiles][2];
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) {
@@ -412,30 +459,30 @@ __global__ __launch_bounds__(kSplitThreads) void es_kv_split_kernel(AttendArgs a
                     }
                 }
             }
-            // scores of this lane's 16 keys: key_of(4 k + i) in s[k][i]
-            auto key_of = [&](int x) {
-                const int k = x >> 2, i = x & 3;
-                return key0 + (kBytes ? 16 * g + 4 * k + i
-                                      : 32 * (k >> 1) + 8 * g + 4 * (k & 1) + i);
+            // scores of this lane's 16 keys: key0 + base_key + place(i)
+            auto place = [](int i) {
+                return kBytes ? i : 32 * (i >> 3) + (i & 7);
             };
             float x[16];
 #pragma unroll
             for (int k = 0; k < 16; ++k)
                 x[k] = kBytes ? s[k >> 2][k & 3] * ks[k >> 2][k & 3] : s[k >> 2][k & 3];
-            map_scores<kMode>(map[t], x, [&](int k) { return static_cast<float>(pos[t] - key_of(k)); });
+            map_scores<kMode, kBytes>(map[t], x, static_cast<float>(pos[t] - key0 - base_key),
+                                      place, false);
             if (bad) {
 #pragma unroll
                 for (int k = 0; k < 16; ++k) x[k] = nan();
             }
             if (masked) {
+                const int from = first[t] - key0 - base_key, to = limit[t] - key0 - base_key;
 #pragma unroll
                 for (int k = 0; k < 16; ++k)
-                    if (key_of(k) < first[t] || key_of(k) >= limit[t]) x[k] = -inf();
+                    if (place(k) < from || place(k) >= to) x[k] = unseen<kMode>();
             }
-            float peak = -inf();
+            float peak = x[0];
 #pragma unroll
-            for (int k = 0; k < 16; ++k) peak = __builtin_fmaxf(peak, x[k]);
-            peak *= map[t].unit;
+            for (int k = 1; k < 16; ++k) peak = larger<kMode>(peak, x[k]);
+            peak = __builtin_fmaf(peak, map[t].unit, map[t].offset);
             peak = __builtin_fmaxf(peak, __shfl_xor(peak, 16));
             peak = __builtin_fmaxf(peak, __shfl_xor(peak, 32));
             const float now = __builtin_fmaxf(top[t], peak);
@@ -458,10 +505,9 @@ __global__ __launch_bounds__(kSplitThreads) void es_kv_split_kernel(AttendArgs a
                     for (int y = 0; y < 2; ++y) {
                         const int k = 2 * u + (j >> 1), i = 2 * (j & 1) + y;
                         e[y] = __builtin_amdgcn_exp2f(
-                            __builtin_fmaf(x[4 * k + i], map[t].unit, -base));
+                            __builtin_fmaf(x[4 * k + i], map[t].unit, map[t].offset - base));
                         sum[t] += e[y];
-                        // a weight of zero stays zero whatever stands in a slot unseen
-                        if constexpr (kBytes) e[y] = e[y] == 0.0f ? 0.0f : e[y] * vs[k][i];
+                        if constexpr (kBytes) e[y] *= vs[k][i];
                     }
                     w[j] = pack_bf16(e[0], e[1]);
                 }
@@ -469,9 +515,7 @@ __global__ __launch_bounds__(kSplitThreads) void es_kv_split_kernel(AttendArgs a
             }
         }
         if (bad && a.status != nullptr && lane == 0) atomicOr(a.status, ES_KV_BAD_PAGE);
-        if (bad || key0 + kBlock > at.seq.len) {
-            // slots past the sequence's end may hold anything
-            const int left = bad ? 0 : at.seq.len - key0;
+        if (left < kBlock) {
 #pragma unroll
             for (int w = 0; w < kValWords; ++w) {
                 const u32x4_t keep = token_mask<kFmt>(left - (kBytes ? 16 * g : 32 * w + 8 * g));
@@ -720,7 +764,11 @@ es_kv_tile_kernel(AttendArgs a) {
     int first, limit;
     interval(a, at.seq, i, first, limit);
     const int pos = at.seq.len - at.seq.n + i;
-    const ScoreMap map = score_map<kMode>(a, head);
+    const ScoreMap map = score_map<kMode, kBytes>(a, head);
+    // positions grow with rows.  Steep slopes take distances one by one: a block's
+    // term of the row rounds to 2^-24 of up to 128 slopes
+    const int pos_first =
+        __any(map.slope > 4.0f || map.slope < -4.0f) ? -1 : __builtin_amdgcn_readfirstlane(pos);
 
     bf16x8_t q[kSteps];
     {
@@ -809,7 +857,9 @@ es_kv_tile_kernel(AttendArgs a) {
         if (bad_next && a.status != nullptr && threadIdx.x == 0)
             atomicOr(a.status, ES_KV_BAD_PAGE);
     };
-    auto stage = [&](uint8_t* buf, float* scales) {
+    // (keys' scales carry the scores' first factor; values' past the sequence's
+    // end, where slots may hold anything, are 0)
+    auto stage = [&](int b, uint8_t* buf, float* scales) {
         if constexpr (kBytes) {
 #pragma unroll
             for (int x = 0; x < kStage; ++x) {
@@ -825,7 +875,11 @@ es_kv_tile_kernel(AttendArgs a) {
                 *reinterpret_cast<u32x4_t*>(buf + S::kKeyBytes + val_word(vr, 2 * vc + 1)) =
                     codes_to_bf16<kFmt>(u32x2_t{sv[x][2], sv[x][3]});
             }
-            if (threadIdx.x < 2 * kBlock) scales[threadIdx.x] = sscale;
+            if (threadIdx.x < kBlock)
+                scales[threadIdx.x] = sscale * map.factor;
+            else if (threadIdx.x < 2 * kBlock)
+                scales[threadIdx.x] =
+                    bad_next || b * kBlock + int(threadIdx.x) - kBlock >= at.seq.len ? 0.0f : sscale;
         }
     };
     // the block has landed in LDS for every wave
@@ -847,7 +901,7 @@ es_kv_tile_kernel(AttendArgs a) {
 
     if (b_begin < b_end) {
         fetch(b_begin, lds);
-        stage(lds, scales0);
+        stage(b_begin, lds, scales0);
         arrive();
     }
     for (int b = b_begin; b < b_end; ++b) {
@@ -894,9 +948,8 @@ es_kv_tile_kernel(AttendArgs a) {
                 }
             }
             const float away = static_cast<float>(pos - (key0 + 8 * g));
-            map_scores<kMode>(map, x, [&](int y) {
-                return away - static_cast<float>(32 * (y >> 4) + 16 * ((y >> 3) & 1) + (y & 7));
-            });
+            auto place = [](int y) { return 32 * (y >> 4) + 16 * ((y >> 3) & 1) + (y & 7); };
+            map_scores<kMode, kBytes>(map, x, away, place, key0 + kBlock - 1 <= pos_first);
             if (bad) {
 #pragma unroll
                 for (int y = 0; y < 32; ++y) x[y] = nan();
@@ -906,14 +959,14 @@ es_kv_tile_kernel(AttendArgs a) {
                 const int from = first - (key0 + 8 * g), to = limit - (key0 + 8 * g);
 #pragma unroll
                 for (int y = 0; y < 32; ++y) {
-                    const int k = 32 * (y >> 4) + 16 * ((y >> 3) & 1) + (y & 7);
-                    if (k < from || k >= to) x[y] = -inf();
+                    if (place(y) < from || place(y) >= to) x[y] = unseen<kMode>();
                 }
             }
             float peak = x[0];
 #pragma unroll
-            for (int y = 1; y < 32; ++y) peak = __builtin_fmaxf(peak, x[y]);
-            const float now = __builtin_fmaxf(top, max_halves(peak) * map.unit);
+            for (int y = 1; y < 32; ++y) peak = larger<kMode>(peak, x[y]);
+            peak = max_halves(__builtin_fmaf(peak, map.unit, map.offset));
+            const float now = __builtin_fmaxf(top, peak);
             if (__any(now > top + kSlack)) {
                 const float shrink = __builtin_amdgcn_exp2f(top - (now == -inf() ? 0.0f : now));
                 sum *= shrink;
@@ -922,7 +975,7 @@ es_kv_tile_kernel(AttendArgs a) {
                 top = now;
             }
             // nothing seen so far: any finite stand-in gives weights of zero
-            const float base = top == -inf() ? 0.0f : top;
+            const float base = map.offset - (top == -inf() ? 0.0f : top);
             bf16x8_t p[4];
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
@@ -936,10 +989,9 @@ es_kv_tile_kernel(AttendArgs a) {
 #pragma unroll
                     for (int y = 0; y < 4; ++y) {
                         e[y] = __builtin_amdgcn_exp2f(
-                            __builtin_fmaf(x[8 * u + 4 * j + y], map.unit, -base));
+                            __builtin_fmaf(x[8 * u + 4 * j + y], map.unit, base));
                         sum += e[y];
-                        // a weight of zero stays zero whatever stands in a slot unseen
-                        if constexpr (kBytes) e[y] = e[y] == 0.0f ? 0.0f : e[y] * v4[y];
+                        if constexpr (kBytes) e[y] *= v4[y];
                     }
                     w[2 * j] = pack_bf16(e[0], e[1]);
                     w[2 * j + 1] = pack_bf16(e[2], e[3]);
@@ -955,7 +1007,7 @@ es_kv_tile_kernel(AttendArgs a) {
                     o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p[u], o[d], 0, 0, 0);
                 }
         }
-        if (more) stage(lds + (cur ^ 1) * S::kBuffer, scales0 + (cur ^ 1) * 128);
+        if (more) stage(b + 1, lds + (cur ^ 1) * S::kBuffer, scales0 + (cur ^ 1) * 128);
         arrive();
     }
 

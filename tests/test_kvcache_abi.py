@@ -139,7 +139,7 @@ def _attend(**kw):
     (dict(n_seqs=65537), E, "n_seqs"), (dict(q_heads=0), E, "q_heads"), (dict(q_heads=3), E, "q_heads"),
     (dict(q_heads=130), E, "q_heads"), (dict(scale=float("inf")), E, "scale"),
     (dict(scale=float("nan")), E, "scale"), (dict(cap=-1.0), E, "cap"),
-    (dict(cap=float("nan")), E, "cap"), (dict(cap=float("inf")), E, "cap"),
+    (dict(cap=float("nan")), E, "cap"), (dict(cap=1e-20), E, "cap"), (dict(cap=float("inf")), E, "cap"),
     (dict(table_stride=0), E, "table_stride"), (dict(q=None), E, "null"), (dict(out=None), E, "null"),
     (dict(tables=None), E, "null"), (dict(lengths=None), E, "null"), (dict(starts=None), E, "null"),
     (dict(out_stride=255), E, "overlap"), (dict(out=0x20001), esopt.ES_ERR_ALIGN, "aligned"),
