@@ -827,31 +827,36 @@ es_kv_tile_kernel(AttendArgs a) {
     float sscale = 0.0f;
     bool bad = false, bad_next = false;
     const int32_t* table = a.tables + uint64_t(at.s) * a.table_stride;
-    auto fetch = [&](int b, uint8_t* buf) {
-        const int key0 = b * kBlock;
-        const uint32_t page = load_uniform(table + (key0 >> a.c.page_shift));
+    // a block's page, asked for a block ahead of its keys and values
+    auto page_of = [&](int b) -> uint32_t {
+        return b < b_end ? load_uniform(table + ((b * kBlock) >> a.c.page_shift)) : 0u;
+    };
+    auto fetch = [&](int b, uint32_t page, uint8_t* buf) {
         bad_next = page >= a.c.n_pages;
         const uint64_t head_at = uint64_t(bad_next ? 0u : page) * a.c.heads + h;
-        const uint32_t off = uint32_t(key0) & (a.c.page - 1);
-        const uint64_t token = head_at * a.c.page + off;
-        const uint8_t* ksrc = a.c.k + token * (D * kCodeBytes<kFmt>);
-        const uint8_t* vsrc = a.c.v + (head_at * D * a.c.page + off) * kCodeBytes<kFmt>;
+        const uint32_t off = uint32_t(b * kBlock) & (a.c.page - 1);
+        const uint64_t token = (head_at << a.c.page_shift) + off;
+        const Buffer keys = buffer_of(a.c.k + token * (D * kCodeBytes<kFmt>),
+                                      kBlock * D * kCodeBytes<kFmt>);
+        const Buffer values =
+            buffer_of(a.c.v + ((head_at << a.c.page_shift) * D + off) * kCodeBytes<kFmt>,
+                      val_row * D - off * kCodeBytes<kFmt>);
         if constexpr (kBytes) {
 #pragma unroll
             for (int x = 0; x < kStage; ++x) {
-                const int w = threadIdx.x + S::kThreads * x;
-                sk[x] = load<u32x4_t>(ksrc + 16 * w);
-                sv[x] = load<u32x4_t>(vsrc + uint32_t(w / kValWords) * val_row +
-                                      16 * (w % kValWords));
+                const uint32_t w = threadIdx.x + S::kThreads * x;
+                sk[x] = load_buffer(keys, 16 * w);
+                sv[x] = load_buffer(values, (w / kValWords) * val_row + 16 * (w % kValWords));
             }
             if (threadIdx.x < 2 * kBlock)
-                sscale = load<float>((threadIdx.x < kBlock ? a.c.ks : a.c.vs) + token +
-                                     (threadIdx.x & (kBlock - 1)));
+                sscale = load_buffer_float(
+                    buffer_of((wave < kBlock / 64 ? a.c.ks : a.c.vs) + token, 4 * kBlock),
+                    4 * (threadIdx.x & (kBlock - 1)));
         } else {
 #pragma unroll
             for (int x = 0; x < kStage; ++x) {
-                load_to_lds(ksrc + k_off[x], buf + (wave * kStage + x) * 1024);
-                load_to_lds(vsrc + v_off[x], buf + S::kKeyBytes + (wave * kStage + x) * 1024);
+                load_to_lds(keys, k_off[x], buf + (wave * kStage + x) * 1024);
+                load_to_lds(values, v_off[x], buf + S::kKeyBytes + (wave * kStage + x) * 1024);
             }
         }
         if (bad_next && a.status != nullptr && threadIdx.x == 0)
@@ -899,8 +904,9 @@ es_kv_tile_kernel(AttendArgs a) {
     // the key that row m of a tile of S^T stands for: bits 2 and 3 exchanged
     const int krow = (n & 0x13) | ((n & 4) << 1) | ((n & 8) >> 1);
 
+    uint32_t page = page_of(b_begin + 1);
     if (b_begin < b_end) {
-        fetch(b_begin, lds);
+        fetch(b_begin, page_of(b_begin), lds);
         stage(b_begin, lds, scales0);
         arrive();
     }
@@ -911,7 +917,8 @@ es_kv_tile_kernel(AttendArgs a) {
         const bool more = b + 1 < b_end;
         const int key0 = b * kBlock;
         bad = bad_next;
-        if (more) fetch(b + 1, lds + (cur ^ 1) * S::kBuffer);
+        if (more) fetch(b + 1, page, lds + (cur ^ 1) * S::kBuffer);
+        page = page_of(b + 2);
         if (bad || key0 + kBlock > at.seq.len) {
             // slots past the sequence's end may hold anything: their values are cleared
             const int left = bad ? 0 : at.seq.len - key0;
@@ -925,15 +932,23 @@ es_kv_tile_kernel(AttendArgs a) {
         if (key0 < hi_any && key0 + kBlock > lo_any) {
             f32x16_t s[2];
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
+            for (int c = 0; c < kSteps; ++c)
 #pragma unroll
-                for (int c = 0; c < kSteps; ++c) {
+                for (int t = 0; t < 2; ++t) {
                     const bf16x8_t k = *reinterpret_cast<const bf16x8_t*>(
                         buf + key_word<D>(32 * t + krow, 2 * c + g));
                     s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[c], c == 0 ? f32x16_t{} : s[t],
                                                                    0, 0, 0);
                 }
+            // four words of keys ahead of the products that take them
+            constexpr int kDsRead = 0x100, kMatrix = 0x8;
+            __builtin_amdgcn_sched_group_barrier(kDsRead, 4, 0);
+#pragma unroll
+            for (int c = 0; c < 2 * kSteps - 4; ++c) {
+                __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(kDsRead, 1, 0);
             }
+            __builtin_amdgcn_sched_group_barrier(kMatrix, 4, 0);
             // register x of tile t: key 32 t + 16 (x / 8) + 8 g + x % 8
             float x[32];
 #pragma unroll

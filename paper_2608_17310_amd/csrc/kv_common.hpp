@@ -64,14 +64,27 @@ constexpr float kTinyRow = 0x1p-100f;       // rows whose largest |x| is below r
 
 constexpr float kLog2e = 1.4426950408889634f;
 
+// `bytes` bytes of global memory as the buffer instructions address them: a base
+// in scalar registers and one 32-bit offset a lane, so that a wave's loads need no
+// 64-bit address arithmetic.
+typedef __amdgpu_buffer_rsrc_t Buffer;
+__device__ __forceinline__ Buffer buffer_of(const void* base, uint32_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, bytes, 0x00020000);
+}
+__device__ __forceinline__ u32x4_t load_buffer(Buffer b, uint32_t offset) {
+    return __builtin_amdgcn_raw_buffer_load_b128(b, offset, 0, 0);
+}
+__device__ __forceinline__ float load_buffer_float(Buffer b, uint32_t offset) {
+    return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(b, offset, 0, 0));
+}
 // 16 bytes a lane from memory into LDS, at `dst` (the same for the wave) + 16 lane,
 // without passing registers; wait_loads() before the wave's own barrier.
-__device__ __forceinline__ void load_to_lds(const void* src, void* dst) {
-    __builtin_amdgcn_global_load_lds(
-        reinterpret_cast<const ESKV_GLOBAL void*>(reinterpret_cast<uintptr_t>(src)),
+__device__ __forceinline__ void load_to_lds(Buffer b, uint32_t offset, void* dst) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(
+        b,
         reinterpret_cast<__attribute__((address_space(3))) void*>(
             static_cast<uint32_t>(reinterpret_cast<uintptr_t>(dst))),
-        16, 0, 0);
+        16, offset, 0, 0, 0);
 }
 __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
