@@ -31,9 +31,9 @@ struct es_kv {
 
 namespace {
 
-// Tiles of 16 rows that a wave of the split kernel holds at most: one of wide heads, whose
-// keys, values and accumulators fill the registers.
-constexpr uint32_t split_tiles_max(uint32_t dim) { return dim == 256 ? 1 : 2; }
+// Tiles of 16 rows that a wave of the split kernel holds at most: two of wide heads, whose
+// keys, values and accumulators are twice as long.
+constexpr uint32_t split_tiles_max(uint32_t dim) { return dim == 256 ? 2 : 4; }
 
 int check_kv_device(const es_kv_t* kv, const char* name) {
     int dev = -1;
@@ -90,7 +90,7 @@ template <int T, int kMode>
 struct MakeSplit {
     template <int D, int F>
     struct Of {
-        static AttendKernel get() { return es_kv_split_kernel<D, (D == 256 ? 1 : T), F, kMode>; }
+        static AttendKernel get() { return es_kv_split_kernel<D, (D == 256 && T > 2 ? 2 : T), F, kMode>; }
     };
 };
 template <int kMode>
@@ -363,15 +363,17 @@ int es_kv_attend(es_kv_t* kv, const es_kv_attend_t* args, es_stream_t stream) tr
     const uint64_t all_rows = uint64_t(x.rows) * a.group;      // of one key head
     const uint64_t seq_rows = std::min<uint64_t>(x.rows, std::max(1u, x.max_rows)) * a.group;
     if (seq_rows <= 64) {
-        const uint32_t tiles = seq_rows <= 16 ? 1 : split_tiles_max(dim);
-        // a history's scores cost nothing beside its bytes: one kernel for every mode but plain
+        const uint32_t tiles = seq_rows <= 16 ? 1 : seq_rows <= 32 ? 2 : split_tiles_max(dim);
+        // a history's scores cost little beside its bytes: one kernel for every mode but plain
+        const bool plain = mode == kPlain;
         const AttendKernel kernel =
-            tiles == 1 ? (mode == kPlain
-                              ? by_dim_format<AttendKernel, MakeSplit<1, kPlain>::Of>(dim, format)
-                              : by_dim_format<AttendKernel, MakeSplit<1, kAny>::Of>(dim, format))
-                       : (mode == kPlain
-                              ? by_dim_format<AttendKernel, MakeSplit<2, kPlain>::Of>(dim, format)
-                              : by_dim_format<AttendKernel, MakeSplit<2, kAny>::Of>(dim, format));
+            tiles == 1 ? (plain ? by_dim_format<AttendKernel, MakeSplit<1, kPlain>::Of>(dim, format)
+                                : by_dim_format<AttendKernel, MakeSplit<1, kAny>::Of>(dim, format))
+            : tiles == 2
+                ? (plain ? by_dim_format<AttendKernel, MakeSplit<2, kPlain>::Of>(dim, format)
+                         : by_dim_format<AttendKernel, MakeSplit<2, kAny>::Of>(dim, format))
+                : (plain ? by_dim_format<AttendKernel, MakeSplit<4, kPlain>::Of>(dim, format)
+                         : by_dim_format<AttendKernel, MakeSplit<4, kAny>::Of>(dim, format));
         const uint32_t tile_rows = 16 * tiles;
         // tiles of all sequences at most, and parts: one more than its share for each
         const uint64_t n_tiles = all_rows / tile_rows + x.n_seqs;

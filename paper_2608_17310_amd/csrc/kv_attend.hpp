@@ -176,6 +176,23 @@ __device__ __forceinline__ void map_scores(const ScoreMap& m, float (&x)[N], flo
     }
 }
 
+// A running maximum is kept until a score exceeds it by this much (log2): weights
+// are at most 2^8 then, and the accumulators are seldom rescaled.
+constexpr float kSlack = 8.0f;
+
+// The larger of a value and the other half-wave's.
+__device__ __forceinline__ float max_halves(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false,
+                                                    false);
+    return __builtin_fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+// The largest of a value in the four lanes of a column of a 16-wide tile.
+__device__ __forceinline__ float max_quarters(float x) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false,
+                                                    false);
+    return max_halves(__builtin_fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+
 // ----------------------------------------------------------------------------
 // Few rows over long histories: the keys of every sequence are cut into parts,
 // a workgroup each, and joined by a second kernel.  Bound by the cache's bytes:
@@ -191,6 +208,12 @@ __device__ __forceinline__ void map_scores(const ScoreMap& m, float (&x)[N], flo
 constexpr int kSplitThreads = 256;
 constexpr int kSplitWaves = kSplitThreads / 64;
 constexpr int kScanRows = 64;               // rows of a sequence whose intervals the scan reads
+
+// Waves of a SIMD that the registers leave.
+template <int D, int kTiles, int kFmt>
+constexpr int split_waves() {
+        return D * kTiles <= 64 ? 4 : D * kTiles <= 128 ? (kFmt == kBf16 ? 3 : 2) : D * kTiles <= 256 ? 2 : 1;
+}
 
 struct Span {                               // a sequence's blocks
     Seq seq;
@@ -226,15 +249,23 @@ __device__ __forceinline__ Span read_span(const AttendArgs& a, uint32_t s, int t
     return p;
 }
 
-__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {          // inclusive
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int m = 1; m < 64; m *= 2) {
-        const uint32_t y = __shfl_up(x, m);
-        if (lane >= m) x += y;
-    }
-    return x;
+// Inclusive sums over the lanes of a wave, in six adds of neighbouring registers:
+// within rows of 16 lanes, then each row's last lane into the next rows.
+template <int kControl, int kRows>
+__device__ __forceinline__ uint32_t add_moved(uint32_t x) {
+    return x + static_cast<uint32_t>(__builtin_amdgcn_update_dpp(
+                   0, static_cast<int>(x), kControl, kRows, 0xF, false));
 }
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
+    constexpr int kRowShr = 0x110, kRowBcast15 = 0x142, kRowBcast31 = 0x143;
+    x = add_moved<kRowShr | 1, 0xF>(x);
+    x = add_moved<kRowShr | 2, 0xF>(x);
+    x = add_moved<kRowShr | 4, 0xF>(x);
+    x = add_moved<kRowShr | 8, 0xF>(x);
+    x = add_moved<kRowBcast15, 0xA>(x);
+    return add_moved<kRowBcast31, 0xC>(x);
+}
+
 __device__ __forceinline__ int from_lane(int x, int lane) {
     return __builtin_amdgcn_readlane(x, lane);
 }
@@ -254,18 +285,25 @@ struct Place {
 template <bool kParts>
 __device__ __forceinline__ Place find_place(const AttendArgs& a, int tile_rows, uint32_t unit) {
     const uint32_t lane = threadIdx.x & 63;
-    Span mine = read_span(a, lane, tile_rows);
-    uint64_t total = uint64_t(mine.blocks) * mine.tiles;
-    for (uint32_t s0 = 64; s0 < a.n_seqs; s0 += 64) {
-        const Span p = read_span(a, s0 + lane, tile_rows);
-        total += uint64_t(p.blocks) * p.tiles;
+    const Span mine = read_span(a, lane, tile_rows);
+    // all blocks of one head, a wave's sum at a time (tiles and blocks of a sequence
+    // are below 2^26 and 2^25: sums are held in 64 bits, in two halves a lane)
+    uint64_t total = 0;
+    for (uint32_t s0 = 0; s0 < a.n_seqs; s0 += 64) {
+        const Span p = s0 == 0 ? mine : read_span(a, s0 + lane, tile_rows);
+        const uint64_t work = uint64_t(p.blocks) * p.tiles;
+        const uint32_t lo = wave_scan(static_cast<uint32_t>(work & 0xFFFFFFu));
+        const uint32_t hi = wave_scan(static_cast<uint32_t>(work >> 24) & 0x3FFFFFFu);
+        total += (uint64_t(from_lane(hi, 63)) << 24) + uint32_t(from_lane(lo, 63));
     }
-#pragma unroll
-    for (int m = 1; m < 64; m *= 2) total += __shfl_xor(total, m);
-    total *= a.c.heads;
-    const uint64_t per64 = max((total + a.target - 1) / a.target, uint64_t(a.min_blocks));
+    // 32 bits hold the quotients: 2^51 blocks over at least 2^5 parts of at most 2^26 tiles each
+    // would not fit, but no cache holds them (2^31 tokens: 2^25 blocks, 2^26 tiles of rows)
+    const uint64_t all = total * a.c.heads;
+    uint32_t per = a.min_blocks;
+    if (all > uint64_t(a.min_blocks) * a.target)
+        per = static_cast<uint32_t>(min((all + a.target - 1) / a.target, uint64_t(1) << 30));
     Place r;
-    r.per = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(per64));
+    r.per = __builtin_amdgcn_readfirstlane(per);
     r.found = false;
     uint32_t units0 = 0, slots0 = 0;
     for (uint32_t s0 = 0; s0 < a.n_seqs; s0 += 64) {
@@ -314,18 +352,22 @@ __device__ __forceinline__ u32x4_t token_mask(int n) {
 }
 
 template <int D, int kTiles, int kFmt, int kMode>
-__global__ __launch_bounds__(kSplitThreads) void es_kv_split_kernel(AttendArgs a) {
+__global__ __launch_bounds__(kSplitThreads, (split_waves<D, kTiles, kFmt>())) void es_kv_split_kernel(AttendArgs a) {
     constexpr int kRowsOfTile = 16 * kTiles;
     constexpr int kSteps = D / 32;                           // 32 dimensions a product
     constexpr int kDims = D / 16;                            // 16 dimensions a tile of O^T
     constexpr bool kBytes = kFmt != kBf16;
-    // 16-byte words of a lane: of a key's row, and of a dimension's 64 tokens
-    constexpr int kKeyWords = kBytes ? kSteps / 2 : kSteps;
-    constexpr int kValWords = kBytes ? 1 : 2;
+    // A step takes 4 L keys, as tiles of 16: a lane holds L tokens of each of its
+    // dimensions, 16 bytes, or 8 where the registers leave no room for more
+    constexpr int L = kBytes && D * kTiles <= 128 ? 16 : 8;
+    constexpr int kKeys = 4 * L, kKeyTiles = L / 4, kPairs = L / 8;
+    typedef uint32_t Tokens __attribute__((ext_vector_type(L * kCodeBytes<kFmt> / 4)));
+    constexpr int kRowBytes = D * kCodeBytes<kFmt>;
+    constexpr int kKeyWords = kRowBytes / 64;                // 16-byte words of a lane of a key's row
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 15, g = lane >> 4;
-    const int base_key = (kBytes ? 16 : 8) * g;              // of this lane's keys in a block
+    const int base_key = L * g;                              // of this lane's keys in a step
     const uint32_t h = blockIdx.x % a.c.heads;
 
     const Place at = find_place<true>(a, kRowsOfTile, blockIdx.x / a.c.heads);
@@ -383,131 +425,134 @@ __global__ __launch_bounds__(kSplitThreads) void es_kv_split_kernel(AttendArgs a
         for (int d = 0; d < kDims; ++d) o[t][d] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
     }
 
-    const int b_end0 = at.block0 + at.blocks;
-    const int b_begin = at.block0 + static_cast<int>(at.chunk * at.per);
-    const int b_end = min(b_end0, b_begin + static_cast<int>(at.per));
+    // the part's keys that some row of the tile sees, in whole steps
+    const int part0 = at.block0 + static_cast<int>(at.chunk * at.per);
+    const int part1 = min(at.block0 + at.blocks, part0 + static_cast<int>(at.per));
+    const int k_begin = max(part0 * kBlock, lo_any / kKeys * kKeys);
+    const int k_end = min(part1 * kBlock, hi_any);
     const int32_t* table = a.tables + uint64_t(at.s) * a.table_stride;
-    for (int b = b_begin + wave; b < b_end; b += kSplitWaves) {
-        const int key0 = b * kBlock;
-        if (key0 >= hi_any || key0 + kBlock <= lo_any) continue;
-        const uint32_t page = load_uniform(table + (key0 >> a.c.page_shift));
+    const uint32_t val_row = a.c.page * kCodeBytes<kFmt>;    // bytes of a dimension's page
+    const uint32_t k_off = (L * (n >> 2) + (n & 3)) * kRowBytes + 16 * g;
+    const uint32_t v_off = n * val_row + base_key * kCodeBytes<kFmt>;
+    auto page_of = [&](int key0) -> uint32_t {
+        return key0 < k_end ? load_uniform(table + (key0 >> a.c.page_shift)) : 0u;
+    };
+    uint32_t page = page_of(k_begin + wave * kKeys);
+    for (int key0 = k_begin + wave * kKeys; key0 < k_end; key0 += kSplitWaves * kKeys) {
         const bool bad = page >= a.c.n_pages;
         const uint64_t head_at = uint64_t(bad ? 0u : page) * a.c.heads + h;
+        page = page_of(key0 + kSplitWaves * kKeys);
         const uint32_t off = uint32_t(key0) & (a.c.page - 1);
-        const uint64_t token = head_at * a.c.page + off;
+        const uint64_t token = (head_at << a.c.page_shift) + off;
 
-        // the block's keys: word w of the key that row n of tile t stands for
-        u32x4_t kw[4][kKeyWords];
+        // the step's keys: word w of the key that row n of tile t stands for
+        const Buffer keys = buffer_of(a.c.k + token * kRowBytes, kKeys * kRowBytes);
+        u32x4_t kw[kKeyTiles][kKeyWords];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const int key = kBytes ? 16 * (n >> 2) + 4 * t + (n & 3)
-                                   : 32 * (t >> 1) + 8 * (n >> 2) + 4 * (t & 1) + (n & 3);
-            const uint8_t* src = a.c.k + (token + key) * (D * kCodeBytes<kFmt>) + 16 * g;
+        for (int t = 0; t < kKeyTiles; ++t)
 #pragma unroll
-            for (int w = 0; w < kKeyWords; ++w) kw[t][w] = load<u32x4_t>(src + 64 * w);
-        }
-        // its values: dimension 16 d + n, this lane's tokens
-        u32x4_t vw[kDims][kValWords];
-        const uint8_t* vsrc =
-            a.c.v + ((head_at * D + n) * a.c.page + off) * kCodeBytes<kFmt> + 16 * g;
-        const uint64_t vstep = uint64_t(16) * a.c.page * kCodeBytes<kFmt>;
+            for (int w = 0; w < kKeyWords; ++w)
+                kw[t][w] = load_buffer(keys, k_off + 4 * t * kRowBytes + 64 * w);
+        // its values: this lane's tokens of dimension 16 d + n
+        const Buffer values =
+            buffer_of(a.c.v + ((head_at << a.c.page_shift) * D + off) * kCodeBytes<kFmt>,
+                      val_row * D - off * kCodeBytes<kFmt>);
+        Tokens vw[kDims];
 #pragma unroll
         for (int d = 0; d < kDims; ++d)
-#pragma unroll
-            for (int w = 0; w < kValWords; ++w) vw[d][w] = load<u32x4_t>(vsrc + d * vstep + 64 * w);
-        // its scales: this lane's keys are 16 g .. 16 g + 15
-        f32x4_t ks[4], vs[4];
+            vw[d] = load_buffer_as<Tokens>(values, v_off, 16 * d * val_row);
+        // its scales
+        f32x4_t ks[kKeyTiles], vs[kKeyTiles];
         if constexpr (kBytes) {
+            const Buffer k_scales = buffer_of(a.c.ks + token, 4 * kKeys);
+            const Buffer v_scales = buffer_of(a.c.vs + token, 4 * kKeys);
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                ks[t] = load<f32x4_t>(a.c.ks + token + 16 * g + 4 * t);
-                vs[t] = load<f32x4_t>(a.c.vs + token + 16 * g + 4 * t);
+            for (int t = 0; t < kKeyTiles; ++t) {
+                ks[t] = __builtin_bit_cast(f32x4_t, load_buffer(k_scales, 4 * (base_key + 4 * t)));
+                vs[t] = __builtin_bit_cast(f32x4_t, load_buffer(v_scales, 4 * (base_key + 4 * t)));
             }
         }
-        const int left = bad ? 0 : at.seq.len - key0;        // tokens of the block
 
-        const bool masked = key0 < lo_all || key0 + kBlock > hi_all;
+        // tokens of the step: slots past the sequence's end may hold anything
+        const int left = bad ? 0 : at.seq.len - key0;
+        const bool masked = key0 < lo_all || key0 + kKeys > hi_all;
         if constexpr (kBytes) {
 #pragma unroll
-            for (int t = 0; t < 4; ++t) ks[t] *= map[0].factor;
-            if (left < kBlock) {
-                // slots past the sequence's end may hold anything
+            for (int t = 0; t < kKeyTiles; ++t) ks[t] *= map[0].factor;
+            if (left < kKeys) {
 #pragma unroll
-                for (int t = 0; t < 16; ++t)
-                    if (16 * g + t >= left) vs[t >> 2][t & 3] = 0.0f;
+                for (int t = 0; t < L; ++t)
+                    if (base_key + t >= left) vs[t >> 2][t & 3] = 0.0f;
             }
         }
-        bf16x8_t p[kTiles][2];
+        // S^T of every tile of rows: a word of keys is converted once for all of them
+        f32x4_t s[kTiles][kKeyTiles];
 #pragma unroll
-        for (int t = 0; t < kTiles; ++t) {
-            f32x4_t s[4];
+        for (int k = 0; k < kKeyTiles; ++k)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                s[k] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+            for (int w = 0; w < kKeyWords; ++w) {
+                constexpr int kHalves = kBytes ? 2 : 1;
 #pragma unroll
-                for (int w = 0; w < kKeyWords; ++w) {
-                    if constexpr (kBytes) {
-                        const u32x4_t x0 = codes_to_bf16<kFmt>(u32x2_t{kw[k][w][0], kw[k][w][1]});
-                        const u32x4_t x1 = codes_to_bf16<kFmt>(u32x2_t{kw[k][w][2], kw[k][w][3]});
-                        s[k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                            __builtin_bit_cast(bf16x8_t, x0), q[t][2 * w], s[k], 0, 0, 0);
-                        s[k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                            __builtin_bit_cast(bf16x8_t, x1), q[t][2 * w + 1], s[k], 0, 0, 0);
-                    } else {
-                        s[k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                            __builtin_bit_cast(bf16x8_t, kw[k][w]), q[t][w], s[k], 0, 0, 0);
-                    }
+                for (int y = 0; y < kHalves; ++y) {
+                    bf16x8_t x;
+                    if constexpr (kBytes)
+                        x = __builtin_bit_cast(
+                            bf16x8_t,
+                            codes_to_bf16<kFmt>(u32x2_t{kw[k][w][2 * y], kw[k][w][2 * y + 1]}));
+                    else
+                        x = __builtin_bit_cast(bf16x8_t, kw[k][w]);
+#pragma unroll
+                    for (int t = 0; t < kTiles; ++t)
+                        s[t][k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                            x, q[t][kHalves * w + y], w + y == 0 ? f32x4_t{} : s[t][k], 0, 0, 0);
                 }
             }
-            // scores of this lane's 16 keys: key0 + base_key + place(i)
-            auto place = [](int i) {
-                return kBytes ? i : 32 * (i >> 3) + (i & 7);
-            };
-            float x[16];
+        bf16x8_t p[kTiles][kPairs];
 #pragma unroll
-            for (int k = 0; k < 16; ++k)
-                x[k] = kBytes ? s[k >> 2][k & 3] * ks[k >> 2][k & 3] : s[k >> 2][k & 3];
+        for (int t = 0; t < kTiles; ++t) {
+            // scores of this lane's keys key0 + base_key + 0 .. L - 1
+            float x[L];
+#pragma unroll
+            for (int k = 0; k < L; ++k)
+                x[k] = kBytes ? s[t][k >> 2][k & 3] * ks[k >> 2][k & 3] : s[t][k >> 2][k & 3];
             map_scores<kMode, kBytes>(map[t], x, static_cast<float>(pos[t] - key0 - base_key),
-                                      place, false);
+                                      [](int i) { return i; }, false);
             if (bad) {
 #pragma unroll
-                for (int k = 0; k < 16; ++k) x[k] = nan();
+                for (int k = 0; k < L; ++k) x[k] = nan();
             }
             if (masked) {
                 const int from = first[t] - key0 - base_key, to = limit[t] - key0 - base_key;
 #pragma unroll
-                for (int k = 0; k < 16; ++k)
-                    if (place(k) < from || place(k) >= to) x[k] = unseen<kMode>();
+                for (int k = 0; k < L; ++k)
+                    if (k < from || k >= to) x[k] = unseen<kMode>();
             }
             float peak = x[0];
 #pragma unroll
-            for (int k = 1; k < 16; ++k) peak = larger<kMode>(peak, x[k]);
-            peak = __builtin_fmaf(peak, map[t].unit, map[t].offset);
-            peak = __builtin_fmaxf(peak, __shfl_xor(peak, 16));
-            peak = __builtin_fmaxf(peak, __shfl_xor(peak, 32));
+            for (int k = 1; k < L; ++k) peak = larger<kMode>(peak, x[k]);
+            peak = max_quarters(__builtin_fmaf(peak, map[t].unit, map[t].offset));
             const float now = __builtin_fmaxf(top[t], peak);
-            // nothing seen so far: any finite stand-in gives weights of zero
-            const float base = now == -inf() ? 0.0f : now;
-            if (__any(now > top[t])) {
-                const float shrink = __builtin_amdgcn_exp2f(top[t] - base);
+            if (__any(now > top[t] + kSlack)) {
+                const float shrink = __builtin_amdgcn_exp2f(top[t] - (now == -inf() ? 0.0f : now));
                 sum[t] *= shrink;
 #pragma unroll
                 for (int d = 0; d < kDims; ++d) o[t][d] *= shrink;
+                top[t] = now;
             }
-            top[t] = now;
+            // nothing seen so far: any finite stand-in gives weights of zero
+            const float base = map[t].offset - (top[t] == -inf() ? 0.0f : top[t]);
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
+            for (int u = 0; u < kPairs; ++u) {
                 u32x4_t w;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     float e[2];
 #pragma unroll
                     for (int y = 0; y < 2; ++y) {
-                        const int k = 2 * u + (j >> 1), i = 2 * (j & 1) + y;
-                        e[y] = __builtin_amdgcn_exp2f(
-                            __builtin_fmaf(x[4 * k + i], map[t].unit, map[t].offset - base));
+                        const int k = 8 * u + 2 * j + y;
+                        e[y] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[k], map[t].unit, base));
                         sum[t] += e[y];
-                        if constexpr (kBytes) e[y] *= vs[k][i];
+                        if constexpr (kBytes) e[y] *= vs[k >> 2][k & 3];
                     }
                     w[j] = pack_bf16(e[0], e[1]);
                 }
@@ -515,31 +560,28 @@ __global__ __launch_bounds__(kSplitThreads) void es_kv_split_kernel(AttendArgs a
             }
         }
         if (bad && a.status != nullptr && lane == 0) atomicOr(a.status, ES_KV_BAD_PAGE);
-        if (left < kBlock) {
+        if (left < kKeys) {
+            const u32x4_t keep = token_mask<kFmt>(left - base_key);
 #pragma unroll
-            for (int w = 0; w < kValWords; ++w) {
-                const u32x4_t keep = token_mask<kFmt>(left - (kBytes ? 16 * g : 32 * w + 8 * g));
+            for (int d = 0; d < kDims; ++d)
 #pragma unroll
-                for (int d = 0; d < kDims; ++d) vw[d][w] &= keep;
-            }
+                for (int w = 0; w < L * kCodeBytes<kFmt> / 4; ++w) vw[d][w] &= keep[w];
         }
 #pragma unroll
         for (int d = 0; d < kDims; ++d) {
-            bf16x8_t v[2];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
+            for (int u = 0; u < kPairs; ++u) {
+                bf16x8_t v;
                 if constexpr (kBytes)
-                    v[u] = __builtin_bit_cast(
-                        bf16x8_t, codes_to_bf16<kFmt>(u32x2_t{vw[d][0][2 * u], vw[d][0][2 * u + 1]}));
+                    v = __builtin_bit_cast(
+                        bf16x8_t, codes_to_bf16<kFmt>(u32x2_t{vw[d][2 * u], vw[d][2 * u + 1]}));
                 else
-                    v[u] = __builtin_bit_cast(bf16x8_t, vw[d][u]);
-            }
+                    v = __builtin_bit_cast(bf16x8_t, vw[d]);
 #pragma unroll
-            for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-                for (int u = 0; u < 2; ++u)
+                for (int t = 0; t < kTiles; ++t)
                     o[t][d] =
-                        __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[u], p[t][u], o[t][d], 0, 0, 0);
+                        __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[t][u], o[t][d], 0, 0, 0);
+            }
         }
     }
 
@@ -690,9 +732,6 @@ struct TileShape {
     static constexpr int kPerSimd = D == 256 ? 1 : 2;        // waves of a SIMD that the registers leave
 };
 
-// A running maximum is kept until a score exceeds it by this much (log2): weights
-// are at most 2^8 then, and the accumulators are seldom rescaled.
-constexpr float kSlack = 8.0f;
 
 // Byte offsets of 16-byte words in the staged tiles.
 template <int D>
@@ -729,13 +768,6 @@ __device__ __forceinline__ Place find_tile(const AttendArgs& a, int tile_rows, u
         units0 += from_lane(units1, 63);
     }
     return r;
-}
-
-// The larger of a value and the other half-wave's.
-__device__ __forceinline__ float max_halves(float x) {
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false,
-                                                    false);
-    return __builtin_fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
 template <int D, int kFmt, int kMode>

@@ -71,8 +71,15 @@ typedef __amdgpu_buffer_rsrc_t Buffer;
 __device__ __forceinline__ Buffer buffer_of(const void* base, uint32_t bytes) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, bytes, 0x00020000);
 }
-__device__ __forceinline__ u32x4_t load_buffer(Buffer b, uint32_t offset) {
-    return __builtin_amdgcn_raw_buffer_load_b128(b, offset, 0, 0);
+__device__ __forceinline__ u32x4_t load_buffer(Buffer b, uint32_t offset, uint32_t more = 0) {
+    return __builtin_amdgcn_raw_buffer_load_b128(b, offset, more, 0);    // more: of the wave
+}
+template <class T>
+__device__ __forceinline__ T load_buffer_as(Buffer b, uint32_t offset, uint32_t more) {
+    if constexpr (sizeof(T) == 16)
+        return __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b128(b, offset, more, 0));
+    else
+        return __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b64(b, offset, more, 0));
 }
 __device__ __forceinline__ float load_buffer_float(Buffer b, uint32_t offset) {
     return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(b, offset, 0, 0));
