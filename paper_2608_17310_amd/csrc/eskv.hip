@@ -244,7 +244,10 @@ int es_kv_append(es_kv_t* kv, const es_kv_append_t* args, es_stream_t stream) tr
     a.adjacent = (x.flags & ES_KV_ADJACENT) != 0;
     a.c = kv->c;
     const AppendKernel kernel = by_dim_format<AppendKernel, MakeAppend>(dim, kv->d.format);
-    const dim3 grid((x.tokens + kPlaceTokens - 1) / kPlaceTokens, x.q_heads + kv->d.kv_heads);
+    const uint32_t q_tokens = kPlaceThreads * 8 / dim;       // of a workgroup of queries
+    a.q_parts = (x.q_heads + kPlaceHeads - 1) / kPlaceHeads;
+    a.q_blocks = (x.tokens + q_tokens - 1) / q_tokens * a.q_parts;
+    const dim3 grid(a.q_blocks + (x.tokens + kPlaceTokens - 1) / kPlaceTokens * kv->d.kv_heads);
     hipLaunchKernelGGL(kernel, grid, dim3(kPlaceThreads), 0, static_cast<hipStream_t>(stream), a);
     return launch_error("es_kv_append_kernel launch");
 } catch (const std::bad_alloc&) {
@@ -282,7 +285,7 @@ int es_kv_read(es_kv_t* kv, const int64_t* slots, uint32_t tokens, void* k_out, 
     a.tokens = tokens;
     a.c = kv->c;
     const ReadKernel kernel = by_dim_format<ReadKernel, MakeRead>(kv->d.head_dim, kv->d.format);
-    const dim3 grid((tokens + kPlaceTokens - 1) / kPlaceTokens, kv->d.kv_heads);
+    const dim3 grid((tokens + kPlaceTokens - 1) / kPlaceTokens * kv->d.kv_heads);
     hipLaunchKernelGGL(kernel, grid, dim3(kPlaceThreads), 0, static_cast<hipStream_t>(stream), a);
     return launch_error("es_kv_read_kernel launch");
 } catch (const std::bad_alloc&) {

@@ -1,14 +1,17 @@
 // Appending to the cache and reading it back.
 //
 // Both move every byte once and compute little: they are bound by memory, and at
-// few tokens by latency.  A workgroup takes 64 tokens and one head: a
-// query head (normalise, rotate, store), or a key head with its value head.
-// D / 8 lanes hold a row, 8 elements (one 16-byte access) each, so a norm is a
-// sum over neighbouring lanes and a rotation's other half an exchange with the
-// lane rot / 16 away (the halves' pairing) or nothing (the adjacent pairing).
+// few tokens by latency.  D / 8 lanes hold a row, 8 elements (one 16-byte access)
+// each, so a norm is a sum over neighbouring lanes and a rotation's other half an
+// exchange with the lane rot / 16 away (the halves' pairing) or nothing (the
+// adjacent pairing).
 //
-// Values are stored by dimension: a workgroup turns its 64 tokens in LDS and
-// writes runs of tokens.  Runs are cut where the slots' 16-byte words are: the
+// Queries: a workgroup takes one token for each D / 8 of its lanes and up to 8
+// heads, so that a token's row of the rotation table is read once for 8
+// rows, and 8 rows are on their way at a time.
+// Keys and values: a workgroup takes 64 tokens of one head, all of its rows on
+// their way at once.  Values are stored by dimension: the tokens are turned in
+// LDS and written as runs of tokens, cut where the slots' 16-byte words are: the
 // LDS columns are shifted by the first slot's place in its word, so that a word
 // whose tokens lie in consecutive slots (a prompt, wherever its page list jumps)
 // is read from LDS and written to memory in one access.  Words at the ends of
@@ -20,7 +23,8 @@
 namespace eskv {
 
 constexpr int kPlaceThreads = 256;
-constexpr int kPlaceTokens = 64;            // tokens of a workgroup
+constexpr int kPlaceTokens = 64;            // tokens of a workgroup of keys and values
+constexpr int kPlaceHeads = 8;              // heads of a workgroup of queries
 
 struct AppendArgs {
     const uint16_t* q;
@@ -37,6 +41,7 @@ struct AppendArgs {
     uint32_t tokens, q_heads, rot, rope_rows;
     float eps;
     uint32_t adjacent;
+    uint32_t q_parts, q_blocks;             // workgroups of queries: of a token block, of all
     Cache c;
 };
 
@@ -78,24 +83,64 @@ __device__ __forceinline__ uint32_t max_bits(const float x[8]) {
     return m;
 }
 
-// Normalise and rotate the row of which this lane (lane `lr` of the row's
-// kLanes) holds x[0..7].  `turn`: the row of the rotation table, or null.
+// What a row is multiplied by: the gain of this lane's 8 elements, and the
+// cosines and sines of its rotation.
+struct Turn {
+    float c[8], s[8];                       // of its elements, or (adjacent) of its 4 pairs
+    int away;                               // lanes to the other half; 0: none
+};
+constexpr int kUnturned = 1;                // away of an adjacent lane beyond rot
+
+// This lane's part of a row of the rotation table.  The first half takes
+// a c - b s and the second b c + a s: the sines carry the sign.
 template <int kLanes>
-__device__ __forceinline__ void norm_rotate(float x[8], int lr, bool norm, const float gain[8],
-                                            float eps, uint32_t rot, bool adjacent,
-                                            const float* turn) {
+__device__ __forceinline__ Turn load_turn(const float* turn, int lr, uint32_t rot, bool adjacent) {
+    Turn t;
+    t.away = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        t.c[i] = 1.0f;
+        t.s[i] = 0.0f;
+    }
+    if (8u * lr >= rot) {
+        t.away = adjacent ? kUnturned : 0;
+        return t;
+    }
+    const int half = static_cast<int>(rot) / 16;             // lanes of one half
+    if (adjacent) {
+        const f32x4_t c = load_float4(turn + 4 * lr), s = load_float4(turn + rot / 2 + 4 * lr);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            t.c[i] = c[i];
+            t.s[i] = s[i];
+        }
+    } else {
+        t.away = lr < half ? half : -half;
+        const float* p = turn + 8 * (lr < half ? lr : lr - half);
+        const f32x4_t c0 = load_float4(p), c1 = load_float4(p + 4);
+        const f32x4_t s0 = load_float4(p + rot / 2), s1 = load_float4(p + rot / 2 + 4);
+        const float sign = lr < half ? -1.0f : 1.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            t.c[i] = i < 4 ? c0[i & 3] : c1[i & 3];
+            t.s[i] = sign * (i < 4 ? s0[i & 3] : s1[i & 3]);
+        }
+    }
+    return t;
+}
+
+// Normalise and rotate the row of which this lane (lane `lr` of the row's
+// kLanes) holds x[0..7].
+template <int kLanes>
+__device__ __forceinline__ void norm_rotate(float x[8], bool norm, const float gain[8], float eps,
+                                            uint32_t rot, bool adjacent, const Turn& t) {
     constexpr float kInvD = 1.0f / (8 * kLanes);
     if (norm) {
         float ss = 0.0f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) ss = __builtin_fmaf(x[i], x[i], ss);
         ss = row_sum<kLanes>(ss);
-        float r;
-        if (ss < 0x1p120f) {
-            r = 1.0f / __builtin_sqrtf(__builtin_fmaf(ss, kInvD, eps));
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = x[i] * r * gain[i];
-        } else {
+        if (!(ss < 0x1p120f)) {
             // elements beyond about 2^58: squares are summed in units of 2^160,
             // beside which eps is nothing (eps is at most the largest binary32)
             ss = 0.0f;
@@ -105,41 +150,28 @@ __device__ __forceinline__ void norm_rotate(float x[8], int lr, bool norm, const
                 ss = __builtin_fmaf(x[i], x[i], ss);
             }
             ss = row_sum<kLanes>(ss);
-            r = 1.0f / __builtin_sqrtf(__builtin_fmaf(ss, kInvD, eps * 0x1p-80f * 0x1p-80f));
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = x[i] * r * gain[i];
+            eps *= 0x1p-80f * 0x1p-80f;
         }
+        const float r = 1.0f / __builtin_sqrtf(__builtin_fmaf(ss, kInvD, eps));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = x[i] * r * gain[i];
     }
     if (rot == 0) return;
     if (adjacent) {
-        if (8u * lr < rot) {
-            const f32x4_t c = load_float4(turn + 4 * lr);
-            const f32x4_t s = load_float4(turn + rot / 2 + 4 * lr);
+        // (dimensions beyond rot: cosine 1 and sine 0)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float a = x[2 * i], b = x[2 * i + 1];
-                x[2 * i] = a * c[i] - b * s[i];
-                x[2 * i + 1] = b * c[i] + a * s[i];
-            }
+        for (int i = 0; i < 4; ++i) {
+            const float a = x[2 * i], b = x[2 * i + 1];
+            x[2 * i] = t.away == kUnturned ? a : a * t.c[i] - b * t.s[i];
+            x[2 * i + 1] = t.away == kUnturned ? b : b * t.c[i] + a * t.s[i];
         }
         return;
     }
-    const int half = static_cast<int>(rot) / 16;             // lanes of one half
-    const int away = lr < half ? half : lr < 2 * half ? -half : 0;
     const int lane = static_cast<int>(threadIdx.x) & 63;
-    float other[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) other[i] = __shfl(x[i], lane + away);
-    if (away != 0) {
-        const float* t = turn + 8 * (away > 0 ? lr : lr - half);
-        const f32x4_t c0 = load_float4(t), c1 = load_float4(t + 4);
-        const f32x4_t s0 = load_float4(t + rot / 2), s1 = load_float4(t + rot / 2 + 4);
-        const float sign = away > 0 ? -1.0f : 1.0f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float c = i < 4 ? c0[i & 3] : c1[i & 3], s = i < 4 ? s0[i & 3] : s1[i & 3];
-            x[i] = x[i] * c + sign * (other[i] * s);
-        }
+    for (int i = 0; i < 8; ++i) {
+        const float other = __shfl(x[i], lane + t.away);
+        x[i] = t.away == 0 ? x[i] : x[i] * t.c[i] + other * t.s[i];
     }
 }
 
@@ -178,76 +210,113 @@ __device__ __forceinline__ void find_words(const int64_t* slot, int n, uint64_t 
     }
 }
 
+__device__ __forceinline__ int log2_up(int x) {              // of 1 .. 2^30
+    return x <= 1 ? 0 : 32 - __builtin_clz(static_cast<uint32_t>(x - 1));
+}
+
+// Where slot s keeps dimension d of head h's value.
+template <int D, int kFmt>
+__device__ __forceinline__ uint8_t* value_at(const Cache& c, int64_t s, uint32_t h, int d) {
+    const uint64_t page = uint64_t(s) >> c.page_shift;
+    const uint32_t off = uint32_t(s) & (c.page - 1);
+    return c.v + (((page * c.heads + h) * D + d) * c.page + off) * kCodeBytes<kFmt>;
+}
+
+__device__ __forceinline__ void load_gain(const uint16_t* g, int lr, float gain[8]) {
+    if (g == nullptr) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) gain[i] = 1.0f;
+    } else {
+        unpack8(load_row8(g + 8 * lr), gain);
+    }
+}
+
+// Queries of one token for each kLanes lanes and up to kPlaceHeads heads.
+template <int D>
+__device__ __forceinline__ void append_queries(const AppendArgs& a, uint32_t block) {
+    constexpr int kLanes = D / 8;                            // lanes of a row
+    constexpr int kTokens = kPlaceThreads / kLanes;
+    const int lr = threadIdx.x % kLanes;
+    const uint32_t token = block / a.q_parts * kTokens + threadIdx.x / kLanes;
+    const uint32_t t = min(token, a.tokens - 1);             // lanes exchange: none leaves
+    const uint32_t h0 = block % a.q_parts * kPlaceHeads;
+    const uint16_t* src = a.q + t * a.q_stride + h0 * D + 8 * lr;
+    uint16_t* dst = a.q_out + t * a.q_out_stride + h0 * D + 8 * lr;
+    u32x4_t raw[kPlaceHeads];
+#pragma unroll
+    for (int h = 0; h < kPlaceHeads; ++h)
+        if (h0 + h < a.q_heads) raw[h] = load_row8(src + h * D);
+    const int32_t pos = a.rot != 0 ? a.positions[t] : 0;
+    const bool ok = a.rot == 0 || (pos >= 0 && uint32_t(pos) < a.rope_rows);
+    float gain[8];
+    load_gain(a.q_gain, lr, gain);
+    const Turn turn =
+        load_turn<kLanes>(a.rope + uint64_t(ok ? pos : 0) * a.rot, lr, a.rot, a.adjacent);
+    if (!ok && lr == 0 && a.status != nullptr) atomicOr(a.status, ES_KV_BAD_POSITION);
+#pragma unroll
+    for (int h = 0; h < kPlaceHeads; ++h) {
+        if (h0 + h >= a.q_heads) break;
+        float x[8];
+        unpack8(raw[h], x);
+        norm_rotate<kLanes>(x, a.q_gain != nullptr, gain, a.eps, a.rot, a.adjacent, turn);
+        u32x4_t out;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            out[i] = ok ? pack_bf16(x[2 * i], x[2 * i + 1]) : 0x7FC07FC0u;
+        if (token < a.tokens) store_row8(dst + h * D, out);
+    }
+}
+
 template <int D, int kFmt>
 __global__ __launch_bounds__(kPlaceThreads) void es_kv_append_kernel(AppendArgs a) {
-    using T = Turned<kFmt>;
-    constexpr int kLanes = D / 8;                            // lanes of a row
-    constexpr int kRows = kPlaceThreads / kLanes;            // rows of a pass
-    const int lr = threadIdx.x % kLanes, row = threadIdx.x / kLanes;
-    const uint32_t t0 = blockIdx.x * kPlaceTokens;
-    const int n = static_cast<int>(min(uint32_t(kPlaceTokens), a.tokens - t0));
-    const uint32_t head = blockIdx.y;
-
-    // the row of the rotation table of token t, and whether it has one
-    auto turn_of = [&](uint32_t t, bool& ok) -> const float* {
-        ok = true;
-        if (a.rot == 0) return nullptr;
-        const int32_t p = a.positions[t];
-        ok = p >= 0 && uint32_t(p) < a.rope_rows;
-        return a.rope + uint64_t(ok ? p : 0) * a.rot;
-    };
-    auto load_gain = [&](const uint16_t* g, float gain[8]) {
-        if (g == nullptr) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) gain[i] = 1.0f;
-        } else {
-            unpack8(load_row8(g + 8 * lr), gain);
-        }
-    };
-    float gain[8];
-
-    if (head < a.q_heads) {
-        load_gain(a.q_gain, gain);
-        for (int j = row; j - row < n; j += kRows) {         // whole passes: lanes exchange
-            const uint32_t t = t0 + min(j, n - 1);
-            bool ok;
-            const float* turn = turn_of(t, ok);
-            float x[8];
-            unpack8(load_row8(a.q + t * a.q_stride + head * D + 8 * lr), x);
-            norm_rotate<kLanes>(x, lr, a.q_gain != nullptr, gain, a.eps, a.rot, a.adjacent, turn);
-            if (!ok) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = nan();
-                if (lr == 0 && a.status != nullptr) atomicOr(a.status, ES_KV_BAD_POSITION);
-            }
-            u32x4_t out;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) out[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
-            if (j < n) store_row8(a.q_out + t * a.q_out_stride + head * D + 8 * lr, out);
-        }
+    if (blockIdx.x < a.q_blocks) {
+        append_queries<D>(a, blockIdx.x);
         return;
     }
+    using T = Turned<kFmt>;
+    constexpr int kLanes = D / 8;
+    constexpr int kRows = kPlaceThreads / kLanes;            // rows of a pass
+    constexpr int kPasses = kPlaceTokens / kRows;
+    const int lr = threadIdx.x % kLanes, row = threadIdx.x / kLanes;
+    const uint32_t block = blockIdx.x - a.q_blocks;
+    const uint32_t h = block % a.c.heads, t0 = block / a.c.heads * kPlaceTokens;
+    const int n = static_cast<int>(min(uint32_t(kPlaceTokens), a.tokens - t0));
 
     __shared__ __attribute__((aligned(16))) uint8_t turned[D * T::kRowBytes];
     __shared__ int64_t slot[kPlaceTokens];
     __shared__ uint32_t whole[T::kWords];
-    const uint32_t h = head - a.q_heads;
     const uint64_t pool = uint64_t(a.c.n_pages) << a.c.page_shift;
+
+    // everything that this lane's rows need is asked for before any of it is used
+    // (rows past the last repeat it and are not stored: lanes exchange, none leaves)
+    u32x4_t kw[kPasses], vw[kPasses];
+    int32_t pos[kPasses];
+#pragma unroll
+    for (int p = 0; p < kPasses; ++p) {
+        const uint32_t t = t0 + min(kRows * p + row, n - 1);
+        pos[p] = a.rot != 0 ? a.positions[t] : 0;
+        kw[p] = load_row8(a.k + t * a.k_stride + h * D + 8 * lr);
+        vw[p] = load_row8(a.v + t * a.v_stride + h * D + 8 * lr);
+    }
     if (threadIdx.x < kPlaceTokens)
         slot[threadIdx.x] = static_cast<int>(threadIdx.x) < n ? a.slots[t0 + threadIdx.x] : -1;
+    float gain[8];
+    load_gain(a.k_gain, lr, gain);
     __syncthreads();
     int shift;
     find_words<kFmt>(slot, n, pool, shift, whole);
 
-    load_gain(a.k_gain, gain);
-    for (int j = row; j - row < n; j += kRows) {
-        const uint32_t t = t0 + min(j, n - 1);
-        bool ok;
-        const float* turn = turn_of(t, ok);
+#pragma unroll
+    for (int p = 0; p < kPasses; ++p) {
+        const int j = kRows * p + row;
+        if (kRows * p >= n) break;
+        const bool ok = a.rot == 0 || (pos[p] >= 0 && uint32_t(pos[p]) < a.rope_rows);
+        const Turn turn =
+            load_turn<kLanes>(a.rope + uint64_t(ok ? pos[p] : 0) * a.rot, lr, a.rot, a.adjacent);
         float x[8], y[8];
-        unpack8(load_row8(a.k + t * a.k_stride + h * D + 8 * lr), x);
-        unpack8(load_row8(a.v + t * a.v_stride + h * D + 8 * lr), y);
-        norm_rotate<kLanes>(x, lr, a.k_gain != nullptr, gain, a.eps, a.rot, a.adjacent, turn);
+        unpack8(kw[p], x);
+        unpack8(vw[p], y);
+        norm_rotate<kLanes>(x, a.k_gain != nullptr, gain, a.eps, a.rot, a.adjacent, turn);
         const uint32_t mx = row_max<kLanes>(max_bits(x)), my = row_max<kLanes>(max_bits(y));
         const bool dead = !ok || mx >= 0x7F800000u || my >= 0x7F800000u;
         const int64_t s = slot[min(j, n - 1)];
@@ -266,7 +335,7 @@ __global__ __launch_bounds__(kPlaceThreads) void es_kv_append_kernel(AppendArgs 
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 out[i] = dead ? 0x7FC07FC0u : pack_bf16(x[2 * i], x[2 * i + 1]);
-                const uint32_t w = dead ? 0u : pack_bf16(y[2 * i], y[2 * i + 1]);
+                const uint32_t w = dead ? 0u : vw[p][i];
                 if (j < n) {
                     *reinterpret_cast<uint16_t*>(column + 2 * i * T::kRowBytes) =
                         static_cast<uint16_t>(w);
@@ -298,26 +367,28 @@ __global__ __launch_bounds__(kPlaceThreads) void es_kv_append_kernel(AppendArgs 
     }
     __syncthreads();
 
-    // the values' rows of tokens
-    for (int i = threadIdx.x; i < D * T::kWords; i += kPlaceThreads) {
-        const int d = i / T::kWords, w = i % T::kWords;
-        const int j0 = T::kWord * w - shift;
+    // the values' rows of tokens, by words; neighbouring lanes take a row's words
+    const int words = (n + shift + T::kWord - 1) / T::kWord;
+    const int lanes = log2_up(words);
+    for (int i = threadIdx.x; i < D << lanes; i += kPlaceThreads) {
+        const int d = i >> lanes, w = i & ((1 << lanes) - 1);
+        if (w >= words) continue;
         const uint8_t* src = turned + d * T::kRowBytes + 16 * w;
-        auto address = [&](int64_t s) {
-            const uint64_t page = uint64_t(s) >> a.c.page_shift;
-            const uint32_t off = uint32_t(s) & (a.c.page - 1);
-            return a.c.v + (((page * a.c.heads + h) * D + d) * a.c.page + off) * kCodeBytes<kFmt>;
-        };
         if (whole[w]) {
-            store<u32x4_t>(address(slot[j0]), *reinterpret_cast<const u32x4_t*>(src));
+            store<u32x4_t>(value_at<D, kFmt>(a.c, slot[T::kWord * w - shift], h, d),
+                           *reinterpret_cast<const u32x4_t*>(src));
         } else {
-            for (int e = max(0, -j0); e < T::kWord && j0 + e < n; ++e) {
-                const int64_t s = slot[j0 + e];
+            const u32x4_t tokens = *reinterpret_cast<const u32x4_t*>(src);
+#pragma unroll
+            for (int e = 0; e < T::kWord; ++e) {
+                const int j = T::kWord * w - shift + e;
+                const int64_t s = j >= 0 && j < n ? slot[j] : -1;
                 if (s < 0 || uint64_t(s) >= pool) continue;
+                uint8_t* dst = value_at<D, kFmt>(a.c, s, h, d);
                 if constexpr (kFmt == kBf16)
-                    store<uint16_t>(address(s), reinterpret_cast<const uint16_t*>(src)[e]);
+                    store<uint16_t>(dst, static_cast<uint16_t>(tokens[e / 2] >> (16 * (e & 1))));
                 else
-                    store<uint8_t>(address(s), src[e]);
+                    store<uint8_t>(dst, static_cast<uint8_t>(tokens[e / 4] >> (8 * (e & 3))));
             }
         }
     }
@@ -328,10 +399,11 @@ __global__ __launch_bounds__(kPlaceThreads) void es_kv_read_kernel(ReadArgs a) {
     using T = Turned<kFmt>;
     constexpr int kLanes = D / 8;
     constexpr int kRows = kPlaceThreads / kLanes;
+    constexpr int kPasses = kPlaceTokens / kRows;
+    typedef uint32_t Codes __attribute__((ext_vector_type(2 * kCodeBytes<kFmt>)));
     const int lr = threadIdx.x % kLanes, row = threadIdx.x / kLanes;
-    const uint32_t t0 = blockIdx.x * kPlaceTokens;
+    const uint32_t h = blockIdx.x % a.c.heads, t0 = blockIdx.x / a.c.heads * kPlaceTokens;
     const int n = static_cast<int>(min(uint32_t(kPlaceTokens), a.tokens - t0));
-    const uint32_t h = blockIdx.y;
     const uint64_t pool = uint64_t(a.c.n_pages) << a.c.page_shift;
 
     __shared__ __attribute__((aligned(16))) uint8_t turned[D * T::kRowBytes];
@@ -344,59 +416,82 @@ __global__ __launch_bounds__(kPlaceThreads) void es_kv_read_kernel(ReadArgs a) {
     find_words<kFmt>(slot, n, pool, shift, whole);
     __syncthreads();
 
-    for (int i = threadIdx.x; i < D * T::kWords; i += kPlaceThreads) {
-        const int d = i / T::kWords, w = i % T::kWords;
-        const int j0 = T::kWord * w - shift;
-        uint8_t* dst = turned + d * T::kRowBytes + 16 * w;
-        auto address = [&](int64_t s) {
-            const uint64_t page = uint64_t(s) >> a.c.page_shift;
-            const uint32_t off = uint32_t(s) & (a.c.page - 1);
-            return a.c.v + (((page * a.c.heads + h) * D + d) * a.c.page + off) * kCodeBytes<kFmt>;
-        };
-        if (whole[w]) {
-            *reinterpret_cast<u32x4_t*>(dst) = load<u32x4_t>(address(slot[j0]));
-        } else {
-            for (int e = max(0, -j0); e < T::kWord && j0 + e < n; ++e) {
-                const int64_t s = slot[j0 + e];
-                if (s < 0 || uint64_t(s) >= pool) continue;
-                if constexpr (kFmt == kBf16)
-                    reinterpret_cast<uint16_t*>(dst)[e] = load<uint16_t>(address(s));
-                else
-                    dst[e] = load<uint8_t>(address(s));
+    // this lane's keys and their scales, on their way while the values are turned
+    Codes ck[kPasses];
+    float sk[kPasses], sv[kPasses];
+#pragma unroll
+    for (int p = 0; p < kPasses; ++p) {
+        const int j = kRows * p + row;
+        const int64_t s = j < n ? slot[j] : -1;
+        const bool in = s >= 0 && uint64_t(s) < pool;
+        const uint64_t page = uint64_t(in ? s : 0) >> a.c.page_shift;
+        const uint32_t off = uint32_t(in ? s : 0) & (a.c.page - 1);
+        const uint64_t at = (page * a.c.heads + h) * a.c.page + off;
+        sk[p] = sv[p] = 0.0f;
+        if (in) {
+            ck[p] = load<Codes>(a.c.k + (at * D + 8 * lr) * kCodeBytes<kFmt>);
+            if constexpr (kFmt == kBf16) {
+                sk[p] = bf16_lo(load<uint16_t>(a.c.k + at * D * 2));     // NaN: a void token
+            } else {
+                sk[p] = load<float>(a.c.ks + at);
+                sv[p] = load<float>(a.c.vs + at);
             }
         }
     }
+    const int words = (n + shift + T::kWord - 1) / T::kWord;
+    const int lanes = log2_up(words);
+    for (int i = threadIdx.x; i < D << lanes; i += kPlaceThreads) {
+        const int d = i >> lanes, w = i & ((1 << lanes) - 1);
+        if (w >= words) continue;
+        u32x4_t tokens = {0u, 0u, 0u, 0u};
+        if (whole[w]) {
+            tokens = load<u32x4_t>(value_at<D, kFmt>(a.c, slot[T::kWord * w - shift], h, d));
+        } else {
+            // every token's load is under way before the first is used
+            uint32_t one[T::kWord];
+#pragma unroll
+            for (int e = 0; e < T::kWord; ++e) {
+                const int j = T::kWord * w - shift + e;
+                const int64_t s = j >= 0 && j < n ? slot[j] : -1;
+                one[e] = 0;
+                if (s >= 0 && uint64_t(s) < pool) {
+                    const uint8_t* src = value_at<D, kFmt>(a.c, s, h, d);
+                    one[e] = kFmt == kBf16 ? load<uint16_t>(src) : load<uint8_t>(src);
+                }
+            }
+            constexpr int kPer = T::kWord / 4;
+#pragma unroll
+            for (int e = 0; e < T::kWord; ++e)
+                tokens[e / kPer] |= one[e] << (8 * kCodeBytes<kFmt> * (e % kPer));
+        }
+        *reinterpret_cast<u32x4_t*>(turned + d * T::kRowBytes + 16 * w) = tokens;
+    }
     __syncthreads();
 
-    for (int j = row; j < n; j += kRows) {
+#pragma unroll
+    for (int p = 0; p < kPasses; ++p) {
+        const int j = kRows * p + row;
+        if (j >= n) break;
         const uint32_t t = t0 + j;
         const int64_t s = slot[j];
         const bool in = s >= 0 && uint64_t(s) < pool;
-        u32x4_t ko, vo;
-        ko = u32x4_t{0u, 0u, 0u, 0u};
-        vo = ko;
+        u32x4_t ko = {0u, 0u, 0u, 0u}, vo = {0u, 0u, 0u, 0u};
+        const u32x4_t not_a_number = {0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u};
         if (in) {
-            const uint64_t page = uint64_t(s) >> a.c.page_shift;
-            const uint32_t off = uint32_t(s) & (a.c.page - 1);
-            const uint64_t at = (page * a.c.heads + h) * a.c.page + off;
+            const bool dead = sk[p] != sk[p];
             const uint8_t* column =
                 turned + (8 * lr) * T::kRowBytes + (j + shift) * kCodeBytes<kFmt>;
             if constexpr (kFmt == kBf16) {
-                ko = load<u32x4_t>(a.c.k + (at * D + 8 * lr) * 2);
-                const uint16_t k0 = load<uint16_t>(a.c.k + at * D * 2);
-                const bool dead = (k0 & 0x7FFFu) > 0x7F80u;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const uint32_t lo =
                         *reinterpret_cast<const uint16_t*>(column + 2 * i * T::kRowBytes);
                     const uint32_t hi =
                         *reinterpret_cast<const uint16_t*>(column + (2 * i + 1) * T::kRowBytes);
-                    vo[i] = dead ? 0x7FC07FC0u : lo | (hi << 16);
+                    ko[i] = ck[p][i];
+                    vo[i] = lo | (hi << 16);
                 }
             } else {
-                const u32x2_t ck = load<u32x2_t>(a.c.k + at * D + 8 * lr);
-                const float sk = load<float>(a.c.ks + at);
-                const float sv = sk == sk ? load<float>(a.c.vs + at) : nan();
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     uint32_t cv = 0;
@@ -404,17 +499,17 @@ __global__ __launch_bounds__(kPlaceThreads) void es_kv_read_kernel(ReadArgs a) {
                     for (int e = 0; e < 4; ++e)
                         cv |= uint32_t(column[(4 * i + e) * T::kRowBytes]) << (8 * e);
                     float xk[4], xv[4];
-                    decode4<kFmt>(ck[i], xk);
+                    decode4<kFmt>(ck[p][i], xk);
                     decode4<kFmt>(cv, xv);
-                    ko[2 * i] = pack_bf16(xk[0] * sk, xk[1] * sk);
-                    ko[2 * i + 1] = pack_bf16(xk[2] * sk, xk[3] * sk);
-                    vo[2 * i] = pack_bf16(xv[0] * sv, xv[1] * sv);
-                    vo[2 * i + 1] = pack_bf16(xv[2] * sv, xv[3] * sv);
+                    ko[2 * i] = pack_bf16(xk[0] * sk[p], xk[1] * sk[p]);
+                    ko[2 * i + 1] = pack_bf16(xk[2] * sk[p], xk[3] * sk[p]);
+                    vo[2 * i] = pack_bf16(xv[0] * sv[p], xv[1] * sv[p]);
+                    vo[2 * i + 1] = pack_bf16(xv[2] * sv[p], xv[3] * sv[p]);
                 }
             }
+            if (dead) vo = not_a_number;
         } else if (s >= 0) {
-            ko = u32x4_t{0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u};
-            vo = ko;
+            ko = vo = not_a_number;
             if (lr == 0 && h == 0 && a.status != nullptr) atomicOr(a.status, ES_KV_BAD_SLOT);
         }
         store_row8(a.k_out + t * a.k_stride + h * D + 8 * lr, ko);
