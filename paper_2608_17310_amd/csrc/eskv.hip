@@ -78,9 +78,12 @@ K by_dim_format(uint32_t dim, uint32_t format) {
                                           : Make<256, kBf16>::get();
     }
 }
-template <int D, int F>
+template <bool kWhole>
 struct MakeAppend {
-    static AppendKernel get() { return es_kv_append_kernel<D, F>; }
+    template <int D, int F>
+    struct Of {
+        static AppendKernel get() { return es_kv_append_kernel<D, F, kWhole>; }
+    };
 };
 template <int D, int F>
 struct MakeRead {
@@ -243,7 +246,10 @@ int es_kv_append(es_kv_t* kv, const es_kv_append_t* args, es_stream_t stream) tr
     a.eps = x.eps;
     a.adjacent = (x.flags & ES_KV_ADJACENT) != 0;
     a.c = kv->c;
-    const AppendKernel kernel = by_dim_format<AppendKernel, MakeAppend>(dim, kv->d.format);
+    const AppendKernel kernel =
+        x.rot == dim && (x.flags & ES_KV_ADJACENT) == 0
+            ? by_dim_format<AppendKernel, MakeAppend<true>::Of>(dim, kv->d.format)
+            : by_dim_format<AppendKernel, MakeAppend<false>::Of>(dim, kv->d.format);
     const uint32_t q_tokens = kPlaceThreads * 8 / dim;       // of a workgroup of queries
     a.q_parts = (x.q_heads + kPlaceHeads - 1) / kPlaceHeads;
     a.q_blocks = (x.tokens + q_tokens - 1) / q_tokens * a.q_parts;

@@ -55,20 +55,59 @@ struct ReadArgs {
     Cache c;
 };
 
-template <int kLanes>
-__device__ __forceinline__ float row_sum(float x) {
-#pragma unroll
-    for (int m = 1; m < kLanes; m *= 2) x += __shfl_xor(x, m);
+// A register of another lane of the same 16: by data-parallel moves, which cost
+// an instruction and no trip through LDS.
+template <int kControl>
+__device__ __forceinline__ uint32_t moved(uint32_t x) {
+    return static_cast<uint32_t>(
+        __builtin_amdgcn_update_dpp(0, static_cast<int>(x), kControl, 0xF, 0xF, true));
+}
+constexpr int kQuadSwap1 = 0xB1, kQuadSwap2 = 0x4E, kHalfMirror = 0x141, kMirror = 0x140;
+constexpr int kRor4 = 0x124, kRor8 = 0x128, kRor12 = 0x12C;
+
+// The value of the lane 16 away (of each 32).
+__device__ __forceinline__ uint32_t other_row(uint32_t x) {
+    const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    return (threadIdx.x & 16) != 0 ? r[0] : r[1];
+}
+
+// `op` over the kLanes lanes of a row, the same in all of them: over pairs, pairs
+// of pairs, the mirrored half and the mirrored 16.
+template <int kLanes, class Op>
+__device__ __forceinline__ uint32_t row_all(uint32_t x, Op op) {
+    x = op(x, moved<kQuadSwap1>(x));
+    x = op(x, moved<kQuadSwap2>(x));
+    x = op(x, moved<kHalfMirror>(x));
+    if constexpr (kLanes >= 16) x = op(x, moved<kMirror>(x));
+    if constexpr (kLanes >= 32) x = op(x, other_row(x));
     return x;
 }
 template <int kLanes>
+__device__ __forceinline__ float row_sum(float x) {
+    return __uint_as_float(row_all<kLanes>(__float_as_uint(x), [](uint32_t p, uint32_t q) {
+        return __float_as_uint(__uint_as_float(p) + __uint_as_float(q));
+    }));
+}
+template <int kLanes>
 __device__ __forceinline__ uint32_t row_max(uint32_t x) {
-#pragma unroll
-    for (int m = 1; m < kLanes; m *= 2) {
-        const uint32_t y = __shfl_xor(x, m);
-        x = x > y ? x : y;
+    return row_all<kLanes>(x, [](uint32_t p, uint32_t q) { return p > q ? p : q; });
+}
+
+// The value of the lane `away` lanes on: the other half's.  kWhole: the halves are
+// those of the whole row (rot is D).
+template <int kLanes, bool kWhole>
+__device__ __forceinline__ float exchanged(float x, int away) {
+    const uint32_t u = __float_as_uint(x);
+    if constexpr (!kWhole) {
+        return __shfl(x, (static_cast<int>(threadIdx.x) & 63) + away);
+    } else if constexpr (kLanes == 32) {
+        return __uint_as_float(other_row(u));
+    } else if constexpr (kLanes == 16) {
+        return __uint_as_float(moved<kRor8>(u));
+    } else {
+        const uint32_t up = moved<kRor12>(u), down = moved<kRor4>(u);
+        return __uint_as_float(away > 0 ? up : down);
     }
-    return x;
 }
 
 // The largest |x| of 8 elements as bits, which order as magnitudes do with
@@ -131,7 +170,7 @@ __device__ __forceinline__ Turn load_turn(const float* turn, int lr, uint32_t ro
 
 // Normalise and rotate the row of which this lane (lane `lr` of the row's
 // kLanes) holds x[0..7].
-template <int kLanes>
+template <int kLanes, bool kWhole>
 __device__ __forceinline__ void norm_rotate(float x[8], bool norm, const float gain[8], float eps,
                                             uint32_t rot, bool adjacent, const Turn& t) {
     constexpr float kInvD = 1.0f / (8 * kLanes);
@@ -156,8 +195,8 @@ __device__ __forceinline__ void norm_rotate(float x[8], bool norm, const float g
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = x[i] * r * gain[i];
     }
-    if (rot == 0) return;
-    if (adjacent) {
+    if (!kWhole && rot == 0) return;
+    if (!kWhole && adjacent) {
         // (dimensions beyond rot: cosine 1 and sine 0)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -167,12 +206,12 @@ __device__ __forceinline__ void norm_rotate(float x[8], bool norm, const float g
         }
         return;
     }
-    const int lane = static_cast<int>(threadIdx.x) & 63;
+    float other[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float other = __shfl(x[i], lane + t.away);
-        x[i] = t.away == 0 ? x[i] : x[i] * t.c[i] + other * t.s[i];
-    }
+    for (int i = 0; i < 8; ++i) other[i] = exchanged<kLanes, kWhole>(x[i], t.away);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        x[i] = !kWhole && t.away == 0 ? x[i] : x[i] * t.c[i] + other[i] * t.s[i];
 }
 
 // LDS of the turned values: a row per dimension of 64 tokens and up to a word's
@@ -231,8 +270,11 @@ __device__ __forceinline__ void load_gain(const uint16_t* g, int lr, float gain[
     }
 }
 
-// Queries of one token for each kLanes lanes and up to kPlaceHeads heads.
-template <int D>
+// Queries of one token for each kLanes lanes and up to kPlaceHeads heads.  The
+// loop is not unrolled, here and over the passes of keys: a call at few tokens waits
+// for its instructions as much as for its data, and one that fills the card has
+// other waves' rows on their way.
+template <int D, bool kWhole>
 __device__ __forceinline__ void append_queries(const AppendArgs& a, uint32_t block) {
     constexpr int kLanes = D / 8;                            // lanes of a row
     constexpr int kTokens = kPlaceThreads / kLanes;
@@ -240,12 +282,10 @@ __device__ __forceinline__ void append_queries(const AppendArgs& a, uint32_t blo
     const uint32_t token = block / a.q_parts * kTokens + threadIdx.x / kLanes;
     const uint32_t t = min(token, a.tokens - 1);             // lanes exchange: none leaves
     const uint32_t h0 = block % a.q_parts * kPlaceHeads;
+    const int heads = static_cast<int>(min(uint32_t(kPlaceHeads), a.q_heads - h0));
     const uint16_t* src = a.q + t * a.q_stride + h0 * D + 8 * lr;
     uint16_t* dst = a.q_out + t * a.q_out_stride + h0 * D + 8 * lr;
-    u32x4_t raw[kPlaceHeads];
-#pragma unroll
-    for (int h = 0; h < kPlaceHeads; ++h)
-        if (h0 + h < a.q_heads) raw[h] = load_row8(src + h * D);
+    u32x4_t raw = load_row8(src), next = load_row8(src + min(1, heads - 1) * D);
     const int32_t pos = a.rot != 0 ? a.positions[t] : 0;
     const bool ok = a.rot == 0 || (pos >= 0 && uint32_t(pos) < a.rope_rows);
     float gain[8];
@@ -253,30 +293,31 @@ __device__ __forceinline__ void append_queries(const AppendArgs& a, uint32_t blo
     const Turn turn =
         load_turn<kLanes>(a.rope + uint64_t(ok ? pos : 0) * a.rot, lr, a.rot, a.adjacent);
     if (!ok && lr == 0 && a.status != nullptr) atomicOr(a.status, ES_KV_BAD_POSITION);
-#pragma unroll
-    for (int h = 0; h < kPlaceHeads; ++h) {
-        if (h0 + h >= a.q_heads) break;
+#pragma unroll 1
+    for (int h = 0; h < heads; ++h) {
+        const u32x4_t after = load_row8(src + min(h + 2, heads - 1) * D);
         float x[8];
-        unpack8(raw[h], x);
-        norm_rotate<kLanes>(x, a.q_gain != nullptr, gain, a.eps, a.rot, a.adjacent, turn);
+        unpack8(raw, x);
+        norm_rotate<kLanes, kWhole>(x, a.q_gain != nullptr, gain, a.eps, a.rot, a.adjacent, turn);
         u32x4_t out;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             out[i] = ok ? pack_bf16(x[2 * i], x[2 * i + 1]) : 0x7FC07FC0u;
         if (token < a.tokens) store_row8(dst + h * D, out);
+        raw = next;
+        next = after;
     }
 }
 
-template <int D, int kFmt>
+template <int D, int kFmt, bool kWhole>
 __global__ __launch_bounds__(kPlaceThreads) void es_kv_append_kernel(AppendArgs a) {
     if (blockIdx.x < a.q_blocks) {
-        append_queries<D>(a, blockIdx.x);
+        append_queries<D, kWhole>(a, blockIdx.x);
         return;
     }
     using T = Turned<kFmt>;
     constexpr int kLanes = D / 8;
     constexpr int kRows = kPlaceThreads / kLanes;            // rows of a pass
-    constexpr int kPasses = kPlaceTokens / kRows;
     const int lr = threadIdx.x % kLanes, row = threadIdx.x / kLanes;
     const uint32_t block = blockIdx.x - a.q_blocks;
     const uint32_t h = block % a.c.heads, t0 = block / a.c.heads * kPlaceTokens;
@@ -287,17 +328,19 @@ __global__ __launch_bounds__(kPlaceThreads) void es_kv_append_kernel(AppendArgs 
     __shared__ uint32_t whole[T::kWords];
     const uint64_t pool = uint64_t(a.c.n_pages) << a.c.page_shift;
 
-    // everything that this lane's rows need is asked for before any of it is used
-    // (rows past the last repeat it and are not stored: lanes exchange, none leaves)
-    u32x4_t kw[kPasses], vw[kPasses];
-    int32_t pos[kPasses];
-#pragma unroll
-    for (int p = 0; p < kPasses; ++p) {
+    // a pass's rows are asked for a pass ahead (rows past the last repeat it and are
+    // not stored: lanes exchange, none leaves)
+    struct Ahead {
+        u32x4_t k, v;
+        int32_t pos;
+    };
+    auto ask = [&](int p) {
         const uint32_t t = t0 + min(kRows * p + row, n - 1);
-        pos[p] = a.rot != 0 ? a.positions[t] : 0;
-        kw[p] = load_row8(a.k + t * a.k_stride + h * D + 8 * lr);
-        vw[p] = load_row8(a.v + t * a.v_stride + h * D + 8 * lr);
-    }
+        return Ahead{load_row8(a.k + t * a.k_stride + h * D + 8 * lr),
+                     load_row8(a.v + t * a.v_stride + h * D + 8 * lr),
+                     a.rot != 0 ? a.positions[t] : 0};
+    };
+    Ahead next = ask(0);
     if (threadIdx.x < kPlaceTokens)
         slot[threadIdx.x] = static_cast<int>(threadIdx.x) < n ? a.slots[t0 + threadIdx.x] : -1;
     float gain[8];
@@ -306,17 +349,18 @@ __global__ __launch_bounds__(kPlaceThreads) void es_kv_append_kernel(AppendArgs 
     int shift;
     find_words<kFmt>(slot, n, pool, shift, whole);
 
-#pragma unroll
-    for (int p = 0; p < kPasses; ++p) {
+#pragma unroll 1
+    for (int p = 0; kRows * p < n; ++p) {
         const int j = kRows * p + row;
-        if (kRows * p >= n) break;
-        const bool ok = a.rot == 0 || (pos[p] >= 0 && uint32_t(pos[p]) < a.rope_rows);
+        const Ahead now = next;
+        const bool ok = a.rot == 0 || (now.pos >= 0 && uint32_t(now.pos) < a.rope_rows);
         const Turn turn =
-            load_turn<kLanes>(a.rope + uint64_t(ok ? pos[p] : 0) * a.rot, lr, a.rot, a.adjacent);
+            load_turn<kLanes>(a.rope + uint64_t(ok ? now.pos : 0) * a.rot, lr, a.rot, a.adjacent);
+        next = ask(p + 1);
         float x[8], y[8];
-        unpack8(kw[p], x);
-        unpack8(vw[p], y);
-        norm_rotate<kLanes>(x, a.k_gain != nullptr, gain, a.eps, a.rot, a.adjacent, turn);
+        unpack8(now.k, x);
+        unpack8(now.v, y);
+        norm_rotate<kLanes, kWhole>(x, a.k_gain != nullptr, gain, a.eps, a.rot, a.adjacent, turn);
         const uint32_t mx = row_max<kLanes>(max_bits(x)), my = row_max<kLanes>(max_bits(y));
         const bool dead = !ok || mx >= 0x7F800000u || my >= 0x7F800000u;
         const int64_t s = slot[min(j, n - 1)];
@@ -335,7 +379,7 @@ __global__ __launch_bounds__(kPlaceThreads) void es_kv_append_kernel(AppendArgs 
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 out[i] = dead ? 0x7FC07FC0u : pack_bf16(x[2 * i], x[2 * i + 1]);
-                const uint32_t w = dead ? 0u : vw[p][i];
+                const uint32_t w = dead ? 0u : now.v[i];
                 if (j < n) {
                     *reinterpret_cast<uint16_t*>(column + 2 * i * T::kRowBytes) =
                         static_cast<uint16_t>(w);
