@@ -59,6 +59,12 @@ int launch_error(const char* what) {
     return e == hipSuccess ? ES_OK : hip_fail(e, what);
 }
 
+// Blocks of `per` tokens, a multiple of 8 where there are as many (block_part).
+uint32_t token_blocks(uint32_t tokens, uint32_t per) {
+    const uint32_t n = (tokens + per - 1) / per;
+    return n >= 8 ? (n + 7) / 8 * 8 : n;
+}
+
 using AppendKernel = void (*)(AppendArgs);
 using ReadKernel = void (*)(ReadArgs);
 using AttendKernel = void (*)(AttendArgs);
@@ -252,8 +258,9 @@ int es_kv_append(es_kv_t* kv, const es_kv_append_t* args, es_stream_t stream) tr
             : by_dim_format<AppendKernel, MakeAppend<false>::Of>(dim, kv->d.format);
     const uint32_t q_tokens = kPlaceThreads * 8 / dim;       // of a workgroup of queries
     a.q_parts = (x.q_heads + kPlaceHeads - 1) / kPlaceHeads;
-    a.q_blocks = (x.tokens + q_tokens - 1) / q_tokens * a.q_parts;
-    const dim3 grid(a.q_blocks + (x.tokens + kPlaceTokens - 1) / kPlaceTokens * kv->d.kv_heads);
+    a.q_blocks = x.q_heads == 0 ? 0 : token_blocks(x.tokens, q_tokens);
+    a.kv_blocks = token_blocks(x.tokens, kPlaceTokens);
+    const dim3 grid(a.kv_blocks * kv->d.kv_heads + a.q_blocks * a.q_parts);
     hipLaunchKernelGGL(kernel, grid, dim3(kPlaceThreads), 0, static_cast<hipStream_t>(stream), a);
     return launch_error("es_kv_append_kernel launch");
 } catch (const std::bad_alloc&) {
@@ -291,7 +298,8 @@ int es_kv_read(es_kv_t* kv, const int64_t* slots, uint32_t tokens, void* k_out, 
     a.tokens = tokens;
     a.c = kv->c;
     const ReadKernel kernel = by_dim_format<ReadKernel, MakeRead>(kv->d.head_dim, kv->d.format);
-    const dim3 grid((tokens + kPlaceTokens - 1) / kPlaceTokens * kv->d.kv_heads);
+    a.blocks = token_blocks(tokens, kPlaceTokens);
+    const dim3 grid(a.blocks * kv->d.kv_heads);
     hipLaunchKernelGGL(kernel, grid, dim3(kPlaceThreads), 0, static_cast<hipStream_t>(stream), a);
     return launch_error("es_kv_read_kernel launch");
 } catch (const std::bad_alloc&) {

@@ -41,7 +41,7 @@ struct AppendArgs {
     uint32_t tokens, q_heads, rot, rope_rows;
     float eps;
     uint32_t adjacent;
-    uint32_t q_parts, q_blocks;             // workgroups of queries: of a token block, of all
+    uint32_t kv_blocks, q_blocks, q_parts;  // blocks of tokens, for keys and for queries; its parts
     Cache c;
 };
 
@@ -51,9 +51,21 @@ struct ReadArgs {
     uint16_t* v_out;
     uint64_t k_stride, v_stride;
     uint32_t* status;
-    uint32_t tokens;
+    uint32_t tokens, blocks;
     Cache c;
 };
+
+// Workgroup `id` of `blocks` blocks of tokens with `parts` parts each: a block's
+// parts on one of the eight dies (workgroups go round them), near in time, so that
+// a die's L2 holds the block's rows of the rotation table for all of them.  The
+// host rounds `blocks` up to a multiple of 8 where there are as many.
+__device__ __forceinline__ void block_part(uint32_t id, uint32_t blocks, uint32_t parts,
+                                           uint32_t& block, uint32_t& part) {
+    const uint32_t dies = blocks >= 8 ? 8 : 1;
+    const uint32_t rest = id / dies;
+    part = rest % parts;
+    block = rest / parts * dies + id % dies;
+}
 
 // A register of another lane of the same 16: by data-parallel moves, which cost
 // an instruction and no trip through LDS.
@@ -215,20 +227,34 @@ __device__ __forceinline__ void norm_rotate(float x[8], bool norm, const float g
 }
 
 // LDS of the turned values: a row per dimension of 64 tokens and up to a word's
-// shift, padded so that neighbouring rows start in different banks.
+// shift.  A token's elements of one lane lie 8 rows from the next lane's, which
+// is the same bank or its opposite: the words of a row are moved round by the
+// number of its 8 rows, so that 16 lanes meet in a bank by twos.
 template <int kFmt>
 struct Turned {
     static constexpr int kWord = 16 / kCodeBytes<kFmt>;      // tokens of a 16-byte word
     static constexpr int kWords = kPlaceTokens / kWord + 1;
-    static constexpr int kRowBytes = 16 * kWords + 16;
+    static constexpr int kRowBytes = 16 * kWords;
+    // where word w of dimension d lies
+    static __device__ __forceinline__ int at(int d, int w) {
+        const int r = w + (d >> 3) % kWords;
+        return d * kRowBytes + 16 * (r < kWords ? r : r - kWords);
+    }
+    // where column c (a token and the shift) of dimension 8 lr lies; the next
+    // dimensions follow kRowBytes apart
+    static __device__ __forceinline__ int column(int lr, int c) {
+        return at(8 * lr, c / kWord) + c % kWord * kCodeBytes<kFmt>;
+    }
 };
 
 // Where token 0 of the workgroup sits in its 16-byte word of slots (the columns'
-// shift), and for every word whether its tokens are all here and in
-// consecutive slots of one word.
-template <int kFmt>
+// shift), and for every word whether its tokens lie in consecutive slots of one
+// word: all of them here (kAll: the word is written whole), or those that are (it
+// may be read whole; the others of its slots are not used).  The word's first
+// slot then, or -1.
+template <int kFmt, bool kAll>
 __device__ __forceinline__ void find_words(const int64_t* slot, int n, uint64_t pool, int& shift,
-                                           uint32_t* whole) {
+                                           int64_t* whole) {
     using T = Turned<kFmt>;
     // the first token that has a slot sets the phase
     const int lane = threadIdx.x & 63;
@@ -239,13 +265,12 @@ __device__ __forceinline__ void find_words(const int64_t* slot, int n, uint64_t 
     shift = has ? (at - lead) & (T::kWord - 1) : 0;
     if (threadIdx.x < T::kWords) {
         const int j0 = T::kWord * static_cast<int>(threadIdx.x) - shift;
-        bool ok = j0 >= 0 && j0 + T::kWord <= n;
-        if (ok) {
-            const int64_t s0 = slot[j0];
-            ok = s0 >= 0 && uint64_t(s0) + T::kWord <= pool && (s0 & (T::kWord - 1)) == 0;
-            for (int i = 1; i < T::kWord; ++i) ok = ok && slot[j0 + i] == s0 + i;
-        }
-        whole[threadIdx.x] = ok ? 1u : 0u;
+        const int a = max(j0, 0), b = min(j0 + T::kWord, n);
+        const int64_t s0 = a < b ? slot[a] - (a - j0) : -1;
+        bool ok = (!kAll || b - a == T::kWord) && s0 >= 0 && uint64_t(s0) + T::kWord <= pool &&
+                  (s0 & (T::kWord - 1)) == 0;
+        for (int i = a + 1; i < b; ++i) ok = ok && slot[i] == s0 + (i - j0);
+        whole[threadIdx.x] = ok ? s0 : -1;
     }
 }
 
@@ -279,9 +304,12 @@ __device__ __forceinline__ void append_queries(const AppendArgs& a, uint32_t blo
     constexpr int kLanes = D / 8;                            // lanes of a row
     constexpr int kTokens = kPlaceThreads / kLanes;
     const int lr = threadIdx.x % kLanes;
-    const uint32_t token = block / a.q_parts * kTokens + threadIdx.x / kLanes;
+    uint32_t tb, part;
+    block_part(block, a.q_blocks, a.q_parts, tb, part);
+    if (tb * kTokens >= a.tokens) return;
+    const uint32_t token = tb * kTokens + threadIdx.x / kLanes;
     const uint32_t t = min(token, a.tokens - 1);             // lanes exchange: none leaves
-    const uint32_t h0 = block % a.q_parts * kPlaceHeads;
+    const uint32_t h0 = part * kPlaceHeads;
     const int heads = static_cast<int>(min(uint32_t(kPlaceHeads), a.q_heads - h0));
     const uint16_t* src = a.q + t * a.q_stride + h0 * D + 8 * lr;
     uint16_t* dst = a.q_out + t * a.q_out_stride + h0 * D + 8 * lr;
@@ -311,21 +339,25 @@ __device__ __forceinline__ void append_queries(const AppendArgs& a, uint32_t blo
 
 template <int D, int kFmt, bool kWhole>
 __global__ __launch_bounds__(kPlaceThreads) void es_kv_append_kernel(AppendArgs a) {
-    if (blockIdx.x < a.q_blocks) {
-        append_queries<D, kWhole>(a, blockIdx.x);
+    // keys and values first: their workgroups take longest
+    const uint32_t kv_groups = a.kv_blocks * a.c.heads;
+    if (blockIdx.x >= kv_groups) {
+        append_queries<D, kWhole>(a, blockIdx.x - kv_groups);
         return;
     }
     using T = Turned<kFmt>;
     constexpr int kLanes = D / 8;
     constexpr int kRows = kPlaceThreads / kLanes;            // rows of a pass
     const int lr = threadIdx.x % kLanes, row = threadIdx.x / kLanes;
-    const uint32_t block = blockIdx.x - a.q_blocks;
-    const uint32_t h = block % a.c.heads, t0 = block / a.c.heads * kPlaceTokens;
+    uint32_t tb, h;
+    block_part(blockIdx.x, a.kv_blocks, a.c.heads, tb, h);
+    const uint32_t t0 = tb * kPlaceTokens;
+    if (t0 >= a.tokens) return;
     const int n = static_cast<int>(min(uint32_t(kPlaceTokens), a.tokens - t0));
 
     __shared__ __attribute__((aligned(16))) uint8_t turned[D * T::kRowBytes];
     __shared__ int64_t slot[kPlaceTokens];
-    __shared__ uint32_t whole[T::kWords];
+    __shared__ int64_t whole[T::kWords];
     const uint64_t pool = uint64_t(a.c.n_pages) << a.c.page_shift;
 
     // a pass's rows are asked for a pass ahead (rows past the last repeat it and are
@@ -347,7 +379,7 @@ __global__ __launch_bounds__(kPlaceThreads) void es_kv_append_kernel(AppendArgs 
     load_gain(a.k_gain, lr, gain);
     __syncthreads();
     int shift;
-    find_words<kFmt>(slot, n, pool, shift, whole);
+    find_words<kFmt, true>(slot, n, pool, shift, whole);
 
 #pragma unroll 1
     for (int p = 0; kRows * p < n; ++p) {
@@ -373,7 +405,7 @@ __global__ __launch_bounds__(kPlaceThreads) void es_kv_append_kernel(AppendArgs 
         const uint64_t page = uint64_t(in ? s : 0) >> a.c.page_shift;
         const uint32_t off = uint32_t(in ? s : 0) & (a.c.page - 1);
         const uint64_t at = (page * a.c.heads + h) * a.c.page + off;
-        uint8_t* column = turned + (8 * lr) * T::kRowBytes + (j + shift) * kCodeBytes<kFmt>;
+        uint8_t* column = turned + T::column(lr, j + shift);
         if constexpr (kFmt == kBf16) {
             u32x4_t out;
 #pragma unroll
@@ -417,9 +449,9 @@ __global__ __launch_bounds__(kPlaceThreads) void es_kv_append_kernel(AppendArgs 
     for (int i = threadIdx.x; i < D << lanes; i += kPlaceThreads) {
         const int d = i >> lanes, w = i & ((1 << lanes) - 1);
         if (w >= words) continue;
-        const uint8_t* src = turned + d * T::kRowBytes + 16 * w;
-        if (whole[w]) {
-            store<u32x4_t>(value_at<D, kFmt>(a.c, slot[T::kWord * w - shift], h, d),
+        const uint8_t* src = turned + T::at(d, w);
+        if (whole[w] >= 0) {
+            store<u32x4_t>(value_at<D, kFmt>(a.c, whole[w], h, d),
                            *reinterpret_cast<const u32x4_t*>(src));
         } else {
             const u32x4_t tokens = *reinterpret_cast<const u32x4_t*>(src);
@@ -446,18 +478,21 @@ __global__ __launch_bounds__(kPlaceThreads) void es_kv_read_kernel(ReadArgs a) {
     constexpr int kPasses = kPlaceTokens / kRows;
     typedef uint32_t Codes __attribute__((ext_vector_type(2 * kCodeBytes<kFmt>)));
     const int lr = threadIdx.x % kLanes, row = threadIdx.x / kLanes;
-    const uint32_t h = blockIdx.x % a.c.heads, t0 = blockIdx.x / a.c.heads * kPlaceTokens;
+    uint32_t tb, h;
+    block_part(blockIdx.x, a.blocks, a.c.heads, tb, h);
+    const uint32_t t0 = tb * kPlaceTokens;
+    if (t0 >= a.tokens) return;
     const int n = static_cast<int>(min(uint32_t(kPlaceTokens), a.tokens - t0));
     const uint64_t pool = uint64_t(a.c.n_pages) << a.c.page_shift;
 
     __shared__ __attribute__((aligned(16))) uint8_t turned[D * T::kRowBytes];
     __shared__ int64_t slot[kPlaceTokens];
-    __shared__ uint32_t whole[T::kWords];
+    __shared__ int64_t whole[T::kWords];
     if (threadIdx.x < kPlaceTokens)
         slot[threadIdx.x] = static_cast<int>(threadIdx.x) < n ? a.slots[t0 + threadIdx.x] : -1;
     __syncthreads();
     int shift;
-    find_words<kFmt>(slot, n, pool, shift, whole);
+    find_words<kFmt, false>(slot, n, pool, shift, whole);
     __syncthreads();
 
     // this lane's keys and their scales, on their way while the values are turned
@@ -484,31 +519,42 @@ __global__ __launch_bounds__(kPlaceThreads) void es_kv_read_kernel(ReadArgs a) {
     }
     const int words = (n + shift + T::kWord - 1) / T::kWord;
     const int lanes = log2_up(words);
-    for (int i = threadIdx.x; i < D << lanes; i += kPlaceThreads) {
-        const int d = i >> lanes, w = i & ((1 << lanes) - 1);
-        if (w >= words) continue;
-        u32x4_t tokens = {0u, 0u, 0u, 0u};
-        if (whole[w]) {
-            tokens = load<u32x4_t>(value_at<D, kFmt>(a.c, slot[T::kWord * w - shift], h, d));
-        } else {
-            // every token's load is under way before the first is used
-            uint32_t one[T::kWord];
+    // kAsk words of a lane at a time, all on their way before the first is used
+    constexpr int kAsk = 2;
+#pragma unroll 1
+    for (int i0 = threadIdx.x; i0 < D << lanes; i0 += kAsk * kPlaceThreads) {
+        u32x4_t tokens[kAsk];
+        bool run[kAsk];
 #pragma unroll
-            for (int e = 0; e < T::kWord; ++e) {
-                const int j = T::kWord * w - shift + e;
-                const int64_t s = j >= 0 && j < n ? slot[j] : -1;
-                one[e] = 0;
-                if (s >= 0 && uint64_t(s) < pool) {
-                    const uint8_t* src = value_at<D, kFmt>(a.c, s, h, d);
-                    one[e] = kFmt == kBf16 ? load<uint16_t>(src) : load<uint8_t>(src);
-                }
-            }
-            constexpr int kPer = T::kWord / 4;
-#pragma unroll
-            for (int e = 0; e < T::kWord; ++e)
-                tokens[e / kPer] |= one[e] << (8 * kCodeBytes<kFmt> * (e % kPer));
+        for (int k = 0; k < kAsk; ++k) {
+            const int i = i0 + k * kPlaceThreads, d = i >> lanes, w = i & ((1 << lanes) - 1);
+            tokens[k] = u32x4_t{0u, 0u, 0u, 0u};
+            run[k] = d < D && w < words && whole[w] >= 0;
+            if (run[k]) tokens[k] = load<u32x4_t>(value_at<D, kFmt>(a.c, whole[w], h, d));
         }
-        *reinterpret_cast<u32x4_t*>(turned + d * T::kRowBytes + 16 * w) = tokens;
+#pragma unroll
+        for (int k = 0; k < kAsk; ++k) {
+            const int i = i0 + k * kPlaceThreads, d = i >> lanes, w = i & ((1 << lanes) - 1);
+            if (d >= D || w >= words) continue;
+            if (!run[k]) {
+                uint32_t one[T::kWord];
+#pragma unroll
+                for (int e = 0; e < T::kWord; ++e) {
+                    const int j = T::kWord * w - shift + e;
+                    const int64_t s = j >= 0 && j < n ? slot[j] : -1;
+                    one[e] = 0;
+                    if (s >= 0 && uint64_t(s) < pool) {
+                        const uint8_t* src = value_at<D, kFmt>(a.c, s, h, d);
+                        one[e] = kFmt == kBf16 ? load<uint16_t>(src) : load<uint8_t>(src);
+                    }
+                }
+                constexpr int kPer = T::kWord / 4;
+#pragma unroll
+                for (int e = 0; e < T::kWord; ++e)
+                    tokens[k][e / kPer] |= one[e] << (8 * kCodeBytes<kFmt> * (e % kPer));
+            }
+            *reinterpret_cast<u32x4_t*>(turned + T::at(d, w)) = tokens[k];
+        }
     }
     __syncthreads();
 
@@ -523,8 +569,7 @@ __global__ __launch_bounds__(kPlaceThreads) void es_kv_read_kernel(ReadArgs a) {
         const u32x4_t not_a_number = {0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u};
         if (in) {
             const bool dead = sk[p] != sk[p];
-            const uint8_t* column =
-                turned + (8 * lr) * T::kRowBytes + (j + shift) * kCodeBytes<kFmt>;
+            const uint8_t* column = turned + T::column(lr, j + shift);
             if constexpr (kFmt == kBf16) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {

@@ -232,6 +232,40 @@ def test_a_token_is_stored_the_same_alone_and_in_a_batch(form):
         assert torch.equal(a.k_scales, b.k_scales) and torch.equal(a.v_scales, b.v_scales)
 
 
+@pytest.mark.parametrize("form", FORMATS)
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_packed_sequences_of_any_lengths_and_places(form, dim):
+    """Runs of consecutive slots that begin anywhere in a 16-byte word, several
+    to a workgroup, with padding between: bits as from one token at a time."""
+    rng = np.random.default_rng([24, dim])
+    heads, page, pages = 2, 64, 24
+    for lengths in ([10, 54], [63, 1], [1, 63], [30, 20, 14], [64, 64, 7], [5, 100, 3], [1, 1, 62],
+                    [17, 47, 33, 31], [128], [90, 100], [7] * 9):
+        order, at, slots = rng.permutation(pages), 0, []
+        for n in lengths:
+            begin = int(rng.integers(0, 40))
+            i = begin + np.arange(n)
+            slots.append(order[at + i // page] * page + i % page)
+            at += 1 + (begin + n - 1) // page
+        slots = np.concatenate(slots)
+        slots[rng.integers(0, len(slots))] = -1
+        tokens = len(slots)
+        k, v = rows(rng, tokens, heads, dim), rows(rng, tokens, heads, dim)
+        s = dev(slots, torch.int64)
+        a, b = (KVCache.allocate(pages, heads, dim, form, page) for _ in range(2))
+        a.append(k, v, s)
+        for t in range(tokens):
+            b.append(k[t:t + 1], v[t:t + 1], s[t:t + 1])
+        for x, y in ((a.k_pages, b.k_pages), (a.v_pages, b.v_pages)):
+            assert torch.equal(x.view(torch.uint8), y.view(torch.uint8)), lengths
+        if form != "bf16":
+            assert torch.equal(a.k_scales, b.k_scales) and torch.equal(a.v_scales, b.v_scales)
+        rk, rv = a.read(s)
+        for t in range(tokens):
+            k1, v1 = b.read(s[t:t + 1])
+            assert torch.equal(rk[t:t + 1], k1) and torch.equal(rv[t:t + 1], v1), (lengths, t)
+
+
 def test_slots_and_positions_out_of_range_are_reported():
     rng = np.random.default_rng(12)
     dim = 64
