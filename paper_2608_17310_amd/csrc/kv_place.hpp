@@ -14,8 +14,10 @@
 // LDS and written as runs of tokens, cut where the slots' 16-byte words are: the
 // LDS columns are shifted by the first slot's place in its word, so that a word
 // whose tokens lie in consecutive slots (a prompt, wherever its page list jumps)
-// is read from LDS and written to memory in one access.  Words at the ends of
-// runs, and tokens of different sequences (a generation step), go one by one.
+// is read from LDS and written to memory in one access.  The tokens of the other
+// words (at the ends of runs, of several sequences, of a generation step) go one
+// by one, a lane each, dimension after dimension: neighbours' elements are then
+// written by one instruction, into as few lines as there are runs.
 #pragma once
 
 #include "kv_common.hpp"
@@ -240,11 +242,12 @@ struct Turned {
         const int r = w + (d >> 3) % kWords;
         return d * kRowBytes + 16 * (r < kWords ? r : r - kWords);
     }
-    // where column c (a token and the shift) of dimension 8 lr lies; the next
-    // dimensions follow kRowBytes apart
-    static __device__ __forceinline__ int column(int lr, int c) {
-        return at(8 * lr, c / kWord) + c % kWord * kCodeBytes<kFmt>;
+    // where column c (a token and the shift) of dimension d lies
+    static __device__ __forceinline__ int token(int d, int c) {
+        return at(d, c / kWord) + c % kWord * kCodeBytes<kFmt>;
     }
+    // of dimension 8 lr; the next seven follow kRowBytes apart
+    static __device__ __forceinline__ int column(int lr, int c) { return token(8 * lr, c); }
 };
 
 // Where token 0 of the workgroup sits in its 16-byte word of slots (the columns'
@@ -449,23 +452,22 @@ __global__ __launch_bounds__(kPlaceThreads) void es_kv_append_kernel(AppendArgs 
     for (int i = threadIdx.x; i < D << lanes; i += kPlaceThreads) {
         const int d = i >> lanes, w = i & ((1 << lanes) - 1);
         if (w >= words) continue;
-        const uint8_t* src = turned + T::at(d, w);
-        if (whole[w] >= 0) {
+        if (whole[w] >= 0)
             store<u32x4_t>(value_at<D, kFmt>(a.c, whole[w], h, d),
-                           *reinterpret_cast<const u32x4_t*>(src));
-        } else {
-            const u32x4_t tokens = *reinterpret_cast<const u32x4_t*>(src);
-#pragma unroll
-            for (int e = 0; e < T::kWord; ++e) {
-                const int j = T::kWord * w - shift + e;
-                const int64_t s = j >= 0 && j < n ? slot[j] : -1;
-                if (s < 0 || uint64_t(s) >= pool) continue;
-                uint8_t* dst = value_at<D, kFmt>(a.c, s, h, d);
-                if constexpr (kFmt == kBf16)
-                    store<uint16_t>(dst, static_cast<uint16_t>(tokens[e / 2] >> (16 * (e & 1))));
-                else
-                    store<uint8_t>(dst, static_cast<uint8_t>(tokens[e / 4] >> (8 * (e & 3))));
-            }
+                           *reinterpret_cast<const u32x4_t*>(turned + T::at(d, w)));
+    }
+    const int j = threadIdx.x & 63;
+    const int64_t s = j < n && whole[(j + shift) / T::kWord] < 0 ? slot[j] : -1;
+    if (s >= 0 && uint64_t(s) < pool) {
+        uint8_t* const dst = value_at<D, kFmt>(a.c, s, h, 0);
+        const uint32_t step = a.c.page * kCodeBytes<kFmt>;
+#pragma unroll 4
+        for (int d = threadIdx.x >> 6; d < D; d += kPlaceThreads / 64) {
+            const uint8_t* src = turned + T::token(d, j + shift);
+            if constexpr (kFmt == kBf16)
+                store<uint16_t>(dst + d * step, *reinterpret_cast<const uint16_t*>(src));
+            else
+                store<uint8_t>(dst + d * step, *src);
         }
     }
 }
@@ -535,25 +537,23 @@ __global__ __launch_bounds__(kPlaceThreads) void es_kv_read_kernel(ReadArgs a) {
 #pragma unroll
         for (int k = 0; k < kAsk; ++k) {
             const int i = i0 + k * kPlaceThreads, d = i >> lanes, w = i & ((1 << lanes) - 1);
-            if (d >= D || w >= words) continue;
-            if (!run[k]) {
-                uint32_t one[T::kWord];
-#pragma unroll
-                for (int e = 0; e < T::kWord; ++e) {
-                    const int j = T::kWord * w - shift + e;
-                    const int64_t s = j >= 0 && j < n ? slot[j] : -1;
-                    one[e] = 0;
-                    if (s >= 0 && uint64_t(s) < pool) {
-                        const uint8_t* src = value_at<D, kFmt>(a.c, s, h, d);
-                        one[e] = kFmt == kBf16 ? load<uint16_t>(src) : load<uint8_t>(src);
-                    }
-                }
-                constexpr int kPer = T::kWord / 4;
-#pragma unroll
-                for (int e = 0; e < T::kWord; ++e)
-                    tokens[k][e / kPer] |= one[e] << (8 * kCodeBytes<kFmt> * (e % kPer));
+            if (run[k]) *reinterpret_cast<u32x4_t*>(turned + T::at(d, w)) = tokens[k];
+        }
+    }
+    {
+        const int j = threadIdx.x & 63;
+        const int64_t s = j < n && whole[(j + shift) / T::kWord] < 0 ? slot[j] : -1;
+        if (s >= 0 && uint64_t(s) < pool) {
+            const uint8_t* const src = value_at<D, kFmt>(a.c, s, h, 0);
+            const uint32_t step = a.c.page * kCodeBytes<kFmt>;
+#pragma unroll 8
+            for (int d = threadIdx.x >> 6; d < D; d += kPlaceThreads / 64) {
+                uint8_t* dst = turned + T::token(d, j + shift);
+                if constexpr (kFmt == kBf16)
+                    *reinterpret_cast<uint16_t*>(dst) = load<uint16_t>(src + d * step);
+                else
+                    *dst = load<uint8_t>(src + d * step);
             }
-            *reinterpret_cast<u32x4_t*>(turned + T::at(d, w)) = tokens[k];
         }
     }
     __syncthreads();
