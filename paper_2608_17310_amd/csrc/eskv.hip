@@ -16,9 +16,10 @@
 using namespace es_host;
 using namespace eskv;
 
-// Parts that a split launch aims at, and the rows of a tile at most: they bound the scratch.
-static constexpr uint32_t kTargetParts = 1024;
+// Parts that a launch cuts its histories into at most: they bound the scratch.
+static constexpr uint32_t kMaxParts = 1024;
 static constexpr uint32_t kMinBlocks = 4;          // blocks of a part at least: one a wave
+static constexpr uint32_t kTileMinBlocks = 4;      //   and of a part of a tile of many rows
 
 struct es_kv {
     int device = -1;
@@ -68,7 +69,7 @@ uint32_t token_blocks(uint32_t tokens, uint32_t per) {
 using AppendKernel = void (*)(AppendArgs);
 using ReadKernel = void (*)(ReadArgs);
 using AttendKernel = void (*)(AttendArgs);
-using JoinKernel = void (*)(AttendArgs, int);
+using JoinKernel = void (*)(AttendArgs, int, int);
 
 template <class K, template <int, int> class Make>
 K by_dim_format(uint32_t dim, uint32_t format) {
@@ -109,6 +110,43 @@ struct MakeTile {
         static AttendKernel get() { return es_kv_tile_kernel<D, F, kMode>; }
     };
 };
+
+struct TileLaunch {
+    uint32_t rows, threads, resident;              // of a workgroup; workgroups of the card
+    size_t lds;
+};
+template <int D>
+TileLaunch tile_launch() {
+    using S = TileShape<D>;
+    return TileLaunch{S::kRows, S::kThreads, 256u * S::kPerSimd, S::kLds};
+}
+
+constexpr uint64_t kMaxGroups = uint64_t(1) << 24; // workgroups of a launch: below 2^32 lanes
+
+// A kernel that cuts histories into a.target parts, and the join of the parts.
+int launch_parts(AttendKernel kernel, const AttendArgs& a, uint32_t tile_rows, uint32_t threads,
+                 size_t lds, uint64_t seq_rows, uint32_t dim, hipStream_t s) {
+    const uint32_t heads = a.c.heads;
+    // tiles of all sequences at most, and parts: one more than its share for each
+    const uint64_t n_tiles = uint64_t(a.rows) * a.group / tile_rows + a.n_seqs;
+    const uint64_t n_parts = a.target / heads + n_tiles;
+    if (n_parts * heads >= kMaxGroups)
+        return fail(ES_ERR_INVALID_ARG, "es_kv_attend: too many rows for one call");
+    hipLaunchKernelGGL(kernel, dim3(n_parts * heads), dim3(threads), lds, s, a);
+    const int rc = launch_error("es_kv_attend kernel launch");
+    if (rc != ES_OK) return rc;
+    const JoinKernel join = dim == 64    ? es_kv_join_kernel<64>
+                            : dim == 128 ? es_kv_join_kernel<128>
+                                         : es_kv_join_kernel<256>;
+    // a row in many parts takes a workgroup, rows in few share one
+    const uint64_t rows = std::min<uint64_t>(tile_rows, seq_rows);
+    const bool spread = rows <= 16;
+    const uint64_t together = 4 * kSplitThreads / dim;         // rows of a workgroup's groups
+    const uint64_t y = spread ? rows : (rows + together - 1) / together;
+    hipLaunchKernelGGL(join, dim3(n_tiles * heads, y), dim3(kSplitThreads), 0, s, a,
+                       static_cast<int>(tile_rows), spread ? 1 : 0);
+    return launch_error("es_kv_join_kernel launch");
+}
 
 }  // namespace
 
@@ -165,7 +203,7 @@ int es_kv_create(const es_kv_desc_t* desc, es_kv_t** out) try {
                   static_cast<uint32_t>(__builtin_ctz(d.page))};
     // at most two slots for each part aimed at (a sequence cut into c > 1 parts
     // has more than c - 1 parts' blocks)
-    const uint64_t slot_rows = uint64_t(2) * kTargetParts * 16 * split_tiles_max(d.head_dim);
+    const uint64_t slot_rows = uint64_t(2) * kMaxParts * 16 * split_tiles_max(d.head_dim);
     kv->scratch_bytes = slot_rows * (d.head_dim + 2) * 4;
     const hipError_t e = hipMalloc(reinterpret_cast<void**>(&kv->scratch), kv->scratch_bytes);
     if (e != hipSuccess) {
@@ -365,8 +403,6 @@ int es_kv_attend(es_kv_t* kv, const es_kv_attend_t* args, es_stream_t stream) tr
     a.table_stride = x.table_stride;
     a.q_heads = x.q_heads;
     a.group = x.q_heads / heads;
-    a.target = kTargetParts;
-    a.min_blocks = kMinBlocks;
     a.scale = x.scale;
     a.cap = x.cap;
     a.c = kv->c;
@@ -391,41 +427,31 @@ int es_kv_attend(es_kv_t* kv, const es_kv_attend_t* args, es_stream_t stream) tr
                          : by_dim_format<AttendKernel, MakeSplit<2, kAny>::Of>(dim, format))
                 : (plain ? by_dim_format<AttendKernel, MakeSplit<4, kPlain>::Of>(dim, format)
                          : by_dim_format<AttendKernel, MakeSplit<4, kAny>::Of>(dim, format));
-        const uint32_t tile_rows = 16 * tiles;
-        // tiles of all sequences at most, and parts: one more than its share for each
-        const uint64_t n_tiles = all_rows / tile_rows + x.n_seqs;
-        const uint64_t n_parts = kTargetParts / heads + n_tiles;
-        if (n_parts * heads >= (uint64_t(1) << 24))
-            return fail_in(ES_ERR_INVALID_ARG, name, "too many rows for one call");
-        hipLaunchKernelGGL(kernel, dim3(n_parts * heads), dim3(kSplitThreads), 0, s, a);
-        rc = launch_error("es_kv_split_kernel launch");
-        if (rc != ES_OK) return rc;
-        const JoinKernel join = dim == 64    ? es_kv_join_kernel<64>
-                                : dim == 128 ? es_kv_join_kernel<128>
-                                             : es_kv_join_kernel<256>;
-        const uint32_t y = static_cast<uint32_t>(std::min<uint64_t>(tile_rows, seq_rows));
-        hipLaunchKernelGGL(join, dim3(n_tiles * heads, y), dim3(kSplitThreads), 0, s, a,
-                           static_cast<int>(tile_rows));
-        return launch_error("es_kv_join_kernel launch");
+        a.target = kMaxParts;
+        a.min_blocks = kMinBlocks;
+        return launch_parts(kernel, a, 16 * tiles, kSplitThreads, 0, seq_rows, dim, s);
     }
     const AttendKernel kernel =
         mode == kPlain    ? by_dim_format<AttendKernel, MakeTile<kPlain>::Of>(dim, format)
         : mode == kCapped ? by_dim_format<AttendKernel, MakeTile<kCapped>::Of>(dim, format)
         : mode == kSloped ? by_dim_format<AttendKernel, MakeTile<kSloped>::Of>(dim, format)
                           : by_dim_format<AttendKernel, MakeTile<kAny>::Of>(dim, format);
-    const uint32_t tile_rows = dim == 64    ? TileShape<64>::kRows
-                               : dim == 128 ? TileShape<128>::kRows
-                                            : TileShape<256>::kRows;
-    const uint32_t threads = dim == 64    ? TileShape<64>::kThreads
-                             : dim == 128 ? TileShape<128>::kThreads
-                                          : TileShape<256>::kThreads;
-    const size_t lds = dim == 64    ? TileShape<64>::kLds
-                       : dim == 128 ? TileShape<128>::kLds
-                                    : TileShape<256>::kLds;
-    const uint64_t n_tiles = all_rows / tile_rows + x.n_seqs;
-    if (n_tiles * heads >= (uint64_t(1) << 22))
+    const TileLaunch tile = dim == 64    ? tile_launch<64>()
+                            : dim == 128 ? tile_launch<128>()
+                                         : tile_launch<256>();
+    // tiles that do not fill the card are cut along long histories
+    const uint64_t n_tiles = all_rows / tile.rows + x.n_seqs;
+    const uint64_t expected =
+        std::min<uint64_t>(n_tiles, (seq_rows + tile.rows - 1) / tile.rows * x.n_seqs) * heads;
+    const uint64_t blocks = (uint64_t(x.max_length) + kBlock - 1) / kBlock;
+    if (expected < tile.resident && blocks >= 2 * kTileMinBlocks) {
+        a.target = tile.resident;
+        a.min_blocks = kTileMinBlocks;
+        return launch_parts(kernel, a, tile.rows, tile.threads, tile.lds, seq_rows, dim, s);
+    }
+    if (n_tiles * heads >= kMaxGroups)
         return fail_in(ES_ERR_INVALID_ARG, name, "too many rows for one call");
-    hipLaunchKernelGGL(kernel, dim3(n_tiles * heads), dim3(threads), lds, s, a);
+    hipLaunchKernelGGL(kernel, dim3(n_tiles * heads), dim3(tile.threads), tile.lds, s, a);
     return launch_error("es_kv_tile_kernel launch");
 } catch (const std::bad_alloc&) {
     return fail(ES_ERR_NOMEM, "es_kv_attend: host allocation failed");

@@ -646,27 +646,31 @@ __global__ __launch_bounds__(kSplitThreads, (split_waves<D, kTiles, kFmt>())) vo
 }
 
 // Join the parts of each row: out = sum_c 2^(m_c - M) o_c / sum_c 2^(m_c - M) l_c.
-// A workgroup per row of a tile (rows blockIdx.y, + gridDim.y, ...); D / 4 lanes
-// hold a row, and the others take other parts.
+// D / 4 lanes hold a row.  With `spread` a workgroup takes one row, its lanes'
+// groups every so many parts each, joined in LDS (a row in many parts); without,
+// every group takes a row of its own.  Rows blockIdx.y, + gridDim.y, ... (of
+// groups of rows) of the tile.
 template <int D>
-__global__ __launch_bounds__(kSplitThreads) void es_kv_join_kernel(AttendArgs a, int tile_rows) {
+__global__ __launch_bounds__(kSplitThreads) void es_kv_join_kernel(AttendArgs a, int tile_rows,
+                                                                   int spread) {
     constexpr int kLanes = D / 4;
     constexpr int kGroups = kSplitThreads / kLanes;
     const uint32_t h = blockIdx.x % a.c.heads;
     const Place at = find_place<false>(a, tile_rows, blockIdx.x / a.c.heads);
     if (!at.found || at.chunks <= 1) return;
-    const int n_rows = at.seq.n * static_cast<int>(a.group);
+    const int n_rows = min(at.seq.n * static_cast<int>(a.group) -
+                               static_cast<int>(at.tile) * tile_rows, tile_rows);
     const int lane = threadIdx.x % kLanes, grp = threadIdx.x / kLanes;
     __shared__ float ml[kGroups][2];
     __shared__ __attribute__((aligned(16))) f32x4_t part[kGroups][kLanes];
-    for (int y = blockIdx.y; y < tile_rows; y += gridDim.y) {
-        const int r = static_cast<int>(at.tile) * tile_rows + y;
-        if (r >= n_rows) break;
+    const int per = spread ? 1 : kGroups;                    // rows of a workgroup at a time
+    for (int y0 = blockIdx.y * per; y0 < n_rows; y0 += gridDim.y * per) {
+        const int y = spread ? y0 : min(y0 + grp, n_rows - 1);
         float m = -inf(), l = 0.0f;
         f32x4_t o = {0.0f, 0.0f, 0.0f, 0.0f};
-        for (uint32_t c = grp; c < at.chunks; c += kGroups) {
-            const uint64_t slot =
-                ((uint64_t(at.slot) + c) * a.c.heads + h) * tile_rows + y;
+#pragma unroll 4
+        for (uint32_t c = spread ? grp : 0; c < at.chunks; c += spread ? kGroups : 1) {
+            const uint64_t slot = ((uint64_t(at.slot) + c) * a.c.heads + h) * tile_rows + y;
             const float mc = a.part_ml[2 * slot], lc = a.part_ml[2 * slot + 1];
             const f32x4_t oc = load<f32x4_t>(a.part_o + slot * D + 4 * lane);
             const float now = __builtin_fmaxf(m, mc);
@@ -676,33 +680,36 @@ __global__ __launch_bounds__(kSplitThreads) void es_kv_join_kernel(AttendArgs a,
             o = o * x + oc * z;
             m = now;
         }
-        if (lane == 0) {
-            ml[grp][0] = m;
-            ml[grp][1] = l;
-        }
-        part[grp][lane] = o;
-        __syncthreads();
-        if (grp == 0) {
-            float top = -inf(), total = 0.0f;
+        if (spread) {
+            if (lane == 0) {
+                ml[grp][0] = m;
+                ml[grp][1] = l;
+            }
+            part[grp][lane] = o;
+            __syncthreads();
+            m = -inf();
 #pragma unroll
-            for (int k = 0; k < kGroups; ++k) top = __builtin_fmaxf(top, ml[k][0]);
-            const float base = top == -inf() ? 0.0f : top;
-            f32x4_t x = {0.0f, 0.0f, 0.0f, 0.0f};
+            for (int k = 0; k < kGroups; ++k) m = __builtin_fmaxf(m, ml[k][0]);
+            const float base = m == -inf() ? 0.0f : m;
+            o = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+            l = 0.0f;
 #pragma unroll
             for (int k = 0; k < kGroups; ++k) {
                 const float z = __builtin_amdgcn_exp2f(ml[k][0] - base);
-                total += ml[k][1] * z;
-                x += part[k][lane] * z;
+                l += ml[k][1] * z;
+                o += part[k][lane] * z;
             }
-            x *= total > 0.0f || total != total ? 1.0f / total : 0.0f;
+            __syncthreads();
+        }
+        if (spread ? grp == 0 : y0 + grp < n_rows) {
+            o *= l > 0.0f || l != l ? 1.0f / l : 0.0f;
+            const int r = static_cast<int>(at.tile) * tile_rows + y;
             const int i = r / static_cast<int>(a.group);
             const uint32_t head = h * a.group + (r - i * static_cast<int>(a.group));
-            u32x2_t w;
-            w = u32x2_t{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
             store_row4(a.out + uint64_t(at.seq.start + i) * a.out_stride + uint64_t(head) * D +
-                            4 * lane, w);
+                           4 * lane,
+                       u32x2_t{pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3])});
         }
-        __syncthreads();
     }
 }
 
@@ -785,7 +792,9 @@ es_kv_tile_kernel(AttendArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     __shared__ int bounds[2][S::kWaves];
 
-    const Place at = find_tile(a, S::kRows, blockIdx.x / a.c.heads);
+    const bool parts = a.target != 0;
+    const Place at = parts ? find_place<true>(a, S::kRows, blockIdx.x / a.c.heads)
+                           : find_tile(a, S::kRows, blockIdx.x / a.c.heads);
     if (!at.found) return;
 
     const int n_rows = at.seq.n * static_cast<int>(a.group);
@@ -837,7 +846,12 @@ es_kv_tile_kernel(AttendArgs a) {
     }
     lo = __builtin_amdgcn_readfirstlane(lo);
     hi = __builtin_amdgcn_readfirstlane(hi);
-    const int b_begin = lo / kBlock, b_end = hi > lo ? (hi - 1) / kBlock + 1 : b_begin;
+    int b_begin = lo / kBlock, b_end = hi > lo ? (hi - 1) / kBlock + 1 : b_begin;
+    if (parts) {
+        const int part0 = at.block0 + static_cast<int>(at.chunk * at.per);
+        b_begin = max(b_begin, part0);
+        b_end = min(b_end, min(at.block0 + at.blocks, part0 + static_cast<int>(at.per)));
+    }
 
     // staging: 16-byte words of codes, each thread kStage of the keys' and of the values'
     constexpr int kStage = kBlock * D * kCodeBytes<kFmt> / 16 / S::kThreads;
@@ -1059,8 +1073,24 @@ es_kv_tile_kernel(AttendArgs a) {
     }
 
     sum += __shfl_xor(sum, 32);
-    const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
     if (r >= n_rows) return;
+    if (parts && at.chunks > 1) {
+        const uint64_t slot =
+            ((uint64_t(at.slot) + at.chunk) * a.c.heads + h) * S::kRows + 32 * wave + n;
+#pragma unroll
+        for (int d = 0; d < kDims; ++d)
+#pragma unroll
+            for (int y = 0; y < 4; ++y)
+                store<f32x4_t>(a.part_o + slot * D + 32 * d + 8 * y + 4 * g,
+                               f32x4_t{o[d][4 * y], o[d][4 * y + 1], o[d][4 * y + 2],
+                                       o[d][4 * y + 3]});
+        if (g == 0) {
+            a.part_ml[2 * slot] = top;
+            a.part_ml[2 * slot + 1] = sum;
+        }
+        return;
+    }
+    const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
     uint16_t* out = a.out + uint64_t(at.seq.start + i) * a.out_stride + uint64_t(head) * D;
 #pragma unroll
     for (int d = 0; d < kDims; ++d)
