@@ -17,9 +17,10 @@ using namespace es_host;
 using namespace eskv;
 
 // Parts that a launch cuts its histories into at most: they bound the scratch.
-static constexpr uint32_t kMaxParts = 1024;
+static constexpr uint32_t kMaxParts = 512;
 static constexpr uint32_t kMinBlocks = 4;          // blocks of a part at least: one a wave
 static constexpr uint32_t kTileMinBlocks = 4;      //   and of a part of a tile of many rows
+static constexpr uint32_t kCutBlocks = 16;         // blocks of a history worth cutting for such tiles
 
 struct es_kv {
     int device = -1;
@@ -31,10 +32,6 @@ struct es_kv {
 };
 
 namespace {
-
-// Tiles of 16 rows that a wave of the split kernel holds at most: two of wide heads, whose
-// keys, values and accumulators are twice as long.
-constexpr uint32_t split_tiles_max(uint32_t dim) { return dim == 256 ? 2 : 4; }
 
 int check_kv_device(const es_kv_t* kv, const char* name) {
     int dev = -1;
@@ -96,11 +93,11 @@ template <int D, int F>
 struct MakeRead {
     static ReadKernel get() { return es_kv_read_kernel<D, F>; }
 };
-template <int T, int kMode>
+template <int kMode>
 struct MakeSplit {
     template <int D, int F>
     struct Of {
-        static AttendKernel get() { return es_kv_split_kernel<D, (D == 256 && T > 2 ? 2 : T), F, kMode>; }
+        static AttendKernel get() { return es_kv_split_kernel<D, F, kMode>; }
     };
 };
 template <int kMode>
@@ -114,6 +111,7 @@ struct MakeTile {
 struct TileLaunch {
     uint32_t rows, threads, resident;              // of a workgroup; workgroups of the card
     size_t lds;
+    uint64_t slots() const { return uint64_t(rows) * resident; }
 };
 template <int D>
 TileLaunch tile_launch() {
@@ -124,23 +122,32 @@ TileLaunch tile_launch() {
 constexpr uint64_t kMaxGroups = uint64_t(1) << 24; // workgroups of a launch: below 2^32 lanes
 
 // A kernel that cuts histories into a.target parts, and the join of the parts.
-int launch_parts(AttendKernel kernel, const AttendArgs& a, uint32_t tile_rows, uint32_t threads,
-                 size_t lds, uint64_t seq_rows, uint32_t dim, hipStream_t s) {
+int launch_parts(AttendKernel kernel, AttendArgs a, uint32_t tile_rows, uint32_t threads, size_t lds,
+                 uint64_t seq_rows, uint32_t max_length, uint32_t dim, hipStream_t s) {
     const uint32_t heads = a.c.heads;
-    // tiles of all sequences at most, and parts: one more than its share for each
+    // tiles of all sequences, at most and as expected; a history as long as expected
+    // leaves no more parts than these
     const uint64_t n_tiles = uint64_t(a.rows) * a.group / tile_rows + a.n_seqs;
-    const uint64_t n_parts = a.target / heads + n_tiles;
+    const uint64_t expected =
+        std::min<uint64_t>(n_tiles, (seq_rows + tile_rows - 1) / tile_rows * a.n_seqs);
+    const uint64_t part = uint64_t(a.min_blocks) * kBlock;
+    const uint64_t parts = std::max<uint64_t>(1, (max_length + part - 1) / part);
+    a.target = static_cast<uint32_t>(std::min<uint64_t>(a.target, expected * heads * parts));
+    // histories expected to be a part each are not cut, however long they turn out
+    if (parts == 1) a.min_blocks = 1u << 25;
+    // parts: a tile's last may be short, so one more for each
+    const uint64_t n_parts = a.target / heads + 1 + n_tiles;
     if (n_parts * heads >= kMaxGroups)
         return fail(ES_ERR_INVALID_ARG, "es_kv_attend: too many rows for one call");
     hipLaunchKernelGGL(kernel, dim3(n_parts * heads), dim3(threads), lds, s, a);
     const int rc = launch_error("es_kv_attend kernel launch");
-    if (rc != ES_OK) return rc;
+    if (rc != ES_OK || parts == 1) return rc;
     const JoinKernel join = dim == 64    ? es_kv_join_kernel<64>
                             : dim == 128 ? es_kv_join_kernel<128>
                                          : es_kv_join_kernel<256>;
     // a row in many parts takes a workgroup, rows in few share one
     const uint64_t rows = std::min<uint64_t>(tile_rows, seq_rows);
-    const bool spread = rows <= 16;
+    const bool spread = rows <= 16 || a.target > 8 * expected * heads;
     const uint64_t together = 4 * kSplitThreads / dim;         // rows of a workgroup's groups
     const uint64_t y = spread ? rows : (rows + together - 1) / together;
     hipLaunchKernelGGL(join, dim3(n_tiles * heads, y), dim3(kSplitThreads), 0, s, a,
@@ -203,7 +210,11 @@ int es_kv_create(const es_kv_desc_t* desc, es_kv_t** out) try {
                   static_cast<uint32_t>(__builtin_ctz(d.page))};
     // at most two slots for each part aimed at (a sequence cut into c > 1 parts
     // has more than c - 1 parts' blocks)
-    const uint64_t slot_rows = uint64_t(2) * kMaxParts * 16 * split_tiles_max(d.head_dim);
+    const uint64_t slot_rows = std::max(
+        uint64_t(2) * kMaxParts * kSplitRows,
+        uint64_t(2) * (d.head_dim == 64    ? tile_launch<64>().slots()
+                       : d.head_dim == 128 ? tile_launch<128>().slots()
+                                           : tile_launch<256>().slots()));
     kv->scratch_bytes = slot_rows * (d.head_dim + 2) * 4;
     const hipError_t e = hipMalloc(reinterpret_cast<void**>(&kv->scratch), kv->scratch_bytes);
     if (e != hipSuccess) {
@@ -415,21 +426,21 @@ int es_kv_attend(es_kv_t* kv, const es_kv_attend_t* args, es_stream_t stream) tr
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const uint64_t all_rows = uint64_t(x.rows) * a.group;      // of one key head
     const uint64_t seq_rows = std::min<uint64_t>(x.rows, std::max(1u, x.max_rows)) * a.group;
-    if (seq_rows <= 64) {
-        const uint32_t tiles = seq_rows <= 16 ? 1 : seq_rows <= 32 ? 2 : split_tiles_max(dim);
+    if (seq_rows <= kSplitRows) {
         // a history's scores cost little beside its bytes: one kernel for every mode but plain
-        const bool plain = mode == kPlain;
         const AttendKernel kernel =
-            tiles == 1 ? (plain ? by_dim_format<AttendKernel, MakeSplit<1, kPlain>::Of>(dim, format)
-                                : by_dim_format<AttendKernel, MakeSplit<1, kAny>::Of>(dim, format))
-            : tiles == 2
-                ? (plain ? by_dim_format<AttendKernel, MakeSplit<2, kPlain>::Of>(dim, format)
-                         : by_dim_format<AttendKernel, MakeSplit<2, kAny>::Of>(dim, format))
-                : (plain ? by_dim_format<AttendKernel, MakeSplit<4, kPlain>::Of>(dim, format)
-                         : by_dim_format<AttendKernel, MakeSplit<4, kAny>::Of>(dim, format));
-        a.target = kMaxParts;
+            mode == kPlain ? by_dim_format<AttendKernel, MakeSplit<kPlain>::Of>(dim, format)
+                           : by_dim_format<AttendKernel, MakeSplit<kAny>::Of>(dim, format);
+        // Two workgroups a compute unit stream as fast as more, and a part left over
+        // for a second round costs as long as all of the first: with few histories,
+        // room for each one's short last part.  8 histories of 50000 to 65537 tokens
+        // (int8) aimed at 512, 448 and 1024 parts: 230, 200 and 194 us; 64 of 2000
+        // (bf16) at 512 and 1024: 100 and 108; 8 of 20000 (bf16, 16 heads over 4 x
+        // 256): 127 and 136.
+        const uint64_t pairs = uint64_t(x.n_seqs) * heads;
+        a.target = kMaxParts - (pairs <= kMaxParts / 4 ? static_cast<uint32_t>(pairs) : 0u);
         a.min_blocks = kMinBlocks;
-        return launch_parts(kernel, a, 16 * tiles, kSplitThreads, 0, seq_rows, dim, s);
+        return launch_parts(kernel, a, kSplitRows, kSplitThreads, 0, seq_rows, x.max_length, dim, s);
     }
     const AttendKernel kernel =
         mode == kPlain    ? by_dim_format<AttendKernel, MakeTile<kPlain>::Of>(dim, format)
@@ -439,15 +450,20 @@ int es_kv_attend(es_kv_t* kv, const es_kv_attend_t* args, es_stream_t stream) tr
     const TileLaunch tile = dim == 64    ? tile_launch<64>()
                             : dim == 128 ? tile_launch<128>()
                                          : tile_launch<256>();
-    // tiles that do not fill the card are cut along long histories
+    // Tiles that fill less than half of the card are cut along long histories.  40
+    // heads over 8 x 128, bf16, cut and whole: 13 rows after 12000 tokens 38 and 213
+    // us, 200 rows 68 and 214; 800 rows of 3000 tokens (half a card) 69 and 65; a
+    // prompt of 517 tokens (16 heads of 64) 14.4 and 12.2.
     const uint64_t n_tiles = all_rows / tile.rows + x.n_seqs;
     const uint64_t expected =
         std::min<uint64_t>(n_tiles, (seq_rows + tile.rows - 1) / tile.rows * x.n_seqs) * heads;
     const uint64_t blocks = (uint64_t(x.max_length) + kBlock - 1) / kBlock;
-    if (expected < tile.resident && blocks >= 2 * kTileMinBlocks) {
-        a.target = tile.resident;
+    if (expected < tile.resident / 2 && blocks >= kCutBlocks) {
+        // a part more than its share for each tile, all on the card at once
+        a.target = tile.resident - static_cast<uint32_t>(expected);
         a.min_blocks = kTileMinBlocks;
-        return launch_parts(kernel, a, tile.rows, tile.threads, tile.lds, seq_rows, dim, s);
+        return launch_parts(kernel, a, tile.rows, tile.threads, tile.lds, seq_rows, x.max_length, dim,
+                            s);
     }
     if (n_tiles * heads >= kMaxGroups)
         return fail_in(ES_ERR_INVALID_ARG, name, "too many rows for one call");

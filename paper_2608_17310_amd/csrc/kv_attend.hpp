@@ -207,12 +207,13 @@ __device__ __forceinline__ float max_quarters(float x) {
 
 constexpr int kSplitThreads = 256;
 constexpr int kSplitWaves = kSplitThreads / 64;
+constexpr int kSplitRows = 16;              // of a tile
 constexpr int kScanRows = 64;               // rows of a sequence whose intervals the scan reads
 
 // Waves of a SIMD that the registers leave.
-template <int D, int kTiles, int kFmt>
+template <int D, int kFmt>
 constexpr int split_waves() {
-        return D * kTiles <= 64 ? 4 : D * kTiles <= 128 ? (kFmt == kBf16 ? 3 : 2) : D * kTiles <= 256 ? 2 : 1;
+    return D == 64 ? 4 : D == 128 && kFmt == kBf16 ? 3 : 2;
 }
 
 struct Span {                               // a sequence's blocks
@@ -351,15 +352,14 @@ __device__ __forceinline__ u32x4_t token_mask(int n) {
     return m;
 }
 
-template <int D, int kTiles, int kFmt, int kMode>
-__global__ __launch_bounds__(kSplitThreads, (split_waves<D, kTiles, kFmt>())) void es_kv_split_kernel(AttendArgs a) {
-    constexpr int kRowsOfTile = 16 * kTiles;
+template <int D, int kFmt, int kMode>
+__global__ __launch_bounds__(kSplitThreads, (split_waves<D, kFmt>())) void es_kv_split_kernel(AttendArgs a) {
     constexpr int kSteps = D / 32;                           // 32 dimensions a product
     constexpr int kDims = D / 16;                            // 16 dimensions a tile of O^T
     constexpr bool kBytes = kFmt != kBf16;
     // A step takes 4 L keys, as tiles of 16: a lane holds L tokens of each of its
-    // dimensions, 16 bytes, or 8 where the registers leave no room for more
-    constexpr int L = kBytes && D * kTiles <= 128 ? 16 : 8;
+    // dimensions, 16 bytes, or 8 of wide heads, whose registers leave no room for more
+    constexpr int L = kBytes && D <= 128 ? 16 : 8;
     constexpr int kKeys = 4 * L, kKeyTiles = L / 4, kPairs = L / 8;
     typedef uint32_t Tokens __attribute__((ext_vector_type(L * kCodeBytes<kFmt> / 4)));
     constexpr int kRowBytes = D * kCodeBytes<kFmt>;
@@ -370,37 +370,30 @@ __global__ __launch_bounds__(kSplitThreads, (split_waves<D, kTiles, kFmt>())) vo
     const int base_key = L * g;                              // of this lane's keys in a step
     const uint32_t h = blockIdx.x % a.c.heads;
 
-    const Place at = find_place<true>(a, kRowsOfTile, blockIdx.x / a.c.heads);
+    const Place at = find_place<true>(a, kSplitRows, blockIdx.x / a.c.heads);
     if (!at.found) return;
 
-    // this lane's rows: column n of each tile of 16.  Columns past the last row
-    // repeat it and are not written.
+    // this lane's row: column n of the tile.  Columns past the last row repeat it
+    // and are not written.
     const int n_rows = at.seq.n * static_cast<int>(a.group);
-    const int row0 = static_cast<int>(at.tile) * kRowsOfTile;
-    ScoreMap map[kTiles];
-    int first[kTiles], limit[kTiles], pos[kTiles];
-    bf16x8_t q[kTiles][kSteps];
-    int lo_any = at.seq.len, hi_any = 0, lo_all = 0, hi_all = at.seq.len;
-#pragma unroll
-    for (int t = 0; t < kTiles; ++t) {
-        const int r = min(row0 + 16 * t + n, n_rows - 1);
-        const int i = r / static_cast<int>(a.group);
-        const uint32_t head = h * a.group + (r - i * static_cast<int>(a.group));
-        interval(a, at.seq, i, first[t], limit[t]);
-        pos[t] = at.seq.len - at.seq.n + i;
-        map[t] = score_map<kMode, kBytes>(a, head);
-        if (first[t] < limit[t]) {
-            lo_any = min(lo_any, first[t]);
-            hi_any = max(hi_any, limit[t]);
-        }
-        lo_all = max(lo_all, first[t]);
-        hi_all = min(hi_all, limit[t]);
+    const int row0 = static_cast<int>(at.tile) * kSplitRows;
+    const int r = row0 + n, rr = min(r, n_rows - 1);
+    const int i = rr / static_cast<int>(a.group);
+    const uint32_t head = h * a.group + (rr - i * static_cast<int>(a.group));
+    int first, limit;
+    interval(a, at.seq, i, first, limit);
+    const int pos = at.seq.len - at.seq.n + i;
+    const ScoreMap map = score_map<kMode, kBytes>(a, head);
+    int lo_any = first < limit ? first : at.seq.len, hi_any = limit;
+    int lo_all = first, hi_all = limit;
+    bf16x8_t q[kSteps];
+    {
         const uint16_t* src = a.q + uint64_t(at.seq.start + i) * a.q_stride + uint64_t(head) * D;
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
             // the dimensions that a lane's words of a key hold: 8 of 32, or 16 of 64
             const int d = kBytes ? 64 * (s / 2) + 16 * g + 8 * (s & 1) : 32 * s + 8 * g;
-            q[t][s] = __builtin_bit_cast(bf16x8_t, load_row8(src + d));
+            q[s] = __builtin_bit_cast(bf16x8_t, load_row8(src + d));
         }
     }
 #pragma unroll
@@ -415,15 +408,10 @@ __global__ __launch_bounds__(kSplitThreads, (split_waves<D, kTiles, kFmt>())) vo
     lo_all = __builtin_amdgcn_readfirstlane(lo_all);
     hi_all = __builtin_amdgcn_readfirstlane(hi_all);
 
-    float top[kTiles], sum[kTiles];
-    f32x4_t o[kTiles][kDims];
+    float top = -inf(), sum = 0.0f;
+    f32x4_t o[kDims];
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t) {
-        top[t] = -inf();
-        sum[t] = 0.0f;
-#pragma unroll
-        for (int d = 0; d < kDims; ++d) o[t][d] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-    }
+    for (int d = 0; d < kDims; ++d) o[d] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
 
     // the part's keys that some row of the tile sees, in whole steps
     const int part0 = at.block0 + static_cast<int>(at.chunk * at.per);
@@ -478,15 +466,14 @@ __global__ __launch_bounds__(kSplitThreads, (split_waves<D, kTiles, kFmt>())) vo
         const bool masked = key0 < lo_all || key0 + kKeys > hi_all;
         if constexpr (kBytes) {
 #pragma unroll
-            for (int t = 0; t < kKeyTiles; ++t) ks[t] *= map[0].factor;
+            for (int t = 0; t < kKeyTiles; ++t) ks[t] *= map.factor;
             if (left < kKeys) {
 #pragma unroll
                 for (int t = 0; t < L; ++t)
                     if (base_key + t >= left) vs[t >> 2][t & 3] = 0.0f;
             }
         }
-        // S^T of every tile of rows: a word of keys is converted once for all of them
-        f32x4_t s[kTiles][kKeyTiles];
+        f32x4_t s[kKeyTiles];
 #pragma unroll
         for (int k = 0; k < kKeyTiles; ++k)
 #pragma unroll
@@ -501,63 +488,58 @@ __global__ __launch_bounds__(kSplitThreads, (split_waves<D, kTiles, kFmt>())) vo
                             codes_to_bf16<kFmt>(u32x2_t{kw[k][w][2 * y], kw[k][w][2 * y + 1]}));
                     else
                         x = __builtin_bit_cast(bf16x8_t, kw[k][w]);
-#pragma unroll
-                    for (int t = 0; t < kTiles; ++t)
-                        s[t][k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                            x, q[t][kHalves * w + y], w + y == 0 ? f32x4_t{} : s[t][k], 0, 0, 0);
+                    s[k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                        x, q[kHalves * w + y], w + y == 0 ? f32x4_t{} : s[k], 0, 0, 0);
                 }
             }
-        bf16x8_t p[kTiles][kPairs];
+        // scores of this lane's keys key0 + base_key + 0 .. L - 1
+        float x[L];
 #pragma unroll
-        for (int t = 0; t < kTiles; ++t) {
-            // scores of this lane's keys key0 + base_key + 0 .. L - 1
-            float x[L];
+        for (int k = 0; k < L; ++k)
+            x[k] = kBytes ? s[k >> 2][k & 3] * ks[k >> 2][k & 3] : s[k >> 2][k & 3];
+        map_scores<kMode, kBytes>(map, x, static_cast<float>(pos - key0 - base_key),
+                                  [](int i) { return i; }, false);
+        if (bad) {
+#pragma unroll
+            for (int k = 0; k < L; ++k) x[k] = nan();
+        }
+        if (masked) {
+            const int from = first - key0 - base_key, to = limit - key0 - base_key;
 #pragma unroll
             for (int k = 0; k < L; ++k)
-                x[k] = kBytes ? s[t][k >> 2][k & 3] * ks[k >> 2][k & 3] : s[t][k >> 2][k & 3];
-            map_scores<kMode, kBytes>(map[t], x, static_cast<float>(pos[t] - key0 - base_key),
-                                      [](int i) { return i; }, false);
-            if (bad) {
+                if (k < from || k >= to) x[k] = unseen<kMode>();
+        }
+        float peak = x[0];
 #pragma unroll
-                for (int k = 0; k < L; ++k) x[k] = nan();
-            }
-            if (masked) {
-                const int from = first[t] - key0 - base_key, to = limit[t] - key0 - base_key;
+        for (int k = 1; k < L; ++k) peak = larger<kMode>(peak, x[k]);
+        peak = max_quarters(__builtin_fmaf(peak, map.unit, map.offset));
+        const float now = __builtin_fmaxf(top, peak);
+        if (__any(now > top + kSlack)) {
+            const float shrink = __builtin_amdgcn_exp2f(top - (now == -inf() ? 0.0f : now));
+            sum *= shrink;
 #pragma unroll
-                for (int k = 0; k < L; ++k)
-                    if (k < from || k >= to) x[k] = unseen<kMode>();
-            }
-            float peak = x[0];
+            for (int d = 0; d < kDims; ++d) o[d] *= shrink;
+            top = now;
+        }
+        // nothing seen so far: any finite stand-in gives weights of zero
+        const float base = map.offset - (top == -inf() ? 0.0f : top);
+        bf16x8_t p[kPairs];
 #pragma unroll
-            for (int k = 1; k < L; ++k) peak = larger<kMode>(peak, x[k]);
-            peak = max_quarters(__builtin_fmaf(peak, map[t].unit, map[t].offset));
-            const float now = __builtin_fmaxf(top[t], peak);
-            if (__any(now > top[t] + kSlack)) {
-                const float shrink = __builtin_amdgcn_exp2f(top[t] - (now == -inf() ? 0.0f : now));
-                sum[t] *= shrink;
+        for (int u = 0; u < kPairs; ++u) {
+            u32x4_t w;
 #pragma unroll
-                for (int d = 0; d < kDims; ++d) o[t][d] *= shrink;
-                top[t] = now;
-            }
-            // nothing seen so far: any finite stand-in gives weights of zero
-            const float base = map[t].offset - (top[t] == -inf() ? 0.0f : top[t]);
+            for (int j = 0; j < 4; ++j) {
+                float e[2];
 #pragma unroll
-            for (int u = 0; u < kPairs; ++u) {
-                u32x4_t w;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    float e[2];
-#pragma unroll
-                    for (int y = 0; y < 2; ++y) {
-                        const int k = 8 * u + 2 * j + y;
-                        e[y] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[k], map[t].unit, base));
-                        sum[t] += e[y];
-                        if constexpr (kBytes) e[y] *= vs[k >> 2][k & 3];
-                    }
-                    w[j] = pack_bf16(e[0], e[1]);
+                for (int y = 0; y < 2; ++y) {
+                    const int k = 8 * u + 2 * j + y;
+                    e[y] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[k], map.unit, base));
+                    sum += e[y];
+                    if constexpr (kBytes) e[y] *= vs[k >> 2][k & 3];
                 }
-                p[t][u] = __builtin_bit_cast(bf16x8_t, w);
+                w[j] = pack_bf16(e[0], e[1]);
             }
+            p[u] = __builtin_bit_cast(bf16x8_t, w);
         }
         if (bad && a.status != nullptr && lane == 0) atomicOr(a.status, ES_KV_BAD_PAGE);
         if (left < kKeys) {
@@ -577,10 +559,7 @@ __global__ __launch_bounds__(kSplitThreads, (split_waves<D, kTiles, kFmt>())) vo
                         bf16x8_t, codes_to_bf16<kFmt>(u32x2_t{vw[d][2 * u], vw[d][2 * u + 1]}));
                 else
                     v = __builtin_bit_cast(bf16x8_t, vw[d]);
-#pragma unroll
-                for (int t = 0; t < kTiles; ++t)
-                    o[t][d] =
-                        __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[t][u], o[t][d], 0, 0, 0);
+                o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[u], o[d], 0, 0, 0);
             }
         }
     }
@@ -588,60 +567,48 @@ __global__ __launch_bounds__(kSplitThreads, (split_waves<D, kTiles, kFmt>())) vo
     // join the waves: the others hand their sums to wave 0 through LDS
     __shared__ float ml[kSplitWaves][2][16];
     __shared__ __attribute__((aligned(16))) f32x4_t part[kSplitWaves - 1][kDims][64];
+    sum += __shfl_xor(sum, 16);
+    sum += __shfl_xor(sum, 32);
+    if (g == 0) {
+        ml[wave][0][n] = top;
+        ml[wave][1][n] = sum;
+    }
+    __syncthreads();
+    float m = -inf();
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t) {
-        float l = sum[t];
-        l += __shfl_xor(l, 16);
-        l += __shfl_xor(l, 32);
-        if (t > 0) __syncthreads();
-        if (g == 0) {
-            ml[wave][0][n] = top[t];
-            ml[wave][1][n] = l;
+    for (int w = 0; w < kSplitWaves; ++w) m = __builtin_fmaxf(m, ml[w][0][n]);
+    const float base = m == -inf() ? 0.0f : m;
+    const float mine = __builtin_amdgcn_exp2f(top - base);
+    if (wave > 0) {
+#pragma unroll
+        for (int d = 0; d < kDims; ++d) part[wave - 1][d][lane] = o[d] * mine;
+    }
+    __syncthreads();
+    if (wave > 0 || r >= n_rows) return;
+    float total = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kSplitWaves; ++w)
+        total += ml[w][1][n] * __builtin_amdgcn_exp2f(ml[w][0][n] - base);
+    const bool whole = at.chunks == 1;
+    const float inv = total > 0.0f || total != total ? 1.0f / total : 0.0f;
+    const uint64_t slot = ((uint64_t(at.slot) + at.chunk) * a.c.heads + h) * kSplitRows + n;
+    uint16_t* out = a.out + uint64_t(at.seq.start + i) * a.out_stride + uint64_t(head) * D;
+#pragma unroll
+    for (int d = 0; d < kDims; ++d) {
+        f32x4_t x = o[d] * mine;
+#pragma unroll
+        for (int w = 0; w < kSplitWaves - 1; ++w) x += part[w][d][lane];
+        if (whole) {
+            x *= inv;
+            store_row4(out + 16 * d + 4 * g,
+                       u32x2_t{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])});
+        } else {
+            store<f32x4_t>(a.part_o + slot * D + 16 * d + 4 * g, x);
         }
-        __syncthreads();
-        float m = -inf();
-#pragma unroll
-        for (int w = 0; w < kSplitWaves; ++w) m = __builtin_fmaxf(m, ml[w][0][n]);
-        const float base = m == -inf() ? 0.0f : m;
-        const float mine = __builtin_amdgcn_exp2f(top[t] - base);
-        if (wave > 0) {
-#pragma unroll
-            for (int d = 0; d < kDims; ++d) part[wave - 1][d][lane] = o[t][d] * mine;
-        }
-        __syncthreads();
-        if (wave > 0) continue;
-        float total = 0.0f;
-#pragma unroll
-        for (int w = 0; w < kSplitWaves; ++w)
-            total += ml[w][1][n] * __builtin_amdgcn_exp2f(ml[w][0][n] - base);
-        const int r = row0 + 16 * t + n;
-        const bool real = r < n_rows;
-        const int i = min(r, n_rows - 1) / static_cast<int>(a.group);
-        const uint32_t head = h * a.group + (min(r, n_rows - 1) - i * static_cast<int>(a.group));
-        const bool whole = at.chunks == 1;
-        const float inv = total > 0.0f || total != total ? 1.0f / total : 0.0f;
-        const uint64_t slot =
-            ((uint64_t(at.slot) + at.chunk) * a.c.heads + h) * kRowsOfTile + 16 * t + n;
-        uint16_t* out = a.out + uint64_t(at.seq.start + i) * a.out_stride + uint64_t(head) * D;
-#pragma unroll
-        for (int d = 0; d < kDims; ++d) {
-            f32x4_t x = o[t][d] * mine;
-#pragma unroll
-            for (int w = 0; w < kSplitWaves - 1; ++w) x += part[w][d][lane];
-            if (!real) continue;
-            if (whole) {
-                x *= inv;
-                u32x2_t y;
-                y = u32x2_t{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
-                store_row4(out + 16 * d + 4 * g, y);
-            } else {
-                store<f32x4_t>(a.part_o + slot * D + 16 * d + 4 * g, x);
-            }
-        }
-        if (real && !whole && g == 0) {
-            a.part_ml[2 * slot] = m;
-            a.part_ml[2 * slot + 1] = total;
-        }
+    }
+    if (!whole && g == 0) {
+        a.part_ml[2 * slot] = m;
+        a.part_ml[2 * slot + 1] = total;
     }
 }
 
