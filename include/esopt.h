@@ -598,8 +598,9 @@ int es_tile_layout(uint64_t addr, uint64_t numel, uint32_t offset8, es_tile_info
  * quantized plans' two formats with one binary32 scale per token and head in
  *   k_scales[n_pages][kv_heads][page], v_scales[n_pages][kv_heads][page]:
  * with M the largest |x| of the head's row and Q = 127 or 448, the scale is
- * M / Q and the code RNE(x (Q / M)), all in binary32.  A row with M < 2^-100 has
- * scale 0 and codes 0 (it reads back as zeros).
+ * M / Q and the code RNE(x (Q (1 / M))), every operation in binary32 (a bf16 value
+ * often lies halfway between two codes: which it takes is defined to the bit).  A
+ * row with M < 2^-100 has scale 0 and codes 0 (it reads back as zeros).
  * A token whose rotated key or whose value is not finite throughout in some
  * head is void there: its key reads as NaN, its value is stored as zeros and
  * reads back as NaN.  A row that sees a void token returns NaN in that head; a
@@ -616,7 +617,8 @@ int es_tile_layout(uint64_t addr, uint64_t numel, uint32_t offset8, es_tile_info
 #define ES_KV_BAD_POSITION 2u  /* append: position outside the rotation table: the token is void and
                                   its query NaN */
 #define ES_KV_BAD_PAGE     4u  /* attend: a page that a row sees is not in the pool: the row is NaN */
-#define ES_KV_BAD_LENGTH   8u  /* attend: lengths or starts out of range: clamped into it */
+#define ES_KV_BAD_LENGTH   8u  /* attend: lengths or starts out of range (clamped
+                                  into it), or a sequence with more rows than tokens */
 
 typedef struct es_kv_desc {
     void*    k_pages;           /* 16-byte aligned */

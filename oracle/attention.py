@@ -42,13 +42,13 @@ def norm_rotate(x, gain=None, eps=1e-6, turn=None, adjacent=False):
 
 def quantise_f32(x, form):
     """Codes and scales of binary32 rows x, in the cache's own arithmetic
-    (binary32 scale, reciprocal and product; one rounding to nearest even)."""
+    (binary32 scale, reciprocal and products; one rounding to nearest even)."""
     x = np.asarray(x, np.float32)
     top = np.max(np.abs(x), axis=-1, keepdims=True)
     live = top >= np.float32(TINY_ROW)
     big = np.float32(CODE_MAX[form])
     safe = np.where(live, top, np.float32(1.0))
-    y = np.where(live, x * (big / safe), np.float32(0.0)).astype(np.float32)
+    y = np.where(live, x * (big * (np.float32(1.0) / safe)), np.float32(0.0)).astype(np.float32)
     scale = np.where(live, safe / big, np.float32(0.0)).astype(np.float32)
     if form == "int8":
         return np.rint(y).astype(np.int8), scale[..., 0]

@@ -156,7 +156,7 @@ __device__ __forceinline__ u32x4_t codes_to_bf16(u32x2_t c) {
 }
 
 // Eight values times `inv` as codes (RNE; |x inv| is at most the format's largest
-// value up to a rounding of binary32, which the integer rounding and E4M3's
+// value up to roundings of binary32, which the integer rounding and E4M3's
 // rounding to 448 both absorb).
 template <int kFmt>
 __device__ __forceinline__ u32x2_t encode8(const float x[8], float inv) {

@@ -428,8 +428,8 @@ __global__ __launch_bounds__(kPlaceThreads) void es_kv_append_kernel(AppendArgs 
             const float fx = __uint_as_float(mx), fy = __uint_as_float(my);
             const bool lx = !dead && fx >= kTinyRow, ly = !dead && fy >= kTinyRow;
             u32x2_t cx = {0u, 0u}, cy = {0u, 0u};
-            if (lx) cx = encode8<kFmt>(x, kCodeMax<kFmt> / fx);
-            if (ly) cy = encode8<kFmt>(y, kCodeMax<kFmt> / fy);
+            if (lx) cx = encode8<kFmt>(x, kCodeMax<kFmt> * (1.0f / fx));
+            if (ly) cy = encode8<kFmt>(y, kCodeMax<kFmt> * (1.0f / fy));
             if (j < n) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
