@@ -412,7 +412,6 @@ int es_kv_attend(es_kv_t* kv, const es_kv_attend_t* args, es_stream_t stream) tr
     a.rows = x.rows;
     a.n_seqs = x.n_seqs;
     a.table_stride = x.table_stride;
-    a.q_heads = x.q_heads;
     a.group = x.q_heads / heads;
     a.scale = x.scale;
     a.cap = x.cap;

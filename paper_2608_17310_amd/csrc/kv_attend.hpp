@@ -36,10 +36,10 @@ struct AttendArgs {
     const int32_t* limit;
     const float* slopes;
     uint32_t* status;
-    float* part_o;                          // [slots][rows of a tile][D], split kernel
+    float* part_o;                          // [slots][rows of a tile][D]
     float* part_ml;                         // [slots][rows of a tile][2]: maximum, sum
-    uint32_t rows, n_seqs, table_stride, q_heads, group;
-    uint32_t target, min_blocks;            // split kernel: parts aimed at, blocks of a part at least
+    uint32_t rows, n_seqs, table_stride, group;
+    uint32_t target, min_blocks;            // parts aimed at (0: none), blocks of a part at least
     float scale, cap;
     Cache c;
 };
@@ -291,8 +291,8 @@ template <bool kParts>
 __device__ __forceinline__ Place find_place(const AttendArgs& a, int tile_rows, uint32_t unit) {
     const uint32_t lane = threadIdx.x & 63;
     const Span mine = read_span(a, lane, tile_rows);
-    // all blocks of one head, a wave's sum at a time (tiles and blocks of a sequence
-    // are below 2^26 and 2^25: sums are held in 64 bits, in two halves a lane)
+    // all blocks of one head, 64 sequences at a time, in two sums of 32 bits (a cache
+    // has at most 2^25 blocks); a part of 2^30 blocks or more is all of any history
     uint64_t total = 0;
     for (uint32_t s0 = 0; s0 < a.n_seqs; s0 += 64) {
         const Span p = s0 == 0 ? mine : read_span(a, s0 + lane, tile_rows);
@@ -301,8 +301,6 @@ __device__ __forceinline__ Place find_place(const AttendArgs& a, int tile_rows, 
         const uint32_t hi = wave_scan(static_cast<uint32_t>(work >> 24) & 0x3FFFFFFu);
         total += (uint64_t(from_lane(hi, 63)) << 24) + uint32_t(from_lane(lo, 63));
     }
-    // 32 bits hold the quotients: 2^51 blocks over at least 2^5 parts of at most 2^26 tiles each
-    // would not fit, but no cache holds them (2^31 tokens: 2^25 blocks, 2^26 tiles of rows)
     const uint64_t all = total * a.c.heads;
     uint32_t per = a.min_blocks;
     if (all > uint64_t(a.min_blocks) * a.target)
@@ -338,9 +336,6 @@ __device__ __forceinline__ Place find_place(const AttendArgs& a, int tile_rows, 
     }
     return r;
 }
-
-// This lane's 16 bytes of a token-major row or of a dimension's row of tokens.
-__device__ __forceinline__ u32x4_t zero4() { return u32x4_t{0u, 0u, 0u, 0u}; }
 
 // Keep the first n of the tokens of a 16-byte word.
 template <int kFmt>
@@ -715,7 +710,6 @@ struct TileShape {
     static constexpr int kLds = 2 * kBuffer + 256 * 4;       //   and the scales of both
     static constexpr int kPerSimd = D == 256 ? 1 : 2;        // waves of a SIMD that the registers leave
 };
-
 
 // Byte offsets of 16-byte words in the staged tiles.
 template <int D>
