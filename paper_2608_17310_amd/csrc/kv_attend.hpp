@@ -775,6 +775,8 @@ es_kv_tile_kernel(AttendArgs a) {
     const uint32_t head = h * a.group + (rr - i * static_cast<int>(a.group));
     int first, limit;
     interval(a, at.seq, i, first, limit);
+    // a wave of no rows (the last tile's) sees nothing and passes every block
+    if (static_cast<int>(at.tile) * S::kRows + 32 * wave >= n_rows) first = limit = 0;
     const int pos = at.seq.len - at.seq.n + i;
     const ScoreMap map = score_map<kMode, kBytes>(a, head);
     // positions grow with rows.  Steep slopes take distances one by one: a block's
