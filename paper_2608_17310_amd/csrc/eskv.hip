@@ -20,6 +20,7 @@ using namespace eskv;
 static constexpr uint32_t kMaxParts = 512;
 static constexpr uint32_t kMinBlocks = 4;          // blocks of a part at least: one a wave
 static constexpr uint32_t kTileMinBlocks = 4;      //   and of a part of a tile of many rows
+static constexpr uint32_t kPairLength = 1280;      // tokens of a history worth two columns of rows
 static constexpr uint32_t kCutBlocks = 16;         // blocks of a history worth cutting for such tiles
 
 struct es_kv {
@@ -93,11 +94,13 @@ template <int D, int F>
 struct MakeRead {
     static ReadKernel get() { return es_kv_read_kernel<D, F>; }
 };
-template <int kMode>
+template <int kMode, int kCols>
 struct MakeSplit {
     template <int D, int F>
     struct Of {
-        static AttendKernel get() { return es_kv_split_kernel<D, F, kMode>; }
+        static AttendKernel get() {
+            return es_kv_split_kernel<D, F, kMode, D == 256 || F == kBf16 ? 1 : kCols>;
+        }
     };
 };
 template <int kMode>
@@ -211,7 +214,7 @@ int es_kv_create(const es_kv_desc_t* desc, es_kv_t** out) try {
     // at most two slots for each part aimed at (a sequence cut into c > 1 parts
     // has more than c - 1 parts' blocks)
     const uint64_t slot_rows = std::max(
-        uint64_t(2) * kMaxParts * kSplitRows,
+        uint64_t(2) * kMaxParts * 2 * kSplitRows,
         uint64_t(2) * (d.head_dim == 64    ? tile_launch<64>().slots()
                        : d.head_dim == 128 ? tile_launch<128>().slots()
                                            : tile_launch<256>().slots()));
@@ -425,11 +428,26 @@ int es_kv_attend(es_kv_t* kv, const es_kv_attend_t* args, es_stream_t stream) tr
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const uint64_t all_rows = uint64_t(x.rows) * a.group;      // of one key head
     const uint64_t seq_rows = std::min<uint64_t>(x.rows, std::max(1u, x.max_rows)) * a.group;
-    if (seq_rows <= kSplitRows) {
+    // Codes of long histories: up to 32 rows of a key head share one conversion in
+    // registers, where the tile kernel would turn them for 128 (wide heads leave no
+    // registers for it).  20 rows (40 heads over 8 x 128), E4M3, in split and tile
+    // kernel: 64 histories of 3000 tokens 88 and 109 us, of 1500 52 and 58, of 800 33
+    // and 32, 256 of 800 156 and 136; int8, 20 rows of 16 heads of 64, 64 of 2000 69
+    // and 125.  bf16, which the tile kernel loads straight into LDS, 16 of 2000: 36
+    // and 32.
+    const uint32_t cols = seq_rows > kSplitRows && format != kBf16 && dim < 256 &&
+                                  x.max_length >= kPairLength
+                              ? 2
+                              : 1;
+    if (seq_rows <= kSplitRows * cols) {
         // a history's scores cost little beside its bytes: one kernel for every mode but plain
         const AttendKernel kernel =
-            mode == kPlain ? by_dim_format<AttendKernel, MakeSplit<kPlain>::Of>(dim, format)
-                           : by_dim_format<AttendKernel, MakeSplit<kAny>::Of>(dim, format);
+            cols == 1 ? (mode == kPlain
+                             ? by_dim_format<AttendKernel, MakeSplit<kPlain, 1>::Of>(dim, format)
+                             : by_dim_format<AttendKernel, MakeSplit<kAny, 1>::Of>(dim, format))
+                      : (mode == kPlain
+                             ? by_dim_format<AttendKernel, MakeSplit<kPlain, 2>::Of>(dim, format)
+                             : by_dim_format<AttendKernel, MakeSplit<kAny, 2>::Of>(dim, format));
         // Two workgroups a compute unit stream as fast as more, and a part left over
         // for a second round costs as long as all of the first: with few histories,
         // room for each one's short last part.  8 histories of 50000 to 65537 tokens
@@ -439,7 +457,7 @@ int es_kv_attend(es_kv_t* kv, const es_kv_attend_t* args, es_stream_t stream) tr
         const uint64_t pairs = uint64_t(x.n_seqs) * heads;
         a.target = kMaxParts - (pairs <= kMaxParts / 4 ? static_cast<uint32_t>(pairs) : 0u);
         a.min_blocks = kMinBlocks;
-        return launch_parts(kernel, a, kSplitRows, kSplitThreads, 0, seq_rows, x.max_length, dim, s);
+        return launch_parts(kernel, a, kSplitRows * cols, kSplitThreads, 0, seq_rows, x.max_length, dim, s);
     }
     const AttendKernel kernel =
         mode == kPlain    ? by_dim_format<AttendKernel, MakeTile<kPlain>::Of>(dim, format)

@@ -204,6 +204,9 @@ __device__ __forceinline__ float max_quarters(float x) {
 // number of blocks, C = ceil(all blocks / target), and a workgroup finds its
 // sequence by a scan over the batch (a wave, 64 sequences at a time).
 //
+// The matrix unit's columns are 16 rows of a tile (kCols of them): two share the
+// loads and conversions of codes.
+//
 // Measured (one row, 40 query heads over 8 of 128): 8 histories of 30000, bf16,
 // 182 us, 5.4 TB/s; 8 of 60000, E4M3, 181 us, 5.5 TB/s; 32 of 201 to 16384, E4M3, 63
 // us with the join.
@@ -211,13 +214,13 @@ __device__ __forceinline__ float max_quarters(float x) {
 
 constexpr int kSplitThreads = 256;
 constexpr int kSplitWaves = kSplitThreads / 64;
-constexpr int kSplitRows = 16;              // of a tile
+constexpr int kSplitRows = 16;              // of a tile's column of operands
 constexpr int kScanRows = 64;               // rows of a sequence whose intervals the scan reads
 
 // Waves of a SIMD that the registers leave.
-template <int D, int kFmt>
+template <int D, int kFmt, int kCols>
 constexpr int split_waves() {
-    return D == 64 ? 4 : D == 128 && kFmt == kBf16 ? 3 : 2;
+    return D == 64 ? 4 / kCols : D == 128 && kFmt == kBf16 && kCols == 1 ? 3 : 2;
 }
 
 struct Span {                               // a sequence's blocks
@@ -351,8 +354,9 @@ __device__ __forceinline__ u32x4_t token_mask(int n) {
     return m;
 }
 
-template <int D, int kFmt, int kMode>
-__global__ __launch_bounds__(kSplitThreads, (split_waves<D, kFmt>())) void es_kv_split_kernel(AttendArgs a) {
+template <int D, int kFmt, int kMode, int kCols>
+__global__ __launch_bounds__(kSplitThreads, (split_waves<D, kFmt, kCols>())) void
+es_kv_split_kernel(AttendArgs a) {
     constexpr int kSteps = D / 32;                           // 32 dimensions a product
     constexpr int kDims = D / 16;                            // 16 dimensions a tile of O^T
     constexpr bool kBytes = kFmt != kBf16;
@@ -369,30 +373,38 @@ __global__ __launch_bounds__(kSplitThreads, (split_waves<D, kFmt>())) void es_kv
     const int base_key = L * g;                              // of this lane's keys in a step
     const uint32_t h = blockIdx.x % a.c.heads;
 
-    const Place at = find_place<true>(a, kSplitRows, blockIdx.x / a.c.heads);
+    const Place at = find_place<true>(a, kSplitRows * kCols, blockIdx.x / a.c.heads);
     if (!at.found) return;
 
-    // this lane's row: column n of the tile.  Columns past the last row repeat it
-    // and are not written.
+    // this lane's rows: columns n, 16 + n of the tile.  Columns past the last row
+    // repeat it and are not written.
     const int n_rows = at.seq.n * static_cast<int>(a.group);
-    const int row0 = static_cast<int>(at.tile) * kSplitRows;
-    const int r = row0 + n, rr = min(r, n_rows - 1);
-    const int i = rr / static_cast<int>(a.group);
-    const uint32_t head = h * a.group + (rr - i * static_cast<int>(a.group));
-    int first, limit;
-    interval(a, at.seq, i, first, limit);
-    const int pos = at.seq.len - at.seq.n + i;
-    const ScoreMap map = score_map<kMode, kBytes>(a, head);
-    int lo_any = first < limit ? first : at.seq.len, hi_any = limit;
-    int lo_all = first, hi_all = limit;
-    bf16x8_t q[kSteps];
-    {
-        const uint16_t* src = a.q + uint64_t(at.seq.start + i) * a.q_stride + uint64_t(head) * D;
+    const int row0 = static_cast<int>(at.tile) * kSplitRows * kCols;
+    int row_i[kCols], first[kCols], limit[kCols], pos[kCols];
+    uint32_t head[kCols];
+    ScoreMap map[kCols];
+    bf16x8_t q[kCols][kSteps];
+    int lo_any = at.seq.len, hi_any = 0, lo_all = 0, hi_all = at.seq.len;
+#pragma unroll
+    for (int c = 0; c < kCols; ++c) {
+        const int rr = min(row0 + kSplitRows * c + n, n_rows - 1);
+        const int i = rr / static_cast<int>(a.group);
+        row_i[c] = i;
+        head[c] = h * a.group + (rr - i * static_cast<int>(a.group));
+        interval(a, at.seq, i, first[c], limit[c]);
+        pos[c] = at.seq.len - at.seq.n + i;
+        map[c] = score_map<kMode, kBytes>(a, head[c]);
+        lo_any = min(lo_any, first[c] < limit[c] ? first[c] : at.seq.len);
+        hi_any = max(hi_any, limit[c]);
+        lo_all = max(lo_all, first[c]);
+        hi_all = min(hi_all, limit[c]);
+        const uint16_t* src =
+            a.q + uint64_t(at.seq.start + i) * a.q_stride + uint64_t(head[c]) * D;
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
             // the dimensions that a lane's words of a key hold: 8 of 32, or 16 of 64
             const int d = kBytes ? 64 * (s / 2) + 16 * g + 8 * (s & 1) : 32 * s + 8 * g;
-            q[s] = __builtin_bit_cast(bf16x8_t, load_row8(src + d));
+            q[c][s] = __builtin_bit_cast(bf16x8_t, load_row8(src + d));
         }
     }
 #pragma unroll
@@ -407,10 +419,15 @@ __global__ __launch_bounds__(kSplitThreads, (split_waves<D, kFmt>())) void es_kv
     lo_all = __builtin_amdgcn_readfirstlane(lo_all);
     hi_all = __builtin_amdgcn_readfirstlane(hi_all);
 
-    float top = -inf(), sum = 0.0f;
-    f32x4_t o[kDims];
+    float top[kCols], sum[kCols];
+    f32x4_t o[kCols][kDims];
 #pragma unroll
-    for (int d = 0; d < kDims; ++d) o[d] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int c = 0; c < kCols; ++c) {
+        top[c] = -inf();
+        sum[c] = 0.0f;
+#pragma unroll
+        for (int d = 0; d < kDims; ++d) o[c][d] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    }
 
     // the part's keys that some row of the tile sees, in whole steps
     const int part0 = at.block0 + static_cast<int>(at.chunk * at.per);
@@ -465,14 +482,14 @@ __global__ __launch_bounds__(kSplitThreads, (split_waves<D, kFmt>())) void es_kv
         const bool masked = key0 < lo_all || key0 + kKeys > hi_all;
         if constexpr (kBytes) {
 #pragma unroll
-            for (int t = 0; t < kKeyTiles; ++t) ks[t] *= map.factor;
+            for (int t = 0; t < kKeyTiles; ++t) ks[t] *= map[0].factor;
             if (left < kKeys) {
 #pragma unroll
                 for (int t = 0; t < L; ++t)
                     if (base_key + t >= left) vs[t >> 2][t & 3] = 0.0f;
             }
         }
-        f32x4_t s[kKeyTiles];
+        f32x4_t s[kCols][kKeyTiles];
 #pragma unroll
         for (int k = 0; k < kKeyTiles; ++k)
 #pragma unroll
@@ -487,58 +504,63 @@ __global__ __launch_bounds__(kSplitThreads, (split_waves<D, kFmt>())) void es_kv
                             codes_to_bf16<kFmt>(u32x2_t{kw[k][w][2 * y], kw[k][w][2 * y + 1]}));
                     else
                         x = __builtin_bit_cast(bf16x8_t, kw[k][w]);
-                    s[k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                        x, q[kHalves * w + y], w + y == 0 ? f32x4_t{} : s[k], 0, 0, 0);
+#pragma unroll
+                    for (int c = 0; c < kCols; ++c)
+                        s[c][k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                            x, q[c][kHalves * w + y], w + y == 0 ? f32x4_t{} : s[c][k], 0, 0, 0);
                 }
             }
-        // scores of this lane's keys key0 + base_key + 0 .. L - 1
-        float x[L];
+        bf16x8_t p[kCols][kPairs];
 #pragma unroll
-        for (int k = 0; k < L; ++k)
-            x[k] = kBytes ? s[k >> 2][k & 3] * ks[k >> 2][k & 3] : s[k >> 2][k & 3];
-        map_scores<kMode, kBytes>(map, x, static_cast<float>(pos - key0 - base_key),
-                                  [](int i) { return i; }, false);
-        if (bad) {
-#pragma unroll
-            for (int k = 0; k < L; ++k) x[k] = nan();
-        }
-        if (masked) {
-            const int from = first - key0 - base_key, to = limit - key0 - base_key;
+        for (int c = 0; c < kCols; ++c) {
+            // scores of a row and this lane's keys key0 + base_key + 0 .. L - 1
+            float x[L];
 #pragma unroll
             for (int k = 0; k < L; ++k)
-                if (k < from || k >= to) x[k] = unseen<kMode>();
-        }
-        float peak = x[0];
+                x[k] = kBytes ? s[c][k >> 2][k & 3] * ks[k >> 2][k & 3] : s[c][k >> 2][k & 3];
+            map_scores<kMode, kBytes>(map[c], x, static_cast<float>(pos[c] - key0 - base_key),
+                                      [](int i) { return i; }, false);
+            if (bad) {
 #pragma unroll
-        for (int k = 1; k < L; ++k) peak = larger<kMode>(peak, x[k]);
-        peak = max_quarters(__builtin_fmaf(peak, map.unit, map.offset));
-        const float now = __builtin_fmaxf(top, peak);
-        if (__any(now > top + kSlack)) {
-            const float shrink = __builtin_amdgcn_exp2f(top - (now == -inf() ? 0.0f : now));
-            sum *= shrink;
-#pragma unroll
-            for (int d = 0; d < kDims; ++d) o[d] *= shrink;
-            top = now;
-        }
-        // nothing seen so far: any finite stand-in gives weights of zero
-        const float base = map.offset - (top == -inf() ? 0.0f : top);
-        bf16x8_t p[kPairs];
-#pragma unroll
-        for (int u = 0; u < kPairs; ++u) {
-            u32x4_t w;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                float e[2];
-#pragma unroll
-                for (int y = 0; y < 2; ++y) {
-                    const int k = 8 * u + 2 * j + y;
-                    e[y] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[k], map.unit, base));
-                    sum += e[y];
-                    if constexpr (kBytes) e[y] *= vs[k >> 2][k & 3];
-                }
-                w[j] = pack_bf16(e[0], e[1]);
+                for (int k = 0; k < L; ++k) x[k] = nan();
             }
-            p[u] = __builtin_bit_cast(bf16x8_t, w);
+            if (masked) {
+                const int from = first[c] - key0 - base_key, to = limit[c] - key0 - base_key;
+#pragma unroll
+                for (int k = 0; k < L; ++k)
+                    if (k < from || k >= to) x[k] = unseen<kMode>();
+            }
+            float peak = x[0];
+#pragma unroll
+            for (int k = 1; k < L; ++k) peak = larger<kMode>(peak, x[k]);
+            peak = max_quarters(__builtin_fmaf(peak, map[c].unit, map[c].offset));
+            const float now = __builtin_fmaxf(top[c], peak);
+            if (__any(now > top[c] + kSlack)) {
+                const float shrink = __builtin_amdgcn_exp2f(top[c] - (now == -inf() ? 0.0f : now));
+                sum[c] *= shrink;
+#pragma unroll
+                for (int d = 0; d < kDims; ++d) o[c][d] *= shrink;
+                top[c] = now;
+            }
+            // nothing seen so far: any finite stand-in gives weights of zero
+            const float base = map[c].offset - (top[c] == -inf() ? 0.0f : top[c]);
+#pragma unroll
+            for (int u = 0; u < kPairs; ++u) {
+                u32x4_t w;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    float e[2];
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        const int k = 8 * u + 2 * j + y;
+                        e[y] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[k], map[c].unit, base));
+                        sum[c] += e[y];
+                        if constexpr (kBytes) e[y] *= vs[k >> 2][k & 3];
+                    }
+                    w[j] = pack_bf16(e[0], e[1]);
+                }
+                p[c][u] = __builtin_bit_cast(bf16x8_t, w);
+            }
         }
         if (bad && a.status != nullptr && lane == 0) atomicOr(a.status, ES_KV_BAD_PAGE);
         if (left < kKeys) {
@@ -558,56 +580,71 @@ __global__ __launch_bounds__(kSplitThreads, (split_waves<D, kFmt>())) void es_kv
                         bf16x8_t, codes_to_bf16<kFmt>(u32x2_t{vw[d][2 * u], vw[d][2 * u + 1]}));
                 else
                     v = __builtin_bit_cast(bf16x8_t, vw[d]);
-                o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[u], o[d], 0, 0, 0);
+#pragma unroll
+                for (int c = 0; c < kCols; ++c)
+                    o[c][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[c][u], o[c][d], 0, 0, 0);
             }
         }
     }
 
     // join the waves: the others hand their sums to wave 0 through LDS
-    __shared__ float ml[kSplitWaves][2][16];
-    __shared__ __attribute__((aligned(16))) f32x4_t part[kSplitWaves - 1][kDims][64];
-    sum += __shfl_xor(sum, 16);
-    sum += __shfl_xor(sum, 32);
-    if (g == 0) {
-        ml[wave][0][n] = top;
-        ml[wave][1][n] = sum;
-    }
-    __syncthreads();
-    float m = -inf();
+    __shared__ float ml[kCols][kSplitWaves][2][16];
+    __shared__ __attribute__((aligned(16))) f32x4_t part[kCols][kSplitWaves - 1][kDims][64];
 #pragma unroll
-    for (int w = 0; w < kSplitWaves; ++w) m = __builtin_fmaxf(m, ml[w][0][n]);
-    const float base = m == -inf() ? 0.0f : m;
-    const float mine = __builtin_amdgcn_exp2f(top - base);
-    if (wave > 0) {
-#pragma unroll
-        for (int d = 0; d < kDims; ++d) part[wave - 1][d][lane] = o[d] * mine;
-    }
-    __syncthreads();
-    if (wave > 0 || r >= n_rows) return;
-    float total = 0.0f;
-#pragma unroll
-    for (int w = 0; w < kSplitWaves; ++w)
-        total += ml[w][1][n] * __builtin_amdgcn_exp2f(ml[w][0][n] - base);
-    const bool whole = at.chunks == 1;
-    const float inv = total > 0.0f || total != total ? 1.0f / total : 0.0f;
-    const uint64_t slot = ((uint64_t(at.slot) + at.chunk) * a.c.heads + h) * kSplitRows + n;
-    uint16_t* out = a.out + uint64_t(at.seq.start + i) * a.out_stride + uint64_t(head) * D;
-#pragma unroll
-    for (int d = 0; d < kDims; ++d) {
-        f32x4_t x = o[d] * mine;
-#pragma unroll
-        for (int w = 0; w < kSplitWaves - 1; ++w) x += part[w][d][lane];
-        if (whole) {
-            x *= inv;
-            store_row4(out + 16 * d + 4 * g,
-                       u32x2_t{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])});
-        } else {
-            store<f32x4_t>(a.part_o + slot * D + 16 * d + 4 * g, x);
+    for (int c = 0; c < kCols; ++c) {
+        sum[c] += __shfl_xor(sum[c], 16);
+        sum[c] += __shfl_xor(sum[c], 32);
+        if (g == 0) {
+            ml[c][wave][0][n] = top[c];
+            ml[c][wave][1][n] = sum[c];
         }
     }
-    if (!whole && g == 0) {
-        a.part_ml[2 * slot] = m;
-        a.part_ml[2 * slot + 1] = total;
+    __syncthreads();
+    float m[kCols], mine[kCols];
+#pragma unroll
+    for (int c = 0; c < kCols; ++c) {
+        m[c] = -inf();
+#pragma unroll
+        for (int w = 0; w < kSplitWaves; ++w) m[c] = __builtin_fmaxf(m[c], ml[c][w][0][n]);
+        mine[c] = __builtin_amdgcn_exp2f(top[c] - (m[c] == -inf() ? 0.0f : m[c]));
+        if (wave > 0) {
+#pragma unroll
+            for (int d = 0; d < kDims; ++d) part[c][wave - 1][d][lane] = o[c][d] * mine[c];
+        }
+    }
+    __syncthreads();
+    if (wave > 0) return;
+    const bool whole = at.chunks == 1;
+#pragma unroll
+    for (int c = 0; c < kCols; ++c) {
+        if (row0 + kSplitRows * c + n >= n_rows) continue;
+        const float base = m[c] == -inf() ? 0.0f : m[c];
+        float total = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kSplitWaves; ++w)
+            total += ml[c][w][1][n] * __builtin_amdgcn_exp2f(ml[c][w][0][n] - base);
+        const float inv = total > 0.0f || total != total ? 1.0f / total : 0.0f;
+        const uint64_t slot =
+            (((uint64_t(at.slot) + at.chunk) * a.c.heads + h) * kCols + c) * kSplitRows + n;
+        uint16_t* out =
+            a.out + uint64_t(at.seq.start + row_i[c]) * a.out_stride + uint64_t(head[c]) * D;
+#pragma unroll
+        for (int d = 0; d < kDims; ++d) {
+            f32x4_t x = o[c][d] * mine[c];
+#pragma unroll
+            for (int w = 0; w < kSplitWaves - 1; ++w) x += part[c][w][d][lane];
+            if (whole) {
+                x *= inv;
+                store_row4(out + 16 * d + 4 * g,
+                           u32x2_t{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])});
+            } else {
+                store<f32x4_t>(a.part_o + slot * D + 16 * d + 4 * g, x);
+            }
+        }
+        if (!whole && g == 0) {
+            a.part_ml[2 * slot] = m[c];
+            a.part_ml[2 * slot + 1] = total;
+        }
     }
 }
 

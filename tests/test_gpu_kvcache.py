@@ -403,6 +403,29 @@ def test_few_rows_of_long_histories(form, dim, group, kv_heads):
 
 
 @pytest.mark.parametrize("form", FORMATS)
+@pytest.mark.parametrize("dim,group,kv_heads", [(64, 3, 2), (128, 5, 2), (128, 17, 1), (256, 5, 1)])
+def test_seventeen_to_thirty_two_rows(form, dim, group, kv_heads):
+    """Rows of a key head between one tile's columns of the matrix unit and
+    two, beside fewer and none, plain, with every change of the scores, with
+    intervals, and where more rows come than the caller's bound says."""
+    rng = np.random.default_rng([dim, group, 17])
+    top = 32 // group
+    b = Batch(rng, form, dim, group, kv_heads, 64, [3000, 1300, 64, 129, 9, 0, 700],
+              [top, max(1, top - 1), 1, 1, top, 0, top])
+    b.check(b.attend())
+    slopes = 2.0 ** -rng.integers(0, 6, group * kv_heads)
+    b.check(b.attend(slopes=slopes, cap=3.0, scale=0.2), slopes=slopes, cap=3.0, scale=0.2)
+    total = int(b.starts[-1])
+    first, limit = rng.integers(-5, 1400, total), rng.integers(-5, 3100, total)
+    first[0], limit[0] = 40, 40                            # beside rows that see something
+    b.check(b.attend(first=first, limit=limit), first=first, limit=limit)
+    assert not b.attend(first=np.full(total, 8), limit=np.full(total, 8)).any()
+    more = Batch(rng, form, dim, group, kv_heads, 128, [1500, 200, 77], [3 * top, 1, 2 * top + 1])
+    more.check(more.attend(max_rows=top))
+    more.check(more.attend(max_rows=top, max_length=1280))
+
+
+@pytest.mark.parametrize("form", FORMATS)
 @pytest.mark.parametrize("dim,group,kv_heads,page", [(64, 1, 3, 64), (128, 5, 2, 128), (256, 4, 1, 256),
                                                      (128, 1, 2, 1024), (64, 7, 1, 64)])
 def test_prompts(form, dim, group, kv_heads, page):
