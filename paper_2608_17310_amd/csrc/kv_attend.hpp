@@ -830,32 +830,46 @@ es_kv_tile_kernel(AttendArgs a) {
     }
 
     // what the wave's rows see, some and all of them; and the workgroup's
-    int lo_any = first < limit ? first : at.seq.len, hi_any = limit;
-    int lo_all = first, hi_all = limit;
+    int lo_any, hi_any, lo_all, hi_all, lo, hi;
+    if (a.first == nullptr && a.limit == nullptr) {
+        // up to their own positions, which grow with rows: no wave waits for another
+        lo_all = lo = 0;
+        hi_all = from_lane(limit, 0);
+        hi_any = from_lane(limit, 31);
+        lo_any = hi_any > 0 ? 0 : at.seq.len;
+        const int last = min(static_cast<int>(at.tile + 1) * S::kRows, n_rows) - 1;
+        hi = min(at.seq.len, at.seq.len - at.seq.n + last / static_cast<int>(a.group) + 1);
+    } else {
+        lo_any = first < limit ? first : at.seq.len;
+        hi_any = limit;
+        lo_all = first;
+        hi_all = limit;
 #pragma unroll
-    for (int m = 1; m < 32; m *= 2) {
-        lo_any = min(lo_any, __shfl_xor(lo_any, m));
-        hi_any = max(hi_any, __shfl_xor(hi_any, m));
-        lo_all = max(lo_all, __shfl_xor(lo_all, m));
-        hi_all = min(hi_all, __shfl_xor(hi_all, m));
-    }
-    lo_any = __builtin_amdgcn_readfirstlane(lo_any);
-    hi_any = __builtin_amdgcn_readfirstlane(hi_any);
-    lo_all = __builtin_amdgcn_readfirstlane(lo_all);
-    hi_all = __builtin_amdgcn_readfirstlane(hi_all);
-    if (lane == 0) {
-        bounds[0][wave] = lo_any;
-        bounds[1][wave] = hi_any;
-    }
-    __syncthreads();
-    int lo = at.seq.len, hi = 0;
+        for (int m = 1; m < 32; m *= 2) {
+            lo_any = min(lo_any, __shfl_xor(lo_any, m));
+            hi_any = max(hi_any, __shfl_xor(hi_any, m));
+            lo_all = max(lo_all, __shfl_xor(lo_all, m));
+            hi_all = min(hi_all, __shfl_xor(hi_all, m));
+        }
+        lo_any = __builtin_amdgcn_readfirstlane(lo_any);
+        hi_any = __builtin_amdgcn_readfirstlane(hi_any);
+        lo_all = __builtin_amdgcn_readfirstlane(lo_all);
+        hi_all = __builtin_amdgcn_readfirstlane(hi_all);
+        if (lane == 0) {
+            bounds[0][wave] = lo_any;
+            bounds[1][wave] = hi_any;
+        }
+        __syncthreads();
+        lo = at.seq.len;
+        hi = 0;
 #pragma unroll
-    for (int w = 0; w < S::kWaves; ++w) {
-        lo = min(lo, bounds[0][w]);
-        hi = max(hi, bounds[1][w]);
+        for (int w = 0; w < S::kWaves; ++w) {
+            lo = min(lo, bounds[0][w]);
+            hi = max(hi, bounds[1][w]);
+        }
+        lo = __builtin_amdgcn_readfirstlane(lo);
+        hi = __builtin_amdgcn_readfirstlane(hi);
     }
-    lo = __builtin_amdgcn_readfirstlane(lo);
-    hi = __builtin_amdgcn_readfirstlane(hi);
     int b_begin = lo / kBlock, b_end = hi > lo ? (hi - 1) / kBlock + 1 : b_begin;
     if (parts) {
         const int part0 = at.block0 + static_cast<int>(at.chunk * at.per);
