@@ -1301,13 +1301,15 @@ def _counters_for(path, kind, label):
 
 
 def _kernel_source_hash():
-    """Hash of the device code the counters describe: the device headers and
-    the device section of esopt.hip (host-side edits leave the kernels, and so
-    the counters, unchanged)."""
+    """Hash of the device code the counters describe: the device section of
+    esopt.hip and its device headers (host-side edits, and the cache's and
+    attention's kernels, kv_*.hpp, leave these kernels, and so the counters,
+    unchanged)."""
     import hashlib
     csrc = os.path.join(REPO, "paper_2608_17310_amd", "csrc")
     h = hashlib.sha256()
-    for f in sorted(x for x in os.listdir(csrc) if x.endswith(".hpp")):
+    for f in sorted(x for x in os.listdir(csrc) if x.endswith(".hpp")
+                    and x != "es_host.hpp" and not x.startswith("kv_")):
         h.update(open(os.path.join(csrc, f), "rb").read())
     src = open(os.path.join(csrc, "esopt.hip"), "rb").read()
     start, end = src.index(b"// Device code"), src.index(b"// Host side")

@@ -2,6 +2,7 @@
 noise the update generates, and the refusal of more than one GPU."""
 import json
 import os
+import shutil
 import subprocess
 import sys
 
@@ -149,3 +150,21 @@ def test_kernel_names_keep_their_template_arguments():
             ("__amd_rocclr_copyBuffer", "__amd_rocclr_copyBuffer")):
         assert bench._short_name(name) == short
     assert bench._short_name("void f<" + "x" * 200 + ">(int)") == "f<" + "x" * 85 + "..."
+
+
+def test_counters_belong_to_the_kernels_they_describe(tmp_path, monkeypatch):
+    """Edits of other kernels and of host code keep the counters, edits of the
+    passes' kernels or headers drop them."""
+    csrc = tmp_path / "paper_2608_17310_amd" / "csrc"
+    shutil.copytree(os.path.join(bench.REPO, "paper_2608_17310_amd", "csrc"), csrc)
+    monkeypatch.setattr(bench, "REPO", str(tmp_path))
+    before = bench._kernel_source_hash()
+    for name in ("es_host.hpp", "kv_common.hpp", "kv_attend.hpp", "kv_place.hpp", "eskv.hip"):
+        with open(csrc / name, "a") as f:
+            f.write("// more\n")
+        assert bench._kernel_source_hash() == before, name
+    for name in ("es_noise.hpp", "es_quant.hpp", "es_fp8.hpp"):
+        with open(csrc / name, "a") as f:
+            f.write("// more\n")
+        assert bench._kernel_source_hash() != before, name
+        before = bench._kernel_source_hash()
