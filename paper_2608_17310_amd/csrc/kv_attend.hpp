@@ -727,8 +727,8 @@ __global__ __launch_bounds__(kSplitThreads) void es_kv_join_kernel(AttendArgs a,
 // another workgroup's fill the other unit meanwhile (one of eight waves was as fast
 // in bf16 and 8 % slower from codes).
 //
-// Measured: a prompt of 8192 (40 heads over 8 of 128, bf16) 672 us, 1.02 PFLOP/s of
-// visible products, the matrix unit busy 49 % of cycles at 1.95 GHz; without the
+// Measured: a prompt of 8192 (40 heads over 8 of 128, bf16) 660 us, 1.04 PFLOP/s of
+// visible products, the matrix unit busy 53 % of cycles at 1.95 GHz; without the
 // staging loads 14 % less, without the exponentials 7 %.  16 ragged prompts up to
 // 2039 (int8, bias) 205 us, 0.56 PFLOP/s.
 //
