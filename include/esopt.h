@@ -647,7 +647,7 @@ uint64_t es_kv_device_bytes(const es_kv_t* kv);
 /* One call appends `tokens` new tokens, and normalises and rotates their
  * queries in the same pass.  A row is one head of one token (head_dim bf16
  * values); heads of a token are adjacent, tokens are `*_stride` elements apart
- * (any stride: a packed projection can be passed as it is).
+ * (any stride up to 2^38: a packed projection can be passed as it is).
  *
  * For queries and keys, in binary32: x <- x rsqrt(mean(x^2) + eps) gain
  * (where the gain is given), then the rotation of the first `rot` dimensions:

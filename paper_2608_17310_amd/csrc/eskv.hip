@@ -45,11 +45,15 @@ int check_kv_device(const es_kv_t* kv, const char* name) {
 
 bool odd(const void* p, uintptr_t align) { return reinterpret_cast<uintptr_t>(p) % align != 0; }
 
-// `rows` rows of `width` bf16, `stride` elements apart.
+// Elements from row to row at most: 2^24 rows of them are 2^63 bytes, so that the
+// extent of an array fits 64 bits.
+constexpr uint64_t kMaxStride = uint64_t(1) << 38;
+
+bool too_wide(uint64_t rows, uint64_t stride) { return rows > 1 && stride > kMaxStride; }
+
+// `rows` rows of `width` bf16, `stride` elements apart (at most kMaxStride).
 void check_rows(Accesses& x, const void* p, uint64_t rows, uint64_t width, uint64_t stride,
                 const char* part) {
-    if (x.rc == ES_OK && stride > (uint64_t(1) << 40))
-        x.rc = fail(ES_ERR_INVALID_ARG, std::string(x.name) + part + ": stride above 2^40");
     x.check(p, 2 * ((rows - 1) * stride + width), part);
 }
 
@@ -261,6 +265,9 @@ int es_kv_append(es_kv_t* kv, const es_kv_append_t* args, es_stream_t stream) tr
         return fail_in(ES_ERR_INVALID_ARG, name, "null pointer");
     if (x.q_heads != 0 && x.tokens > 1 && x.q_out_stride < uint64_t(x.q_heads) * dim)
         return fail_in(ES_ERR_INVALID_ARG, name, "q_out's rows overlap");
+    if (too_wide(x.tokens, x.k_stride) || too_wide(x.tokens, x.v_stride) ||
+        (x.q_heads != 0 && (too_wide(x.tokens, x.q_stride) || too_wide(x.tokens, x.q_out_stride))))
+        return fail_in(ES_ERR_INVALID_ARG, name, "stride above 2^38");
     if (odd(x.q, 2) || odd(x.k, 2) || odd(x.v, 2) || odd(x.q_out, 2) || odd(x.q_gain, 2) ||
         odd(x.k_gain, 2) || odd(x.rope, 4) || odd(x.positions, 4) || odd(x.slots, 8) ||
         odd(x.status, 4))
@@ -330,6 +337,8 @@ int es_kv_read(es_kv_t* kv, const int64_t* slots, uint32_t tokens, void* k_out, 
     const uint64_t width = uint64_t(kv->d.kv_heads) * kv->d.head_dim;
     if (tokens > 1 && (k_stride < width || v_stride < width))
         return fail_in(ES_ERR_INVALID_ARG, name, "the output's rows overlap");
+    if (too_wide(tokens, k_stride) || too_wide(tokens, v_stride))
+        return fail_in(ES_ERR_INVALID_ARG, name, "stride above 2^38");
     if (odd(slots, 8) || odd(k_out, 2) || odd(v_out, 2) || odd(status, 4))
         return fail_in(ES_ERR_ALIGN, name, "array not aligned to its elements");
     const int rc = check_kv_device(kv, name);
@@ -382,6 +391,8 @@ int es_kv_attend(es_kv_t* kv, const es_kv_attend_t* args, es_stream_t stream) tr
     const uint64_t width = uint64_t(x.q_heads) * dim;
     if (x.rows > 1 && x.out_stride < width)
         return fail_in(ES_ERR_INVALID_ARG, name, "the output's rows overlap");
+    if (too_wide(x.rows, x.q_stride) || too_wide(x.rows, x.out_stride))
+        return fail_in(ES_ERR_INVALID_ARG, name, "stride above 2^38");
     if (odd(x.q, 2) || odd(x.out, 2) || odd(x.tables, 4) || odd(x.lengths, 4) || odd(x.starts, 4) ||
         odd(x.first, 4) || odd(x.limit, 4) || odd(x.slopes, 4) || odd(x.status, 4))
         return fail_in(ES_ERR_ALIGN, name, "array not aligned to its elements");

@@ -167,3 +167,21 @@ def test_binding_refuses_shapes_and_types():
         kvc.KVCache(bf, bf[:, :1])
     with pytest.raises(ValueError, match="format"):
         kvc.KVCache.allocate(1, 1, 64, "fp4", device="cpu")
+
+
+def test_strides_whose_extent_leaves_64_bits_are_refused(lib, fake):
+    """2^23 rows of 2^40 elements are 2^64 bytes: an extent that wraps to a few
+    bytes would pass the check of the allocation.  No device is asked."""
+    h, n, far = ctypes.byref(fake), (1 << 23) + 1, 1 << 40
+    for name in ("q_stride", "k_stride", "v_stride", "q_out_stride"):
+        for stride in (far, (1 << 38) + 1, (1 << 64) - 1):
+            a = _append(tokens=n, **{name: stride})
+            assert lib.es_kv_append(h, ctypes.byref(a), None) == E, name
+            assert "stride" in esopt.last_error()
+    for strides in ((far, 128), (128, far)):
+        assert lib.es_kv_read(h, 0x1000, n, 0x2000, strides[0], 0x3000, strides[1], None, None) == E
+        assert "stride" in esopt.last_error()
+    for name in ("q_stride", "out_stride"):
+        a = _attend(rows=n, **{name: far})
+        assert lib.es_kv_attend(h, ctypes.byref(a), None) == E
+        assert "stride" in esopt.last_error()
