@@ -689,7 +689,7 @@ int es_kv_read(es_kv_t* kv, const int64_t* slots, uint32_t tokens, void* k_out, 
 
 /* Attention of `rows` query rows (tokens of all sequences, packed) over the
  * cache.  Sequence s has the rows starts[s] .. starts[s + 1] and lengths[s]
- * tokens in the cache, its rows' own tokens among them: row i of its n
+ * tokens (at most 2^31 - 1024) in the cache, its rows' own among them: row i of its n
  * stands at position p = lengths[s] - n + i.  It sees the keys first <= j < limit,
  * by default 0 <= j <= p; first[row] and limit[row] set other intervals (packed
  * documents, a prefix that all rows see, a window), clipped to 0 .. lengths[s].

@@ -24,6 +24,9 @@
 namespace eskv {
 
 constexpr int kBlock = 64;                  // keys of a block: never more than a page
+// Tokens of a sequence at most: the kernels count keys in 32 bits with a sign, up to 512
+// (two steps of a workgroup) past the last.
+constexpr int64_t kMaxLength = (int64_t(1) << 31) - 1024;
 
 struct AttendArgs {
     const uint16_t* q;
@@ -53,7 +56,7 @@ struct Seq {
 __device__ __forceinline__ Seq read_seq(const AttendArgs& a, uint32_t s) {
     const int rows = static_cast<int>(a.rows);
     const int s0 = a.starts[s], s1 = a.starts[s + 1], len = a.lengths[s];
-    const int64_t room = int64_t(a.table_stride) << a.c.page_shift;
+    const int64_t room = min(int64_t(a.table_stride) << a.c.page_shift, kMaxLength);
     Seq q;
     q.start = min(max(s0, 0), rows);
     q.n = min(max(s1, q.start), rows) - q.start;

@@ -733,3 +733,39 @@ def test_memory_that_the_device_cannot_use_is_refused():
     assert "past the end" in esopt.last_error()
     with pytest.raises(ValueError):
         cache.attend(k.float(), *[slots] * 3)
+
+
+@pytest.mark.parametrize("form", FORMATS)
+@pytest.mark.parametrize("n", [1, 40])
+def test_the_longest_sequences(form, n):
+    """The last keys of 2^31 - 1024 tokens are reached, and a longer sequence is
+    cut to as many and reported: a key's number, and that of the keys asked for
+    ahead of it, stays below 2^31."""
+    rng = np.random.default_rng([25, n])
+    heads, group, dim, page, seen = 1, 4, 64, 1024, 100
+    longest = (1 << 31) - 1024
+    cache = KVCache.allocate(2, heads, dim, form, page)
+    k, v = rows(rng, seen, heads, dim), rows(rng, seen, heads, dim)
+    slots = dev(page + np.arange(page - seen, page), torch.int64)
+    cache.append(k, v, slots)
+    if form == "bf16":
+        kx, vx = f64(k), f64(v)
+    else:
+        kx, vx = (oa.code_values(t.view(torch.uint8)[1].cpu().numpy().transpose(axes)[-seen:],
+                                 s[1].cpu().numpy().T[-seen:], form)
+                  for t, s, axes in ((cache.k_pages, cache.k_scales, (1, 0, 2)),
+                                     (cache.v_pages, cache.v_scales, (2, 0, 1))))
+    table = torch.zeros(1, 1 << 21, dtype=torch.int32, device="cuda")
+    table[0, (1 << 21) - 2] = 1                            # the page of the last 1024 tokens
+    q = rows(rng, n, heads * group, dim)
+    first = dev(np.full(n, longest - seen), torch.int32)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    for length, want in ((longest, 0), (longest + 1, kvc.ES_KV_BAD_LENGTH),
+                         ((1 << 31) - 1, kvc.ES_KV_BAD_LENGTH)):
+        status.zero_()
+        got = cache.attend(q, table, dev([length], torch.int32), dev([0, n], torch.int32),
+                           first=first, status=status)
+        assert status.item() == want
+        exact, spread = oa.attend(f64(q), kx, vx, dim ** -0.5)
+        assert np.all(np.abs(f64(got) - exact)
+                      <= U * np.abs(exact) + (U * (1 + 2.0 ** -6) + 2.0 ** -16) * spread)
