@@ -697,9 +697,12 @@ int es_kv_read(es_kv_t* kv, const int64_t* slots, uint32_t tokens, void* k_out, 
  *   t_j = scale q . k_j;  t_j <- cap tanh(t_j / cap) where cap > 0;
  *   t_j <- t_j - slopes[h] |p - j| where slopes are given;
  *   out = sum_j softmax(t)_j v_j, rounded once to bf16 (RNE).
- * A row that sees nothing returns zeros.  Rows that no sequence has are not
- * written.  Sums, maxima and products are held in binary32; the softmax's
- * weights (times the values' scales) are rounded to bf16 for the matrix unit.
+ * A row that sees nothing returns zeros.  Slots that a row does not see do not
+ * reach it, whatever they hold (never stored, reused, not finite); a slot that it
+ * sees must have been stored: its value and value scale are finite then.  Rows
+ * that no sequence has are not written.  Sums, maxima and products are held in
+ * binary32; the softmax's weights (times the values' scales) are rounded to bf16
+ * for the matrix unit.
  * max_rows and max_length are the largest rows and lengths[s] that the caller
  * expects: they choose how the work is cut, and nothing is lost where a
  * sequence exceeds them.  Calls on one handle must be ordered (one stream, or

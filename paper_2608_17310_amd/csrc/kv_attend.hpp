@@ -343,20 +343,6 @@ __device__ __forceinline__ Place find_place(const AttendArgs& a, int tile_rows, 
     return r;
 }
 
-// Keep the first n of the tokens of a 16-byte word.
-template <int kFmt>
-__device__ __forceinline__ u32x4_t token_mask(int n) {
-    constexpr int kPer = 4 / kCodeBytes<kFmt>;               // tokens of a 32-bit word
-    constexpr int kBits = 8 * kCodeBytes<kFmt>;
-    u32x4_t m;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-        const int k = n - kPer * w;
-        m[w] = k <= 0 ? 0u : k >= kPer ? ~0u : (1u << (kBits * k)) - 1u;
-    }
-    return m;
-}
-
 template <int D, int kFmt, int kMode, int kCols>
 __global__ __launch_bounds__(kSplitThreads, (split_waves<D, kFmt, kCols>())) void
 es_kv_split_kernel(AttendArgs a) {
@@ -480,16 +466,15 @@ es_kv_split_kernel(AttendArgs a) {
             }
         }
 
-        // tokens of the step: slots past the sequence's end may hold anything
-        const int left = bad ? 0 : at.seq.len - key0;
+        // slots that a row does not see may hold anything; its weight of zero meets
+        // finite values
         const bool masked = key0 < lo_all || key0 + kKeys > hi_all;
         if constexpr (kBytes) {
 #pragma unroll
             for (int t = 0; t < kKeyTiles; ++t) ks[t] *= map[0].factor;
-            if (left < kKeys) {
+            if (masked) {
 #pragma unroll
-                for (int t = 0; t < L; ++t)
-                    if (base_key + t >= left) vs[t >> 2][t & 3] = 0.0f;
+                for (int t = 0; t < L; ++t) vs[t >> 2][t & 3] = finite_scale(vs[t >> 2][t & 3]);
             }
         }
         f32x4_t s[kCols][kKeyTiles];
@@ -566,12 +551,11 @@ es_kv_split_kernel(AttendArgs a) {
             }
         }
         if (bad && a.status != nullptr && lane == 0) atomicOr(a.status, ES_KV_BAD_PAGE);
-        if (left < kKeys) {
-            const u32x4_t keep = token_mask<kFmt>(left - base_key);
+        if (masked && kFmt != kInt8) {
 #pragma unroll
             for (int d = 0; d < kDims; ++d)
 #pragma unroll
-                for (int w = 0; w < L * kCodeBytes<kFmt> / 4; ++w) vw[d][w] &= keep[w];
+                for (int w = 0; w < L * kCodeBytes<kFmt> / 4; ++w) vw[d][w] = finite<kFmt>(vw[d][w]);
         }
 #pragma unroll
         for (int d = 0; d < kDims; ++d) {
@@ -801,7 +785,7 @@ es_kv_tile_kernel(AttendArgs a) {
     const uint32_t h = blockIdx.x % a.c.heads;
 
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
-    __shared__ int bounds[2][S::kWaves];
+    __shared__ int bounds[4][S::kWaves];
 
     const bool parts = a.target != 0;
     const Place at = parts ? find_place<true>(a, S::kRows, blockIdx.x / a.c.heads)
@@ -816,7 +800,8 @@ es_kv_tile_kernel(AttendArgs a) {
     int first, limit;
     interval(a, at.seq, i, first, limit);
     // a wave of no rows (the last tile's) sees nothing and passes every block
-    if (static_cast<int>(at.tile) * S::kRows + 32 * wave >= n_rows) first = limit = 0;
+    const bool has_rows = static_cast<int>(at.tile) * S::kRows + 32 * wave < n_rows;
+    if (!has_rows) first = limit = 0;
     const int pos = at.seq.len - at.seq.n + i;
     const ScoreMap map = score_map<kMode, kBytes>(a, head);
     // positions grow with rows.  Steep slopes take distances one by one: a block's
@@ -832,16 +817,18 @@ es_kv_tile_kernel(AttendArgs a) {
             q[s] = __builtin_bit_cast(bf16x8_t, load_row8(src + 16 * s + 8 * g));
     }
 
-    // what the wave's rows see, some and all of them; and the workgroup's
-    int lo_any, hi_any, lo_all, hi_all, lo, hi;
+    // what the wave's rows see, some and all of them; and the workgroup's (whole: all)
+    int lo_any, hi_any, lo_all, hi_all, lo, hi, whole_lo, whole_hi;
     if (a.first == nullptr && a.limit == nullptr) {
         // up to their own positions, which grow with rows: no wave waits for another
-        lo_all = lo = 0;
+        lo_all = lo = whole_lo = 0;
         hi_all = from_lane(limit, 0);
         hi_any = from_lane(limit, 31);
         lo_any = hi_any > 0 ? 0 : at.seq.len;
         const int last = min(static_cast<int>(at.tile + 1) * S::kRows, n_rows) - 1;
         hi = min(at.seq.len, at.seq.len - at.seq.n + last / static_cast<int>(a.group) + 1);
+        const int lead = static_cast<int>(at.tile) * S::kRows / static_cast<int>(a.group);
+        whole_hi = min(at.seq.len, at.seq.len - at.seq.n + lead + 1);
     } else {
         lo_any = first < limit ? first : at.seq.len;
         hi_any = limit;
@@ -861,17 +848,23 @@ es_kv_tile_kernel(AttendArgs a) {
         if (lane == 0) {
             bounds[0][wave] = lo_any;
             bounds[1][wave] = hi_any;
+            bounds[2][wave] = has_rows ? lo_all : 0;
+            bounds[3][wave] = has_rows ? hi_all : at.seq.len;
         }
         __syncthreads();
-        lo = at.seq.len;
-        hi = 0;
+        lo = whole_hi = at.seq.len;
+        hi = whole_lo = 0;
 #pragma unroll
         for (int w = 0; w < S::kWaves; ++w) {
             lo = min(lo, bounds[0][w]);
             hi = max(hi, bounds[1][w]);
+            whole_lo = max(whole_lo, bounds[2][w]);
+            whole_hi = min(whole_hi, bounds[3][w]);
         }
         lo = __builtin_amdgcn_readfirstlane(lo);
         hi = __builtin_amdgcn_readfirstlane(hi);
+        whole_lo = __builtin_amdgcn_readfirstlane(whole_lo);
+        whole_hi = __builtin_amdgcn_readfirstlane(whole_hi);
     }
     int b_begin = lo / kBlock, b_end = hi > lo ? (hi - 1) / kBlock + 1 : b_begin;
     if (parts) {
@@ -896,6 +889,10 @@ es_kv_tile_kernel(AttendArgs a) {
         k_off[x] = key_word<D>(kr, kw);
         v_off[x] = vr * val_row + 16 * (vw ^ ((vr >> 1) & 7));
     }
+    // Slots that a row does not see may hold anything: in blocks that not all rows
+    // see in full, values that are not finite are cleared, so that a weight of zero
+    // gives zero.  (Stored tokens have none; in other blocks every row sees them.)
+    auto unclear = [&](int b) { return b * kBlock < whole_lo || (b + 1) * kBlock > whole_hi; };
     u32x4_t sk[kBytes ? kStage : 1], sv[kBytes ? kStage : 1];
     float sscale = 0.0f;
     bool bad = false, bad_next = false;
@@ -935,10 +932,13 @@ es_kv_tile_kernel(AttendArgs a) {
         if (bad_next && a.status != nullptr && threadIdx.x == 0)
             atomicOr(a.status, ES_KV_BAD_PAGE);
     };
-    // (keys' scales carry the scores' first factor; values' past the sequence's
-    // end, where slots may hold anything, are 0)
+    // (keys' scales carry the scores' first factor)
     auto stage = [&](int b, uint8_t* buf, float* scales) {
         if constexpr (kBytes) {
+            if (unclear(b)) {
+                make_finite<kFmt>(sv);
+                if (wave >= kBlock / 64) sscale = finite_scale(sscale);
+            }
 #pragma unroll
             for (int x = 0; x < kStage; ++x) {
                 const int w = threadIdx.x + S::kThreads * x;
@@ -956,13 +956,25 @@ es_kv_tile_kernel(AttendArgs a) {
             if (threadIdx.x < kBlock)
                 scales[threadIdx.x] = sscale * map.factor;
             else if (threadIdx.x < 2 * kBlock)
-                scales[threadIdx.x] =
-                    bad_next || b * kBlock + int(threadIdx.x) - kBlock >= at.seq.len ? 0.0f : sscale;
+                scales[threadIdx.x] = sscale;
         }
     };
     // the block has landed in LDS for every wave
-    auto arrive = [&]() {
-        if constexpr (!kBytes) wait_loads();
+    auto arrive = [&](int b, uint8_t* buf) {
+        if constexpr (!kBytes) {
+            wait_loads();
+            if (b < b_end && unclear(b)) {
+                u32x4_t* const v =               // the words that this lane loaded
+                    reinterpret_cast<u32x4_t*>(buf + S::kKeyBytes + wave * kStage * 1024) + lane;
+                u32x4_t x[kStage];
+#pragma unroll
+                for (int y = 0; y < kStage; ++y) x[y] = v[64 * y];
+                if (make_finite<kFmt>(x)) {
+#pragma unroll
+                    for (int y = 0; y < kStage; ++y) v[64 * y] = x[y];
+                }
+            }
+        }
         __syncthreads();
     };
 
@@ -981,7 +993,7 @@ es_kv_tile_kernel(AttendArgs a) {
     if (b_begin < b_end) {
         fetch(b_begin, page_of(b_begin), lds);
         stage(b_begin, lds, scales0);
-        arrive();
+        arrive(b_begin, lds);
     }
     for (int b = b_begin; b < b_end; ++b) {
         const int cur = (b - b_begin) & 1;
@@ -992,16 +1004,6 @@ es_kv_tile_kernel(AttendArgs a) {
         bad = bad_next;
         if (more) fetch(b + 1, page, lds + (cur ^ 1) * S::kBuffer);
         page = page_of(b + 2);
-        if (bad || key0 + kBlock > at.seq.len) {
-            // slots past the sequence's end may hold anything: their values are cleared
-            const int left = bad ? 0 : at.seq.len - key0;
-            for (int w = threadIdx.x; w < D * 8; w += S::kThreads) {
-                u32x4_t* const v =
-                    reinterpret_cast<u32x4_t*>(buf + S::kKeyBytes + val_word(w >> 3, w & 7));
-                *v &= token_mask<kBf16>(left - 8 * (w & 7));
-            }
-            __syncthreads();
-        }
         if (key0 < hi_any && key0 + kBlock > lo_any) {
             f32x16_t s[2];
 #pragma unroll
@@ -1096,7 +1098,7 @@ es_kv_tile_kernel(AttendArgs a) {
                 }
         }
         if (more) stage(b + 1, lds + (cur ^ 1) * S::kBuffer, scales0 + (cur ^ 1) * 128);
-        arrive();
+        arrive(b + 1, lds + (cur ^ 1) * S::kBuffer);
     }
 
     sum += __shfl_xor(sum, 32);

@@ -155,6 +155,36 @@ __device__ __forceinline__ u32x4_t codes_to_bf16(u32x2_t c) {
     return out;
 }
 
+// Values that are not finite have every exponent bit set in bf16, and every bit but
+// the sign in E4M3; no int8 code is one.  One more in that place carries into the
+// sign's: these bits of a word, for its values, are the test.
+template <int kFmt>
+__device__ __forceinline__ uint32_t not_finite(uint32_t w) {
+    if constexpr (kFmt == kBf16) return ((w & 0x7FFF7FFFu) + 0x00800080u) & 0x80008000u;
+    if constexpr (kFmt == kE4M3) return ((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
+    return 0u;
+}
+// The word with zeros for them.
+template <int kFmt>
+__device__ __forceinline__ uint32_t finite(uint32_t w) {
+    const uint32_t top = not_finite<kFmt>(w);
+    return w & ~((top << 1) - (top >> (8 * kCodeBytes<kFmt> - 1)));
+}
+__device__ __forceinline__ float finite_scale(float x) {
+    return __builtin_fabsf(x) < __builtin_inff() ? x : 0.0f;
+}
+// N 16-byte words of values, tested first: one is seldom found.  True: some were.
+template <int kFmt, int N>
+__device__ __forceinline__ bool make_finite(u32x4_t (&x)[N]) {
+    uint32_t any = 0;
+#pragma unroll
+    for (int i = 0; i < 4 * N; ++i) any |= not_finite<kFmt>(x[i / 4][i % 4]);
+    if (any == 0) return false;
+#pragma unroll
+    for (int i = 0; i < 4 * N; ++i) x[i / 4][i % 4] = finite<kFmt>(x[i / 4][i % 4]);
+    return true;
+}
+
 // Eight values times `inv` as codes (RNE; |x inv| is at most the format's largest
 // value up to roundings of binary32, which the integer rounding and E4M3's
 // rounding to 448 both absorb).

@@ -769,3 +769,61 @@ def test_the_longest_sequences(form, n):
         exact, spread = oa.attend(f64(q), kx, vx, dim ** -0.5)
         assert np.all(np.abs(f64(got) - exact)
                       <= U * np.abs(exact) + (U * (1 + 2.0 ** -6) + 2.0 ** -16) * spread)
+
+
+def _poison(b, s, hidden):
+    """Not-a-number bits in slots of sequence s of a Batch, as in a pool that was
+    never cleared: keys, values and (8 bits) scales."""
+    pages = torch.from_numpy(b.table[s, hidden // b.page].astype(np.int64)).cuda()
+    off = torch.from_numpy(hidden % b.page).cuda()
+    c = b.cache
+    raw, bits = (torch.int16, 0x7FC1) if b.form == "bf16" else (torch.uint8, 0x7F)
+    c.k_pages.view(raw)[pages, :, off] = bits
+    c.v_pages.view(raw)[pages, :, :, off] = bits
+    if b.form != "bf16":
+        c.k_scales[pages, :, off] = float("nan")
+        c.v_scales[pages, :, off] = float("inf")
+
+
+@pytest.mark.parametrize("form", FORMATS)
+@pytest.mark.parametrize("dim,group", [(64, 1), (128, 5), (256, 4)])
+@pytest.mark.parametrize("n,length", [(1, 300), (3, 1500), (6, 1500), (70, 300), (70, 2200), (300, 300)])
+def test_slots_that_a_row_does_not_see_may_hold_anything(form, dim, group, n, length):
+    """Slots never stored, hidden by `first` inside a block, by a gap between
+    documents, and ahead of the rows: rows that do not see them give the same
+    bits as over a clean cache.  Rows that do see them may give anything."""
+    rng = np.random.default_rng([26, dim, n, length])
+    b = Batch(rng, form, dim, group, 2, 64, [length, 90], [n, 1])
+    pos = np.arange(length - n, length)
+    total = n + 1
+
+    def both(hidden, rows_clean, **kw):
+        want = b.attend(**kw)
+        b.check(want, **kw)
+        kept = [t.clone() for t in (b.cache.k_pages, b.cache.v_pages, b.cache.k_scales,
+                                    b.cache.v_scales) if t is not None]
+        _poison(b, 0, hidden)
+        got = b.attend(**kw)
+        for t, x in zip((b.cache.k_pages, b.cache.v_pages, b.cache.k_scales, b.cache.v_scales), kept):
+            t.view(torch.uint8).copy_(x.view(torch.uint8))
+        keep = torch.from_numpy(np.append(rows_clean, True)).cuda()
+        assert torch.equal(got[keep], want[keep])
+
+    # padding before the tokens
+    pad = 37
+    first = np.append(np.full(n, pad), 0)
+    both(np.arange(pad), np.ones(n, bool), first=first)
+    # two documents and padding between them: the later half of the rows sees the second
+    late = np.arange(n) >= n // 2
+    first = np.append(np.where(late, 170, 0), 0)
+    limit = np.append(np.where(late, pos + 1, 150), 90)
+    both(np.arange(150, 170), np.ones(n, bool), first=first, limit=np.maximum(limit, first))
+    # rows at the end that store nothing (padding) see what is there, and earlier ones do not
+    cut = length - max(1, n // 3)
+    both(np.arange(cut, length), pos < cut)
+    # and a hole that every other row sees
+    hole = np.arange(100, 107)
+    sees = np.arange(n) % 2 == 1
+    first = np.append(np.where(sees, 0, 107), 0)
+    both(hole, ~sees, first=first)
+    assert total == len(b.q)
