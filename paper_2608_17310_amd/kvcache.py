@@ -8,7 +8,10 @@ over it: the binding of es_kv_* in include/esopt.h, which defines every result.
 
 Argument marshalling only: the work runs in the library's HIP kernels.  Calls
 are stream-ordered, allocate nothing but the outputs that the caller does not
-give, and can be captured in a graph.
+give, and can be captured in a graph.  `stream` (a torch.cuda.Stream or a raw
+handle; default: the current one) is where a call runs and where its outputs'
+memory belongs: as under torch.cuda.stream, other streams wait for it before
+they use them.
 """
 
 import ctypes
@@ -43,6 +46,18 @@ def _current_stream(stream):
     if stream is None:
         return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     return _stream(stream)
+
+
+def _output(shape, device, stream):
+    """A bf16 output for a call on `stream`, in that stream's memory: a block of
+    the current stream's may still be in use by work queued there, and would be
+    handed out again while the call's stream uses it."""
+    if stream is None:
+        return torch.empty(shape, dtype=torch.bfloat16, device=device)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(stream), device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=torch.bfloat16, device=device)
 
 
 def _rows(t, shape, what):
@@ -181,7 +196,7 @@ class KVCache:
             shape = (tokens, q_heads, dim)
             q_at, q_stride = _rows(q, shape, "q")
             if q_out is None:
-                q_out = torch.empty(shape, dtype=torch.bfloat16, device=q.device)
+                q_out = _output(shape, q.device, stream)
             out_at, out_stride = _rows(q_out, shape, "q_out")
         elif q_out is not None:
             raise ValueError("q_out without q")
@@ -212,8 +227,7 @@ class KVCache:
         tokens = slots.numel()
         shape = (tokens, self.kv_heads, self.head_dim)
         if k_out is None and v_out is None:
-            k_out, v_out = torch.empty((2,) + shape, dtype=torch.bfloat16,
-                                       device=self.device).unbind(0)
+            k_out, v_out = _output((2,) + shape, self.device, stream).unbind(0)
         elif k_out is None or v_out is None:
             raise ValueError("give both outputs or none")
         k_at, k_stride = _rows(k_out, shape, "k_out")
@@ -243,7 +257,7 @@ class KVCache:
         shape = (rows, heads, self.head_dim)
         q_at, q_stride = _rows(q, shape, "q")
         if out is None:
-            out = torch.empty(shape, dtype=torch.bfloat16, device=q.device)
+            out = _output(shape, q.device, stream)
         out_at, out_stride = _rows(out, shape, "out")
         if tables.dim() != 2:
             raise ValueError("tables must be [seqs, pages]")

@@ -827,3 +827,44 @@ def test_slots_that_a_row_does_not_see_may_hold_anything(form, dim, group, n, le
     first = np.append(np.where(sees, 0, 107), 0)
     both(hole, ~sees, first=first)
     assert total == len(b.q)
+
+
+def test_outputs_lie_in_the_memory_of_the_calls_stream():
+    """An output that a call makes is a block of the stream that it runs on: not
+    one that work of the current stream may still use, nor one that is handed to
+    it while the call's stream does."""
+    rng = np.random.default_rng(27)
+    b = Batch(rng, "bf16", 128, 4, 2, 64, [300, 200], [1, 1])
+    args = b.args()
+    k, v = rows(rng, 2, 2, 128), rows(rng, 2, 2, 128)
+    slots = dev(b.table[:, 0].astype(np.int64) * 64, torch.int64)
+    nowhere = torch.full_like(slots, -1)
+    attended, read_k = b.attend(), b.cache.read(slots)[0]
+    appended = b.cache.append(k, v, nowhere, q=b.q)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    calls = (
+        (tuple(b.q.shape), attended,
+         lambda s: b.cache.attend(b.q, *args, max_rows=1, max_length=300, stream=s)),
+        ((2,) + tuple(k.shape), read_k, lambda s: b.cache.read(slots, stream=s)[0]),
+        (tuple(b.q.shape), appended,
+         lambda s: b.cache.append(k, v, nowhere, q=b.q, stream=s)))
+    for shape, want, call in calls:
+        for stream in (side, side.cuda_stream):
+            free = torch.empty(shape, dtype=torch.bfloat16, device="cuda")
+            here = free.data_ptr()
+            del free                                       # the current stream's next block of this size
+            torch.cuda.synchronize()
+            got = call(stream)
+            side.synchronize()
+            assert torch.equal(got, want)
+            at = got.data_ptr()
+            assert at != here
+            again = torch.empty(shape, dtype=torch.bfloat16, device="cuda")
+            assert again.data_ptr() == here
+            del got, again
+            other = [torch.empty(shape, dtype=torch.bfloat16, device="cuda") for _ in range(3)]
+            assert at not in [t.data_ptr() for t in other]
+            with torch.cuda.stream(side):
+                assert torch.empty(shape, dtype=torch.bfloat16, device="cuda").data_ptr() == at
+            del other
