@@ -151,4 +151,7 @@ class Decoder:
         rows = torch.nonzero((positions >= begin[seq] - 1) & (positions + 1 < size[seq])).flatten()
         logp = F.linear(x[rows], self.head).float().log_softmax(-1)
         got = logp.gather(1, tokens[rows + 1][:, None])[:, 0]
-        return torch.zeros(len(sizes), device=got.device).index_add_(0, seq[rows], got)
+        # a row for each sequence, summed in one order: rewards are the same every time
+        terms = torch.zeros(len(sizes), max(map(len, targets)), dtype=torch.float64, device=got.device)
+        terms[seq[rows], positions[rows] + 1 - begin[seq[rows]]] = got.double()
+        return terms.sum(1).float()

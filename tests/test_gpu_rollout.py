@@ -133,3 +133,31 @@ def test_a_generation_scored_by_the_decoder_replays():
     for p, e in zip(params, end):
         assert torch.equal(p.view(torch.int16), e.view(torch.int16))
     plan.close()
+
+
+def test_long_likelihoods_are_the_same_every_time():
+    """The sum over a target's tokens has one order: the same bits on every
+    call, and next to the sum in 64 bits."""
+    rng = np.random.default_rng(36)
+    params = _params(37)
+    model = Decoder(params, HQ, H, D, False, seqs=4, length=4096, format="bf16")
+    sizes = [4000, 3001, 1, 2500]
+    prompts, targets = _prompts(rng, [3, 17, 64, 1]), _prompts(rng, sizes)
+    tokens = sum(len(p) + n for p, n in zip(prompts, sizes))
+    hidden = torch.from_numpy(rng.standard_normal((tokens, HIDDEN)).astype(np.float32)).to(
+        torch.bfloat16).cuda()
+    model._forward = lambda *args: hidden                  # the sum alone is looked at
+    got = model.log_likelihood(prompts, targets)
+    for _ in range(20):
+        assert torch.equal(model.log_likelihood(prompts, targets), got)
+    logp = (hidden @ params[-1].t()).float().log_softmax(-1).double().cpu().numpy()
+    at = 0
+    for s in range(4):
+        ids = prompts[s] + targets[s]
+        r = np.arange(len(prompts[s]) - 1, len(ids) - 1)
+        want = logp[at + r, np.array(ids)[r + 1]].sum()
+        # terms as float32 (2^-24 of each, half of it at most lost), the logits' rounding to bf16
+        # the same in both but for products summed in another order (one bf16 step, 2^-8 of a logit
+        # of at most 20, in a row)
+        assert abs(got[s].item() - want) <= sizes[s] * 20 * 2.0 ** -8
+        at += len(ids)
