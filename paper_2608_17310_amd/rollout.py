@@ -141,8 +141,14 @@ class Decoder:
 
     def log_likelihood(self, prompts, targets):
         """Sum of the log-probabilities of each target's tokens after its prompt,
-        [seqs] (float32): the usual reward of a supervised task."""
-        whole = [list(p) + list(t) for p, t in zip(prompts, targets)]
+        [seqs] (float32): the usual reward of a supervised task.  Prompts have at
+        least one token: a sequence's first is predicted by nothing."""
+        prompts, targets = list(map(list, prompts)), list(map(list, targets))
+        if len(prompts) != len(targets):
+            raise ValueError(f"{len(prompts)} prompts for {len(targets)} targets")
+        if not all(prompts):
+            raise ValueError("prompts must have at least one token")
+        whole = [p + t for p, t in zip(prompts, targets)]
         tokens, seq, positions, starts, sizes = self._pack(whole)
         x = self._forward(tokens, seq, positions, starts, max(sizes))
         begin = torch.tensor([len(p) for p in prompts], device=tokens.device)

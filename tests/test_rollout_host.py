@@ -1,0 +1,59 @@
+"""The decoder's bookkeeping without a GPU: what a call refuses, what it leaves
+as it was, and the sums of log-probabilities over given hidden states."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2608_17310_amd.rollout import Decoder
+
+VOCAB, HIDDEN, SEQS, LENGTH = 11, 5, 3, 40
+
+
+@pytest.fixture
+def model():
+    """A decoder on the CPU with hidden states of its own in place of the layers."""
+    gen = torch.Generator().manual_seed(1)
+    m = Decoder.__new__(Decoder)
+    m.embedding = torch.randn(VOCAB, HIDDEN, generator=gen)
+    m.head = torch.randn(VOCAB, HIDDEN, generator=gen)
+    m.length = LENGTH
+    m.lengths = torch.zeros(SEQS, dtype=torch.int32)
+    m.longest = 0
+    m.calls = []
+    m.hidden = torch.randn(SEQS * LENGTH, HIDDEN, generator=gen)
+
+    def forward(tokens, seq, positions, starts, max_rows):
+        m.calls.append((tokens.tolist(), starts.tolist(), max_rows))
+        return m.hidden[:len(tokens)]
+    m._forward = forward
+    return m
+
+
+def _state(m):
+    return m.lengths.tolist(), m.longest, len(m.calls)
+
+
+def test_likelihood_refuses_what_has_no_prediction(model):
+    """The first token of a sequence is predicted by nothing, and prompts and
+    targets go in pairs."""
+    model.prefill([[1, 2], [3], [4, 5, 6]])
+    before = _state(model)
+    for prompts, targets in (([[1], [], [2]], [[3], [4], [5]]),
+                             ([[1], [2], [3]], [[4], [5], [6], [7]]),
+                             ([[1], [2], [3], [4]], [[4], [5], [6]]),
+                             ([[1], [2]], [[4], [5]])):
+        with pytest.raises(ValueError):
+            model.log_likelihood(prompts, targets)
+        assert _state(model) == before
+
+
+def test_likelihood_sums_the_targets_terms(model):
+    prompts, targets = [[1, 2], [3], [4, 5, 6]], [[7, 8, 9], [], iter([10])]
+    got = model.log_likelihood(prompts, targets)
+    logp = (model.hidden @ model.head.t()).double().log_softmax(-1)
+    # rows: 0 .. 4 of the first sequence, 5 of the second, 6 .. 9 of the third
+    want = [logp[1, 7] + logp[2, 8] + logp[3, 9], 0.0, logp[8, 10]]
+    # three terms of float32 logits and logarithms, each off by a few 2^-24 of up to 2^4
+    np.testing.assert_allclose(got.numpy(), [float(w) for w in want], rtol=0, atol=2.0 ** -16)
+    assert got.dtype == torch.float32
+    assert not model.log_likelihood(prompts, [[], [], []]).any()
