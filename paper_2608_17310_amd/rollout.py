@@ -119,6 +119,8 @@ class Decoder:
 
     def step(self, tokens):
         """Append one token to each sequence; logits [seqs, vocabulary] (float32)."""
+        if tokens.shape != self.lengths.shape:
+            raise ValueError(f"tokens of shape {tuple(tokens.shape)} for {len(self.lengths)} sequences")
         if self.longest >= self.length:
             raise ValueError(f"sequences have at most {self.length} tokens")
         dev = self.embedding.device

@@ -57,3 +57,19 @@ def test_likelihood_sums_the_targets_terms(model):
     np.testing.assert_allclose(got.numpy(), [float(w) for w in want], rtol=0, atol=2.0 ** -16)
     assert got.dtype == torch.float32
     assert not model.log_likelihood(prompts, [[], [], []]).any()
+
+
+@pytest.mark.parametrize("count", [0, 1, 2, 4])
+def test_a_refused_step_leaves_the_decoder_as_it_was(model, count):
+    model.prefill([[1, 2], [3], [4, 5, 6]])
+    before = _state(model)
+    for tokens in (torch.zeros(count, dtype=torch.long), torch.zeros(SEQS, 1, dtype=torch.long)):
+        with pytest.raises(ValueError):
+            model.step(tokens)
+        assert _state(model) == before
+    model.step(torch.zeros(SEQS, dtype=torch.long))
+    assert model.lengths.tolist() == [3, 2, 4] and model.longest == 4
+    model.longest = LENGTH                                 # and when the cache is full
+    with pytest.raises(ValueError):
+        model.step(torch.zeros(SEQS, dtype=torch.long))
+    assert model.lengths.tolist() == [3, 2, 4]
