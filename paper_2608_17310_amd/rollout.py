@@ -133,13 +133,15 @@ class Decoder:
 
     def generate(self, prompts, count):
         """`count` greedy tokens after each prompt, [seqs, count] (ties: the lowest)."""
+        if count < 0:
+            raise ValueError(f"count must not be negative, got {count}")
         logits = self.prefill(prompts)
-        out = []
+        out = torch.empty(len(logits), count, dtype=torch.long, device=logits.device)
         for i in range(count):
-            out.append(logits.argmax(-1))
+            out[:, i] = logits.argmax(-1)
             if i + 1 < count:
-                logits = self.step(out[-1])
-        return torch.stack(out, 1)
+                logits = self.step(out[:, i])
+        return out
 
     def log_likelihood(self, prompts, targets):
         """Sum of the log-probabilities of each target's tokens after its prompt,

@@ -73,3 +73,12 @@ def test_a_refused_step_leaves_the_decoder_as_it_was(model, count):
     with pytest.raises(ValueError):
         model.step(torch.zeros(SEQS, dtype=torch.long))
     assert model.lengths.tolist() == [3, 2, 4]
+
+
+def test_no_tokens_can_be_generated(model):
+    prompts = [[1, 2], [3], [4, 5, 6]]
+    out = model.generate(prompts, 0)
+    assert out.shape == (SEQS, 0) and out.dtype == torch.long
+    assert model.generate(prompts, 2).shape == (SEQS, 2)
+    with pytest.raises(ValueError):
+        model.generate(prompts, -1)
