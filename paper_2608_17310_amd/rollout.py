@@ -72,6 +72,12 @@ class Decoder:
         y = x.float()
         return (y * torch.rsqrt(y.square().mean(-1, keepdim=True) + self.eps) * gain.float()).to(x.dtype)
 
+    def _check_ids(self, tokens):
+        """Refuse token ids outside the vocabulary, which would index past the embedding."""
+        low, high = (int(x) for x in tokens.aminmax())
+        if low < 0 or high >= len(self.embedding):
+            raise ValueError(f"token ids must lie in [0, {len(self.embedding)}), got {low} .. {high}")
+
     def _forward(self, tokens, seq, positions, starts, max_rows):
         """Hidden states [tokens, hidden] of packed tokens, whose keys and values
         are appended; self.lengths already counts them."""
@@ -101,7 +107,9 @@ class Decoder:
         if min(sizes) < 1 or max(sizes) > self.length:
             raise ValueError(f"prompts must have 1 .. {self.length} tokens")
         dev = self.embedding.device
-        tokens = torch.cat([torch.as_tensor(p, dtype=torch.long) for p in prompts]).to(dev)
+        tokens = torch.cat([torch.as_tensor(p, dtype=torch.long) for p in prompts])
+        self._check_ids(tokens)
+        tokens = tokens.to(dev)
         n = torch.tensor(sizes, dtype=torch.int32)
         starts = torch.cat([torch.zeros(1, dtype=torch.int32), n.cumsum(0, dtype=torch.int32)])
         seq = torch.repeat_interleave(torch.arange(len(sizes)), n)
@@ -118,11 +126,14 @@ class Decoder:
         return F.linear(x[starts[1:].long() - 1], self.head).float()
 
     def step(self, tokens):
-        """Append one token to each sequence; logits [seqs, vocabulary] (float32)."""
+        """Append one token to each sequence; logits [seqs, vocabulary] (float32).
+        Ids on the GPU are not read back to be checked."""
         if tokens.shape != self.lengths.shape:
             raise ValueError(f"tokens of shape {tuple(tokens.shape)} for {len(self.lengths)} sequences")
         if self.longest >= self.length:
             raise ValueError(f"sequences have at most {self.length} tokens")
+        if not tokens.is_cuda:
+            self._check_ids(tokens)
         dev = self.embedding.device
         positions = self.lengths.long()
         self.lengths += 1

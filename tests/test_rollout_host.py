@@ -82,3 +82,22 @@ def test_no_tokens_can_be_generated(model):
     assert model.generate(prompts, 2).shape == (SEQS, 2)
     with pytest.raises(ValueError):
         model.generate(prompts, -1)
+
+
+@pytest.mark.parametrize("bad", [-1, VOCAB, 1 << 40])
+def test_tokens_outside_the_vocabulary_are_refused(model, bad):
+    """-1 would read the embedding's last row, and others past its end."""
+    model.prefill([[1, 2], [3], [4, 5, 6]])
+    before = _state(model)
+    for prompts in ([[bad], [1], [2]], [[1, 2], [3, 4, bad], [5]]):
+        for call in (lambda: model.prefill(prompts), lambda: model.generate(prompts, 1),
+                     lambda: model.log_likelihood(prompts, [[1], [2], [3]]),
+                     lambda: model.log_likelihood([[1], [2], [3]], prompts),
+                     lambda: model.prefill([torch.tensor(p) for p in prompts])):
+            with pytest.raises(ValueError):
+                call()
+            assert _state(model) == before
+    with pytest.raises(ValueError):
+        model.step(torch.tensor([1, bad, 2]))
+    assert _state(model) == before
+    model.prefill([[0, VOCAB - 1], [0], [VOCAB - 1]])
