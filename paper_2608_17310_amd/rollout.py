@@ -22,6 +22,10 @@ import torch.nn.functional as F
 
 from .kvcache import KVCache
 
+# Logits that log_likelihood holds at once (in bf16 and float32, and their
+# log-softmax: 10 bytes each).
+LOGITS_AT_A_TIME = 1 << 28
+
 
 def rope_table(positions, rot, base=10000.0, device="cuda"):
     """Cosines and sines of the rotation, [positions, rot] float32, from 64 bits."""
@@ -170,8 +174,12 @@ class Decoder:
         # row r predicts token r + 1; rows from the prompt's last on, but the sequence's last
         size = (starts[1:] - starts[:-1]).long()
         rows = torch.nonzero((positions >= begin[seq] - 1) & (positions + 1 < size[seq])).flatten()
-        logp = F.linear(x[rows], self.head).float().log_softmax(-1)
-        got = logp.gather(1, tokens[rows + 1][:, None])[:, 0]
+        got = torch.empty(len(rows), dtype=torch.float32, device=rows.device)
+        slab = max(1, LOGITS_AT_A_TIME // len(self.head))
+        for i in range(0, len(rows), slab):
+            r = rows[i:i + slab]
+            logp = F.linear(x[r], self.head).float().log_softmax(-1)
+            got[i:i + slab] = logp.gather(1, tokens[r + 1][:, None])[:, 0]
         # a row for each sequence, summed in one order: rewards are the same every time
         terms = torch.zeros(len(sizes), max(map(len, targets)), dtype=torch.float64, device=got.device)
         terms[seq[rows], positions[rows] + 1 - begin[seq[rows]]] = got.double()

@@ -4,6 +4,7 @@ import numpy as np
 import pytest
 import torch
 
+from paper_2608_17310_amd import rollout
 from paper_2608_17310_amd.rollout import Decoder
 
 VOCAB, HIDDEN, SEQS, LENGTH = 11, 5, 3, 40
@@ -101,3 +102,26 @@ def test_tokens_outside_the_vocabulary_are_refused(model, bad):
         model.step(torch.tensor([1, bad, 2]))
     assert _state(model) == before
     model.prefill([[0, VOCAB - 1], [0], [VOCAB - 1]])
+
+
+@pytest.mark.parametrize("rows", [1, 2, 4, 100])
+def test_likelihood_holds_few_logits_at_a_time(model, monkeypatch, rows):
+    """Logits are made a slab of rows at a time, whatever the targets' lengths,
+    and the sums do not depend on it."""
+    prompts, targets = [[1, 2], [3], [4, 5, 6]], [[7, 8, 9, 0, 1], [2], [10, 4]]
+    want = model.log_likelihood(prompts, targets)
+    sizes = []
+    linear = rollout.F.linear
+
+    def counted(x, w):
+        sizes.append(len(x))
+        return linear(x, w)
+    monkeypatch.setattr(rollout.F, "linear", counted)
+    monkeypatch.setattr(rollout, "LOGITS_AT_A_TIME", rows * VOCAB + VOCAB - 1)
+    got = model.log_likelihood(prompts, targets)
+    assert sum(sizes) == 8 and max(sizes) <= rows
+    # float32 logits of products summed in another order: 2^-24 of up to 2^5, five terms and their
+    # normalisers
+    np.testing.assert_allclose(got.numpy(), want.numpy(), rtol=0, atol=10 * 2.0 ** -19)
+    monkeypatch.setattr(rollout, "LOGITS_AT_A_TIME", VOCAB - 1)
+    assert torch.isfinite(model.log_likelihood(prompts, targets)).all()
