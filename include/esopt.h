@@ -658,7 +658,10 @@ uint64_t es_kv_device_bytes(const es_kv_t* kv);
  * from binary32, values as they come.
  * slots[t] is where token t is stored; a negative slot stores nothing (a padding
  * row).  Two tokens of one call must not share a slot.  Which values a
- * token's slot holds never depends on the other tokens of the call. */
+ * token's slot holds never depends on the other tokens of the call.
+ * Here, in es_kv_read and in es_kv_attend a call of so many tokens and heads
+ * that a launch would have 2^32 lanes is refused (INVALID_ARG): from about 2^29
+ * rows (tokens times heads) on, or 2^24 sequences times key heads. */
 #define ES_KV_ADJACENT 1u
 typedef struct es_kv_append {
     const void*    q;           /* bf16 [tokens][q_heads][head_dim], or NULL with q_heads 0 */

@@ -272,6 +272,13 @@ int es_kv_append(es_kv_t* kv, const es_kv_append_t* args, es_stream_t stream) tr
         odd(x.k_gain, 2) || odd(x.rope, 4) || odd(x.positions, 4) || odd(x.slots, 8) ||
         odd(x.status, 4))
         return fail_in(ES_ERR_ALIGN, name, "array not aligned to its elements");
+    const uint32_t q_parts = (x.q_heads + kPlaceHeads - 1) / kPlaceHeads;
+    const uint32_t q_blocks =
+        x.q_heads == 0 ? 0 : token_blocks(x.tokens, kPlaceThreads * 8 / dim);
+    const uint32_t kv_blocks = token_blocks(x.tokens, kPlaceTokens);
+    const uint64_t groups = uint64_t(kv_blocks) * kv->d.kv_heads + uint64_t(q_blocks) * q_parts;
+    if (groups >= kMaxGroups)
+        return fail_in(ES_ERR_INVALID_ARG, name, "too many tokens for one call");
     const int rc = check_kv_device(kv, name);
     if (rc != ES_OK) return rc;
     const uint64_t kw = uint64_t(kv->d.kv_heads) * dim, qw = uint64_t(x.q_heads) * dim;
@@ -315,12 +322,10 @@ int es_kv_append(es_kv_t* kv, const es_kv_append_t* args, es_stream_t stream) tr
         x.rot == dim && (x.flags & ES_KV_ADJACENT) == 0
             ? by_dim_format<AppendKernel, MakeAppend<true>::Of>(dim, kv->d.format)
             : by_dim_format<AppendKernel, MakeAppend<false>::Of>(dim, kv->d.format);
-    const uint32_t q_tokens = kPlaceThreads * 8 / dim;       // of a workgroup of queries
-    a.q_parts = (x.q_heads + kPlaceHeads - 1) / kPlaceHeads;
-    a.q_blocks = x.q_heads == 0 ? 0 : token_blocks(x.tokens, q_tokens);
-    a.kv_blocks = token_blocks(x.tokens, kPlaceTokens);
-    const dim3 grid(a.kv_blocks * kv->d.kv_heads + a.q_blocks * a.q_parts);
-    hipLaunchKernelGGL(kernel, grid, dim3(kPlaceThreads), 0, static_cast<hipStream_t>(stream), a);
+    a.q_parts = q_parts;
+    a.q_blocks = q_blocks;
+    a.kv_blocks = kv_blocks;
+    hipLaunchKernelGGL(kernel, dim3(groups), dim3(kPlaceThreads), 0, static_cast<hipStream_t>(stream), a);
     return launch_error("es_kv_append_kernel launch");
 } catch (const std::bad_alloc&) {
     return fail(ES_ERR_NOMEM, "es_kv_append: host allocation failed");
@@ -341,6 +346,9 @@ int es_kv_read(es_kv_t* kv, const int64_t* slots, uint32_t tokens, void* k_out, 
         return fail_in(ES_ERR_INVALID_ARG, name, "stride above 2^38");
     if (odd(slots, 8) || odd(k_out, 2) || odd(v_out, 2) || odd(status, 4))
         return fail_in(ES_ERR_ALIGN, name, "array not aligned to its elements");
+    const uint32_t blocks = token_blocks(tokens, kPlaceTokens);
+    if (uint64_t(blocks) * kv->d.kv_heads >= kMaxGroups)
+        return fail_in(ES_ERR_INVALID_ARG, name, "too many tokens for one call");
     const int rc = check_kv_device(kv, name);
     if (rc != ES_OK) return rc;
     Accesses ok{kv->device, name, {}};
@@ -359,9 +367,8 @@ int es_kv_read(es_kv_t* kv, const int64_t* slots, uint32_t tokens, void* k_out, 
     a.tokens = tokens;
     a.c = kv->c;
     const ReadKernel kernel = by_dim_format<ReadKernel, MakeRead>(kv->d.head_dim, kv->d.format);
-    a.blocks = token_blocks(tokens, kPlaceTokens);
-    const dim3 grid(a.blocks * kv->d.kv_heads);
-    hipLaunchKernelGGL(kernel, grid, dim3(kPlaceThreads), 0, static_cast<hipStream_t>(stream), a);
+    a.blocks = blocks;
+    hipLaunchKernelGGL(kernel, dim3(blocks * kv->d.kv_heads), dim3(kPlaceThreads), 0, static_cast<hipStream_t>(stream), a);
     return launch_error("es_kv_read_kernel launch");
 } catch (const std::bad_alloc&) {
     return fail(ES_ERR_NOMEM, "es_kv_read: host allocation failed");

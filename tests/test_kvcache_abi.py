@@ -185,3 +185,19 @@ def test_strides_whose_extent_leaves_64_bits_are_refused(lib, fake):
         a = _attend(rows=n, **{name: far})
         assert lib.es_kv_attend(h, ctypes.byref(a), None) == E
         assert "stride" in esopt.last_error()
+
+
+def test_calls_beyond_a_launch_are_refused(lib, fake):
+    """A launch has fewer than 2^32 lanes: more tokens than it can take are
+    refused before any device is asked."""
+    n = 1 << 24
+    a = _append(tokens=n, q_heads=1024, q_stride=1024 * 64, q_out_stride=1024 * 64)
+    assert lib.es_kv_append(ctypes.byref(fake), ctypes.byref(a), None) == E
+    assert "too many tokens" in esopt.last_error()
+    wide = FakeCache(0, _desc(kv_heads=1024))
+    a = _append(tokens=n, q=None, q_out=None, q_heads=0)
+    assert lib.es_kv_append(ctypes.byref(wide), ctypes.byref(a), None) == E
+    assert "too many tokens" in esopt.last_error()
+    row = 1024 * 64
+    assert lib.es_kv_read(ctypes.byref(wide), 0x1000, n, 0x2000, row, 0x3000, row, None, None) == E
+    assert "too many tokens" in esopt.last_error()
