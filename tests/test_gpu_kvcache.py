@@ -868,3 +868,97 @@ def test_outputs_lie_in_the_memory_of_the_calls_stream():
             with torch.cuda.stream(side):
                 assert torch.empty(shape, dtype=torch.bfloat16, device="cuda").data_ptr() == at
             del other
+
+
+def _bias_room(b, slopes, first, limit):
+    """What a bias by distance may be off by, in outputs: 2^-22 (four roundings
+    of 2^-24) of slope (distance + 64), as the kernels add a block's term to a
+    key's, through the weights and through their sum; one array a sequence."""
+    out, q = [], f64(b.q)
+    for s, n in enumerate(b.rows_of):
+        r = slice(int(b.starts[s]), int(b.starts[s + 1]))
+        length, room = b.lengths[s], np.zeros((n, q.shape[1], b.dim))
+        f, m = (None if x is None else np.asarray(x)[r] for x in (first, limit))
+        see = oa.visible(length, n, f, m)
+        pos = np.arange(length - n, length)
+        away = np.abs(pos[:, None] - np.arange(length))
+        for i in range(q.shape[1]):
+            j = i // b.group
+            t = q[r][:, i] @ b.k[s][:, j].T * b.dim ** -0.5 - float(np.float32(slopes[i])) * away
+            t = np.where(see, t, -np.inf)
+            rows_ = see.any(axis=1)
+            p = np.zeros_like(t)
+            p[rows_] = np.exp(t[rows_] - t[rows_].max(axis=1, keepdims=True))
+            p[rows_] /= p[rows_].sum(axis=1, keepdims=True)
+            off = abs(float(slopes[i])) * (away + 64) * 2.0 ** -22
+            size = np.abs(b.v[s][:, j])
+            room[:, i] = (p * off) @ size + (p * off).sum(axis=1, keepdims=True) * (p @ size)
+        out.append(room)
+    return out
+
+
+def _check_biased(b, slopes, first=None, limit=None, **kw):
+    got = f64(b.attend(slopes=slopes, first=first, limit=limit, **kw))
+    q, slopes = f64(b.q), np.asarray(slopes, np.float32).astype(np.float64)
+    for s, room in enumerate(_bias_room(b, slopes, first, limit)):
+        r = slice(int(b.starts[s]), int(b.starts[s + 1]))
+        f, m = (None if x is None else np.asarray(x)[r] for x in (first, limit))
+        want, spread = oa.attend(q[r], b.k[s], b.v[s], b.dim ** -0.5, 0.0, slopes, f, m)
+        j = np.arange(q.shape[1]) // b.group
+        size = np.linalg.norm(q[r], axis=-1) * np.linalg.norm(b.k[s], axis=-1).max(axis=0, initial=0.0)[j]
+        size = size * b.dim ** -0.5
+        # (2^-134: half of bf16's smallest step, to which steep slopes' results come)
+        bound = (U * np.abs(want) + (U * (1 + 2.0 ** -6) + 2.0 ** -21 * size[..., None]) * spread + room
+                 + 2.0 ** -134)
+        off = np.abs(got[r] - want)
+        assert np.all(off <= bound), (s, float(np.max(off - bound)), np.argwhere(~(off <= bound))[:4])
+
+
+# a head's slope in units of log2 up to 4 (2.77 in these) lets a block's distances be one
+# term of the key and one of the row; steeper ones are taken key by key
+GENTLE = [2.0 ** -1, 2.0 ** -8, 2.75, 0.0, 2.0 ** -4, 1.0, 2.0 ** -2]
+STEEP = [2.8, 2.0 ** -3, 2.75, 100.0, 2.0 ** -6, -0.01, 5.0]
+
+
+@pytest.mark.parametrize("form", FORMATS)
+@pytest.mark.parametrize("dim,group,kv_heads,page", [(64, 1, 3, 64), (128, 5, 2, 128), (256, 4, 1, 256),
+                                                     (128, 1, 2, 64), (64, 7, 1, 64)])
+@pytest.mark.parametrize("slopes", [GENTLE, STEEP])
+def test_bias_by_distance_alone(form, dim, group, kv_heads, page, slopes):
+    """Prompts, prompts behind a history and few rows, with a bias and no cap:
+    keys behind the rows, keys ahead of them, and rows that see far keys alone."""
+    rng = np.random.default_rng([28, dim, group, page])
+    heads = group * kv_heads
+    slopes = np.resize(slopes, heads)
+    for lengths, rows_of in (([300, 65, 1, 700, 64, 130], [300, 65, 1, 200, 64, 129]),
+                             ([5000, 3, 129, 700], [3, 2, 5, 1]), ([1500], [40])):
+        b = Batch(rng, form, dim, group, kv_heads, page, lengths, rows_of)
+        _check_biased(b, slopes)
+        pos = np.concatenate([np.arange(m - n, m) for m, n in zip(lengths, rows_of)])
+        _check_biased(b, slopes, limit=pos + 1 + rng.integers(0, 300, len(pos)))
+        _check_biased(b, slopes, first=pos // 2, limit=np.maximum(pos // 2 + 1, pos - 10))
+        _check_biased(b, slopes, limit=np.minimum(pos + 1, 70))
+
+
+@pytest.mark.parametrize("form", FORMATS)
+@pytest.mark.parametrize("dim,group,kv_heads", [(64, 2, 2), (128, 4, 2), (256, 3, 1)])
+def test_intervals_of_many_rows_over_cut_histories(form, dim, group, kv_heads):
+    """More rows than a scan reads the intervals of, over histories that are cut
+    along the keys: parts in which a tile sees nothing among them."""
+    rng = np.random.default_rng([29, dim, group])
+    b = Batch(rng, form, dim, group, kv_heads, 64, [2600, 2100, 90], [100, 300, 65])
+    pos = np.concatenate([np.arange(m - n, m) for m, n in zip(b.lengths, b.rows_of)])
+    total = len(pos)
+    slopes = np.resize(GENTLE, group * kv_heads)
+    for first, limit in (
+            (pos // 397 * 397, pos + 1),                   # packed documents
+            (None, np.maximum(pos + 1, 1250)),             # a prefix, and keys ahead of the row
+            (np.maximum(0, pos - 170), None),              # a window
+            (rng.integers(-5, 2650, total), rng.integers(-5, 2650, total)),
+            (np.full(total, 10), np.full(total, 10)),      # nothing at all
+            (np.where(np.arange(total) % 3 == 0, 2000, 5), np.where(np.arange(total) % 3 == 0, 2040, 9))):
+        got = b.attend(first=first, limit=limit)
+        b.check(got, first=first, limit=limit)
+        got = b.attend(first=first, limit=limit, cap=4.0)
+        b.check(got, first=first, limit=limit, cap=4.0)
+        _check_biased(b, slopes, first=first, limit=limit)
