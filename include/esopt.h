@@ -685,8 +685,9 @@ typedef struct es_kv_append {
 int es_kv_append(es_kv_t* kv, const es_kv_append_t* args, es_stream_t stream);
 
 /* Read tokens back: row t of k_out and v_out (bf16 [tokens][kv_heads][head_dim],
- * `*_stride` elements from token to token) is what slots[t] holds, code times
- * scale rounded once (RNE).  A negative slot gives zeros. */
+ * `*_stride` elements from token to token) is what slots[t] holds: bf16 values
+ * as they are, and the product of code and scale in binary32, rounded to bf16
+ * (RNE).  A negative slot gives zeros. */
 int es_kv_read(es_kv_t* kv, const int64_t* slots, uint32_t tokens, void* k_out, uint64_t k_stride,
                void* v_out, uint64_t v_stride, uint32_t* status, es_stream_t stream);
 
@@ -705,7 +706,9 @@ int es_kv_read(es_kv_t* kv, const int64_t* slots, uint32_t tokens, void* k_out, 
  * sees must have been stored: its value and value scale are finite then.  Rows
  * that no sequence has are not written.  Sums, maxima and products are held in
  * binary32; the softmax's weights (times the values' scales) are rounded to bf16
- * for the matrix unit.
+ * for the matrix unit.  Weights are relative to a maximum that may lag by 2^8, and
+ * are divided by their sum at the end: where 2^8 times the sum of the seen |v|
+ * leaves binary32, infinities may come out of finite values.
  * max_rows and max_length are the largest rows and lengths[s] that the caller
  * expects: they choose how the work is cut, and nothing is lost where a
  * sequence exceeds them.  Calls on one handle must be ordered (one stream, or

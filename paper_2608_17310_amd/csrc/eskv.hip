@@ -469,9 +469,10 @@ int es_kv_attend(es_kv_t* kv, const es_kv_attend_t* args, es_stream_t stream) tr
         // Two workgroups a compute unit stream as fast as more, and a part left over
         // for a second round costs as long as all of the first: with few histories,
         // room for each one's short last part.  8 histories of 50000 to 65537 tokens
-        // (int8) aimed at 512, 448 and 1024 parts: 230, 200 and 194 us; 64 of 2000
-        // (bf16) at 512 and 1024: 100 and 108; 8 of 20000 (bf16, 16 heads over 4 x
-        // 256): 127 and 136.
+        // (int8) aimed at 512 and 448 parts: 230 and 200 us.  Not 1024, two rounds
+        // of half the length: 194 there, but 108 for 100 at 64 of 2000 (bf16) and 136
+        // for 127 at 8 of 20000 (bf16, 16 heads over 4 x 256).  How the histories'
+        // remainders fall is not looked at: it moves a time by a few percent.
         const uint64_t pairs = uint64_t(x.n_seqs) * heads;
         a.target = kMaxParts - (pairs <= kMaxParts / 4 ? static_cast<uint32_t>(pairs) : 0u);
         a.min_blocks = kMinBlocks;

@@ -21,7 +21,7 @@
 //
 // Measured: 8362 tokens of 32 ragged prompts (40 query heads over 8 of 128, E4M3)
 // appended in 47 us, 4.7 TB/s, and read back in 14; 32771 tokens (16 heads over
-// 16 of 64, bf16) in 92 us, 4.4 TB/s, and 50 to 60.  One token: 5.8 and 3.5 us.
+// 16 of 64, bf16) in 92 us, 4.4 TB/s, and 58 to 60.  One token: 6.9 to 7.8 and 3.3 to 3.6 us.
 #pragma once
 
 #include "kv_common.hpp"

@@ -102,7 +102,12 @@ class KVCache:
     v_pages [pages, heads, dim, page] (torch.bfloat16, torch.int8 or
     torch.float8_e4m3fn, which sets the format) and, for the 8-bit formats,
     k_scales and v_scales [pages, heads, page] in float32.  The object keeps
-    references to them.  `allocate` makes them."""
+    references to them.  `allocate` makes them.
+
+    The parts of a long history are joined in scratch that belongs to the
+    object: calls of `attend` on one cache, from any streams or threads, must be
+    ordered one after another (two caches over the same pages have a scratch
+    each)."""
 
     def __init__(self, k_pages, v_pages, k_scales=None, v_scales=None):
         self._h = None
