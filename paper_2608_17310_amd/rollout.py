@@ -132,6 +132,7 @@ class Decoder:
     def step(self, tokens):
         """Append one token to each sequence; logits [seqs, vocabulary] (float32).
         Ids on the GPU are not read back to be checked."""
+        tokens = torch.as_tensor(tokens, dtype=torch.long)
         if tokens.shape != self.lengths.shape:
             raise ValueError(f"tokens of shape {tuple(tokens.shape)} for {len(self.lengths)} sequences")
         if self.longest >= self.length:
@@ -143,7 +144,7 @@ class Decoder:
         self.lengths += 1
         self.longest += 1
         rows = torch.arange(len(tokens) + 1, dtype=torch.int32, device=dev)
-        x = self._forward(tokens, rows[:-1].long(), positions, rows, 1)
+        x = self._forward(tokens.to(dev), rows[:-1].long(), positions, rows, 1)
         return F.linear(x, self.head).float()
 
     def generate(self, prompts, count):

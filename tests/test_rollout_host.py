@@ -125,3 +125,16 @@ def test_likelihood_holds_few_logits_at_a_time(model, monkeypatch, rows):
     np.testing.assert_allclose(got.numpy(), want.numpy(), rtol=0, atol=10 * 2.0 ** -19)
     monkeypatch.setattr(rollout, "LOGITS_AT_A_TIME", VOCAB - 1)
     assert torch.isfinite(model.log_likelihood(prompts, targets)).all()
+
+
+@pytest.mark.parametrize("kind", [list, tuple, np.array, lambda t: torch.tensor(t, dtype=torch.int32)])
+def test_a_steps_tokens_may_be_any_sequence(model, kind):
+    model.prefill([[1, 2], [3], [4, 5, 6]])
+    want = model.step(torch.tensor([7, 8, 9]))
+    model.prefill([[1, 2], [3], [4, 5, 6]])
+    assert torch.equal(model.step(kind([7, 8, 9])), want)
+    assert model.calls[-1][0] == [7, 8, 9]
+    with pytest.raises(ValueError):
+        model.step(kind([7, 8]))
+    with pytest.raises(ValueError):
+        model.step(kind([7, 8, VOCAB]))
