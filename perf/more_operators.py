@@ -218,7 +218,7 @@ def _own_distill(c):
 
 
 def _own_adapt(c):
-    return c["adapters"].project(c["x"], c["weight"], c["index"])
+    return {"y": c["adapters"].project(c["x"], c["weight"], c["index"])}
 
 
 def _plain_logits(c):
