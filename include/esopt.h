@@ -734,6 +734,124 @@ typedef struct es_kv_attend {
 } es_kv_attend_t;
 int es_kv_attend(es_kv_t* kv, const es_kv_attend_t* args, es_stream_t stream);
 
+/* ---------------------------------------------------------------------------
+ * Scoring a member: its head.
+ *
+ * The log-probabilities of given tokens under a head with a large vocabulary,
+ * the divergence from a teacher that is known by its top logits, and the
+ * gradients of both for the hidden rows and for the head (a warm start before
+ * evolution strategies, or a gradient to hold their estimate against).  The
+ * logits are never stored: memory beside the outputs is es_head_*_bytes.
+ *
+ * x is bf16 [rows][hidden], weight bf16 [vocab][hidden], both with any stride
+ * between rows (at most 2^22 elements) and any alignment to 2 bytes.  For a row
+ *   z_v = scale x . weight_v,  lse = log sum_v exp z_v,
+ * and for each of its `entries` ids
+ *   logp = z_id - lse.
+ * A negative id is absent (its logp is 0, whatever stands beside it).  A row
+ * with no id is dead: its results are 0, it has no gradient, and what x holds
+ * there reaches nothing.  A row with an id of `vocab` or more is void: its
+ * results and its gradient's row are NaN, and it adds nothing to the head's.
+ *
+ * Without a teacher there is one id a row, the target.  With one, teacher[e] is
+ * its logit at ids[e] (binary32; -infinity leaves that id no weight) and
+ *   q = softmax(scale teacher) over the row's present ids,
+ *   loss = sum_e q_e (log q_e - logp_e),
+ * the divergence of the student from the teacher within its top logits; a row
+ * whose teacher leaves nothing (-infinity throughout) has loss 0.  The same id
+ * twice in a row counts twice.
+ *
+ * Products are sums in binary32 of exact products; maxima, sums and scores are
+ * binary32.  The same inputs give the same bits.
+ * ------------------------------------------------------------------------- */
+#define ES_HEAD_BAD_ID 1u      /* status: an id >= vocab */
+
+typedef struct es_head_score {
+    const void*    x;           /* bf16 [rows][hidden] */
+    const void*    weight;      /* bf16 [vocab][hidden] */
+    uint64_t       x_stride, w_stride;         /* elements from row to row, at most 2^22 */
+    const int64_t* ids;         /* [rows][entries] */
+    const float*   teacher;     /* [rows][entries], or NULL with entries 1 */
+    float*         loss;        /* [rows] with a teacher; otherwise NULL */
+    float*         logp;        /* [rows][entries] */
+    float*         lse;         /* [rows] */
+    uint32_t*      status;      /* a device uint32 which ES_HEAD_BAD_ID is ORed into, or NULL */
+    void*          workspace;   /* device memory of the call's own, 256-byte aligned */
+    uint64_t       workspace_bytes;            /* at least es_head_score_bytes() */
+    uint32_t       rows;        /* 0 .. 65536 */
+    uint32_t       vocab;       /* 1 .. 2^24 */
+    uint32_t       hidden;      /* 1 .. 65536 */
+    uint32_t       entries;     /* 1 .. 256 */
+    float          scale;       /* finite */
+    uint32_t       reserved;    /* 0 */
+} es_head_score_t;
+/* Bytes of workspace of such a call (0 for arguments that it refuses). */
+uint64_t es_head_score_bytes(const es_head_score_t* args);
+int es_head_score(const es_head_score_t* args, es_stream_t stream);
+
+/* Gradients, for weights grad[row], of
+ *   sum_row grad logp   without a teacher,  sum_row grad loss   with one,
+ * for x and for weight, from what es_head_score gave for the same inputs.  With q
+ * as above (1 at the target), Q = sum q and f = -scale grad or scale grad, the
+ * logits' gradients are d_v = f (Q softmax(z)_v - q_v), rounded to bf16 (RNE) for the
+ * matrix unit; d_x = sum_v d_v weight_v and d_weight_v = sum_row d_v x are summed in
+ * binary32 and rounded once to bf16. */
+typedef struct es_head_gradient {
+    const void*    x;
+    const void*    weight;
+    uint64_t       x_stride, w_stride;
+    const int64_t* ids;
+    const float*   teacher;
+    const float*   logp;        /* [rows][entries], of es_head_score */
+    const float*   lse;         /* [rows], likewise */
+    const float*   grad;        /* [rows] */
+    void*          d_x;         /* bf16 [rows][hidden], or NULL: not wanted */
+    void*          d_weight;    /* bf16 [vocab][hidden], or NULL: not wanted */
+    uint64_t       dx_stride, dw_stride;
+    uint32_t*      status;
+    void*          workspace;
+    uint64_t       workspace_bytes;            /* at least es_head_gradient_bytes() */
+    uint32_t       rows, vocab, hidden, entries;
+    float          scale;
+    uint32_t       reserved;
+} es_head_gradient_t;
+uint64_t es_head_gradient_bytes(const es_head_gradient_t* args);
+int es_head_gradient(const es_head_gradient_t* args, es_stream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * Scoring a population at once: a shared projection and, beside it, the
+ * low-rank adapters of many members, one member's for each row:
+ *   y = W x + s_i B_i (A_i x),  i = index[row].
+ * A row with a negative index has no adapter; one of `members` or more is NaN.  The
+ * adapters are tensors that plans can move like any other parameters.
+ * A_i x is summed in binary32, multiplied by s_i and rounded to bf16 (RNE) for the
+ * matrix unit; y is summed in binary32 and rounded once.  What a member's
+ * adapter or a row holds reaches no other row.
+ * ------------------------------------------------------------------------- */
+#define ES_ADAPT_BAD_INDEX 1u  /* status: an index >= members */
+
+typedef struct es_adapt {
+    const void*    x;           /* bf16 [rows][inner], any alignment to 2 bytes */
+    const void*    weight;      /* bf16 [outer][inner], 16-byte aligned */
+    void*          out;         /* bf16 [rows][outer], any alignment to 2 bytes; not x */
+    uint64_t       x_stride, w_stride, out_stride;   /* elements, at most 2^22; w_stride a multiple of 8 */
+    const void*    a;           /* bf16 [members][rank][inner], 16-byte aligned */
+    const void*    b;           /* bf16 [members][outer][rank], 16-byte aligned */
+    const float*   scales;      /* [members], or NULL: ones */
+    const int32_t* index;       /* [rows] */
+    uint32_t*      status;      /* or NULL */
+    void*          workspace;   /* device memory of the call's own, 256-byte aligned */
+    uint64_t       workspace_bytes;            /* at least es_adapt_bytes() */
+    uint32_t       rows;        /* 0 .. 2^20 */
+    uint32_t       inner;       /* a multiple of 8, 8 .. 65536 */
+    uint32_t       outer;       /* 1 .. 2^20 */
+    uint32_t       members;     /* 1 .. 65536 */
+    uint32_t       rank;        /* a multiple of 8, 8 .. 128 */
+    uint32_t       reserved;    /* 0 */
+} es_adapt_t;
+uint64_t es_adapt_bytes(const es_adapt_t* args);
+int es_adapt_project(const es_adapt_t* args, es_stream_t stream);
+
 /* Static name of an error code; detail of the calling thread's last error. */
 const char* es_strerror(int code);
 const char* es_last_error(void);

@@ -7,7 +7,7 @@ import tempfile
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
-SOURCES = [os.path.join(HERE, "csrc", f) for f in ("esopt.hip", "eskv.hip")]
+SOURCES = [os.path.join(HERE, "csrc", f) for f in ("esopt.hip", "eskv.hip", "eshead.hip")]
 OUT = os.path.join(HERE, "libesopt.so")
 
 HIPCC_FLAGS = [

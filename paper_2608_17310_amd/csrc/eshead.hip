@@ -1,0 +1,607 @@
+// Scoring a member at its head, and a population at its projections
+// (include/esopt.h, es_head_*, es_adapt_*).  Host side: checks of arguments, the
+// division of a call's workspace and launches; the kernels are in head.hpp,
+// adapt.hpp and mm_tile.hpp.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+#include <new>
+
+#include "../../include/esopt.h"
+#include "es_host.hpp"
+#include "adapt.hpp"
+#include "head.hpp"
+
+using namespace es_host;
+using esmm::kDepth;
+using esmm::kLdsBytes;
+using esmm::kThreads;
+using esmm::kTile;
+using esmm::Product;
+using esmm::Side;
+
+namespace {
+
+constexpr uint64_t kMaxStride = uint64_t(1) << 22;
+constexpr uint32_t kCus = 256;
+
+// Gradients of logits, and copies of a head's rows, that a call holds at a time:
+// what the last cache level keeps between the products that write and read them.
+constexpr uint64_t kPieceBytes = uint64_t(256) << 20;
+
+bool odd(const void* p, uintptr_t align) { return reinterpret_cast<uintptr_t>(p) % align != 0; }
+uint64_t up(uint64_t x, uint64_t to) { return (x + to - 1) / to * to; }
+
+// `rows` rows of `width` bf16, `stride` elements apart.
+uint64_t extent(uint64_t rows, uint64_t width, uint64_t stride) {
+    return 2 * ((rows - 1) * stride + width);
+}
+
+int launch_error(const char* what) {
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? ES_OK : hip_fail(e, what);
+}
+
+// A workspace handed out in order; without memory, only measured.
+struct Room {
+    uint8_t* at;
+    uint64_t used = 0;
+    template <class T>
+    T* take(uint64_t n) {
+        uint8_t* const p = at == nullptr ? nullptr : at + used;
+        used += up(n * sizeof(T), 256);
+        return reinterpret_cast<T*>(p);
+    }
+};
+
+bool word_rows(const void* p, uint64_t stride, uint32_t width) {
+    return !odd(p, 16) && stride % 8 == 0 && width % 8 == 0;
+}
+
+// --------------------------------------------------------------------- head --
+
+int check_head(const char* name, const void* x, const void* weight, uint64_t x_stride,
+               uint64_t w_stride, const int64_t* ids, const float* teacher, uint32_t rows,
+               uint32_t vocab, uint32_t hidden, uint32_t entries, float scale, uint32_t reserved) {
+    if (rows > 65536) return fail_in(ES_ERR_INVALID_ARG, name, "rows above 65536");
+    if (vocab == 0 || vocab > (1u << 24))
+        return fail_in(ES_ERR_INVALID_ARG, name, "vocab out of range (1 .. 2^24)");
+    if (hidden == 0 || hidden > 65536)
+        return fail_in(ES_ERR_INVALID_ARG, name, "hidden out of range (1 .. 65536)");
+    if (entries == 0 || entries > eshead::kMaxEntries)
+        return fail_in(ES_ERR_INVALID_ARG, name, "entries out of range (1 .. 256)");
+    if (!std::isfinite(scale)) return fail_in(ES_ERR_INVALID_ARG, name, "scale is not finite");
+    if (reserved != 0) return fail_in(ES_ERR_INVALID_ARG, name, "reserved is not 0");
+    if (x_stride > kMaxStride || w_stride > kMaxStride)
+        return fail_in(ES_ERR_INVALID_ARG, name, "stride above 2^22");
+    if (teacher == nullptr && entries != 1)
+        return fail_in(ES_ERR_INVALID_ARG, name, "without a teacher a row has one id");
+    if (rows == 0) return ES_OK;
+    if (x == nullptr || weight == nullptr || ids == nullptr)
+        return fail_in(ES_ERR_INVALID_ARG, name, "null pointer");
+    if (odd(x, 2) || odd(weight, 2) || odd(ids, 8) || odd(teacher, 4))
+        return fail_in(ES_ERR_ALIGN, name, "array not aligned to its elements");
+    return ES_OK;
+}
+
+// The head's rows as the products take them: as they are where each starts at a word
+// of 16 bytes, otherwise copied, a piece at a time.
+struct HeadRows {
+    bool copied;
+    uint32_t padded, piece, pieces;        // row width; rows of a piece
+    HeadRows(const void* w, uint64_t stride, uint32_t vocab, uint32_t hidden, uint64_t row_bytes) {
+        copied = !word_rows(w, stride, hidden);
+        padded = static_cast<uint32_t>(up(hidden, kDepth));
+        uint64_t each = row_bytes;
+        if (copied) each = std::max<uint64_t>(each, 2 * padded);
+        const uint64_t whole = up(vocab, kTile);
+        const uint64_t most = each == 0 ? whole
+                                        : std::max<uint64_t>(kTile, kPieceBytes / each / kTile * kTile);
+        pieces = static_cast<uint32_t>((whole + most - 1) / most);
+        // pieces of about one size
+        piece = static_cast<uint32_t>(up((whole + pieces - 1) / pieces, kTile));
+        pieces = static_cast<uint32_t>((whole + piece - 1) / piece);
+    }
+};
+
+struct Lists {
+    uint8_t* flags;
+    uint32_t *list, *count;
+    uint16_t* x;
+    uint32_t rows, padded;                 // of the packed rows
+    Lists(Room& room, uint32_t n, uint32_t hidden) {
+        rows = static_cast<uint32_t>(up(n, kTile));
+        padded = static_cast<uint32_t>(up(hidden, kDepth));
+        flags = room.take<uint8_t>(n);
+        list = room.take<uint32_t>(n);
+        count = room.take<uint32_t>(1);
+        x = room.take<uint16_t>(uint64_t(rows) * padded);
+    }
+    Side deep() const { return Side{x, padded, rows}; }
+    Side wide() const { return Side{x, padded, padded}; }
+};
+
+struct ScorePlan {
+    HeadRows head;
+    Lists lists;
+    uint32_t tiles;
+    float* parts;
+    uint16_t* w;
+    ScorePlan(Room& room, const es_head_score_t& x)
+        : head(x.weight, x.w_stride, x.vocab, x.hidden, 0), lists(room, x.rows, x.hidden) {
+        tiles = (x.vocab + kTile - 1) / kTile;
+        parts = room.take<float>(uint64_t(2) * lists.rows * tiles);
+        w = head.copied ? room.take<uint16_t>(uint64_t(head.piece) * head.padded) : nullptr;
+    }
+};
+
+struct GradientPlan {
+    Lists lists;
+    HeadRows head;
+    float *factor, *minus_lse, *parts;
+    uint16_t *d, *w;
+    uint32_t splits, split_depth;
+    GradientPlan(Room& room, const es_head_gradient_t& x)
+        : lists(room, x.rows, x.hidden),
+          head(x.weight, x.w_stride, x.vocab, x.hidden, 2 * uint64_t(lists.rows)) {
+        factor = room.take<float>(lists.rows);
+        minus_lse = room.take<float>(lists.rows);
+        d = room.take<uint16_t>(uint64_t(lists.rows) * head.piece);
+        w = head.copied ? room.take<uint16_t>(uint64_t(head.piece) * head.padded) : nullptr;
+        splits = 1;
+        split_depth = head.piece;
+        parts = nullptr;
+        if (x.d_x == nullptr) return;
+        // the sum over the vocabulary in as many parts as fill the card
+        const uint32_t tiles = lists.rows / kTile * ((x.hidden + kTile - 1) / kTile);
+        const uint32_t most = std::max(1u, head.piece / 1024);
+        splits = std::min(most, std::max(1u, kCus / tiles));
+        split_depth = static_cast<uint32_t>(up((head.piece + splits - 1) / splits, kDepth));
+        splits = (head.piece + split_depth - 1) / split_depth;
+        if (splits > 1 || head.pieces > 1)
+            parts = room.take<float>(uint64_t(splits) * lists.rows * lists.padded);
+    }
+};
+
+Product product(Side a, Side b, uint32_t m, uint32_t n, uint32_t depth, const uint32_t* count) {
+    Product p{};
+    p.a = a;
+    p.b = b;
+    p.depth = depth;
+    p.m_tiles = (m + kTile - 1) / kTile;
+    p.n_tiles = (n + kTile - 1) / kTile;
+    p.splits = 1;
+    p.split_depth = depth;
+    p.count = count;
+    return p;
+}
+
+dim3 grid_of(const Product& p) { return dim3(p.m_tiles * p.n_tiles * p.splits); }
+
+// Flags, list and packed rows of a call.
+int list_rows(const char* name, const eshead::RowArgs& rows, const Lists& l, const void* x,
+              uint64_t x_stride, eshead::PackArgs pack, hipStream_t s) {
+    const uint32_t per = rows.entries == 1 && rows.dx == nullptr ? 256 : 4;
+    hipLaunchKernelGGL(eshead::es_head_rows_kernel, dim3((rows.rows + per - 1) / per), dim3(256), 0, s,
+                       rows);
+    hipLaunchKernelGGL(eshead::es_head_list_kernel, dim3(1), dim3(1024), 0, s,
+                       eshead::ListArgs{l.flags, l.list, l.count, rows.rows});
+    pack.from = static_cast<const uint16_t*>(x);
+    pack.to = l.x;
+    pack.stride = x_stride;
+    pack.list = l.list;
+    pack.count = l.count;
+    pack.rows = rows.rows;
+    pack.width = rows.hidden;
+    pack.padded = l.padded;
+    pack.flags = l.flags;
+    hipLaunchKernelGGL(eshead::es_head_pack_kernel, dim3(l.rows / 4), dim3(256), 0, s, pack);
+    return launch_error(name);
+}
+
+// Rows v0 .. of the head, copied if need be, as a deep side and the stride and start of its rows.
+Side head_side(const HeadRows& h, const void* w, uint64_t stride, uint16_t* room, uint32_t v0,
+               uint32_t have, uint32_t hidden, hipStream_t s) {
+    const uint16_t* const from = static_cast<const uint16_t*>(w) + v0 * stride;
+    if (!h.copied) return Side{from, stride, have};
+    eshead::PackArgs pack{};
+    pack.from = from;
+    pack.to = room;
+    pack.stride = stride;
+    pack.rows = have;
+    pack.width = hidden;
+    pack.padded = h.padded;
+    hipLaunchKernelGGL(eshead::es_head_pack_kernel, dim3(static_cast<uint32_t>(up(have, kTile) / 4)),
+                       dim3(256), 0, s, pack);
+    return Side{room, h.padded, have};
+}
+
+}  // namespace
+
+extern "C" {
+
+uint64_t es_head_score_bytes(const es_head_score_t* args) {
+    if (args == nullptr) return 0;
+    const es_head_score_t& x = *args;
+    if (check_head("es_head_score_bytes", x.x, x.weight, x.x_stride, x.w_stride, x.ids, x.teacher,
+                   x.rows, x.vocab, x.hidden, x.entries, x.scale, x.reserved) != ES_OK ||
+        x.rows == 0)
+        return 0;
+    Room room{nullptr};
+    const ScorePlan plan(room, x);
+    return room.used;
+}
+
+int es_head_score(const es_head_score_t* args, es_stream_t stream) try {
+    const char* const name = "es_head_score";
+    if (args == nullptr) return fail_in(ES_ERR_INVALID_ARG, name, "null pointer");
+    const es_head_score_t& x = *args;
+    int rc = check_head(name, x.x, x.weight, x.x_stride, x.w_stride, x.ids, x.teacher, x.rows,
+                        x.vocab, x.hidden, x.entries, x.scale, x.reserved);
+    if (rc != ES_OK) return rc;
+    if (x.rows == 0) return ES_OK;
+    if (x.logp == nullptr || x.lse == nullptr || (x.loss == nullptr) != (x.teacher == nullptr))
+        return fail_in(ES_ERR_INVALID_ARG, name, "logp and lse are needed, and loss with a teacher");
+    if (odd(x.logp, 4) || odd(x.lse, 4) || odd(x.loss, 4) || odd(x.status, 4) || odd(x.workspace, 256))
+        return fail_in(ES_ERR_ALIGN, name, "array not aligned to its elements");
+    int device = -1;
+    rc = current_device(&device);
+    if (rc != ES_OK) return rc;
+    Room room{static_cast<uint8_t*>(x.workspace)};
+    const ScorePlan plan(room, x);
+    if (x.workspace == nullptr || x.workspace_bytes < room.used)
+        return fail_in(ES_ERR_INVALID_ARG, name, "workspace smaller than es_head_score_bytes");
+    const uint64_t pairs = uint64_t(x.rows) * x.entries;
+    Accesses ok{device, name, {}};
+    ok.check(x.x, extent(x.rows, x.hidden, x.x_stride), ": rows");
+    ok.check(x.weight, extent(x.vocab, x.hidden, x.w_stride), ": weight");
+    ok.check(x.ids, 8 * pairs, ": ids");
+    ok.check(x.teacher, x.teacher != nullptr ? 4 * pairs : 0, ": teacher");
+    ok.check(x.loss, x.loss != nullptr ? uint64_t(4) * x.rows : 0, ": loss");
+    ok.check(x.logp, 4 * pairs, ": logp");
+    ok.check(x.lse, uint64_t(4) * x.rows, ": lse");
+    ok.check(x.status, x.status != nullptr ? 4 : 0, ": status");
+    ok.check(x.workspace, room.used, ": workspace");
+    if (ok.rc != ES_OK) return ok.rc;
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    eshead::RowArgs rows{};
+    rows.ids = x.ids;
+    rows.teacher = x.teacher;
+    rows.flags = plan.lists.flags;
+    rows.loss = x.loss;
+    rows.logp = x.logp;
+    rows.lse = x.lse;
+    rows.status = x.status;
+    rows.rows = x.rows;
+    rows.vocab = x.vocab;
+    rows.entries = x.entries;
+    rows.hidden = x.hidden;
+    rc = list_rows(name, rows, plan.lists, x.x, x.x_stride, eshead::PackArgs{}, s);
+    if (rc != ES_OK) return rc;
+    for (uint32_t v0 = 0; v0 < x.vocab; v0 += plan.head.piece) {
+        const uint32_t have = std::min(plan.head.piece, x.vocab - v0);
+        const Side w = head_side(plan.head, x.weight, x.w_stride, plan.w, v0, have, x.hidden, s);
+        eshead::StatsArgs a{};
+        a.p = product(w, plan.lists.deep(), have, x.rows, x.hidden, plan.lists.count);
+        a.parts = plan.parts;
+        a.parts_stride = plan.tiles;
+        a.part0 = v0 / kTile;
+        a.factor = x.scale * eshead::kLog2e;
+        hipLaunchKernelGGL(eshead::es_head_stats_kernel, grid_of(a.p), dim3(kThreads), kLdsBytes, s, a);
+        rc = launch_error("es_head_stats_kernel launch");
+        if (rc != ES_OK) return rc;
+    }
+    eshead::ScoreArgs a{};
+    a.parts = plan.parts;
+    a.parts_stride = plan.tiles;
+    a.n_parts = plan.tiles;
+    a.list = plan.lists.list;
+    a.count = plan.lists.count;
+    a.x = plan.lists.x;
+    a.x_stride = plan.lists.padded;
+    a.w = static_cast<const uint16_t*>(x.weight);
+    a.w_stride = x.w_stride;
+    a.ids = x.ids;
+    a.teacher = x.teacher;
+    a.loss = x.loss;
+    a.logp = x.logp;
+    a.lse = x.lse;
+    a.hidden = x.hidden;
+    a.entries = x.entries;
+    a.scale = x.scale;
+    hipLaunchKernelGGL(eshead::es_head_score_kernel, dim3(x.rows), dim3(256), 0, s, a);
+    return launch_error("es_head_score_kernel launch");
+} catch (const std::bad_alloc&) {
+    return fail(ES_ERR_NOMEM, "es_head_score: host allocation failed");
+}
+
+uint64_t es_head_gradient_bytes(const es_head_gradient_t* args) {
+    if (args == nullptr) return 0;
+    const es_head_gradient_t& x = *args;
+    if (check_head("es_head_gradient_bytes", x.x, x.weight, x.x_stride, x.w_stride, x.ids, x.teacher,
+                   x.rows, x.vocab, x.hidden, x.entries, x.scale, x.reserved) != ES_OK ||
+        x.rows == 0)
+        return 0;
+    Room room{nullptr};
+    const GradientPlan plan(room, x);
+    return room.used;
+}
+
+int es_head_gradient(const es_head_gradient_t* args, es_stream_t stream) try {
+    const char* const name = "es_head_gradient";
+    if (args == nullptr) return fail_in(ES_ERR_INVALID_ARG, name, "null pointer");
+    const es_head_gradient_t& x = *args;
+    int rc = check_head(name, x.x, x.weight, x.x_stride, x.w_stride, x.ids, x.teacher, x.rows,
+                        x.vocab, x.hidden, x.entries, x.scale, x.reserved);
+    if (rc != ES_OK) return rc;
+    if (x.dx_stride > kMaxStride || x.dw_stride > kMaxStride)
+        return fail_in(ES_ERR_INVALID_ARG, name, "stride above 2^22");
+    if (x.rows == 0 && x.d_weight != nullptr)
+        return fail_in(ES_ERR_INVALID_ARG, name, "no rows: the head's gradient is not written");
+    if (x.rows == 0) return ES_OK;
+    if (x.logp == nullptr || x.lse == nullptr || x.grad == nullptr)
+        return fail_in(ES_ERR_INVALID_ARG, name, "null pointer");
+    if ((x.d_x != nullptr && x.rows > 1 && x.dx_stride < x.hidden) ||
+        (x.d_weight != nullptr && x.vocab > 1 && x.dw_stride < x.hidden))
+        return fail_in(ES_ERR_INVALID_ARG, name, "a gradient's rows overlap");
+    if (odd(x.logp, 4) || odd(x.lse, 4) || odd(x.grad, 4) || odd(x.d_x, 2) || odd(x.d_weight, 2) ||
+        odd(x.status, 4) || odd(x.workspace, 256))
+        return fail_in(ES_ERR_ALIGN, name, "array not aligned to its elements");
+    int device = -1;
+    rc = current_device(&device);
+    if (rc != ES_OK) return rc;
+    Room room{static_cast<uint8_t*>(x.workspace)};
+    const GradientPlan plan(room, x);
+    if (x.workspace == nullptr || x.workspace_bytes < room.used)
+        return fail_in(ES_ERR_INVALID_ARG, name, "workspace smaller than es_head_gradient_bytes");
+    const uint64_t pairs = uint64_t(x.rows) * x.entries;
+    Accesses ok{device, name, {}};
+    ok.check(x.x, extent(x.rows, x.hidden, x.x_stride), ": rows");
+    ok.check(x.weight, extent(x.vocab, x.hidden, x.w_stride), ": weight");
+    ok.check(x.ids, 8 * pairs, ": ids");
+    ok.check(x.teacher, x.teacher != nullptr ? 4 * pairs : 0, ": teacher");
+    ok.check(x.logp, 4 * pairs, ": logp");
+    ok.check(x.lse, uint64_t(4) * x.rows, ": lse");
+    ok.check(x.grad, uint64_t(4) * x.rows, ": grad");
+    if (x.d_x != nullptr) ok.check(x.d_x, extent(x.rows, x.hidden, x.dx_stride), ": rows' gradient");
+    if (x.d_weight != nullptr)
+        ok.check(x.d_weight, extent(x.vocab, x.hidden, x.dw_stride), ": weight's gradient");
+    ok.check(x.status, x.status != nullptr ? 4 : 0, ": status");
+    ok.check(x.workspace, room.used, ": workspace");
+    if (ok.rc != ES_OK) return ok.rc;
+    if (x.d_x == nullptr && x.d_weight == nullptr) return ES_OK;
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    const Lists& l = plan.lists;
+    eshead::RowArgs rows{};
+    rows.ids = x.ids;
+    rows.teacher = x.teacher;
+    rows.flags = l.flags;
+    rows.dx = static_cast<uint16_t*>(x.d_x);
+    rows.dx_stride = x.dx_stride;
+    rows.status = x.status;
+    rows.rows = x.rows;
+    rows.vocab = x.vocab;
+    rows.entries = x.entries;
+    rows.hidden = x.hidden;
+    const float signed_scale = x.teacher == nullptr ? -x.scale : x.scale;
+    eshead::PackArgs pack{};
+    pack.grad = x.grad;
+    pack.lse = x.lse;
+    pack.factor = plan.factor;
+    pack.minus_lse = plan.minus_lse;
+    pack.scale = signed_scale;
+    rc = list_rows(name, rows, l, x.x, x.x_stride, pack, s);
+    if (rc != ES_OK) return rc;
+    for (uint32_t v0 = 0; v0 < x.vocab; v0 += plan.head.piece) {
+        const uint32_t have = std::min(plan.head.piece, x.vocab - v0);
+        const Side w = head_side(plan.head, x.weight, x.w_stride, plan.w, v0, have, x.hidden, s);
+        eshead::ProbArgs a{};
+        a.p = product(w, l.deep(), have, x.rows, x.hidden, l.count);
+        a.factor = plan.factor;
+        a.minus_lse = plan.minus_lse;
+        a.d = plan.d;
+        a.d_stride = plan.head.piece;
+        a.scale = x.scale * eshead::kLog2e;
+        hipLaunchKernelGGL(eshead::es_head_prob_kernel, grid_of(a.p), dim3(kThreads), kLdsBytes, s, a);
+        eshead::EntryArgs e{};
+        e.list = l.list;
+        e.count = l.count;
+        e.flags = l.flags;
+        e.ids = x.ids;
+        e.teacher = x.teacher;
+        e.logp = x.logp;
+        e.grad = x.grad;
+        e.d = plan.d;
+        e.d_stride = plan.head.piece;
+        e.entries = x.entries;
+        e.v0 = v0;
+        e.v_end = v0 + have;
+        e.scale = x.scale;
+        e.sign_scale = signed_scale;
+        hipLaunchKernelGGL(eshead::es_head_entries_kernel, dim3(x.rows), dim3(256), 0, s, e);
+        rc = launch_error("es_head_prob_kernel launch");
+        if (rc != ES_OK) return rc;
+        const Side d_deep{plan.d, plan.head.piece, l.rows};
+        if (x.d_x != nullptr) {
+            eshead::RowGradArgs g{};
+            // along the tile the head's rows are as wide as they are stored
+            const uint32_t width = plan.head.copied ? plan.head.padded : x.hidden;
+            g.p = product(Side{w.at, w.stride, width}, d_deep, x.hidden, x.rows, have, l.count);
+            g.p.splits = plan.splits;
+            g.p.split_depth = plan.split_depth;
+            g.parts = plan.parts;
+            g.parts_rows = l.rows;
+            g.parts_stride = l.padded;
+            g.hidden = x.hidden;
+            g.add = v0 != 0;
+            if (plan.parts == nullptr) {
+                g.out = static_cast<uint16_t*>(x.d_x);
+                g.out_stride = x.dx_stride;
+                g.list = l.list;
+            }
+            hipLaunchKernelGGL(eshead::es_head_row_grad_kernel, grid_of(g.p), dim3(kThreads), kLdsBytes,
+                               s, g);
+        }
+        if (x.d_weight != nullptr) {
+            eshead::HeadGradArgs g{};
+            const Side d_wide{plan.d, plan.head.piece, plan.head.piece};
+            g.p = product(l.wide(), d_wide, x.hidden, have, l.rows, l.count);
+            g.out = static_cast<uint16_t*>(x.d_weight) + v0 * x.dw_stride;
+            g.out_stride = x.dw_stride;
+            g.n_have = have;
+            g.hidden = x.hidden;
+            hipLaunchKernelGGL(eshead::es_head_weight_grad_kernel, grid_of(g.p), dim3(kThreads), kLdsBytes,
+                               s, g);
+        }
+        rc = launch_error("es_head_gradient kernel launch");
+        if (rc != ES_OK) return rc;
+    }
+    if (x.d_x != nullptr && plan.parts != nullptr) {
+        eshead::JoinArgs j{};
+        j.parts = plan.parts;
+        j.parts_rows = l.rows;
+        j.parts_stride = l.padded;
+        j.splits = plan.splits;
+        j.hidden = x.hidden;
+        j.list = l.list;
+        j.count = l.count;
+        j.out = static_cast<uint16_t*>(x.d_x);
+        j.out_stride = x.dx_stride;
+        hipLaunchKernelGGL(eshead::es_head_join_kernel, dim3((x.hidden + 1023) / 1024, x.rows), dim3(256),
+                           0, s, j);
+    }
+    return launch_error("es_head_join_kernel launch");
+} catch (const std::bad_alloc&) {
+    return fail(ES_ERR_NOMEM, "es_head_gradient: host allocation failed");
+}
+
+}  // extern "C"
+
+// ----------------------------------------------------------------- adapters --
+
+namespace {
+
+int check_adapt(const char* name, const es_adapt_t& x) {
+    if (x.rows > (1u << 20)) return fail_in(ES_ERR_INVALID_ARG, name, "rows above 2^20");
+    if (x.inner == 0 || x.inner % 8 != 0 || x.inner > 65536)
+        return fail_in(ES_ERR_INVALID_ARG, name, "inner is not a multiple of 8 up to 65536");
+    if (x.outer == 0 || x.outer > (1u << 20))
+        return fail_in(ES_ERR_INVALID_ARG, name, "outer out of range (1 .. 2^20)");
+    if (x.members == 0 || x.members > 65536)
+        return fail_in(ES_ERR_INVALID_ARG, name, "members out of range (1 .. 65536)");
+    if (x.rank == 0 || x.rank % 8 != 0 || x.rank > esadapt::kMaxRank)
+        return fail_in(ES_ERR_INVALID_ARG, name, "rank is not a multiple of 8 up to 128");
+    if (x.reserved != 0) return fail_in(ES_ERR_INVALID_ARG, name, "reserved is not 0");
+    if (x.x_stride > kMaxStride || x.w_stride > kMaxStride || x.out_stride > kMaxStride)
+        return fail_in(ES_ERR_INVALID_ARG, name, "stride above 2^22");
+    if (x.rows == 0) return ES_OK;
+    if (x.x == nullptr || x.weight == nullptr || x.out == nullptr || x.a == nullptr ||
+        x.b == nullptr || x.index == nullptr)
+        return fail_in(ES_ERR_INVALID_ARG, name, "null pointer");
+    if (x.out == x.x) return fail_in(ES_ERR_INVALID_ARG, name, "out is x");
+    if (x.rows > 1 && x.out_stride < x.outer)
+        return fail_in(ES_ERR_INVALID_ARG, name, "the output's rows overlap");
+    if (odd(x.x, 2) || odd(x.out, 2) || odd(x.scales, 4) || odd(x.index, 4) || odd(x.status, 4))
+        return fail_in(ES_ERR_ALIGN, name, "array not aligned to its elements");
+    if (odd(x.weight, 16) || (x.outer > 1 && x.w_stride % 8 != 0) || odd(x.a, 16) || odd(x.b, 16))
+        return fail_in(ES_ERR_ALIGN, name, "weight's rows or adapters not 16-byte aligned");
+    return ES_OK;
+}
+
+struct AdaptPlan {
+    uint16_t *u, *x;
+    uint32_t padded, packed_rows;
+    AdaptPlan(Room& room, const es_adapt_t& a) {
+        u = room.take<uint16_t>(uint64_t(a.rows) * a.rank);
+        padded = static_cast<uint32_t>(up(a.inner, kDepth));
+        packed_rows = static_cast<uint32_t>(up(a.rows, kTile));
+        // the products take rows that start at a word of 16 bytes and end in whole stages
+        const bool copied = padded != a.inner || !word_rows(a.x, a.x_stride, a.inner);
+        x = nullptr;
+        if (copied) x = room.take<uint16_t>(uint64_t(packed_rows) * padded);
+        is_copied = copied;
+    }
+    bool is_copied;
+};
+
+}  // namespace
+
+extern "C" {
+
+uint64_t es_adapt_bytes(const es_adapt_t* args) {
+    if (args == nullptr || check_adapt("es_adapt_bytes", *args) != ES_OK || args->rows == 0) return 0;
+    Room room{nullptr};
+    const AdaptPlan plan(room, *args);
+    return room.used;
+}
+
+int es_adapt_project(const es_adapt_t* args, es_stream_t stream) try {
+    const char* const name = "es_adapt_project";
+    if (args == nullptr) return fail_in(ES_ERR_INVALID_ARG, name, "null pointer");
+    const es_adapt_t& x = *args;
+    int rc = check_adapt(name, x);
+    if (rc != ES_OK) return rc;
+    if (x.rows == 0) return ES_OK;
+    if (odd(x.workspace, 256)) return fail_in(ES_ERR_ALIGN, name, "workspace not 256-byte aligned");
+    int device = -1;
+    rc = current_device(&device);
+    if (rc != ES_OK) return rc;
+    Room room{static_cast<uint8_t*>(x.workspace)};
+    const AdaptPlan plan(room, x);
+    if (x.workspace == nullptr || x.workspace_bytes < room.used)
+        return fail_in(ES_ERR_INVALID_ARG, name, "workspace smaller than es_adapt_bytes");
+    Accesses ok{device, name, {}};
+    ok.check(x.x, extent(x.rows, x.inner, x.x_stride), ": rows");
+    ok.check(x.weight, extent(x.outer, x.inner, x.w_stride), ": weight");
+    ok.check(x.out, extent(x.rows, x.outer, x.out_stride), ": output");
+    ok.check(x.a, 2 * uint64_t(x.members) * x.rank * x.inner, ": a");
+    ok.check(x.b, 2 * uint64_t(x.members) * x.rank * x.outer, ": b");
+    ok.check(x.scales, x.scales != nullptr ? uint64_t(4) * x.members : 0, ": scales");
+    ok.check(x.index, uint64_t(4) * x.rows, ": index");
+    ok.check(x.status, x.status != nullptr ? 4 : 0, ": status");
+    ok.check(x.workspace, room.used, ": workspace");
+    if (ok.rc != ES_OK) return ok.rc;
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    esadapt::SmallArgs small{};
+    small.x = static_cast<const uint16_t*>(x.x);
+    small.x_stride = x.x_stride;
+    small.a = static_cast<const uint16_t*>(x.a);
+    small.scales = x.scales;
+    small.index = x.index;
+    small.u = plan.u;
+    small.status = x.status;
+    small.rows = x.rows;
+    small.inner = x.inner;
+    small.members = x.members;
+    small.rank = x.rank;
+    hipLaunchKernelGGL(esadapt::es_adapt_small_kernel,
+                       dim3((x.rows + esadapt::kSmallRows - 1) / esadapt::kSmallRows), dim3(kThreads), 0, s,
+                       small);
+    esadapt::TileArgs a{};
+    Side rows{static_cast<const uint16_t*>(x.x), x.x_stride, x.rows};
+    if (plan.is_copied) {
+        eshead::PackArgs pack{};
+        pack.from = static_cast<const uint16_t*>(x.x);
+        pack.to = plan.x;
+        pack.stride = x.x_stride;
+        pack.rows = x.rows;
+        pack.width = x.inner;
+        pack.padded = plan.padded;
+        hipLaunchKernelGGL(eshead::es_head_pack_kernel, dim3(plan.packed_rows / 4), dim3(256), 0, s, pack);
+        rows = Side{plan.x, plan.padded, plan.packed_rows};
+    }
+    a.p = product(Side{static_cast<const uint16_t*>(x.weight), x.w_stride, x.outer}, rows, x.outer, x.rows,
+                  x.inner, nullptr);
+    a.add = esadapt::AddArgs{x.index, plan.u, static_cast<const uint16_t*>(x.b), x.rows, x.outer,
+                             x.members, x.rank};
+    a.out = static_cast<uint16_t*>(x.out);
+    a.out_stride = x.out_stride;
+    hipLaunchKernelGGL(esadapt::es_adapt_tile_kernel, grid_of(a.p), dim3(kThreads), kLdsBytes, s, a);
+    return launch_error("es_adapt_project kernel launch");
+} catch (const std::bad_alloc&) {
+    return fail(ES_ERR_NOMEM, "es_adapt_project: host allocation failed");
+}
+
+}  // extern "C"

@@ -1,0 +1,513 @@
+// Scores of targets over a large vocabulary and the divergence from a teacher's
+// top logits, with their gradients, without keeping the logits.
+//
+// With z = scale x . w_v and lse = log sum_v exp z_v, a row's scores are z_id - lse;
+// its gradient is f (Q softmax(z) - q), q the wanted weights at its ids, Q their
+// sum (1, or 0 where a teacher leaves nothing).  The logits of a tile live in
+// registers: the scores keep a maximum and a sum of each row and tile, and the
+// gradients f Q softmax(z) as bf16, for a piece of the vocabulary at a time.
+#pragma once
+
+#include "mm_tile.hpp"
+
+namespace eshead {
+
+using namespace esmm;
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr uint32_t kMaxEntries = 256;
+
+// What becomes of a row, by its ids.
+enum Row : uint8_t { kDead = 0, kLive = 1, kVoid = 2, kEmpty = 3 };   // kEmpty: live, Q = 0
+
+// ------------------------------------------------------------------- rows --
+
+struct RowArgs {
+    const int64_t* ids;
+    const float* teacher;                  // or null
+    uint8_t* flags;                        // [rows]
+    float *loss, *logp, *lse;              // of dead rows zeros, of void ones NaN; or null
+    uint16_t* dx;                          //   likewise
+    uint64_t dx_stride;
+    uint32_t* status;
+    uint32_t rows, vocab, entries, hidden;
+};
+
+// One wave a row (one lane where it has one entry and no gradient to clear).
+__global__ __launch_bounds__(256) void es_head_rows_kernel(RowArgs a) {
+    const uint32_t lane = threadIdx.x & 63;
+    if (a.entries == 1 && a.dx == nullptr) {
+        const uint32_t r = blockIdx.x * 256 + threadIdx.x;
+        if (r >= a.rows) return;
+        const int64_t id = a.ids[r];
+        uint8_t flag = id < 0 ? kDead : id < int64_t(a.vocab) ? kLive : kVoid;
+        if (flag == kLive && a.teacher != nullptr && a.teacher[r] == -eskv::inf()) flag = kEmpty;
+        a.flags[r] = flag;
+        if (flag == kVoid && a.status != nullptr) atomicOr(a.status, ES_HEAD_BAD_ID);
+        if (flag == kDead || flag == kVoid) {
+            const float v = flag == kVoid ? eskv::nan() : 0.0f;
+            if (a.loss != nullptr) a.loss[r] = v;
+            if (a.logp != nullptr) a.logp[r] = v;
+            if (a.lse != nullptr) a.lse[r] = v;
+        }
+        return;
+    }
+    const uint32_t r = blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (r >= a.rows) return;
+    bool some = false, bad = false, weight = a.teacher == nullptr;
+    for (uint32_t e = lane; e < a.entries; e += 64) {
+        const int64_t id = a.ids[uint64_t(r) * a.entries + e];
+        some |= id >= 0;
+        bad |= id >= int64_t(a.vocab);
+        if (id >= 0 && a.teacher != nullptr)
+            weight |= a.teacher[uint64_t(r) * a.entries + e] != -eskv::inf();
+    }
+    some = __any(some);
+    bad = __any(bad);
+    weight = __any(weight);
+    const uint8_t flag = bad ? kVoid : !some ? kDead : weight ? kLive : kEmpty;
+    if (lane == 0) {
+        a.flags[r] = flag;
+        if (bad && a.status != nullptr) atomicOr(a.status, ES_HEAD_BAD_ID);
+    }
+    if (flag != kDead && flag != kVoid) return;
+    const float v = bad ? eskv::nan() : 0.0f;
+    if (lane == 0) {
+        if (a.loss != nullptr) a.loss[r] = v;
+        if (a.lse != nullptr) a.lse[r] = v;
+    }
+    if (a.logp != nullptr)
+        for (uint32_t e = lane; e < a.entries; e += 64) a.logp[uint64_t(r) * a.entries + e] = v;
+    if (a.dx != nullptr)
+        for (uint32_t h = lane; h < a.hidden; h += 64)
+            a.dx[r * a.dx_stride + h] = bad ? 0x7FC0u : 0u;
+}
+
+struct ListArgs {
+    const uint8_t* flags;
+    uint32_t* list;                        // live rows in order
+    uint32_t* count;                       // [0]: how many
+    uint32_t rows;
+};
+
+// One workgroup: 16 rows a thread at a time.
+__global__ __launch_bounds__(1024) void es_head_list_kernel(ListArgs a) {
+    __shared__ uint32_t waves[16];
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint32_t base = 0;
+    for (uint32_t r0 = 0; r0 < a.rows; r0 += 16384) {
+        const uint32_t mine = r0 + 16 * threadIdx.x;
+        uint32_t live = 0;
+        for (uint32_t i = 0; i < 16; ++i) {
+            if (mine + i >= a.rows) break;
+            const uint8_t f = a.flags[mine + i];
+            live |= uint32_t(f == kLive || f == kEmpty) << i;
+        }
+        const uint32_t n = __popc(live);
+        uint32_t sum = n;                  // over this lane and those before it
+        for (uint32_t d = 1; d < 64; d *= 2) {
+            const uint32_t y = __shfl_up(sum, d);
+            if (lane >= d) sum += y;
+        }
+        if (lane == 63) waves[wave] = sum;
+        __syncthreads();
+        uint32_t before = base, all = 0;
+        for (uint32_t w = 0; w < 16; ++w) {
+            if (w < wave) before += waves[w];
+            all += waves[w];
+        }
+        uint32_t at = before + sum - n;
+        for (uint32_t i = 0; i < 16; ++i)
+            if (live >> i & 1) a.list[at++] = mine + i;
+        base += all;
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) *a.count = base;
+}
+
+struct PackArgs {
+    const uint16_t* from;
+    uint16_t* to;
+    uint64_t stride;                       // of `from`; `to` has rows of `padded`
+    const uint32_t* list;                  // row i of `to` is row list[i] of `from`; null: row i
+    const uint32_t* count;                 // rows that there are; null: `rows`
+    uint32_t rows, width, padded;
+    // of the gradients: what a row's products are scaled by (null: none)
+    const uint8_t* flags;
+    const float *grad, *lse;
+    float *factor, *minus_lse;
+    float scale;                           // with its sign
+};
+
+// Rows copied to where every row starts at a word of 16 bytes and ends in zeros; the
+// rows behind the last one, up to a tile's end, are zeros.  One wave a row.
+__global__ __launch_bounds__(256) void es_head_pack_kernel(PackArgs a) {
+    const uint32_t lane = threadIdx.x & 63;
+    const uint32_t i = blockIdx.x * 4 + (threadIdx.x >> 6);
+    const uint32_t count = a.count != nullptr ? *a.count : a.rows;
+    if (i >= (count + kTile - 1) / kTile * kTile) return;
+    const bool live = i < count;
+    const uint32_t row = !live ? 0 : a.list != nullptr ? a.list[i] : i;
+    const uint16_t* const from = a.from + row * a.stride;
+    uint16_t* const to = a.to + uint64_t(i) * a.padded;
+    for (uint32_t k = 8 * lane; k < a.padded; k += 512) {
+        u32x4_t v = {0, 0, 0, 0};
+        if (live && k + 8 <= a.width) {
+            v = load_row8(from + k);
+        } else if (live) {
+            for (uint32_t e = 0; k + e < a.width; ++e)
+                v[e / 2] |= uint32_t(load<uint16_t>(from + k + e)) << (16 * (e % 2));
+        }
+        store<u32x4_t>(to + k, v);
+    }
+    if (a.factor != nullptr && lane == 0) {
+        a.factor[i] = live && a.flags[row] != kEmpty ? a.scale * a.grad[row] : 0.0f;
+        a.minus_lse[i] = live ? -a.lse[row] * kLog2e : 0.0f;
+    }
+}
+
+// ----------------------------------------------------------------- scores --
+
+struct StatsArgs {
+    Product p;                             // a: the vocabulary's rows, b: the packed rows
+    float* parts;                          // [rows][parts_stride] pairs: maximum, sum
+    uint64_t parts_stride;
+    uint32_t part0;                        // of this launch's first tile
+    float factor;                          // scale log2(e)
+};
+
+// A tile's rows of logits as maxima and sums, in units of log 2.
+__global__ __launch_bounds__(kThreads, 2) void es_head_stats_kernel(StatsArgs a) {
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+    const Place at = place_of(blockIdx.x, a.p);
+    const uint32_t m0 = at.m * kTile, n0 = at.n * kTile;
+    const uint32_t count = *a.p.count;
+    if (n0 >= count) return;
+    Tile c;
+    product_tile<false, false>(a.p, m0, n0, 0, a.p.depth, lds, c);
+    __syncthreads();
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint32_t m_have = a.p.a.extent - m0;
+    float* const pair = reinterpret_cast<float*>(lds);   // [2 waves of m][256 n] pairs
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        float top = -eskv::inf();
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int x = 0; x < 16; ++x) {
+                const uint32_t m = 128 * (wave & 1) + 32 * i + 8 * (x / 4) + 4 * (lane >> 5) + x % 4;
+                const float t = c.x[i][j][x] * a.factor;
+                c.x[i][j][x] = m < m_have ? t : -eskv::inf();
+                top = fmaxf(top, c.x[i][j][x]);
+            }
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float from = top == -eskv::inf() ? 0.0f : top;
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int x = 0; x < 16; ++x) sum += __builtin_amdgcn_exp2f(c.x[i][j][x] - from);
+        sum += __shfl_xor(sum, 32);
+        if (lane < 32) {
+            const uint32_t n = 64 * (wave >> 1) + 32 * j + lane;
+            pair[2 * (256 * (wave & 1) + n)] = top;
+            pair[2 * (256 * (wave & 1) + n) + 1] = sum;
+        }
+    }
+    __syncthreads();
+    const uint32_t n = threadIdx.x;
+    if (n < kTile && n0 + n < count) {
+        const float t0 = pair[2 * n], t1 = pair[2 * (256 + n)];
+        const float top = fmaxf(t0, t1), from = top == -eskv::inf() ? 0.0f : top;
+        const float sum = pair[2 * n + 1] * __builtin_amdgcn_exp2f(t0 - from) +
+                          pair[2 * (256 + n) + 1] * __builtin_amdgcn_exp2f(t1 - from);
+        float* const to = a.parts + 2 * ((n0 + n) * a.parts_stride + a.part0 + at.m);
+        to[0] = top;
+        to[1] = sum;
+    }
+}
+
+struct ScoreArgs {
+    const float* parts;
+    uint64_t parts_stride;
+    uint32_t n_parts;
+    const uint32_t *list, *count;
+    const uint16_t *x, *w;                 // x: the packed rows
+    uint64_t x_stride, w_stride;
+    const int64_t* ids;
+    const float* teacher;
+    float *loss, *logp, *lse;
+    uint32_t hidden, entries;
+    float scale;
+};
+
+__device__ __forceinline__ float wave_sum(float x) {
+#pragma unroll
+    for (int d = 32; d >= 1; d /= 2) x += __shfl_xor(x, d);
+    return x;
+}
+__device__ __forceinline__ float wave_max(float x) {
+#pragma unroll
+    for (int d = 32; d >= 1; d /= 2) x = fmaxf(x, __shfl_xor(x, d));
+    return x;
+}
+
+// Of 256 threads: sum and maximum, in one order.
+__device__ __forceinline__ float block_sum(float x, float* room) {
+    x = wave_sum(x);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) room[threadIdx.x >> 6] = x;
+    __syncthreads();
+    return (room[0] + room[1]) + (room[2] + room[3]);
+}
+__device__ __forceinline__ float block_max(float x, float* room) {
+    x = wave_max(x);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) room[threadIdx.x >> 6] = x;
+    __syncthreads();
+    return fmaxf(fmaxf(room[0], room[1]), fmaxf(room[2], room[3]));
+}
+
+// The teacher's weight of thread e's entry (0: absent), and its logarithm.
+__device__ __forceinline__ float teacher_weight(bool here, float t, float scale, float* room,
+                                                float& log_q) {
+    const float z = here ? t * scale : -eskv::inf();
+    const float top = block_max(z, room);
+    const float from = top == -eskv::inf() ? 0.0f : top;
+    const float e = here ? expf(z - from) : 0.0f;
+    const float sum = block_sum(e, room);
+    const float q = sum > 0.0f ? e / sum : e;          // (NaN stays NaN)
+    log_q = q > 0.0f ? z - from - logf(sum) : 0.0f;
+    return sum != sum ? sum : q;
+}
+
+// A live row's parts joined, and its scores: each id's logit is a product of its own.
+// One workgroup a row, waves by turns over the entries.
+__global__ __launch_bounds__(256) void es_head_score_kernel(ScoreArgs a) {
+    __shared__ float room[4], logits[kMaxEntries];
+    const uint32_t i = blockIdx.x;
+    if (i >= *a.count) return;
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint32_t row = a.list[i];
+    const float* const parts = a.parts + 2 * i * a.parts_stride;
+    float top = -eskv::inf();
+    for (uint32_t m = threadIdx.x; m < a.n_parts; m += 256) top = fmaxf(top, parts[2 * m]);
+    top = block_max(top, room);
+    const float from = top == -eskv::inf() ? 0.0f : top;
+    float sum = 0.0f;
+    for (uint32_t m = threadIdx.x; m < a.n_parts; m += 256)
+        sum += parts[2 * m + 1] * __builtin_amdgcn_exp2f(parts[2 * m] - from);
+    sum = block_sum(sum, room);
+    const float lse = (from + log2f(sum)) * kLn2;
+
+    const uint16_t* const x = a.x + i * a.x_stride;
+    const uint32_t whole = a.hidden / 8 * 8;
+    for (uint32_t e = wave; e < a.entries; e += 4) {
+        const int64_t id = a.ids[uint64_t(row) * a.entries + e];
+        if (id < 0) continue;
+        const uint16_t* const w = a.w + uint64_t(id) * a.w_stride;
+        float dot = 0.0f;
+        for (uint32_t k = 8 * lane; k < whole; k += 512) {
+            float u[8], v[8];
+            eskv::unpack8(load_row8(x + k), u);
+            eskv::unpack8(load_row8(w + k), v);
+#pragma unroll
+            for (int y = 0; y < 8; ++y) dot = __builtin_fmaf(u[y], v[y], dot);
+        }
+        if (whole + lane < a.hidden)
+            dot = __builtin_fmaf(eskv::bf16_lo(load<uint16_t>(x + whole + lane)),
+                                 eskv::bf16_lo(load<uint16_t>(w + whole + lane)), dot);
+        dot = wave_sum(dot);
+        if (lane == 0) logits[e] = dot * a.scale;
+    }
+    __syncthreads();
+    const uint32_t e = threadIdx.x;
+    const uint64_t at = uint64_t(row) * a.entries + e;
+    const bool here = e < a.entries && a.ids[at] >= 0;
+    const float logp = here ? logits[e] - lse : 0.0f;
+    if (e < a.entries) a.logp[at] = logp;
+    if (e == 0) a.lse[row] = lse;
+    if (a.teacher != nullptr) {
+        float log_q;
+        const float q = teacher_weight(here, here ? a.teacher[at] : 0.0f, a.scale, room, log_q);
+        // (a weight of zero takes nothing, whatever the student gives its entry)
+        const float loss = block_sum(here && q != 0.0f ? q * (log_q - logp) : 0.0f, room);
+        if (e == 0) a.loss[row] = loss;
+    }
+}
+
+// -------------------------------------------------------------- gradients --
+
+struct ProbArgs {
+    Product p;                             // a: a piece of the vocabulary, b: the packed rows
+    const float *factor, *minus_lse;       // of a packed row
+    uint16_t* d;                           // [rows][d_stride]
+    uint64_t d_stride;
+    float scale;                           // scale log2(e)
+};
+
+// The logits' gradients without what their ids add: factor softmax(z), as bf16 (RNE):
+// both products that take them have the matrix unit's operands.
+__global__ __launch_bounds__(kThreads, 2) void es_head_prob_kernel(ProbArgs a) {
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+    const Place at = place_of(blockIdx.x, a.p);
+    const uint32_t m0 = at.m * kTile, n0 = at.n * kTile;
+    if (n0 >= *a.p.count) return;
+    Tile c;
+    product_tile<false, false>(a.p, m0, n0, 0, a.p.depth, lds, c);
+    __syncthreads();
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint32_t m_have = a.p.a.extent - m0;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const uint32_t n = n0 + 64 * (wave >> 1) + 32 * j + (lane & 31);
+        const float f = a.factor[n], l = a.minus_lse[n];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int x = 0; x < 16; ++x) {
+                const uint32_t m = 128 * (wave & 1) + 32 * i + 8 * (x / 4) + 4 * (lane >> 5) + x % 4;
+                const float p = f * __builtin_amdgcn_exp2f(__builtin_fmaf(c.x[i][j][x], a.scale, l));
+                c.x[i][j][x] = m < m_have ? p : 0.0f;
+            }
+    }
+    tile_to_lds(c, lds);
+    __syncthreads();
+    store_rows(lds, a.d, a.d_stride, m0, kTile, [&](uint32_t n) { return int64_t(n0 + n); });
+}
+
+struct EntryArgs {
+    const uint32_t *list, *count;
+    const uint8_t* flags;
+    const int64_t* ids;
+    const float *teacher, *logp, *grad;
+    uint16_t* d;
+    uint64_t d_stride;
+    uint32_t entries, v0, v_end;           // the piece
+    float scale, sign_scale;
+};
+
+// The gradients at the ids, f (Q p - q) with the weights of equal ids summed, take
+// the places of f Q p: rounded once, where q and p nearly cancel too.
+__global__ __launch_bounds__(256) void es_head_entries_kernel(EntryArgs a) {
+    __shared__ float room[4], weights[kMaxEntries];
+    __shared__ int64_t ids[kMaxEntries];
+    const uint32_t i = blockIdx.x;
+    if (i >= *a.count) return;
+    const uint32_t row = a.list[i], e = threadIdx.x;
+    const uint64_t at = uint64_t(row) * a.entries + e;
+    const int64_t id = e < a.entries ? a.ids[at] : -1;
+    float q = id >= 0 ? 1.0f : 0.0f;
+    if (a.teacher != nullptr) {
+        float log_q;
+        q = teacher_weight(id >= 0, id >= 0 ? a.teacher[at] : 0.0f, a.scale, room, log_q);
+    }
+    ids[e] = id;
+    weights[e] = q;
+    __syncthreads();
+    if (id < int64_t(a.v0) || id >= int64_t(a.v_end)) return;
+    float all = 0.0f;
+    for (uint32_t k = 0; k < a.entries; ++k) all += ids[k] == id ? weights[k] : 0.0f;
+    const float p = a.flags[row] == kEmpty ? 0.0f : expf(a.logp[at]);
+    const float d = a.sign_scale * a.grad[row] * (p - all);
+    a.d[i * a.d_stride + (id - a.v0)] = static_cast<uint16_t>(pack_bf16(d, 0.0f));
+}
+
+struct RowGradArgs {
+    Product p;                             // a: the piece (wide), b: d
+    float* parts;                          // [splits][rows][parts_stride] binary32
+    uint64_t parts_rows, parts_stride;
+    uint32_t hidden, add;                  // add: to what is there
+    uint16_t* out;                         // or, with one split and one piece, bf16
+    uint64_t out_stride;
+    const uint32_t* list;
+};
+
+__global__ __launch_bounds__(kThreads, 2) void es_head_row_grad_kernel(RowGradArgs a) {
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+    const Place at = place_of(blockIdx.x, a.p);
+    const uint32_t m0 = at.m * kTile, n0 = at.n * kTile;
+    const uint32_t count = *a.p.count;
+    if (n0 >= count) return;
+    const uint32_t k0 = at.split * a.p.split_depth;
+    Tile c;
+    product_tile<true, false>(a.p, m0, n0, k0, min(a.p.depth, k0 + a.p.split_depth), lds, c);
+    if (a.out != nullptr) {
+        __syncthreads();
+        tile_to_lds(c, lds);
+        __syncthreads();
+        store_rows(lds, a.out, a.out_stride, m0, a.hidden - m0, [&](uint32_t n) {
+            return n0 + n < count ? int64_t(a.list[n0 + n]) : int64_t(-1);
+        });
+        return;
+    }
+    float* const to = a.parts + (at.split * a.parts_rows + n0) * a.parts_stride + m0;
+    const uint32_t m_have = a.p.a.extent - m0, n_have = count - n0;
+    for_words([&](int i, int j, int y, uint32_t m, uint32_t n) {
+        if (m >= m_have || n >= n_have) return;          // (extents are multiples of 8)
+        float* const q = to + n * a.parts_stride + m;
+        f32x4_t v = {c.x[i][j][4 * y], c.x[i][j][4 * y + 1], c.x[i][j][4 * y + 2],
+                     c.x[i][j][4 * y + 3]};
+        if (a.add) {
+            const f32x4_t was = load<f32x4_t>(q);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] += was[e];
+        }
+        store<f32x4_t>(q, v);
+    });
+}
+
+struct JoinArgs {
+    const float* parts;
+    uint64_t parts_rows, parts_stride;
+    uint32_t splits, hidden;
+    const uint32_t *list, *count;
+    uint16_t* out;
+    uint64_t out_stride;
+};
+
+// The splits' sums, in one order, rounded once.
+__global__ __launch_bounds__(256) void es_head_join_kernel(JoinArgs a) {
+    const uint32_t i = blockIdx.y, h = 4 * (blockIdx.x * 256 + threadIdx.x);
+    if (i >= *a.count || h >= a.hidden) return;
+    const float* p = a.parts + i * a.parts_stride + h;
+    f32x4_t v = load<f32x4_t>(p);
+    for (uint32_t s = 1; s < a.splits; ++s) {
+        const f32x4_t w = load<f32x4_t>(p + s * a.parts_rows * a.parts_stride);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] += w[e];
+    }
+    uint16_t* const to = a.out + a.list[i] * a.out_stride + h;
+    const u32x2_t w = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+    if (h + 4 <= a.hidden) {
+        eskv::store_row4(to, w);
+    } else {
+        for (uint32_t e = 0; h + e < a.hidden; ++e)
+            store<uint16_t>(to + e, static_cast<uint16_t>(w[e / 2] >> (16 * (e % 2))));
+    }
+}
+
+struct HeadGradArgs {
+    Product p;                             // a: the packed rows (wide), b: d (wide)
+    uint16_t* out;                         // the piece's first row
+    uint64_t out_stride;
+    uint32_t n_have, hidden;               // rows of the piece
+};
+
+__global__ __launch_bounds__(kThreads, 2) void es_head_weight_grad_kernel(HeadGradArgs a) {
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+    const Place at = place_of(blockIdx.x, a.p);
+    const uint32_t m0 = at.m * kTile, n0 = at.n * kTile;
+    const uint32_t depth = (*a.p.count + kDepth - 1) / kDepth * kDepth;   // zeros behind the rows
+    Tile c;
+    product_tile<true, true>(a.p, m0, n0, 0, depth, lds, c);
+    __syncthreads();
+    tile_to_lds(c, lds);
+    __syncthreads();
+    store_rows(lds, a.out, a.out_stride, m0, a.hidden - m0, [&](uint32_t n) {
+        return n0 + n < a.n_have ? int64_t(n0 + n) : int64_t(-1);
+    });
+}
+
+}  // namespace eshead

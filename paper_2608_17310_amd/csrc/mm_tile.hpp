@@ -1,0 +1,299 @@
+// The matrix product that the head and the projections are made of: tiles of
+// 256 x 256 results on the matrix unit, from operands in either order, with what
+// becomes of a tile (its epilogue) as a parameter.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "kv_common.hpp"
+
+namespace esmm {
+
+using eskv::bf16x8_t;
+using eskv::f32x16_t;
+using eskv::f32x4_t;
+using eskv::load;
+using eskv::load_row8;
+using eskv::pack_bf16;
+using eskv::store;
+using eskv::store_row8;
+using eskv::u32x2_t;
+using eskv::u32x4_t;
+
+constexpr int kTile = 256;                 // results of a tile in either direction
+constexpr int kDepth = 64;                 // of the summed dimension, staged at a time
+constexpr int kThreads = 512;
+constexpr uint32_t kSideBytes = kTile * kDepth * 2;
+constexpr uint32_t kPitch = kTile * 2 + 16;          // of a row of results in LDS
+constexpr uint32_t kLdsBytes = kTile * kPitch;       // the results are the most that it holds
+
+// One operand.  Deep: element (i, k) at at[i stride + k], wide: at[k stride + i],
+// i along the tile and k along the sum.  16-byte aligned, stride a multiple of 8.
+struct Side {
+    const uint16_t* at;
+    uint64_t stride;
+    uint32_t extent;                       // rows i that exist (wide: a multiple of 8)
+};
+
+// results[n][m] = sum_k a(m, k) b(n, k).  Beyond the operands' extents the last
+// row is read again, and beyond `depth` other valid elements of a; b is zero
+// there (stored to a multiple of 64).
+struct Product {
+    Side a, b;
+    uint32_t depth;
+    uint32_t m_tiles, n_tiles, splits;     // splits: of the sum, `split_depth` each
+    uint32_t split_depth;                  // a multiple of 64
+    const uint32_t* count;                 // rows n that exist, where the device knows it
+    uint32_t count_is_depth;               //   or, of a product over them, the sum's length
+};
+
+struct Place {
+    uint32_t m, n, split;
+};
+
+// Workgroups go round the eight dies in turn: each die takes a contiguous run of
+// tiles, ordered in groups of `kGroup` tiles along m over all of n, so that the
+// 32 workgroups that a die runs at a time share rows of both operands in its L2.
+constexpr uint32_t kGroup = 4;
+__device__ __forceinline__ Place place_of(uint32_t id, const Product& p) {
+    const uint32_t tiles = p.m_tiles * p.n_tiles, total = tiles * p.splits;
+    const uint32_t die = id % 8, q = total / 8, r = total % 8;
+    uint32_t at = die * q + (die < r ? die : r) + id / 8;
+    Place x;
+    x.split = at / tiles;
+    at -= x.split * tiles;
+    const uint32_t g = at / (kGroup * p.n_tiles);
+    at -= g * kGroup * p.n_tiles;
+    const uint32_t left = p.m_tiles - g * kGroup, wide = left < kGroup ? left : kGroup;
+    x.n = at / wide;
+    x.m = g * kGroup + at % wide;
+    return x;
+}
+
+// 16 bytes a lane from memory into LDS, at byte `dst` (of the wave) + 16 lane.
+// (In asm, which has no register output: the compiler would make every later read
+// of LDS wait for it.)  wait_staged() and a barrier before the data are read.
+__device__ __forceinline__ void load_lds(u32x4_t buffer, uint32_t offset, uint32_t dst) {
+    asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                 :: "s"(dst), "v"(offset), "s"(buffer) : "memory");
+}
+__device__ __forceinline__ void wait_staged() {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+}
+
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ uint64_t uniform(uint64_t x) {
+    return uint64_t(uniform(uint32_t(x >> 32))) << 32 | uniform(uint32_t(x));
+}
+
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+    return static_cast<uint32_t>(reinterpret_cast<uintptr_t>(p));   // of the shared aperture
+}
+
+// A side's way into LDS.  A stage of 64 of the sum is 32 KB.  Deep: [256 rows][8
+// words of 16 bytes], word w of row i stored at w ^ ((i >> 1) & 7): sixteen rows' words
+// of one w, which a read of an operand takes at a time, fill the banks once.
+// Wide: [64][32 words], word w of row k at w ^ (4 (k & 3)): four k's words beside
+// each other do, which a transposing read takes at a time.
+template <bool kWide>
+struct Stage {
+    uint64_t base;                         // of the next stage
+    uint64_t bytes;                        // from there to the array's end
+    uint64_t step;                         // bytes from stage to stage
+    uint32_t off[4];
+    uint32_t dst, lane_k, word;
+
+    __device__ __forceinline__ void init(const Side& s, uint32_t i0, uint32_t k0, uint32_t k_end,
+                                         uint32_t wave, uint32_t lane) {
+        const uint32_t last = s.extent - 1 - i0;         // i0 < extent
+        dst = wave * 4096;
+        if constexpr (kWide) {
+            base = reinterpret_cast<uint64_t>(s.at) + 2 * (k0 * s.stride + i0);
+            bytes = 2 * ((k_end - 1 - k0) * s.stride + last + 1);
+            step = 2 * kDepth * s.stride;
+#pragma unroll
+            for (uint32_t x = 0; x < 4; ++x) {
+                const uint32_t k = (wave * 4 + x) * 2 + (lane >> 5);
+                const uint32_t w = (lane & 31) ^ ((k & 3) << 2);
+                off[x] = k * uint32_t(2 * s.stride) + 16 * min(w, last / 8);
+            }
+        } else {
+            base = reinterpret_cast<uint64_t>(s.at) + 2 * (i0 * s.stride + k0);
+            bytes = 2 * (last * s.stride + (k_end + 7) / 8 * 8 - k0);   // rows end with a word
+            step = 2 * kDepth;
+#pragma unroll
+            for (uint32_t x = 0; x < 4; ++x) {
+                const uint32_t i = (wave * 4 + x) * 8 + (lane >> 3);
+                const uint32_t w = (lane & 7) ^ ((i >> 1) & 7);
+                off[x] = min(i, last) * uint32_t(2 * s.stride) + 16 * w;
+            }
+        }
+        base = uniform(base);
+        bytes = uniform(bytes);
+        step = uniform(step);
+    }
+
+    // Stage the next 64, of which `have` exist (the other side is zero beyond them).
+    __device__ __forceinline__ void issue(uint32_t lds, uint32_t have, const Side& s, uint32_t wave,
+                                          uint32_t lane) {
+        const u32x4_t buffer = {uint32_t(base), uint32_t(base >> 32) & 0xFFFFu,
+                                bytes > 0xFFFFFFFFull ? 0xFFFFFFFFu : uint32_t(bytes), 0x00020000u};
+        if (have >= kDepth) {
+#pragma unroll
+            for (uint32_t x = 0; x < 4; ++x) load_lds(buffer, off[x], lds + dst + 1024 * x);
+        } else {
+#pragma unroll
+            for (uint32_t x = 0; x < 4; ++x) {
+                uint32_t o = off[x];
+                if constexpr (kWide) {
+                    const uint32_t k = (wave * 4 + x) * 2 + (lane >> 5);
+                    if (k >= have) o -= (k - (have - 1)) * uint32_t(2 * s.stride);
+                } else {
+                    const uint32_t i = (wave * 4 + x) * 8 + (lane >> 3);
+                    const uint32_t w = (lane & 7) ^ ((i >> 1) & 7);
+                    if (8 * w >= have) o -= 16 * w;
+                }
+                load_lds(buffer, o, lds + dst + 1024 * x);
+            }
+        }
+        base += step;
+        bytes -= min(bytes, step);
+    }
+};
+
+// A wave's reads of a side: block b of 32 rows from row `from`, step s of 16 of the sum.
+// The operand of lane l: row l % 32 of the block, elements 8 (l / 32) .. of the step.
+template <bool kWide, int kBlocks>
+struct Reader {
+    uint32_t at[kWide ? kBlocks : 4];
+
+    __device__ __forceinline__ void init(uint32_t from, uint32_t lane) {
+        if constexpr (kWide) {
+            const uint32_t kk = (lane & 15) >> 2, k = 8 * (lane >> 5) + kk;
+#pragma unroll
+            for (uint32_t b = 0; b < kBlocks; ++b) {
+                const uint32_t i = from + 32 * b + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+                at[b] = k * 512 + (((i >> 3) ^ (kk << 2)) << 4) + ((i & 4) << 1);
+            }
+        } else {
+            const uint32_t i = from + (lane & 31);
+#pragma unroll
+            for (uint32_t s = 0; s < 4; ++s)
+                at[s] = i * 128 + (((2 * s + (lane >> 5)) ^ ((i >> 1) & 7)) << 4);
+        }
+    }
+    __device__ __forceinline__ bf16x8_t read(const uint8_t* lds, int s, int b) const {
+        if constexpr (kWide) {
+            typedef short i16x4_t __attribute__((ext_vector_type(4)));
+            typedef __attribute__((address_space(3))) i16x4_t Shared;
+            union { i16x4_t half[2]; bf16x8_t whole; } x;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+                x.half[t] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (Shared*)(lds + at[b] + 8192 * s + 2048 * t));
+            return x.whole;
+        } else {
+            return *reinterpret_cast<const bf16x8_t*>(lds + at[s] + 4096 * b);
+        }
+    }
+};
+
+// What a wave holds of a tile: rows m 128 (wave % 2) + 32 i + 8 (x / 4) + 4 (lane /
+// 32) + x % 4 in register x, and rows n 64 (wave / 2) + 32 j + lane % 32 (the waves' order
+// is m first).
+struct Tile {
+    f32x16_t x[4][2];
+};
+
+template <bool kWideA, bool kWideB>
+__device__ __forceinline__ void product_tile(const Product& p, uint32_t m0, uint32_t n0, uint32_t k0,
+                                             uint32_t k_end, uint8_t* lds, Tile& c) {
+    const uint32_t lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int x = 0; x < 16; ++x) c.x[i][j][x] = 0.0f;
+    if (k0 >= k_end) return;
+    Stage<kWideA> sa;
+    Stage<kWideB> sb;
+    sa.init(p.a, m0, k0, k_end, wave, lane);
+    sb.init(p.b, n0, k0, k_end, wave, lane);
+    Reader<kWideA, 4> ra;
+    Reader<kWideB, 2> rb;
+    ra.init(128 * (wave & 1), lane);
+    rb.init(64 * (wave >> 1), lane);
+    const uint32_t lds_at = uniform(lds_address(lds));
+    for (uint32_t k = k0; k < k_end; k += kDepth) {
+        __syncthreads();
+        sa.issue(lds_at, k_end - k, p.a, wave, lane);
+        // (the right side is stored to a multiple of 64)
+        sb.issue(lds_at + kSideBytes, kDepth, p.b, wave, lane);
+        wait_staged();
+        __syncthreads();
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            bf16x8_t a[4], b[2];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) a[i] = ra.read(lds, s, i);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) b[j] = rb.read(lds + kSideBytes, s, j);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    c.x[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[i], b[j], c.x[i][j], 0, 0, 0);
+        }
+    }
+}
+
+// f(i, j, y, m, n): words of four results, registers 4 y .. 4 y + 3 of block (i, j), rows m ..
+// m + 3 and row n of the tile.
+template <class F>
+__device__ __forceinline__ void for_words(F f) {
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int y = 0; y < 4; ++y)
+                f(i, j, y, 128 * (wave & 1) + 32 * i + 8 * y + 4 * (lane >> 5),
+                  64 * (wave >> 1) + 32 * j + (lane & 31));
+}
+
+// Results as bf16 (RNE) into LDS, [n][m]; all waves have read their last operands.
+__device__ __forceinline__ void tile_to_lds(const Tile& c, uint8_t* lds) {
+    for_words([&](int i, int j, int y, uint32_t m, uint32_t n) {
+        const f32x16_t& x = c.x[i][j];
+        *reinterpret_cast<u32x2_t*>(lds + n * kPitch + 2 * m) =
+            u32x2_t{pack_bf16(x[4 * y], x[4 * y + 1]), pack_bf16(x[4 * y + 2], x[4 * y + 3])};
+    });
+}
+
+// Rows of the tile from LDS to `out` (bf16, `stride` elements from row to row): row n
+// to row_of(n), which is negative for a row that is not written; m_have
+// results of each.
+template <class F>
+__device__ __forceinline__ void store_rows(const uint8_t* lds, uint16_t* out, uint64_t stride,
+                                           uint32_t m0, uint32_t m_have, F row_of) {
+    const uint32_t word = threadIdx.x & 31;
+#pragma unroll 4
+    for (uint32_t n = threadIdx.x >> 5; n < kTile; n += kThreads / 32) {
+        const int64_t row = row_of(n);
+        if (row < 0 || 8 * word >= m_have) continue;
+        const u32x4_t v = *reinterpret_cast<const u32x4_t*>(lds + n * kPitch + 16 * word);
+        uint16_t* const to = out + uint64_t(row) * stride + m0 + 8 * word;
+        if (8 * word + 8 <= m_have) {
+            store_row8(to, v);
+        } else {
+            for (uint32_t e = 0; 8 * word + e < m_have; ++e)
+                store<uint16_t>(to + e, static_cast<uint16_t>(v[e / 2] >> (16 * (e % 2))));
+        }
+    }
+}
+
+}  // namespace esmm

@@ -91,6 +91,31 @@ class EsKvAttend(ctypes.Structure):
                 ("max_rows", _u32), ("max_length", _u32), ("scale", _f32), ("cap", _f32)]
 
 
+class EsHeadScore(ctypes.Structure):
+    _fields_ = [("x", _vp), ("weight", _vp), ("x_stride", _u64), ("w_stride", _u64),
+                ("ids", _vp), ("teacher", _vp), ("loss", _vp), ("logp", _vp), ("lse", _vp),
+                ("status", _vp), ("workspace", _vp), ("workspace_bytes", _u64), ("rows", _u32),
+                ("vocab", _u32), ("hidden", _u32), ("entries", _u32), ("scale", _f32),
+                ("reserved", _u32)]
+
+
+class EsHeadGradient(ctypes.Structure):
+    _fields_ = [("x", _vp), ("weight", _vp), ("x_stride", _u64), ("w_stride", _u64),
+                ("ids", _vp), ("teacher", _vp), ("logp", _vp), ("lse", _vp), ("grad", _vp),
+                ("d_x", _vp), ("d_weight", _vp), ("dx_stride", _u64), ("dw_stride", _u64),
+                ("status", _vp), ("workspace", _vp), ("workspace_bytes", _u64), ("rows", _u32),
+                ("vocab", _u32), ("hidden", _u32), ("entries", _u32), ("scale", _f32),
+                ("reserved", _u32)]
+
+
+class EsAdapt(ctypes.Structure):
+    _fields_ = [("x", _vp), ("weight", _vp), ("out", _vp), ("x_stride", _u64),
+                ("w_stride", _u64), ("out_stride", _u64), ("a", _vp), ("b", _vp),
+                ("scales", _vp), ("index", _vp), ("status", _vp), ("workspace", _vp),
+                ("workspace_bytes", _u64), ("rows", _u32), ("inner", _u32), ("outer", _u32),
+                ("members", _u32), ("rank", _u32), ("reserved", _u32)]
+
+
 SIGNATURES = {
     "es_plan_create": (ctypes.c_int, [ctypes.POINTER(EsTensor), _u32, ctypes.POINTER(_vp)]),
     "es_plan_create_blocks": (ctypes.c_int, [ctypes.POINTER(EsBlock), _u32,
@@ -144,6 +169,12 @@ SIGNATURES = {
     "es_kv_append": (ctypes.c_int, [_vp, _vp, _vp]),
     "es_kv_read": (ctypes.c_int, [_vp, _vp, _u32, _vp, _u64, _vp, _u64, _vp, _vp]),
     "es_kv_attend": (ctypes.c_int, [_vp, _vp, _vp]),
+    "es_head_score_bytes": (_u64, [_vp]),
+    "es_head_score": (ctypes.c_int, [_vp, _vp]),
+    "es_head_gradient_bytes": (_u64, [_vp]),
+    "es_head_gradient": (ctypes.c_int, [_vp, _vp]),
+    "es_adapt_bytes": (_u64, [_vp]),
+    "es_adapt_project": (ctypes.c_int, [_vp, _vp]),
     "es_strerror": (ctypes.c_char_p, [ctypes.c_int]),
     "es_last_error": (ctypes.c_char_p, []),
 }

@@ -1,0 +1,414 @@
+"""Scores at a head and divergences from a teacher's top logits, with their
+gradients (es_head_*), against the fp64 oracle.
+
+Tolerances are the kernels' roundings.  E = 2^-24 is half a binary32 step.  A logit
+is a binary32 sum of H exact products: off by at most H steps of 2 E (a matrix unit's
+sum may be cut instead of rounded) of the sum S of their sizes; Z below.  A
+normaliser is off by its logits' error, by exp2's (2 E of a value below
+2^6 and the function's own 2 E, all relative to the sum) and by the sum's over a
+tile's 64 values and 6 joins, and its logarithm by 4 E of it.  A log-probability
+takes two logits.  bf16's rounding is off by at most U = 2^-8 of a value.  Gradients:
+one rounding of each logit's gradient d (U sum |d w|), its binary32 errors (that of
+exp(z - lse), twice a logit's), and one of the result.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import head as oh
+from paper_2608_17310_amd import esopt
+from paper_2608_17310_amd.head import ES_HEAD_BAD_ID, Head
+
+pytestmark = pytest.mark.gpu
+
+E = 2.0 ** -24
+U = 2.0 ** -8
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    torch.cuda.set_device(0)
+
+
+def f64(t):
+    return t.detach().float().cpu().numpy().astype(np.float64)
+
+
+def mat(rng, rows, width, std=1.0, stride=None, at=0):
+    """A bf16 matrix of `rows` rows, `stride` elements apart, `at` elements into its memory."""
+    stride = width if stride is None else stride
+    room = torch.full((at + rows * stride + 8,), float("nan"), dtype=torch.bfloat16, device="cuda")
+    t = room[at:at + rows * stride].view(rows, stride)[:, :width]
+    t.copy_(torch.from_numpy((rng.standard_normal((rows, width)) * std).astype(np.float32)))
+    return t
+
+
+def dev(x, dtype):
+    return torch.from_numpy(np.ascontiguousarray(x)).to(dtype).cuda()
+
+
+def slack(x, w, scale):
+    """The error of a row's logits, and of its normaliser beside theirs."""
+    s = (np.abs(x) @ np.abs(w).T).max(1) * abs(scale)
+    z = 2 * E * x.shape[1] * s + 4 * E * s
+    return z, 2 * E * 64 + 100 * E + 8 * E * s
+
+
+def make(rng, rows, vocab, hidden, entries=None, masked=0.2, std=None, **kw):
+    x = mat(rng, rows, hidden, **kw)
+    w = mat(rng, vocab, hidden, (3.0 if std is None else std) / np.sqrt(hidden), **kw)
+    k = entries or 1
+    ids = rng.integers(0, vocab, (rows, k))
+    if entries:
+        ids[rng.random((rows, k)) < 0.25] = -1
+    ids[rng.random(rows) < masked] = -100
+    ids[rows // 2] = rng.integers(0, vocab, k)
+    teacher = rng.standard_normal((rows, k)).astype(np.float32) * 3 if entries else None
+    grad = rng.standard_normal(rows).astype(np.float32)
+    return x, w, ids, teacher, grad
+
+
+def check(x, w, ids, teacher, grad, scale, status=None):
+    """A call of each direction against the oracle; its outputs."""
+    head = Head(w)
+    X, W = np.where((ids >= 0).any(1)[:, None], f64(x), 0.0), f64(w)
+    T = None if teacher is None else teacher.astype(np.float64)
+    d_ids = dev(ids if teacher is not None else ids[:, 0], torch.int64)
+    d_grad = dev(grad, torch.float32)
+    s = float(np.float32(scale))
+    loss, logp, lse = oh.score(X, W, ids, s, T)
+    if teacher is None:
+        g_logp, g_lse = head.score(x, d_ids, scale=scale, status=status)
+        outs = (g_logp, g_lse)
+        dx, dw = head.score_gradient(x, d_ids, g_logp, g_lse, d_grad, scale=scale)
+    else:
+        d_t = dev(teacher, torch.float32)
+        g_loss, g_logp, g_lse = head.distill(x, d_ids, d_t, scale=scale, status=status)
+        outs = (g_loss, g_logp, g_lse)
+        dx, dw = head.distill_gradient(x, d_ids, d_t, g_logp, g_lse, d_grad, scale=scale)
+    z, norm = slack(X, W, s)
+    live, void = oh.kinds(ids, len(W))
+    np.testing.assert_array_equal(np.isnan(f64(g_lse)), void)
+    ok = ~void
+    assert np.all(np.abs(f64(g_lse) - lse)[ok] <= (z + norm + 4 * E * np.abs(lse))[ok])
+    got = f64(g_logp).reshape(logp.shape)
+    tol = (2 * z + norm)[:, None] + 8 * E * (np.abs(logp) + np.abs(lse)[:, None])
+    assert np.all(np.abs(got - logp)[ok] <= tol[ok])
+    if teacher is not None:
+        q, log_q = oh.weights(ids, T, s)
+        # q's own error: its exponent's, of a product rounded once, and its sum's
+        q_err = q * (4 * E * (np.abs(np.where(q > 0, T, 0.0)) * s + 64))
+        some = np.where(q > 0, np.abs(log_q - logp), 0.0)
+        tol = (q * (tol + 16 * E * (1 + np.abs(log_q)))).sum(1) + (q_err * (some + 1)).sum(1) + \
+            300 * E * (q * some).sum(1)
+        assert np.all(np.abs(f64(g_loss) - loss)[ok] <= tol[ok] + 1e-37)
+    d = oh.logit_gradients(X, W, ids, grad, s, T)
+    want_x, want_w = oh.gradients(X, W, ids, grad, s, T)
+    # of f p: both logits' and the normaliser's errors, and a few roundings
+    f = np.abs(np.where(live, grad, 0.0) * s)[:, None]
+    p_err = (2 * z + norm + 32 * E)[:, None] + 4 * E * np.abs(lse)[:, None]
+    p_err = np.where(ok[:, None], p_err, 0.0)
+    q, _ = oh.weights(ids, T, s)
+    full = np.zeros_like(d)
+    for r in range(len(ids)):
+        if live[r]:
+            for e in np.flatnonzero(ids[r] >= 0):
+                full[r, ids[r, e]] += q[r, e]
+    # (what is below binary32's smallest normal value, 2^-126, may be zero)
+    d_err = U * np.abs(d) + (np.abs(d) + 2 * f * full) * (p_err + 64 * E * 3) + 2.0 ** -126
+    k = 2 * E * (len(W) + 64)
+    tol = U * np.abs(want_x) + (d_err + k * np.abs(d)) @ np.abs(W) + 2.0 ** -126
+    np.testing.assert_array_equal(np.isnan(f64(dx)).any(1), void)
+    assert np.all(np.abs(f64(dx) - want_x)[ok] <= tol[ok] * (1 + U))
+    k = 2 * E * (len(X) + 64)
+    tol = U * np.abs(want_w) + (d_err + k * np.abs(d)).T @ np.abs(X) + 2.0 ** -126
+    assert np.all(np.abs(f64(dw) - want_w) <= tol * (1 + U))
+    return outs + (dx, dw)
+
+
+SIZES = [(1, 97, 128), (2, 1, 8), (7, 500, 64), (33, 256, 72), (64, 513, 104), (65, 1031, 1000),
+         (256, 300, 320), (257, 1030, 192), (300, 5003, 64), (130, 777, 2056)]
+
+
+@pytest.mark.parametrize("rows,vocab,hidden", SIZES)
+@pytest.mark.parametrize("entries", [None, 1, 20])
+def test_scores_and_gradients(rows, vocab, hidden, entries):
+    rng = np.random.default_rng([rows, vocab, hidden, entries or 0])
+    check(*make(rng, rows, vocab, hidden, entries), float(rng.choice([1.0, 0.5, 1.7])))
+
+
+@pytest.mark.parametrize("rows,vocab,hidden", [(1, 97, 5), (3, 50, 1), (40, 300, 63), (70, 600, 1001),
+                                               (259, 511, 130)])
+@pytest.mark.parametrize("entries", [None, 7])
+def test_odd_widths_strides_and_alignments(rows, vocab, hidden, entries):
+    """Rows that start anywhere, between NaN that no row holds."""
+    rng = np.random.default_rng([hidden, entries or 0])
+    args = make(rng, rows, vocab, hidden, entries, stride=hidden + int(rng.integers(1, 9)),
+                at=int(rng.integers(1, 8)))
+    check(*args, 1.0)
+
+
+@pytest.mark.parametrize("rows", [3, 64, 65, 300])
+def test_aligned_rows_between_others(rows):
+    rng = np.random.default_rng(rows)
+    check(*make(rng, rows, 400, 128, None, stride=144, at=8), 1.0)
+    check(*make(rng, rows, 400, 128, 5, stride=144, at=8), 1.0)
+
+
+@pytest.mark.parametrize("rows", [5, 64, 100, 600])
+@pytest.mark.parametrize("entries", [None, 6])
+def test_rows_without_ids_reach_nothing(rows, entries):
+    """Dead rows hold NaN and infinities: results zero, gradients zero, and no
+    other row's or the head's differ by a bit from those without them."""
+    rng = np.random.default_rng([rows, entries or 0])
+    x, w, ids, teacher, grad = make(rng, rows, 700, 136, entries, masked=0.6)
+    dead = (ids < 0).all(1)
+    assert dead.any() and not dead.all()
+    outs = check(x, w, ids, teacher, grad, 1.0)
+    for bad in (float("nan"), float("inf")):
+        y = x.clone()
+        y[dev(dead, torch.bool)] = bad
+        g = grad.copy()
+        g[dead] = bad
+        t = None if teacher is None else np.where(ids < 0, np.float32(bad), teacher)
+        again = check(y, w, ids, t, g, 1.0)
+        for a, b in zip(outs, again):
+            assert torch.equal(a, b)
+    for out in outs[:-1]:
+        assert not out[dev(dead, torch.bool)].any()
+
+
+@pytest.mark.parametrize("rows", [1, 64, 129])
+@pytest.mark.parametrize("entries", [None, 3])
+def test_no_row_has_an_id(rows, entries):
+    rng = np.random.default_rng(rows)
+    x, w, ids, teacher, grad = make(rng, rows, 333, 64, entries)
+    ids[:] = -1
+    for out in check(x, w, ids, teacher, grad, 1.0):
+        assert not out.any()
+
+
+@pytest.mark.parametrize("rows", [4, 90])
+@pytest.mark.parametrize("entries", [None, 4])
+def test_ids_past_the_vocabulary_are_reported(rows, entries):
+    rng = np.random.default_rng(rows)
+    x, w, ids, teacher, grad = make(rng, rows, 100, 64, entries)
+    ids[1, -1], ids[3, 0] = 100, 1 << 40
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    check(x, w, ids, teacher, grad, 1.0, status=status)
+    assert status.item() == ES_HEAD_BAD_ID
+    status.zero_()
+    ids[ids >= 100] = 99
+    check(x, w, ids, teacher, grad, 1.0, status=status)
+    assert status.item() == 0
+
+
+def test_a_teacher_that_leaves_nothing_and_repeated_ids():
+    rng = np.random.default_rng(5)
+    x, w, ids, teacher, grad = make(rng, 70, 200, 96, 9, masked=0.0)
+    teacher[3] = -np.inf
+    teacher[4, 2:] = -np.inf
+    ids[6] = 17
+    ids[7, :4] = ids[7, 5]
+    loss, logp, lse, dx, dw = check(x, w, ids, teacher, grad, 1.0)
+    assert loss[3].item() == 0.0 and not dx[3].any() and lse[3].item() != 0.0
+    assert torch.equal(logp[6], logp[6, :1].expand(9))
+
+
+def test_a_student_that_is_the_teacher():
+    """Where every id is given and the teacher's logits are the student's, the
+    divergence is a sum of terms that cancel and its gradient nearly nothing."""
+    rng = np.random.default_rng(6)
+    x, w, _, _, grad = make(rng, 80, 200, 64)
+    ids = np.stack([rng.permutation(200) for _ in range(80)])
+    z = f64(x) @ f64(w).T
+    teacher = np.take_along_axis(z, ids, 1).astype(np.float32)
+    loss, *_ = check(x, w, ids, teacher, grad, 1.0)
+    assert loss.abs().max().item() <= 1e-5
+
+
+@pytest.mark.parametrize("rows", [3, 100])
+def test_wide_logits(rows):
+    """Logits of some thousands: one token has all of the weight, or none."""
+    rng = np.random.default_rng(7)
+    x, w, ids, teacher, grad = make(rng, rows, 500, 64, None, std=3000.0)
+    z = f64(x) @ f64(w).T
+    ids[:rows // 2, 0] = z.argmax(1)[:rows // 2]
+    logp, lse, *_ = check(x, w, ids, teacher, grad, 1.0)
+    assert torch.isfinite(logp).all() and torch.isfinite(lse).all()
+
+
+def test_rows_that_are_not_finite_are_nan_alone():
+    rng = np.random.default_rng(8)
+    x, w, ids, _, _ = make(rng, 300, 500, 64, masked=0.0)
+    t = dev(ids[:, 0], torch.int64)
+    want = Head(w).score(x, t)
+    x[5, 3], x[299, 0] = float("nan"), float("inf")
+    got = Head(w).score(x, t)
+    keep = torch.ones(300, dtype=torch.bool, device="cuda")
+    keep[[5, 299]] = False
+    for a, b in zip(got, want):
+        assert torch.isnan(a[~keep]).all() and torch.equal(a[keep], b[keep])
+
+
+@pytest.mark.parametrize("entries", [None, 5])
+def test_gradients_against_differences(entries):
+    """The gradient along a direction against the outputs' difference over it, both
+    from the kernels: the gradient's roundings (U of sum |d w| |v|) and the loss's
+    binary32 errors over the step."""
+    rng = np.random.default_rng(9)
+    x, w, ids, teacher, grad = make(rng, 40, 300, 64, entries, masked=0.1)
+    head = Head(w)
+    d_ids = dev(ids if entries else ids[:, 0], torch.int64)
+    t = dev(teacher, torch.float32) if entries else None
+    g = dev(grad, torch.float32)
+
+    def out(h, y):
+        if entries:
+            loss, logp, lse = h.distill(y, d_ids, t)
+            return loss, logp, lse
+        logp, lse = h.score(y, d_ids)
+        return logp, logp, lse
+
+    o, logp, lse = out(head, x)
+    args = (d_ids, t, logp, lse, g) if entries else (d_ids, logp, lse, g)
+    dx, dw = (head.distill_gradient if entries else head.score_gradient)(x, *args)
+    h = 2.0 ** -4                                          # steps that bf16 inputs take exactly
+    for _ in range(3):
+        for at, grads in ((x, dx), (w, dw)):
+            v = torch.from_numpy(rng.integers(-1, 2, tuple(at.shape)).astype(np.float32)).cuda()
+            step = h * at.abs().max().item() * 2.0 ** -3
+            up, down = (at.float() + step * v).bfloat16(), (at.float() - step * v).bfloat16()
+            real = (up.double() - down.double())
+            if at is x:
+                hi, lo = out(head, up)[0], out(head, down)[0]
+            else:
+                hi, lo = out(Head(up), x)[0], out(Head(down), x)[0]
+            diff = ((hi.double() - lo.double()) * g.double()).sum().item()
+            got = (grads.double() * real).sum().item()
+            scale = (grads.double().abs() * real.abs()).sum().item()
+            # second differences cancel; the third's share of a step of a 50th of the logits' spread
+            assert abs(diff - got) <= (2 * U + 0.02) * scale
+
+
+def test_only_the_wanted_gradients():
+    rng = np.random.default_rng(10)
+    x, w, ids, _, grad = make(rng, 50, 400, 64)
+    head, t, g = Head(w), dev(ids[:, 0], torch.int64), dev(grad, torch.float32)
+    logp, lse = head.score(x, t)
+    dx, dw = head.score_gradient(x, t, logp, lse, g)
+    assert head.score_gradient(x, t, logp, lse, g, weight_grad=False)[1] is None
+    assert torch.equal(head.score_gradient(x, t, logp, lse, g, weight_grad=False)[0], dx)
+    only = head.score_gradient(x, t, logp, lse, g, hidden_grad=False)
+    assert only[0] is None and torch.equal(only[1], dw)
+    assert head.score_gradient(x, t, logp, lse, g, hidden_grad=False, weight_grad=False) == (None, None)
+
+
+def test_no_rows():
+    w = torch.randn(100, 64, device="cuda").bfloat16()
+    x, t = w[:0], torch.zeros(0, dtype=torch.int64, device="cuda")
+    head = Head(w)
+    logp, lse = head.score(x, t)
+    assert logp.shape == lse.shape == (0,)
+    e = torch.zeros(0, device="cuda")
+    dx, dw = head.score_gradient(x, t, logp, lse, e)
+    assert dx.shape == (0, 64) and dw.shape == w.shape and not dw.any()
+    loss, logp, lse = head.distill(x, t.view(0, 1), e.view(0, 1))
+    assert loss.shape == (0,) and logp.shape == (0, 1)
+
+
+def test_the_same_bits_every_time_and_under_a_graph():
+    """Replays among eager calls of the same and of other sizes, new inputs in place."""
+    rng = np.random.default_rng(11)
+    x, w, ids, teacher, grad = make(rng, 130, 900, 192, 6)
+    head = Head(w)
+    t, q, g = dev(ids, torch.int64), dev(teacher, torch.float32), dev(grad, torch.float32)
+
+    def step():
+        loss, logp, lse = head.distill(x, t, q, scale=0.5)
+        return (loss, logp, lse) + head.distill_gradient(x, t, q, logp, lse, g, scale=0.5)
+
+    want = [o.clone() for o in step()]
+    for _ in range(3):
+        for a, b in zip(step(), want):
+            assert torch.equal(a, b)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = step()
+    for round_ in range(4):
+        y, _, ids2, teacher2, grad2 = make(rng, 130, 900, 192, 6, masked=0.3 * round_)
+        x.copy_(y)
+        t.copy_(dev(ids2, torch.int64))
+        q.copy_(dev(teacher2, torch.float32))
+        g.copy_(dev(grad2, torch.float32))
+        want = [o.clone() for o in step()]
+        for o in outs:
+            o.fill_(7.0)
+        Head(w[:77]).score(x[:9], t[:9, 0].clamp(max=76))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(outs, want):
+            assert torch.equal(a, b)
+
+
+def test_calls_on_two_streams_at_once():
+    """A workspace each: calls on one head overlap without a trace."""
+    rng = np.random.default_rng(12)
+    sets = [make(rng, n, 3000, 256, None) for n in (70, 300)]
+    w = sets[0][1]
+    head = Head(w)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    args = [(x, dev(ids[:, 0], torch.int64), dev(grad, torch.float32)) for x, _, ids, _, grad in sets]
+    want = []
+    for x, t, g in args:
+        logp, lse = head.score(x, t)
+        want.append((logp, lse) + head.score_gradient(x, t, logp, lse, g))
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(5):
+        for i, (x, t, g) in enumerate(args):
+            logp, lse = head.score(x, t, stream=streams[i])
+            grads = head.score_gradient(x, t, logp, lse, g, stream=streams[i])
+            got[i].append((logp, lse) + grads)
+    torch.cuda.synchronize()
+    for i in range(2):
+        for outs in got[i]:
+            for a, b in zip(outs, want[i]):
+                assert torch.equal(a, b)
+
+
+def test_refusals():
+    w = torch.zeros(100, 64, dtype=torch.bfloat16, device="cuda")
+    x = torch.zeros(4, 64, dtype=torch.bfloat16, device="cuda")
+    t = torch.zeros(4, dtype=torch.int64, device="cuda")
+    head = Head(w)
+    f = torch.zeros(4, device="cuda")
+    for call in (lambda: Head(w.float()), lambda: Head(w.cpu()), lambda: Head(w.t()),
+                 lambda: Head(w[:0]), lambda: Head(w[None]), lambda: Head(w[:1].expand(5, 64)),
+                 lambda: head.score(x.float(), t), lambda: head.score(x[:, :32], t),
+                 lambda: head.score(x, t.int()), lambda: head.score(x, t[:3]),
+                 lambda: head.score(x, t[:, None]), lambda: head.score(x, t.cpu()),
+                 lambda: head.score(x.cpu(), t), lambda: head.score(x[0], t[:1]),
+                 lambda: head.score(x[:, ::2], t),
+                 lambda: head.distill(x, t, f), lambda: head.distill(x, t[:, None], f),
+                 lambda: head.distill(x, t[:, None], f[:, None].double()),
+                 lambda: head.score_gradient(x, t, f[:3], f, f),
+                 lambda: head.score_gradient(x, t, f, f, f.double()),
+                 lambda: head.score(x, t, status=torch.zeros(1, device="cuda"))):
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: head.score(x, t, scale=float("nan")),
+                 lambda: head.score(x, t, scale=float("inf")),
+                 lambda: head.distill(x, t[:, None].expand(4, 257).contiguous(),
+                                      torch.zeros(4, 257, device="cuda")),
+                 lambda: head.distill(x, t[:, None][:, :0].contiguous(), f[:, None][:, :0].contiguous())):
+        with pytest.raises(esopt.EsError):
+            call()
