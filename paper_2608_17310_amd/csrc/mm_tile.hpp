@@ -227,25 +227,44 @@ __device__ __forceinline__ void product_tile(const Product& p, uint32_t m0, uint
     ra.init(128 * (wave & 1), lane);
     rb.init(64 * (wave >> 1), lane);
     const uint32_t lds_at = uniform(lds_address(lds));
-    for (uint32_t k = k0; k < k_end; k += kDepth) {
-        __syncthreads();
-        sa.issue(lds_at, k_end - k, p.a, wave, lane);
+    uint32_t buf = 0;                                    // of the stage in use, 0 or 2 sides
+    auto issue = [&](uint32_t k, uint32_t at) {
+        sa.issue(lds_at + at, k_end - k, p.a, wave, lane);
         // (the right side is stored to a multiple of 64)
-        sb.issue(lds_at + kSideBytes, kDepth, p.b, wave, lane);
-        wait_staged();
-        __syncthreads();
+        sb.issue(lds_at + at + kSideBytes, kDepth, p.b, wave, lane);
+    };
+    bf16x8_t a[2][4], b[2][2];
+    auto read = [&](int s) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) b[s & 1][j] = rb.read(lds + buf + kSideBytes, s, j);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a[s & 1][i] = ra.read(lds + buf, s, i);
+    };
+    issue(k0, 0);
+    wait_staged();
+    __builtin_amdgcn_s_barrier();
+    if (k0 + kDepth < k_end) issue(k0 + kDepth, 2 * kSideBytes);
+    read(0);
+    for (uint32_t k = k0; k < k_end; k += kDepth) {
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
-            bf16x8_t a[4], b[2];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) a[i] = ra.read(lds, s, i);
-#pragma unroll
-            for (int j = 0; j < 2; ++j) b[j] = rb.read(lds + kSideBytes, s, j);
+            // the next step's operands are read behind this one's products
+            if (s < 3) {
+                read(s + 1);
+            } else if (k + kDepth < k_end) {
+                // all of the stage is in registers, and the next has landed
+                wait_staged();
+                __builtin_amdgcn_s_barrier();
+                if (k + 2 * kDepth < k_end) issue(k + 2 * kDepth, buf);
+                buf ^= 2 * kSideBytes;
+                read(0);
+            }
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int j = 0; j < 2; ++j)
-                    c.x[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[i], b[j], c.x[i][j], 0, 0, 0);
+                    c.x[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[s & 1][i], b[s & 1][j],
+                                                                        c.x[i][j], 0, 0, 0);
         }
     }
 }
