@@ -207,6 +207,11 @@ struct Tile {
     f32x16_t x[4][2];
 };
 
+template <int n>
+struct Count {
+    static constexpr int value = n;
+};
+
 template <bool kWideA, bool kWideB>
 __device__ __forceinline__ void product_tile(const Product& p, uint32_t m0, uint32_t n0, uint32_t k0,
                                              uint32_t k_end, uint8_t* lds, Tile& c) {
@@ -240,33 +245,53 @@ __device__ __forceinline__ void product_tile(const Product& p, uint32_t m0, uint
 #pragma unroll
         for (int i = 0; i < 4; ++i) a[s & 1][i] = ra.read(lds + buf, s, i);
     };
+    auto multiply = [&](int s, int from, int to) {
+#pragma unroll
+        for (int i = from; i < to; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                c.x[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[s & 1][i], b[s & 1][j], c.x[i][j],
+                                                                    0, 0, 0);
+    };
+    // reads go out one or two to a product, from the first on
+    constexpr int kReads = (kWideA ? 8 : 4) + (kWideB ? 4 : 2), kMatrix = 0x8, kDsRead = 0x100;
+    auto interleave = [&](auto products) {
+        constexpr int n = decltype(products)::value, each = (kReads + n - 1) / n;
+#pragma unroll
+        for (int x = 0; x < n; ++x) {
+            if (x * each < kReads) __builtin_amdgcn_sched_group_barrier(kDsRead, each, 0);
+            __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 0);
+        }
+    };
+    auto steps = [&](int from, int to) {                 // each with the reads of the next
+#pragma unroll
+        for (int s = from; s < to; ++s) {
+            read(s + 1);
+            multiply(s, 0, 4);
+            interleave(Count<8>{});
+        }
+    };
     issue(k0, 0);
     wait_staged();
     __builtin_amdgcn_s_barrier();
     if (k0 + kDepth < k_end) issue(k0 + kDepth, 2 * kSideBytes);
     read(0);
-    for (uint32_t k = k0; k < k_end; k += kDepth) {
-#pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            // the next step's operands are read behind this one's products
-            if (s < 3) {
-                read(s + 1);
-            } else if (k + kDepth < k_end) {
-                // all of the stage is in registers, and the next has landed
-                wait_staged();
-                __builtin_amdgcn_s_barrier();
-                if (k + 2 * kDepth < k_end) issue(k + 2 * kDepth, buf);
-                buf ^= 2 * kSideBytes;
-                read(0);
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-                    c.x[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[s & 1][i], b[s & 1][j],
-                                                                        c.x[i][j], 0, 0, 0);
-        }
+    uint32_t k = k0;
+    for (; k + kDepth < k_end; k += kDepth) {
+        steps(0, 3);
+        // all of the stage is in registers, and the next has landed
+        wait_staged();
+        __builtin_amdgcn_s_barrier();
+        const uint32_t old = buf;
+        buf ^= 2 * kSideBytes;
+        read(0);
+        multiply(3, 0, 2);
+        interleave(Count<4>{});
+        if (k + 2 * kDepth < k_end) issue(k + 2 * kDepth, old);
+        multiply(3, 2, 4);
     }
+    steps(0, 3);
+    multiply(3, 0, 4);
 }
 
 // f(i, j, y, m, n): words of four results, registers 4 y .. 4 y + 3 of block (i, j), rows m ..
