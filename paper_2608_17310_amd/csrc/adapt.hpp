@@ -4,6 +4,7 @@
 // the large one then adds B_i u to its tiles before they are rounded.
 #pragma once
 
+#include "few.hpp"
 #include "mm_tile.hpp"
 
 namespace esadapt {
@@ -72,6 +73,33 @@ __global__ __launch_bounds__(kThreads) void es_adapt_small_kernel(SmallArgs a) {
             }
         }
     }
+}
+
+// u of few rows: a wave for each of its elements.
+__global__ __launch_bounds__(256) void es_adapt_few_small_kernel(SmallArgs a) {
+    const uint32_t lane = threadIdx.x & 63, n = blockIdx.x;
+    const uint32_t r = uniform(blockIdx.y * 4 + (threadIdx.x >> 6));
+    const int32_t member = a.index[n];
+    if (member >= int32_t(a.members) && a.status != nullptr && blockIdx.y == 0 && threadIdx.x == 0)
+        atomicOr(a.status, ES_ADAPT_BAD_INDEX);
+    if (member < 0 || member >= int32_t(a.members) || r >= a.rank) return;
+    const uint16_t* const x = a.x + uint64_t(n) * a.x_stride;
+    const uint16_t* const row = a.a + (uint64_t(member) * a.rank + r) * a.inner;
+    float sum[8] = {};
+#pragma unroll 4
+    for (uint32_t k = 8 * lane; k < a.inner; k += 512) {
+        float u[8], v[8];
+        eskv::unpack8(load<u32x4_t>(row + k), u);
+        eskv::unpack8(load_row8(x + k), v);
+#pragma unroll
+        for (int y = 0; y < 8; ++y) sum[y] = __builtin_fmaf(u[y], v[y], sum[y]);
+    }
+    float all = ((sum[0] + sum[1]) + (sum[2] + sum[3])) + ((sum[4] + sum[5]) + (sum[6] + sum[7]));
+#pragma unroll
+    for (int d = 32; d >= 1; d /= 2) all += __shfl_xor(all, d);
+    if (lane == 0)
+        a.u[uint64_t(n) * a.rank + r] = static_cast<uint16_t>(
+            pack_bf16((a.scales != nullptr ? a.scales[member] : 1.0f) * all, 0.0f));
 }
 
 struct AddArgs {
@@ -153,6 +181,58 @@ __global__ __launch_bounds__(kThreads, 2) void es_adapt_tile_kernel(TileArgs a) 
     store_rows(lds, a.out, a.out_stride, m0, a.add.outer - m0, [&](uint32_t n) {
         return n0 + n < a.add.rows ? int64_t(n0 + n) : int64_t(-1);
     });
+}
+
+struct FewArgs {
+    esfew::FewArgs f;
+    AddArgs add;
+    uint16_t* out;
+    uint64_t out_stride;
+};
+
+// Up to 64 rows: the waves' sums of a block meet in LDS, where each result takes its
+// own member's B u.
+template <int kBlocks, int kCols>
+__global__ __launch_bounds__(512, kCols == 1 ? 4 : 2) void es_adapt_few_kernel(FewArgs a) {
+    using namespace esfew;
+    constexpr uint32_t kEach = kBlocks * kCols * 256;
+    __shared__ __attribute__((aligned(16))) float sums[kWaves][kEach];
+    const uint32_t lane = threadIdx.x & 63;
+    const Part<kBlocks> at(a.f);
+    Few<kBlocks, kCols> t;
+    t.run(a.f, at.row0, at.k0, at.k1);
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b)      // [column block][row of x][row of the matrix]
+#pragma unroll
+        for (int j = 0; j < kCols; ++j)
+            *reinterpret_cast<f32x4_t*>(&sums[at.wave][(j * 16 + (lane & 15)) * (16 * kBlocks) + 16 * b +
+                                                       4 * (lane >> 4)]) = t.c[b][j];
+    __syncthreads();
+    const uint32_t groups = kWaves / a.f.slices;
+    for (uint32_t e = threadIdx.x; e < groups * kEach; e += 64 * kWaves) {
+        const uint32_t g = e / kEach, y = e % kEach;
+        const uint32_t n = y / (16 * kBlocks), i = y % (16 * kBlocks);
+        const uint32_t m = (blockIdx.x * groups + g) * 16 * kBlocks + i;
+        if (n >= a.f.rows || m >= a.f.w_rows) continue;
+        float sum = 0.0f;
+        for (uint32_t w = 0; w < a.f.slices; ++w) sum += sums[g * a.f.slices + w][y];
+        const int32_t member = a.add.index[n];
+        if (member >= int32_t(a.add.members)) sum = eskv::nan();
+        if (member >= 0 && member < int32_t(a.add.members)) {
+            const uint16_t* const b = a.add.b + (uint64_t(member) * a.add.outer + m) * a.add.rank;
+            const uint16_t* const u = a.add.u + uint64_t(n) * a.add.rank;
+            float low = 0.0f;
+            for (uint32_t r = 0; r < a.add.rank; r += 8) {
+                float p[8], q[8];
+                eskv::unpack8(load<u32x4_t>(b + r), p);
+                eskv::unpack8(load<u32x4_t>(u + r), q);
+#pragma unroll
+                for (int z = 0; z < 8; ++z) low = __builtin_fmaf(p[z], q[z], low);
+            }
+            sum += low;
+        }
+        store<uint16_t>(a.out + uint64_t(n) * a.out_stride + m, static_cast<uint16_t>(pack_bf16(sum, 0.0f)));
+    }
 }
 
 }  // namespace esadapt

@@ -123,14 +123,38 @@ struct Lists {
     Side wide() const { return Side{x, padded, padded}; }
 };
 
+// How few rows' products are divided: blocks of 16 rows of the matrix a wave, and
+// the waves that share a block's sum.
+struct FewPlan {
+    uint32_t cols, slices, groups;
+    FewPlan(uint32_t rows, uint32_t w_rows, uint32_t width, uint32_t blocks) {
+        cols = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+        slices = 1;
+        while (slices < esfew::kWaves && width / (2 * slices) >= 32 * esfew::kSteps) slices *= 2;
+        const uint32_t per = esfew::kWaves / slices * 16 * blocks;
+        groups = (w_rows + per - 1) / per;
+    }
+};
+
 struct ScorePlan {
+    bool few;
     HeadRows head;
     Lists lists;
+    FewPlan division;
     uint32_t tiles;
     float* parts;
     uint16_t* w;
     ScorePlan(Room& room, const es_head_score_t& x)
-        : head(x.weight, x.w_stride, x.vocab, x.hidden, 0), lists(room, x.rows, x.hidden) {
+        : few(x.rows <= esfew::kRows),
+          head(x.weight, x.w_stride, x.vocab, x.hidden, 0),
+          lists(room, few ? 0 : x.rows, x.hidden),
+          division(x.rows, x.vocab, x.hidden, 2) {
+        if (few) {
+            tiles = division.groups;
+            parts = room.take<float>(uint64_t(2) * x.rows * tiles);
+            w = nullptr;
+            return;
+        }
         tiles = (x.vocab + kTile - 1) / kTile;
         parts = room.take<float>(uint64_t(2) * lists.rows * tiles);
         w = head.copied ? room.take<uint16_t>(uint64_t(head.piece) * head.padded) : nullptr;
@@ -218,6 +242,20 @@ Side head_side(const HeadRows& h, const void* w, uint64_t stride, uint16_t* room
     return Side{room, h.padded, have};
 }
 
+esfew::FewArgs few_args(const FewPlan& d, const void* w, uint64_t w_stride, uint32_t w_rows, const void* x,
+                        uint64_t x_stride, uint32_t rows, uint32_t width) {
+    esfew::FewArgs f{};
+    f.w = static_cast<const uint16_t*>(w);
+    f.x = static_cast<const uint16_t*>(x);
+    f.w_stride = w_stride;
+    f.x_stride = x_stride;
+    f.w_rows = w_rows;
+    f.rows = rows;
+    f.width = width;
+    f.slices = d.slices;
+    return f;
+}
+
 }  // namespace
 
 extern "C" {
@@ -266,6 +304,37 @@ int es_head_score(const es_head_score_t* args, es_stream_t stream) try {
     ok.check(x.workspace, room.used, ": workspace");
     if (ok.rc != ES_OK) return ok.rc;
     const hipStream_t s = static_cast<hipStream_t>(stream);
+    eshead::ScoreArgs a{};
+    a.parts = plan.parts;
+    a.parts_stride = plan.tiles;
+    a.n_parts = plan.tiles;
+    a.w = static_cast<const uint16_t*>(x.weight);
+    a.w_stride = x.w_stride;
+    a.ids = x.ids;
+    a.teacher = x.teacher;
+    a.loss = x.loss;
+    a.logp = x.logp;
+    a.lse = x.lse;
+    a.status = x.status;
+    a.hidden = x.hidden;
+    a.entries = x.entries;
+    a.vocab = x.vocab;
+    a.scale = x.scale;
+    if (plan.few) {
+        eshead::FewStatsArgs f{};
+        f.f = few_args(plan.division, x.weight, x.w_stride, x.vocab, x.x, x.x_stride, x.rows, x.hidden);
+        f.parts = plan.parts;
+        f.factor = x.scale * eshead::kLog2e;
+        constexpr int b = 2;
+        const auto kernel = plan.division.cols == 1   ? eshead::es_head_few_kernel<b, 1>
+                            : plan.division.cols == 2 ? eshead::es_head_few_kernel<b, 2>
+                                                      : eshead::es_head_few_kernel<b, 4>;
+        hipLaunchKernelGGL(kernel, dim3(plan.division.groups), dim3(64 * esfew::kWaves), 0, s, f);
+        a.x = static_cast<const uint16_t*>(x.x);
+        a.x_stride = x.x_stride;
+        hipLaunchKernelGGL(eshead::es_head_score_kernel, dim3(x.rows), dim3(256), 0, s, a);
+        return launch_error("es_head_few_kernel launch");
+    }
     eshead::RowArgs rows{};
     rows.ids = x.ids;
     rows.teacher = x.teacher;
@@ -283,34 +352,20 @@ int es_head_score(const es_head_score_t* args, es_stream_t stream) try {
     for (uint32_t v0 = 0; v0 < x.vocab; v0 += plan.head.piece) {
         const uint32_t have = std::min(plan.head.piece, x.vocab - v0);
         const Side w = head_side(plan.head, x.weight, x.w_stride, plan.w, v0, have, x.hidden, s);
-        eshead::StatsArgs a{};
-        a.p = product(w, plan.lists.deep(), have, x.rows, x.hidden, plan.lists.count);
-        a.parts = plan.parts;
-        a.parts_stride = plan.tiles;
-        a.part0 = v0 / kTile;
-        a.factor = x.scale * eshead::kLog2e;
-        hipLaunchKernelGGL(eshead::es_head_stats_kernel, grid_of(a.p), dim3(kThreads), kLdsBytes, s, a);
+        eshead::StatsArgs t{};
+        t.p = product(w, plan.lists.deep(), have, x.rows, x.hidden, plan.lists.count);
+        t.parts = plan.parts;
+        t.parts_stride = plan.tiles;
+        t.part0 = v0 / kTile;
+        t.factor = x.scale * eshead::kLog2e;
+        hipLaunchKernelGGL(eshead::es_head_stats_kernel, grid_of(t.p), dim3(kThreads), kLdsBytes, s, t);
         rc = launch_error("es_head_stats_kernel launch");
         if (rc != ES_OK) return rc;
     }
-    eshead::ScoreArgs a{};
-    a.parts = plan.parts;
-    a.parts_stride = plan.tiles;
-    a.n_parts = plan.tiles;
     a.list = plan.lists.list;
     a.count = plan.lists.count;
     a.x = plan.lists.x;
     a.x_stride = plan.lists.padded;
-    a.w = static_cast<const uint16_t*>(x.weight);
-    a.w_stride = x.w_stride;
-    a.ids = x.ids;
-    a.teacher = x.teacher;
-    a.loss = x.loss;
-    a.logp = x.logp;
-    a.lse = x.lse;
-    a.hidden = x.hidden;
-    a.entries = x.entries;
-    a.scale = x.scale;
     hipLaunchKernelGGL(eshead::es_head_score_kernel, dim3(x.rows), dim3(256), 0, s, a);
     return launch_error("es_head_score_kernel launch");
 } catch (const std::bad_alloc&) {
@@ -518,12 +573,13 @@ struct AdaptPlan {
         padded = static_cast<uint32_t>(up(a.inner, kDepth));
         packed_rows = static_cast<uint32_t>(up(a.rows, kTile));
         // the products take rows that start at a word of 16 bytes and end in whole stages
-        const bool copied = padded != a.inner || !word_rows(a.x, a.x_stride, a.inner);
+        few = a.rows <= esfew::kRows;
+        const bool copied = !few && (padded != a.inner || !word_rows(a.x, a.x_stride, a.inner));
         x = nullptr;
         if (copied) x = room.take<uint16_t>(uint64_t(packed_rows) * padded);
         is_copied = copied;
     }
-    bool is_copied;
+    bool is_copied, few;
 };
 
 }  // namespace
@@ -576,6 +632,27 @@ int es_adapt_project(const es_adapt_t* args, es_stream_t stream) try {
     small.inner = x.inner;
     small.members = x.members;
     small.rank = x.rank;
+    const esadapt::AddArgs add{x.index, plan.u, static_cast<const uint16_t*>(x.b), x.rows, x.outer,
+                               x.members, x.rank};
+    if (plan.few) {
+        hipLaunchKernelGGL(esadapt::es_adapt_few_small_kernel, dim3(x.rows, (x.rank + 3) / 4), dim3(256), 0,
+                           s, small);
+        const bool narrow = x.outer <= 8192;
+        const FewPlan d(x.rows, x.outer, x.inner, narrow ? 1 : 2);
+        esadapt::FewArgs f{};
+        f.f = few_args(d, x.weight, x.w_stride, x.outer, x.x, x.x_stride, x.rows, x.inner);
+        f.add = add;
+        f.out = static_cast<uint16_t*>(x.out);
+        f.out_stride = x.out_stride;
+        const auto kernel = d.cols == 1   ? (narrow ? esadapt::es_adapt_few_kernel<1, 1>
+                                                    : esadapt::es_adapt_few_kernel<2, 1>)
+                            : d.cols == 2 ? (narrow ? esadapt::es_adapt_few_kernel<1, 2>
+                                                    : esadapt::es_adapt_few_kernel<2, 2>)
+                                          : (narrow ? esadapt::es_adapt_few_kernel<1, 4>
+                                                    : esadapt::es_adapt_few_kernel<2, 4>);
+        hipLaunchKernelGGL(kernel, dim3(d.groups), dim3(64 * esfew::kWaves), 0, s, f);
+        return launch_error("es_adapt_few_kernel launch");
+    }
     hipLaunchKernelGGL(esadapt::es_adapt_small_kernel,
                        dim3((x.rows + esadapt::kSmallRows - 1) / esadapt::kSmallRows), dim3(kThreads), 0, s,
                        small);
@@ -594,8 +671,7 @@ int es_adapt_project(const es_adapt_t* args, es_stream_t stream) try {
     }
     a.p = product(Side{static_cast<const uint16_t*>(x.weight), x.w_stride, x.outer}, rows, x.outer, x.rows,
                   x.inner, nullptr);
-    a.add = esadapt::AddArgs{x.index, plan.u, static_cast<const uint16_t*>(x.b), x.rows, x.outer,
-                             x.members, x.rank};
+    a.add = add;
     a.out = static_cast<uint16_t*>(x.out);
     a.out_stride = x.out_stride;
     hipLaunchKernelGGL(esadapt::es_adapt_tile_kernel, grid_of(a.p), dim3(kThreads), kLdsBytes, s, a);

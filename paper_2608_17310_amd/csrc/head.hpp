@@ -8,6 +8,7 @@
 // gradients f Q softmax(z) as bf16, for a piece of the vocabulary at a time.
 #pragma once
 
+#include "few.hpp"
 #include "mm_tile.hpp"
 
 namespace eshead {
@@ -228,17 +229,96 @@ __global__ __launch_bounds__(kThreads, 2) void es_head_stats_kernel(StatsArgs a)
     }
 }
 
+struct FewStatsArgs {
+    esfew::FewArgs f;
+    float* parts;                          // [rows][workgroups] pairs
+    float factor;
+};
+
+// The same of up to 64 rows, as they are: a workgroup's blocks are a part.
+template <int kBlocks, int kCols>
+__global__ __launch_bounds__(512, kCols == 1 ? 4 : 2) void es_head_few_kernel(FewStatsArgs a) {
+    using namespace esfew;
+    __shared__ __attribute__((aligned(16))) float sums[kWaves][kBlocks * kCols * 256];
+    __shared__ float pair[kWaves][16 * kCols][2];
+    const uint32_t lane = threadIdx.x & 63;
+    const Part<kBlocks> at(a.f);
+    Few<kBlocks, kCols> t;
+    t.run(a.f, at.row0, at.k0, at.k1);
+    if (a.f.slices > 1) {                  // a block's first wave adds the others'
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+            for (int j = 0; j < kCols; ++j)
+                *reinterpret_cast<f32x4_t*>(&sums[at.wave][(b * kCols + j) * 256 + 4 * lane]) = t.c[b][j];
+        __syncthreads();
+        if (at.slice == 0) {
+            for (uint32_t w = 1; w < a.f.slices; ++w)
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                    for (int j = 0; j < kCols; ++j) {
+                        const f32x4_t v = *reinterpret_cast<const f32x4_t*>(
+                            &sums[at.wave + w][(b * kCols + j) * 256 + 4 * lane]);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) t.c[b][j][e] += v[e];
+                    }
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < kCols; ++j) {
+        float top = -eskv::inf();
+        float z[kBlocks][4];
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const bool here = at.row0 + 16 * b + 4 * (lane >> 4) + e < a.f.w_rows && at.slice == 0;
+                z[b][e] = here ? t.c[b][j][e] * a.factor : -eskv::inf();
+                top = fmaxf(top, z[b][e]);
+            }
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float from = top == -eskv::inf() ? 0.0f : top;
+        float sum = 0.0f;
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f(z[b][e] - from);
+        sum += __shfl_xor(sum, 16);
+        sum += __shfl_xor(sum, 32);
+        if (lane < 16) {
+            pair[at.wave][16 * j + lane][0] = top;
+            pair[at.wave][16 * j + lane][1] = sum;
+        }
+    }
+    __syncthreads();
+    const uint32_t n = threadIdx.x;
+    if (n < 16 * kCols && n < a.f.rows) {
+        float top = -eskv::inf();
+        for (uint32_t w = 0; w < kWaves; ++w) top = fmaxf(top, pair[w][n][0]);
+        const float from = top == -eskv::inf() ? 0.0f : top;
+        float sum = 0.0f;
+        for (uint32_t w = 0; w < kWaves; ++w)
+            sum += pair[w][n][1] * __builtin_amdgcn_exp2f(pair[w][n][0] - from);
+        float* const to = a.parts + 2 * (uint64_t(n) * gridDim.x + blockIdx.x);
+        to[0] = top;
+        to[1] = sum;
+    }
+}
+
 struct ScoreArgs {
     const float* parts;
     uint64_t parts_stride;
     uint32_t n_parts;
-    const uint32_t *list, *count;
-    const uint16_t *x, *w;                 // x: the packed rows
+    const uint32_t *list, *count;          // null: all rows, which are looked at here
+    const uint16_t *x, *w;                 // x: the packed rows, or all
     uint64_t x_stride, w_stride;
     const int64_t* ids;
     const float* teacher;
     float *loss, *logp, *lse;
-    uint32_t hidden, entries;
+    uint32_t* status;
+    uint32_t hidden, entries, vocab;
     float scale;
 };
 
@@ -287,9 +367,23 @@ __device__ __forceinline__ float teacher_weight(bool here, float t, float scale,
 __global__ __launch_bounds__(256) void es_head_score_kernel(ScoreArgs a) {
     __shared__ float room[4], logits[kMaxEntries];
     const uint32_t i = blockIdx.x;
-    if (i >= *a.count) return;
+    if (a.count != nullptr && i >= *a.count) return;
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const uint32_t row = a.list[i];
+    const uint32_t row = a.list != nullptr ? a.list[i] : i;
+    if (a.list == nullptr) {
+        const int64_t id = threadIdx.x < a.entries ? a.ids[uint64_t(row) * a.entries + threadIdx.x] : -1;
+        const bool some = __syncthreads_or(id >= 0), bad = __syncthreads_or(id >= int64_t(a.vocab));
+        if (!some || bad) {                // dead or void
+            const float v = bad ? eskv::nan() : 0.0f;
+            if (threadIdx.x < a.entries) a.logp[uint64_t(row) * a.entries + threadIdx.x] = v;
+            if (threadIdx.x == 0) {
+                a.lse[row] = v;
+                if (a.loss != nullptr) a.loss[row] = v;
+                if (bad && a.status != nullptr) atomicOr(a.status, ES_HEAD_BAD_ID);
+            }
+            return;
+        }
+    }
     const float* const parts = a.parts + 2 * i * a.parts_stride;
     float top = -eskv::inf();
     for (uint32_t m = threadIdx.x; m < a.n_parts; m += 256) top = fmaxf(top, parts[2 * m]);
