@@ -6,6 +6,8 @@
 
 #include "few.hpp"
 #include "mm_tile.hpp"
+#include "ring.hpp"
+#include "stream.hpp"
 
 namespace esadapt {
 
@@ -26,51 +28,56 @@ struct SmallArgs {
 
 constexpr uint32_t kSmallRows = 32;
 
-// A workgroup takes 32 rows, and their members one by one; its waves share the sum, 16
-// of it at a time in turn.  u is rounded to bf16 (RNE) for the matrix unit: it is off by as much
-// as y's own rounding, of a smaller term.
-__global__ __launch_bounds__(kThreads) void es_adapt_small_kernel(SmallArgs a) {
-    __shared__ float part[8][32][33];      // [wave][row of A][row]
+// A workgroup takes 32 rows, and their members one by one: a product of the member's A
+// with those rows, whose sum its waves share.  u is rounded to bf16 (RNE) for the matrix
+// unit: it is off by as much as y's own rounding, of a smaller term.
+template <int kBlocks, int kParts>         // blocks of 16 of the rank, at a time
+__global__ __launch_bounds__(512, 2) void es_adapt_small_kernel(SmallArgs a) {
+    using R = esring::Ring<kBlocks, 2, kParts>;
+    constexpr uint32_t kWaves = esfew::kWaves, kEach = kBlocks * 512;
+    static_assert(kWaves * kEach * 4 <= kWaves * R::kBytes, "the waves' sums fit their rings");
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+    float* const sums = reinterpret_cast<float*>(lds);   // [wave][row][of the rank]
     const uint32_t lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
     const uint32_t n0 = blockIdx.x * kSmallRows, n = n0 + (lane & 31);
     const int32_t mine = n < a.rows ? a.index[n] : -1;
     const bool bad = mine >= int32_t(a.members);
     if (bad && wave == 0 && a.status != nullptr) atomicOr(a.status, ES_ADAPT_BAD_INDEX);
     uint32_t left = uint32_t(__ballot(mine >= 0 && !bad));
-    const uint16_t* const x = a.x + uint64_t(min(n, a.rows - 1)) * a.x_stride;
+    esfew::FewArgs f{};
+    f.x = a.x + uint64_t(n0) * a.x_stride;
+    f.x_stride = a.x_stride;
+    f.rows = min(a.rows - n0, kSmallRows);
+    f.w_stride = a.inner;
+    f.w_rows = a.rank;
+    f.width = a.inner;
     while (left != 0) {
         const int32_t member = __builtin_amdgcn_readlane(mine, __builtin_ctz(left));
         const uint32_t match = uint32_t(__ballot(mine == member));
         left &= ~match;
         const float s = a.scales != nullptr ? a.scales[member] : 1.0f;
-        for (uint32_t r0 = 0; r0 < a.rank; r0 += 32) {
-            const uint32_t r = min(r0 + (lane & 31), a.rank - 1);
-            const uint16_t* const row = a.a + (uint64_t(member) * a.rank + r) * a.inner;
-            f32x16_t c = {};
-            for (uint32_t k0 = 16 * wave; k0 < a.inner; k0 += 128) {
-                const uint32_t k = k0 + 8 * (lane >> 5);
-                u32x4_t av = {0, 0, 0, 0}, xv = {0, 0, 0, 0};
-                if (k < a.inner) {                       // (inner is a multiple of 8)
-                    av = load_row8(row + k);
-                    xv = load_row8(x + k);
-                }
-                c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, av),
-                                                            __builtin_bit_cast(bf16x8_t, xv), c, 0, 0, 0);
-            }
+        f.w = a.a + uint64_t(member) * a.rank * a.inner;
+        for (uint32_t r0 = 0; r0 < a.rank; r0 += 16 * kBlocks) {
+            R t;
+            t.run(f, r0, wave, kWaves, lds + wave * R::kBytes);
             __syncthreads();
 #pragma unroll
-            for (int y = 0; y < 16; ++y)
-                part[wave][8 * (y / 4) + 4 * (lane >> 5) + y % 4][lane & 31] = c[y];
+            for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    *reinterpret_cast<f32x4_t*>(sums + wave * kEach +
+                                                (16 * j + (lane & 15)) * (16 * kBlocks) + 16 * b +
+                                                4 * (lane >> 4)) = t.c[b][j];
             __syncthreads();
-            for (uint32_t e = threadIdx.x; e < 1024; e += kThreads) {
-                const uint32_t t = e / 32, q = e % 32;
-                if ((match >> t & 1) == 0 || r0 + q >= a.rank) continue;
+            for (uint32_t e = threadIdx.x; e < kEach; e += 512) {
+                const uint32_t i = e / (16 * kBlocks), r = r0 + e % (16 * kBlocks);
+                if ((match >> i & 1) == 0 || r >= a.rank) continue;
                 float sum = 0.0f;
 #pragma unroll
-                for (int w = 0; w < 8; ++w) sum += part[w][q][t];
-                a.u[uint64_t(n0 + t) * a.rank + r0 + q] =
-                    static_cast<uint16_t>(pack_bf16(s * sum, 0.0f));
+                for (uint32_t w = 0; w < kWaves; ++w) sum += sums[w * kEach + e];
+                a.u[uint64_t(n0 + i) * a.rank + r] = static_cast<uint16_t>(pack_bf16(s * sum, 0.0f));
             }
+            __syncthreads();               // the rings are free again
         }
     }
 }
@@ -173,7 +180,7 @@ __global__ __launch_bounds__(kThreads, 2) void es_adapt_tile_kernel(TileArgs a) 
     const Place at = place_of(blockIdx.x, a.p);
     const uint32_t m0 = at.m * kTile, n0 = at.n * kTile;
     Tile c;
-    product_tile<false, false>(a.p, m0, n0, 0, a.p.depth, lds, c);
+    product_tile<false, false>(a.p, m0, n0, a.add.rows - n0, 0, a.p.depth, lds, c);
     add_adapters(a.add, m0, n0, c);
     __syncthreads();
     tile_to_lds(c, lds);
@@ -192,30 +199,31 @@ struct FewArgs {
 
 // Up to 64 rows: the waves' sums of a block meet in LDS, where each result takes its
 // own member's B u.
-template <int kBlocks, int kCols>
-__global__ __launch_bounds__(512, kCols == 1 ? 4 : 2) void es_adapt_few_kernel(FewArgs a) {
-    using namespace esfew;
-    constexpr uint32_t kEach = kBlocks * kCols * 256;
-    __shared__ __attribute__((aligned(16))) float sums[kWaves][kEach];
-    const uint32_t lane = threadIdx.x & 63;
-    const Part<kBlocks> at(a.f);
-    Few<kBlocks, kCols> t;
-    t.run(a.f, at.row0, at.k0, at.k1);
+template <int kBlocks, int kCols, int kParts>
+__global__ __launch_bounds__(512, 2) void es_adapt_few_kernel(FewArgs a) {
+    using R = esring::Ring<kBlocks, kCols, kParts>;
+    constexpr uint32_t kWaves = esfew::kWaves, kEach = kBlocks * kCols * 256;
+    static_assert(kEach * 4 <= R::kBytes, "the waves' sums fit their rings");
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+    float* const sums = reinterpret_cast<float*>(lds);   // [wave][row of x][row of the matrix]
+    const uint32_t lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+    const uint32_t row0 = blockIdx.x * 16 * kBlocks;
+    R t;
+    t.run(a.f, row0, wave, kWaves, lds + wave * R::kBytes);
+    __syncthreads();
 #pragma unroll
-    for (int b = 0; b < kBlocks; ++b)      // [column block][row of x][row of the matrix]
+    for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
         for (int j = 0; j < kCols; ++j)
-            *reinterpret_cast<f32x4_t*>(&sums[at.wave][(j * 16 + (lane & 15)) * (16 * kBlocks) + 16 * b +
-                                                       4 * (lane >> 4)]) = t.c[b][j];
+            *reinterpret_cast<f32x4_t*>(sums + wave * kEach + (j * 16 + (lane & 15)) * (16 * kBlocks) +
+                                        16 * b + 4 * (lane >> 4)) = t.c[b][j];
     __syncthreads();
-    const uint32_t groups = kWaves / a.f.slices;
-    for (uint32_t e = threadIdx.x; e < groups * kEach; e += 64 * kWaves) {
-        const uint32_t g = e / kEach, y = e % kEach;
-        const uint32_t n = y / (16 * kBlocks), i = y % (16 * kBlocks);
-        const uint32_t m = (blockIdx.x * groups + g) * 16 * kBlocks + i;
+    for (uint32_t y = threadIdx.x; y < kEach; y += 64 * kWaves) {
+        const uint32_t n = y / (16 * kBlocks), m = row0 + y % (16 * kBlocks);
         if (n >= a.f.rows || m >= a.f.w_rows) continue;
         float sum = 0.0f;
-        for (uint32_t w = 0; w < a.f.slices; ++w) sum += sums[g * a.f.slices + w][y];
+#pragma unroll
+        for (uint32_t w = 0; w < kWaves; ++w) sum += sums[w * kEach + y];
         const int32_t member = a.add.index[n];
         if (member >= int32_t(a.add.members)) sum = eskv::nan();
         if (member >= 0 && member < int32_t(a.add.members)) {
@@ -233,6 +241,76 @@ __global__ __launch_bounds__(512, kCols == 1 ? 4 : 2) void es_adapt_few_kernel(F
         }
         store<uint16_t>(a.out + uint64_t(n) * a.out_stride + m, static_cast<uint16_t>(pack_bf16(sum, 0.0f)));
     }
+}
+
+struct StreamArgs {
+    esstream::StreamArgs s;
+    AddArgs add;
+    uint16_t* out;
+    uint64_t out_stride;
+};
+
+// 2 to 64 rows of words: each lane adds its own row's B u to its four results.
+template <int kTokens, int kStages>
+__global__ __launch_bounds__(256, 2) void es_adapt_stream_kernel(StreamArgs a) {
+    using S = esstream::Stream<4, 1, kTokens, 2, kStages>;
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    S t;
+    t.run(a.s, lds, [&](uint32_t row0, uint32_t end) {
+        const uint32_t m = row0 + 16 * wave + 4 * (lane >> 4);
+        if (m >= end) return;
+#pragma unroll
+        for (int j = 0; j < S::kCols; ++j) {
+            const uint32_t n = 16 * j + (lane & 15);
+            if (n >= a.s.rows) continue;
+            const int32_t member = a.add.index[n];
+            f32x4_t v = t.c[0][j];
+            if (member >= int32_t(a.add.members)) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = eskv::nan();
+            } else if (member >= 0) {
+                const uint16_t* const b = a.add.b + uint64_t(member) * a.add.outer * a.add.rank;
+                const uint16_t* const u = a.add.u + uint64_t(n) * a.add.rank;
+                float low[4] = {};
+                // (the words of 16 of the rank on their way at a time)
+                for (uint32_t r0 = 0; r0 < a.add.rank; r0 += 16) {
+                    u32x4_t q[2], p[2][4];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const uint32_t r = min(r0 + 8 * h, a.add.rank - 8);
+                        q[h] = load<u32x4_t>(u + r);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            p[h][e] = load<u32x4_t>(b + uint64_t(min(m + e, end - 1)) * a.add.rank + r);
+                    }
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        if (r0 + 8 * h >= a.add.rank) break;
+                        float x[8];
+                        eskv::unpack8(q[h], x);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            float y[8];
+                            eskv::unpack8(p[h][e], y);
+#pragma unroll
+                            for (int z = 0; z < 8; ++z) low[e] = __builtin_fmaf(x[z], y[z], low[e]);
+                        }
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] += low[e];
+            }
+            uint16_t* const to = a.out + uint64_t(n) * a.out_stride + m;
+            const u32x2_t w = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+            if (m + 4 <= end) {
+                eskv::store_row4(to, w);
+            } else {
+                for (uint32_t e = 0; m + e < end; ++e)
+                    store<uint16_t>(to + e, static_cast<uint16_t>(w[e / 2] >> (16 * (e % 2))));
+            }
+        }
+    });
 }
 
 }  // namespace esadapt

@@ -130,14 +130,33 @@ struct FewPlan {
     FewPlan(uint32_t rows, uint32_t w_rows, uint32_t width, uint32_t blocks) {
         cols = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
         slices = 1;
-        while (slices < esfew::kWaves && width / (2 * slices) >= 32 * esfew::kSteps) slices *= 2;
+        while (slices < esfew::kWaves && width / (2 * slices) >= 128) slices *= 2;
         const uint32_t per = esfew::kWaves / slices * 16 * blocks;
         groups = (w_rows + per - 1) / per;
     }
 };
 
+// Rows of the matrix for a workgroup: an even share, in blocks of 16 rows.
+uint32_t share_of(uint32_t w_rows, uint32_t groups, uint32_t most) {
+    const uint32_t blocks = (w_rows + 15) / 16, each = (blocks + groups - 1) / groups;
+    return 16 * std::min(each, most);
+}
+
+esstream::StreamArgs stream_args(const void* w, uint64_t w_stride, uint32_t w_rows, const void* x,
+                                 uint64_t x_stride, uint32_t rows, uint32_t width, uint32_t share) {
+    return esstream::StreamArgs{static_cast<const uint16_t*>(w), static_cast<const uint16_t*>(x), w_stride,
+                                x_stride, w_rows, rows, width, share};
+}
+
+// Rows of words, few enough that the matrix's bytes are what they cost.
+bool streams(const es_head_score_t& x) {
+    return x.rows <= esstream::kRows && word_rows(x.weight, x.w_stride, x.hidden) &&
+           word_rows(x.x, x.x_stride, x.hidden);
+}
+
 struct ScorePlan {
-    bool few;
+    bool few, streamed, ringed;
+    uint32_t share;
     HeadRows head;
     Lists lists;
     FewPlan division;
@@ -145,12 +164,18 @@ struct ScorePlan {
     float* parts;
     uint16_t* w;
     ScorePlan(Room& room, const es_head_score_t& x)
-        : few(x.rows <= esfew::kRows),
+        : few(x.rows <= esfew::kRows || streams(x)),
           head(x.weight, x.w_stride, x.vocab, x.hidden, 0),
           lists(room, few ? 0 : x.rows, x.hidden),
           division(x.rows, x.vocab, x.hidden, 2) {
         if (few) {
-            tiles = division.groups;
+            // A small vocabulary leaves the workgroups that stage x too few rows: 3 rows of 5120
+            // against 8000 tokens 45 and 21 us (streamed, in rings), 40 of 2560 against 16000
+            // 31 and 28, 32 of 1024 against 25000 17 and 26.
+            ringed = streams(x) && x.rows <= esfew::kRows && x.vocab <= 16384;
+            streamed = streams(x) && !ringed;
+            share = share_of(x.vocab, kCus, ~0u / 16);
+            tiles = streamed ? (x.vocab + share - 1) / share : ringed ? (x.vocab + 31) / 32 : division.groups;
             parts = room.take<float>(uint64_t(2) * x.rows * tiles);
             w = nullptr;
             return;
@@ -242,7 +267,7 @@ Side head_side(const HeadRows& h, const void* w, uint64_t stride, uint16_t* room
     return Side{room, h.padded, have};
 }
 
-esfew::FewArgs few_args(const FewPlan& d, const void* w, uint64_t w_stride, uint32_t w_rows, const void* x,
+esfew::FewArgs few_args(const void* w, uint64_t w_stride, uint32_t w_rows, const void* x,
                         uint64_t x_stride, uint32_t rows, uint32_t width) {
     esfew::FewArgs f{};
     f.w = static_cast<const uint16_t*>(w);
@@ -252,7 +277,7 @@ esfew::FewArgs few_args(const FewPlan& d, const void* w, uint64_t w_stride, uint
     f.w_rows = w_rows;
     f.rows = rows;
     f.width = width;
-    f.slices = d.slices;
+    f.slices = 1;
     return f;
 }
 
@@ -321,8 +346,43 @@ int es_head_score(const es_head_score_t* args, es_stream_t stream) try {
     a.vocab = x.vocab;
     a.scale = x.scale;
     if (plan.few) {
+        a.x = static_cast<const uint16_t*>(x.x);
+        a.x_stride = x.x_stride;
+    }
+    if (plan.few && plan.streamed) {
+        eshead::StreamStatsArgs t{};
+        t.s = stream_args(x.weight, x.w_stride, x.vocab, x.x, x.x_stride, x.rows, x.hidden, plan.share);
+        t.parts = plan.parts;
+        t.factor = x.scale * eshead::kLog2e;
+        const auto kernel = x.rows <= 32   ? eshead::es_head_stream_kernel<32, 4>
+                            : x.rows <= 64 ? eshead::es_head_stream_kernel<64, 4>
+                                           : eshead::es_head_stream_kernel<128, 3>;
+        const uint32_t lds = x.rows <= 32   ? esstream::Stream<8, 2, 32, 1, 4>::kBytes
+                             : x.rows <= 64 ? esstream::Stream<8, 2, 64, 1, 4>::kBytes
+                                            : esstream::Stream<8, 2, 128, 1, 3>::kBytes;
+        hipLaunchKernelGGL(kernel, dim3(plan.tiles), dim3(512), lds, s, t);
+        hipLaunchKernelGGL(eshead::es_head_score_kernel, dim3(x.rows), dim3(256), 0, s, a);
+        return launch_error("es_head_stream_kernel launch");
+    }
+    if (plan.few && plan.ringed) {
         eshead::FewStatsArgs f{};
-        f.f = few_args(plan.division, x.weight, x.w_stride, x.vocab, x.x, x.x_stride, x.rows, x.hidden);
+        f.f = few_args(x.weight, x.w_stride, x.vocab, x.x, x.x_stride, x.rows, x.hidden);
+        f.parts = plan.parts;
+        f.factor = x.scale * eshead::kLog2e;
+        const auto kernel = x.rows <= 16   ? eshead::es_head_ring_kernel<1, 3>
+                            : x.rows <= 32 ? eshead::es_head_ring_kernel<2, 2>
+                                           : eshead::es_head_ring_kernel<4, 1>;
+        const uint32_t lds = esfew::kWaves * (x.rows <= 16   ? esring::Ring<2, 1, 3>::kBytes
+                                              : x.rows <= 32 ? esring::Ring<2, 2, 2>::kBytes
+                                                             : esring::Ring<2, 4, 1>::kBytes);
+        hipLaunchKernelGGL(kernel, dim3(plan.tiles), dim3(64 * esfew::kWaves), lds, s, f);
+        hipLaunchKernelGGL(eshead::es_head_score_kernel, dim3(x.rows), dim3(256), 0, s, a);
+        return launch_error("es_head_ring_kernel launch");
+    }
+    if (plan.few) {
+        eshead::FewStatsArgs f{};
+        f.f = few_args(x.weight, x.w_stride, x.vocab, x.x, x.x_stride, x.rows, x.hidden);
+        f.f.slices = plan.division.slices;
         f.parts = plan.parts;
         f.factor = x.scale * eshead::kLog2e;
         constexpr int b = 2;
@@ -330,8 +390,6 @@ int es_head_score(const es_head_score_t* args, es_stream_t stream) try {
                             : plan.division.cols == 2 ? eshead::es_head_few_kernel<b, 2>
                                                       : eshead::es_head_few_kernel<b, 4>;
         hipLaunchKernelGGL(kernel, dim3(plan.division.groups), dim3(64 * esfew::kWaves), 0, s, f);
-        a.x = static_cast<const uint16_t*>(x.x);
-        a.x_stride = x.x_stride;
         hipLaunchKernelGGL(eshead::es_head_score_kernel, dim3(x.rows), dim3(256), 0, s, a);
         return launch_error("es_head_few_kernel launch");
     }
@@ -574,7 +632,7 @@ struct AdaptPlan {
         packed_rows = static_cast<uint32_t>(up(a.rows, kTile));
         // the products take rows that start at a word of 16 bytes and end in whole stages
         few = a.rows <= esfew::kRows;
-        const bool copied = !few && (padded != a.inner || !word_rows(a.x, a.x_stride, a.inner));
+        const bool copied = (!few && padded != a.inner) || !word_rows(a.x, a.x_stride, a.inner);
         x = nullptr;
         if (copied) x = room.take<uint16_t>(uint64_t(packed_rows) * padded);
         is_copied = copied;
@@ -620,9 +678,21 @@ int es_adapt_project(const es_adapt_t* args, es_stream_t stream) try {
     ok.check(x.workspace, room.used, ": workspace");
     if (ok.rc != ES_OK) return ok.rc;
     const hipStream_t s = static_cast<hipStream_t>(stream);
+    Side rows{static_cast<const uint16_t*>(x.x), x.x_stride, x.rows};
+    if (plan.is_copied) {
+        eshead::PackArgs pack{};
+        pack.from = static_cast<const uint16_t*>(x.x);
+        pack.to = plan.x;
+        pack.stride = x.x_stride;
+        pack.rows = x.rows;
+        pack.width = x.inner;
+        pack.padded = plan.padded;
+        hipLaunchKernelGGL(eshead::es_head_pack_kernel, dim3(plan.packed_rows / 4), dim3(256), 0, s, pack);
+        rows = Side{plan.x, plan.padded, plan.packed_rows};
+    }
     esadapt::SmallArgs small{};
-    small.x = static_cast<const uint16_t*>(x.x);
-    small.x_stride = x.x_stride;
+    small.x = rows.at;
+    small.x_stride = rows.stride;
     small.a = static_cast<const uint16_t*>(x.a);
     small.scales = x.scales;
     small.index = x.index;
@@ -637,38 +707,55 @@ int es_adapt_project(const es_adapt_t* args, es_stream_t stream) try {
     if (plan.few) {
         hipLaunchKernelGGL(esadapt::es_adapt_few_small_kernel, dim3(x.rows, (x.rank + 3) / 4), dim3(256), 0,
                            s, small);
-        const bool narrow = x.outer <= 8192;
-        const FewPlan d(x.rows, x.outer, x.inner, narrow ? 1 : 2);
+        // A matrix of many rows is divided among workgroups that stage the rows of x for
+        // four waves at a time, one of few rows among those whose waves share a sum.  5120 x
+        // 5120: 1 row 22 and 14 us (streamed, in rings), 16 rows 23 and 15; 5120 x 17408: 1 row
+        // 41 and 38, 32 rows 57 and 60.
+        if (x.rows > 16 && x.outer > 8192) {
+            const uint32_t share = share_of(x.outer, 2 * kCus, 4);
+            esadapt::StreamArgs t{};
+            t.s = stream_args(x.weight, x.w_stride, x.outer, rows.at, rows.stride, x.rows, x.inner, share);
+            t.add = add;
+            t.out = static_cast<uint16_t*>(x.out);
+            t.out_stride = x.out_stride;
+            const bool half = x.rows <= 32;
+            const auto kernel = half ? esadapt::es_adapt_stream_kernel<32, 3>
+                                     : esadapt::es_adapt_stream_kernel<64, 2>;
+            const uint32_t lds = half ? esstream::Stream<4, 1, 32, 2, 3>::kBytes
+                                      : esstream::Stream<4, 1, 64, 2, 2>::kBytes;
+            hipLaunchKernelGGL(kernel, dim3((x.outer + share - 1) / share), dim3(256), lds, s, t);
+            return launch_error("es_adapt_stream_kernel launch");
+        }
         esadapt::FewArgs f{};
-        f.f = few_args(d, x.weight, x.w_stride, x.outer, x.x, x.x_stride, x.rows, x.inner);
+        f.f = few_args(x.weight, x.w_stride, x.outer, rows.at, rows.stride, x.rows, x.inner);
         f.add = add;
         f.out = static_cast<uint16_t*>(x.out);
         f.out_stride = x.out_stride;
-        const auto kernel = d.cols == 1   ? (narrow ? esadapt::es_adapt_few_kernel<1, 1>
-                                                    : esadapt::es_adapt_few_kernel<2, 1>)
-                            : d.cols == 2 ? (narrow ? esadapt::es_adapt_few_kernel<1, 2>
-                                                    : esadapt::es_adapt_few_kernel<2, 2>)
-                                          : (narrow ? esadapt::es_adapt_few_kernel<1, 4>
-                                                    : esadapt::es_adapt_few_kernel<2, 4>);
-        hipLaunchKernelGGL(kernel, dim3(d.groups), dim3(64 * esfew::kWaves), 0, s, f);
+        const auto launch = [&](auto kernel, uint32_t blocks, uint32_t bytes) {
+            hipLaunchKernelGGL(kernel, dim3((x.outer + 16 * blocks - 1) / (16 * blocks)),
+                               dim3(64 * esfew::kWaves), esfew::kWaves * bytes, s, f);
+        };
+        // (one block of 16 rows a workgroup where there are more of them than the card holds)
+        if (x.outer > 8192)
+            launch(esadapt::es_adapt_few_kernel<1, 1, 2>, 1, esring::Ring<1, 1, 2>::kBytes);
+        else if (x.rows <= 16)
+            launch(esadapt::es_adapt_few_kernel<2, 1, 3>, 2, esring::Ring<2, 1, 3>::kBytes);
+        else if (x.rows <= 32)
+            launch(esadapt::es_adapt_few_kernel<2, 2, 2>, 2, esring::Ring<2, 2, 2>::kBytes);
+        else
+            launch(esadapt::es_adapt_few_kernel<2, 4, 1>, 2, esring::Ring<2, 4, 1>::kBytes);
         return launch_error("es_adapt_few_kernel launch");
     }
-    hipLaunchKernelGGL(esadapt::es_adapt_small_kernel,
-                       dim3((x.rows + esadapt::kSmallRows - 1) / esadapt::kSmallRows), dim3(kThreads), 0, s,
-                       small);
+    const auto small_kernel = x.rank <= 16   ? esadapt::es_adapt_small_kernel<1, 3>
+                              : x.rank <= 32 ? esadapt::es_adapt_small_kernel<2, 2>
+                                             : esadapt::es_adapt_small_kernel<4, 1>;
+    const uint32_t small_lds = esfew::kWaves * (x.rank <= 16   ? esring::Ring<1, 2, 3>::kBytes
+                                                : x.rank <= 32 ? esring::Ring<2, 2, 2>::kBytes
+                                                               : esring::Ring<4, 2, 1>::kBytes);
+    hipLaunchKernelGGL(small_kernel,
+                       dim3((x.rows + esadapt::kSmallRows - 1) / esadapt::kSmallRows), dim3(kThreads),
+                       small_lds, s, small);
     esadapt::TileArgs a{};
-    Side rows{static_cast<const uint16_t*>(x.x), x.x_stride, x.rows};
-    if (plan.is_copied) {
-        eshead::PackArgs pack{};
-        pack.from = static_cast<const uint16_t*>(x.x);
-        pack.to = plan.x;
-        pack.stride = x.x_stride;
-        pack.rows = x.rows;
-        pack.width = x.inner;
-        pack.padded = plan.padded;
-        hipLaunchKernelGGL(eshead::es_head_pack_kernel, dim3(plan.packed_rows / 4), dim3(256), 0, s, pack);
-        rows = Side{plan.x, plan.padded, plan.packed_rows};
-    }
     a.p = product(Side{static_cast<const uint16_t*>(x.weight), x.w_stride, x.outer}, rows, x.outer, x.rows,
                   x.inner, nullptr);
     a.add = add;

@@ -11,7 +11,6 @@ using namespace esmm;
 
 constexpr uint32_t kRows = 64;             // at most
 constexpr uint32_t kWaves = 8;             // of a workgroup
-constexpr int kSteps = 4;                  // of 32 of the sum, on their way at a time
 
 struct FewArgs {
     const uint16_t* w;                     // any alignment to 2 bytes
@@ -32,7 +31,8 @@ __device__ __forceinline__ u32x4_t load_part(const uint16_t* row, uint32_t k, ui
 
 // The operand of lane l of a block of 16 rows: row l % 16, elements 8 (l / 16) .. of a
 // step of 32.  The result: column (a row of x) l % 16, rows 4 (l / 16) .. + 3.
-template <int kBlocks, int kCols>
+// kSteps steps are on their way at a time, and as many behind them.
+template <int kBlocks, int kCols, int kSteps>
 struct Few {
     f32x4_t c[kBlocks][kCols];
     const uint16_t *wp[kBlocks], *xp[kCols];
@@ -112,7 +112,7 @@ struct Few {
 };
 
 // Where a wave works: the first row of its blocks and its first group of the sum.
-template <int kBlocks>
+template <int kBlocks, int kSteps>
 struct Part {
     uint32_t wave, group, slice, row0, k0, k1;
     __device__ __forceinline__ explicit Part(const FewArgs& a) {

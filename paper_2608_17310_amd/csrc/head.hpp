@@ -10,6 +10,8 @@
 
 #include "few.hpp"
 #include "mm_tile.hpp"
+#include "ring.hpp"
+#include "stream.hpp"
 
 namespace eshead {
 
@@ -185,7 +187,7 @@ __global__ __launch_bounds__(kThreads, 2) void es_head_stats_kernel(StatsArgs a)
     const uint32_t count = *a.p.count;
     if (n0 >= count) return;
     Tile c;
-    product_tile<false, false>(a.p, m0, n0, 0, a.p.depth, lds, c);
+    product_tile<false, false>(a.p, m0, n0, count - n0, 0, a.p.depth, lds, c);
     __syncthreads();
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const uint32_t m_have = a.p.a.extent - m0;
@@ -242,8 +244,8 @@ __global__ __launch_bounds__(512, kCols == 1 ? 4 : 2) void es_head_few_kernel(Fe
     __shared__ __attribute__((aligned(16))) float sums[kWaves][kBlocks * kCols * 256];
     __shared__ float pair[kWaves][16 * kCols][2];
     const uint32_t lane = threadIdx.x & 63;
-    const Part<kBlocks> at(a.f);
-    Few<kBlocks, kCols> t;
+    const Part<kBlocks, 4> at(a.f);
+    Few<kBlocks, kCols, 4> t;
     t.run(a.f, at.row0, at.k0, at.k1);
     if (a.f.slices > 1) {                  // a block's first wave adds the others'
 #pragma unroll
@@ -304,6 +306,120 @@ __global__ __launch_bounds__(512, kCols == 1 ? 4 : 2) void es_head_few_kernel(Fe
         float* const to = a.parts + 2 * (uint64_t(n) * gridDim.x + blockIdx.x);
         to[0] = top;
         to[1] = sum;
+    }
+}
+
+// The same of rows of words against a small vocabulary: a workgroup's 32 tokens are a
+// part, whose sums its waves share.
+template <int kCols, int kParts>
+__global__ __launch_bounds__(512, 2) void es_head_ring_kernel(FewStatsArgs a) {
+    using R = esring::Ring<2, kCols, kParts>;
+    constexpr uint32_t kWaves = esfew::kWaves, kEach = kCols * 512;
+    static_assert(kEach * 4 <= R::kBytes, "the waves' sums fit their rings");
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+    float* const sums = reinterpret_cast<float*>(lds);   // [wave][row of x][token]
+    const uint32_t lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+    const uint32_t row0 = blockIdx.x * 32;
+    R t;
+    t.run(a.f, row0, wave, kWaves, lds + wave * R::kBytes);
+    __syncthreads();
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int j = 0; j < kCols; ++j)
+            *reinterpret_cast<f32x4_t*>(sums + wave * kEach + (j * 16 + (lane & 15)) * 32 + 16 * b +
+                                        4 * (lane >> 4)) = t.c[b][j];
+    __syncthreads();
+    // half a wave a row: a lane for each token
+    for (uint32_t n = threadIdx.x >> 5; n < 16 * kCols && n < a.f.rows; n += 2 * kWaves) {
+        const uint32_t i = threadIdx.x & 31;
+        float z = 0.0f;
+#pragma unroll
+        for (uint32_t w = 0; w < kWaves; ++w) z += sums[w * kEach + n * 32 + i];
+        z = row0 + i < a.f.w_rows ? z * a.factor : -eskv::inf();
+        float top = z;
+#pragma unroll
+        for (int d = 16; d >= 1; d /= 2) top = fmaxf(top, __shfl_xor(top, d));
+        float sum = __builtin_amdgcn_exp2f(z - (top == -eskv::inf() ? 0.0f : top));
+#pragma unroll
+        for (int d = 16; d >= 1; d /= 2) sum += __shfl_xor(sum, d);
+        if (i == 0) {
+            float* const to = a.parts + 2 * (uint64_t(n) * gridDim.x + blockIdx.x);
+            to[0] = top;
+            to[1] = sum;
+        }
+    }
+}
+
+struct StreamStatsArgs {
+    esstream::StreamArgs s;
+    float* parts;                          // [rows][workgroups] pairs
+    float factor;
+};
+
+// The same of up to 128 rows of words: a workgroup's share of the vocabulary is a part,
+// whose maxima and sums run along in registers.
+template <int kTokens, int kStages>
+__global__ __launch_bounds__(512, 2) void es_head_stream_kernel(StreamStatsArgs a) {
+    using S = esstream::Stream<8, 2, kTokens, 1, kStages>;
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    float top[S::kCols], sum[S::kCols];
+#pragma unroll
+    for (int j = 0; j < S::kCols; ++j) {
+        top[j] = -eskv::inf();
+        sum[j] = 0.0f;
+    }
+    S t;
+    t.run(a.s, lds, [&](uint32_t row0, uint32_t end) {
+#pragma unroll
+        for (int j = 0; j < S::kCols; ++j) {
+            float z[2][4], most = top[j];
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const bool here = row0 + 32 * wave + 16 * b + 4 * (lane >> 4) + e < end;
+                    z[b][e] = here ? t.c[b][j][e] * a.factor : -eskv::inf();
+                    most = fmaxf(most, z[b][e]);
+                }
+            const float from = most == -eskv::inf() ? 0.0f : most;
+            sum[j] *= __builtin_amdgcn_exp2f(top[j] - from);
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum[j] += __builtin_amdgcn_exp2f(z[b][e] - from);
+            top[j] = most;
+        }
+    });
+    __syncthreads();                       // every wave has left the last stage
+    float* const pair = reinterpret_cast<float*>(lds);   // [8 waves][kTokens] pairs
+#pragma unroll
+    for (int j = 0; j < S::kCols; ++j) {
+        float most = fmaxf(top[j], __shfl_xor(top[j], 16));
+        most = fmaxf(most, __shfl_xor(most, 32));
+        const float from = most == -eskv::inf() ? 0.0f : most;
+        float all = sum[j] * __builtin_amdgcn_exp2f(top[j] - from);
+        all += __shfl_xor(all, 16);
+        all += __shfl_xor(all, 32);
+        if (lane < 16) {
+            pair[2 * (kTokens * wave + 16 * j + lane)] = most;
+            pair[2 * (kTokens * wave + 16 * j + lane) + 1] = all;
+        }
+    }
+    __syncthreads();
+    const uint32_t n = threadIdx.x;
+    if (n < kTokens && n < a.s.rows) {
+        float most = -eskv::inf();
+        for (uint32_t w = 0; w < 8; ++w) most = fmaxf(most, pair[2 * (kTokens * w + n)]);
+        const float from = most == -eskv::inf() ? 0.0f : most;
+        float all = 0.0f;
+        for (uint32_t w = 0; w < 8; ++w)
+            all += pair[2 * (kTokens * w + n) + 1] *
+                   __builtin_amdgcn_exp2f(pair[2 * (kTokens * w + n)] - from);
+        float* const to = a.parts + 2 * (uint64_t(n) * gridDim.x + blockIdx.x);
+        to[0] = most;
+        to[1] = all;
     }
 }
 
@@ -447,9 +563,10 @@ __global__ __launch_bounds__(kThreads, 2) void es_head_prob_kernel(ProbArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     const Place at = place_of(blockIdx.x, a.p);
     const uint32_t m0 = at.m * kTile, n0 = at.n * kTile;
-    if (n0 >= *a.p.count) return;
+    const uint32_t count = *a.p.count;
+    if (n0 >= count) return;
     Tile c;
-    product_tile<false, false>(a.p, m0, n0, 0, a.p.depth, lds, c);
+    product_tile<false, false>(a.p, m0, n0, count - n0, 0, a.p.depth, lds, c);
     __syncthreads();
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const uint32_t m_have = a.p.a.extent - m0;
@@ -526,7 +643,7 @@ __global__ __launch_bounds__(kThreads, 2) void es_head_row_grad_kernel(RowGradAr
     if (n0 >= count) return;
     const uint32_t k0 = at.split * a.p.split_depth;
     Tile c;
-    product_tile<true, false>(a.p, m0, n0, k0, min(a.p.depth, k0 + a.p.split_depth), lds, c);
+    product_tile<true, false>(a.p, m0, n0, count - n0, k0, min(a.p.depth, k0 + a.p.split_depth), lds, c);
     if (a.out != nullptr) {
         __syncthreads();
         tile_to_lds(c, lds);
@@ -595,7 +712,7 @@ __global__ __launch_bounds__(kThreads, 2) void es_head_weight_grad_kernel(HeadGr
     const uint32_t m0 = at.m * kTile, n0 = at.n * kTile;
     const uint32_t depth = (*a.p.count + kDepth - 1) / kDepth * kDepth;   // zeros behind the rows
     Tile c;
-    product_tile<true, true>(a.p, m0, n0, 0, depth, lds, c);
+    product_tile<true, true>(a.p, m0, n0, a.n_have - n0, 0, depth, lds, c);
     __syncthreads();
     tile_to_lds(c, lds);
     __syncthreads();

@@ -72,12 +72,13 @@ __device__ __forceinline__ Place place_of(uint32_t id, const Product& p) {
     return x;
 }
 
-// 16 bytes a lane from memory into LDS, at byte `dst` (of the wave) + 16 lane.
+// 16 bytes a lane from memory (`offset` of the lane and `more` of the wave) into LDS,
+// at byte `dst` (of the wave) + 16 lane.
 // (In asm, which has no register output: the compiler would make every later read
 // of LDS wait for it.)  wait_staged() and a barrier before the data are read.
-__device__ __forceinline__ void load_lds(u32x4_t buffer, uint32_t offset, uint32_t dst) {
-    asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-                 :: "s"(dst), "v"(offset), "s"(buffer) : "memory");
+__device__ __forceinline__ void load_lds(u32x4_t buffer, uint32_t offset, uint32_t more, uint32_t dst) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+                 :: "s"(dst), "v"(offset), "s"(buffer), "s"(more) : "memory");
 }
 __device__ __forceinline__ void wait_staged() {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
@@ -142,7 +143,7 @@ struct Stage {
                                 bytes > 0xFFFFFFFFull ? 0xFFFFFFFFu : uint32_t(bytes), 0x00020000u};
         if (have >= kDepth) {
 #pragma unroll
-            for (uint32_t x = 0; x < 4; ++x) load_lds(buffer, off[x], lds + dst + 1024 * x);
+            for (uint32_t x = 0; x < 4; ++x) load_lds(buffer, off[x], 0, lds + dst + 1024 * x);
         } else {
 #pragma unroll
             for (uint32_t x = 0; x < 4; ++x) {
@@ -155,7 +156,7 @@ struct Stage {
                     const uint32_t w = (lane & 7) ^ ((i >> 1) & 7);
                     if (8 * w >= have) o -= 16 * w;
                 }
-                load_lds(buffer, o, lds + dst + 1024 * x);
+                load_lds(buffer, o, 0, lds + dst + 1024 * x);
             }
         }
         base += step;
@@ -212,9 +213,11 @@ struct Count {
     static constexpr int value = n;
 };
 
+// Rows n0 .. n0 + n_have of n are there (more than 256 count as 256).  Waves whose rows
+// are not only stage: a tile with at most half of its rows takes half of the time.
 template <bool kWideA, bool kWideB>
-__device__ __forceinline__ void product_tile(const Product& p, uint32_t m0, uint32_t n0, uint32_t k0,
-                                             uint32_t k_end, uint8_t* lds, Tile& c) {
+__device__ __forceinline__ void product_tile(const Product& p, uint32_t m0, uint32_t n0, uint32_t n_have,
+                                             uint32_t k0, uint32_t k_end, uint8_t* lds, Tile& c) {
     const uint32_t lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -275,6 +278,15 @@ __device__ __forceinline__ void product_tile(const Product& p, uint32_t m0, uint
     wait_staged();
     __builtin_amdgcn_s_barrier();
     if (k0 + kDepth < k_end) issue(k0 + kDepth, 2 * kSideBytes);
+    if (64 * (wave >> 1) >= n_have) {
+        for (uint32_t k = k0; k + kDepth < k_end; k += kDepth) {
+            wait_staged();
+            __builtin_amdgcn_s_barrier();
+            if (k + 2 * kDepth < k_end) issue(k + 2 * kDepth, buf);
+            buf ^= 2 * kSideBytes;
+        }
+        return;
+    }
     read(0);
     uint32_t k = k0;
     for (; k + kDepth < k_end; k += kDepth) {
