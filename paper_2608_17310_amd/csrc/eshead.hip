@@ -753,7 +753,7 @@ int es_adapt_project(const es_adapt_t* args, es_stream_t stream) try {
                                                 : x.rank <= 32 ? esring::Ring<2, 2, 2>::kBytes
                                                                : esring::Ring<4, 2, 1>::kBytes);
     hipLaunchKernelGGL(small_kernel,
-                       dim3((x.rows + esadapt::kSmallRows - 1) / esadapt::kSmallRows), dim3(kThreads),
+                       dim3((x.rows + esadapt::kSmallRows - 1) / esadapt::kSmallRows), dim3(64 * esfew::kWaves),
                        small_lds, s, small);
     esadapt::TileArgs a{};
     a.p = product(Side{static_cast<const uint16_t*>(x.weight), x.w_stride, x.outer}, rows, x.outer, x.rows,

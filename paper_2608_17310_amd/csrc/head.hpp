@@ -193,27 +193,29 @@ __global__ __launch_bounds__(kThreads, 2) void es_head_stats_kernel(StatsArgs a)
     const uint32_t m_have = a.p.a.extent - m0;
     float* const pair = reinterpret_cast<float*>(lds);   // [2 waves of m][256 n] pairs
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
+    for (int j = 0; j < 4; ++j) {
         float top = -eskv::inf();
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 8; ++i)
 #pragma unroll
-            for (int x = 0; x < 16; ++x) {
-                const uint32_t m = 128 * (wave & 1) + 32 * i + 8 * (x / 4) + 4 * (lane >> 5) + x % 4;
-                const float t = c.x[i][j][x] * a.factor;
-                c.x[i][j][x] = m < m_have ? t : -eskv::inf();
-                top = fmaxf(top, c.x[i][j][x]);
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t m = 128 * (wave & 1) + 16 * i + 4 * (lane >> 4) + e;
+                const float z = m < m_have ? c.x[i][j][e] * a.factor : -eskv::inf();
+                c.x[i][j][e] = z;
+                top = fmaxf(top, z);
             }
+        top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
         const float from = top == -eskv::inf() ? 0.0f : top;
         float sum = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 8; ++i)
 #pragma unroll
-            for (int x = 0; x < 16; ++x) sum += __builtin_amdgcn_exp2f(c.x[i][j][x] - from);
+            for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f(c.x[i][j][e] - from);
+        sum += __shfl_xor(sum, 16);
         sum += __shfl_xor(sum, 32);
-        if (lane < 32) {
-            const uint32_t n = 64 * (wave >> 1) + 32 * j + lane;
+        if (lane < 16) {
+            const uint32_t n = 64 * (wave >> 1) + 16 * j + lane;
             pair[2 * (256 * (wave & 1) + n)] = top;
             pair[2 * (256 * (wave & 1) + n) + 1] = sum;
         }
@@ -571,16 +573,16 @@ __global__ __launch_bounds__(kThreads, 2) void es_head_prob_kernel(ProbArgs a) {
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const uint32_t m_have = a.p.a.extent - m0;
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const uint32_t n = n0 + 64 * (wave >> 1) + 32 * j + (lane & 31);
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t n = n0 + 64 * (wave >> 1) + 16 * j + (lane & 15);
         const float f = a.factor[n], l = a.minus_lse[n];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 8; ++i)
 #pragma unroll
-            for (int x = 0; x < 16; ++x) {
-                const uint32_t m = 128 * (wave & 1) + 32 * i + 8 * (x / 4) + 4 * (lane >> 5) + x % 4;
-                const float p = f * __builtin_amdgcn_exp2f(__builtin_fmaf(c.x[i][j][x], a.scale, l));
-                c.x[i][j][x] = m < m_have ? p : 0.0f;
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t m = 128 * (wave & 1) + 16 * i + 4 * (lane >> 4) + e;
+                const float p = f * __builtin_amdgcn_exp2f(__builtin_fmaf(c.x[i][j][e], a.scale, l));
+                c.x[i][j][e] = m < m_have ? p : 0.0f;
             }
     }
     tile_to_lds(c, lds);
@@ -655,11 +657,9 @@ __global__ __launch_bounds__(kThreads, 2) void es_head_row_grad_kernel(RowGradAr
     }
     float* const to = a.parts + (at.split * a.parts_rows + n0) * a.parts_stride + m0;
     const uint32_t m_have = a.p.a.extent - m0, n_have = count - n0;
-    for_words([&](int i, int j, int y, uint32_t m, uint32_t n) {
+    for_words(c, [&](f32x4_t v, uint32_t m, uint32_t n) {
         if (m >= m_have || n >= n_have) return;          // (extents are multiples of 8)
         float* const q = to + n * a.parts_stride + m;
-        f32x4_t v = {c.x[i][j][4 * y], c.x[i][j][4 * y + 1], c.x[i][j][4 * y + 2],
-                     c.x[i][j][4 * y + 3]};
         if (a.add) {
             const f32x4_t was = load<f32x4_t>(q);
 #pragma unroll
