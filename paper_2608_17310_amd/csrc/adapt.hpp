@@ -116,57 +116,67 @@ struct AddArgs {
     uint32_t rows, outer, members, rank;
 };
 
-// B u added to a tile, for the members of each 16 rows one by one.  Where one
-// member has all of them its products go straight into the tile; otherwise into
+// B u added to a tile, for the members of a wave's 64 rows one by one.  Where a
+// member has all of 16 rows its products go straight into the tile; otherwise into
 // results of their own, of which its rows take theirs: a member that holds
 // infinities or NaN reaches no other's rows.
 __device__ __forceinline__ void add_adapters(const AddArgs& a, uint32_t m0, uint32_t n0, Tile& c) {
     const uint32_t lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+    const uint32_t n1 = n0 + 64 * (wave >> 1);
+    int32_t mine[4];                       // of the lane's row of each block
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const uint32_t n = n0 + 64 * (wave >> 1) + 16 * j + (lane & 15);
-        const int32_t mine = n < a.rows ? a.index[n] : -1;
-        const bool bad = mine >= int32_t(a.members);
-        uint32_t left = uint32_t(__ballot(mine >= 0 && !bad)) & 0xFFFFu;
-        while (left != 0) {
-            const int32_t member = __builtin_amdgcn_readlane(mine, __builtin_ctz(left));
-            const bool match = mine == member;
-            const uint32_t all = uint32_t(__ballot(match)) & 0xFFFFu;
-            left &= ~all;
-            f32x4_t t[8];
+        const uint32_t n = n1 + 16 * j + (lane & 15);
+        mine[j] = n < a.rows ? a.index[n] : -1;
+    }
+    const int32_t every = n1 + lane < a.rows ? a.index[n1 + lane] : -1;
+    uint64_t left = __ballot(every >= 0 && every < int32_t(a.members));
+    while (left != 0) {
+        const int32_t member = __builtin_amdgcn_readlane(every, __builtin_ctzll(left));
+        const uint64_t rows = __ballot(every == member);
+        left &= ~rows;
+        for (uint32_t r0 = 0; r0 < a.rank; r0 += 32) {
+            const uint32_t r = r0 + 8 * (lane >> 4);
+            u32x4_t bv[8], uv[4];
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) t[i][e] = all == 0xFFFFu ? c.x[i][j][e] : 0.0f;
-            for (uint32_t r0 = 0; r0 < a.rank; r0 += 32) {
-                const uint32_t r = r0 + 8 * (lane >> 4);
-                u32x4_t uv = {0, 0, 0, 0};
-                if (match && r < a.rank) uv = load<u32x4_t>(a.u + uint64_t(n) * a.rank + r);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const uint32_t m = min(m0 + 128 * (wave & 1) + 16 * i + (lane & 15), a.outer - 1);
-                    u32x4_t bv = {0, 0, 0, 0};
-                    if (r < a.rank)
-                        bv = load<u32x4_t>(a.b + (uint64_t(member) * a.outer + m) * a.rank + r);
-                    t[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, bv),
-                                                                   __builtin_bit_cast(bf16x8_t, uv),
-                                                                   t[i], 0, 0, 0);
-                }
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t m = min(m0 + 128 * (wave & 1) + 16 * i + (lane & 15), a.outer - 1);
+                bv[i] = r < a.rank ? load<u32x4_t>(a.b + (uint64_t(member) * a.outer + m) * a.rank + r)
+                                   : u32x4_t{0, 0, 0, 0};
             }
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
+            for (int j = 0; j < 4; ++j)
+                uv[j] = mine[j] == member && r < a.rank
+                            ? load<u32x4_t>(a.u + uint64_t(n1 + 16 * j + (lane & 15)) * a.rank + r)
+                            : u32x4_t{0, 0, 0, 0};
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    c.x[i][j][e] = all == 0xFFFFu ? t[i][e]
-                                   : match        ? c.x[i][j][e] + t[i][e]
-                                                  : c.x[i][j][e];
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t some = uint32_t(rows >> (16 * j)) & 0xFFFFu;
+                if (some == 0) continue;
+                const bool whole = some == 0xFFFFu;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const f32x4_t from = whole ? c.x[i][j] : f32x4_t{0, 0, 0, 0};
+                    const f32x4_t t = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                        __builtin_bit_cast(bf16x8_t, bv[i]), __builtin_bit_cast(bf16x8_t, uv[j]), from, 0, 0,
+                        0);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        c.x[i][j][e] = whole                ? t[e]
+                                       : mine[j] == member ? c.x[i][j][e] + t[e]
+                                                           : c.x[i][j][e];
+                }
+            }
         }
-        if (__any(bad)) {
+    }
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
+    for (int j = 0; j < 4; ++j) {
+        if (!__any(mine[j] >= int32_t(a.members))) continue;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) c.x[i][j][e] = bad ? eskv::nan() : c.x[i][j][e];
-        }
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                c.x[i][j][e] = mine[j] >= int32_t(a.members) ? eskv::nan() : c.x[i][j][e];
     }
 }
 

@@ -284,7 +284,7 @@ __device__ __forceinline__ void product_tile(const Product& p, uint32_t m0, uint
         return;
     }
     read(0);
-    auto turn = [&]() {                                  // to the next stage
+    auto first_step = [&]() {
         read(1);
         multiply(0, 0, 8);
         interleave(Count<32>{});
@@ -292,32 +292,37 @@ __device__ __forceinline__ void product_tile(const Product& p, uint32_t m0, uint
         wait_staged();
         __builtin_amdgcn_s_barrier();
         buf ^= 2 * kSideBytes;
-        read(0);
-        multiply(1, 0, 4);
-        interleave(Count<16>{});
+    };
+    auto product = [&](int y) {                          // of the second step
+        c.x[y / 4][y % 4] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[1][y / 4], b[1][y % 4],
+                                                                    c.x[y / 4][y % 4], 0, 0, 0);
     };
     uint32_t k = k0;
     for (; k + 3 * kDepth <= k_end; k += kDepth) {       // the stage after the next is whole
-        turn();
+        first_step();
         const uint32_t old = lds_at + (buf ^ 2 * kSideBytes);
         const u32x4_t ba = sa.take(), bb = sb.take();
 #pragma unroll
-        for (uint32_t x = 0; x < 8; ++x) {               // a load to two products
+        for (uint32_t x = 0; x < 8; ++x) {               // a load to a product
             if (x < 4)
                 sa.load(ba, old, x);
             else
                 sb.load(bb, old + kSideBytes, x - 4);
-#pragma unroll
-            for (int y = 2 * x; y < 2 * int(x) + 2; ++y)
-                c.x[4 + y / 4][y % 4] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                    a[1][4 + y / 4], b[1][y % 4], c.x[4 + y / 4][y % 4], 0, 0, 0);
+            product(x);
             __builtin_amdgcn_sched_barrier(0);
         }
+        read(0);
+#pragma unroll
+        for (int y = 8; y < 32; ++y) product(y);
+        interleave(Count<24>{});
     }
     for (; k + kDepth < k_end; k += kDepth) {
-        turn();
+        first_step();
         if (k + 2 * kDepth < k_end) issue(k + 2 * kDepth, buf ^ 2 * kSideBytes);
-        multiply(1, 4, 8);
+        read(0);
+#pragma unroll
+        for (int y = 0; y < 32; ++y) product(y);
+        interleave(Count<32>{});
     }
     read(1);
     multiply(0, 0, 8);
