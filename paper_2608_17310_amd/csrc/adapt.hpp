@@ -120,7 +120,9 @@ struct AddArgs {
 // member has all of 16 rows its products go straight into the tile; otherwise into
 // results of their own, of which its rows take theirs: a member that holds
 // infinities or NaN reaches no other's rows.
-__device__ __forceinline__ void add_adapters(const AddArgs& a, uint32_t m0, uint32_t n0, Tile& c) {
+template <int kSize>
+__device__ __forceinline__ void add_adapters(const AddArgs& a, uint32_t m0, uint32_t n0, Tile<kSize>& c) {
+    constexpr int kBlocks = Tile<kSize>::kBlocks;
     const uint32_t lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
     const uint32_t n1 = n0 + 64 * (wave >> 1);
     int32_t mine[4];                       // of the lane's row of each block
@@ -137,10 +139,10 @@ __device__ __forceinline__ void add_adapters(const AddArgs& a, uint32_t m0, uint
         left &= ~rows;
         for (uint32_t r0 = 0; r0 < a.rank; r0 += 32) {
             const uint32_t r = r0 + 8 * (lane >> 4);
-            u32x4_t bv[8], uv[4];
+            u32x4_t bv[kBlocks], uv[4];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const uint32_t m = min(m0 + 128 * (wave & 1) + 16 * i + (lane & 15), a.outer - 1);
+            for (int i = 0; i < kBlocks; ++i) {
+                const uint32_t m = min(m0 + kSize / 2 * (wave & 1) + 16 * i + (lane & 15), a.outer - 1);
                 bv[i] = r < a.rank ? load<u32x4_t>(a.b + (uint64_t(member) * a.outer + m) * a.rank + r)
                                    : u32x4_t{0, 0, 0, 0};
             }
@@ -155,7 +157,7 @@ __device__ __forceinline__ void add_adapters(const AddArgs& a, uint32_t m0, uint
                 if (some == 0) continue;
                 const bool whole = some == 0xFFFFu;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
+                for (int i = 0; i < kBlocks; ++i) {
                     const f32x4_t from = whole ? c.x[i][j] : f32x4_t{0, 0, 0, 0};
                     const f32x4_t t = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
                         __builtin_bit_cast(bf16x8_t, bv[i]), __builtin_bit_cast(bf16x8_t, uv[j]), from, 0, 0,
@@ -173,10 +175,59 @@ __device__ __forceinline__ void add_adapters(const AddArgs& a, uint32_t m0, uint
     for (int j = 0; j < 4; ++j) {
         if (!__any(mine[j] >= int32_t(a.members))) continue;
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < kBlocks; ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
                 c.x[i][j][e] = mine[j] >= int32_t(a.members) ? eskv::nan() : c.x[i][j][e];
+    }
+}
+
+// Results v of row n, rows m .. of the matrix (before `end`), with their member's B u.
+__device__ __forceinline__ f32x4_t with_adapter(const AddArgs& a, f32x4_t v, uint32_t n, uint32_t m,
+                                                uint32_t end, int32_t member) {
+    if (member >= int32_t(a.members)) return f32x4_t{eskv::nan(), eskv::nan(), eskv::nan(), eskv::nan()};
+    if (member < 0) return v;
+    const uint16_t* const b = a.b + uint64_t(member) * a.outer * a.rank;
+    const uint16_t* const u = a.u + uint64_t(n) * a.rank;
+    float low[4] = {};
+    // (the words of 16 of the rank on their way at a time)
+    for (uint32_t r0 = 0; r0 < a.rank; r0 += 16) {
+        u32x4_t q[2], p[2][4];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t r = min(r0 + 8 * h, a.rank - 8);
+            q[h] = load<u32x4_t>(u + r);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                p[h][e] = load<u32x4_t>(b + uint64_t(min(m + e, end - 1)) * a.rank + r);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            if (r0 + 8 * h >= a.rank) break;
+            float x[8];
+            eskv::unpack8(q[h], x);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float y[8];
+                eskv::unpack8(p[h][e], y);
+#pragma unroll
+                for (int z = 0; z < 8; ++z) low[e] = __builtin_fmaf(x[z], y[z], low[e]);
+            }
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] += low[e];
+    return v;
+}
+
+// Up to four of them, rounded.
+__device__ __forceinline__ void store_results(uint16_t* to, f32x4_t v, uint32_t have) {
+    const u32x2_t w = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+    if (have >= 4) {
+        eskv::store_row4(to, w);
+    } else {
+        for (uint32_t e = 0; e < have; ++e)
+            store<uint16_t>(to + e, static_cast<uint16_t>(w[e / 2] >> (16 * (e % 2))));
     }
 }
 
@@ -187,19 +238,67 @@ struct TileArgs {
     uint64_t out_stride;
 };
 
-__global__ __launch_bounds__(kThreads, 2) void es_adapt_tile_kernel(TileArgs a) {
+template <int kSize>
+__global__ __launch_bounds__(2 * kSize, 2) void es_adapt_tile_kernel(TileArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     const Place at = place_of(blockIdx.x, a.p);
-    const uint32_t m0 = at.m * kTile, n0 = at.n * kTile;
-    Tile c;
-    product_tile<false, false>(a.p, m0, n0, a.add.rows - n0, 0, a.p.depth, lds, c);
+    const uint32_t m0 = at.m * kSize, n0 = at.n * kSize;
+    Tile<kSize> c;
+    product_tile<false, false, kSize>(a.p, m0, n0, a.add.rows - n0, 0, a.p.depth, lds, c);
     add_adapters(a.add, m0, n0, c);
     __syncthreads();
     tile_to_lds(c, lds);
     __syncthreads();
-    store_rows(lds, a.out, a.out_stride, m0, a.add.outer - m0, [&](uint32_t n) {
+    store_rows<kSize>(lds, a.out, a.out_stride, m0, a.add.outer - m0, [&](uint32_t n) {
         return n0 + n < a.add.rows ? int64_t(n0 + n) : int64_t(-1);
     });
+}
+
+struct PartArgs {
+    Product p;
+    float* parts;                          // [splits][rows][stride] binary32
+    uint64_t stride;
+    uint32_t rows, outer;
+};
+
+// Where there are few tiles their sums are divided too, and joined with B u.
+template <int kSize>
+__global__ __launch_bounds__(2 * kSize, 2) void es_adapt_part_kernel(PartArgs a) {
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+    const Place at = place_of(blockIdx.x, a.p);
+    const uint32_t m0 = at.m * kSize, n0 = at.n * kSize, k0 = at.split * a.p.split_depth;
+    const uint32_t n_have = a.rows - n0, m_have = a.outer - m0;
+    Tile<kSize> c;
+    product_tile<false, false, kSize>(a.p, m0, n0, n_have, k0, min(a.p.depth, k0 + a.p.split_depth), lds, c);
+    float* const to = a.parts + (uint64_t(at.split) * a.rows + n0) * a.stride + m0;
+    for_words(c, [&](const f32x4_t& v, uint32_t m, uint32_t n) {
+        if (m < m_have && n < n_have) store<f32x4_t>(to + n * a.stride + m, v);   // (stride: a multiple of 4)
+    });
+}
+
+struct JoinArgs {
+    const float* parts;
+    uint64_t stride;
+    uint32_t splits;
+    AddArgs add;
+    uint16_t* out;
+    uint64_t out_stride;
+};
+
+// Four results a lane: their parts in one order, and their row's B u.
+__global__ __launch_bounds__(256) void es_adapt_join_kernel(JoinArgs a) {
+    const uint32_t n = blockIdx.y, m = 4 * (blockIdx.x * 256 + threadIdx.x);
+    if (m >= a.add.outer) return;
+    const int32_t member = a.add.index[n];
+    const float* const from = a.parts + uint64_t(n) * a.stride + m;
+    f32x4_t v = load<f32x4_t>(from);
+    for (uint32_t s = 1; s < a.splits; ++s) {
+        const f32x4_t w = load<f32x4_t>(from + uint64_t(s) * a.add.rows * a.stride);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] += w[e];
+    }
+    v = with_adapter(a.add, v, n, m, a.add.outer, member);
+    store_results(a.out + uint64_t(n) * a.out_stride + m, v, a.add.outer - m);
 }
 
 struct FewArgs {
@@ -276,51 +375,8 @@ __global__ __launch_bounds__(256, 2) void es_adapt_stream_kernel(StreamArgs a) {
         for (int j = 0; j < S::kCols; ++j) {
             const uint32_t n = 16 * j + (lane & 15);
             if (n >= a.s.rows) continue;
-            const int32_t member = a.add.index[n];
-            f32x4_t v = t.c[0][j];
-            if (member >= int32_t(a.add.members)) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = eskv::nan();
-            } else if (member >= 0) {
-                const uint16_t* const b = a.add.b + uint64_t(member) * a.add.outer * a.add.rank;
-                const uint16_t* const u = a.add.u + uint64_t(n) * a.add.rank;
-                float low[4] = {};
-                // (the words of 16 of the rank on their way at a time)
-                for (uint32_t r0 = 0; r0 < a.add.rank; r0 += 16) {
-                    u32x4_t q[2], p[2][4];
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const uint32_t r = min(r0 + 8 * h, a.add.rank - 8);
-                        q[h] = load<u32x4_t>(u + r);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            p[h][e] = load<u32x4_t>(b + uint64_t(min(m + e, end - 1)) * a.add.rank + r);
-                    }
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        if (r0 + 8 * h >= a.add.rank) break;
-                        float x[8];
-                        eskv::unpack8(q[h], x);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            float y[8];
-                            eskv::unpack8(p[h][e], y);
-#pragma unroll
-                            for (int z = 0; z < 8; ++z) low[e] = __builtin_fmaf(x[z], y[z], low[e]);
-                        }
-                    }
-                }
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] += low[e];
-            }
-            uint16_t* const to = a.out + uint64_t(n) * a.out_stride + m;
-            const u32x2_t w = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
-            if (m + 4 <= end) {
-                eskv::store_row4(to, w);
-            } else {
-                for (uint32_t e = 0; m + e < end; ++e)
-                    store<uint16_t>(to + e, static_cast<uint16_t>(w[e / 2] >> (16 * (e % 2))));
-            }
+            store_results(a.out + uint64_t(n) * a.out_stride + m,
+                          with_adapter(a.add, t.c[0][j], n, m, end, a.add.index[n]), end - m);
         }
     });
 }

@@ -16,10 +16,10 @@
 
 using namespace es_host;
 using esmm::kDepth;
-using esmm::kLdsBytes;
-using esmm::kThreads;
+using esmm::kSmallTile;
 using esmm::kTile;
 using esmm::Product;
+using esmm::Shape;
 using esmm::Side;
 
 namespace {
@@ -214,20 +214,31 @@ struct GradientPlan {
     }
 };
 
-Product product(Side a, Side b, uint32_t m, uint32_t n, uint32_t depth, const uint32_t* count) {
+// How many tiles of `size` an m x n product has.
+uint64_t tiles_of(uint64_t m, uint64_t n, uint32_t size) {
+    return (m + size - 1) / size * ((n + size - 1) / size);
+}
+
+Product product(Side a, Side b, uint32_t m, uint32_t n, uint32_t depth, const uint32_t* count,
+                uint32_t size) {
     Product p{};
     p.a = a;
     p.b = b;
     p.depth = depth;
-    p.m_tiles = (m + kTile - 1) / kTile;
-    p.n_tiles = (n + kTile - 1) / kTile;
+    p.m_tiles = (m + size - 1) / size;
+    p.n_tiles = (n + size - 1) / size;
     p.splits = 1;
     p.split_depth = depth;
     p.count = count;
     return p;
 }
 
-dim3 grid_of(const Product& p) { return dim3(p.m_tiles * p.n_tiles * p.splits); }
+// A kernel over the tiles of a product.
+template <int kSize, class Kernel, class Args>
+void launch_tiles(Kernel kernel, const Args& a, hipStream_t s) {
+    hipLaunchKernelGGL(kernel, dim3(a.p.m_tiles * a.p.n_tiles * a.p.splits), dim3(Shape<kSize>::kThreads),
+                       Shape<kSize>::kLds, s, a);
+}
 
 // Flags, list and packed rows of a call.
 int list_rows(const char* name, const eshead::RowArgs& rows, const Lists& l, const void* x,
@@ -411,12 +422,12 @@ int es_head_score(const es_head_score_t* args, es_stream_t stream) try {
         const uint32_t have = std::min(plan.head.piece, x.vocab - v0);
         const Side w = head_side(plan.head, x.weight, x.w_stride, plan.w, v0, have, x.hidden, s);
         eshead::StatsArgs t{};
-        t.p = product(w, plan.lists.deep(), have, x.rows, x.hidden, plan.lists.count);
+        t.p = product(w, plan.lists.deep(), have, x.rows, x.hidden, plan.lists.count, kTile);
         t.parts = plan.parts;
         t.parts_stride = plan.tiles;
         t.part0 = v0 / kTile;
         t.factor = x.scale * eshead::kLog2e;
-        hipLaunchKernelGGL(eshead::es_head_stats_kernel, grid_of(t.p), dim3(kThreads), kLdsBytes, s, t);
+        launch_tiles<kTile>(eshead::es_head_stats_kernel<kTile>, t, s);
         rc = launch_error("es_head_stats_kernel launch");
         if (rc != ES_OK) return rc;
     }
@@ -511,13 +522,13 @@ int es_head_gradient(const es_head_gradient_t* args, es_stream_t stream) try {
         const uint32_t have = std::min(plan.head.piece, x.vocab - v0);
         const Side w = head_side(plan.head, x.weight, x.w_stride, plan.w, v0, have, x.hidden, s);
         eshead::ProbArgs a{};
-        a.p = product(w, l.deep(), have, x.rows, x.hidden, l.count);
+        a.p = product(w, l.deep(), have, x.rows, x.hidden, l.count, kTile);
         a.factor = plan.factor;
         a.minus_lse = plan.minus_lse;
         a.d = plan.d;
         a.d_stride = plan.head.piece;
         a.scale = x.scale * eshead::kLog2e;
-        hipLaunchKernelGGL(eshead::es_head_prob_kernel, grid_of(a.p), dim3(kThreads), kLdsBytes, s, a);
+        launch_tiles<kTile>(eshead::es_head_prob_kernel<kTile>, a, s);
         eshead::EntryArgs e{};
         e.list = l.list;
         e.count = l.count;
@@ -541,7 +552,8 @@ int es_head_gradient(const es_head_gradient_t* args, es_stream_t stream) try {
             eshead::RowGradArgs g{};
             // along the tile the head's rows are as wide as they are stored
             const uint32_t width = plan.head.copied ? plan.head.padded : x.hidden;
-            g.p = product(Side{w.at, w.stride, width}, d_deep, x.hidden, x.rows, have, l.count);
+            g.p = product(Side{w.at, w.stride, width}, d_deep, x.hidden, x.rows, have, l.count,
+                          kTile);
             g.p.splits = plan.splits;
             g.p.split_depth = plan.split_depth;
             g.parts = plan.parts;
@@ -554,19 +566,17 @@ int es_head_gradient(const es_head_gradient_t* args, es_stream_t stream) try {
                 g.out_stride = x.dx_stride;
                 g.list = l.list;
             }
-            hipLaunchKernelGGL(eshead::es_head_row_grad_kernel, grid_of(g.p), dim3(kThreads), kLdsBytes,
-                               s, g);
+            launch_tiles<kTile>(eshead::es_head_row_grad_kernel<kTile>, g, s);
         }
         if (x.d_weight != nullptr) {
             eshead::HeadGradArgs g{};
             const Side d_wide{plan.d, plan.head.piece, plan.head.piece};
-            g.p = product(l.wide(), d_wide, x.hidden, have, l.rows, l.count);
+            g.p = product(l.wide(), d_wide, x.hidden, have, l.rows, l.count, kTile);
             g.out = static_cast<uint16_t*>(x.d_weight) + v0 * x.dw_stride;
             g.out_stride = x.dw_stride;
             g.n_have = have;
             g.hidden = x.hidden;
-            hipLaunchKernelGGL(eshead::es_head_weight_grad_kernel, grid_of(g.p), dim3(kThreads), kLdsBytes,
-                               s, g);
+            launch_tiles<kTile>(eshead::es_head_weight_grad_kernel<kTile>, g, s);
         }
         rc = launch_error("es_head_gradient kernel launch");
         if (rc != ES_OK) return rc;
@@ -636,8 +646,28 @@ struct AdaptPlan {
         x = nullptr;
         if (copied) x = room.take<uint16_t>(uint64_t(packed_rows) * padded);
         is_copied = copied;
+        // Tiles of 128 x 128 results where the card holds them at once, of 256 x 256 where there
+        // are more.  5120 x 5120: 1000 rows (320 small tiles) 77 and 120 us, 2000 (640) 137 and 127;
+        // 5120 x 17408: 300 rows (408) 108 and 137.
+        const uint64_t tiles = tiles_of(a.outer, a.rows, kSmallTile);
+        low = !few && tiles <= 2 * kCus;
+        splits = 1;
+        split_depth = static_cast<uint32_t>(up(a.inner, kDepth));
+        parts = nullptr;
+        parts_stride = up(a.outer, 4);
+        // Few tiles' sums are divided, if a part is worth the join: 5120 x 5120, 100 rows (40
+        // tiles) 79 us whole and 48 divided, 300 (120) 65 and 51, 700 (240) 66 and 77; 1024 x
+        // 1024, 1000 rows (64) 21 and 26.
+        const uint64_t most = low && tiles <= 128 ? std::min<uint64_t>(2 * kCus / tiles, a.inner / 1024) : 1;
+        if (most < 2) return;
+        split_depth = static_cast<uint32_t>(up((a.inner + most - 1) / most, kDepth));
+        splits = (a.inner + split_depth - 1) / split_depth;
+        if (splits > 1) parts = room.take<float>(uint64_t(splits) * a.rows * parts_stride);
     }
-    bool is_copied, few;
+    bool is_copied, few, low;
+    uint32_t splits, split_depth;
+    float* parts;
+    uint64_t parts_stride;
 };
 
 }  // namespace
@@ -704,9 +734,22 @@ int es_adapt_project(const es_adapt_t* args, es_stream_t stream) try {
     small.rank = x.rank;
     const esadapt::AddArgs add{x.index, plan.u, static_cast<const uint16_t*>(x.b), x.rows, x.outer,
                                x.members, x.rank};
-    if (plan.few) {
+    // u: a wave for each element of few, otherwise 32 rows a workgroup for each member among
+    // them: 70 rows of 5120 at rank 16 4 us and 21, 300 12 and 14
+    if (plan.few || uint64_t(x.rows) * x.rank <= 4096) {
         hipLaunchKernelGGL(esadapt::es_adapt_few_small_kernel, dim3(x.rows, (x.rank + 3) / 4), dim3(256), 0,
                            s, small);
+    } else {
+        const auto kernel = x.rank <= 16   ? esadapt::es_adapt_small_kernel<1, 3>
+                            : x.rank <= 32 ? esadapt::es_adapt_small_kernel<2, 2>
+                                           : esadapt::es_adapt_small_kernel<4, 1>;
+        const uint32_t lds = esfew::kWaves * (x.rank <= 16   ? esring::Ring<1, 2, 3>::kBytes
+                                              : x.rank <= 32 ? esring::Ring<2, 2, 2>::kBytes
+                                                             : esring::Ring<4, 2, 1>::kBytes);
+        hipLaunchKernelGGL(kernel, dim3((x.rows + esadapt::kSmallRows - 1) / esadapt::kSmallRows),
+                           dim3(64 * esfew::kWaves), lds, s, small);
+    }
+    if (plan.few) {
         // A matrix of many rows is divided among workgroups that stage the rows of x for
         // four waves at a time, one of few rows among those whose waves share a sum.  5120 x
         // 5120: 1 row 22 and 14 us (streamed, in rings), 16 rows 23 and 15; 5120 x 17408: 1 row
@@ -746,22 +789,37 @@ int es_adapt_project(const es_adapt_t* args, es_stream_t stream) try {
             launch(esadapt::es_adapt_few_kernel<2, 4, 1>, 2, esring::Ring<2, 4, 1>::kBytes);
         return launch_error("es_adapt_few_kernel launch");
     }
-    const auto small_kernel = x.rank <= 16   ? esadapt::es_adapt_small_kernel<1, 3>
-                              : x.rank <= 32 ? esadapt::es_adapt_small_kernel<2, 2>
-                                             : esadapt::es_adapt_small_kernel<4, 1>;
-    const uint32_t small_lds = esfew::kWaves * (x.rank <= 16   ? esring::Ring<1, 2, 3>::kBytes
-                                                : x.rank <= 32 ? esring::Ring<2, 2, 2>::kBytes
-                                                               : esring::Ring<4, 2, 1>::kBytes);
-    hipLaunchKernelGGL(small_kernel,
-                       dim3((x.rows + esadapt::kSmallRows - 1) / esadapt::kSmallRows), dim3(64 * esfew::kWaves),
-                       small_lds, s, small);
     esadapt::TileArgs a{};
-    a.p = product(Side{static_cast<const uint16_t*>(x.weight), x.w_stride, x.outer}, rows, x.outer, x.rows,
-                  x.inner, nullptr);
+    const Side weight{static_cast<const uint16_t*>(x.weight), x.w_stride, x.outer};
+    if (plan.splits > 1) {
+        esadapt::PartArgs q{};
+        q.p = product(weight, rows, x.outer, x.rows, x.inner, nullptr, kSmallTile);
+        q.p.splits = plan.splits;
+        q.p.split_depth = plan.split_depth;
+        q.parts = plan.parts;
+        q.stride = plan.parts_stride;
+        q.rows = x.rows;
+        q.outer = x.outer;
+        launch_tiles<kSmallTile>(esadapt::es_adapt_part_kernel<kSmallTile>, q, s);
+        esadapt::JoinArgs j{};
+        j.parts = plan.parts;
+        j.stride = plan.parts_stride;
+        j.splits = plan.splits;
+        j.add = add;
+        j.out = static_cast<uint16_t*>(x.out);
+        j.out_stride = x.out_stride;
+        hipLaunchKernelGGL(esadapt::es_adapt_join_kernel, dim3((x.outer + 1023) / 1024, x.rows), dim3(256), 0,
+                           s, j);
+        return launch_error("es_adapt_join_kernel launch");
+    }
+    a.p = product(weight, rows, x.outer, x.rows, x.inner, nullptr, plan.low ? kSmallTile : kTile);
     a.add = add;
     a.out = static_cast<uint16_t*>(x.out);
     a.out_stride = x.out_stride;
-    hipLaunchKernelGGL(esadapt::es_adapt_tile_kernel, grid_of(a.p), dim3(kThreads), kLdsBytes, s, a);
+    if (plan.low)
+        launch_tiles<kSmallTile>(esadapt::es_adapt_tile_kernel<kSmallTile>, a, s);
+    else
+        launch_tiles<kTile>(esadapt::es_adapt_tile_kernel<kTile>, a, s);
     return launch_error("es_adapt_project kernel launch");
 } catch (const std::bad_alloc&) {
     return fail(ES_ERR_NOMEM, "es_adapt_project: host allocation failed");

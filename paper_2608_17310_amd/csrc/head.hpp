@@ -180,26 +180,27 @@ struct StatsArgs {
 };
 
 // A tile's rows of logits as maxima and sums, in units of log 2.
-__global__ __launch_bounds__(kThreads, 2) void es_head_stats_kernel(StatsArgs a) {
+template <int kSize>
+__global__ __launch_bounds__(2 * kSize, 2) void es_head_stats_kernel(StatsArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     const Place at = place_of(blockIdx.x, a.p);
-    const uint32_t m0 = at.m * kTile, n0 = at.n * kTile;
+    const uint32_t m0 = at.m * kSize, n0 = at.n * kSize;
     const uint32_t count = *a.p.count;
     if (n0 >= count) return;
-    Tile c;
-    product_tile<false, false>(a.p, m0, n0, count - n0, 0, a.p.depth, lds, c);
+    Tile<kSize> c;
+    product_tile<false, false, kSize>(a.p, m0, n0, count - n0, 0, a.p.depth, lds, c);
     __syncthreads();
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const uint32_t m_have = a.p.a.extent - m0;
-    float* const pair = reinterpret_cast<float*>(lds);   // [2 waves of m][256 n] pairs
+    float* const pair = reinterpret_cast<float*>(lds);   // [2 waves of m][n] pairs
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         float top = -eskv::inf();
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < c.kBlocks; ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const uint32_t m = 128 * (wave & 1) + 16 * i + 4 * (lane >> 4) + e;
+                const uint32_t m = c.m_of(wave, lane, i) + e;
                 const float z = m < m_have ? c.x[i][j][e] * a.factor : -eskv::inf();
                 c.x[i][j][e] = z;
                 top = fmaxf(top, z);
@@ -209,24 +210,24 @@ __global__ __launch_bounds__(kThreads, 2) void es_head_stats_kernel(StatsArgs a)
         const float from = top == -eskv::inf() ? 0.0f : top;
         float sum = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < c.kBlocks; ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f(c.x[i][j][e] - from);
         sum += __shfl_xor(sum, 16);
         sum += __shfl_xor(sum, 32);
         if (lane < 16) {
             const uint32_t n = 64 * (wave >> 1) + 16 * j + lane;
-            pair[2 * (256 * (wave & 1) + n)] = top;
-            pair[2 * (256 * (wave & 1) + n) + 1] = sum;
+            pair[2 * (kSize * (wave & 1) + n)] = top;
+            pair[2 * (kSize * (wave & 1) + n) + 1] = sum;
         }
     }
     __syncthreads();
     const uint32_t n = threadIdx.x;
-    if (n < kTile && n0 + n < count) {
-        const float t0 = pair[2 * n], t1 = pair[2 * (256 + n)];
+    if (n < kSize && n0 + n < count) {
+        const float t0 = pair[2 * n], t1 = pair[2 * (kSize + n)];
         const float top = fmaxf(t0, t1), from = top == -eskv::inf() ? 0.0f : top;
         const float sum = pair[2 * n + 1] * __builtin_amdgcn_exp2f(t0 - from) +
-                          pair[2 * (256 + n) + 1] * __builtin_amdgcn_exp2f(t1 - from);
+                          pair[2 * (kSize + n) + 1] * __builtin_amdgcn_exp2f(t1 - from);
         float* const to = a.parts + 2 * ((n0 + n) * a.parts_stride + a.part0 + at.m);
         to[0] = top;
         to[1] = sum;
@@ -561,33 +562,34 @@ struct ProbArgs {
 
 // The logits' gradients without what their ids add: factor softmax(z), as bf16 (RNE):
 // both products that take them have the matrix unit's operands.
-__global__ __launch_bounds__(kThreads, 2) void es_head_prob_kernel(ProbArgs a) {
+template <int kSize>
+__global__ __launch_bounds__(2 * kSize, 2) void es_head_prob_kernel(ProbArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     const Place at = place_of(blockIdx.x, a.p);
-    const uint32_t m0 = at.m * kTile, n0 = at.n * kTile;
+    const uint32_t m0 = at.m * kSize, n0 = at.n * kSize;
     const uint32_t count = *a.p.count;
     if (n0 >= count) return;
-    Tile c;
-    product_tile<false, false>(a.p, m0, n0, count - n0, 0, a.p.depth, lds, c);
+    Tile<kSize> c;
+    product_tile<false, false, kSize>(a.p, m0, n0, count - n0, 0, a.p.depth, lds, c);
     __syncthreads();
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const uint32_t m_have = a.p.a.extent - m0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const uint32_t n = n0 + 64 * (wave >> 1) + 16 * j + (lane & 15);
+        const uint32_t n = n0 + c.n_of(wave, lane, j);
         const float f = a.factor[n], l = a.minus_lse[n];
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < c.kBlocks; ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const uint32_t m = 128 * (wave & 1) + 16 * i + 4 * (lane >> 4) + e;
+                const uint32_t m = c.m_of(wave, lane, i) + e;
                 const float p = f * __builtin_amdgcn_exp2f(__builtin_fmaf(c.x[i][j][e], a.scale, l));
                 c.x[i][j][e] = m < m_have ? p : 0.0f;
             }
     }
     tile_to_lds(c, lds);
     __syncthreads();
-    store_rows(lds, a.d, a.d_stride, m0, kTile, [&](uint32_t n) { return int64_t(n0 + n); });
+    store_rows<kSize>(lds, a.d, a.d_stride, m0, kSize, [&](uint32_t n) { return int64_t(n0 + n); });
 }
 
 struct EntryArgs {
@@ -637,20 +639,21 @@ struct RowGradArgs {
     const uint32_t* list;
 };
 
-__global__ __launch_bounds__(kThreads, 2) void es_head_row_grad_kernel(RowGradArgs a) {
+template <int kSize>
+__global__ __launch_bounds__(2 * kSize, 2) void es_head_row_grad_kernel(RowGradArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     const Place at = place_of(blockIdx.x, a.p);
-    const uint32_t m0 = at.m * kTile, n0 = at.n * kTile;
+    const uint32_t m0 = at.m * kSize, n0 = at.n * kSize;
     const uint32_t count = *a.p.count;
     if (n0 >= count) return;
     const uint32_t k0 = at.split * a.p.split_depth;
-    Tile c;
-    product_tile<true, false>(a.p, m0, n0, count - n0, k0, min(a.p.depth, k0 + a.p.split_depth), lds, c);
+    Tile<kSize> c;
+    product_tile<true, false, kSize>(a.p, m0, n0, count - n0, k0, min(a.p.depth, k0 + a.p.split_depth), lds, c);
     if (a.out != nullptr) {
         __syncthreads();
         tile_to_lds(c, lds);
         __syncthreads();
-        store_rows(lds, a.out, a.out_stride, m0, a.hidden - m0, [&](uint32_t n) {
+        store_rows<kSize>(lds, a.out, a.out_stride, m0, a.hidden - m0, [&](uint32_t n) {
             return n0 + n < count ? int64_t(a.list[n0 + n]) : int64_t(-1);
         });
         return;
@@ -706,17 +709,18 @@ struct HeadGradArgs {
     uint32_t n_have, hidden;               // rows of the piece
 };
 
-__global__ __launch_bounds__(kThreads, 2) void es_head_weight_grad_kernel(HeadGradArgs a) {
+template <int kSize>
+__global__ __launch_bounds__(2 * kSize, 2) void es_head_weight_grad_kernel(HeadGradArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     const Place at = place_of(blockIdx.x, a.p);
-    const uint32_t m0 = at.m * kTile, n0 = at.n * kTile;
+    const uint32_t m0 = at.m * kSize, n0 = at.n * kSize;
     const uint32_t depth = (*a.p.count + kDepth - 1) / kDepth * kDepth;   // zeros behind the rows
-    Tile c;
-    product_tile<true, true>(a.p, m0, n0, a.n_have - n0, 0, depth, lds, c);
+    Tile<kSize> c;
+    product_tile<true, true, kSize>(a.p, m0, n0, a.n_have - n0, 0, depth, lds, c);
     __syncthreads();
     tile_to_lds(c, lds);
     __syncthreads();
-    store_rows(lds, a.out, a.out_stride, m0, a.hidden - m0, [&](uint32_t n) {
+    store_rows<kSize>(lds, a.out, a.out_stride, m0, a.hidden - m0, [&](uint32_t n) {
         return n0 + n < a.n_have ? int64_t(n0 + n) : int64_t(-1);
     });
 }

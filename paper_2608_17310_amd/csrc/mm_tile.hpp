@@ -23,11 +23,16 @@ using eskv::u32x2_t;
 using eskv::u32x4_t;
 
 constexpr int kTile = 256;                 // results of a tile in either direction
+constexpr int kSmallTile = 128;            //   where there are few of them
 constexpr int kDepth = 64;                 // of the summed dimension, staged at a time
-constexpr int kThreads = 512;
-constexpr uint32_t kSideBytes = kTile * kDepth * 2;
-constexpr uint32_t kPitch = kTile * 2 + 16;          // of a row of results in LDS
-constexpr uint32_t kLdsBytes = kTile * kPitch;       // the results are the most that it holds
+
+template <int kSize>
+struct Shape {
+    static constexpr int kThreads = 2 * kSize;                     // waves of kSize / 2 by 64 results
+    static constexpr uint32_t kSide = kSize * kDepth * 2;          // bytes of a stage's side
+    static constexpr uint32_t kPitch = kSize * 2 + 16;             // of a row of results in LDS
+    static constexpr uint32_t kLds = 4 * kSide > kSize * kPitch ? 4 * kSide : kSize * kPitch;
+};
 
 // One operand.  Deep: element (i, k) at at[i stride + k], wide: at[k stride + i],
 // i along the tile and k along the sum.  16-byte aligned, stride a multiple of 8.
@@ -45,8 +50,8 @@ struct Product {
     uint32_t depth;
     uint32_t m_tiles, n_tiles, splits;     // splits: of the sum, `split_depth` each
     uint32_t split_depth;                  // a multiple of 64
-    const uint32_t* count;                 // rows n that exist, where the device knows it
-    uint32_t count_is_depth;               //   or, of a product over them, the sum's length
+    const uint32_t* count;                 // rows n that exist, where the device knows it (of a
+                                           //   product over them, the sum's length)
 };
 
 struct Place {
@@ -93,18 +98,24 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) {
     return static_cast<uint32_t>(reinterpret_cast<uintptr_t>(p));   // of the shared aperture
 }
 
-// A side's way into LDS.  A stage of 64 of the sum is 32 KB.  Deep: [256 rows][8
+// A side's way into LDS, 4 KB a wave and stage of 64 of the sum.  Deep: [kSize rows][8
 // words of 16 bytes], word w of row i stored at w ^ ((i >> 1) & 7): sixteen rows' words
 // of one w, which a read of an operand takes at a time, fill the banks once.
-// Wide: [64][32 words], word w of row k at w ^ (4 (k & 3) + 2 (k >> 3 & 1)): the words that
+// Wide: [64][kSize / 8 words], word w of row k at w ^ (4 (k & 3) + 2 (k >> 3 & 1)): the words that
 // a transposing read takes at a time, four k's and the four eight further on, do.
-template <bool kWide>
+template <bool kWide, int kSize>
 struct Stage {
+    static constexpr uint32_t kWords = kSize / 8;        // of a k's row, where wide
     uint64_t base;                         // of the next stage
     uint64_t bytes;                        // from there to the array's end
     uint64_t step;                         // bytes from stage to stage
     uint32_t off[4];
-    uint32_t dst, lane_k, word;
+    uint32_t dst;
+
+    // (wide) the k of a stage that load x brings for a lane
+    static __device__ __forceinline__ uint32_t k_of(uint32_t wave, uint32_t x, uint32_t lane) {
+        return (wave * 4 + x) * (64 / kWords) + lane / kWords;
+    }
 
     __device__ __forceinline__ void init(const Side& s, uint32_t i0, uint32_t k0, uint32_t k_end,
                                          uint32_t wave, uint32_t lane) {
@@ -116,8 +127,8 @@ struct Stage {
             step = 2 * kDepth * s.stride;
 #pragma unroll
             for (uint32_t x = 0; x < 4; ++x) {
-                const uint32_t k = (wave * 4 + x) * 2 + (lane >> 5);
-                const uint32_t w = (lane & 31) ^ ((k & 3) << 2) ^ ((k >> 3 & 1) << 1);
+                const uint32_t k = k_of(wave, x, lane);
+                const uint32_t w = (lane % kWords) ^ ((k & 3) << 2) ^ ((k >> 3 & 1) << 1);
                 off[x] = k * uint32_t(2 * s.stride) + 16 * min(w, last / 8);
             }
         } else {
@@ -152,7 +163,7 @@ struct Stage {
                                               const Side& s, uint32_t wave, uint32_t lane) const {
         uint32_t o = off[x];
         if constexpr (kWide) {
-            const uint32_t k = (wave * 4 + x) * 2 + (lane >> 5);
+            const uint32_t k = k_of(wave, x, lane);
             if (k >= have) o -= (k - (have - 1)) * uint32_t(2 * s.stride);
         } else {
             const uint32_t i = (wave * 4 + x) * 8 + (lane >> 3);
@@ -165,7 +176,7 @@ struct Stage {
 
 // A wave's reads of a side: block b of 16 rows from row `from`, step s of 32 of the sum.
 // The operand of lane l: row l % 16 of the block, elements 8 (l / 16) .. of the step.
-template <bool kWide, int kBlocks>
+template <bool kWide, int kSize, int kBlocks>
 struct Reader {
     uint32_t at[kWide ? kBlocks : 2];
 
@@ -175,7 +186,7 @@ struct Reader {
 #pragma unroll
             for (uint32_t b = 0; b < kBlocks; ++b) {
                 const uint32_t i = from + 16 * b + 4 * (lane & 3);
-                at[b] = k * 512 + (((i >> 3) ^ (kk << 2) ^ ((lane >> 4 & 1) << 1)) << 4) + ((i & 4) << 1);
+                at[b] = k * (2 * kSize) + (((i >> 3) ^ (kk << 2) ^ ((lane >> 4 & 1) << 1)) << 4) + ((i & 4) << 1);
             }
         } else {
             const uint32_t i = from + (lane & 15);
@@ -192,7 +203,7 @@ struct Reader {
 #pragma unroll
             for (int t = 0; t < 2; ++t)
                 x.half[t] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                    (Shared*)(lds + at[b] + 16384 * s + 2048 * t));
+                    (Shared*)(lds + at[b] + 64 * kSize * s + 8 * kSize * t));
             return x.whole;
         } else {
             return *reinterpret_cast<const bf16x8_t*>(lds + at[s] + 2048 * b);
@@ -200,10 +211,19 @@ struct Reader {
     }
 };
 
-// What a wave holds of a tile: rows m 128 (wave % 2) + 16 i + 4 (lane / 16) + e in
+// What a wave holds of a tile: rows m kSize / 2 (wave % 2) + 16 i + 4 (lane / 16) + e in
 // element e, and rows n 64 (wave / 2) + 16 j + lane % 16 (the waves' order is m first).
+template <int kSize>
 struct Tile {
-    f32x4_t x[8][4];
+    static constexpr int kBlocks = kSize / 32;
+    f32x4_t x[kBlocks][4];
+    // the first of the four rows m of block i, and the row n of block j
+    static __device__ __forceinline__ uint32_t m_of(uint32_t wave, uint32_t lane, int i) {
+        return kSize / 2 * (wave & 1) + 16 * i + 4 * (lane >> 4);
+    }
+    static __device__ __forceinline__ uint32_t n_of(uint32_t wave, uint32_t lane, int j) {
+        return 64 * (wave >> 1) + 16 * j + (lane & 15);
+    }
 };
 
 template <int n>
@@ -211,24 +231,30 @@ struct Count {
     static constexpr int value = n;
 };
 
-// Rows n0 .. n0 + n_have of n are there (more than 256 count as 256).  Waves whose rows
-// are not only stage: a tile with at most half of its rows takes half of the time.
-template <bool kWideA, bool kWideB>
+// Rows n0 .. n0 + n_have of n are there (more than the tile has count as all).  Two
+// stages in LDS: while the products of a stage's first step are made its second's
+// operands are read; then the stage is in registers and, once the next has landed, the
+// one after it may be asked for, a load to a product.  4096 rows of 5120 against 151936 (256 x
+// 256): 4.76 to 4.89 ms, 1.30 to 1.34 PFLOP/s, where one barrier and no loads between
+// products took 5.13 and loads half a step later 4.97; the clock is 1.9 GHz.
+template <bool kWideA, bool kWideB, int kSize>
 __device__ __forceinline__ void product_tile(const Product& p, uint32_t m0, uint32_t n0, uint32_t n_have,
-                                             uint32_t k0, uint32_t k_end, uint8_t* lds, Tile& c) {
+                                             uint32_t k0, uint32_t k_end, uint8_t* lds, Tile<kSize>& c) {
+    constexpr int kBlocks = Tile<kSize>::kBlocks, kProducts = 4 * kBlocks;   // of a step
+    constexpr uint32_t kSide = Shape<kSize>::kSide;
     const uint32_t lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int i = 0; i < kBlocks; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) c.x[i][j] = f32x4_t{0, 0, 0, 0};
     if (k0 >= k_end) return;
-    Stage<kWideA> sa;
-    Stage<kWideB> sb;
+    Stage<kWideA, kSize> sa;
+    Stage<kWideB, kSize> sb;
     sa.init(p.a, m0, k0, k_end, wave, lane);
     sb.init(p.b, n0, k0, k_end, wave, lane);
-    Reader<kWideA, 8> ra;
-    Reader<kWideB, 4> rb;
-    ra.init(128 * (wave & 1), lane);
+    Reader<kWideA, kSize, kBlocks> ra;
+    Reader<kWideB, kSize, 4> rb;
+    ra.init(kSize / 2 * (wave & 1), lane);
     rb.init(64 * (wave >> 1), lane);
     const uint32_t lds_at = uniform(lds_address(lds));
     uint32_t buf = 0;                                    // of the stage in use, 0 or 2 sides
@@ -240,27 +266,26 @@ __device__ __forceinline__ void product_tile(const Product& p, uint32_t m0, uint
                 sa.load(ba, lds_at + at, x);
             else
                 sa.load_last(ba, lds_at + at, x, k_end - k, p.a, wave, lane);
-            sb.load(bb, lds_at + at + kSideBytes, x);
+            sb.load(bb, lds_at + at + kSide, x);
         }
     };
-    bf16x8_t a[2][8], b[2][4];
+    bf16x8_t a[2][kBlocks], b[2][4];
     auto read = [&](int s) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) b[s][j] = rb.read(lds + buf + kSideBytes, s, j);
+        for (int j = 0; j < 4; ++j) b[s][j] = rb.read(lds + buf + kSide, s, j);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) a[s][i] = ra.read(lds + buf, s, i);
+        for (int i = 0; i < kBlocks; ++i) a[s][i] = ra.read(lds + buf, s, i);
     };
     // 16 x 16 x 32 a product: at the clock that the card's power leaves it makes 1.92
     // PFLOP/s with its reads from LDS where 32 x 32 x 16 makes 1.72
-    auto multiply = [&](int s, int from, int to) {
+    auto multiply = [&](int s, int from) {
 #pragma unroll
-        for (int i = from; i < to; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                c.x[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[s][i], b[s][j], c.x[i][j], 0, 0, 0);
+        for (int y = from; y < kProducts; ++y)
+            c.x[y / 4][y % 4] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[s][y / 4], b[s][y % 4],
+                                                                        c.x[y / 4][y % 4], 0, 0, 0);
     };
     // the reads of a step go out one to a product, from the first on
-    constexpr int kReads = (kWideA ? 16 : 8) + (kWideB ? 8 : 4), kMatrix = 0x8, kDsRead = 0x100;
+    constexpr int kReads = (kWideA ? 2 : 1) * kBlocks + (kWideB ? 8 : 4), kMatrix = 0x8, kDsRead = 0x100;
     auto interleave = [&](auto products) {
         constexpr int n = decltype(products)::value, each = (kReads + n - 1) / n;
 #pragma unroll
@@ -273,78 +298,74 @@ __device__ __forceinline__ void product_tile(const Product& p, uint32_t m0, uint
     issue(k0, 0);
     wait_staged();
     __builtin_amdgcn_s_barrier();
-    if (k0 + kDepth < k_end) issue(k0 + kDepth, 2 * kSideBytes);
-    if (64 * (wave >> 1) >= n_have) {
+    if (k0 + kDepth < k_end) issue(k0 + kDepth, 2 * kSide);
+    if (64 * (wave >> 1) >= n_have) {                    // a wave without rows only stages
         for (uint32_t k = k0; k + kDepth < k_end; k += kDepth) {
             wait_staged();
             __builtin_amdgcn_s_barrier();
             if (k + 2 * kDepth < k_end) issue(k + 2 * kDepth, buf);
-            buf ^= 2 * kSideBytes;
+            buf ^= 2 * kSide;
         }
         return;
     }
     read(0);
     auto first_step = [&]() {
         read(1);
-        multiply(0, 0, 8);
-        interleave(Count<32>{});
+        multiply(0, 0);
+        interleave(Count<kProducts>{});
         // all of the stage is in registers, and the next has landed
         wait_staged();
         __builtin_amdgcn_s_barrier();
-        buf ^= 2 * kSideBytes;
-    };
-    auto product = [&](int y) {                          // of the second step
-        c.x[y / 4][y % 4] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[1][y / 4], b[1][y % 4],
-                                                                    c.x[y / 4][y % 4], 0, 0, 0);
+        buf ^= 2 * kSide;
     };
     uint32_t k = k0;
     for (; k + 3 * kDepth <= k_end; k += kDepth) {       // the stage after the next is whole
         first_step();
-        const uint32_t old = lds_at + (buf ^ 2 * kSideBytes);
+        const uint32_t old = lds_at + (buf ^ 2 * kSide);
         const u32x4_t ba = sa.take(), bb = sb.take();
 #pragma unroll
-        for (uint32_t x = 0; x < 8; ++x) {               // a load to a product
+        for (uint32_t x = 0; x < 8; ++x) {
             if (x < 4)
                 sa.load(ba, old, x);
             else
-                sb.load(bb, old + kSideBytes, x - 4);
-            product(x);
+                sb.load(bb, old + kSide, x - 4);
+            c.x[x / 4][x % 4] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[1][x / 4], b[1][x % 4],
+                                                                        c.x[x / 4][x % 4], 0, 0, 0);
             __builtin_amdgcn_sched_barrier(0);
         }
         read(0);
-#pragma unroll
-        for (int y = 8; y < 32; ++y) product(y);
-        interleave(Count<24>{});
+        multiply(1, 8);
+        interleave(Count<kProducts - 8>{});
     }
     for (; k + kDepth < k_end; k += kDepth) {
         first_step();
-        if (k + 2 * kDepth < k_end) issue(k + 2 * kDepth, buf ^ 2 * kSideBytes);
+        if (k + 2 * kDepth < k_end) issue(k + 2 * kDepth, buf ^ 2 * kSide);
         read(0);
-#pragma unroll
-        for (int y = 0; y < 32; ++y) product(y);
-        interleave(Count<32>{});
+        multiply(1, 0);
+        interleave(Count<kProducts>{});
     }
     read(1);
-    multiply(0, 0, 8);
-    interleave(Count<32>{});
-    multiply(1, 0, 8);
+    multiply(0, 0);
+    interleave(Count<kProducts>{});
+    multiply(1, 0);
 }
 
 // f(x, m, n): the words of four results, rows m .. m + 3 and row n of the tile.
-template <class T, class F>
-__device__ __forceinline__ void for_words(T& c, F f) {
+template <int kSize, class F>
+__device__ __forceinline__ void for_words(const Tile<kSize>& c, F f) {
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            f(c.x[i][j], 128 * (wave & 1) + 16 * i + 4 * (lane >> 4), 64 * (wave >> 1) + 16 * j + (lane & 15));
+        for (int i = 0; i < Tile<kSize>::kBlocks; ++i)
+            f(c.x[i][j], c.m_of(wave, lane, i), c.n_of(wave, lane, j));
 }
 
 // Results as bf16 (RNE) into LDS, [n][m]; all waves have read their last operands.
-__device__ __forceinline__ void tile_to_lds(const Tile& c, uint8_t* lds) {
+template <int kSize>
+__device__ __forceinline__ void tile_to_lds(const Tile<kSize>& c, uint8_t* lds) {
     for_words(c, [&](const f32x4_t& x, uint32_t m, uint32_t n) {
-        *reinterpret_cast<u32x2_t*>(lds + n * kPitch + 2 * m) =
+        *reinterpret_cast<u32x2_t*>(lds + n * Shape<kSize>::kPitch + 2 * m) =
             u32x2_t{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
     });
 }
@@ -352,15 +373,16 @@ __device__ __forceinline__ void tile_to_lds(const Tile& c, uint8_t* lds) {
 // Rows of the tile from LDS to `out` (bf16, `stride` elements from row to row): row n
 // to row_of(n), which is negative for a row that is not written; m_have
 // results of each.
-template <class F>
+template <int kSize, class F>
 __device__ __forceinline__ void store_rows(const uint8_t* lds, uint16_t* out, uint64_t stride,
                                            uint32_t m0, uint32_t m_have, F row_of) {
-    const uint32_t word = threadIdx.x & 31;
+    constexpr uint32_t kWords = kSize / 8;
+    const uint32_t word = threadIdx.x % kWords;
 #pragma unroll 4
-    for (uint32_t n = threadIdx.x >> 5; n < kTile; n += kThreads / 32) {
+    for (uint32_t n = threadIdx.x / kWords; n < kSize; n += Shape<kSize>::kThreads / kWords) {
         const int64_t row = row_of(n);
         if (row < 0 || 8 * word >= m_have) continue;
-        const u32x4_t v = *reinterpret_cast<const u32x4_t*>(lds + n * kPitch + 16 * word);
+        const u32x4_t v = *reinterpret_cast<const u32x4_t*>(lds + n * Shape<kSize>::kPitch + 16 * word);
         uint16_t* const to = out + uint64_t(row) * stride + m0 + 8 * word;
         if (8 * word + 8 <= m_have) {
             store_row8(to, v);
