@@ -243,11 +243,12 @@ void launch_tiles(Kernel kernel, const Args& a, hipStream_t s) {
 // Flags, list and packed rows of a call.
 int list_rows(const char* name, const eshead::RowArgs& rows, const Lists& l, const void* x,
               uint64_t x_stride, eshead::PackArgs pack, hipStream_t s) {
-    const uint32_t per = rows.entries == 1 && rows.dx == nullptr ? 256 : 4;
-    hipLaunchKernelGGL(eshead::es_head_rows_kernel, dim3((rows.rows + per - 1) / per), dim3(256), 0, s,
-                       rows);
+    // (one id a row: the list's kernel looks at it)
+    if (rows.entries > 1)
+        hipLaunchKernelGGL(eshead::es_head_rows_kernel, dim3((rows.rows + 3) / 4), dim3(256), 0, s, rows);
     hipLaunchKernelGGL(eshead::es_head_list_kernel, dim3(1), dim3(1024), 0, s,
-                       eshead::ListArgs{l.flags, l.list, l.count, rows.rows});
+                       eshead::ListArgs{rows, l.list, l.count});
+    pack.out = rows;
     pack.from = static_cast<const uint16_t*>(x);
     pack.to = l.x;
     pack.stride = x_stride;
@@ -734,9 +735,13 @@ int es_adapt_project(const es_adapt_t* args, es_stream_t stream) try {
     small.rank = x.rank;
     const esadapt::AddArgs add{x.index, plan.u, static_cast<const uint16_t*>(x.b), x.rows, x.outer,
                                x.members, x.rank};
-    // u: a wave for each element of few, otherwise 32 rows a workgroup for each member among
-    // them: 70 rows of 5120 at rank 16 4 us and 21, 300 12 and 14
-    if (plan.few || uint64_t(x.rows) * x.rank <= 4096) {
+    // u: a wave for each of its elements reads two rows of `inner`, which the second cache
+    // serves at about 8 TB/s; a workgroup of 32 rows reads them and A once for each member among
+    // them, in some 7 us each at 5120.  Rank 16, of 5120: 70 rows of 8 members 4 and 21 us, 300 of
+    // 8 12 and 14, 300 of 300 12 and 310, 8403 of 16 (2560, rank 32) about 330 and 25.
+    const double one_by_one = 5e-7 * x.rows * x.rank * x.inner;
+    const double by_member = (1 + 32.0 * std::min(x.members, x.rows) / x.rows) * (1 + x.inner / 850.0);
+    if (plan.few || one_by_one < by_member) {
         hipLaunchKernelGGL(esadapt::es_adapt_few_small_kernel, dim3(x.rows, (x.rank + 3) / 4), dim3(256), 0,
                            s, small);
     } else {

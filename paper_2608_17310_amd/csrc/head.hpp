@@ -36,26 +36,9 @@ struct RowArgs {
     uint32_t rows, vocab, entries, hidden;
 };
 
-// One wave a row (one lane where it has one entry and no gradient to clear).
+// What becomes of a row of several ids: one wave a row.
 __global__ __launch_bounds__(256) void es_head_rows_kernel(RowArgs a) {
-    const uint32_t lane = threadIdx.x & 63;
-    if (a.entries == 1 && a.dx == nullptr) {
-        const uint32_t r = blockIdx.x * 256 + threadIdx.x;
-        if (r >= a.rows) return;
-        const int64_t id = a.ids[r];
-        uint8_t flag = id < 0 ? kDead : id < int64_t(a.vocab) ? kLive : kVoid;
-        if (flag == kLive && a.teacher != nullptr && a.teacher[r] == -eskv::inf()) flag = kEmpty;
-        a.flags[r] = flag;
-        if (flag == kVoid && a.status != nullptr) atomicOr(a.status, ES_HEAD_BAD_ID);
-        if (flag == kDead || flag == kVoid) {
-            const float v = flag == kVoid ? eskv::nan() : 0.0f;
-            if (a.loss != nullptr) a.loss[r] = v;
-            if (a.logp != nullptr) a.logp[r] = v;
-            if (a.lse != nullptr) a.lse[r] = v;
-        }
-        return;
-    }
-    const uint32_t r = blockIdx.x * 4 + (threadIdx.x >> 6);
+    const uint32_t lane = threadIdx.x & 63, r = blockIdx.x * 4 + (threadIdx.x >> 6);
     if (r >= a.rows) return;
     bool some = false, bad = false, weight = a.teacher == nullptr;
     for (uint32_t e = lane; e < a.entries; e += 64) {
@@ -68,12 +51,14 @@ __global__ __launch_bounds__(256) void es_head_rows_kernel(RowArgs a) {
     some = __any(some);
     bad = __any(bad);
     weight = __any(weight);
-    const uint8_t flag = bad ? kVoid : !some ? kDead : weight ? kLive : kEmpty;
-    if (lane == 0) {
-        a.flags[r] = flag;
-        if (bad && a.status != nullptr) atomicOr(a.status, ES_HEAD_BAD_ID);
-    }
-    if (flag != kDead && flag != kVoid) return;
+    if (lane == 0) a.flags[r] = bad ? kVoid : !some ? kDead : weight ? kLive : kEmpty;
+    if (bad && lane == 0 && a.status != nullptr) atomicOr(a.status, ES_HEAD_BAD_ID);
+}
+
+// Its results, where it has none of its own.  A wave's lanes.
+__device__ __forceinline__ void clear_row(const RowArgs& a, uint32_t r, uint32_t lane) {
+    const bool bad = a.flags[r] == kVoid;
+    if (!bad && a.flags[r] != kDead) return;
     const float v = bad ? eskv::nan() : 0.0f;
     if (lane == 0) {
         if (a.loss != nullptr) a.loss[r] = v;
@@ -82,28 +67,37 @@ __global__ __launch_bounds__(256) void es_head_rows_kernel(RowArgs a) {
     if (a.logp != nullptr)
         for (uint32_t e = lane; e < a.entries; e += 64) a.logp[uint64_t(r) * a.entries + e] = v;
     if (a.dx != nullptr)
-        for (uint32_t h = lane; h < a.hidden; h += 64)
-            a.dx[r * a.dx_stride + h] = bad ? 0x7FC0u : 0u;
+        for (uint32_t h = lane; h < a.hidden; h += 64) a.dx[r * a.dx_stride + h] = bad ? 0x7FC0u : 0u;
 }
 
 struct ListArgs {
-    const uint8_t* flags;
+    RowArgs rows;
     uint32_t* list;                        // live rows in order
     uint32_t* count;                       // [0]: how many
-    uint32_t rows;
 };
 
 // One workgroup: 16 rows a thread at a time.
 __global__ __launch_bounds__(1024) void es_head_list_kernel(ListArgs a) {
     __shared__ uint32_t waves[16];
-    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, rows = a.rows.rows;
     uint32_t base = 0;
-    for (uint32_t r0 = 0; r0 < a.rows; r0 += 16384) {
-        const uint32_t mine = r0 + 16 * threadIdx.x;
+    for (uint32_t r0 = 0; r0 < rows; r0 += 16384) {
+        // (rows of few calls are spread over the threads)
+        const uint32_t each = min((rows - r0 + 1023) / 1024, 16u), mine = r0 + each * threadIdx.x;
         uint32_t live = 0;
-        for (uint32_t i = 0; i < 16; ++i) {
-            if (mine + i >= a.rows) break;
-            const uint8_t f = a.flags[mine + i];
+        for (uint32_t i = 0; i < each; ++i) {
+            const uint32_t r = mine + i;
+            if (r >= rows) break;
+            uint8_t f;
+            if (a.rows.entries == 1) {
+                const int64_t id = a.rows.ids[r];
+                f = id < 0 ? kDead : id < int64_t(a.rows.vocab) ? kLive : kVoid;
+                if (f == kLive && a.rows.teacher != nullptr && a.rows.teacher[r] == -eskv::inf()) f = kEmpty;
+                if (f == kVoid && a.rows.status != nullptr) atomicOr(a.rows.status, ES_HEAD_BAD_ID);
+                a.rows.flags[r] = f;
+            } else {
+                f = a.rows.flags[r];
+            }
             live |= uint32_t(f == kLive || f == kEmpty) << i;
         }
         const uint32_t n = __popc(live);
@@ -140,6 +134,7 @@ struct PackArgs {
     const float *grad, *lse;
     float *factor, *minus_lse;
     float scale;                           // with its sign
+    RowArgs out;                           // of a call's rows: those that are not live are cleared
 };
 
 // Rows copied to where every row starts at a word of 16 bytes and ends in zeros; the
@@ -148,6 +143,7 @@ __global__ __launch_bounds__(256) void es_head_pack_kernel(PackArgs a) {
     const uint32_t lane = threadIdx.x & 63;
     const uint32_t i = blockIdx.x * 4 + (threadIdx.x >> 6);
     const uint32_t count = a.count != nullptr ? *a.count : a.rows;
+    if (a.list != nullptr && i < a.rows) clear_row(a.out, i, lane);
     if (i >= (count + kTile - 1) / kTile * kTile) return;
     const bool live = i < count;
     const uint32_t row = !live ? 0 : a.list != nullptr ? a.list[i] : i;
