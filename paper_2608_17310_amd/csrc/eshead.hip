@@ -60,6 +60,18 @@ bool word_rows(const void* p, uint64_t stride, uint32_t width) {
     return !odd(p, 16) && stride % 8 == 0 && width % 8 == 0;
 }
 
+// How many tiles of `size` an m x n product has.
+uint64_t tiles_of(uint64_t m, uint64_t n, uint32_t size) {
+    return (m + size - 1) / size * ((n + size - 1) / size);
+}
+
+// Tiles of 128 x 128 results where the card holds them at once (two a compute unit), of
+// 256 x 256 where there are more.  5120 x 5120: 1000 rows (320 small tiles) 77 and 120 us,
+// 2000 (640) 137 and 127; 5120 x 17408: 300 rows (408) 108 and 137.
+uint32_t tile_for(uint64_t m, uint64_t n) {
+    return tiles_of(m, n, kSmallTile) <= 2 * kCus ? kSmallTile : kTile;
+}
+
 // --------------------------------------------------------------------- head --
 
 int check_head(const char* name, const void* x, const void* weight, uint64_t x_stride,
@@ -156,6 +168,7 @@ bool streams(const es_head_score_t& x) {
 
 struct ScorePlan {
     bool few, streamed, ringed;
+    uint32_t size;                         // of a tile
     uint32_t share;
     HeadRows head;
     Lists lists;
@@ -172,7 +185,7 @@ struct ScorePlan {
             // A small vocabulary leaves the workgroups that stage x too few rows: 3 rows of 5120
             // against 8000 tokens 45 and 21 us (streamed, in rings), 40 of 2560 against 16000
             // 31 and 28, 32 of 1024 against 25000 17 and 26.
-            ringed = streams(x) && x.rows <= esfew::kRows && x.vocab <= 16384;
+            ringed = streams(x) && x.vocab <= 16384;
             streamed = streams(x) && !ringed;
             share = share_of(x.vocab, kCus, ~0u / 16);
             tiles = streamed ? (x.vocab + share - 1) / share : ringed ? (x.vocab + 31) / 32 : division.groups;
@@ -180,7 +193,8 @@ struct ScorePlan {
             w = nullptr;
             return;
         }
-        tiles = (x.vocab + kTile - 1) / kTile;
+        size = tile_for(head.piece, x.rows);
+        tiles = (x.vocab + size - 1) / size;
         parts = room.take<float>(uint64_t(2) * lists.rows * tiles);
         w = head.copied ? room.take<uint16_t>(uint64_t(head.piece) * head.padded) : nullptr;
     }
@@ -191,7 +205,7 @@ struct GradientPlan {
     HeadRows head;
     float *factor, *minus_lse, *parts;
     uint16_t *d, *w;
-    uint32_t splits, split_depth;
+    uint32_t splits, split_depth, size;    // of the rows' gradient, and its tiles
     GradientPlan(Room& room, const es_head_gradient_t& x)
         : lists(room, x.rows, x.hidden),
           head(x.weight, x.w_stride, x.vocab, x.hidden, 2 * uint64_t(lists.rows)) {
@@ -204,20 +218,18 @@ struct GradientPlan {
         parts = nullptr;
         if (x.d_x == nullptr) return;
         // the sum over the vocabulary in as many parts as fill the card
-        const uint32_t tiles = lists.rows / kTile * ((x.hidden + kTile - 1) / kTile);
-        const uint32_t most = std::max(1u, head.piece / 1024);
-        splits = std::min(most, std::max(1u, kCus / tiles));
+        const bool low = x.rows <= kSmallTile;
+        size = low ? kSmallTile : kTile;
+        const uint64_t tiles = tiles_of(x.rows, x.hidden, size);
+        const uint32_t most = std::max(1u, head.piece / (low ? 512 : 1024));
+        splits = static_cast<uint32_t>(
+            std::min<uint64_t>(most, std::max<uint64_t>(1, (low ? 2 * kCus : kCus) / tiles)));
         split_depth = static_cast<uint32_t>(up((head.piece + splits - 1) / splits, kDepth));
         splits = (head.piece + split_depth - 1) / split_depth;
         if (splits > 1 || head.pieces > 1)
             parts = room.take<float>(uint64_t(splits) * lists.rows * lists.padded);
     }
 };
-
-// How many tiles of `size` an m x n product has.
-uint64_t tiles_of(uint64_t m, uint64_t n, uint32_t size) {
-    return (m + size - 1) / size * ((n + size - 1) / size);
-}
 
 Product product(Side a, Side b, uint32_t m, uint32_t n, uint32_t depth, const uint32_t* count,
                 uint32_t size) {
@@ -387,7 +399,7 @@ int es_head_score(const es_head_score_t* args, es_stream_t stream) try {
         const uint32_t lds = esfew::kWaves * (x.rows <= 16   ? esring::Ring<2, 1, 3>::kBytes
                                               : x.rows <= 32 ? esring::Ring<2, 2, 2>::kBytes
                                                              : esring::Ring<2, 4, 1>::kBytes);
-        hipLaunchKernelGGL(kernel, dim3(plan.tiles), dim3(64 * esfew::kWaves), lds, s, f);
+        hipLaunchKernelGGL(kernel, dim3(plan.tiles, (x.rows + 63) / 64), dim3(64 * esfew::kWaves), lds, s, f);
         hipLaunchKernelGGL(eshead::es_head_score_kernel, dim3(x.rows), dim3(256), 0, s, a);
         return launch_error("es_head_ring_kernel launch");
     }
@@ -423,12 +435,15 @@ int es_head_score(const es_head_score_t* args, es_stream_t stream) try {
         const uint32_t have = std::min(plan.head.piece, x.vocab - v0);
         const Side w = head_side(plan.head, x.weight, x.w_stride, plan.w, v0, have, x.hidden, s);
         eshead::StatsArgs t{};
-        t.p = product(w, plan.lists.deep(), have, x.rows, x.hidden, plan.lists.count, kTile);
+        t.p = product(w, plan.lists.deep(), have, x.rows, x.hidden, plan.lists.count, plan.size);
         t.parts = plan.parts;
         t.parts_stride = plan.tiles;
-        t.part0 = v0 / kTile;
+        t.part0 = v0 / plan.size;
         t.factor = x.scale * eshead::kLog2e;
-        launch_tiles<kTile>(eshead::es_head_stats_kernel<kTile>, t, s);
+        if (plan.size == kTile)
+            launch_tiles<kTile>(eshead::es_head_stats_kernel<kTile>, t, s);
+        else
+            launch_tiles<kSmallTile>(eshead::es_head_stats_kernel<kSmallTile>, t, s);
         rc = launch_error("es_head_stats_kernel launch");
         if (rc != ES_OK) return rc;
     }
@@ -523,13 +538,17 @@ int es_head_gradient(const es_head_gradient_t* args, es_stream_t stream) try {
         const uint32_t have = std::min(plan.head.piece, x.vocab - v0);
         const Side w = head_side(plan.head, x.weight, x.w_stride, plan.w, v0, have, x.hidden, s);
         eshead::ProbArgs a{};
-        a.p = product(w, l.deep(), have, x.rows, x.hidden, l.count, kTile);
+        const uint32_t size = tile_for(plan.head.piece, x.rows);
+        a.p = product(w, l.deep(), have, x.rows, x.hidden, l.count, size);
         a.factor = plan.factor;
         a.minus_lse = plan.minus_lse;
         a.d = plan.d;
         a.d_stride = plan.head.piece;
         a.scale = x.scale * eshead::kLog2e;
-        launch_tiles<kTile>(eshead::es_head_prob_kernel<kTile>, a, s);
+        if (size == kTile)
+            launch_tiles<kTile>(eshead::es_head_prob_kernel<kTile>, a, s);
+        else
+            launch_tiles<kSmallTile>(eshead::es_head_prob_kernel<kSmallTile>, a, s);
         eshead::EntryArgs e{};
         e.list = l.list;
         e.count = l.count;
@@ -554,7 +573,7 @@ int es_head_gradient(const es_head_gradient_t* args, es_stream_t stream) try {
             // along the tile the head's rows are as wide as they are stored
             const uint32_t width = plan.head.copied ? plan.head.padded : x.hidden;
             g.p = product(Side{w.at, w.stride, width}, d_deep, x.hidden, x.rows, have, l.count,
-                          kTile);
+                          plan.size);
             g.p.splits = plan.splits;
             g.p.split_depth = plan.split_depth;
             g.parts = plan.parts;
@@ -567,17 +586,24 @@ int es_head_gradient(const es_head_gradient_t* args, es_stream_t stream) try {
                 g.out_stride = x.dx_stride;
                 g.list = l.list;
             }
-            launch_tiles<kTile>(eshead::es_head_row_grad_kernel<kTile>, g, s);
+            if (plan.size == kTile)
+                launch_tiles<kTile>(eshead::es_head_row_grad_kernel<kTile>, g, s);
+            else
+                launch_tiles<kSmallTile>(eshead::es_head_row_grad_kernel<kSmallTile>, g, s);
         }
         if (x.d_weight != nullptr) {
             eshead::HeadGradArgs g{};
             const Side d_wide{plan.d, plan.head.piece, plan.head.piece};
-            g.p = product(l.wide(), d_wide, x.hidden, have, l.rows, l.count, kTile);
+            const uint32_t small = tile_for(plan.head.piece, x.hidden);
+            g.p = product(l.wide(), d_wide, x.hidden, have, l.rows, l.count, small);
             g.out = static_cast<uint16_t*>(x.d_weight) + v0 * x.dw_stride;
             g.out_stride = x.dw_stride;
             g.n_have = have;
             g.hidden = x.hidden;
-            launch_tiles<kTile>(eshead::es_head_weight_grad_kernel<kTile>, g, s);
+            if (small == kTile)
+                launch_tiles<kTile>(eshead::es_head_weight_grad_kernel<kTile>, g, s);
+            else
+                launch_tiles<kSmallTile>(eshead::es_head_weight_grad_kernel<kSmallTile>, g, s);
         }
         rc = launch_error("es_head_gradient kernel launch");
         if (rc != ES_OK) return rc;
@@ -647,19 +673,24 @@ struct AdaptPlan {
         x = nullptr;
         if (copied) x = room.take<uint16_t>(uint64_t(packed_rows) * padded);
         is_copied = copied;
-        // Tiles of 128 x 128 results where the card holds them at once, of 256 x 256 where there
-        // are more.  5120 x 5120: 1000 rows (320 small tiles) 77 and 120 us, 2000 (640) 137 and 127;
-        // 5120 x 17408: 300 rows (408) 108 and 137.
         const uint64_t tiles = tiles_of(a.outer, a.rows, kSmallTile);
-        low = !few && tiles <= 2 * kCus;
+        low = !few && tile_for(a.outer, a.rows) == kSmallTile;
         splits = 1;
         split_depth = static_cast<uint32_t>(up(a.inner, kDepth));
         parts = nullptr;
         parts_stride = up(a.outer, 4);
-        // Few tiles' sums are divided, if a part is worth the join: 5120 x 5120, 100 rows (40
-        // tiles) 79 us whole and 48 divided, 300 (120) 65 and 51, 700 (240) 66 and 77; 1024 x
-        // 1024, 1000 rows (64) 21 and 26.
-        const uint64_t most = low && tiles <= 128 ? std::min<uint64_t>(2 * kCus / tiles, a.inner / 1024) : 1;
+        // Few tiles' sums are divided, if a part is worth the join: a stage of 64 takes 0.6 us,
+        // the join's launch and its bytes the rest.  5120 x 5120, 100 rows (40 tiles) 79 us
+        // whole and 48 divided, 300 (120) 65 and 51, 700 (240) 66 and 77; 1024 x 1024, 1000 rows
+        // (64) 21 and 26.
+        uint64_t most = 1;
+        const double whole = 0.6 * a.inner / kDepth, join = 8e-6 * a.rows * a.outer / 2.5;
+        double best = whole;
+        for (uint64_t n = 2; low && n <= 2 * kCus / tiles && n <= a.inner / 1024; ++n)
+            if (whole / n + 10 + join * n < best) {
+                best = whole / n + 10 + join * n;
+                most = n;
+            }
         if (most < 2) return;
         split_depth = static_cast<uint32_t>(up((a.inner + most - 1) / most, kDepth));
         splits = (a.inner + split_depth - 1) / split_depth;

@@ -318,7 +318,9 @@ __global__ __launch_bounds__(512, 2) void es_head_ring_kernel(FewStatsArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     float* const sums = reinterpret_cast<float*>(lds);   // [wave][row of x][token]
     const uint32_t lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
-    const uint32_t row0 = blockIdx.x * 32;
+    const uint32_t row0 = blockIdx.x * 32, n0 = blockIdx.y * 64;   // 64 rows of x a workgroup
+    a.f.x += n0 * a.f.x_stride;
+    a.f.rows = min(a.f.rows - n0, 64u);
     R t;
     t.run(a.f, row0, wave, kWaves, lds + wave * R::kBytes);
     __syncthreads();
@@ -343,7 +345,7 @@ __global__ __launch_bounds__(512, 2) void es_head_ring_kernel(FewStatsArgs a) {
 #pragma unroll
         for (int d = 16; d >= 1; d /= 2) sum += __shfl_xor(sum, d);
         if (i == 0) {
-            float* const to = a.parts + 2 * (uint64_t(n) * gridDim.x + blockIdx.x);
+            float* const to = a.parts + 2 * (uint64_t(n0 + n) * gridDim.x + blockIdx.x);
             to[0] = top;
             to[1] = sum;
         }
