@@ -35,7 +35,9 @@ scaled value stochastically onto it; the paper lists quantized ES as future
 work (Appendix A.2).
 
 attention.py holds the rows of the paged cache (norm, rotation, quantisation)
-and the attention over it, with which a member is scored.
+and the attention over it, with which a member is scored; head.py the scores
+at its head, the divergence from a teacher, their gradients and projections
+under many members' adapters.
 
 Pin status of every function is listed in the module docstrings; all functions
 are pinned (none is "parity unpinned").
@@ -55,9 +57,10 @@ from . import fp8
 from .fp8 import (E4M3_MAX, e4m3_decode, e4m3_encode, grid_floor, round_onto_grid, f8perturb,
                   f8restore, f8update_values, f8update)
 from . import attention
+from . import head
 
 __all__ = [
-    "attention",
+    "attention", "head",
     "philox4x32_10", "philox4x32_10_bigint", "MASK32",
     "key_words", "counter_words", "uniform_from_word", "angle_from_word", "box_muller",
     "noise_words", "normals", "rounding_draws", "spare_draws",

@@ -75,7 +75,10 @@ def check(x, w, a, b, scales, index, got):
 @pytest.mark.parametrize("rows,inner,outer,rank,members", [
     (1, 64, 64, 8, 1), (1, 1000, 513, 16, 3), (3, 8, 1, 128, 2), (16, 512, 300, 16, 16),
     (17, 136, 100, 24, 5), (33, 1024, 257, 64, 40), (64, 328, 1025, 32, 7), (65, 256, 256, 16, 3),
-    (129, 72, 771, 40, 200), (300, 1032, 520, 128, 4), (513, 192, 264, 8, 30)])
+    (129, 72, 771, 40, 200), (300, 1032, 520, 128, 4), (513, 192, 264, 8, 30),
+    (2, 264, 8193, 16, 3), (16, 64, 9001, 24, 16), (20, 136, 8200, 16, 9), (33, 72, 9000, 64, 3),   # many outputs
+    (70, 2104, 130, 32, 6), (200, 4096, 257, 16, 5),                                # divided sums
+    (1300, 72, 6000, 16, 11), (2100, 64, 4100, 64, 6)])                             # large tiles
 @pytest.mark.parametrize("how", ["mixed", "runs", "each", "one", "none"])
 def test_project(rows, inner, outer, rank, members, how):
     rng = np.random.default_rng([rows, inner, outer, rank])

@@ -150,6 +150,44 @@ def test_odd_widths_strides_and_alignments(rows, vocab, hidden, entries):
     check(*args, 1.0)
 
 
+@pytest.mark.parametrize("rows,vocab,hidden", [
+    (1, 20000, 64), (17, 16400, 200), (64, 20001, 72), (65, 17000, 64), (128, 16385, 136),   # streamed
+    (70, 900, 72), (128, 16384, 64), (128, 33, 264),                                         # in rings
+    (129, 40001, 64), (260, 30000, 72)])                                                     # large tiles
+@pytest.mark.parametrize("entries", [None, 5])
+def test_large_and_small_vocabularies(rows, vocab, hidden, entries):
+    rng = np.random.default_rng([rows, vocab])
+    check(*make(rng, rows, vocab, hidden, entries), 1.0)
+
+
+@pytest.mark.parametrize("rows,vocab,hidden", [(1500, 100003, 64), (1500, 100003, 65), (5000, 30000, 72)])
+def test_vocabularies_of_several_pieces(rows, vocab, hidden):
+    """Gradients of logits beyond what a call holds at a time, against the formula
+    in 64 bits on the card."""
+    rng = np.random.default_rng([rows, hidden])
+    x, w, ids, _, grad = make(rng, rows, vocab, hidden)
+    head, t, g = Head(w), dev(ids[:, 0], torch.int64), dev(grad, torch.float32)
+    logp, lse = head.score(x, t)
+    dx, dw = head.score_gradient(x, t, logp, lse, g)
+    live, X, W = t >= 0, x.double(), w.double()
+    z = X @ W.t()
+    want = torch.logsumexp(z, -1)
+    s = X.abs().amax() * W.abs().sum(1).amax()           # no product's sizes add up to more
+    z_err = (2 * E * hidden + 4 * E) * s
+    assert ((lse - want).abs()[live] <= z_err + 200 * E + 8 * E * s + 4 * E * want.abs()[live]).all()
+    d = z.sub_(want[:, None]).exp_()
+    d[torch.arange(rows, device="cuda"), t.clamp(min=0)] -= 1
+    d *= torch.where(live, -g.double(), 0.0)[:, None]
+    full = torch.zeros_like(d)
+    full[torch.arange(rows, device="cuda"), t.clamp(min=0)] = torch.where(live, g.double().abs(), 0.0)
+    p_err = 2 * z_err + 12 * E * s + 300 * E + 8 * E * want.abs().amax()
+    d_err = U * d.abs() + (d.abs() + 2 * full) * p_err + 2.0 ** -126
+    for got, ref, size, n in ((dx, d @ W, lambda a: a @ W.abs(), vocab),
+                              (dw, d.t() @ X, lambda a: a.t() @ X.abs(), rows)):
+        tol = U * ref.abs() + size(d_err) + 2 * E * (n + 64) * size(d.abs()) + 2.0 ** -126
+        assert ((got.double() - ref).abs() <= tol * (1 + U)).all()
+
+
 @pytest.mark.parametrize("rows", [3, 64, 65, 300])
 def test_aligned_rows_between_others(rows):
     rng = np.random.default_rng(rows)
