@@ -758,8 +758,8 @@ int es_kv_attend(es_kv_t* kv, const es_kv_attend_t* args, es_stream_t stream);
  *   q = softmax(scale teacher) over the row's present ids,
  *   loss = sum_e q_e (log q_e - logp_e),
  * the divergence of the student from the teacher within its top logits; a row
- * whose teacher leaves nothing (-infinity throughout) has loss 0.  The same id
- * twice in a row counts twice.
+ * whose teacher leaves nothing (-infinity throughout) has loss 0 and no gradient:
+ * nothing there reaches the head's.  The same id twice in a row counts twice.
  *
  * Products are sums in binary32 of exact products; maxima, sums and scores are
  * binary32.  The same inputs give the same bits.
@@ -779,7 +779,7 @@ typedef struct es_head_score {
     void*          workspace;   /* device memory of the call's own, 256-byte aligned */
     uint64_t       workspace_bytes;            /* at least es_head_score_bytes() */
     uint32_t       rows;        /* 0 .. 65536 */
-    uint32_t       vocab;       /* 1 .. 2^24 */
+    uint32_t       vocab;       /* 1 .. 2^24; rows times vocab at most 2^36 */
     uint32_t       hidden;      /* 1 .. 65536 */
     uint32_t       entries;     /* 1 .. 256 */
     float          scale;       /* finite */
@@ -844,7 +844,7 @@ typedef struct es_adapt {
     uint64_t       workspace_bytes;            /* at least es_adapt_bytes() */
     uint32_t       rows;        /* 0 .. 2^20 */
     uint32_t       inner;       /* a multiple of 8, 8 .. 65536 */
-    uint32_t       outer;       /* 1 .. 2^20 */
+    uint32_t       outer;       /* 1 .. 2^20; rows times outer at most 2^36 */
     uint32_t       members;     /* 1 .. 65536 */
     uint32_t       rank;        /* a multiple of 8, 8 .. 128 */
     uint32_t       reserved;    /* 0 */

@@ -15,6 +15,7 @@ def weights(ids, teacher, scale):
     here = ids >= 0
     if teacher is None:
         return here.astype(np.float64), np.zeros(ids.shape)
+    here = here & ~np.isneginf(teacher)
     t = np.where(here, np.where(here, teacher, 0.0) * scale, -np.inf)
     top = t.max(1, keepdims=True)
     e = np.exp(t - np.where(np.isneginf(top), 0.0, top))
@@ -65,10 +66,13 @@ def logit_gradients(x, w, ids, grad, scale=1.0, teacher=None):
 def gradients(x, w, ids, grad, scale=1.0, teacher=None):
     """(d_x, d_w); rows that are void have NaN and add nothing."""
     live, void = kinds(ids, len(w))
+    if teacher is not None:
+        live &= ((ids >= 0) & ~np.isneginf(teacher)).any(1)
+    x = np.where(live[:, None], x, 0.0)
     d = logit_gradients(x, w, ids, grad, scale, teacher)
     dx = d @ w
     dx[void] = np.nan
-    return dx, d.T @ np.where(live[:, None], x, 0.0)
+    return dx, d.T @ x
 
 
 def project(x, w, a, b, index, scales=None):

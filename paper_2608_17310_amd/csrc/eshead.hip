@@ -25,6 +25,8 @@ using esmm::Side;
 namespace {
 
 constexpr uint64_t kMaxStride = uint64_t(1) << 22;
+// Results of a product: their tiles' lanes stay below 2^32, a launch's limit.
+constexpr uint64_t kMaxResults = uint64_t(1) << 36;
 constexpr uint32_t kCus = 256;
 
 // Gradients of logits, and copies of a head's rows, that a call holds at a time:
@@ -82,6 +84,8 @@ int check_head(const char* name, const void* x, const void* weight, uint64_t x_s
         return fail_in(ES_ERR_INVALID_ARG, name, "vocab out of range (1 .. 2^24)");
     if (hidden == 0 || hidden > 65536)
         return fail_in(ES_ERR_INVALID_ARG, name, "hidden out of range (1 .. 65536)");
+    if (uint64_t(rows) * vocab > kMaxResults)
+        return fail_in(ES_ERR_INVALID_ARG, name, "rows times vocab above 2^36");
     if (entries == 0 || entries > eshead::kMaxEntries)
         return fail_in(ES_ERR_INVALID_ARG, name, "entries out of range (1 .. 256)");
     if (!std::isfinite(scale)) return fail_in(ES_ERR_INVALID_ARG, name, "scale is not finite");
@@ -269,7 +273,6 @@ int list_rows(const char* name, const eshead::RowArgs& rows, const Lists& l, con
     pack.rows = rows.rows;
     pack.width = rows.hidden;
     pack.padded = l.padded;
-    pack.flags = l.flags;
     hipLaunchKernelGGL(eshead::es_head_pack_kernel, dim3(l.rows / 4), dim3(256), 0, s, pack);
     return launch_error(name);
 }
@@ -520,6 +523,7 @@ int es_head_gradient(const es_head_gradient_t* args, es_stream_t stream) try {
     rows.flags = l.flags;
     rows.dx = static_cast<uint16_t*>(x.d_x);
     rows.dx_stride = x.dx_stride;
+    rows.weighed = x.teacher != nullptr;
     rows.status = x.status;
     rows.rows = x.rows;
     rows.vocab = x.vocab;
@@ -552,7 +556,6 @@ int es_head_gradient(const es_head_gradient_t* args, es_stream_t stream) try {
         eshead::EntryArgs e{};
         e.list = l.list;
         e.count = l.count;
-        e.flags = l.flags;
         e.ids = x.ids;
         e.teacher = x.teacher;
         e.logp = x.logp;
@@ -619,7 +622,7 @@ int es_head_gradient(const es_head_gradient_t* args, es_stream_t stream) try {
         j.count = l.count;
         j.out = static_cast<uint16_t*>(x.d_x);
         j.out_stride = x.dx_stride;
-        hipLaunchKernelGGL(eshead::es_head_join_kernel, dim3((x.hidden + 1023) / 1024, x.rows), dim3(256),
+        hipLaunchKernelGGL(eshead::es_head_join_kernel, dim3(x.rows, (x.hidden + 1023) / 1024), dim3(256),
                            0, s, j);
     }
     return launch_error("es_head_join_kernel launch");
@@ -639,6 +642,8 @@ int check_adapt(const char* name, const es_adapt_t& x) {
         return fail_in(ES_ERR_INVALID_ARG, name, "inner is not a multiple of 8 up to 65536");
     if (x.outer == 0 || x.outer > (1u << 20))
         return fail_in(ES_ERR_INVALID_ARG, name, "outer out of range (1 .. 2^20)");
+    if (uint64_t(x.rows) * x.outer > kMaxResults)
+        return fail_in(ES_ERR_INVALID_ARG, name, "rows times outer above 2^36");
     if (x.members == 0 || x.members > 65536)
         return fail_in(ES_ERR_INVALID_ARG, name, "members out of range (1 .. 65536)");
     if (x.rank == 0 || x.rank % 8 != 0 || x.rank > esadapt::kMaxRank)

@@ -3,7 +3,7 @@
 //
 // With z = scale x . w_v and lse = log sum_v exp z_v, a row's scores are z_id - lse;
 // its gradient is f (Q softmax(z) - q), q the wanted weights at its ids, Q their
-// sum (1, or 0 where a teacher leaves nothing).  The logits of a tile live in
+// sum (1; a row whose teacher leaves nothing has no gradient).  The logits of a tile live in
 // registers: the scores keep a maximum and a sum of each row and tile, and the
 // gradients f Q softmax(z) as bf16, for a piece of the vocabulary at a time.
 #pragma once
@@ -21,7 +21,7 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr uint32_t kMaxEntries = 256;
 
 // What becomes of a row, by its ids.
-enum Row : uint8_t { kDead = 0, kLive = 1, kVoid = 2, kEmpty = 3 };   // kEmpty: live, Q = 0
+enum Row : uint8_t { kDead = 0, kLive = 1, kVoid = 2 };
 
 // ------------------------------------------------------------------- rows --
 
@@ -34,24 +34,25 @@ struct RowArgs {
     uint64_t dx_stride;
     uint32_t* status;
     uint32_t rows, vocab, entries, hidden;
+    bool weighed;                          // a row whose teacher leaves nothing is dead
 };
 
 // What becomes of a row of several ids: one wave a row.
 __global__ __launch_bounds__(256) void es_head_rows_kernel(RowArgs a) {
     const uint32_t lane = threadIdx.x & 63, r = blockIdx.x * 4 + (threadIdx.x >> 6);
     if (r >= a.rows) return;
-    bool some = false, bad = false, weight = a.teacher == nullptr;
+    bool some = false, bad = false, weight = !a.weighed;
     for (uint32_t e = lane; e < a.entries; e += 64) {
         const int64_t id = a.ids[uint64_t(r) * a.entries + e];
         some |= id >= 0;
         bad |= id >= int64_t(a.vocab);
-        if (id >= 0 && a.teacher != nullptr)
+        if (id >= 0 && a.weighed)
             weight |= a.teacher[uint64_t(r) * a.entries + e] != -eskv::inf();
     }
     some = __any(some);
     bad = __any(bad);
     weight = __any(weight);
-    if (lane == 0) a.flags[r] = bad ? kVoid : !some ? kDead : weight ? kLive : kEmpty;
+    if (lane == 0) a.flags[r] = bad ? kVoid : some && weight ? kLive : kDead;
     if (bad && lane == 0 && a.status != nullptr) atomicOr(a.status, ES_HEAD_BAD_ID);
 }
 
@@ -92,13 +93,13 @@ __global__ __launch_bounds__(1024) void es_head_list_kernel(ListArgs a) {
             if (a.rows.entries == 1) {
                 const int64_t id = a.rows.ids[r];
                 f = id < 0 ? kDead : id < int64_t(a.rows.vocab) ? kLive : kVoid;
-                if (f == kLive && a.rows.teacher != nullptr && a.rows.teacher[r] == -eskv::inf()) f = kEmpty;
+                if (f == kLive && a.rows.weighed && a.rows.teacher[r] == -eskv::inf()) f = kDead;
                 if (f == kVoid && a.rows.status != nullptr) atomicOr(a.rows.status, ES_HEAD_BAD_ID);
                 a.rows.flags[r] = f;
             } else {
                 f = a.rows.flags[r];
             }
-            live |= uint32_t(f == kLive || f == kEmpty) << i;
+            live |= uint32_t(f == kLive) << i;
         }
         const uint32_t n = __popc(live);
         uint32_t sum = n;                  // over this lane and those before it
@@ -130,7 +131,6 @@ struct PackArgs {
     const uint32_t* count;                 // rows that there are; null: `rows`
     uint32_t rows, width, padded;
     // of the gradients: what a row's products are scaled by (null: none)
-    const uint8_t* flags;
     const float *grad, *lse;
     float *factor, *minus_lse;
     float scale;                           // with its sign
@@ -160,7 +160,7 @@ __global__ __launch_bounds__(256) void es_head_pack_kernel(PackArgs a) {
         store<u32x4_t>(to + k, v);
     }
     if (a.factor != nullptr && lane == 0) {
-        a.factor[i] = live && a.flags[row] != kEmpty ? a.scale * a.grad[row] : 0.0f;
+        a.factor[i] = live ? a.scale * a.grad[row] : 0.0f;
         a.minus_lse[i] = live ? -a.lse[row] * kLog2e : 0.0f;
     }
 }
@@ -466,9 +466,11 @@ __device__ __forceinline__ float block_max(float x, float* room) {
     return fmaxf(fmaxf(room[0], room[1]), fmaxf(room[2], room[3]));
 }
 
-// The teacher's weight of thread e's entry (0: absent), and its logarithm.
+// The teacher's weight of thread e's entry (0: absent), and its logarithm.  A logit of
+// -infinity has none at any scale.
 __device__ __forceinline__ float teacher_weight(bool here, float t, float scale, float* room,
                                                 float& log_q) {
+    here = here && t != -eskv::inf();
     const float z = here ? t * scale : -eskv::inf();
     const float top = block_max(z, room);
     const float from = top == -eskv::inf() ? 0.0f : top;
@@ -592,7 +594,6 @@ __global__ __launch_bounds__(2 * kSize, 2) void es_head_prob_kernel(ProbArgs a) 
 
 struct EntryArgs {
     const uint32_t *list, *count;
-    const uint8_t* flags;
     const int64_t* ids;
     const float *teacher, *logp, *grad;
     uint16_t* d;
@@ -622,8 +623,7 @@ __global__ __launch_bounds__(256) void es_head_entries_kernel(EntryArgs a) {
     if (id < int64_t(a.v0) || id >= int64_t(a.v_end)) return;
     float all = 0.0f;
     for (uint32_t k = 0; k < a.entries; ++k) all += ids[k] == id ? weights[k] : 0.0f;
-    const float p = a.flags[row] == kEmpty ? 0.0f : expf(a.logp[at]);
-    const float d = a.sign_scale * a.grad[row] * (p - all);
+    const float d = a.sign_scale * a.grad[row] * (expf(a.logp[at]) - all);
     a.d[i * a.d_stride + (id - a.v0)] = static_cast<uint16_t>(pack_bf16(d, 0.0f));
 }
 
@@ -681,7 +681,7 @@ struct JoinArgs {
 
 // The splits' sums, in one order, rounded once.
 __global__ __launch_bounds__(256) void es_head_join_kernel(JoinArgs a) {
-    const uint32_t i = blockIdx.y, h = 4 * (blockIdx.x * 256 + threadIdx.x);
+    const uint32_t i = blockIdx.x, h = 4 * (blockIdx.y * 256 + threadIdx.x);
     if (i >= *a.count || h >= a.hidden) return;
     const float* p = a.parts + i * a.parts_stride + h;
     f32x4_t v = load<f32x4_t>(p);

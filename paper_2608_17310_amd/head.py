@@ -68,6 +68,7 @@ class Head:
         hidden [rows, hidden] (bf16), and the logarithms [rows] of the normalisers,
         float32, with logits scale hidden weight^T.  status: a CUDA tensor of one
         int32 that collects ES_HEAD_BAD_ID."""
+        _matrix(hidden, (None, self.hidden), "hidden")
         rows = hidden.shape[0]
         if targets.dim() != 1:
             raise ValueError("targets must be [rows]")
@@ -82,6 +83,7 @@ class Head:
         normalisers.  scale, the inverse temperature, applies to both sides."""
         if ids.dim() != 2 or logits.shape != ids.shape:
             raise ValueError("ids and logits must be [rows, entries]")
+        _matrix(hidden, (ids.shape[0], self.hidden), "hidden")
         rows, entries = ids.shape
         out = _empty((2, rows), torch.float32, hidden.device, stream)
         logp = _empty((rows, entries), torch.float32, hidden.device, stream)

@@ -450,3 +450,44 @@ def test_refusals():
                  lambda: head.distill(x, t[:, None][:, :0].contiguous(), f[:, None][:, :0].contiguous())):
         with pytest.raises(esopt.EsError):
             call()
+
+
+@pytest.mark.parametrize("entries", [1, 6])
+@pytest.mark.parametrize("rows", [9, 140])
+def test_rows_whose_teacher_leaves_nothing(rows, entries):
+    """Their loss and their gradient are 0, and what x holds there reaches nothing: the
+    others' are those of a call without them."""
+    rng = np.random.default_rng([rows, entries])
+    x, w, ids, teacher, grad = make(rng, rows, 300, 128, entries, masked=0.0)
+    ids[:, 0] = rng.integers(0, 300, rows)                 # every row has one
+    empty = rng.random(rows) < 0.4
+    empty[1] = True
+    teacher[empty] = -np.inf
+    x[torch.from_numpy(empty).cuda()] = float("nan")
+    head, d_t, d_grad = Head(w), dev(teacher, torch.float32), dev(grad, torch.float32)
+    got = []
+    for i in (ids, np.where(empty[:, None], -1, ids)):
+        d_ids = dev(i, torch.int64)
+        loss, logp, lse = head.distill(x, d_ids, d_t)
+        got.append((loss,) + head.distill_gradient(x, d_ids, d_t, logp, lse, d_grad))
+    for a, b in zip(*got):
+        assert torch.isfinite(a).all() and torch.equal(a, b)
+    assert not got[0][0][torch.from_numpy(empty).cuda()].any()
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.5])
+def test_a_teachers_infinities_at_any_scale(scale):
+    """-infinity leaves an id no weight: the divergence without it."""
+    rng = np.random.default_rng(31)
+    x, w, ids, teacher, grad = make(rng, 40, 300, 128, 6, masked=0.0)
+    ids = np.abs(ids) % 300
+    teacher[:, 2] = -np.inf
+    teacher[5] = -np.inf
+    without = np.where(np.isneginf(teacher), -1, ids)
+    head, d_t = Head(w), dev(teacher, torch.float32)
+    loss, logp, lse = head.distill(x, dev(ids, torch.int64), d_t, scale=scale)
+    assert torch.equal(loss, head.distill(x, dev(without, torch.int64), d_t, scale=scale)[0])
+    assert loss.isfinite().all() and loss[5] == 0
+    for t in head.distill_gradient(x, dev(ids, torch.int64), d_t, logp, lse, dev(grad, torch.float32),
+                                   scale=scale):
+        assert t.isfinite().all()

@@ -72,6 +72,7 @@ def _adapt(**kw):
 
 
 BOTH = [(dict(rows=65537), E, "rows"), (dict(vocab=0), E, "vocab"), (dict(vocab=(1 << 24) + 1), E, "vocab"),
+        (dict(rows=65536, vocab=(1 << 20) + 1), E, "rows times vocab"),
         (dict(hidden=0), E, "hidden"), (dict(hidden=65537), E, "hidden"), (dict(entries=0), E, "entries"),
         (dict(entries=257, teacher=P), E, "entries"), (dict(entries=2), E, "teacher"),
         (dict(scale=float("nan")), E, "scale"), (dict(scale=float("-inf")), E, "scale"),
@@ -106,6 +107,7 @@ def test_gradient_refuses(lib, change, code, word):
 @pytest.mark.parametrize("change,code,word", [
     (dict(rows=(1 << 20) + 1), E, "rows"), (dict(inner=0), E, "inner"), (dict(inner=60), E, "inner"),
     (dict(inner=65544), E, "inner"), (dict(outer=0), E, "outer"), (dict(outer=(1 << 20) + 1), E, "outer"),
+    (dict(rows=1 << 17, outer=1 << 20, out_stride=1 << 20), E, "rows times outer"),
     (dict(members=0), E, "members"), (dict(members=65537), E, "members"), (dict(rank=0), E, "rank"),
     (dict(rank=4), E, "rank"), (dict(rank=136), E, "rank"), (dict(reserved=1), E, "reserved"),
     (dict(x_stride=1 << 23), E, "stride"), (dict(out_stride=1 << 23), E, "stride"),

@@ -103,3 +103,18 @@ def test_projections_are_those_of_merged_weights():
             merged = w if i < 0 else w + s[i] * b[i] @ a[i]
             assert np.allclose(got[r], merged @ x[r])
     assert np.isnan(got[6]).all()
+
+
+@pytest.mark.parametrize("scale", [1.0, 0.0, -0.5])
+def test_a_teacher_that_leaves_nothing(scale):
+    x, w, ids, t, grad = make(9, entries=3)
+    t[2] = -np.inf
+    t[3, 1] = -np.inf
+    loss, _, _ = oh.score(x, w, ids, scale, t)
+    gone = np.where(np.isneginf(t), -1, ids)
+    assert np.isfinite(loss).all() and loss[2] == 0
+    assert loss[3] == oh.score(x, w, gone, scale, t)[0][3]
+    x[2] = np.nan
+    dx, dw = oh.gradients(x, w, ids, grad, scale, t)
+    wx, ww = oh.gradients(x, w, gone, grad, scale, t)
+    assert np.array_equal(dx, wx) and np.array_equal(dw, ww) and not dx[2].any()
