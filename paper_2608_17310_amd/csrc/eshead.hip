@@ -222,7 +222,9 @@ struct GradientPlan {
         parts = nullptr;
         if (x.d_x == nullptr) return;
         // the sum over the vocabulary in as many parts as fill the card
-        const bool low = x.rows <= kSmallTile;
+        // (in small tiles where these leave out a quarter of the padded rows: 266 rows against
+        // 32003 x 1000 36 and 31 us, and their parts' join 10 and 7.5)
+        const bool low = 4 * up(x.rows, kSmallTile) <= 3 * up(x.rows, kTile);
         size = low ? kSmallTile : kTile;
         const uint64_t tiles = tiles_of(x.rows, x.hidden, size);
         const uint32_t most = std::max(1u, head.piece / (low ? 512 : 1024));

@@ -589,7 +589,10 @@ __global__ __launch_bounds__(2 * kSize, 2) void es_head_prob_kernel(ProbArgs a) 
     }
     tile_to_lds(c, lds);
     __syncthreads();
-    store_rows<kSize>(lds, a.d, a.d_stride, m0, kSize, [&](uint32_t n) { return int64_t(n0 + n); });
+    // (rows behind the last, zeros, as far as a sum over the rows goes)
+    const uint32_t rows = (count + kDepth - 1) / kDepth * kDepth;
+    store_rows<kSize>(lds, a.d, a.d_stride, m0, kSize,
+                      [&](uint32_t n) { return n0 + n < rows ? int64_t(n0 + n) : int64_t(-1); });
 }
 
 struct EntryArgs {

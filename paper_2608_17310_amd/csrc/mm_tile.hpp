@@ -88,6 +88,10 @@ __device__ __forceinline__ void load_lds(u32x4_t buffer, uint32_t offset, uint32
 __device__ __forceinline__ void wait_staged() {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
 }
+template <int n>                           // but the last n loads
+__device__ __forceinline__ void wait_all_but() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(n) : "memory");
+}
 
 __device__ __forceinline__ uint32_t uniform(uint32_t x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ __forceinline__ uint64_t uniform(uint64_t x) {
@@ -296,9 +300,13 @@ __device__ __forceinline__ void product_tile(const Product& p, uint32_t m0, uint
         __builtin_amdgcn_sched_barrier(0);
     };
     issue(k0, 0);
-    wait_staged();
+    if (k0 + kDepth < k_end) {
+        issue(k0 + kDepth, 2 * kSide);
+        wait_all_but<8>();
+    } else {
+        wait_staged();
+    }
     __builtin_amdgcn_s_barrier();
-    if (k0 + kDepth < k_end) issue(k0 + kDepth, 2 * kSide);
     if (64 * (wave >> 1) >= n_have) {                    // a wave without rows only stages
         for (uint32_t k = k0; k + kDepth < k_end; k += kDepth) {
             wait_staged();
