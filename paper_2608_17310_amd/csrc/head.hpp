@@ -53,13 +53,22 @@ __global__ __launch_bounds__(256) void es_head_rows_kernel(RowArgs a) {
     bad = __any(bad);
     weight = __any(weight);
     if (lane == 0) a.flags[r] = bad ? kVoid : some && weight ? kLive : kDead;
-    if (bad && lane == 0 && a.status != nullptr) atomicOr(a.status, ES_HEAD_BAD_ID);
+}
+
+// The same, where a row has one id; of several, what es_head_rows_kernel found.
+__device__ __forceinline__ uint8_t kind_of(const RowArgs& a, uint32_t r) {
+    if (a.entries > 1) return a.flags[r];
+    const int64_t id = a.ids[r];
+    if (id >= int64_t(a.vocab)) return kVoid;
+    return id < 0 || (a.weighed && a.teacher[r] == -eskv::inf()) ? kDead : kLive;
 }
 
 // Its results, where it has none of its own.  A wave's lanes.
 __device__ __forceinline__ void clear_row(const RowArgs& a, uint32_t r, uint32_t lane) {
-    const bool bad = a.flags[r] == kVoid;
-    if (!bad && a.flags[r] != kDead) return;
+    const uint8_t kind = kind_of(a, r);
+    if (kind == kLive) return;
+    const bool bad = kind == kVoid;
+    if (bad && lane == 0 && a.status != nullptr) atomicOr(a.status, ES_HEAD_BAD_ID);
     const float v = bad ? eskv::nan() : 0.0f;
     if (lane == 0) {
         if (a.loss != nullptr) a.loss[r] = v;
@@ -89,17 +98,7 @@ __global__ __launch_bounds__(1024) void es_head_list_kernel(ListArgs a) {
         for (uint32_t i = 0; i < each; ++i) {
             const uint32_t r = mine + i;
             if (r >= rows) break;
-            uint8_t f;
-            if (a.rows.entries == 1) {
-                const int64_t id = a.rows.ids[r];
-                f = id < 0 ? kDead : id < int64_t(a.rows.vocab) ? kLive : kVoid;
-                if (f == kLive && a.rows.weighed && a.rows.teacher[r] == -eskv::inf()) f = kDead;
-                if (f == kVoid && a.rows.status != nullptr) atomicOr(a.rows.status, ES_HEAD_BAD_ID);
-                a.rows.flags[r] = f;
-            } else {
-                f = a.rows.flags[r];
-            }
-            live |= uint32_t(f == kLive) << i;
+            live |= uint32_t(kind_of(a.rows, r) == kLive) << i;
         }
         const uint32_t n = __popc(live);
         uint32_t sum = n;                  // over this lane and those before it
@@ -127,8 +126,8 @@ struct PackArgs {
     const uint16_t* from;
     uint16_t* to;
     uint64_t stride;                       // of `from`; `to` has rows of `padded`
-    const uint32_t* list;                  // row i of `to` is row list[i] of `from`; null: row i
-    const uint32_t* count;                 // rows that there are; null: `rows`
+    uint32_t *list, *count;                // row i of `to` is row list[i] of `from`; null: row i of `rows`
+    bool lists;                            // (they are made here)
     uint32_t rows, width, padded;
     // of the gradients: what a row's products are scaled by (null: none)
     const float *grad, *lse;
@@ -137,16 +136,8 @@ struct PackArgs {
     RowArgs out;                           // of a call's rows: those that are not live are cleared
 };
 
-// Rows copied to where every row starts at a word of 16 bytes and ends in zeros; the
-// rows behind the last one, up to a tile's end, are zeros.  One wave a row.
-__global__ __launch_bounds__(256) void es_head_pack_kernel(PackArgs a) {
-    const uint32_t lane = threadIdx.x & 63;
-    const uint32_t i = blockIdx.x * 4 + (threadIdx.x >> 6);
-    const uint32_t count = a.count != nullptr ? *a.count : a.rows;
-    if (a.list != nullptr && i < a.rows) clear_row(a.out, i, lane);
-    if (i >= (count + kTile - 1) / kTile * kTile) return;
-    const bool live = i < count;
-    const uint32_t row = !live ? 0 : a.list != nullptr ? a.list[i] : i;
+// Row i of the copies: row `row` of the others, or zeros.
+__device__ __forceinline__ void pack_row(const PackArgs& a, uint32_t i, uint32_t row, bool live, uint32_t lane) {
     const uint16_t* const from = a.from + row * a.stride;
     uint16_t* const to = a.to + uint64_t(i) * a.padded;
     for (uint32_t k = 8 * lane; k < a.padded; k += 512) {
@@ -163,6 +154,51 @@ __global__ __launch_bounds__(256) void es_head_pack_kernel(PackArgs a) {
         a.factor[i] = live ? a.scale * a.grad[row] : 0.0f;
         a.minus_lse[i] = live ? -a.lse[row] * kLog2e : 0.0f;
     }
+}
+
+// Rows copied to where every row starts at a word of 16 bytes and ends in zeros; the
+// rows behind the last one, up to a tile's end, are zeros.  One wave a row.  Where there
+// are few rows each wave looks at all of them for its own's place: a launch less.
+__global__ __launch_bounds__(256) void es_head_pack_kernel(PackArgs a) {
+    const uint32_t lane = threadIdx.x & 63;
+    const uint32_t i = uniform(blockIdx.x * 4 + (threadIdx.x >> 6));
+    if (a.list != nullptr && i < a.rows) clear_row(a.out, i, lane);
+    if (!a.lists) {
+        const uint32_t count = a.count != nullptr ? *a.count : a.rows;
+        if (i < count)
+            pack_row(a, i, a.list != nullptr ? a.list[i] : i, true, lane);
+        else if (i < (count + kTile - 1) / kTile * kTile)
+            pack_row(a, i, 0, false, lane);
+        return;
+    }
+    uint32_t before = 0, count = 0;
+    bool live = false;
+    for (uint32_t q0 = 0; q0 < a.rows; q0 += 256) {
+        bool is[4];
+#pragma unroll
+        for (uint32_t y = 0; y < 4; ++y) {
+            const uint32_t r = q0 + 64 * y + lane;
+            is[y] = r < a.rows && kind_of(a.out, r) == kLive;
+        }
+#pragma unroll
+        for (uint32_t y = 0; y < 4; ++y) {
+            const uint32_t r0 = q0 + 64 * y;
+            const uint64_t some = __ballot(is[y]);
+            count += __popcll(some);
+            if (r0 + 64 <= i) {
+                before += __popcll(some);
+            } else if (r0 <= i) {
+                before += __popcll(some & ((uint64_t(1) << (i - r0)) - 1));
+                live = some >> (i - r0) & 1;
+            }
+        }
+    }
+    if (i == 0 && lane == 0) *a.count = count;
+    if (live) {
+        if (lane == 0) a.list[before] = i;
+        pack_row(a, before, i, true, lane);
+    }
+    if (i >= count && i < (count + kTile - 1) / kTile * kTile) pack_row(a, i, 0, false, lane);
 }
 
 // ----------------------------------------------------------------- scores --

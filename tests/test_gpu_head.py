@@ -491,3 +491,22 @@ def test_a_teachers_infinities_at_any_scale(scale):
     for t in head.distill_gradient(x, dev(ids, torch.int64), d_t, logp, lse, dev(grad, torch.float32),
                                    scale=scale):
         assert t.isfinite().all()
+
+
+@pytest.mark.parametrize("entries", [None, 1, 5])
+@pytest.mark.parametrize("rows", [511, 512, 513, 700])
+def test_lists_of_rows(rows, entries):
+    """Live rows among dead and void ones, where their list has a launch of its own and
+    where it has none."""
+    rng = np.random.default_rng([rows, entries or 0])
+    args = make(rng, rows, 200, 64, entries, masked=0.5)
+    args[2][rng.random(rows) < 0.1, 0] = 200
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    check(*args, 1.0, status)
+    assert status.item() == ES_HEAD_BAD_ID
+
+
+@pytest.mark.parametrize("entries", [None, 2])
+def test_more_rows_than_a_list_takes_at_a_time(entries):
+    rng = np.random.default_rng(20001)
+    check(*make(rng, 20001, 70, 16, entries, masked=0.3), 1.0)
