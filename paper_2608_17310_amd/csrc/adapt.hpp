@@ -308,8 +308,8 @@ struct FewArgs {
     uint64_t out_stride;
 };
 
-// Up to 64 rows: the waves' sums of a block meet in LDS, where each result takes its
-// own member's B u.
+// Up to 64 rows and a matrix of few: the waves' sums of a block meet in LDS, where each
+// result takes its own member's B u.
 template <int kBlocks, int kCols, int kParts>
 __global__ __launch_bounds__(512, 2) void es_adapt_few_kernel(FewArgs a) {
     using R = esring::Ring<kBlocks, kCols, kParts>;
@@ -361,10 +361,18 @@ struct StreamArgs {
     uint64_t out_stride;
 };
 
-// 2 to 64 rows of words: each lane adds its own row's B u to its four results.
-template <int kTokens, int kStages>
-__global__ __launch_bounds__(256, 2) void es_adapt_stream_kernel(StreamArgs a) {
-    using S = esstream::Stream<4, 1, kTokens, 2, kStages>;
+// Rows of words and a matrix of many rows: each lane adds its own row's B u to its four
+// results.  Bound by the matrix's bytes, so by how many of them are on their way: LDS is
+// full of stages.  32 rows of 32 members, 5120 x 17408: 46 us with the small product, where
+// two workgroups a compute unit of three stages each took 57.
+template <int kWaves, int kTokens>
+using AdaptStream = esstream::Stream<
+    kWaves, 1, kTokens, 2,
+    esstream::stages_for(16 * kWaves, kTokens, 2, 2 * (2 + (kTokens / 8 + kWaves - 1) / kWaves))>;
+
+template <int kWaves, int kTokens>
+__global__ __launch_bounds__(64 * kWaves, 1) void es_adapt_stream_kernel(StreamArgs a) {
+    using S = AdaptStream<kWaves, kTokens>;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     S t;

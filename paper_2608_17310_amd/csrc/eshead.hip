@@ -153,9 +153,8 @@ struct FewPlan {
 };
 
 // Rows of the matrix for a workgroup: an even share, in blocks of 16 rows.
-uint32_t share_of(uint32_t w_rows, uint32_t groups, uint32_t most) {
-    const uint32_t blocks = (w_rows + 15) / 16, each = (blocks + groups - 1) / groups;
-    return 16 * std::min(each, most);
+uint32_t share_of(uint32_t w_rows, uint32_t groups) {
+    return 16 * (((w_rows + 15) / 16 + groups - 1) / groups);
 }
 
 esstream::StreamArgs stream_args(const void* w, uint64_t w_stride, uint32_t w_rows, const void* x,
@@ -191,7 +190,7 @@ struct ScorePlan {
             // 31 and 28, 32 of 1024 against 25000 17 and 26.
             ringed = streams(x) && x.vocab <= 16384;
             streamed = streams(x) && !ringed;
-            share = share_of(x.vocab, kCus, ~0u / 16);
+            share = share_of(x.vocab, kCus);
             tiles = streamed ? (x.vocab + share - 1) / share : ringed ? (x.vocab + 31) / 32 : division.groups;
             parts = room.take<float>(uint64_t(2) * x.rows * tiles);
             w = nullptr;
@@ -712,6 +711,22 @@ struct AdaptPlan {
     uint64_t parts_stride;
 };
 
+template <int kWaves, int kTokens>
+void launch_stream(const esadapt::StreamArgs& t, uint32_t share, hipStream_t s) {
+    const auto kernel = esadapt::es_adapt_stream_kernel<kWaves, kTokens>;
+    const uint32_t lds = esadapt::AdaptStream<kWaves, kTokens>::kBytes;
+    hipLaunchKernelGGL(kernel, dim3((t.s.w_rows + share - 1) / share), dim3(64 * kWaves), lds, s, t);
+}
+template <int kWaves>
+void launch_stream(const esadapt::StreamArgs& t, uint32_t share, hipStream_t s) {
+    if (t.s.rows <= 16)
+        launch_stream<kWaves, 16>(t, share, s);
+    else if (t.s.rows <= 32)
+        launch_stream<kWaves, 32>(t, share, s);
+    else
+        launch_stream<kWaves, 64>(t, share, s);
+}
+
 }  // namespace
 
 extern "C" {
@@ -796,23 +811,27 @@ int es_adapt_project(const es_adapt_t* args, es_stream_t stream) try {
                            dim3(64 * esfew::kWaves), lds, s, small);
     }
     if (plan.few) {
-        // A matrix of many rows is divided among workgroups that stage the rows of x for
-        // four waves at a time, one of few rows among those whose waves share a sum.  5120 x
-        // 5120: 1 row 22 and 14 us (streamed, in rings), 16 rows 23 and 15; 5120 x 17408: 1 row
-        // 41 and 38, 32 rows 57 and 60.
-        if (x.rows > 16 && x.outer > 8192) {
-            const uint32_t share = share_of(x.outer, 2 * kCus, 4);
+        // A matrix of many rows passes through a workgroup on each compute unit, with as many
+        // waves as the unit has blocks of 16 rows of it (or half as many and two rounds, and so
+        // on); one of few rows among those whose waves share a sum.  5120 x 5120: 1 row 17 and 14
+        // us (streamed, in rings), 32 rows 22 and 18; 5120 x 8192: 32 rows 27 and 26; 5120 x
+        // 17408: 1 row 38 and 38, 16 rows 39 and 46.
+        if (x.outer > 8192) {
+            const uint32_t blocks = share_of(x.outer, kCus) / 16, rounds = (blocks + 7) / 8;
+            const uint32_t waves = (blocks + rounds - 1) / rounds, share = 16 * waves * rounds;
             esadapt::StreamArgs t{};
             t.s = stream_args(x.weight, x.w_stride, x.outer, rows.at, rows.stride, x.rows, x.inner, share);
             t.add = add;
             t.out = static_cast<uint16_t*>(x.out);
             t.out_stride = x.out_stride;
-            const bool half = x.rows <= 32;
-            const auto kernel = half ? esadapt::es_adapt_stream_kernel<32, 3>
-                                     : esadapt::es_adapt_stream_kernel<64, 2>;
-            const uint32_t lds = half ? esstream::Stream<4, 1, 32, 2, 3>::kBytes
-                                      : esstream::Stream<4, 1, 64, 2, 2>::kBytes;
-            hipLaunchKernelGGL(kernel, dim3((x.outer + share - 1) / share), dim3(256), lds, s, t);
+            switch (waves) {
+                case 3: launch_stream<3>(t, share, s); break;
+                case 4: launch_stream<4>(t, share, s); break;
+                case 5: launch_stream<5>(t, share, s); break;
+                case 6: launch_stream<6>(t, share, s); break;
+                case 7: launch_stream<7>(t, share, s); break;
+                default: launch_stream<8>(t, share, s); break;
+            }
             return launch_error("es_adapt_stream_kernel launch");
         }
         esadapt::FewArgs f{};
@@ -820,19 +839,16 @@ int es_adapt_project(const es_adapt_t* args, es_stream_t stream) try {
         f.add = add;
         f.out = static_cast<uint16_t*>(x.out);
         f.out_stride = x.out_stride;
-        const auto launch = [&](auto kernel, uint32_t blocks, uint32_t bytes) {
-            hipLaunchKernelGGL(kernel, dim3((x.outer + 16 * blocks - 1) / (16 * blocks)),
-                               dim3(64 * esfew::kWaves), esfew::kWaves * bytes, s, f);
+        const auto launch = [&](auto kernel, uint32_t bytes) {
+            hipLaunchKernelGGL(kernel, dim3((x.outer + 31) / 32), dim3(64 * esfew::kWaves),
+                               esfew::kWaves * bytes, s, f);
         };
-        // (one block of 16 rows a workgroup where there are more of them than the card holds)
-        if (x.outer > 8192)
-            launch(esadapt::es_adapt_few_kernel<1, 1, 2>, 1, esring::Ring<1, 1, 2>::kBytes);
-        else if (x.rows <= 16)
-            launch(esadapt::es_adapt_few_kernel<2, 1, 3>, 2, esring::Ring<2, 1, 3>::kBytes);
+        if (x.rows <= 16)
+            launch(esadapt::es_adapt_few_kernel<2, 1, 3>, esring::Ring<2, 1, 3>::kBytes);
         else if (x.rows <= 32)
-            launch(esadapt::es_adapt_few_kernel<2, 2, 2>, 2, esring::Ring<2, 2, 2>::kBytes);
+            launch(esadapt::es_adapt_few_kernel<2, 2, 2>, esring::Ring<2, 2, 2>::kBytes);
         else
-            launch(esadapt::es_adapt_few_kernel<2, 4, 1>, 2, esring::Ring<2, 4, 1>::kBytes);
+            launch(esadapt::es_adapt_few_kernel<2, 4, 1>, esring::Ring<2, 4, 1>::kBytes);
         return launch_error("es_adapt_few_kernel launch");
     }
     esadapt::TileArgs a{};

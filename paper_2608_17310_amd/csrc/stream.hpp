@@ -19,6 +19,12 @@ struct StreamArgs {
     uint32_t share;                        // rows of the matrix for a workgroup, a multiple of 16
 };
 
+// As many stages as LDS holds, and as a wave's loads can be counted.
+constexpr int stages_for(int tall, int tokens, int sub, int loads) {
+    const int held = 163840 / (sub * (tall + tokens) * 128), counted = 63 / loads + 1;
+    return held < counted ? held : counted;
+}
+
 template <int kOutstanding>
 __device__ __forceinline__ void wait_stage() {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(kOutstanding) : "memory");
@@ -31,7 +37,7 @@ template <int kWaves, int kBlocks, int kTokens, int kSub, int kStages>
 struct Stream {
     static constexpr uint32_t kTall = 16 * kBlocks * kWaves, kLength = kDepth * kSub;
     static constexpr int kWLoads = 2 * kBlocks;                                   // of a wave and 64
-    static constexpr int kXLoads = kTokens * 128 / 1024 < kWaves ? 1 : kTokens * 128 / 1024 / kWaves;
+    static constexpr int kXLoads = (kTokens / 8 + kWaves - 1) / kWaves;
     static constexpr int kLoads = kSub * (kWLoads + kXLoads);
     static constexpr uint32_t kXAt = kTall * 128, kPart = kXAt + kTokens * 128, kStage = kSub * kPart;
     static constexpr uint32_t kBytes = kStages * kStage;

@@ -88,6 +88,15 @@ def test_project(rows, inner, outer, rank, members, how):
         check(x, w, a, b, None, index, Adapters(a, b).project(x, w, ints(index)))
 
 
+@pytest.mark.parametrize("outer", [8193, 16384, 20003, 24000, 28672, 32761, 40000, 70001])
+@pytest.mark.parametrize("rows,inner,rank", [(1, 72, 8), (17, 200, 16), (33, 64, 40), (64, 136, 8)])
+def test_a_matrix_of_many_rows(outer, rows, inner, rank):
+    """Three to eight waves a compute unit, one round and several, shares that end early."""
+    rng = np.random.default_rng([rows, outer])
+    x, w, a, b, scales, index = make(rng, rows, inner, outer, rank, 3)
+    check(x, w, a, b, scales, index, Adapters(a, b, scales).project(x, w, ints(index)))
+
+
 @pytest.mark.parametrize("rows", [1, 9, 64, 65, 200])
 def test_strides_and_outputs(rows):
     """Rows inside wider ones at any alignment; nothing beside the output is written."""
