@@ -152,10 +152,19 @@ struct FewPlan {
     }
 };
 
-// Rows of the matrix for a workgroup: an even share, in blocks of 16 rows.
-uint32_t share_of(uint32_t w_rows, uint32_t groups) {
-    return 16 * (((w_rows + 15) / 16 + groups - 1) / groups);
-}
+// How a matrix of many rows is divided among a workgroup on each compute unit: an even
+// share, in blocks of 16 rows, and as many waves, of `blocks` blocks each, as make equal
+// rounds of it (151936 x 1024: three rounds of seven waves where eight left the third
+// a third full: 77 rows 63 and 69 us, 1 row 58 and 59; 64 rows of 2560 147 and 145).
+struct StreamPlan {
+    uint32_t waves, share, groups;
+    StreamPlan(uint32_t w_rows, uint32_t blocks) {
+        share = 16 * (((w_rows + 15) / 16 + kCus - 1) / kCus);
+        const uint32_t each = (share / 16 + blocks - 1) / blocks, rounds = (each + 7) / 8;
+        waves = (each + rounds - 1) / rounds;
+        groups = (w_rows + share - 1) / share;
+    }
+};
 
 esstream::StreamArgs stream_args(const void* w, uint64_t w_stride, uint32_t w_rows, const void* x,
                                  uint64_t x_stride, uint32_t rows, uint32_t width, uint32_t share) {
@@ -163,7 +172,8 @@ esstream::StreamArgs stream_args(const void* w, uint64_t w_stride, uint32_t w_ro
                                 x_stride, w_rows, rows, width, share};
 }
 
-// Rows of words, few enough that the matrix's bytes are what they cost.
+// Rows of words, few enough that the matrix's bytes are what they cost.  (128 rows of 2560
+// against 151936 176 us, 129 in tiles 249.)
 bool streams(const es_head_score_t& x) {
     return x.rows <= esstream::kRows && word_rows(x.weight, x.w_stride, x.hidden) &&
            word_rows(x.x, x.x_stride, x.hidden);
@@ -172,7 +182,7 @@ bool streams(const es_head_score_t& x) {
 struct ScorePlan {
     bool few, streamed, ringed;
     uint32_t size;                         // of a tile
-    uint32_t share;
+    uint32_t share, waves;                 // streamed
     HeadRows head;
     Lists lists;
     FewPlan division;
@@ -190,8 +200,10 @@ struct ScorePlan {
             // 31 and 28, 32 of 1024 against 25000 17 and 26.
             ringed = streams(x) && x.vocab <= 16384;
             streamed = streams(x) && !ringed;
-            share = share_of(x.vocab, kCus);
-            tiles = streamed ? (x.vocab + share - 1) / share : ringed ? (x.vocab + 31) / 32 : division.groups;
+            const StreamPlan stream(x.vocab, 2);
+            share = stream.share;
+            waves = stream.waves;
+            tiles = streamed ? stream.groups : ringed ? (x.vocab + 31) / 32 : division.groups;
             parts = room.take<float>(uint64_t(2) * x.rows * tiles);
             w = nullptr;
             return;
@@ -298,6 +310,24 @@ Side head_side(const HeadRows& h, const void* w, uint64_t stride, uint16_t* room
     return Side{room, h.padded, have};
 }
 
+template <int kWaves, int kTokens>
+void launch_stream(const eshead::StreamStatsArgs& t, uint32_t groups, hipStream_t s) {
+    const auto kernel = eshead::es_head_stream_kernel<kWaves, kTokens>;
+    const uint32_t lds = eshead::HeadStream<kWaves, kTokens>::kBytes;
+    hipLaunchKernelGGL(kernel, dim3(groups), dim3(64 * kWaves), lds, s, t);
+}
+template <int kWaves>
+void launch_stream(const eshead::StreamStatsArgs& t, uint32_t groups, hipStream_t s) {
+    if (t.s.rows <= 32)
+        launch_stream<kWaves, 32>(t, groups, s);
+    else if (t.s.rows <= 64)
+        launch_stream<kWaves, 64>(t, groups, s);
+    else if (t.s.rows <= 96)
+        launch_stream<kWaves, 96>(t, groups, s);
+    else
+        launch_stream<kWaves, 128>(t, groups, s);
+}
+
 esfew::FewArgs few_args(const void* w, uint64_t w_stride, uint32_t w_rows, const void* x,
                         uint64_t x_stride, uint32_t rows, uint32_t width) {
     esfew::FewArgs f{};
@@ -385,13 +415,14 @@ int es_head_score(const es_head_score_t* args, es_stream_t stream) try {
         t.s = stream_args(x.weight, x.w_stride, x.vocab, x.x, x.x_stride, x.rows, x.hidden, plan.share);
         t.parts = plan.parts;
         t.factor = x.scale * eshead::kLog2e;
-        const auto kernel = x.rows <= 32   ? eshead::es_head_stream_kernel<32, 4>
-                            : x.rows <= 64 ? eshead::es_head_stream_kernel<64, 4>
-                                           : eshead::es_head_stream_kernel<128, 3>;
-        const uint32_t lds = x.rows <= 32   ? esstream::Stream<8, 2, 32, 1, 4>::kBytes
-                             : x.rows <= 64 ? esstream::Stream<8, 2, 64, 1, 4>::kBytes
-                                            : esstream::Stream<8, 2, 128, 1, 3>::kBytes;
-        hipLaunchKernelGGL(kernel, dim3(plan.tiles), dim3(512), lds, s, t);
+        switch (plan.waves) {
+            case 3: launch_stream<3>(t, plan.tiles, s); break;
+            case 4: launch_stream<4>(t, plan.tiles, s); break;
+            case 5: launch_stream<5>(t, plan.tiles, s); break;
+            case 6: launch_stream<6>(t, plan.tiles, s); break;
+            case 7: launch_stream<7>(t, plan.tiles, s); break;
+            default: launch_stream<8>(t, plan.tiles, s); break;
+        }
         hipLaunchKernelGGL(eshead::es_head_score_kernel, dim3(x.rows), dim3(256), 0, s, a);
         return launch_error("es_head_stream_kernel launch");
     }
@@ -712,19 +743,19 @@ struct AdaptPlan {
 };
 
 template <int kWaves, int kTokens>
-void launch_stream(const esadapt::StreamArgs& t, uint32_t share, hipStream_t s) {
+void launch_stream(const esadapt::StreamArgs& t, uint32_t groups, hipStream_t s) {
     const auto kernel = esadapt::es_adapt_stream_kernel<kWaves, kTokens>;
     const uint32_t lds = esadapt::AdaptStream<kWaves, kTokens>::kBytes;
-    hipLaunchKernelGGL(kernel, dim3((t.s.w_rows + share - 1) / share), dim3(64 * kWaves), lds, s, t);
+    hipLaunchKernelGGL(kernel, dim3(groups), dim3(64 * kWaves), lds, s, t);
 }
 template <int kWaves>
-void launch_stream(const esadapt::StreamArgs& t, uint32_t share, hipStream_t s) {
+void launch_stream(const esadapt::StreamArgs& t, uint32_t groups, hipStream_t s) {
     if (t.s.rows <= 16)
-        launch_stream<kWaves, 16>(t, share, s);
+        launch_stream<kWaves, 16>(t, groups, s);
     else if (t.s.rows <= 32)
-        launch_stream<kWaves, 32>(t, share, s);
+        launch_stream<kWaves, 32>(t, groups, s);
     else
-        launch_stream<kWaves, 64>(t, share, s);
+        launch_stream<kWaves, 64>(t, groups, s);
 }
 
 }  // namespace
@@ -817,20 +848,19 @@ int es_adapt_project(const es_adapt_t* args, es_stream_t stream) try {
         // us (streamed, in rings), 32 rows 22 and 18; 5120 x 8192: 32 rows 27 and 26; 5120 x
         // 17408: 1 row 38 and 38, 16 rows 39 and 46.
         if (x.outer > 8192) {
-            const uint32_t blocks = share_of(x.outer, kCus) / 16, rounds = (blocks + 7) / 8;
-            const uint32_t waves = (blocks + rounds - 1) / rounds, share = 16 * waves * rounds;
+            const StreamPlan plan(x.outer, 1);
             esadapt::StreamArgs t{};
-            t.s = stream_args(x.weight, x.w_stride, x.outer, rows.at, rows.stride, x.rows, x.inner, share);
+            t.s = stream_args(x.weight, x.w_stride, x.outer, rows.at, rows.stride, x.rows, x.inner, plan.share);
             t.add = add;
             t.out = static_cast<uint16_t*>(x.out);
             t.out_stride = x.out_stride;
-            switch (waves) {
-                case 3: launch_stream<3>(t, share, s); break;
-                case 4: launch_stream<4>(t, share, s); break;
-                case 5: launch_stream<5>(t, share, s); break;
-                case 6: launch_stream<6>(t, share, s); break;
-                case 7: launch_stream<7>(t, share, s); break;
-                default: launch_stream<8>(t, share, s); break;
+            switch (plan.waves) {
+                case 3: launch_stream<3>(t, plan.groups, s); break;
+                case 4: launch_stream<4>(t, plan.groups, s); break;
+                case 5: launch_stream<5>(t, plan.groups, s); break;
+                case 6: launch_stream<6>(t, plan.groups, s); break;
+                case 7: launch_stream<7>(t, plan.groups, s); break;
+                default: launch_stream<8>(t, plan.groups, s); break;
             }
             return launch_error("es_adapt_stream_kernel launch");
         }

@@ -395,10 +395,17 @@ struct StreamStatsArgs {
 };
 
 // The same of up to 128 rows of words: a workgroup's share of the vocabulary is a part,
-// whose maxima and sums run along in registers.
-template <int kTokens, int kStages>
-__global__ __launch_bounds__(512, 2) void es_head_stream_kernel(StreamStatsArgs a) {
-    using S = esstream::Stream<8, 2, kTokens, 1, kStages>;
+// whose maxima and sums run along in registers.  Bound by the head's bytes: 32 rows of
+// 5120 against 151936 266 us, 5.9 TB/s, with the scores' kernel; 128 of 2560 171 us, 4.6 TB/s
+// and, with the operands' reads from LDS, not far from the matrix unit's bound.
+template <int kWaves, int kTokens>
+using HeadStream = esstream::Stream<
+    kWaves, 2, kTokens, 1,
+    esstream::stages_for(32 * kWaves, kTokens, 1, 4 + (kTokens / 8 + kWaves - 1) / kWaves)>;
+
+template <int kWaves, int kTokens>
+__global__ __launch_bounds__(64 * kWaves, 1) void es_head_stream_kernel(StreamStatsArgs a) {
+    using S = HeadStream<kWaves, kTokens>;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     float top[S::kCols], sum[S::kCols];
@@ -430,7 +437,7 @@ __global__ __launch_bounds__(512, 2) void es_head_stream_kernel(StreamStatsArgs 
         }
     });
     __syncthreads();                       // every wave has left the last stage
-    float* const pair = reinterpret_cast<float*>(lds);   // [8 waves][kTokens] pairs
+    float* const pair = reinterpret_cast<float*>(lds);   // [kWaves][kTokens] pairs
 #pragma unroll
     for (int j = 0; j < S::kCols; ++j) {
         float most = fmaxf(top[j], __shfl_xor(top[j], 16));
@@ -448,10 +455,10 @@ __global__ __launch_bounds__(512, 2) void es_head_stream_kernel(StreamStatsArgs 
     const uint32_t n = threadIdx.x;
     if (n < kTokens && n < a.s.rows) {
         float most = -eskv::inf();
-        for (uint32_t w = 0; w < 8; ++w) most = fmaxf(most, pair[2 * (kTokens * w + n)]);
+        for (uint32_t w = 0; w < kWaves; ++w) most = fmaxf(most, pair[2 * (kTokens * w + n)]);
         const float from = most == -eskv::inf() ? 0.0f : most;
         float all = 0.0f;
-        for (uint32_t w = 0; w < 8; ++w)
+        for (uint32_t w = 0; w < kWaves; ++w)
             all += pair[2 * (kTokens * w + n) + 1] *
                    __builtin_amdgcn_exp2f(pair[2 * (kTokens * w + n)] - from);
         float* const to = a.parts + 2 * (uint64_t(n) * gridDim.x + blockIdx.x);

@@ -510,3 +510,10 @@ def test_lists_of_rows(rows, entries):
 def test_more_rows_than_a_list_takes_at_a_time(entries):
     rng = np.random.default_rng(20001)
     check(*make(rng, 20001, 70, 16, entries, masked=0.3), 1.0)
+
+
+@pytest.mark.parametrize("vocab", [16400, 25000, 40003, 48000, 56001, 65000, 80009])
+@pytest.mark.parametrize("rows,hidden,entries", [(2, 72, None), (33, 40, 3), (96, 64, None), (97, 8, None)])
+def test_streams_of_any_number_of_waves(vocab, rows, hidden, entries):
+    rng = np.random.default_rng([vocab, rows])
+    check(*make(rng, rows, vocab, hidden, entries), 1.0)
