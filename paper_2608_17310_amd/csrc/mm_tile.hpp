@@ -1,5 +1,5 @@
 // The matrix product that the head and the projections are made of: tiles of
-// 256 x 256 results on the matrix unit, from operands in either order, with what
+// 256 x 256 results (128 x 128 where there are few) on the matrix unit, from operands in either order, with what
 // becomes of a tile (its epilogue) as a parameter.
 #pragma once
 
@@ -31,7 +31,8 @@ struct Shape {
     static constexpr int kThreads = 2 * kSize;                     // waves of kSize / 2 by 64 results
     static constexpr uint32_t kSide = kSize * kDepth * 2;          // bytes of a stage's side
     static constexpr uint32_t kPitch = kSize * 2 + 16;             // of a row of results in LDS
-    static constexpr uint32_t kLds = 4 * kSide > kSize * kPitch ? 4 * kSide : kSize * kPitch;
+    static constexpr uint32_t kLds = 5 * kSide;                    // three stages of a, two of b
+    static_assert(kLds >= kSize * kPitch, "a tile's results fit the stages");
 };
 
 // One operand.  Deep: element (i, k) at at[i stride + k], wide: at[k stride + i],
@@ -235,12 +236,16 @@ struct Count {
     static constexpr int value = n;
 };
 
-// Rows n0 .. n0 + n_have of n are there (more than the tile has count as all).  Two
-// stages in LDS: while the products of a stage's first step are made its second's
-// operands are read; then the stage is in registers and, once the next has landed, the
-// one after it may be asked for, a load to a product.  4096 rows of 5120 against 151936 (256 x
-// 256): 4.76 to 4.89 ms, 1.30 to 1.34 PFLOP/s, where one barrier and no loads between
-// products took 5.13 and loads half a step later 4.97; the clock is 1.9 GHz.
+// Rows n0 .. n0 + n_have of n are there (more than the tile has count as all).  Three
+// stages of a and two of b in LDS, all that it holds: while the products of a stage's first
+// step are made its second's operands are read; then the stage is in registers and, once
+// the next has landed, b's stage after that and a's after that again may be asked for, a
+// load to a product.  A stage takes 1.6 us at any clock from 1.8 GHz (where the card's
+// power leaves it at 5120) to 2.2 (2560): it waits for memory and for the other waves as much as
+// for the matrix unit, which is busy for 66 and 52 % of the time.  4096 rows of 5120 against
+// 151936 (256 x 256): 4.76 ms, 1.34 PFLOP/s; 1021 of 2560 670 us where two stages of a took 697.
+// (With two stages of each 4.79; one barrier a stage and no loads between products 5.13, loads
+// half a step later 4.97.)
 template <bool kWideA, bool kWideB, int kSize>
 __device__ __forceinline__ void product_tile(const Product& p, uint32_t m0, uint32_t n0, uint32_t n_have,
                                              uint32_t k0, uint32_t k_end, uint8_t* lds, Tile<kSize>& c) {
@@ -261,24 +266,41 @@ __device__ __forceinline__ void product_tile(const Product& p, uint32_t m0, uint
     ra.init(kSize / 2 * (wave & 1), lane);
     rb.init(64 * (wave >> 1), lane);
     const uint32_t lds_at = uniform(lds_address(lds));
-    uint32_t buf = 0;                                    // of the stage in use, 0 or 2 sides
-    auto issue = [&](uint32_t k, uint32_t at) {          // (the right side is always whole)
-        const u32x4_t ba = sa.take(), bb = sb.take();
+    uint32_t at_a = 0, at_b = 3 * kSide;                 // of the stage in use
+    auto issue_a = [&](uint32_t k, uint32_t at) {
+        const u32x4_t buffer = sa.take();
 #pragma unroll
         for (uint32_t x = 0; x < 4; ++x) {
             if (k_end - k >= kDepth)
-                sa.load(ba, lds_at + at, x);
+                sa.load(buffer, lds_at + at, x);
             else
-                sa.load_last(ba, lds_at + at, x, k_end - k, p.a, wave, lane);
-            sb.load(bb, lds_at + at + kSide, x);
+                sa.load_last(buffer, lds_at + at, x, k_end - k, p.a, wave, lane);
         }
+    };
+    auto issue_b = [&](uint32_t at) {                    // (always whole)
+        const u32x4_t buffer = sb.take();
+#pragma unroll
+        for (uint32_t x = 0; x < 4; ++x) sb.load(buffer, lds_at + at, x);
+    };
+    // The stage after k's has landed for every wave, of a's loads those for the one after it
+    // may be out.
+    auto landed = [&](uint32_t k) {
+        if (k + 2 * kDepth < k_end)
+            wait_all_but<4>();
+        else
+            wait_staged();
+        __builtin_amdgcn_s_barrier();
+    };
+    auto advance = [&]() {
+        at_a = at_a == 2 * kSide ? 0 : at_a + kSide;
+        at_b = 7 * kSide - at_b;
     };
     bf16x8_t a[2][kBlocks], b[2][4];
     auto read = [&](int s) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) b[s][j] = rb.read(lds + buf + kSide, s, j);
+        for (int j = 0; j < 4; ++j) b[s][j] = rb.read(lds + at_b, s, j);
 #pragma unroll
-        for (int i = 0; i < kBlocks; ++i) a[s][i] = ra.read(lds + buf, s, i);
+        for (int i = 0; i < kBlocks; ++i) a[s][i] = ra.read(lds + at_a, s, i);
     };
     // 16 x 16 x 32 a product: at the clock that the card's power leaves it makes 1.92
     // PFLOP/s with its reads from LDS where 32 x 32 x 16 makes 1.72
@@ -299,9 +321,16 @@ __device__ __forceinline__ void product_tile(const Product& p, uint32_t m0, uint
         }
         __builtin_amdgcn_sched_barrier(0);
     };
-    issue(k0, 0);
+    issue_a(k0, 0);
+    issue_b(3 * kSide);
     if (k0 + kDepth < k_end) {
-        issue(k0 + kDepth, 2 * kSide);
+        issue_a(k0 + kDepth, kSide);
+        issue_b(4 * kSide);
+    }
+    if (k0 + 2 * kDepth < k_end) {
+        issue_a(k0 + 2 * kDepth, 2 * kSide);
+        wait_all_but<12>();
+    } else if (k0 + kDepth < k_end) {
         wait_all_but<8>();
     } else {
         wait_staged();
@@ -309,10 +338,10 @@ __device__ __forceinline__ void product_tile(const Product& p, uint32_t m0, uint
     __builtin_amdgcn_s_barrier();
     if (64 * (wave >> 1) >= n_have) {                    // a wave without rows only stages
         for (uint32_t k = k0; k + kDepth < k_end; k += kDepth) {
-            wait_staged();
-            __builtin_amdgcn_s_barrier();
-            if (k + 2 * kDepth < k_end) issue(k + 2 * kDepth, buf);
-            buf ^= 2 * kSide;
+            landed(k);
+            if (k + 2 * kDepth < k_end) issue_b(at_b);
+            if (k + 3 * kDepth < k_end) issue_a(k + 3 * kDepth, at_a);
+            advance();
         }
         return;
     }
@@ -321,22 +350,22 @@ __device__ __forceinline__ void product_tile(const Product& p, uint32_t m0, uint
         read(1);
         multiply(0, 0);
         interleave(Count<kProducts>{});
-        // all of the stage is in registers, and the next has landed
-        wait_staged();
-        __builtin_amdgcn_s_barrier();
-        buf ^= 2 * kSide;
     };
     uint32_t k = k0;
-    for (; k + 3 * kDepth <= k_end; k += kDepth) {       // the stage after the next is whole
+    for (; k + 4 * kDepth <= k_end; k += kDepth) {       // the stages to ask for are whole
         first_step();
-        const uint32_t old = lds_at + (buf ^ 2 * kSide);
+        // all of the stage is in registers, and the next has landed
+        wait_all_but<4>();
+        __builtin_amdgcn_s_barrier();
+        const uint32_t old_a = lds_at + at_a, old_b = lds_at + at_b;
+        advance();
         const u32x4_t ba = sa.take(), bb = sb.take();
 #pragma unroll
         for (uint32_t x = 0; x < 8; ++x) {
             if (x < 4)
-                sa.load(ba, old, x);
+                sb.load(bb, old_b, x);
             else
-                sb.load(bb, old + kSide, x - 4);
+                sa.load(ba, old_a, x - 4);
             c.x[x / 4][x % 4] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[1][x / 4], b[1][x % 4],
                                                                         c.x[x / 4][x % 4], 0, 0, 0);
             __builtin_amdgcn_sched_barrier(0);
@@ -347,7 +376,10 @@ __device__ __forceinline__ void product_tile(const Product& p, uint32_t m0, uint
     }
     for (; k + kDepth < k_end; k += kDepth) {
         first_step();
-        if (k + 2 * kDepth < k_end) issue(k + 2 * kDepth, buf ^ 2 * kSide);
+        landed(k);
+        if (k + 2 * kDepth < k_end) issue_b(at_b);
+        if (k + 3 * kDepth < k_end) issue_a(k + 3 * kDepth, at_a);
+        advance();
         read(0);
         multiply(1, 0);
         interleave(Count<kProducts>{});
