@@ -33,7 +33,8 @@ from .kvcache import KVCache
 # log-softmax: 10 bytes each).
 LOGITS_AT_A_TIME = 1 << 28
 
-# Rows that `score` and `divergence` take to the head at once: its calls have at most 65536.
+# Rows that `score` and `divergence` take to the head at once, at most: its calls have up to
+# 65536, and 2^36 logits.
 ROWS_AT_A_TIME = 1 << 15
 
 PROJECTIONS = ("q", "k", "v", "o", "gate", "up", "down")
@@ -110,7 +111,9 @@ class Decoder:
         """The member whose adapters each sequence is evaluated under, [seqs]
         (negative: none).  What is already in the cache stays as it is.  Numbers
         on the GPU are not read back to be checked."""
-        members = torch.as_tensor(members, dtype=torch.int32)
+        members = torch.as_tensor(members)
+        if members.is_floating_point():
+            raise ValueError(f"members must be integers, not {members.dtype}")
         if members.shape != self.members.shape:
             raise ValueError(f"members of shape {tuple(members.shape)} for {len(self.members)} sequences")
         if self.adapters is None:
@@ -118,7 +121,7 @@ class Decoder:
         least = min((a.members for layer in self.adapters for a in layer.values()), default=0)
         if not members.is_cuda and len(members) and int(members.max()) >= least:
             raise ValueError(f"members must be below {least}, got {int(members.max())}")
-        self.members.copy_(members)
+        self.members.copy_(members.long().clamp(-1, 2 ** 31 - 1))   # (what int32 cannot hold is no member)
 
     def _forward(self, tokens, seq, positions, starts, max_rows):
         """Hidden states [tokens, hidden] of packed tokens, whose keys and values
@@ -223,6 +226,10 @@ class Decoder:
         at = seq[rows], positions[rows] + 1 - begin[seq[rows]]
         return x, rows, tokens[rows + 1], at, (len(sizes), max(map(len, targets)))
 
+    def _slabs(self, rows):
+        slab = min(ROWS_AT_A_TIME, (1 << 36) // len(self.head))
+        return ((i, i + slab) for i in range(0, rows, slab))
+
     @staticmethod
     def _sums(terms, at, shape):
         """The sum of each sequence's terms, in one order: rewards are the same every time."""
@@ -247,9 +254,8 @@ class Decoder:
         stored: nearer to the model's own by the logits' rounding to bf16."""
         x, rows, tokens, at, shape = self._answers(prompts, targets)
         got = torch.empty(len(rows), dtype=torch.float32, device=rows.device)
-        for i in range(0, len(rows), ROWS_AT_A_TIME):
-            got[i:i + ROWS_AT_A_TIME] = Head(self.head).score(
-                x[rows[i:i + ROWS_AT_A_TIME]], tokens[i:i + ROWS_AT_A_TIME])[0]
+        for i, j in self._slabs(len(rows)):
+            got[i:j] = Head(self.head).score(x[rows[i:j]], tokens[i:j])[0]
         return self._sums(got, at, shape)
 
     def top_logits(self, prompts, targets, count):
@@ -278,7 +284,6 @@ class Decoder:
             raise ValueError(f"a teacher's {len(ids)} rows for {sum(map(len, targets))} tokens")
         x, rows, _, at, shape = self._answers(prompts, targets)
         got = torch.empty(len(rows), dtype=torch.float32, device=rows.device)
-        for i in range(0, len(rows), ROWS_AT_A_TIME):
-            j = i + ROWS_AT_A_TIME
+        for i, j in self._slabs(len(rows)):
             got[i:j] = Head(self.head).distill(x[rows[i:j]], ids[i:j], logits[i:j], scale=scale)[0]
         return self._sums(got, at, shape)

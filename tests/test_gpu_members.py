@@ -203,11 +203,13 @@ def test_what_assign_and_adapters_refuse():
     with pytest.raises(ValueError):
         plain.assign([0, 1])
     model = Decoder(params, HQ, H, D, False, seqs=2, length=64, adapters=adapters)
-    for bad in ([0], [0, 1, 1], [0, 2]):
+    for bad in ([0], [0, 1, 1], [0, 2], [0.0, 1.0], [0, 1 << 32], [[0, 1]]):
         with pytest.raises(ValueError):
             model.assign(bad)
         assert model.members.tolist() == [-1, -1]
-    model.assign(torch.tensor([0, 5]).cuda())              # not read back, but reported
+    model.assign([-(1 << 40), 1])
+    assert model.members.tolist() == [-1, 1]
+    model.assign(torch.tensor([0, 1 << 32]).cuda())        # not read back, but reported
     model.prefill([[1, 2], [3]])
     assert model.member_status.item() == 1
 
