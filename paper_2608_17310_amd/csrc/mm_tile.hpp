@@ -239,13 +239,13 @@ struct Count {
 // Rows n0 .. n0 + n_have of n are there (more than the tile has count as all).  Three
 // stages of a and two of b in LDS, all that it holds: while the products of a stage's first
 // step are made its second's operands are read; then the stage is in registers and, once
-// the next has landed, b's stage after that and a's after that again may be asked for, a
-// load to a product.  A stage takes 1.6 us at any clock from 1.8 GHz (where the card's
-// power leaves it at 5120) to 2.2 (2560): it waits for memory and for the other waves as much as
-// for the matrix unit, which is busy for 66 and 52 % of the time.  4096 rows of 5120 against
-// 151936 (256 x 256): 4.76 ms, 1.34 PFLOP/s; 1021 of 2560 670 us where two stages of a took 697.
-// (With two stages of each 4.79; one barrier a stage and no loads between products 5.13, loads
-// half a step later 4.97.)
+// the next has landed, b's stage after that and a's after that again are asked for, a load
+// to some products each: eight waves that ask for all of it at once wait for the loads'
+// way in.  4096 rows of 5120 against 151936 (256 x 256): 4.65 ms, 1.37 PFLOP/s; 1024 of 2560
+// 672 us.  Two products to a load of b and six to one of a (one each: 4.78 and 697, but with a
+// wide, whose reads are twice as many, it is the faster by 3 to 5 %; a's loads in the next stage's first step 4.80 and 693); two stages of a and one product to a
+// load 4.82 and 712; without loads in the loop 3.70 and 547.  The clock falls to 1.8 GHz
+// at 5120 (the card's power) and stays at 2.2 at 2560.
 template <bool kWideA, bool kWideB, int kSize>
 __device__ __forceinline__ void product_tile(const Product& p, uint32_t m0, uint32_t n0, uint32_t n_have,
                                              uint32_t k0, uint32_t k_end, uint8_t* lds, Tile<kSize>& c) {
@@ -296,27 +296,33 @@ __device__ __forceinline__ void product_tile(const Product& p, uint32_t m0, uint
         at_b = 7 * kSide - at_b;
     };
     bf16x8_t a[2][kBlocks], b[2][4];
+    auto read_one = [&](int s, int r) {
+        if (r < 4)
+            b[s][r] = rb.read(lds + at_b, s, r);
+        else
+            a[s][r - 4] = ra.read(lds + at_a, s, r - 4);
+    };
     auto read = [&](int s) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) b[s][j] = rb.read(lds + at_b, s, j);
-#pragma unroll
-        for (int i = 0; i < kBlocks; ++i) a[s][i] = ra.read(lds + at_a, s, i);
+        for (int r = 0; r < 4 + kBlocks; ++r) read_one(s, r);
     };
     // 16 x 16 x 32 a product: at the clock that the card's power leaves it makes 1.92
     // PFLOP/s with its reads from LDS where 32 x 32 x 16 makes 1.72
-    auto multiply = [&](int s, int from) {
+    auto one = [&](int s, int y) {
+        c.x[y / 4][y % 4] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[s][y / 4], b[s][y % 4],
+                                                                    c.x[y / 4][y % 4], 0, 0, 0);
+    };
+    auto multiply = [&](int s) {
 #pragma unroll
-        for (int y = from; y < kProducts; ++y)
-            c.x[y / 4][y % 4] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[s][y / 4], b[s][y % 4],
-                                                                        c.x[y / 4][y % 4], 0, 0, 0);
+        for (int y = 0; y < kProducts; ++y) one(s, y);
     };
     // the reads of a step go out one to a product, from the first on
     constexpr int kReads = (kWideA ? 2 : 1) * kBlocks + (kWideB ? 8 : 4), kMatrix = 0x8, kDsRead = 0x100;
-    auto interleave = [&](auto products) {
-        constexpr int n = decltype(products)::value, each = (kReads + n - 1) / n;
+    auto interleave = [&](auto products, auto reads) {
+        constexpr int n = decltype(products)::value, m = decltype(reads)::value, each = (m + n - 1) / n;
 #pragma unroll
         for (int x = 0; x < n; ++x) {
-            if (x * each < kReads) __builtin_amdgcn_sched_group_barrier(kDsRead, each, 0);
+            if (x * each < m) __builtin_amdgcn_sched_group_barrier(kDsRead, each, 0);
             __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 0);
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -348,8 +354,8 @@ __device__ __forceinline__ void product_tile(const Product& p, uint32_t m0, uint
     read(0);
     auto first_step = [&]() {
         read(1);
-        multiply(0, 0);
-        interleave(Count<kProducts>{});
+        multiply(0);
+        interleave(Count<kProducts>{}, Count<kReads>{});
     };
     uint32_t k = k0;
     for (; k + 4 * kDepth <= k_end; k += kDepth) {       // the stages to ask for are whole
@@ -360,19 +366,34 @@ __device__ __forceinline__ void product_tile(const Product& p, uint32_t m0, uint
         const uint32_t old_a = lds_at + at_a, old_b = lds_at + at_b;
         advance();
         const u32x4_t ba = sa.take(), bb = sb.take();
+        // products to a load of b and of a, and operands read to one of a (wide: behind them all)
+        constexpr int kToB = kWideA ? 1 : kProducts / 16, kToA = kWideA ? 1 : 3 * kProducts / 16;
+        constexpr int kRow = (4 + kBlocks) / 4, kLeft = kProducts - 4 * kToB - 4 * kToA;
 #pragma unroll
-        for (uint32_t x = 0; x < 8; ++x) {
-            if (x < 4)
-                sb.load(bb, old_b, x);
-            else
-                sa.load(ba, old_a, x - 4);
-            c.x[x / 4][x % 4] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[1][x / 4], b[1][x % 4],
-                                                                        c.x[x / 4][x % 4], 0, 0, 0);
+        for (uint32_t x = 0; x < 4; ++x) {
+            sb.load(bb, old_b, x);
+#pragma unroll
+            for (int y = 0; y < kToB; ++y) one(1, kToB * x + y);
             __builtin_amdgcn_sched_barrier(0);
         }
-        read(0);
-        multiply(1, 8);
-        interleave(Count<kProducts - 8>{});
+#pragma unroll
+        for (uint32_t x = 0; x < 4; ++x) {
+            sa.load(ba, old_a, x);
+            if constexpr (!kWideA) {
+#pragma unroll
+                for (int r = kRow * x; r < kRow * int(x + 1); ++r) read_one(0, r);
+            }
+#pragma unroll
+            for (int y = 0; y < kToA; ++y) one(1, 4 * kToB + kToA * x + y);
+            if constexpr (!kWideA) interleave(Count<kToA>{}, Count<kReads / 4>{});
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if constexpr (kWideA) {
+            read(0);
+#pragma unroll
+            for (int y = kProducts - kLeft; y < kProducts; ++y) one(1, y);
+            interleave(Count<kLeft>{}, Count<kReads>{});
+        }
     }
     for (; k + kDepth < k_end; k += kDepth) {
         first_step();
@@ -381,13 +402,13 @@ __device__ __forceinline__ void product_tile(const Product& p, uint32_t m0, uint
         if (k + 3 * kDepth < k_end) issue_a(k + 3 * kDepth, at_a);
         advance();
         read(0);
-        multiply(1, 0);
-        interleave(Count<kProducts>{});
+        multiply(1);
+        interleave(Count<kProducts>{}, Count<kReads>{});
     }
     read(1);
-    multiply(0, 0);
-    interleave(Count<kProducts>{});
-    multiply(1, 0);
+    multiply(0);
+    interleave(Count<kProducts>{}, Count<kReads>{});
+    multiply(1);
 }
 
 // f(x, m, n): the words of four results, rows m .. m + 3 and row n of the tile.
