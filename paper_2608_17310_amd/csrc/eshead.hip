@@ -68,8 +68,9 @@ uint64_t tiles_of(uint64_t m, uint64_t n, uint32_t size) {
 }
 
 // Tiles of 128 x 128 results where the card holds them at once (two a compute unit), of
-// 256 x 256 where there are more.  5120 x 5120: 1000 rows (320 small tiles) 77 and 120 us,
-// 2000 (640) 137 and 127; 5120 x 17408: 300 rows (408) 108 and 137.
+// 256 x 256 where there are more.  5120 x 5120: 1000 rows (320 small tiles) 81 and 115 us,
+// 2000 (640) 121 and 121; 5120 x 17408: 300 rows (408) 99 and 114; 129 rows against 151936 x
+// 2560 (2374) 260 and 211.
 uint32_t tile_for(uint64_t m, uint64_t n) {
     return tiles_of(m, n, kSmallTile) <= 2 * kCus ? kSmallTile : kTile;
 }
@@ -173,7 +174,7 @@ esstream::StreamArgs stream_args(const void* w, uint64_t w_stride, uint32_t w_ro
 }
 
 // Rows of words, few enough that the matrix's bytes are what they cost.  (128 rows of 2560
-// against 151936 176 us, 129 in tiles 249.)
+// against 151936 171 us, 129 in tiles 211.)
 bool streams(const es_head_score_t& x) {
     return x.rows <= esstream::kRows && word_rows(x.weight, x.w_stride, x.hidden) &&
            word_rows(x.x, x.x_stride, x.hidden);
@@ -720,9 +721,8 @@ struct AdaptPlan {
         parts = nullptr;
         parts_stride = up(a.outer, 4);
         // Few tiles' sums are divided, if a part is worth the join: a stage of 64 takes 0.6 us,
-        // the join's launch and its bytes the rest.  5120 x 5120, 100 rows (40 tiles) 79 us
-        // whole and 48 divided, 300 (120) 65 and 51, 700 (240) 66 and 77; 1024 x 1024, 1000 rows
-        // (64) 21 and 26.
+        // the join's launch and its bytes the rest.  5120 x 5120, 100 rows (40 tiles) 48 us
+        // whole and 25 divided, 300 (120) 48 and 47, 700 (240) 57 and 78.
         uint64_t most = 1;
         const double whole = 0.6 * a.inner / kDepth, join = 8e-6 * a.rows * a.outer / 2.5;
         double best = whole;
