@@ -1,6 +1,8 @@
 // Products of a large matrix with at most 64 rows: bound by the matrix's bytes.
 // Waves stream it from memory into the matrix unit's operands, with no LDS on the
 // way; waves of a workgroup share a block's sum where there are few blocks.
+// For rows of any alignment: those that start at words of 16 bytes come through LDS, where
+// the loads of adjacent lanes belong to one row.
 #pragma once
 
 #include "mm_tile.hpp"
