@@ -78,13 +78,29 @@ __device__ __forceinline__ Place place_of(uint32_t id, const Product& p) {
     return x;
 }
 
-// 16 bytes a lane from memory (`offset` of the lane and `more` of the wave) into LDS,
-// at byte `dst` (of the wave) + 16 lane.
+// An array from some point of it on, as the loads into LDS take it: they bring nothing from
+// `bytes` on.  The point moves along the array; the lanes' offsets from it stay.  (The
+// instruction's scalar offset is not for that: what the bounds check compares is the lanes'
+// offsets, so with it the last row's last words would be read past the array's end.)
+struct Window {
+    uint64_t at;                           // an address
+    uint64_t bytes;                        // from there to the array's end
+    __host__ __device__ uint32_t limit() const { return bytes > 0xFFFFFFFFull ? 0xFFFFFFFFu : uint32_t(bytes); }
+    __host__ __device__ void move(uint64_t step) {
+        at += step;
+        bytes -= bytes < step ? bytes : step;
+    }
+    __device__ __forceinline__ u32x4_t buffer() const {
+        return u32x4_t{uint32_t(at), uint32_t(at >> 32) & 0xFFFFu, limit(), 0x00020000u};
+    }
+};
+
+// 16 bytes a lane from `offset` of the lane into LDS, at byte `dst` (of the wave) + 16 lane.
 // (In asm, which has no register output: the compiler would make every later read
 // of LDS wait for it.)  wait_staged() and a barrier before the data are read.
-__device__ __forceinline__ void load_lds(u32x4_t buffer, uint32_t offset, uint32_t more, uint32_t dst) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
-                 :: "s"(dst), "v"(offset), "s"(buffer), "s"(more) : "memory");
+__device__ __forceinline__ void load_lds(u32x4_t buffer, uint32_t offset, uint32_t dst) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                 :: "s"(dst), "v"(offset), "s"(buffer) : "memory");
 }
 __device__ __forceinline__ void wait_staged() {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
@@ -111,8 +127,7 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) {
 template <bool kWide, int kSize>
 struct Stage {
     static constexpr uint32_t kWords = kSize / 8;        // of a k's row, where wide
-    uint64_t base;                         // of the next stage
-    uint64_t bytes;                        // from there to the array's end
+    Window next;                           // the next stage on
     uint64_t step;                         // bytes from stage to stage
     uint32_t off[4];
     uint32_t dst;
@@ -127,8 +142,8 @@ struct Stage {
         const uint32_t last = s.extent - 1 - i0;         // i0 < extent
         dst = wave * 4096;
         if constexpr (kWide) {
-            base = reinterpret_cast<uint64_t>(s.at) + 2 * (k0 * s.stride + i0);
-            bytes = 2 * ((k_end - 1 - k0) * s.stride + last + 1);
+            next.at = reinterpret_cast<uint64_t>(s.at) + 2 * (k0 * s.stride + i0);
+            next.bytes = 2 * ((k_end - 1 - k0) * s.stride + last + 1);
             step = 2 * kDepth * s.stride;
 #pragma unroll
             for (uint32_t x = 0; x < 4; ++x) {
@@ -137,8 +152,8 @@ struct Stage {
                 off[x] = k * uint32_t(2 * s.stride) + 16 * min(w, last / 8);
             }
         } else {
-            base = reinterpret_cast<uint64_t>(s.at) + 2 * (i0 * s.stride + k0);
-            bytes = 2 * (last * s.stride + (k_end + 7) / 8 * 8 - k0);   // rows end with a word
+            next.at = reinterpret_cast<uint64_t>(s.at) + 2 * (i0 * s.stride + k0);
+            next.bytes = 2 * (last * s.stride + (k_end + 7) / 8 * 8 - k0);   // rows end with a word
             step = 2 * kDepth;
 #pragma unroll
             for (uint32_t x = 0; x < 4; ++x) {
@@ -147,21 +162,19 @@ struct Stage {
                 off[x] = min(i, last) * uint32_t(2 * s.stride) + 16 * w;
             }
         }
-        base = uniform(base);
-        bytes = uniform(bytes);
+        next.at = uniform(next.at);
+        next.bytes = uniform(next.bytes);
         step = uniform(step);
     }
 
     // The next stage's bytes; load x of it, where it exists in full.
     __device__ __forceinline__ u32x4_t take() {
-        const u32x4_t buffer = {uint32_t(base), uint32_t(base >> 32) & 0xFFFFu,
-                                bytes > 0xFFFFFFFFull ? 0xFFFFFFFFu : uint32_t(bytes), 0x00020000u};
-        base += step;
-        bytes -= min(bytes, step);
+        const u32x4_t buffer = next.buffer();
+        next.move(step);
         return buffer;
     }
     __device__ __forceinline__ void load(u32x4_t buffer, uint32_t lds, uint32_t x) const {
-        load_lds(buffer, off[x], 0, lds + dst + 1024 * x);
+        load_lds(buffer, off[x], lds + dst + 1024 * x);
     }
     // Where only `have` of it exist (the other side is zero beyond them).
     __device__ __forceinline__ void load_last(u32x4_t buffer, uint32_t lds, uint32_t x, uint32_t have,
@@ -175,7 +188,7 @@ struct Stage {
             const uint32_t w = (lane & 7) ^ ((i >> 1) & 7);
             if (8 * w >= have) o -= 16 * w;
         }
-        load_lds(buffer, o, 0, lds + dst + 1024 * x);
+        load_lds(buffer, o, lds + dst + 1024 * x);
     }
 };
 

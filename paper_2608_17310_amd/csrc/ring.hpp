@@ -29,10 +29,19 @@ struct Ring {
 
     f32x4_t c[kBlocks][kCols];             // rows 4 (lane / 16) .. of a block, column lane % 16
 
-    static __device__ __forceinline__ u32x4_t buffer(const uint16_t* base, uint64_t bytes) {
-        const uint64_t b = uniform(reinterpret_cast<uint64_t>(base)), n = uniform(bytes);
-        return u32x4_t{uint32_t(b), uint32_t(b >> 32) & 0xFFFFu,
-                       n > 0xFFFFFFFFull ? 0xFFFFFFFFu : uint32_t(n), 0x00020000u};
+    // Rows row0 .. of a side of `rows`, from part `first` of the sum on.  Rows behind the last are
+    // not fetched (or, where rows overlap, are bytes that are there).
+    static __host__ __device__ Window window(const uint16_t* side, uint64_t stride, uint32_t rows,
+                                             uint32_t row0, uint32_t width, uint32_t first) {
+        Window w{reinterpret_cast<uint64_t>(side) + 2 * (row0 * stride),
+                 2 * ((rows - 1 - row0) * stride + width)};
+        w.move(uint64_t(first) * (2 * kDepth));
+        return w;
+    }
+    // Load y of a part: the lane's bytes from there.
+    static __host__ __device__ uint32_t offset(uint32_t y, uint32_t lane, uint64_t stride) {
+        const uint32_t i = 8 * y + (lane >> 3);
+        return i * uint32_t(2 * stride) + 16 * ((lane & 7) ^ ((i >> 1) & 7));
     }
 
     // Rows row0 .. of the matrix (row0 < a.w_rows), parts `first`, first + every, ...; `lds`
@@ -47,16 +56,15 @@ struct Ring {
         const uint32_t parts = (a.width + kDepth - 1) / kDepth;
         if (first >= parts) return;
         const uint32_t count = (parts - first + every - 1) / every;
-        // rows beyond the matrix and beyond x's are beyond the buffers: not fetched
-        const u32x4_t wb = buffer(a.w + row0 * a.w_stride,
-                                  2 * ((a.w_rows - 1 - row0) * a.w_stride + a.width));
-        const u32x4_t xb = buffer(a.x, 2 * ((a.rows - 1) * a.x_stride + a.width));
+        Window ww = window(a.w, a.w_stride, a.w_rows, row0, a.width, first);
+        Window xw = window(a.x, a.x_stride, a.rows, 0, a.width, first);
+        ww = Window{uniform(ww.at), uniform(ww.bytes)};
+        xw = Window{uniform(xw.at), uniform(xw.bytes)};
         uint32_t w_off[2 * kBlocks], x_off[2 * kCols];
 #pragma unroll
         for (uint32_t y = 0; y < 2 * kBlocks || y < 2 * kCols; ++y) {
-            const uint32_t i = 8 * y + (lane >> 3), word = 16 * ((lane & 7) ^ ((i >> 1) & 7));
-            if (y < 2 * kBlocks) w_off[y] = i * uint32_t(2 * a.w_stride) + word;
-            if (y < 2 * kCols) x_off[y] = i * uint32_t(2 * a.x_stride) + word;
+            if (y < 2 * kBlocks) w_off[y] = offset(y, lane, a.w_stride);
+            if (y < 2 * kCols) x_off[y] = offset(y, lane, a.x_stride);
         }
         uint32_t at[2];                    // operands of the two steps
 #pragma unroll
@@ -67,11 +75,14 @@ struct Ring {
         const uint32_t lds_at = uniform(lds_address(lds));
         uint32_t next = first, next_slot = 0;
         auto issue = [&]() {
-            const uint32_t more = next * (2 * kDepth), to = lds_at + next_slot;
+            const u32x4_t wb = ww.buffer(), xb = xw.buffer();
+            const uint32_t to = lds_at + next_slot;
 #pragma unroll
-            for (int y = 0; y < 2 * kBlocks; ++y) load_lds(wb, w_off[y], more, to + 1024 * y);
+            for (int y = 0; y < 2 * kBlocks; ++y) load_lds(wb, w_off[y], to + 1024 * y);
 #pragma unroll
-            for (int y = 0; y < 2 * kCols; ++y) load_lds(xb, x_off[y], more, to + kXAt + 1024 * y);
+            for (int y = 0; y < 2 * kCols; ++y) load_lds(xb, x_off[y], to + kXAt + 1024 * y);
+            ww.move(every * (2 * kDepth));
+            xw.move(every * (2 * kDepth));
             next += every;
             next_slot = next_slot + kPart == kBytes ? 0 : next_slot + kPart;
         };

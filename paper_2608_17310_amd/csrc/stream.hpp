@@ -46,10 +46,17 @@ struct Stream {
 
     f32x4_t c[kBlocks][kCols];             // rows 4 (lane / 16) .. of a block, column lane % 16
 
-    // `bytes` from `base` on; what lies beyond them is not fetched
-    static __device__ __forceinline__ u32x4_t buffer(uint64_t base, uint64_t bytes) {
-        return u32x4_t{uint32_t(base), uint32_t(base >> 32) & 0xFFFFu,
-                       bytes > 0xFFFFFFFFull ? 0xFFFFFFFFu : uint32_t(bytes), 0x00020000u};
+    // Rows `row` .. of a side that has those before `end`: rows from there on are not fetched
+    // (or, where rows overlap, are bytes that are there).
+    static __host__ __device__ Window window(const uint16_t* side, uint64_t stride, uint32_t row,
+                                             uint32_t end, uint32_t width) {
+        return Window{reinterpret_cast<uint64_t>(side) + 2 * (row * stride),
+                      2 * (uint64_t(end - row - 1) * stride + width)};
+    }
+    // The lane's bytes from there, of rows 8 y .. of a stage.
+    static __host__ __device__ uint32_t offset(uint32_t y, uint32_t lane, uint64_t stride) {
+        const uint32_t i = 8 * y + (lane >> 3);
+        return i * uint32_t(2 * stride) + 16 * ((lane & 7) ^ ((i >> 1) & 7));
     }
 
     // done(row0, end): c holds rows row0 + 16 kBlocks wave .. of those before `end`.
@@ -62,15 +69,10 @@ struct Stream {
         const uint32_t total = (end - begin + kTall - 1) / kTall * stages;
         uint32_t w_off[kWLoads], x_off[kXLoads];
 #pragma unroll
-        for (int y = 0; y < kWLoads; ++y) {
-            const uint32_t i = (wave * kWLoads + y) * 8 + (lane >> 3);
-            w_off[y] = i * uint32_t(2 * a.w_stride) + 16 * ((lane & 7) ^ ((i >> 1) & 7));
-        }
+        for (int y = 0; y < kWLoads; ++y) w_off[y] = offset(wave * kWLoads + y, lane, a.w_stride);
 #pragma unroll
-        for (int y = 0; y < kXLoads; ++y) {
-            const uint32_t i = ((wave * kXLoads + y) * 8 + (lane >> 3)) % kTokens;
-            x_off[y] = i * uint32_t(2 * a.x_stride) + 16 * ((lane & 7) ^ ((i >> 1) & 7));
-        }
+        for (int y = 0; y < kXLoads; ++y)
+            x_off[y] = offset((wave * kXLoads + y) % (kTokens / 8), lane, a.x_stride);
         uint32_t w_at[2], x_at[2];         // operands of the two steps of 64
 #pragma unroll
         for (uint32_t s = 0; s < 2; ++s) {
@@ -79,33 +81,35 @@ struct Stream {
             x_at[s] = kXAt + i * 128 + word;
         }
         const uint32_t lds_at = uniform(lds_address(lds));
-        // rows beyond the share and beyond x's are beyond the buffers
-        auto share = [&](uint32_t row) {
-            return buffer(uniform(reinterpret_cast<uint64_t>(a.w) + 2 * (row * a.w_stride)),
-                          uniform(2 * (uint64_t(end - row - 1) * a.w_stride + a.width)));
+        auto from = [&](const uint16_t* side, uint64_t stride, uint32_t row, uint32_t stop) {
+            const Window w = window(side, stride, row, stop, a.width);
+            return Window{uniform(w.at), uniform(w.bytes)};
         };
-        const u32x4_t xb = buffer(uniform(reinterpret_cast<uint64_t>(a.x)),
-                                  uniform(2 * (uint64_t(a.rows - 1) * a.x_stride + a.width)));
-        u32x4_t wb = share(begin);
+        const Window x_start = from(a.x, a.x_stride, 0, a.rows);
+        Window ww = from(a.w, a.w_stride, begin, end), xw = x_start;
         uint32_t next_slot = lds_at, issued = 0, next_k = 0, next_row = begin;
         auto issue = [&]() {
 #pragma unroll
             for (int u = 0; u < kSub; ++u) {
                 const uint32_t to = next_slot + u * kPart;
+                const u32x4_t wb = ww.buffer(), xb = xw.buffer();
 #pragma unroll
                 for (int y = 0; y < kWLoads; ++y)
-                    load_lds(wb, w_off[y], next_k, to + (wave * kWLoads + y) * 1024);
+                    load_lds(wb, w_off[y], to + (wave * kWLoads + y) * 1024);
 #pragma unroll
                 for (int y = 0; y < kXLoads; ++y)
-                    load_lds(xb, x_off[y], next_k, to + kXAt + (wave * kXLoads + y) % (kTokens / 8) * 1024);
-                next_k += 2 * kDepth;
+                    load_lds(xb, x_off[y], to + kXAt + (wave * kXLoads + y) % (kTokens / 8) * 1024);
+                ww.move(2 * kDepth);
+                xw.move(2 * kDepth);
             }
+            next_k += kLength;
             ++issued;
             next_slot = next_slot + kStage == lds_at + kBytes ? lds_at : next_slot + kStage;
-            if (next_k >= 2 * a.width) {   // on to the next rows
+            if (next_k >= a.width) {       // on to the next rows
                 next_k = 0;
                 next_row += kTall;
-                if (next_row < end) wb = share(next_row);
+                if (next_row < end) ww = from(a.w, a.w_stride, next_row, end);
+                xw = x_start;
             }
         };
         auto clear = [&]() {
