@@ -744,7 +744,8 @@ int es_kv_attend(es_kv_t* kv, const es_kv_attend_t* args, es_stream_t stream);
  * logits are never stored: memory beside the outputs is es_head_*_bytes.
  *
  * x is bf16 [rows][hidden], weight bf16 [vocab][hidden], both with any stride
- * between rows (at most 2^22 elements) and any alignment to 2 bytes.  For a row
+ * between rows (at most 2^22 elements; of a single row it is not looked at) and any
+ * alignment to 2 bytes.  For a row
  *   z_v = scale x . weight_v,  lse = log sum_v exp z_v,
  * and for each of its `entries` ids
  *   logp = z_id - lse.
@@ -834,7 +835,8 @@ typedef struct es_adapt {
     const void*    x;           /* bf16 [rows][inner], any alignment to 2 bytes */
     const void*    weight;      /* bf16 [outer][inner], 16-byte aligned */
     void*          out;         /* bf16 [rows][outer], any alignment to 2 bytes; not x */
-    uint64_t       x_stride, w_stride, out_stride;   /* elements, at most 2^22; w_stride a multiple of 8 */
+    uint64_t       x_stride, w_stride, out_stride;   /* elements, at most 2^22; w_stride a multiple of 8
+                                                        (of a single row not looked at) */
     const void*    a;           /* bf16 [members][rank][inner], 16-byte aligned */
     const void*    b;           /* bf16 [members][outer][rank], 16-byte aligned */
     const float*   scales;      /* [members], or NULL: ones */

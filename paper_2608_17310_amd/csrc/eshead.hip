@@ -41,6 +41,28 @@ uint64_t extent(uint64_t rows, uint64_t width, uint64_t stride) {
     return 2 * ((rows - 1) * stride + width);
 }
 
+// A call with strides that mean something: a matrix of one row, or none, takes one of whole words.
+uint64_t stride_of(uint64_t rows, uint64_t width, uint64_t stride) { return rows > 1 ? stride : up(width, 8); }
+
+es_head_score_t settled(es_head_score_t x) {
+    x.x_stride = stride_of(x.rows, x.hidden, x.x_stride);
+    x.w_stride = stride_of(x.vocab, x.hidden, x.w_stride);
+    return x;
+}
+es_head_gradient_t settled(es_head_gradient_t x) {
+    x.x_stride = stride_of(x.rows, x.hidden, x.x_stride);
+    x.w_stride = stride_of(x.vocab, x.hidden, x.w_stride);
+    x.dx_stride = stride_of(x.rows, x.hidden, x.dx_stride);
+    x.dw_stride = stride_of(x.vocab, x.hidden, x.dw_stride);
+    return x;
+}
+es_adapt_t settled(es_adapt_t x) {
+    x.x_stride = stride_of(x.rows, x.inner, x.x_stride);
+    x.w_stride = stride_of(x.outer, x.inner, x.w_stride);
+    x.out_stride = stride_of(x.rows, x.outer, x.out_stride);
+    return x;
+}
+
 int launch_error(const char* what) {
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? ES_OK : hip_fail(e, what);
@@ -349,7 +371,7 @@ extern "C" {
 
 uint64_t es_head_score_bytes(const es_head_score_t* args) {
     if (args == nullptr) return 0;
-    const es_head_score_t& x = *args;
+    const es_head_score_t x = settled(*args);
     if (check_head("es_head_score_bytes", x.x, x.weight, x.x_stride, x.w_stride, x.ids, x.teacher,
                    x.rows, x.vocab, x.hidden, x.entries, x.scale, x.reserved) != ES_OK ||
         x.rows == 0)
@@ -362,7 +384,7 @@ uint64_t es_head_score_bytes(const es_head_score_t* args) {
 int es_head_score(const es_head_score_t* args, es_stream_t stream) try {
     const char* const name = "es_head_score";
     if (args == nullptr) return fail_in(ES_ERR_INVALID_ARG, name, "null pointer");
-    const es_head_score_t& x = *args;
+    const es_head_score_t x = settled(*args);
     int rc = check_head(name, x.x, x.weight, x.x_stride, x.w_stride, x.ids, x.teacher, x.rows,
                         x.vocab, x.hidden, x.entries, x.scale, x.reserved);
     if (rc != ES_OK) return rc;
@@ -498,7 +520,7 @@ int es_head_score(const es_head_score_t* args, es_stream_t stream) try {
 
 uint64_t es_head_gradient_bytes(const es_head_gradient_t* args) {
     if (args == nullptr) return 0;
-    const es_head_gradient_t& x = *args;
+    const es_head_gradient_t x = settled(*args);
     if (check_head("es_head_gradient_bytes", x.x, x.weight, x.x_stride, x.w_stride, x.ids, x.teacher,
                    x.rows, x.vocab, x.hidden, x.entries, x.scale, x.reserved) != ES_OK ||
         x.rows == 0)
@@ -511,7 +533,7 @@ uint64_t es_head_gradient_bytes(const es_head_gradient_t* args) {
 int es_head_gradient(const es_head_gradient_t* args, es_stream_t stream) try {
     const char* const name = "es_head_gradient";
     if (args == nullptr) return fail_in(ES_ERR_INVALID_ARG, name, "null pointer");
-    const es_head_gradient_t& x = *args;
+    const es_head_gradient_t x = settled(*args);
     int rc = check_head(name, x.x, x.weight, x.x_stride, x.w_stride, x.ids, x.teacher, x.rows,
                         x.vocab, x.hidden, x.entries, x.scale, x.reserved);
     if (rc != ES_OK) return rc;
@@ -522,8 +544,7 @@ int es_head_gradient(const es_head_gradient_t* args, es_stream_t stream) try {
     if (x.rows == 0) return ES_OK;
     if (x.logp == nullptr || x.lse == nullptr || x.grad == nullptr)
         return fail_in(ES_ERR_INVALID_ARG, name, "null pointer");
-    if ((x.d_x != nullptr && x.rows > 1 && x.dx_stride < x.hidden) ||
-        (x.d_weight != nullptr && x.vocab > 1 && x.dw_stride < x.hidden))
+    if ((x.d_x != nullptr && x.dx_stride < x.hidden) || (x.d_weight != nullptr && x.dw_stride < x.hidden))
         return fail_in(ES_ERR_INVALID_ARG, name, "a gradient's rows overlap");
     if (odd(x.logp, 4) || odd(x.lse, 4) || odd(x.grad, 4) || odd(x.d_x, 2) || odd(x.d_weight, 2) ||
         odd(x.status, 4) || odd(x.workspace, 256))
@@ -692,11 +713,11 @@ int check_adapt(const char* name, const es_adapt_t& x) {
         x.b == nullptr || x.index == nullptr)
         return fail_in(ES_ERR_INVALID_ARG, name, "null pointer");
     if (x.out == x.x) return fail_in(ES_ERR_INVALID_ARG, name, "out is x");
-    if (x.rows > 1 && x.out_stride < x.outer)
+    if (x.out_stride < x.outer)
         return fail_in(ES_ERR_INVALID_ARG, name, "the output's rows overlap");
     if (odd(x.x, 2) || odd(x.out, 2) || odd(x.scales, 4) || odd(x.index, 4) || odd(x.status, 4))
         return fail_in(ES_ERR_ALIGN, name, "array not aligned to its elements");
-    if (odd(x.weight, 16) || (x.outer > 1 && x.w_stride % 8 != 0) || odd(x.a, 16) || odd(x.b, 16))
+    if (odd(x.weight, 16) || x.w_stride % 8 != 0 || odd(x.a, 16) || odd(x.b, 16))
         return fail_in(ES_ERR_ALIGN, name, "weight's rows or adapters not 16-byte aligned");
     return ES_OK;
 }
@@ -763,16 +784,18 @@ void launch_stream(const esadapt::StreamArgs& t, uint32_t groups, hipStream_t s)
 extern "C" {
 
 uint64_t es_adapt_bytes(const es_adapt_t* args) {
-    if (args == nullptr || check_adapt("es_adapt_bytes", *args) != ES_OK || args->rows == 0) return 0;
+    if (args == nullptr) return 0;
+    const es_adapt_t x = settled(*args);
+    if (check_adapt("es_adapt_bytes", x) != ES_OK || x.rows == 0) return 0;
     Room room{nullptr};
-    const AdaptPlan plan(room, *args);
+    const AdaptPlan plan(room, x);
     return room.used;
 }
 
 int es_adapt_project(const es_adapt_t* args, es_stream_t stream) try {
     const char* const name = "es_adapt_project";
     if (args == nullptr) return fail_in(ES_ERR_INVALID_ARG, name, "null pointer");
-    const es_adapt_t& x = *args;
+    const es_adapt_t x = settled(*args);
     int rc = check_adapt(name, x);
     if (rc != ES_OK) return rc;
     if (x.rows == 0) return ES_OK;

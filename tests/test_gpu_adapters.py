@@ -216,3 +216,28 @@ def test_refusals():
                  lambda: Adapters(a[:, :, :60].contiguous(), b).project(x[:, :60], w[:, :60], i)):
         with pytest.raises(esopt.EsError):
             call()
+
+
+@pytest.mark.parametrize("rows", [1, 20, 40, 70, 300])
+def test_a_matrix_of_one_row(rows):
+    """Its row stride means nothing: a column of words that are two bytes apart, seen as a row."""
+    rng = np.random.default_rng(rows)
+    x, w, a, b, scales, index = make(rng, rows, 264, 1, 16, 3)
+    column = w.view(264, 1).clone()
+    assert column.t().stride() == (1, 1)
+    adapters = Adapters(a, b, scales)
+    got = adapters.project(x, column.t(), ints(index))
+    check(x, w, a, b, scales, index, got)
+    assert torch.equal(got, adapters.project(x, w, ints(index)))
+
+
+def test_a_row_out_of_a_larger_array():
+    """One row, whose stride is beyond what several may have."""
+    rng = np.random.default_rng(6)
+    x, w, a, b, scales, index = make(rng, 1, 4104, 100, 16, 2)
+    room, out_room = torch.empty(1, 1200, 4104, device="cuda").bfloat16(), torch.empty(1, 50000, 100).bfloat16().cuda()
+    room[:, -1], out = x, out_room[:, -1]
+    assert min(room[:, -1].stride(0), out.stride(0)) > 1 << 22
+    adapters = Adapters(a, b, scales)
+    assert adapters.project(room[:, -1], w, ints(index), out=out) is out
+    assert torch.equal(out, adapters.project(x, w, ints(index)))

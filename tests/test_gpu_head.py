@@ -517,3 +517,26 @@ def test_more_rows_than_a_list_takes_at_a_time(entries):
 def test_streams_of_any_number_of_waves(vocab, rows, hidden, entries):
     rng = np.random.default_rng([vocab, rows])
     check(*make(rng, rows, vocab, hidden, entries), 1.0)
+
+
+@pytest.mark.parametrize("vocab", [300, 20000])
+@pytest.mark.parametrize("entries", [None, 4])
+def test_a_row_out_of_a_larger_array(vocab, entries):
+    """The last token of one long sequence: its row stride is beyond what several rows may have."""
+    rng = np.random.default_rng(vocab)
+    x, w, ids, teacher, grad = make(rng, 1, vocab, 2056, entries, masked=0.0)
+    ids[:, 0] = 7
+    room = torch.empty(1, 2200, 2056, device="cuda").bfloat16()
+    room[:, -1] = x
+    assert room[:, -1].stride(0) > 1 << 22
+    for a, b in zip(check(room[:, -1], w, ids, teacher, grad, 1.0), check(x, w, ids, teacher, grad, 1.0)):
+        assert torch.equal(a, b)
+
+
+def test_a_head_of_one_token():
+    rng = np.random.default_rng(41)
+    for rows in (3, 70, 200):
+        x, w, ids, _, grad = make(rng, rows, 1, 264)
+        column = w.view(264, 1).clone()
+        for a, b in zip(check(x, column.t(), ids, None, grad, 1.0), check(x, w, ids, None, grad, 1.0)):
+            assert torch.equal(a, b)

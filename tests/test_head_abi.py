@@ -155,3 +155,26 @@ def test_workspaces_that_are_too_small_are_refused(lib):
                      (lib.es_adapt_project, _adapt)):
         rc = fn(ctypes.byref(make(workspace_bytes=255)), None)
         assert rc in (E, esopt.ES_ERR_HIP) and (rc != E or "workspace" in esopt.last_error())
+
+
+def test_the_stride_of_a_single_row_is_not_looked_at(lib):
+    """A row taken out of a larger array, or a column seen as a row, has any stride: the
+    workspace is that of rows side by side, and the call gets as far as the device."""
+    any_ = (0, 1, 3, 68, (1 << 22) + 8, 1 << 60)
+    for fn, size, make, one in (
+            (lib.es_head_score, lib.es_head_score_bytes, _score, [("rows", "x_stride"), ("vocab", "w_stride")]),
+            (lib.es_head_gradient, lib.es_head_gradient_bytes, _gradient,
+             [("rows", "x_stride"), ("rows", "dx_stride"), ("vocab", "w_stride"), ("vocab", "dw_stride")]),
+            (lib.es_adapt_project, lib.es_adapt_bytes, _adapt,
+             [("rows", "x_stride"), ("rows", "out_stride"), ("outer", "w_stride")])):
+        for rows, stride in one:
+            want = size(ctypes.byref(make(**{rows: 1})))
+            assert want > 0
+            for n in any_:
+                args = make(**{rows: 1, stride: n})
+                assert size(ctypes.byref(args)) == want, (rows, stride, n)
+                # with too little workspace the call ends on the host, with a GPU and without
+                args.workspace_bytes = 1
+                assert fn(ctypes.byref(args), None) in (E, esopt.ES_ERR_HIP)
+                said = esopt.last_error()
+                assert "stride" not in said and "overlap" not in said and "aligned" not in said
