@@ -44,8 +44,8 @@ struct Side {
 };
 
 // results[n][m] = sum_k a(m, k) b(n, k).  Beyond the operands' extents the last
-// row is read again, and beyond `depth` other valid elements of a; b is zero
-// there (stored to a multiple of 64).
+// row is read again.  Beyond `depth` b is zero (stored to a multiple of 64), and so
+// is a once it is in registers: what it holds elsewhere, infinities too, stays there.
 struct Product {
     Side a, b;
     uint32_t depth;
@@ -176,7 +176,7 @@ struct Stage {
     __device__ __forceinline__ void load(u32x4_t buffer, uint32_t lds, uint32_t x) const {
         load_lds(buffer, off[x], lds + dst + 1024 * x);
     }
-    // Where only `have` of it exist (the other side is zero beyond them).
+    // Where only `have` of it exist: others are read again, and cleared in registers.
     __device__ __forceinline__ void load_last(u32x4_t buffer, uint32_t lds, uint32_t x, uint32_t have,
                                               const Side& s, uint32_t wave, uint32_t lane) const {
         uint32_t o = off[x];
@@ -418,9 +418,22 @@ __device__ __forceinline__ void product_tile(const Product& p, uint32_t m0, uint
         multiply(1);
         interleave(Count<kProducts>{}, Count<kReads>{});
     }
+    const uint32_t have = k_end - k;
+    // of a's operands of step s, what lies within the sum
+    auto keep = [&](int s) {
+        const int left = int(have) - int(32 * s + 8 * (lane >> 4));   // of the lane's eight
+        u32x4_t kept;
+#pragma unroll
+        for (int y = 0; y < 4; ++y) kept[y] = left >= 2 * y + 2 ? 0xFFFFFFFFu : left == 2 * y + 1 ? 0xFFFFu : 0u;
+#pragma unroll
+        for (int i = 0; i < kBlocks; ++i)
+            a[s][i] = __builtin_bit_cast(bf16x8_t, __builtin_bit_cast(u32x4_t, a[s][i]) & kept);
+    };
+    if (have < kDepth) keep(0);
     read(1);
     multiply(0);
     interleave(Count<kProducts>{}, Count<kReads>{});
+    if (have < kDepth) keep(1);
     multiply(1);
 }
 

@@ -241,3 +241,21 @@ def test_a_row_out_of_a_larger_array():
     adapters = Adapters(a, b, scales)
     assert adapters.project(room[:, -1], w, ints(index), out=out) is out
     assert torch.equal(out, adapters.project(x, w, ints(index)))
+
+
+@pytest.mark.parametrize("rows,inner,outer", [(3, 72, 100), (64, 72, 9000), (65, 72, 100), (70, 2104, 130),
+                                              (300, 1032, 520), (1300, 72, 6000)])
+def test_an_infinity_in_the_weight(rows, inner, outer):
+    """It reaches its own output, with the sign of the row's factor, and no other; it stands
+    where the sum's last part begins."""
+    rng = np.random.default_rng([rows, inner])
+    x, w, a, b, scales, index = make(rng, rows, inner, outer, 16, 3)
+    at = (inner - 1) // 64 * 64
+    assert (x[:, at] != 0).all()
+    adapters = Adapters(a, b, scales)
+    want = adapters.project(x, w, ints(index))
+    w[outer // 2, at] = float("inf")
+    got = adapters.project(x, w, ints(index))
+    assert torch.equal(got[:, outer // 2], torch.sign(x[:, at]) * float("inf"))
+    keep = torch.arange(outer, device="cuda") != outer // 2
+    assert torch.equal(got[:, keep], want[:, keep])

@@ -540,3 +540,31 @@ def test_a_head_of_one_token():
         column = w.view(264, 1).clone()
         for a, b in zip(check(x, column.t(), ids, None, grad, 1.0), check(x, w, ids, None, grad, 1.0)):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("rows", [5, 70, 128, 129, 300])
+@pytest.mark.parametrize("vocab,hidden", [(500, 72), (501, 200), (20001, 72), (40003, 136), (300, 1001)])
+def test_an_infinity_in_the_head(rows, vocab, hidden):
+    """A token whose logit is -infinity: the scores and the other columns of the rows' gradient
+    are those of a head that has the type's largest number there (its logit's exponential
+    is 0 as well), and in the infinity's own column a row whose target the token is has the
+    infinity that its definition gives.  The infinity stands where the sums' last parts begin."""
+    rng = np.random.default_rng([rows, vocab, hidden])
+    x, w, ids, _, grad = make(rng, rows, vocab, hidden, masked=0.0)
+    at, token = (hidden - 1) // 64 * 64, vocab - 1
+    x[:, at] = -1.0
+    ids[ids == token] = 0
+    grad[1] = 0.75
+    outs = []
+    for value, target in ((float("inf"), 3), (3.3895e38, 3), (float("inf"), token)):
+        w[token, at] = value
+        ids[1] = target
+        t = dev(ids[:, 0], torch.int64)
+        logp, lse = Head(w).score(x, t)
+        dx, _ = Head(w).score_gradient(x, t, logp, lse, dev(grad, torch.float32), weight_grad=False)
+        outs.append((logp, lse, dx))
+    (logp, lse, dx), (logp2, lse2, dx2), (logp3, lse3, dx3) = outs
+    assert torch.isfinite(lse).all() and torch.equal(lse, lse2) and torch.equal(logp, logp2)
+    keep = torch.arange(hidden, device="cuda") != at
+    assert torch.equal(dx[:, keep], dx2[:, keep])
+    assert torch.equal(lse3, lse) and logp3[1] == -float("inf") and dx3[1, at] == float("inf")
