@@ -620,6 +620,7 @@ __global__ __launch_bounds__(2 * kSize, 2) void es_head_prob_kernel(ProbArgs a) 
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const uint32_t n = n0 + c.n_of(wave, lane, j);
+        const uint32_t have = n < count ? m_have : 0;    // rows behind the last: zeros, not 0 times a logit
         const float f = a.factor[n], l = a.minus_lse[n];
 #pragma unroll
         for (int i = 0; i < c.kBlocks; ++i)
@@ -627,12 +628,12 @@ __global__ __launch_bounds__(2 * kSize, 2) void es_head_prob_kernel(ProbArgs a) 
             for (int e = 0; e < 4; ++e) {
                 const uint32_t m = c.m_of(wave, lane, i) + e;
                 const float p = f * __builtin_amdgcn_exp2f(__builtin_fmaf(c.x[i][j][e], a.scale, l));
-                c.x[i][j][e] = m < m_have ? p : 0.0f;
+                c.x[i][j][e] = m < have ? p : 0.0f;
             }
     }
     tile_to_lds(c, lds);
     __syncthreads();
-    // (rows behind the last, zeros, as far as a sum over the rows goes)
+    // (as far as a sum over the rows goes)
     const uint32_t rows = (count + kDepth - 1) / kDepth * kDepth;
     store_rows<kSize>(lds, a.d, a.d_stride, m0, kSize,
                       [&](uint32_t n) { return n0 + n < rows ? int64_t(n0 + n) : int64_t(-1); });

@@ -568,3 +568,28 @@ def test_an_infinity_in_the_head(rows, vocab, hidden):
     keep = torch.arange(hidden, device="cuda") != at
     assert torch.equal(dx[:, keep], dx2[:, keep])
     assert torch.equal(lse3, lse) and logp3[1] == -float("inf") and dx3[1, at] == float("inf")
+
+
+@pytest.mark.parametrize("rows", [1, 5, 70, 129, 300])
+@pytest.mark.parametrize("vocab,hidden", [(500, 64), (501, 200), (40003, 136)])
+@pytest.mark.parametrize("entries", [None, 4])
+def test_an_infinity_in_the_head_and_its_gradient(rows, vocab, hidden, entries):
+    """A token whose logit is -infinity has no gradient, and the others have theirs: those
+    of a head that has the type's largest number there."""
+    rng = np.random.default_rng([rows, vocab])
+    x, w, ids, teacher, grad = make(rng, rows, vocab, hidden, entries, masked=0.3)
+    x[:, 3] = -1.0
+    ids[ids == 11] = 12
+    head = Head(w)
+    d_ids, d_grad = dev(ids if entries else ids[:, 0], torch.int64), dev(grad, torch.float32)
+    got = []
+    for value in (float("inf"), 3.3895e38):
+        w[11, 3] = value
+        if entries:
+            t = dev(teacher, torch.float32)
+            _, logp, lse = head.distill(x, d_ids, t)
+            got.append(head.distill_gradient(x, d_ids, t, logp, lse, d_grad, hidden_grad=False)[1])
+        else:
+            logp, lse = head.score(x, d_ids)
+            got.append(head.score_gradient(x, d_ids, logp, lse, d_grad, hidden_grad=False)[1])
+    assert torch.isfinite(got[0]).all() and torch.equal(*got) and not got[0][11].any()
