@@ -510,17 +510,19 @@ __device__ __forceinline__ float block_max(float x, float* room) {
 }
 
 // The teacher's weight of thread e's entry (0: absent), and its logarithm.  A logit of
-// -infinity has none at any scale.
+// -infinity has none at any scale.  The likeliest entry's logit is taken off before the scale
+// (halves: the difference of two finite logits is finite), so that its own exponential is 1
+// whatever they are, masks of the type's lowest value throughout among them.
 __device__ __forceinline__ float teacher_weight(bool here, float t, float scale, float* room,
                                                 float& log_q) {
     here = here && t != -eskv::inf();
-    const float z = here ? t * scale : -eskv::inf();
-    const float top = block_max(z, room);
-    const float from = top == -eskv::inf() ? 0.0f : top;
-    const float e = here ? expf(z - from) : 0.0f;
+    const float sign = scale < 0.0f ? -1.0f : 1.0f;
+    const float top = sign * block_max(here ? sign * t : -eskv::inf(), room);
+    const float half = (0.5f * t - 0.5f * top) * scale, z = here ? half + half : -eskv::inf();
+    const float e = here ? expf(z) : 0.0f;
     const float sum = block_sum(e, room);
     const float q = sum > 0.0f ? e / sum : e;          // (NaN stays NaN)
-    log_q = q > 0.0f ? z - from - logf(sum) : 0.0f;
+    log_q = q > 0.0f ? z - logf(sum) : 0.0f;
     return sum != sum ? sum : q;
 }
 

@@ -593,3 +593,29 @@ def test_an_infinity_in_the_head_and_its_gradient(rows, vocab, hidden, entries):
             logp, lse = head.score(x, d_ids)
             got.append(head.score_gradient(x, d_ids, logp, lse, d_grad, hidden_grad=False)[1])
     assert torch.isfinite(got[0]).all() and torch.equal(*got) and not got[0][11].any()
+
+
+@pytest.mark.parametrize("scale", [1.4, 1.0, 0.5, 0.0, -1.5])
+@pytest.mark.parametrize("rows", [7, 140])
+def test_a_teachers_largest_numbers(rows, scale):
+    """Masks of the type's lowest value throughout leave equal weights, and so does its highest;
+    one above the other leaves one entry all of them, or none: the results are those of
+    small logits that do."""
+    rng = np.random.default_rng([rows, 43])
+    x, w, _, _, grad = make(rng, rows, 300, 128)
+    ids = np.stack([rng.permutation(300)[:5] for _ in range(rows)])
+    far = np.tile(np.arange(5, dtype=np.float32) / 4, (rows, 1))
+    near = far.copy()
+    low, most = np.finfo(np.float32).min, np.finfo(np.float32).max
+    far[1::4], near[1::4] = low, 0
+    far[2::4], near[2::4] = most, 0
+    far[3::4], near[3::4] = low, -np.inf if scale > 0 else 0
+    far[3::4, 2], near[3::4, 2] = most, -np.inf if scale < 0 else 0
+    head, d_ids, d_grad = Head(w), dev(ids, torch.int64), dev(grad, torch.float32)
+    got = []
+    for t in (far, near):
+        d_t = dev(t, torch.float32)
+        loss, logp, lse = head.distill(x, d_ids, d_t, scale=scale)
+        got.append((loss,) + head.distill_gradient(x, d_ids, d_t, logp, lse, d_grad, scale=scale))
+    for a, b in zip(*got):
+        assert a.isfinite().all() and torch.equal(a, b)
