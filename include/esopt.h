@@ -755,12 +755,15 @@ int es_kv_attend(es_kv_t* kv, const es_kv_attend_t* args, es_stream_t stream);
  * results and its gradient's row are NaN, and it adds nothing to the head's.
  *
  * Without a teacher there is one id a row, the target.  With one, teacher[e] is
- * its logit at ids[e] (binary32; -infinity leaves that id no weight) and
+ * its logit at ids[e] (binary32; -infinity, and infinity at a scale below 0, leave that id
+ * no weight) and
  *   q = softmax(scale teacher) over the row's present ids,
  *   loss = sum_e q_e (log q_e - logp_e),
  * the divergence of the student from the teacher within its top logits; a row
- * whose teacher leaves nothing (-infinity throughout) has loss 0 and no gradient:
- * nothing there reaches the head's.  The same id twice in a row counts twice.
+ * whose teacher leaves nothing has loss 0 and no gradient: nothing there reaches the
+ * head's.  A NaN among its present logits, or an infinity at another scale, makes a row's
+ * loss and its logits' gradients NaN.
+ * The same id twice in a row counts twice.
  *
  * Products are sums in binary32 of exact products; maxima, sums and scores are
  * binary32.  The same inputs give the same bits.

@@ -10,18 +10,23 @@ def kinds(ids, vocab):
     return (ids >= 0).any(1) & ~void, void
 
 
+def weighty(ids, teacher, scale):
+    """The entries that have a weight: -infinity leaves none at any scale, infinity none at one below 0."""
+    return (ids >= 0) & ~np.isneginf(teacher) & ~((scale < 0) & np.isposinf(teacher))
+
+
 def weights(ids, teacher, scale):
     """The wanted weights q [rows, entries] and their logarithms (0 where q is 0)."""
     here = ids >= 0
     if teacher is None:
         return here.astype(np.float64), np.zeros(ids.shape)
-    here = here & ~np.isneginf(teacher)
+    here = weighty(ids, teacher, scale)
     t = np.where(here, np.where(here, teacher, 0.0) * scale, -np.inf)
     top = t.max(1, keepdims=True)
     e = np.exp(t - np.where(np.isneginf(top), 0.0, top))
     total = e.sum(1, keepdims=True)
-    q = np.divide(e, total, out=np.zeros_like(e), where=total > 0)
-    log_q = np.log(q, out=np.zeros_like(q), where=q > 0)
+    q = np.divide(e, total, out=np.zeros_like(e), where=total != 0)      # (NaN stays NaN)
+    log_q = np.log(q, out=np.zeros_like(q), where=q != 0)
     return q, log_q
 
 
@@ -41,7 +46,7 @@ def score(x, w, ids, scale=1.0, teacher=None):
         here = ids[r] >= 0
         logp[r, here] = z[ids[r, here]] - lse[r]
         if teacher is not None:
-            some = q[r] > 0
+            some = q[r] != 0
             loss[r] = (q[r, some] * (log_q[r, some] - logp[r, some])).sum()
     for out in (loss, logp, lse):
         out[void] = np.nan
@@ -67,7 +72,7 @@ def gradients(x, w, ids, grad, scale=1.0, teacher=None):
     """(d_x, d_w); rows that are void have NaN and add nothing."""
     live, void = kinds(ids, len(w))
     if teacher is not None:
-        live &= ((ids >= 0) & ~np.isneginf(teacher)).any(1)
+        live &= weighty(ids, teacher, scale).any(1)
     x = np.where(live[:, None], x, 0.0)
     d = logit_gradients(x, w, ids, grad, scale, teacher)
     dx = d @ w

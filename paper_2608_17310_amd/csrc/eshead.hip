@@ -581,6 +581,7 @@ int es_head_gradient(const es_head_gradient_t* args, es_stream_t stream) try {
     rows.dx = static_cast<uint16_t*>(x.d_x);
     rows.dx_stride = x.dx_stride;
     rows.weighed = x.teacher != nullptr;
+    rows.scale = x.scale;
     rows.status = x.status;
     rows.rows = x.rows;
     rows.vocab = x.vocab;

@@ -20,8 +20,8 @@ using namespace esmm;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr uint32_t kMaxEntries = 256;
 
-// What becomes of a row, by its ids.
-enum Row : uint8_t { kDead = 0, kLive = 1, kVoid = 2 };
+// What becomes of a row, by its ids, and (added to it) that its teacher's weights are NaN.
+enum Row : uint8_t { kDead = 0, kLive = 1, kVoid = 2, kKind = 3, kLost = 4 };
 
 // ------------------------------------------------------------------- rows --
 
@@ -35,32 +35,51 @@ struct RowArgs {
     uint32_t* status;
     uint32_t rows, vocab, entries, hidden;
     bool weighed;                          // a row whose teacher leaves nothing is dead
+    float scale;                           //   at this one
 };
+
+// Whether a teacher's logit leaves its entry a weight: what is -infinity at a scale of that
+// sign, and -infinity itself, leaves none.  Without a number for it (NaN, or an infinity that
+// takes all of the weight) a row's weights are NaN.
+__device__ __forceinline__ bool has_weight(float t, float scale) {
+    return t != -eskv::inf() && (t != eskv::inf() || !(scale < 0.0f));
+}
+__device__ __forceinline__ bool is_number(float t, float scale) {
+    return __builtin_fabsf(t) < eskv::inf() || !has_weight(t, scale);
+}
 
 // What becomes of a row of several ids: one wave a row.
 __global__ __launch_bounds__(256) void es_head_rows_kernel(RowArgs a) {
     const uint32_t lane = threadIdx.x & 63, r = blockIdx.x * 4 + (threadIdx.x >> 6);
     if (r >= a.rows) return;
-    bool some = false, bad = false, weight = !a.weighed;
+    bool some = false, bad = false, weight = !a.weighed, lost = false;
     for (uint32_t e = lane; e < a.entries; e += 64) {
         const int64_t id = a.ids[uint64_t(r) * a.entries + e];
         some |= id >= 0;
         bad |= id >= int64_t(a.vocab);
-        if (id >= 0 && a.weighed)
-            weight |= a.teacher[uint64_t(r) * a.entries + e] != -eskv::inf();
+        if (id >= 0 && a.weighed) {
+            const float t = a.teacher[uint64_t(r) * a.entries + e];
+            weight |= has_weight(t, a.scale);
+            lost |= !is_number(t, a.scale);
+        }
     }
     some = __any(some);
     bad = __any(bad);
     weight = __any(weight);
-    if (lane == 0) a.flags[r] = bad ? kVoid : some && weight ? kLive : kDead;
+    lost = __any(lost);
+    if (lane == 0) a.flags[r] = (bad ? kVoid : some && weight ? kLive : kDead) | (lost ? kLost : 0);
 }
 
 // The same, where a row has one id; of several, what es_head_rows_kernel found.
 __device__ __forceinline__ uint8_t kind_of(const RowArgs& a, uint32_t r) {
-    if (a.entries > 1) return a.flags[r];
+    if (a.entries > 1) return a.flags[r] & kKind;
     const int64_t id = a.ids[r];
     if (id >= int64_t(a.vocab)) return kVoid;
-    return id < 0 || (a.weighed && a.teacher[r] == -eskv::inf()) ? kDead : kLive;
+    return id < 0 || (a.weighed && !has_weight(a.teacher[r], a.scale)) ? kDead : kLive;
+}
+__device__ __forceinline__ bool is_lost(const RowArgs& a, uint32_t r) {
+    if (a.entries > 1) return a.flags[r] & kLost;
+    return a.weighed && !is_number(a.teacher[r], a.scale);
 }
 
 // Its results, where it has none of its own.  A wave's lanes.
@@ -151,7 +170,8 @@ __device__ __forceinline__ void pack_row(const PackArgs& a, uint32_t i, uint32_t
         store<u32x4_t>(to + k, v);
     }
     if (a.factor != nullptr && lane == 0) {
-        a.factor[i] = live ? a.scale * a.grad[row] : 0.0f;
+        // (times the sum of the wanted weights, which is 1 if it is a number)
+        a.factor[i] = !live ? 0.0f : is_lost(a.out, row) ? eskv::nan() : a.scale * a.grad[row];
         a.minus_lse[i] = live ? -a.lse[row] * kLog2e : 0.0f;
     }
 }
@@ -509,13 +529,12 @@ __device__ __forceinline__ float block_max(float x, float* room) {
     return fmaxf(fmaxf(room[0], room[1]), fmaxf(room[2], room[3]));
 }
 
-// The teacher's weight of thread e's entry (0: absent), and its logarithm.  A logit of
-// -infinity has none at any scale.  The likeliest entry's logit is taken off before the scale
+// The teacher's weight of thread e's entry (0: absent), and its logarithm.  The likeliest entry's logit is taken off before the scale
 // (halves: the difference of two finite logits is finite), so that its own exponential is 1
 // whatever they are, masks of the type's lowest value throughout among them.
 __device__ __forceinline__ float teacher_weight(bool here, float t, float scale, float* room,
                                                 float& log_q) {
-    here = here && t != -eskv::inf();
+    here = here && has_weight(t, scale);
     const float sign = scale < 0.0f ? -1.0f : 1.0f;
     const float top = sign * block_max(here ? sign * t : -eskv::inf(), room);
     const float half = (0.5f * t - 0.5f * top) * scale, z = here ? half + half : -eskv::inf();

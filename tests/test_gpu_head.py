@@ -619,3 +619,40 @@ def test_a_teachers_largest_numbers(rows, scale):
         got.append((loss,) + head.distill_gradient(x, d_ids, d_t, logp, lse, d_grad, scale=scale))
     for a, b in zip(*got):
         assert a.isfinite().all() and torch.equal(a, b)
+
+
+@pytest.mark.parametrize("scale", [0.7, 0.0, -0.7])
+@pytest.mark.parametrize("rows,entries", [(7, 1), (7, 5), (140, 70), (600, 1), (600, 3)])
+def test_a_teacher_that_is_no_number(rows, entries, scale):
+    """Such a row's loss and its logits' gradients are NaN, the rows' gradients beside it are
+    those without it, and the head's is NaN throughout, as its definition gives."""
+    rng = np.random.default_rng([rows, entries])
+    x, w, _, _, grad = make(rng, rows, 300, 64)
+    ids = rng.integers(0, 300, (rows, entries))
+    clean = rng.standard_normal(ids.shape).astype(np.float32)
+    head, d_grad = Head(w), dev(grad, torch.float32)
+
+    def run(i, t):
+        d_ids, d_t = dev(i, torch.int64), dev(t, torch.float32)
+        loss, logp, lse = head.distill(x, d_ids, d_t, scale=scale)
+        return (loss, logp, lse) + head.distill_gradient(x, d_ids, d_t, logp, lse, d_grad, scale=scale)
+    want = run(ids, clean)
+    for value in (np.nan, np.inf):
+        t = clean.copy()
+        t[1, 0] = value
+        loss, logp, lse, dx, dw = run(ids, t)
+        # an infinity at a scale below 0 has no weight
+        lost = np.isnan(value) or scale >= 0
+        with np.errstate(invalid="ignore"):
+            W, X = f64(w), f64(x)
+            assert np.isnan(oh.gradients(X, W, ids, grad, scale, t.astype(np.float64))[1]).all() == lost
+        assert torch.isnan(loss[1]) == lost and torch.isnan(dx[1]).all() == lost
+        assert torch.isnan(dw).all() == lost and torch.isnan(dw).any() == lost
+        others = torch.arange(rows, device="cuda") != 1
+        assert torch.equal(loss[others], want[0][others]) and torch.equal(dx[others], want[3][others])
+        assert torch.equal(logp, want[1]) and torch.equal(lse, want[2])
+        if entries > 1:                                    # absent, it is not looked at
+            gone = ids.copy()
+            gone[1, 0] = -1
+            for a in run(gone, t):
+                assert torch.isfinite(a).all()

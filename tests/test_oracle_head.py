@@ -118,3 +118,16 @@ def test_a_teacher_that_leaves_nothing(scale):
     dx, dw = oh.gradients(x, w, ids, grad, scale, t)
     wx, ww = oh.gradients(x, w, gone, grad, scale, t)
     assert np.array_equal(dx, wx) and np.array_equal(dw, ww) and not dx[2].any()
+
+
+def test_a_teacher_that_is_no_number():
+    x, w, ids, t, grad = make(10, entries=3)
+    t[1, 2], t[4, 0] = np.nan, np.inf
+    ids[5, 1], t[5, 1] = -1, np.nan                        # absent: not looked at
+    with np.errstate(invalid="ignore"):
+        for scale, lost in ((0.7, [1, 4]), (-0.7, [1])):
+            loss, logp, lse = oh.score(x, w, ids, scale, t)
+            assert np.flatnonzero(np.isnan(loss)).tolist() == lost and np.isfinite(logp).all()
+            dx, dw = oh.gradients(x, w, ids, grad, scale, t)
+            assert np.flatnonzero(np.isnan(dx).any(1)).tolist() == lost
+            assert np.isnan(dx[lost]).all() and np.isnan(dw).all()
