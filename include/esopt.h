@@ -749,6 +749,7 @@ int es_kv_attend(es_kv_t* kv, const es_kv_attend_t* args, es_stream_t stream);
  *   z_v = scale x . weight_v,  lse = log sum_v exp z_v,
  * and for each of its `entries` ids
  *   logp = z_id - lse.
+ * A logit of -infinity has no probability; one of infinity, or NaN, makes its row's results NaN.
  * A negative id is absent (its logp is 0, whatever stands beside it).  A row
  * with no id is dead: its results are 0, it has no gradient, and what x holds
  * there reaches nothing.  A row with an id of `vocab` or more is void: its

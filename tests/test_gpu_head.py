@@ -656,3 +656,20 @@ def test_a_teacher_that_is_no_number(rows, entries, scale):
             gone[1, 0] = -1
             for a in run(gone, t):
                 assert torch.isfinite(a).all()
+
+
+@pytest.mark.parametrize("rows", [1, 33, 70, 129, 300])
+@pytest.mark.parametrize("vocab,hidden", [(500, 72), (501, 64), (20001, 72), (40003, 136), (300, 63)])
+def test_a_logit_of_infinity(rows, vocab, hidden):
+    """Its row's results are NaN, as the differences of infinities that define them are; rows where
+    that logit is -infinity are finite."""
+    rng = np.random.default_rng([rows, vocab])
+    x, w, ids, _, _ = make(rng, rows, vocab, hidden, masked=0.0)
+    ids[ids == 7] = 8
+    w[7, 5] = float("inf")
+    x[:, 5] = torch.where(torch.arange(rows, device="cuda") % 3 == 1, -1.0, 1.0)
+    up = x[:, 5] > 0
+    logp, lse = Head(w).score(x, dev(ids[:, 0], torch.int64))
+    loss, *_ = Head(w).distill(x, dev(ids, torch.int64), torch.zeros(rows, 1, device="cuda"))
+    for out in (logp, lse, loss):
+        assert torch.equal(torch.isnan(out), up) and torch.isfinite(out[~up]).all()
