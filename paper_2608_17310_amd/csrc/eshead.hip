@@ -437,7 +437,7 @@ int es_head_score(const es_head_score_t* args, es_stream_t stream) try {
         eshead::StreamStatsArgs t{};
         t.s = stream_args(x.weight, x.w_stride, x.vocab, x.x, x.x_stride, x.rows, x.hidden, plan.share);
         t.parts = plan.parts;
-        t.factor = x.scale * eshead::kLog2e;
+        t.scale = x.scale;
         switch (plan.waves) {
             case 3: launch_stream<3>(t, plan.tiles, s); break;
             case 4: launch_stream<4>(t, plan.tiles, s); break;
@@ -453,7 +453,7 @@ int es_head_score(const es_head_score_t* args, es_stream_t stream) try {
         eshead::FewStatsArgs f{};
         f.f = few_args(x.weight, x.w_stride, x.vocab, x.x, x.x_stride, x.rows, x.hidden);
         f.parts = plan.parts;
-        f.factor = x.scale * eshead::kLog2e;
+        f.scale = x.scale;
         const auto kernel = x.rows <= 16   ? eshead::es_head_ring_kernel<1, 3>
                             : x.rows <= 32 ? eshead::es_head_ring_kernel<2, 2>
                                            : eshead::es_head_ring_kernel<4, 1>;
@@ -469,7 +469,7 @@ int es_head_score(const es_head_score_t* args, es_stream_t stream) try {
         f.f = few_args(x.weight, x.w_stride, x.vocab, x.x, x.x_stride, x.rows, x.hidden);
         f.f.slices = plan.division.slices;
         f.parts = plan.parts;
-        f.factor = x.scale * eshead::kLog2e;
+        f.scale = x.scale;
         constexpr int b = 2;
         const auto kernel = plan.division.cols == 1   ? eshead::es_head_few_kernel<b, 1>
                             : plan.division.cols == 2 ? eshead::es_head_few_kernel<b, 2>
@@ -500,7 +500,7 @@ int es_head_score(const es_head_score_t* args, es_stream_t stream) try {
         t.parts = plan.parts;
         t.parts_stride = plan.tiles;
         t.part0 = v0 / plan.size;
-        t.factor = x.scale * eshead::kLog2e;
+        t.scale = x.scale;
         if (plan.size == kTile)
             launch_tiles<kTile>(eshead::es_head_stats_kernel<kTile>, t, s);
         else
@@ -606,7 +606,7 @@ int es_head_gradient(const es_head_gradient_t* args, es_stream_t stream) try {
         a.minus_lse = plan.minus_lse;
         a.d = plan.d;
         a.d_stride = plan.head.piece;
-        a.scale = x.scale * eshead::kLog2e;
+        a.scale = x.scale;
         if (size == kTile)
             launch_tiles<kTile>(eshead::es_head_prob_kernel<kTile>, a, s);
         else

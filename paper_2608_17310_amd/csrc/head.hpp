@@ -17,7 +17,7 @@ namespace eshead {
 
 using namespace esmm;
 
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kLog2e = 1.4426950408889634f;
 constexpr uint32_t kMaxEntries = 256;
 
 // What becomes of a row, by its ids, and (added to it) that its teacher's weights are NaN.
@@ -172,7 +172,7 @@ __device__ __forceinline__ void pack_row(const PackArgs& a, uint32_t i, uint32_t
     if (a.factor != nullptr && lane == 0) {
         // (times the sum of the wanted weights, which is 1 if it is a number)
         a.factor[i] = !live ? 0.0f : is_lost(a.out, row) ? eskv::nan() : a.scale * a.grad[row];
-        a.minus_lse[i] = live ? -a.lse[row] * kLog2e : 0.0f;
+        a.minus_lse[i] = live ? -a.lse[row] : 0.0f;
     }
 }
 
@@ -228,10 +228,14 @@ struct StatsArgs {
     float* parts;                          // [rows][parts_stride] pairs: maximum, sum
     uint64_t parts_stride;
     uint32_t part0;                        // of this launch's first tile
-    float factor;                          // scale log2(e)
+    float scale;
 };
 
-// A tile's rows of logits as maxima and sums, in units of log 2.
+// e^x of differences of logits.  The logits themselves stay in their own units: a maximum of some
+// thousands times log2(e) would be off by a step of its own, a difference of them is not.
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+
+// A tile's rows of logits as maxima and sums.
 template <int kSize>
 __global__ __launch_bounds__(2 * kSize, 2) void es_head_stats_kernel(StatsArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
@@ -253,7 +257,7 @@ __global__ __launch_bounds__(2 * kSize, 2) void es_head_stats_kernel(StatsArgs a
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const uint32_t m = c.m_of(wave, lane, i) + e;
-                const float z = m < m_have ? c.x[i][j][e] * a.factor : -eskv::inf();
+                const float z = m < m_have ? c.x[i][j][e] * a.scale : -eskv::inf();
                 c.x[i][j][e] = z;
                 top = fmaxf(top, z);
             }
@@ -264,7 +268,7 @@ __global__ __launch_bounds__(2 * kSize, 2) void es_head_stats_kernel(StatsArgs a
 #pragma unroll
         for (int i = 0; i < c.kBlocks; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f(c.x[i][j][e] - from);
+            for (int e = 0; e < 4; ++e) sum += exp_of(c.x[i][j][e] - from);
         sum += __shfl_xor(sum, 16);
         sum += __shfl_xor(sum, 32);
         if (lane < 16) {
@@ -278,8 +282,8 @@ __global__ __launch_bounds__(2 * kSize, 2) void es_head_stats_kernel(StatsArgs a
     if (n < kSize && n0 + n < count) {
         const float t0 = pair[2 * n], t1 = pair[2 * (kSize + n)];
         const float top = fmaxf(t0, t1), from = top == -eskv::inf() ? 0.0f : top;
-        const float sum = pair[2 * n + 1] * __builtin_amdgcn_exp2f(t0 - from) +
-                          pair[2 * (kSize + n) + 1] * __builtin_amdgcn_exp2f(t1 - from);
+        const float sum = pair[2 * n + 1] * exp_of(t0 - from) +
+                          pair[2 * (kSize + n) + 1] * exp_of(t1 - from);
         float* const to = a.parts + 2 * ((n0 + n) * a.parts_stride + a.part0 + at.m);
         to[0] = top;
         to[1] = sum;
@@ -289,7 +293,7 @@ __global__ __launch_bounds__(2 * kSize, 2) void es_head_stats_kernel(StatsArgs a
 struct FewStatsArgs {
     esfew::FewArgs f;
     float* parts;                          // [rows][workgroups] pairs
-    float factor;
+    float scale;
 };
 
 // The same of up to 64 rows, as they are: a workgroup's blocks are a part.
@@ -331,7 +335,7 @@ __global__ __launch_bounds__(512, kCols == 1 ? 4 : 2) void es_head_few_kernel(Fe
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const bool here = at.row0 + 16 * b + 4 * (lane >> 4) + e < a.f.w_rows && at.slice == 0;
-                z[b][e] = here ? t.c[b][j][e] * a.factor : -eskv::inf();
+                z[b][e] = here ? t.c[b][j][e] * a.scale : -eskv::inf();
                 top = fmaxf(top, z[b][e]);
             }
         top = fmaxf(top, __shfl_xor(top, 16));
@@ -341,7 +345,7 @@ __global__ __launch_bounds__(512, kCols == 1 ? 4 : 2) void es_head_few_kernel(Fe
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f(z[b][e] - from);
+            for (int e = 0; e < 4; ++e) sum += exp_of(z[b][e] - from);
         sum += __shfl_xor(sum, 16);
         sum += __shfl_xor(sum, 32);
         if (lane < 16) {
@@ -357,7 +361,7 @@ __global__ __launch_bounds__(512, kCols == 1 ? 4 : 2) void es_head_few_kernel(Fe
         const float from = top == -eskv::inf() ? 0.0f : top;
         float sum = 0.0f;
         for (uint32_t w = 0; w < kWaves; ++w)
-            sum += pair[w][n][1] * __builtin_amdgcn_exp2f(pair[w][n][0] - from);
+            sum += pair[w][n][1] * exp_of(pair[w][n][0] - from);
         float* const to = a.parts + 2 * (uint64_t(n) * gridDim.x + blockIdx.x);
         to[0] = top;
         to[1] = sum;
@@ -393,11 +397,11 @@ __global__ __launch_bounds__(512, 2) void es_head_ring_kernel(FewStatsArgs a) {
         float z = 0.0f;
 #pragma unroll
         for (uint32_t w = 0; w < kWaves; ++w) z += sums[w * kEach + n * 32 + i];
-        z = row0 + i < a.f.w_rows ? z * a.factor : -eskv::inf();
+        z = row0 + i < a.f.w_rows ? z * a.scale : -eskv::inf();
         float top = z;
 #pragma unroll
         for (int d = 16; d >= 1; d /= 2) top = fmaxf(top, __shfl_xor(top, d));
-        float sum = __builtin_amdgcn_exp2f(z - (top == -eskv::inf() ? 0.0f : top));
+        float sum = exp_of(z - (top == -eskv::inf() ? 0.0f : top));
 #pragma unroll
         for (int d = 16; d >= 1; d /= 2) sum += __shfl_xor(sum, d);
         if (i == 0) {
@@ -411,7 +415,7 @@ __global__ __launch_bounds__(512, 2) void es_head_ring_kernel(FewStatsArgs a) {
 struct StreamStatsArgs {
     esstream::StreamArgs s;
     float* parts;                          // [rows][workgroups] pairs
-    float factor;
+    float scale;
 };
 
 // The same of up to 128 rows of words: a workgroup's share of the vocabulary is a part,
@@ -444,15 +448,15 @@ __global__ __launch_bounds__(64 * kWaves, 1) void es_head_stream_kernel(StreamSt
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const bool here = row0 + 32 * wave + 16 * b + 4 * (lane >> 4) + e < end;
-                    z[b][e] = here ? t.c[b][j][e] * a.factor : -eskv::inf();
+                    z[b][e] = here ? t.c[b][j][e] * a.scale : -eskv::inf();
                     most = fmaxf(most, z[b][e]);
                 }
             const float from = most == -eskv::inf() ? 0.0f : most;
-            sum[j] *= __builtin_amdgcn_exp2f(top[j] - from);
+            sum[j] *= exp_of(top[j] - from);
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) sum[j] += __builtin_amdgcn_exp2f(z[b][e] - from);
+                for (int e = 0; e < 4; ++e) sum[j] += exp_of(z[b][e] - from);
             top[j] = most;
         }
     });
@@ -463,7 +467,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void es_head_stream_kernel(StreamSt
         float most = fmaxf(top[j], __shfl_xor(top[j], 16));
         most = fmaxf(most, __shfl_xor(most, 32));
         const float from = most == -eskv::inf() ? 0.0f : most;
-        float all = sum[j] * __builtin_amdgcn_exp2f(top[j] - from);
+        float all = sum[j] * exp_of(top[j] - from);
         all += __shfl_xor(all, 16);
         all += __shfl_xor(all, 32);
         if (lane < 16) {
@@ -480,7 +484,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void es_head_stream_kernel(StreamSt
         float all = 0.0f;
         for (uint32_t w = 0; w < kWaves; ++w)
             all += pair[2 * (kTokens * w + n) + 1] *
-                   __builtin_amdgcn_exp2f(pair[2 * (kTokens * w + n)] - from);
+                   exp_of(pair[2 * (kTokens * w + n)] - from);
         float* const to = a.parts + 2 * (uint64_t(n) * gridDim.x + blockIdx.x);
         to[0] = most;
         to[1] = all;
@@ -574,9 +578,9 @@ __global__ __launch_bounds__(256) void es_head_score_kernel(ScoreArgs a) {
     const float from = top == -eskv::inf() ? 0.0f : top;
     float sum = 0.0f;
     for (uint32_t m = threadIdx.x; m < a.n_parts; m += 256)
-        sum += parts[2 * m + 1] * __builtin_amdgcn_exp2f(parts[2 * m] - from);
+        sum += parts[2 * m + 1] * exp_of(parts[2 * m] - from);
     sum = block_sum(sum, room);
-    const float lse = (from + log2f(sum)) * kLn2;
+    const float lse = from + logf(sum);
 
     const uint16_t* const x = a.x + i * a.x_stride;
     const uint32_t whole = a.hidden / 8 * 8;
@@ -621,7 +625,7 @@ struct ProbArgs {
     const float *factor, *minus_lse;       // of a packed row
     uint16_t* d;                           // [rows][d_stride]
     uint64_t d_stride;
-    float scale;                           // scale log2(e)
+    float scale;
 };
 
 // The logits' gradients without what their ids add: factor softmax(z), as bf16 (RNE):
@@ -648,7 +652,7 @@ __global__ __launch_bounds__(2 * kSize, 2) void es_head_prob_kernel(ProbArgs a) 
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const uint32_t m = c.m_of(wave, lane, i) + e;
-                const float p = f * __builtin_amdgcn_exp2f(__builtin_fmaf(c.x[i][j][e], a.scale, l));
+                const float p = f * exp_of(__builtin_fmaf(c.x[i][j][e], a.scale, l));
                 c.x[i][j][e] = m < have ? p : 0.0f;
             }
     }

@@ -673,3 +673,22 @@ def test_a_logit_of_infinity(rows, vocab, hidden):
     loss, *_ = Head(w).distill(x, dev(ids, torch.int64), torch.zeros(rows, 1, device="cuda"))
     for out in (logp, lse, loss):
         assert torch.equal(torch.isnan(out), up) and torch.isfinite(out[~up]).all()
+
+
+@pytest.mark.parametrize("scale", [1.0, 0.5])
+@pytest.mark.parametrize("rows,vocab,hidden", [(1, 20001, 8), (40, 20001, 8), (100, 20001, 8), (3, 500, 8),
+                                               (70, 500, 8), (33, 500, 7), (200, 500, 8), (300, 40003, 8)])
+def test_normalisers_of_large_logits(rows, vocab, hidden, scale):
+    """Integers, whose logits of some thousands are exact: a normaliser is off by its own rounding
+    and by its sum's errors alone (as in `slack`)."""
+    rng = np.random.default_rng([rows, vocab])
+    x, w = (torch.from_numpy(rng.integers(-90, 91, (n, hidden)).astype(np.float32)).cuda().bfloat16()
+            for n in (rows, vocab))
+    t = torch.from_numpy(rng.integers(0, vocab, rows)).cuda()
+    logp, lse = Head(w).score(x, t, scale=scale)
+    z = x.double() @ w.double().t() * scale
+    want = torch.logsumexp(z, -1)
+    assert want.amax() > 3000
+    assert ((lse - want).abs() <= E * want.abs() + 2 * E * 64 + 100 * E).all()
+    got = z.gather(1, t[:, None])[:, 0] - want
+    assert ((logp - got).abs() <= E * (want.abs() + got.abs()) + 2 * E * 64 + 100 * E).all()
