@@ -606,7 +606,9 @@ __global__ __launch_bounds__(256) void es_head_score_kernel(ScoreArgs a) {
     const uint32_t e = threadIdx.x;
     const uint64_t at = uint64_t(row) * a.entries + e;
     const bool here = e < a.entries && a.ids[at] >= 0;
-    const float logp = here ? logits[e] - lse : 0.0f;
+    // (a token with nearly all of the weight: its logit's sum and its normaliser's have their own
+    // orders, and a probability is at most 1)
+    const float diff = here ? logits[e] - lse : 0.0f, logp = diff > 0.0f ? 0.0f : diff;
     if (e < a.entries) a.logp[at] = logp;
     if (e == 0) a.lse[row] = lse;
     if (a.teacher != nullptr) {

@@ -692,3 +692,19 @@ def test_normalisers_of_large_logits(rows, vocab, hidden, scale):
     assert ((lse - want).abs() <= E * want.abs() + 2 * E * 64 + 100 * E).all()
     got = z.gather(1, t[:, None])[:, 0] - want
     assert ((logp - got).abs() <= E * (want.abs() + got.abs()) + 2 * E * 64 + 100 * E).all()
+
+
+@pytest.mark.parametrize("rows,vocab,hidden", [(3, 500, 200), (40, 500, 1001), (100, 20001, 64), (64, 20001, 2056),
+                                               (300, 700, 2056)])
+def test_no_probability_is_above_one(rows, vocab, hidden):
+    """Targets with all of the weight, at logits of some thousands, whose sums round."""
+    rng = np.random.default_rng([rows, hidden])
+    x, w, _, _, _ = make(rng, rows, vocab, hidden, masked=0.0, std=1000.0)
+    z = x.double() @ w.double().t()
+    t = z.argmax(1)
+    logp, lse = Head(w).score(x, t)
+    sure = torch.logsumexp(z, -1) - z.amax(1) == 0
+    assert sure.sum() > rows // 2
+    assert (logp <= 0).all() and not torch.isnan(logp).any()
+    loss, logp, _ = Head(w).distill(x, t[:, None], torch.zeros(rows, 1, device="cuda"))
+    assert (logp <= 0).all() and (loss >= 0).all()
