@@ -267,8 +267,9 @@ class Decoder:
         logits = torch.empty(len(rows), count, dtype=torch.float32, device=rows.device)
         slab = max(1, LOGITS_AT_A_TIME // len(self.head))
         for i in range(0, len(rows), slab):
-            logits[i:i + slab], ids[i:i + slab] = F.linear(
-                x[rows[i:i + slab]], self.head).float().topk(count, -1)
+            # not rounded to bf16 on the way: `divergence` has the student's in 32 bits too
+            logits[i:i + slab], ids[i:i + slab] = torch.mm(
+                x[rows[i:i + slab]], self.head.t(), out_dtype=torch.float32).topk(count, -1)
         return ids, logits
 
     def divergence(self, prompts, targets, ids, logits, scale=1.0):

@@ -265,3 +265,21 @@ def test_a_generation_scored_without_logits():
                          lambda i: model.score(prompts, targets).mean().item())
     assert len(set(rec.rewards)) > 2
     plan.close()
+
+
+@pytest.mark.parametrize("slab", [1 << 28, 97 * 10])
+def test_a_teachers_logits_are_not_rounded(monkeypatch, slab):
+    """They are binary32 sums of exact products of the hidden states and the head (off by at most a
+    step of 2^-23 of the sum of the products' sizes each), and the largest of them."""
+    from paper_2608_17310_amd import rollout
+    monkeypatch.setattr(rollout, "LOGITS_AT_A_TIME", slab)
+    rng = np.random.default_rng(18)
+    model = Decoder(make_params(19), HQ, H, D, False, seqs=2, length=64, format="bf16")
+    prompts, targets = make_prompts(rng, [9, 30]), make_prompts(rng, [20, 7])
+    ids, logits = model.top_logits(prompts, targets, 12)
+    x, rows, *_ = model._answers(prompts, targets)
+    X, W = x[rows].double(), model.head.double()
+    z = X @ W.t()
+    tol = (HIDDEN + 2) * 2.0 ** -23 * (X.abs() @ W.abs().t()).amax()
+    assert logits.dtype == torch.float32 and ((z.gather(1, ids) - logits).abs() <= tol).all()
+    assert ((z.topk(12, -1).values - logits).abs() <= tol).all()
