@@ -259,3 +259,13 @@ def test_an_infinity_in_the_weight(rows, inner, outer):
     assert torch.equal(got[:, outer // 2], torch.sign(x[:, at]) * float("inf"))
     keep = torch.arange(outer, device="cuda") != outer // 2
     assert torch.equal(got[:, keep], want[:, keep])
+
+
+@pytest.mark.parametrize("rows,inner,outer", [(1300, 1096, 6000), (1300, 128, 6000), (1290, 136, 6000),
+                                              (1300, 192, 6001), (1400, 200, 5900), (1300, 256, 6000),
+                                              (1300, 264, 6000), (1300, 320, 6000), (1300, 328, 6100)])
+def test_every_number_of_stages_in_large_tiles(rows, inner, outer):
+    assert -(-outer // 128) * -(-rows // 128) > 512        # (so many small tiles are large ones)
+    rng = np.random.default_rng([rows, inner, outer])
+    x, w, a, b, scales, index = make(rng, rows, inner, outer, 24, 7, "runs")
+    check(x, w, a, b, scales, index, Adapters(a, b, scales).project(x, w, ints(index)))

@@ -708,3 +708,54 @@ def test_no_probability_is_above_one(rows, vocab, hidden):
     assert (logp <= 0).all() and not torch.isnan(logp).any()
     loss, logp, _ = Head(w).distill(x, t[:, None], torch.zeros(rows, 1, device="cuda"))
     assert (logp <= 0).all() and (loss >= 0).all()
+
+
+def check_on_the_card(x, w, ids, grad):
+    """Scores and gradients without a teacher against the formula in 64 bits on the card, with the
+    bounds of test_vocabularies_of_several_pieces."""
+    rows, vocab, hidden = len(x), len(w), x.shape[1]
+    assert -(-vocab // 128) * -(-rows // 128) > 512        # (so many small tiles are large ones)
+    head, t, g = Head(w), dev(ids[:, 0], torch.int64), dev(grad, torch.float32)
+    logp, lse = head.score(x, t)
+    dx, dw = head.score_gradient(x, t, logp, lse, g)
+    live, X, W = t >= 0, x.double(), w.double()
+    here = torch.arange(rows, device="cuda")
+    z = X @ W.t()
+    want = torch.logsumexp(z, -1)
+    s = X.abs().amax() * W.abs().sum(1).amax()
+    z_err = (2 * E * hidden + 4 * E) * s
+    norm = 200 * E + 8 * E * s
+    assert ((lse - want).abs()[live] <= z_err + norm + 4 * E * want.abs()[live]).all()
+    right = z[here, t.clamp(min=0)] - want
+    assert ((logp - right).abs()[live] <= 2 * z_err + norm + 8 * E * (want.abs() + right.abs())[live]).all()
+    assert not lse[~live].any() and not logp[~live].any()
+    d = z.sub_(want[:, None]).exp_()
+    d[here, t.clamp(min=0)] -= 1
+    d *= torch.where(live, -g.double(), 0.0)[:, None]
+    full = torch.zeros_like(d)
+    full[here, t.clamp(min=0)] = torch.where(live, g.double().abs(), 0.0)
+    p_err = 2 * z_err + 12 * E * s + 300 * E + 8 * E * want.abs().amax()
+    d_err = U * d.abs() + (d.abs() + 2 * full) * p_err + 2.0 ** -126
+    for got, ref, size, n in ((dx, d @ W, lambda a: a @ W.abs(), vocab),
+                              (dw, d.t() @ X, lambda a: a.t() @ X.abs(), rows)):
+        tol = U * ref.abs() + size(d_err) + 2 * E * (n + 64) * size(d.abs()) + 2.0 ** -126
+        assert ((got.double() - ref).abs() <= tol * (1 + U)).all()
+
+
+@pytest.mark.parametrize("rows,vocab,hidden", [(700, 40003, 520), (700, 40003, 1001), (1100, 20000, 2056)])
+def test_long_sums_in_large_tiles(rows, vocab, hidden):
+    """Tiles of 256 x 256 whose sums have many stages, for the logits, both gradients and (over the
+    live rows) the head's: rings that wrap, and ends in the middle of a stage."""
+    rng = np.random.default_rng([rows, hidden, 47])
+    x, w, ids, _, grad = make(rng, rows, vocab, hidden, masked=0.2)
+    check_on_the_card(x, w, ids, grad)
+
+
+@pytest.mark.parametrize("rows,hidden", [(129, 136), (191, 192), (192, 193), (193, 200), (256, 256), (257, 264),
+                                         (319, 320), (320, 328), (321, 384), (384, 385), (385, 448)])
+def test_every_number_of_stages_in_large_tiles(rows, hidden):
+    """Sums of three to eight stages, whole and not: along hidden for the logits, over the rows for
+    the head's gradient."""
+    rng = np.random.default_rng([rows, hidden, 53])
+    x, w, ids, _, grad = make(rng, rows, 33000, hidden, masked=0.0)
+    check_on_the_card(x, w, ids, grad)
