@@ -759,3 +759,60 @@ def test_every_number_of_stages_in_large_tiles(rows, hidden):
     rng = np.random.default_rng([rows, hidden, 53])
     x, w, ids, _, grad = make(rng, rows, 33000, hidden, masked=0.0)
     check_on_the_card(x, w, ids, grad)
+
+
+@pytest.mark.parametrize("entries", [None, 5])
+def test_gradients_against_differences_along_themselves(entries):
+    """The outputs' difference over a step against the gradient, in directions where it is large:
+    a step in a quarter of the places, each to its gradient's side.  Inputs and steps are multiples of
+    2^-6, so the logits are exact; what is left is the gradients' rounding (U of a result, and U of
+    each d in it), the scores' binary32 errors, and the third difference: of a logarithm of a sum
+    of exponentials the third derivative is a third central moment, at most R^3 / (6 sqrt 3) of
+    logits whose changes span R.  Along such directions a gradient of another size or sign, or one
+    without its softmax, is told apart."""
+    rng = np.random.default_rng([59, entries or 0])
+    rows, vocab, hidden, step = 40, 300, 64, 2.0 ** -6
+    x, w = (torch.from_numpy(rng.integers(-64, 65, (n, hidden)).astype(np.float32) / 64).cuda().bfloat16()
+            for n in (rows, vocab))
+    _, _, ids, teacher, grad = make(rng, rows, vocab, hidden, entries, masked=0.1)
+    d_ids = dev(ids if entries else ids[:, 0], torch.int64)
+    t = dev(teacher, torch.float32) if entries else None
+    d_grad = dev(grad, torch.float32)
+
+    def out(y, v):
+        if entries:
+            return Head(v).distill(y, d_ids, t)
+        logp, lse = Head(v).score(y, d_ids)
+        return logp, logp, lse
+
+    first, logp, lse = out(x, w)
+    if entries:
+        grads = Head(w).distill_gradient(x, d_ids, t, logp, lse, d_grad)
+    else:
+        grads = Head(w).score_gradient(x, d_ids, logp, lse, d_grad)
+    X, W, T = f64(x), f64(w), None if teacher is None else teacher.astype(np.float64)
+    live, _ = oh.kinds(ids, vocab)
+    g = np.where(live, np.abs(grad), 0.0)
+    d = np.abs(oh.logit_gradients(X, W, ids, grad, 1.0, T))
+    # without the softmax: the wanted weights alone
+    bare = np.zeros_like(d)
+    q, _ = oh.weights(ids, T, 1.0)
+    for r in np.flatnonzero(live):
+        for e in np.flatnonzero(ids[r] >= 0):
+            bare[r, ids[r, e]] += q[r, e] * grad[r] * (-1 if entries else 1)
+    error = 2 * E * 64 + 100 * E + 16 * E * (np.abs(f64(lse)) + np.abs(f64(logp)).reshape(rows, -1).max(1))
+    for at, G in enumerate(map(f64, grads)):
+        v = np.sign(G) * (rng.random(G.shape) < 0.25) * step
+        up, down = (dev(a, torch.float32).bfloat16() for a in ((X, W)[at] + v, (X, W)[at] - v))
+        assert np.array_equal(f64(up) - f64(down), 2 * v)
+        hi, lo = (out(x, y)[0] if at else out(y, w)[0] for y in (up, down))
+        diff = ((f64(hi) - f64(lo)) * grad).sum()
+        got = (2 * v * G).sum()
+        change = X @ v.T if at else v @ W.T
+        span = change.max(1) - change.min(1)
+        size = d.T @ np.abs(X) if at else d @ np.abs(W)
+        tol = (2 * np.abs(v) * U * (np.abs(G) + size) * (1 + U)).sum() + (g * 2 * error).sum() + \
+            (g * span ** 3).sum() / (3 * 6 * 3 ** 0.5)
+        assert abs(diff - got) <= tol
+        without = (2 * v * (bare.T @ X if at else bare @ W)).sum()
+        assert tol <= 0.1 * abs(got) and abs(diff - without) > tol
