@@ -269,3 +269,38 @@ def test_every_number_of_stages_in_large_tiles(rows, inner, outer):
     rng = np.random.default_rng([rows, inner, outer])
     x, w, a, b, scales, index = make(rng, rows, inner, outer, 24, 7, "runs")
     check(x, w, a, b, scales, index, Adapters(a, b, scales).project(x, w, ints(index)))
+
+
+@pytest.mark.parametrize("rows,inner,outer,rank,members", [
+    (270_000, 64, 8200, 8, 3),                             # more than 2^31 results
+    (3, 2560, 900_001, 16, 3), (100, 2560, 900_001, 16, 3),           # elements of the weight
+    (40, 64, 17408, 64, 3000), (40, 64, 5120, 128, 6000), (150, 64, 17408, 64, 3000)])   # of all b
+def test_arrays_beyond_32_bits(rows, inner, outer, rank, members):
+    """Rows among all of them, against 64 bits."""
+    rng = np.random.default_rng([rows, outer])
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(rows)
+
+    def normal(n, width, std):
+        out = torch.empty(n, width, device="cuda", dtype=torch.bfloat16)
+        for part in out.split(max(1, (1 << 28) // width)):
+            part.copy_(torch.randn(*part.shape, device="cuda", generator=gen) * std)
+        return out
+
+    x, w = normal(rows, inner, 1.0), normal(outer, inner, inner ** -0.5)
+    a = normal(members, rank * inner, inner ** -0.5).view(members, rank, inner)
+    b = normal(members, outer * rank, rank ** -0.5).view(members, outer, rank)
+    index = rng.integers(-1, members, rows)
+    index[0], index[-1] = members - 1, members - 2
+    got = Adapters(a, b).project(x, w, ints(index))
+    assert max(got.numel(), w.numel(), b.numel()) > 1 << 31
+    for r in [0, rows - 1] + rng.integers(0, rows, 8).tolist():
+        X, W = x[r].double(), w.double()
+        want, i = W @ X, index[r]
+        tol = 2 * E * (inner + rank + 16) * (W.abs() @ X.abs())
+        if i >= 0:
+            A, B = a[i].double(), b[i].double()
+            want += B @ (A @ X)
+            u_err = U * (A @ X).abs() + 2 * E * (inner + 16) * (A.abs() @ X.abs()) * (1 + U)
+            tol += B.abs() @ u_err + 2 * E * (inner + rank + 16) * (B.abs() @ (A @ X).abs())
+        assert ((got[r].double() - want).abs() <= tol * (1 + U) + U * want.abs()).all()

@@ -816,3 +816,81 @@ def test_gradients_against_differences_along_themselves(entries):
         assert abs(diff - got) <= tol
         without = (2 * v * (bare.T @ X if at else bare @ W)).sum()
         assert tol <= 0.1 * abs(got) and abs(diff - without) > tol
+
+
+@pytest.mark.parametrize("rows,vocab,hidden", [(30, 300, 64), (90, 20001, 136), (200, 400, 72), (140, 33000, 200)])
+def test_rows_that_overlap(rows, vocab, hidden):
+    """Windows of a sequence, 8 elements apart, as rows and as a head."""
+    rng = np.random.default_rng([rows, 61])
+    x, w, ids, _, grad = make(rng, rows, vocab, hidden)
+    long, flat = (mat(rng, 1, 8 * n + hidden)[0] for n in (rows, vocab))
+    y, v = long.as_strided((rows, hidden), (8, 1)), (flat * hidden ** -0.5).as_strided((vocab, hidden), (8, 1))
+    for a, b in ((y, w), (x, v), (y, v)):
+        t, g = dev(ids[:, 0], torch.int64), dev(grad, torch.float32)
+        outs = []
+        for p, q in ((a, b), (a.contiguous(), b.contiguous())):
+            logp, lse = Head(q).score(p, t)
+            outs.append((logp, lse) + Head(q).score_gradient(p, t, logp, lse, g))
+        for got, want in zip(*outs):
+            assert torch.equal(got, want)
+
+
+def test_the_smallest_numbers():
+    """Products of bf16's denormal numbers are exact as well."""
+    for rows, vocab, hidden in ((3, 200, 64), (3, 200, 63), (40, 20001, 64), (200, 300, 64)):
+        x, w = (torch.zeros(n, hidden, device="cuda").bfloat16() for n in (rows, vocab))
+        x[:, 1], w[5, 1] = 2.0 ** -130, 2.0 ** 126
+        x[:, 2], w[6, 2] = 2.0 ** 125, 3 * 2.0 ** -132
+        t = torch.arange(rows, device="cuda") % 3 + 4
+        logp, lse = Head(w).score(x, t, scale=8.0)
+        z = x[:1].double() @ w.double().t() * 8
+        want = torch.logsumexp(z, -1)
+        assert z[0, 5] == 0.5 and z[0, 6] == 0.1875
+        assert ((lse - want).abs() <= 300 * E).all() and ((logp - z[0, t] + want).abs() <= 300 * E).all()
+
+
+@pytest.mark.parametrize("rows,hidden", [(2, 2560), (40, 2561), (100, 2560), (300, 2560)])
+def test_a_head_beyond_32_bits(rows, hidden):
+    """More than 2^32 bytes and 2^31 elements of the head, and of its gradient."""
+    rng = np.random.default_rng([rows, 67])
+    vocab = 900_001
+    w = torch.empty(vocab, hidden, device="cuda", dtype=torch.bfloat16)
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(rows)
+    for part in w.split(100_000):
+        part.copy_(torch.randn(*part.shape, device="cuda", generator=gen) * hidden ** -0.5)
+    x = mat(rng, rows, hidden)
+    t = torch.from_numpy(rng.integers(0, vocab, rows)).cuda()
+    t[0], t[1] = vocab - 1, vocab - 2
+    g = dev(rng.standard_normal(rows), torch.float32)
+    logp, lse = Head(w).score(x, t)
+    X = x.double()
+    tops = []
+    for part in w.split(100_000):
+        tops.append(torch.logsumexp(X @ part.double().t(), -1))
+    want = torch.logsumexp(torch.stack(tops), 0)
+    s = X.abs().amax() * max(part.double().abs().sum(1).amax() for part in w.split(100_000))
+    z_err = (2 * E * hidden + 4 * E) * s
+    assert ((lse - want).abs() <= z_err + 200 * E + 8 * E * s + 4 * E * want.abs()).all()
+    right = (X * w[t].double()).sum(1) - want
+    assert ((logp - right).abs() <= 2 * z_err + 200 * E + 8 * E * (s + want.abs() + right.abs())).all()
+    dx, dw = Head(w).score_gradient(x, t, logp, lse, g)
+    p_err = 2 * z_err + 12 * E * s + 300 * E + 8 * E * want.abs().amax()
+    ref, room, first = torch.zeros_like(X), torch.zeros_like(X), 0
+    for part, got in zip(w.split(100_000), dw.split(100_000)):
+        P = part.double()
+        d = (X @ P.t() - want[:, None]).exp_()
+        full = torch.zeros_like(d)
+        for r in range(rows):
+            if first <= t[r] < first + len(part):
+                d[r, t[r] - first] -= 1
+                full[r, t[r] - first] = g[r].double().abs()
+        d *= -g.double()[:, None]
+        d_err = U * d.abs() + (d.abs() + 2 * full) * p_err + 2.0 ** -126
+        ref += d @ P
+        room += (d_err + 2 * E * (vocab + 64) * d.abs()) @ P.abs()
+        to = d.t() @ X
+        tol = U * to.abs() + (d_err + 2 * E * (rows + 64) * d.abs()).t() @ X.abs() + 2.0 ** -126
+        assert ((got.double() - to).abs() <= tol * (1 + U)).all()
+        first += len(part)
+    assert ((dx.double() - ref).abs() <= (U * ref.abs() + room) * (1 + U)).all()
