@@ -100,7 +100,7 @@ struct Window {
 // of LDS wait for it.)  wait_staged() and a barrier before the data are read.
 __device__ __forceinline__ void load_lds(u32x4_t buffer, uint32_t offset, uint32_t dst) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-                 :: "s"(dst), "v"(offset), "s"(buffer) : "memory", "m0");
+                 :: "s"(dst), "v"(offset), "s"(buffer) : "memory");
 }
 __device__ __forceinline__ void wait_staged() {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
