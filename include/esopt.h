@@ -838,7 +838,7 @@ int es_head_gradient(const es_head_gradient_t* args, es_stream_t stream);
 typedef struct es_adapt {
     const void*    x;           /* bf16 [rows][inner], any alignment to 2 bytes */
     const void*    weight;      /* bf16 [outer][inner], 16-byte aligned */
-    void*          out;         /* bf16 [rows][outer], any alignment to 2 bytes; not x */
+    void*          out;         /* bf16 [rows][outer], any alignment to 2 bytes; shares no element with an input */
     uint64_t       x_stride, w_stride, out_stride;   /* elements, at most 2^22; w_stride a multiple of 8
                                                         (of a single row not looked at) */
     const void*    a;           /* bf16 [members][rank][inner], 16-byte aligned */

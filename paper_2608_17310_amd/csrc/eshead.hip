@@ -63,6 +63,17 @@ es_adapt_t settled(es_adapt_t x) {
     return x;
 }
 
+// Whether rows of two matrices share memory: rows side by side within a common stride need
+// not (with strides that differ, meeting ranges are taken to).
+bool meet(const void* a, uint64_t a_rows, uint64_t a_width, uint64_t a_stride, const void* b, uint64_t b_rows,
+          uint64_t b_width, uint64_t b_stride) {
+    const uint64_t at = reinterpret_cast<uint64_t>(a), bt = reinterpret_cast<uint64_t>(b);
+    if (at >= bt + extent(b_rows, b_width, b_stride) || bt >= at + extent(a_rows, a_width, a_stride)) return false;
+    if (a_rows < 2 || b_rows < 2 || a_stride != b_stride) return true;
+    const uint64_t step = 2 * a_stride, apart = bt >= at ? (bt - at) % step : (step - (at - bt) % step) % step;
+    return apart < 2 * a_width || apart + 2 * b_width > step;
+}
+
 int launch_error(const char* what) {
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? ES_OK : hip_fail(e, what);
@@ -716,6 +727,13 @@ int check_adapt(const char* name, const es_adapt_t& x) {
     if (x.out == x.x) return fail_in(ES_ERR_INVALID_ARG, name, "out is x");
     if (x.out_stride < x.outer)
         return fail_in(ES_ERR_INVALID_ARG, name, "the output's rows overlap");
+    const auto meets_out = [&](const void* p, uint64_t rows, uint64_t width, uint64_t stride) {
+        return meet(x.out, x.rows, x.outer, x.out_stride, p, rows, width, stride);
+    };
+    if (meets_out(x.x, x.rows, x.inner, x.x_stride) || meets_out(x.weight, x.outer, x.inner, x.w_stride) ||
+        meets_out(x.a, 1, uint64_t(x.members) * x.rank * x.inner, 0) ||
+        meets_out(x.b, 1, uint64_t(x.members) * x.rank * x.outer, 0))
+        return fail_in(ES_ERR_INVALID_ARG, name, "out shares memory with an input");
     if (odd(x.x, 2) || odd(x.out, 2) || odd(x.scales, 4) || odd(x.index, 4) || odd(x.status, 4))
         return fail_in(ES_ERR_ALIGN, name, "array not aligned to its elements");
     if (odd(x.weight, 16) || x.w_stride % 8 != 0 || odd(x.a, 16) || odd(x.b, 16))

@@ -304,3 +304,18 @@ def test_arrays_beyond_32_bits(rows, inner, outer, rank, members):
             u_err = U * (A @ X).abs() + 2 * E * (inner + 16) * (A.abs() @ X.abs()) * (1 + U)
             tol += B.abs() @ u_err + 2 * E * (inner + rank + 16) * (B.abs() @ (A @ X).abs())
         assert ((got[r].double() - want).abs() <= tol * (1 + U) + U * want.abs()).all()
+
+
+def test_rows_and_results_side_by_side():
+    """In the columns of one array; an output over its own input is refused."""
+    rng = np.random.default_rng(71)
+    for rows in (1, 30, 100, 700):
+        x, w, a, b, scales, index = make(rng, rows, 128, 96, 16, 3)
+        room = torch.zeros(rows, 224, device="cuda").bfloat16()
+        room[:, :128] = x
+        adapters = Adapters(a, b, scales)
+        adapters.project(room[:, :128], w, ints(index), out=room[:, 128:])
+        check(x, w, a, b, scales, index, room[:, 128:])
+        assert torch.equal(room[:, :128], x)
+        with pytest.raises(esopt.EsError):
+            adapters.project(room[:, :128], w, ints(index), out=room[:, 127:223])

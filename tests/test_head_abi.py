@@ -178,3 +178,28 @@ def test_the_stride_of_a_single_row_is_not_looked_at(lib):
                 assert fn(ctypes.byref(args), None) in (E, esopt.ES_ERR_HIP)
                 said = esopt.last_error()
                 assert "stride" not in said and "overlap" not in said and "aligned" not in said
+
+
+@pytest.mark.parametrize("change,refused", [
+    (dict(out=P + 16), True), (dict(out=P - 2 * 96 * 9), True),              # over x's rows
+    (dict(out=P + 2 * 64 * 10, out_stride=96), False), (dict(out=P - 2 * 96 * 10), False),   # beside them
+    # within common rows of 160: columns 64 .. 159 beside 0 .. 63, and one too early or too late
+    (dict(x_stride=160, out_stride=160, out=P + 2 * 64), False),
+    (dict(x_stride=160, out_stride=160, out=P + 2 * 63), True),
+    (dict(x_stride=160, out_stride=160, out=P + 2 * 65), True),
+    (dict(x_stride=160, out_stride=160, out=P - 2 * 96), False),
+    (dict(x_stride=160, out_stride=160, out=P - 2 * 95), True),
+    (dict(x_stride=160, out_stride=160, out=P + 2 * 160 * 9 + 2 * 64), False),
+    (dict(x_stride=160, out_stride=160, out=P + 2 * 160 * 4 + 2 * 60), True),
+    (dict(rows=1, out=P + 2 * 64), False), (dict(rows=1, out=P + 2 * 63), True),
+    (dict(rows=1, out=P - 2 * 96), False), (dict(rows=1, out=P - 2 * 95), True),
+    (dict(out=2 * P), True), (dict(out=2 * P + 2 * 95 * 64), True), (dict(out=2 * P + 2 * 96 * 64), False),
+    (dict(out=4 * P), True), (dict(out=4 * P + 2 * 3 * 16 * 64), False),
+    (dict(out=5 * P + 2 * 3 * 16 * 96 - 2), True), (dict(out=5 * P + 2 * 3 * 16 * 96), False)])
+def test_an_output_over_an_input_is_refused(lib, change, refused):
+    """Whose rows would be read after they are written."""
+    args = _adapt(**change)
+    assert (lib.es_adapt_bytes(ctypes.byref(args)) == 0) == refused
+    args.workspace_bytes = 1
+    rc = lib.es_adapt_project(ctypes.byref(args), None)
+    assert (rc == E and "shares memory" in esopt.last_error()) == refused
