@@ -97,7 +97,8 @@ struct Window {
 
 // 16 bytes a lane from `offset` of the lane into LDS, at byte `dst` (of the wave) + 16 lane.
 // (In asm, which has no register output: the compiler would make every later read
-// of LDS wait for it.)  wait_staged() and a barrier before the data are read.
+// of LDS wait for it; m0 is a reserved register, in which it keeps nothing over a statement.)
+// wait_staged() and a barrier before the data are read.
 __device__ __forceinline__ void load_lds(u32x4_t buffer, uint32_t offset, uint32_t dst) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                  :: "s"(dst), "v"(offset), "s"(buffer) : "memory");
