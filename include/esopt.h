@@ -829,9 +829,9 @@ int es_head_gradient(const es_head_gradient_t* args, es_stream_t stream);
  *   y = W x + s_i B_i (A_i x),  i = index[row].
  * A row with a negative index has no adapter; one of `members` or more is NaN.  The
  * adapters are tensors that plans can move like any other parameters.
- * A_i x is summed in binary32, multiplied by s_i and rounded to bf16 (RNE) for the
- * matrix unit; y is summed in binary32 and rounded once.  What a member's
- * adapter or a row holds reaches no other row.
+ * A_i x is summed and multiplied by s_i in binary32 (the matrix unit takes it as two bf16
+ * numbers, within 2^-15 of it); y is summed in binary32 and rounded once.  What a
+ * member's adapter or a row holds reaches no other row.
  * ------------------------------------------------------------------------- */
 #define ES_ADAPT_BAD_INDEX 1u  /* status: an index >= members */
 

@@ -21,16 +21,38 @@ struct SmallArgs {
     const uint16_t* a;                     // [members][rank][inner]
     const float* scales;                   // or null
     const int32_t* index;
-    uint16_t* u;                           // [rows][rank]
+    float* u;                              // [rows][rank]
     uint32_t* status;
     uint32_t rows, inner, members, rank;
+    bool split;                            // u as the matrix unit takes it, [rows][2][rank] bf16
 };
+
+// Element r of row n of u.  The matrix unit takes it as the sum of two bf16 numbers, cut and
+// rounded (RNE): within 2^-15 of it.  Both have its sign, and of a normal number neither is
+// 0: an infinity in B times the two is that infinity again, as it is times u.
+__device__ __forceinline__ void store_u(const SmallArgs& a, uint32_t n, uint32_t r, float v) {
+    if (!a.split) {
+        a.u[uint64_t(n) * a.rank + r] = v;
+        return;
+    }
+    const uint32_t word = __float_as_uint(v), sign = word >> 16 & 0x8000u;
+    uint32_t high = word >> 16, low = 0;
+    if (v != v) {
+        high = 0x7FC0u;
+    } else if (v != 0.0f) {
+        if (__builtin_fabsf(v) < eskv::inf())
+            low = pack_bf16(v - __uint_as_float(word & 0xFFFF0000u), 0.0f) & 0x7FFFu;
+        low = sign | (low == 0 ? 1u : low);
+    }
+    uint16_t* const to = reinterpret_cast<uint16_t*>(a.u) + uint64_t(n) * 2 * a.rank + r;
+    to[0] = static_cast<uint16_t>(high);
+    to[a.rank] = static_cast<uint16_t>(low);
+}
 
 constexpr uint32_t kSmallRows = 32;
 
 // A workgroup takes 32 rows, and their members one by one: a product of the member's A
-// with those rows, whose sum its waves share.  u is rounded to bf16 (RNE) for the matrix
-// unit: it is off by as much as y's own rounding, of a smaller term.
+// with those rows, whose sum its waves share.
 template <int kBlocks, int kParts>         // blocks of 16 of the rank, at a time
 __global__ __launch_bounds__(512, 2) void es_adapt_small_kernel(SmallArgs a) {
     using R = esring::Ring<kBlocks, 2, kParts>;
@@ -75,7 +97,7 @@ __global__ __launch_bounds__(512, 2) void es_adapt_small_kernel(SmallArgs a) {
                 float sum = 0.0f;
 #pragma unroll
                 for (uint32_t w = 0; w < kWaves; ++w) sum += sums[w * kEach + e];
-                a.u[uint64_t(n0 + i) * a.rank + r] = static_cast<uint16_t>(pack_bf16(s * sum, 0.0f));
+                store_u(a, n0 + i, r, s * sum);
             }
             __syncthreads();               // the rings are free again
         }
@@ -104,14 +126,12 @@ __global__ __launch_bounds__(256) void es_adapt_few_small_kernel(SmallArgs a) {
     float all = ((sum[0] + sum[1]) + (sum[2] + sum[3])) + ((sum[4] + sum[5]) + (sum[6] + sum[7]));
 #pragma unroll
     for (int d = 32; d >= 1; d /= 2) all += __shfl_xor(all, d);
-    if (lane == 0)
-        a.u[uint64_t(n) * a.rank + r] = static_cast<uint16_t>(
-            pack_bf16((a.scales != nullptr ? a.scales[member] : 1.0f) * all, 0.0f));
+    if (lane == 0) store_u(a, n, r, (a.scales != nullptr ? a.scales[member] : 1.0f) * all);
 }
 
 struct AddArgs {
     const int32_t* index;
-    const uint16_t* u;
+    const float* u;                        // of a tile split
     const uint16_t* b;                     // [members][outer][rank]
     uint32_t rows, outer, members, rank;
 };
@@ -119,8 +139,10 @@ struct AddArgs {
 // B u added to a tile, for the members of a wave's 64 rows one by one.  Where a
 // member has all of 16 rows its products go straight into the tile; otherwise into
 // results of their own, of which its rows take theirs: a member that holds
-// infinities or NaN reaches no other's rows.
-template <int kSize>
+// infinities or NaN reaches no other's rows.  u's two numbers make twice the products (8403
+// rows, 2560 to 9728, rank 32: 374 us, with u rounded to one number 369; 16384 rows of 5120, rank
+// 64: 728 and 717), but ranks up to 16 (kHalves 1) have both in the length of one instruction.
+template <int kHalves, int kSize>
 __device__ __forceinline__ void add_adapters(const AddArgs& a, uint32_t m0, uint32_t n0, Tile<kSize>& c) {
     constexpr int kBlocks = Tile<kSize>::kBlocks;
     const uint32_t lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
@@ -131,6 +153,7 @@ __device__ __forceinline__ void add_adapters(const AddArgs& a, uint32_t m0, uint
         const uint32_t n = n1 + 16 * j + (lane & 15);
         mine[j] = n < a.rows ? a.index[n] : -1;
     }
+    const uint16_t* const u = reinterpret_cast<const uint16_t*>(a.u);
     const int32_t every = n1 + lane < a.rows ? a.index[n1 + lane] : -1;
     uint64_t left = __ballot(every >= 0 && every < int32_t(a.members));
     while (left != 0) {
@@ -138,35 +161,39 @@ __device__ __forceinline__ void add_adapters(const AddArgs& a, uint32_t m0, uint
         const uint64_t rows = __ballot(every == member);
         left &= ~rows;
         for (uint32_t r0 = 0; r0 < a.rank; r0 += 32) {
-            const uint32_t r = r0 + 8 * (lane >> 4);
-            u32x4_t bv[kBlocks], uv[4];
+            const uint32_t r = r0 + 8 * (lane >> 4), of_b = r < a.rank ? r : r - a.rank;
+            const bool here = r < (kHalves == 1 ? 2 * a.rank : a.rank);
+            u32x4_t bv[kBlocks];
 #pragma unroll
             for (int i = 0; i < kBlocks; ++i) {
                 const uint32_t m = min(m0 + kSize / 2 * (wave & 1) + 16 * i + (lane & 15), a.outer - 1);
-                bv[i] = r < a.rank ? load<u32x4_t>(a.b + (uint64_t(member) * a.outer + m) * a.rank + r)
-                                   : u32x4_t{0, 0, 0, 0};
+                bv[i] = here ? load<u32x4_t>(a.b + (uint64_t(member) * a.outer + m) * a.rank + of_b)
+                             : u32x4_t{0, 0, 0, 0};
             }
+#pragma unroll 1
+            for (uint32_t h = 0; h < kHalves; ++h) {     // (unrolled it would spill)
+                u32x4_t uv[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                uv[j] = mine[j] == member && r < a.rank
-                            ? load<u32x4_t>(a.u + uint64_t(n1 + 16 * j + (lane & 15)) * a.rank + r)
-                            : u32x4_t{0, 0, 0, 0};
+                for (int j = 0; j < 4; ++j)
+                    uv[j] = mine[j] == member && here
+                                ? load<u32x4_t>(u + (uint64_t(n1 + 16 * j + (lane & 15)) * 2 + h) * a.rank + r)
+                                : u32x4_t{0, 0, 0, 0};
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const uint32_t some = uint32_t(rows >> (16 * j)) & 0xFFFFu;
-                if (some == 0) continue;
-                const bool whole = some == 0xFFFFu;
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t some = uint32_t(rows >> (16 * j)) & 0xFFFFu;
+                    if (some == 0) continue;
+                    const bool whole = some == 0xFFFFu;
 #pragma unroll
-                for (int i = 0; i < kBlocks; ++i) {
-                    const f32x4_t from = whole ? c.x[i][j] : f32x4_t{0, 0, 0, 0};
-                    const f32x4_t t = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                        __builtin_bit_cast(bf16x8_t, bv[i]), __builtin_bit_cast(bf16x8_t, uv[j]), from, 0, 0,
-                        0);
+                    for (int i = 0; i < kBlocks; ++i) {
+                        const f32x4_t from = whole ? c.x[i][j] : f32x4_t{0, 0, 0, 0};
+                        const f32x4_t t = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                            __builtin_bit_cast(bf16x8_t, bv[i]), __builtin_bit_cast(bf16x8_t, uv[j]), from, 0, 0, 0);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        c.x[i][j][e] = whole                ? t[e]
-                                       : mine[j] == member ? c.x[i][j][e] + t[e]
-                                                           : c.x[i][j][e];
+                        for (int e = 0; e < 4; ++e)
+                            c.x[i][j][e] = whole                ? t[e]
+                                           : mine[j] == member ? c.x[i][j][e] + t[e]
+                                                               : c.x[i][j][e];
+                    }
                 }
             }
         }
@@ -188,15 +215,17 @@ __device__ __forceinline__ f32x4_t with_adapter(const AddArgs& a, f32x4_t v, uin
     if (member >= int32_t(a.members)) return f32x4_t{eskv::nan(), eskv::nan(), eskv::nan(), eskv::nan()};
     if (member < 0) return v;
     const uint16_t* const b = a.b + uint64_t(member) * a.outer * a.rank;
-    const uint16_t* const u = a.u + uint64_t(n) * a.rank;
+    const float* const u = a.u + uint64_t(n) * a.rank;
     float low[4] = {};
     // (the words of 16 of the rank on their way at a time)
     for (uint32_t r0 = 0; r0 < a.rank; r0 += 16) {
-        u32x4_t q[2], p[2][4];
+        f32x4_t q[2][2];
+        u32x4_t p[2][4];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const uint32_t r = min(r0 + 8 * h, a.rank - 8);
-            q[h] = load<u32x4_t>(u + r);
+            q[h][0] = load<f32x4_t>(u + r);
+            q[h][1] = load<f32x4_t>(u + r + 4);
 #pragma unroll
             for (int e = 0; e < 4; ++e)
                 p[h][e] = load<u32x4_t>(b + uint64_t(min(m + e, end - 1)) * a.rank + r);
@@ -204,14 +233,12 @@ __device__ __forceinline__ f32x4_t with_adapter(const AddArgs& a, f32x4_t v, uin
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             if (r0 + 8 * h >= a.rank) break;
-            float x[8];
-            eskv::unpack8(q[h], x);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 float y[8];
                 eskv::unpack8(p[h][e], y);
 #pragma unroll
-                for (int z = 0; z < 8; ++z) low[e] = __builtin_fmaf(x[z], y[z], low[e]);
+                for (int z = 0; z < 8; ++z) low[e] = __builtin_fmaf(q[h][z / 4][z % 4], y[z], low[e]);
             }
         }
     }
@@ -238,14 +265,14 @@ struct TileArgs {
     uint64_t out_stride;
 };
 
-template <int kSize>
+template <int kSize, int kHalves>
 __global__ __launch_bounds__(2 * kSize, 2) void es_adapt_tile_kernel(TileArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     const Place at = place_of(blockIdx.x, a.p);
     const uint32_t m0 = at.m * kSize, n0 = at.n * kSize;
     Tile<kSize> c;
     product_tile<false, false, kSize>(a.p, m0, n0, a.add.rows - n0, 0, a.p.depth, lds, c);
-    add_adapters(a.add, m0, n0, c);
+    add_adapters<kHalves>(a.add, m0, n0, c);
     __syncthreads();
     tile_to_lds(c, lds);
     __syncthreads();
@@ -339,14 +366,14 @@ __global__ __launch_bounds__(512, 2) void es_adapt_few_kernel(FewArgs a) {
         if (member >= int32_t(a.add.members)) sum = eskv::nan();
         if (member >= 0 && member < int32_t(a.add.members)) {
             const uint16_t* const b = a.add.b + (uint64_t(member) * a.add.outer + m) * a.add.rank;
-            const uint16_t* const u = a.add.u + uint64_t(n) * a.add.rank;
+            const float* const u = a.add.u + uint64_t(n) * a.add.rank;
             float low = 0.0f;
             for (uint32_t r = 0; r < a.add.rank; r += 8) {
-                float p[8], q[8];
+                float p[8];
                 eskv::unpack8(load<u32x4_t>(b + r), p);
-                eskv::unpack8(load<u32x4_t>(u + r), q);
+                const f32x4_t q[2] = {load<f32x4_t>(u + r), load<f32x4_t>(u + r + 4)};
 #pragma unroll
-                for (int z = 0; z < 8; ++z) low = __builtin_fmaf(p[z], q[z], low);
+                for (int z = 0; z < 8; ++z) low = __builtin_fmaf(p[z], q[z / 4][z % 4], low);
             }
             sum += low;
         }

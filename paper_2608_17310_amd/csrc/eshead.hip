@@ -742,10 +742,11 @@ int check_adapt(const char* name, const es_adapt_t& x) {
 }
 
 struct AdaptPlan {
-    uint16_t *u, *x;
+    float* u;
+    uint16_t* x;
     uint32_t padded, packed_rows;
     AdaptPlan(Room& room, const es_adapt_t& a) {
-        u = room.take<uint16_t>(uint64_t(a.rows) * a.rank);
+        u = room.take<float>(uint64_t(a.rows) * a.rank);
         padded = static_cast<uint32_t>(up(a.inner, kDepth));
         packed_rows = static_cast<uint32_t>(up(a.rows, kTile));
         // the products take rows that start at a word of 16 bytes and end in whole stages
@@ -862,6 +863,7 @@ int es_adapt_project(const es_adapt_t* args, es_stream_t stream) try {
     small.inner = x.inner;
     small.members = x.members;
     small.rank = x.rank;
+    small.split = !plan.few && plan.splits == 1;
     const esadapt::AddArgs add{x.index, plan.u, static_cast<const uint16_t*>(x.b), x.rows, x.outer,
                                x.members, x.rank};
     // u: a wave for each of its elements reads two rows of `inner`, which the second cache
@@ -950,10 +952,14 @@ int es_adapt_project(const es_adapt_t* args, es_stream_t stream) try {
     a.add = add;
     a.out = static_cast<uint16_t*>(x.out);
     a.out_stride = x.out_stride;
-    if (plan.low)
-        launch_tiles<kSmallTile>(esadapt::es_adapt_tile_kernel<kSmallTile>, a, s);
+    if (plan.low && x.rank <= 16)
+        launch_tiles<kSmallTile>(esadapt::es_adapt_tile_kernel<kSmallTile, 1>, a, s);
+    else if (plan.low)
+        launch_tiles<kSmallTile>(esadapt::es_adapt_tile_kernel<kSmallTile, 2>, a, s);
+    else if (x.rank <= 16)
+        launch_tiles<kTile>(esadapt::es_adapt_tile_kernel<kTile, 1>, a, s);
     else
-        launch_tiles<kTile>(esadapt::es_adapt_tile_kernel<kTile>, a, s);
+        launch_tiles<kTile>(esadapt::es_adapt_tile_kernel<kTile, 2>, a, s);
     return launch_error("es_adapt_project kernel launch");
 } catch (const std::bad_alloc&) {
     return fail(ES_ERR_NOMEM, "es_adapt_project: host allocation failed");

@@ -319,3 +319,52 @@ def test_rows_and_results_side_by_side():
         assert torch.equal(room[:, :128], x)
         with pytest.raises(esopt.EsError):
             adapters.project(room[:, :128], w, ints(index), out=room[:, 127:223])
+
+
+PATHS = [(1, 200, 300), (20, 72, 100), (50, 136, 9000), (64, 72, 9000), (70, 2104, 130), (100, 200, 300),
+         (300, 136, 520), (1300, 200, 6000)]
+
+
+@pytest.mark.parametrize("rows,inner,outer", PATHS)
+@pytest.mark.parametrize("rank", [8, 16, 24, 128])
+def test_the_small_product_is_not_rounded_to_bf16(rows, inner, outer, rank):
+    """Without the shared part, of sums that nearly cancel: a result is off by its own rounding, and
+    by 2^-15 of each term's u, and the sums' binary32 errors."""
+    rng = np.random.default_rng([rows, inner, rank])
+    x, w, a, b, scales, index = make(rng, rows, inner, outer, rank, 5)
+    w.zero_()
+    got = f64(Adapters(a, b, scales).project(x, w, ints(index)))
+    X, A, B, S = map(f64, (x, a, b, scales))
+    for r, i in enumerate(index):
+        if i < 0:
+            assert not got[r].any()
+            continue
+        u = S[i] * (A[i] @ X[r])
+        want = B[i] @ u
+        u_err = 2.0 ** -15 * np.abs(u) + S[i] * 2 * E * (inner + 16) * (np.abs(A[i]) @ np.abs(X[r]))
+        tol = np.abs(B[i]) @ u_err + 2 * E * (rank + 16) * (np.abs(B[i]) @ np.abs(u))
+        assert np.all(np.abs(got[r] - want) <= tol * (1 + U) + U * np.abs(want) + 2.0 ** -126)
+
+
+@pytest.mark.parametrize("rows,inner,outer", PATHS)
+@pytest.mark.parametrize("rank", [8, 24, 64])
+def test_an_infinity_in_an_adapter(rows, inner, outer, rank):
+    """It reaches its own output of its member's rows, with the sign of what it is multiplied by:
+    a number that bf16 holds (integers here) or not."""
+    rng = np.random.default_rng([rows, inner, rank, 73])
+    x, w, a, b, scales, index = make(rng, rows, inner, outer, rank, 3)
+    x, a = (torch.from_numpy(rng.integers(-3, 4, tuple(t.shape)).astype(np.float32)).cuda().bfloat16() for t in (x, a))
+    scales[0], scales[1], scales[2] = 1.0, 0.3, -2.0
+    index[0] = 1
+    adapters = Adapters(a, b, scales)
+    want = adapters.project(x, w, ints(index))
+    b[1, outer // 2, rank - 3] = float("inf")
+    got = adapters.project(x, w, ints(index))
+    mine = torch.from_numpy(index == 1).cuda()
+    u = x.double() @ a[1, rank - 3].double() * 0.3
+    hit = got[mine, outer // 2].double()
+    assert torch.equal(hit[u[mine] != 0], u[mine][u[mine] != 0].sign() * float("inf"))
+    assert torch.isnan(hit[u[mine] == 0]).all()            # (0 times infinity)
+    keep = torch.ones_like(got, dtype=torch.bool)
+    keep[mine, outer // 2] = False
+    assert torch.equal(got[keep], want[keep])
