@@ -207,7 +207,7 @@ esstream::StreamArgs stream_args(const void* w, uint64_t w_stride, uint32_t w_ro
 }
 
 // Rows of words, few enough that the matrix's bytes are what they cost.  (128 rows of 2560
-// against 151936 171 us, 129 in tiles 211.)
+// against 151936 175 us, 129 in tiles 213.)
 bool streams(const es_head_score_t& x) {
     return x.rows <= esstream::kRows && word_rows(x.weight, x.w_stride, x.hidden) &&
            word_rows(x.x, x.x_stride, x.hidden);

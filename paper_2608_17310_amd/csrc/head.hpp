@@ -420,7 +420,7 @@ struct StreamStatsArgs {
 
 // The same of up to 128 rows of words: a workgroup's share of the vocabulary is a part,
 // whose maxima and sums run along in registers.  Bound by the head's bytes: 32 rows of
-// 5120 against 151936 266 us, 5.9 TB/s, with the scores' kernel; 128 of 2560 171 us, 4.6 TB/s
+// 5120 against 151936 266 us, 5.9 TB/s, with the scores' kernel; 128 of 2560 175 us, 4.5 TB/s
 // and, with the operands' reads from LDS, not far from the matrix unit's bound.
 template <int kWaves, int kTokens>
 using HeadStream = esstream::Stream<
