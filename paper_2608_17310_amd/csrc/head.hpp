@@ -533,9 +533,10 @@ __device__ __forceinline__ float block_max(float x, float* room) {
     return fmaxf(fmaxf(room[0], room[1]), fmaxf(room[2], room[3]));
 }
 
-// The teacher's weight of thread e's entry (0: absent), and its logarithm.  The likeliest entry's logit is taken off before the scale
-// (halves: the difference of two finite logits is finite), so that its own exponential is 1
-// whatever they are, masks of the type's lowest value throughout among them.
+// The teacher's weight of thread e's entry (0: absent), and its logarithm.  The likeliest
+// entry's logit is taken off before the scale (halves: the difference of two finite logits is
+// finite), so that its own exponential is 1 whatever they are, masks of the type's lowest
+// value throughout among them.
 __device__ __forceinline__ float teacher_weight(bool here, float t, float scale, float* room,
                                                 float& log_q) {
     here = here && has_weight(t, scale);

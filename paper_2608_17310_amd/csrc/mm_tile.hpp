@@ -133,39 +133,49 @@ struct Stage {
     uint32_t off[4];
     uint32_t dst;
 
-    // (wide) the k of a stage that load x brings for a lane
-    static __device__ __forceinline__ uint32_t k_of(uint32_t wave, uint32_t x, uint32_t lane) {
-        return (wave * 4 + x) * (64 / kWords) + lane / kWords;
+    // Load x of a wave: the row (wide: k of a stage) and the word of it that it brings for a lane.
+    static __host__ __device__ uint32_t row_of(uint32_t wave, uint32_t x, uint32_t lane) {
+        return kWide ? (wave * 4 + x) * (64 / kWords) + lane / kWords : (wave * 4 + x) * 8 + (lane >> 3);
+    }
+    static __host__ __device__ uint32_t word_of(uint32_t wave, uint32_t x, uint32_t lane) {
+        const uint32_t r = row_of(wave, x, lane);
+        return kWide ? (lane % kWords) ^ ((r & 3) << 2) ^ ((r >> 3 & 1) << 1) : (lane & 7) ^ ((r >> 1) & 7);
+    }
+
+    // The side from rows i0 (< extent) and elements k0 of the sum on, up to k_end.
+    static __host__ __device__ Window window(const Side& s, uint32_t i0, uint32_t k0, uint32_t k_end) {
+        const uint64_t last = s.extent - 1 - i0, at = reinterpret_cast<uint64_t>(s.at);
+        if constexpr (kWide)
+            return Window{at + 2 * (k0 * s.stride + i0), 2 * ((k_end - 1 - k0) * s.stride + last + 1)};
+        else                               // (rows end with a word)
+            return Window{at + 2 * (i0 * s.stride + k0), 2 * (last * s.stride + (k_end + 7) / 8 * 8 - k0)};
+    }
+    // The lane's bytes from there: of rows behind the last the last one's.
+    static __host__ __device__ uint32_t offset(const Side& s, uint32_t i0, uint32_t wave, uint32_t x, uint32_t lane) {
+        const uint32_t last = s.extent - 1 - i0, r = row_of(wave, x, lane), w = word_of(wave, x, lane);
+        if constexpr (kWide)
+            return r * uint32_t(2 * s.stride) + 16 * (w < last / 8 ? w : last / 8);
+        else
+            return (r < last ? r : last) * uint32_t(2 * s.stride) + 16 * w;
+    }
+    // Of a last stage of `have` elements of the sum: of those behind them others'.
+    static __host__ __device__ uint32_t last_offset(uint32_t o, uint32_t have, const Side& s, uint32_t wave,
+                                                    uint32_t x, uint32_t lane) {
+        const uint32_t r = row_of(wave, x, lane), w = word_of(wave, x, lane);
+        if constexpr (kWide)
+            return r >= have ? o - (r - (have - 1)) * uint32_t(2 * s.stride) : o;
+        else
+            return 8 * w >= have ? o - 16 * w : o;
     }
 
     __device__ __forceinline__ void init(const Side& s, uint32_t i0, uint32_t k0, uint32_t k_end,
                                          uint32_t wave, uint32_t lane) {
-        const uint32_t last = s.extent - 1 - i0;         // i0 < extent
         dst = wave * 4096;
-        if constexpr (kWide) {
-            next.at = reinterpret_cast<uint64_t>(s.at) + 2 * (k0 * s.stride + i0);
-            next.bytes = 2 * ((k_end - 1 - k0) * s.stride + last + 1);
-            step = 2 * kDepth * s.stride;
+        const Window first = window(s, i0, k0, k_end);
+        next = Window{uniform(first.at), uniform(first.bytes)};
+        step = uniform(kWide ? 2 * kDepth * s.stride : 2 * kDepth);
 #pragma unroll
-            for (uint32_t x = 0; x < 4; ++x) {
-                const uint32_t k = k_of(wave, x, lane);
-                const uint32_t w = (lane % kWords) ^ ((k & 3) << 2) ^ ((k >> 3 & 1) << 1);
-                off[x] = k * uint32_t(2 * s.stride) + 16 * min(w, last / 8);
-            }
-        } else {
-            next.at = reinterpret_cast<uint64_t>(s.at) + 2 * (i0 * s.stride + k0);
-            next.bytes = 2 * (last * s.stride + (k_end + 7) / 8 * 8 - k0);   // rows end with a word
-            step = 2 * kDepth;
-#pragma unroll
-            for (uint32_t x = 0; x < 4; ++x) {
-                const uint32_t i = (wave * 4 + x) * 8 + (lane >> 3);
-                const uint32_t w = (lane & 7) ^ ((i >> 1) & 7);
-                off[x] = min(i, last) * uint32_t(2 * s.stride) + 16 * w;
-            }
-        }
-        next.at = uniform(next.at);
-        next.bytes = uniform(next.bytes);
-        step = uniform(step);
+        for (uint32_t x = 0; x < 4; ++x) off[x] = offset(s, i0, wave, x, lane);
     }
 
     // The next stage's bytes; load x of it, where it exists in full.
@@ -180,15 +190,7 @@ struct Stage {
     // Where only `have` of it exist: others are read again, and cleared in registers.
     __device__ __forceinline__ void load_last(u32x4_t buffer, uint32_t lds, uint32_t x, uint32_t have,
                                               const Side& s, uint32_t wave, uint32_t lane) const {
-        uint32_t o = off[x];
-        if constexpr (kWide) {
-            const uint32_t k = k_of(wave, x, lane);
-            if (k >= have) o -= (k - (have - 1)) * uint32_t(2 * s.stride);
-        } else {
-            const uint32_t i = (wave * 4 + x) * 8 + (lane >> 3);
-            const uint32_t w = (lane & 7) ^ ((i >> 1) & 7);
-            if (8 * w >= have) o -= 16 * w;
-        }
+        const uint32_t o = last_offset(off[x], have, s, wave, x, lane);
         load_lds(buffer, o, lds + dst + 1024 * x);
     }
 };
@@ -274,7 +276,8 @@ __device__ __forceinline__ void product_tile(const Product& p, uint32_t m0, uint
     Stage<kWideA, kSize> sa;
     Stage<kWideB, kSize> sb;
     sa.init(p.a, m0, k0, k_end, wave, lane);
-    sb.init(p.b, n0, k0, k_end, wave, lane);
+    // (b's rows are stored, as zeros, to the end of its last stage: all of that is brought)
+    sb.init(p.b, n0, k0, (k_end + kDepth - 1) / kDepth * kDepth, wave, lane);
     Reader<kWideA, kSize, kBlocks> ra;
     Reader<kWideB, kSize, 4> rb;
     ra.init(kSize / 2 * (wave & 1), lane);

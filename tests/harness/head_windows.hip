@@ -1,4 +1,4 @@
-// Replays on the host which bytes the loads into LDS of ring.hpp and stream.hpp
+// Replays on the host which bytes the loads into LDS of ring.hpp, stream.hpp and mm_tile.hpp
 // address, lane by lane, and what the buffers' bounds check lets through: all of it
 // lies in the array, and all of the array's words are there.  The check is taken as the
 // compiler's documentation of raw buffer loads has it: a lane's offset against
@@ -78,6 +78,45 @@ void stream(const Side& s, uint32_t share) {
     }
 }
 
+// A tile's side, stage by stage.  Of a matrix (`whole` false) a last stage brings what there is;
+// packed rows (`whole`) are stored to the end of their last stage, and all of it is brought.
+template <bool kWide, int kSize>
+void tile(uint32_t rows, uint32_t depth, uint64_t stride, uint32_t splits, bool whole) {
+    using S = esmm::Stage<kWide, kSize>;
+    const uint64_t start = uint64_t(1) << 40;
+    const uint32_t stored = whole ? (depth + 63) / 64 * 64 : depth;
+    const uint64_t end = start + 2 * (kWide ? (stored - 1) * stride + rows : (rows - 1) * stride + stored);
+    const esmm::Side s{reinterpret_cast<const uint16_t*>(start), stride, rows};
+    const uint32_t part = ((depth + splits - 1) / splits + 63) / 64 * 64;
+    auto bad = [&](const char* what, uint32_t i0, uint32_t k) {
+        if (g_failures++ < 20)
+            std::printf("FAIL: tile %s: wide %d, %d, %u rows, sum of %u, stride %llu, from %u, %u\n", what, int(kWide),
+                        kSize, rows, depth, static_cast<unsigned long long>(stride), i0, k);
+    };
+    for (uint32_t i0 = 0; i0 < rows; i0 += kSize)
+        for (uint32_t k0 = 0; k0 < depth; k0 += part) {
+            const uint32_t k_end = std::min(depth, k0 + part), to = whole ? (k_end + 63) / 64 * 64 : k_end;
+            esmm::Window w = S::window(s, i0, k0, to);
+            for (uint32_t k = k0; k < k_end; k += 64) {
+                const uint32_t have = std::min(64u, to - k);
+                for (uint32_t wave = 0; wave < kSize / 32; ++wave)
+                    for (uint32_t x = 0; x < 4; ++x)
+                        for (uint32_t lane = 0; lane < 64; ++lane) {
+                            uint32_t off = S::offset(s, i0, wave, x, lane);
+                            if (have < 64) off = S::last_offset(off, have, s, wave, x, lane);
+                            const bool fetched = off < w.limit();
+                            if (!fetched) bad("missing", i0, k);          // (every load is within the array)
+                            if (w.at + off < start || w.at + off + 16 > end) bad("outside", i0, k);
+                            const uint32_t r = S::row_of(wave, x, lane), e = 8 * S::word_of(wave, x, lane);
+                            if (kWide ? i0 + e >= rows || r >= have : i0 + r >= rows || e >= have) continue;
+                            const uint64_t want = kWide ? (k + r) * stride + i0 + e : (i0 + r) * stride + k + e;
+                            if (w.at + off != start + 2 * want) bad("another word", i0, k);
+                        }
+                w.move(kWide ? 128 * stride : 128);
+            }
+        }
+}
+
 }  // namespace
 
 int main() {
@@ -93,6 +132,19 @@ int main() {
         ring<2, 4, 1>(s, 8);
         stream<3, 2, 32, 1, 4>(s, 16 * (1 + uint32_t(rng() % 9)));
         stream<5, 1, 64, 2, 3>(s, 16 * (1 + uint32_t(rng() % 9)));
+    }
+    for (int trial = 0; trial < 60; ++trial) {
+        const uint32_t rows = 1 + uint32_t(rng() % 600), depth = 8 * uint32_t(1 + rng() % 70);
+        const uint32_t wide = (rows + 7) / 8 * 8, splits = 1 + uint32_t(rng() % 3), any = 1 + uint32_t(rng() % 500);
+        tile<false, 256>(rows, depth, depth + 8 * (rng() % 3), splits, false);
+        tile<false, 128>(rows, depth, depth, splits, false);
+        tile<true, 256>(wide, any, wide + 8 * (rng() % 3), splits, false);
+        tile<true, 128>(wide, any, wide, splits, false);
+        // packed rows, rows of gradients of logits, and both across the sum
+        tile<false, 256>(rows, any, (any + 63) / 64 * 64, splits, true);
+        tile<false, 128>(rows, any, (any + 255) / 256 * 256, splits, true);
+        tile<true, 256>(wide, any, wide, splits, true);
+        tile<true, 128>(wide, any, (wide + 255) / 256 * 256, splits, true);
     }
     // a matrix beyond 2^32 bytes
     Side s{uint64_t(1) << 22, 700, 65536};

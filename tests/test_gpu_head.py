@@ -894,3 +894,10 @@ def test_a_head_beyond_32_bits(rows, hidden):
         assert ((got.double() - to).abs() <= tol * (1 + U)).all()
         first += len(part)
     assert ((dx.double() - ref).abs() <= (U * ref.abs() + room) * (1 + U)).all()
+
+
+@pytest.mark.parametrize("rows,vocab,hidden", [(256, 333, 72), (256, 33000, 136), (512, 301, 200), (512, 20003, 65)])
+def test_live_rows_that_fill_their_tiles(rows, vocab, hidden):
+    """The last packed row is a live one, and the sums end within a stage."""
+    rng = np.random.default_rng([rows, vocab, 79])
+    check(*make(rng, rows, vocab, hidden, masked=0.0), 1.0)

@@ -1,4 +1,4 @@
-"""What the streamed products' loads into LDS address, replayed on the CPU
+"""What the products' loads into LDS address, replayed on the CPU
 (tests/harness/head_windows.hip, host code alone): no lane reads past an array's end,
 whatever the last part of a sum leaves of it."""
 import os
